@@ -459,6 +459,42 @@ gs_status gs_debug_set_grid_cap(int32_t max_blocks);
  * Uses CUDA events (host objects) and a 4-byte device variable of the library; allocates nothing. */
 gs_status gs_alu_ceiling(int32_t what, int32_t milliseconds, void* stream, double* h_units_per_second);
 
+/* ---- Training on sampled blocks: embedding rows, attention over a block, softmax over a table's rows.
+ * What a training step does with a batch: the rows of the input nodes (gs_gather_features for fixed features,
+ * gs_embedding_lookup for learned ones), attention of every hop's destinations over their sampled neighbours, a
+ * softmax over classes or over all nodes; and the gradients of each.  The calls are independent of the caches and
+ * can be used with any arrays.  Types are GS_F32 and GS_BF16; sums, softmax statistics and gradients are kept in
+ * 32 bits and rounded once, to the output's type.  No floating-point atomics: a call's result does not depend on
+ * scheduling.  Workspaces are 256-byte aligned, owned by the caller, and hold nothing between calls. */
+
+/* out[p, :] = scale * table[ids[p], :] for p < count; an id outside [0, table_rows) gives a row of zeros.
+ *   d_table  [table_rows][table_ld] of table_dtype, table_ld >= dim (elements); table_rows < 2^31
+ *   d_out    [count_bound][out_ld] of out_dtype
+ * d_count_or_null, count_bound: as for gs_gather_features.  Accesses are as wide as bases, pitches and dim allow. */
+gs_status gs_embedding_lookup(const void* d_table, gs_dtype table_dtype, int64_t table_rows, int32_t dim, int64_t table_ld,
+                              const int32_t* d_ids, const int32_t* d_count_or_null, int32_t count_bound, float scale,
+                              void* d_out, gs_dtype out_dtype, int64_t out_ld, void* stream);
+
+/* Gradient of gs_embedding_lookup with respect to the table: row r is scale * the sum of the rows dout[p] with
+ * ids[p] == r, added in ascending p (the positions are sorted by id).  Ids outside [0, table_rows) have no part.
+ *   gs_embedding_backward         writes the whole table, rows without an id as zeros
+ *   gs_embedding_backward_sparse  writes only the rows that occur: d_rows[i] their ids, ascending, *d_num_rows
+ *                                 their number, d_grad[i] the sums; behind them, up to count_bound, d_rows is
+ *                                 -1 and d_grad zero, so the arrays can be used at their bound without a host read
+ * Workspace: gs_embedding_workspace_bytes(count_bound, table_rows, dim), enough for either call. */
+gs_status gs_embedding_workspace_bytes(int32_t count_bound, int64_t table_rows, int32_t dim, size_t* bytes);
+gs_status gs_embedding_backward(const void* d_dout, gs_dtype dout_dtype, int64_t dout_ld, const int32_t* d_ids,
+                                const int32_t* d_count_or_null, int32_t count_bound, int64_t table_rows, int32_t dim,
+                                float scale, void* d_dtable, gs_dtype dtable_dtype, int64_t dtable_ld, void* d_workspace,
+                                size_t workspace_bytes, void* stream);
+gs_status gs_embedding_backward_sparse(const void* d_dout, gs_dtype dout_dtype, int64_t dout_ld, const int32_t* d_ids,
+                                       const int32_t* d_count_or_null, int32_t count_bound, int64_t table_rows, int32_t dim,
+                                       float scale, int32_t* d_rows, int32_t* d_num_rows, void* d_grad, gs_dtype grad_dtype,
+                                       int64_t grad_ld, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Synchronises `stream`; GS_ERR_CUDA if a kernel of the training operators ever gave up one of its (bounded) waits. */
+gs_status gs_train_status(void* stream);
+
 /* Number of kernels this library has launched in the calling process (monotonic). */
 int64_t gs_kernel_launches(void);
 

@@ -108,6 +108,12 @@ def _load():
         "gs_alu_ceiling": [i32, i32, vp, ctypes.POINTER(dbl)],
         "gs_cache_set_dedup": [vp, i32],
         "gs_graph_count_dense": [vp, i32, vp, ctypes.POINTER(i64)],
+        "gs_embedding_lookup": [vp, ctypes.c_int, i64, i32, i64, vp, vp, i32, ctypes.c_float, vp, ctypes.c_int, i64, vp],
+        "gs_embedding_workspace_bytes": [i32, i64, i32, psz],
+        "gs_embedding_backward": [vp, ctypes.c_int, i64, vp, vp, i32, i64, i32, ctypes.c_float, vp, ctypes.c_int, i64, vp, sz, vp],
+        "gs_embedding_backward_sparse": [vp, ctypes.c_int, i64, vp, vp, i32, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_int, i64,
+                                         vp, sz, vp],
+        "gs_train_status": [vp],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -618,3 +624,107 @@ def gs_alu_ceiling(what: int, milliseconds: int = 20, stream=None) -> float:
 def gs_cache_set_dedup(cache: Cache, method: int):
     """GS_DEDUP_DIRECT / GS_DEDUP_HASH / GS_DEDUP_SORT for the following batches on this cache."""
     _check(_L.gs_cache_set_dedup(cache.handle, int(method)))
+
+
+# ---------------------------------------------------------------- training operators
+_DTYPE = {torch.float32: GS_F32, torch.bfloat16: GS_BF16}
+
+
+def _dtype(t: torch.dtype) -> int:
+    code = _DTYPE.get(t)
+    if code is None:
+        raise TypeError("float32 or bfloat16 expected, got %s" % t)
+    return code
+
+
+def _rows_2d(t: torch.Tensor, what: str) -> torch.Tensor:
+    if not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise TypeError("%s must be a row-major 2-D CUDA tensor" % what)
+    return t
+
+
+def _ids_1d(t: torch.Tensor, what: str) -> torch.Tensor:
+    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous 1-D int32 CUDA tensor" % what)
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Row pitch; a single row may carry any stride."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def gs_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: torch.Tensor = None,
+                        out_dtype: torch.dtype = None, count: torch.Tensor = None, stream=None) -> torch.Tensor:
+    """out[p] = scale * table[ids[p]]; ids outside the table give rows of zeros.  `count`: a 0-d int32 CUDA tensor
+    with the list's length (`ids` is then the bound)."""
+    _rows_2d(table, "table")
+    _ids_1d(ids, "ids")
+    if out is None:
+        out = torch.empty((ids.numel(), table.shape[1]), dtype=out_dtype or table.dtype, device=table.device)
+    else:
+        _rows_2d(out, "out")
+        if out.shape[0] < ids.numel() or out.shape[1] != table.shape[1]:
+            raise ValueError("out must be [len(ids), dim]")
+    _check(_L.gs_embedding_lookup(_ptr(table), _dtype(table.dtype), table.shape[0], table.shape[1], _ld(table), _ptr(ids),
+                                  _ptr(count), ids.numel(), float(scale), _ptr(out), _dtype(out.dtype), _ld(out),
+                                  _stream(stream)))
+    return out
+
+
+def gs_embedding_workspace_bytes(num_ids: int, table_rows: int, dim: int) -> int:
+    out = ctypes.c_size_t()
+    _check(_L.gs_embedding_workspace_bytes(int(num_ids), int(table_rows), int(dim), ctypes.byref(out)))
+    return out.value
+
+
+def _embedding_grad_args(dout, ids):
+    _rows_2d(dout, "dout")
+    _ids_1d(ids, "ids")
+    if dout.shape[0] < ids.numel():
+        raise ValueError("dout has fewer rows than there are ids")
+
+
+def gs_embedding_backward(dout: torch.Tensor, ids: torch.Tensor, table_rows: int, workspace: torch.Tensor, scale: float = 1.0,
+                          out: torch.Tensor = None, out_dtype: torch.dtype = None, count: torch.Tensor = None,
+                          stream=None) -> torch.Tensor:
+    """Gradient of the whole table: row r = scale * sum of dout[p] over ids[p] == r, zeros elsewhere."""
+    _embedding_grad_args(dout, ids)
+    if out is None:
+        out = torch.empty((int(table_rows), dout.shape[1]), dtype=out_dtype or dout.dtype, device=dout.device)
+    else:
+        _rows_2d(out, "out")
+        if tuple(out.shape) != (int(table_rows), dout.shape[1]):
+            raise ValueError("out must be [table_rows, dim]")
+    _check(_L.gs_embedding_backward(_ptr(dout), _dtype(dout.dtype), _ld(dout), _ptr(ids), _ptr(count), ids.numel(),
+                                    int(table_rows), dout.shape[1], float(scale), _ptr(out), _dtype(out.dtype), _ld(out),
+                                    _ptr(workspace), workspace.numel(), _stream(stream)))
+    return out
+
+
+def gs_embedding_backward_sparse(dout: torch.Tensor, ids: torch.Tensor, table_rows: int, workspace: torch.Tensor,
+                                 scale: float = 1.0, rows: torch.Tensor = None, num_rows: torch.Tensor = None,
+                                 grad: torch.Tensor = None, out_dtype: torch.dtype = None, count: torch.Tensor = None,
+                                 stream=None):
+    """The rows of the gradient that occur: (ids ascending, their number as int32[1], sums); -1 / zeros behind them."""
+    _embedding_grad_args(dout, ids)
+    n, d = ids.numel(), dout.shape[1]
+    if rows is None:
+        rows = torch.empty(n, dtype=torch.int32, device=dout.device)
+    if num_rows is None:
+        num_rows = torch.empty(1, dtype=torch.int32, device=dout.device)
+    if grad is None:
+        grad = torch.empty((n, d), dtype=out_dtype or dout.dtype, device=dout.device)
+    _ids_1d(rows, "rows")
+    _rows_2d(grad, "grad")
+    if rows.numel() < n or grad.shape[0] < n or grad.shape[1] != d:
+        raise ValueError("rows / grad must hold one entry per id")
+    _check(_L.gs_embedding_backward_sparse(_ptr(dout), _dtype(dout.dtype), _ld(dout), _ptr(ids), _ptr(count), n, int(table_rows), d,
+                                           float(scale), _ptr(rows), _ptr(num_rows), _ptr(grad), _dtype(grad.dtype), _ld(grad),
+                                           _ptr(workspace), workspace.numel(), _stream(stream)))
+    return rows, num_rows, grad
+
+
+def gs_train_status(stream=None):
+    """Synchronises; raises if a kernel of the training operators ever gave up waiting."""
+    _check(_L.gs_train_status(_stream(stream)))

@@ -1,0 +1,57 @@
+// Host-side descriptors of the training operators: embedding rows, attention over blocks, softmax over a table's rows.
+#pragma once
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "gs_internal.h"
+
+namespace gs {
+
+// Length of a list whose size only the device may know: *d_n if d_n is set, never more than `bound`.
+struct Count {
+    const int32_t* d_n;
+    int32_t bound;
+};
+
+// ---- stable sort of (key, payload) pairs; result: key << 32 | payload, ascending keys, equal keys in input order ----
+size_t key_sort_bytes(int64_t n_bound);
+// Keys outside [0, key_limit) take the value key_limit and end behind all others.  payload NULL: the position.
+// The sorted words are left in *sorted (inside the workspace), which stays valid until the workspace is used again.
+cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n, int64_t key_limit, void* workspace,
+                            const unsigned long long** sorted, cudaStream_t s);
+// starts[r] = number of sorted words with key < r, r = 0 .. rows (rows from the device if rows.d_n is set).
+cudaError_t launch_row_starts(const unsigned long long* sorted, Count n, Count rows, int32_t* starts, cudaStream_t s);
+// payloads[i] = low word of sorted[i]
+cudaError_t launch_payloads(const unsigned long long* sorted, Count n, int32_t* payloads, cudaStream_t s);
+cudaError_t train_gave_up(cudaStream_t s, int* h_sort);
+
+// ---- embedding rows ----
+struct EmbedLookup {
+    const void* table;
+    void* out;
+    const int32_t* ids;
+    Count n;
+    int64_t table_rows, table_ld, out_ld;
+    int32_t dim;
+    gs_dtype table_dtype, out_dtype;
+    float scale;
+};
+cudaError_t launch_embedding_lookup(const EmbedLookup& p, cudaStream_t s);
+
+struct EmbedGrad {
+    const void* dout;
+    void* grad;              // dense: [table_rows][grad_ld]; sparse: [n bound][grad_ld]
+    const int32_t* ids;
+    Count n;
+    int64_t table_rows, dout_ld, grad_ld;
+    int32_t dim;
+    gs_dtype dout_dtype, grad_dtype;
+    float scale;
+    int32_t* rows;           // sparse only: ids of the rows, ascending, -1 behind them
+    int32_t* d_num_rows;     // sparse only
+};
+size_t embedding_workspace(int64_t n_bound, int64_t table_rows, int32_t dim);
+cudaError_t launch_embedding_grad(const EmbedGrad& p, void* workspace, cudaStream_t s);
+
+}  // namespace gs
