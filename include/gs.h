@@ -492,6 +492,41 @@ gs_status gs_embedding_backward_sparse(const void* d_dout, gs_dtype dout_dtype, 
                                        float scale, int32_t* d_rows, int32_t* d_num_rows, void* d_grad, gs_dtype grad_dtype,
                                        int64_t grad_ld, void* d_workspace, size_t workspace_bytes, void* stream);
 
+/* Attention of a block's destinations over their neighbours.  For destination i, query head h, its key/value head
+ * g = h * kv_heads / q_heads, and the edges e = indptr[i] .. indptr[i+1) with source j = indices[e]:
+ *   s_e = scale * <q[i,h], k[j,g]>,  lse[i,h] = log sum_e exp(s_e),  out[i,h] = sum_e exp(s_e - lse[i,h]) v[j,g]
+ * An edge whose index is outside [0, num_src) is masked (its rows are not read); a destination without an unmasked
+ * edge gets out = 0, lse = -inf and has no part in any gradient.
+ *   block      a block of gs_sample_batch, or one the caller fills: max_* are the sizes, d_num_* device scalars with
+ *              the actual ones, or NULL (the sizes are exact; all three together)
+ *   max_row    an upper bound on the edges of one destination (the fan-out, for a sampled block), or 0 if it is not
+ *              known: rows above 256 edges are then split over the device.  A longer row than promised is slower,
+ *              not wrong.
+ *   gs_heads   [rows][heads][head_dim] of `dtype`, head_dim contiguous, strides in elements (a slice of a fused
+ *              projection is fine); q, out, dout, dq have the destinations' rows and q_heads, k, v, dk, dv the
+ *              sources' rows and kv_heads (a divisor of q_heads); 1 <= head_dim <= 256, q_heads <= 1024
+ *   d_lse      float[max_dst][q_heads]
+ * gs_block_reverse turns the block's edges to source order, once for all layers that use the block: the
+ * destinations of source j, ascending, are d_rev_dst[d_rev_indptr[j] .. d_rev_indptr[j+1]) (int32[max_src + 1] and
+ * int32[max_edges]; masked edges are left out).  The backward pass recomputes the probabilities from lse and sums dk
+ * and dv in that order; dq, dk and dv are written for every row of their counts (zeros where nothing contributes).
+ * Workspace: gs_block_attention_workspace_bytes, enough for any of the three calls. */
+typedef struct {
+    void* d_data;
+    int64_t row_stride, head_stride;
+} gs_heads;
+gs_status gs_block_attention_workspace_bytes(int32_t max_dst, int32_t max_edges, int32_t q_heads, int32_t head_dim, size_t* bytes);
+gs_status gs_block_attention_forward(const gs_block* block, int32_t max_row, gs_dtype dtype, int32_t q_heads, int32_t kv_heads,
+                                     int32_t head_dim, float scale, const gs_heads* q, const gs_heads* k, const gs_heads* v,
+                                     const gs_heads* out, float* d_lse, void* d_workspace, size_t workspace_bytes, void* stream);
+gs_status gs_block_reverse(const gs_block* block, int32_t* d_rev_indptr, int32_t* d_rev_dst, void* d_workspace,
+                           size_t workspace_bytes, void* stream);
+gs_status gs_block_attention_backward(const gs_block* block, int32_t max_row, const int32_t* d_rev_indptr, const int32_t* d_rev_dst,
+                                      gs_dtype dtype, int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale,
+                                      const gs_heads* q, const gs_heads* k, const gs_heads* v, const gs_heads* out,
+                                      const float* d_lse, const gs_heads* dout, const gs_heads* dq, const gs_heads* dk,
+                                      const gs_heads* dv, void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* Synchronises `stream`; GS_ERR_CUDA if a kernel of the training operators ever gave up one of its (bounded) waits. */
 gs_status gs_train_status(void* stream);
 

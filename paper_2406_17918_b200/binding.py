@@ -43,6 +43,10 @@ class _CBlockBuffers(ctypes.Structure):
                 ("d_indices", ctypes.c_void_p), ("indices_capacity", ctypes.c_int64)]
 
 
+class _CHeads(ctypes.Structure):
+    _fields_ = [("d_data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
 NOALLOC_SCRATCH_BYTES = 64 << 20
 
 
@@ -114,6 +118,11 @@ def _load():
         "gs_embedding_backward_sparse": [vp, ctypes.c_int, i64, vp, vp, i32, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_int, i64,
                                          vp, sz, vp],
         "gs_train_status": [vp],
+        "gs_block_attention_workspace_bytes": [i32, i32, i32, i32, psz],
+        "gs_block_attention_forward": [vp, i32, ctypes.c_int, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, sz, vp],
+        "gs_block_reverse": [vp, vp, vp, vp, sz, vp],
+        "gs_block_attention_backward": [vp, i32, vp, vp, ctypes.c_int, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                        vp, sz, vp],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -723,6 +732,98 @@ def gs_embedding_backward_sparse(dout: torch.Tensor, ids: torch.Tensor, table_ro
                                            float(scale), _ptr(rows), _ptr(num_rows), _ptr(grad), _dtype(grad.dtype), _ld(grad),
                                            _ptr(workspace), workspace.numel(), _stream(stream)))
     return rows, num_rows, grad
+
+
+def _csr_block(indptr, indices, num_src, counts):
+    _ids_1d(indptr, "indptr")
+    _ids_1d(indices, "indices")
+    b = _CBlock()
+    b.max_dst, b.max_src, b.max_edges = indptr.numel() - 1, int(num_src), indices.numel()
+    b.d_indptr, b.d_indices = indptr.data_ptr(), indices.data_ptr()
+    if counts is not None:
+        b.d_num_dst, b.d_num_src, b.d_num_edges = (c.data_ptr() for c in counts)
+    return b
+
+
+def _heads(t, what, rows, heads, dim, dtype):
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != dim or \
+            (t.stride(2) != 1 and dim > 1):
+        raise TypeError("%s must be a CUDA tensor [%d, %d, %d] of %s with a contiguous last dimension" % (what, rows, heads, dim, dtype))
+    return ctypes.byref(_CHeads(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), dim),
+                                t.stride(1) if heads > 1 else dim))
+
+
+def gs_block_attention_workspace_bytes(num_dst: int, num_src: int, num_edges: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    """Bytes for gs_block_attention_forward, gs_block_reverse and gs_block_attention_backward on such a block."""
+    out = ctypes.c_size_t()
+    _check(_L.gs_block_attention_workspace_bytes(int(num_dst), int(num_edges), int(q_heads), int(head_dim), ctypes.byref(out)))
+    return out.value
+
+
+def gs_block_attention_forward(indptr: torch.Tensor, indices: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                               workspace: torch.Tensor, scale: float = None, max_row: int = 0, out: torch.Tensor = None,
+                               lse: torch.Tensor = None, counts=None, stream=None):
+    """Attention of a block's destinations (q: [dst, q_heads, head_dim]) over their sources (k, v: [src, kv_heads,
+    head_dim]); indptr, indices: the block's int32 arrays; an index outside [0, src) is masked.  `scale` defaults to
+    1 / sqrt(head_dim); `max_row`: an upper bound on a row's edges (the fan-out) if one is known; `counts`: the
+    device scalars of Block.counts_device() when the arrays are only bounds.  Returns (out, lse)."""
+    n, hq, d = q.shape
+    hk = k.shape[1]
+    if indptr.numel() - 1 > n:
+        raise ValueError("q has fewer rows than the block has destinations")
+    b = _csr_block(indptr, indices, k.shape[0], counts)
+    if out is None:
+        out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((n, hq), dtype=torch.float32, device=q.device)
+    elif lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape[0] < b.max_dst or lse.shape[1] != hq:
+        raise TypeError("lse must be a contiguous float32 tensor [dst, q_heads]")
+    _check(_L.gs_block_attention_forward(ctypes.byref(b), int(max_row), _dtype(q.dtype), hq, hk, d,
+                                         d ** -0.5 if scale is None else float(scale), _heads(q, "q", b.max_dst, hq, d, q.dtype),
+                                         _heads(k, "k", b.max_src, hk, d, q.dtype), _heads(v, "v", b.max_src, hk, d, q.dtype),
+                                         _heads(out, "out", b.max_dst, hq, d, q.dtype), _ptr(lse), _ptr(workspace), workspace.numel(),
+                                         _stream(stream)))
+    return out, lse
+
+
+def gs_block_reverse(indptr: torch.Tensor, indices: torch.Tensor, num_src: int, workspace: torch.Tensor, rev_indptr: torch.Tensor = None,
+                     rev_dst: torch.Tensor = None, counts=None, stream=None):
+    """The block in source order: (int32[num_src + 1] offsets, int32[edges] destinations), masked edges left out."""
+    b = _csr_block(indptr, indices, num_src, counts)
+    if rev_indptr is None:
+        rev_indptr = torch.empty(b.max_src + 1, dtype=torch.int32, device=indptr.device)
+    if rev_dst is None:
+        rev_dst = torch.empty(b.max_edges, dtype=torch.int32, device=indptr.device)
+    if _ids_1d(rev_indptr, "rev_indptr").numel() < b.max_src + 1 or _ids_1d(rev_dst, "rev_dst").numel() < b.max_edges:
+        raise ValueError("rev_indptr / rev_dst are too small")
+    _check(_L.gs_block_reverse(ctypes.byref(b), _ptr(rev_indptr), _ptr(rev_dst), _ptr(workspace), workspace.numel(), _stream(stream)))
+    return rev_indptr, rev_dst
+
+
+def gs_block_attention_backward(indptr: torch.Tensor, indices: torch.Tensor, reverse, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                                out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor, workspace: torch.Tensor, scale: float = None,
+                                max_row: int = 0, dq: torch.Tensor = None, dk: torch.Tensor = None, dv: torch.Tensor = None, counts=None,
+                                stream=None):
+    """Gradients of gs_block_attention_forward; `reverse` is what gs_block_reverse returned.  Returns (dq, dk, dv)."""
+    n, hq, d = q.shape
+    hk = k.shape[1]
+    b = _csr_block(indptr, indices, k.shape[0], counts)
+    rev_indptr, rev_dst = reverse
+    if _ids_1d(rev_indptr, "rev_indptr").numel() < b.max_src + 1 or _ids_1d(rev_dst, "rev_dst").numel() < b.max_edges:
+        raise ValueError("reverse belongs to another block")
+    if lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.shape[0] < b.max_dst or lse.shape[1] != hq:
+        raise TypeError("lse must be a contiguous float32 tensor [dst, q_heads]")
+    dq = torch.empty((n, hq, d), dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty((k.shape[0], hk, d), dtype=q.dtype, device=q.device) if dk is None else dk
+    dv = torch.empty((v.shape[0], hk, d), dtype=q.dtype, device=q.device) if dv is None else dv
+    t = q.dtype
+    _check(_L.gs_block_attention_backward(ctypes.byref(b), int(max_row), _ptr(rev_indptr), _ptr(rev_dst), _dtype(t), hq, hk, d,
+                                          d ** -0.5 if scale is None else float(scale), _heads(q, "q", b.max_dst, hq, d, t),
+                                          _heads(k, "k", b.max_src, hk, d, t), _heads(v, "v", b.max_src, hk, d, t),
+                                          _heads(out, "out", b.max_dst, hq, d, t), _ptr(lse), _heads(dout, "dout", b.max_dst, hq, d, t),
+                                          _heads(dq, "dq", b.max_dst, hq, d, t), _heads(dk, "dk", b.max_src, hk, d, t),
+                                          _heads(dv, "dv", b.max_src, hk, d, t), _ptr(workspace), workspace.numel(), _stream(stream)))
+    return dq, dk, dv
 
 
 def gs_train_status(stream=None):

@@ -1,0 +1,702 @@
+// Softmax attention of a block's destinations over their listed sources, forward and backward.
+//
+// For destination i, query head h, key/value head g(h) and the edges j of row i:
+//   s = scale q_ih . k_jg,  lse_ih = log sum_j exp s,  o_ih = sum_j p v_jg,  p = exp(s - lse_ih);
+//   delta = do . o,  ds = p (do . v - delta) scale,  dq_i = sum_j ds k_j,  dk_j = sum_i ds q_i,  dv_j = sum_i p do_i.
+// One pass over the edges each: the forward keeps a running maximum and sum, the backward recomputes p from lse.
+//
+// Every edge gathers whole rows, so the kernels are bound by the gathered bytes: a group of tl lanes holds one
+// (row, head) with one wide load per lane and operand, U edges are in flight per group, and groups of one row's heads are
+// neighbours in a warp, so that an edge's row is read in one piece.  dk and dv are summed in source order over the
+// reversed block (a stable sort), each row by one group: no atomics, the result does not depend on the schedule.
+// A row longer than AT_CHUNK edges (hubs) is cut into chunks; the chunks' results are joined in order.
+// `slots` groups share one row when there are too few rows to fill the device.
+#include <initializer_list>
+
+#include "gs_device.cuh"
+#include "gs_train.cuh"
+#include "gs_train.h"
+
+namespace gs {
+
+constexpr int AT_THREADS = 256;
+constexpr int AT_CHUNK = 256;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+struct Attend {
+    BlockAttention a;
+    const int32_t* starts;      // row offsets and columns: the block's, or the reversed block's
+    const int32_t* cols;
+    Count rows, columns;
+    int edge_bound;
+    int tl, slots, units_per_row;
+    int split;                  // rows above AT_CHUNK edges go to the chunk list
+    int chunk_mode;             // this launch works through the chunk list
+    int32_t* words;             // [0] chunks, [1] long rows
+    int2* items;                // chunk -> (row, chunk of the row)
+    int4* longs;                // long row -> (row, first chunk, chunks, -)
+    float* partial;
+    float2* stat;               // [dst][q heads]: lse in base 2, delta
+};
+
+__device__ __forceinline__ int length_of(const Count& c) {
+    if (!c.d_n) return c.bound;
+    const int n = __ldg(c.d_n);
+    return n < 0 ? 0 : (n > c.bound ? c.bound : n);
+}
+
+// What one group of lanes works on: a (row, unit of heads) and its range of edges.
+struct Work {
+    int row, unit, item, begin, end;
+    bool live;
+};
+
+// Chunks of a long row join the list once, from the row's first unit.
+__device__ __forceinline__ void list_long_row(const Attend& P, int row, int len) {
+    const int nc = (len + AT_CHUNK - 1) / AT_CHUNK;
+    const int first = atomicAdd(P.words, nc);
+    P.longs[atomicAdd(P.words + 1, 1)] = make_int4(row, first, nc, 0);
+    for (int c = 0; c < nc; ++c) P.items[first + c] = make_int2(row, c);
+}
+
+__device__ __forceinline__ Work find_work(const Attend& P, int64_t u, int64_t units, bool first_lane) {
+    Work w;
+    w.live = u < units;
+    w.row = w.unit = w.item = w.begin = w.end = 0;
+    if (!w.live) return w;
+    const int r = (int)(u / P.units_per_row);
+    w.unit = (int)(u - (int64_t)r * P.units_per_row);
+    w.row = r;
+    int first = 0;
+    if (P.chunk_mode) {
+        w.item = r;
+        const int2 it = P.items[r];
+        w.row = it.x;
+        first = it.y * AT_CHUNK;
+    }
+    int b = __ldg(P.starts + w.row), e = __ldg(P.starts + w.row + 1);
+    b = b < 0 ? 0 : b;
+    e = e > P.edge_bound ? P.edge_bound : e;
+    if (e < b) e = b;
+    if (P.chunk_mode) {
+        w.begin = b + first;
+        w.end = w.begin + AT_CHUNK < e ? w.begin + AT_CHUNK : e;
+    } else {
+        w.begin = b;
+        w.end = e;
+        if (P.split && e - b > AT_CHUNK) {
+            if (w.unit == 0 && first_lane) list_long_row(P, w.row, e - b);
+            w.end = b;
+            w.live = false;
+        }
+    }
+    return w;
+}
+
+template <int N> __device__ __forceinline__ void group_sum(float (&x)[N], int tl) {
+    for (int o = 1; o < tl; o <<= 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(FULL, x[i], o);
+    }
+}
+
+// The lane's elements of one head row: NV pieces of VE, tl pieces apart.
+template <typename T, int VE, int NV> struct Piece {
+    Raw<T, VE> r[NV];
+    __device__ __forceinline__ void load(const T* row, int t, int tl, int dim, bool on) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (t + j * tl) * VE;
+            r[j] = on && c < dim ? load_raw<T, VE>(row + c) : zero_raw<T, VE>();
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[NV * VE]) const {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float y[VE];
+            unpack<T, VE>(r[j], y);
+#pragma unroll
+            for (int i = 0; i < VE; ++i) x[j * VE + i] = y[i];
+        }
+    }
+};
+
+template <typename T, int VE, int NV>
+__device__ __forceinline__ void store_piece(T* row, int t, int tl, int dim, const float (&x)[NV * VE]) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (t + j * tl) * VE;
+        if (c < dim) {
+            float y[VE];
+#pragma unroll
+            for (int i = 0; i < VE; ++i) y[i] = x[j * VE + i];
+            store_vec<T, VE>(row + c, y);
+        }
+    }
+}
+
+template <int VE, int NV> __device__ __forceinline__ void store_partial(float* row, int t, int tl, int dim, const float (&x)[NV * VE]) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (t + j * tl) * VE;
+        if (c < dim) {
+#pragma unroll
+            for (int i = 0; i < VE; ++i) row[c + i] = x[j * VE + i];
+        }
+    }
+}
+
+template <typename T, int VE, int NV, int G, int U>
+__global__ void __launch_bounds__(AT_THREADS) k_attend_forward(const __grid_constant__ Attend P) {
+    constexpr int E = VE * NV;
+    const int lane = threadIdx.x & 31, t = lane & (P.tl - 1), slot = (lane / P.tl) & (P.slots - 1);
+    const int width = P.tl * P.slots, per_block = AT_THREADS / width;
+    const int rows = P.chunk_mode ? __ldcg(P.words) : length_of(P.rows), cols = length_of(P.columns);
+    const int64_t units = (int64_t)rows * P.units_per_row;
+    const float c2 = P.a.scale * LOG2E;
+    const int D = P.a.head_dim;
+    const T* kbase = (const T*)P.a.k.data;
+    const T* vbase = (const T*)P.a.v.data;
+    for (int64_t base = (int64_t)blockIdx.x * per_block; base < units; base += (int64_t)gridDim.x * per_block) {
+        const Work w = find_work(P, base + threadIdx.x / width, units, t == 0 && slot == 0);
+        const int h0 = w.unit * G, g = h0 / (P.a.q_heads / P.a.kv_heads);
+        float q[G][E], acc[G][E], m[G], l[G];
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            Piece<T, VE, NV> p;
+            p.load((const T*)P.a.q.data + (int64_t)w.row * P.a.q.row_stride + (int64_t)(h0 + i) * P.a.q.head_stride, t, P.tl, D, w.live);
+            p.get(q[i]);
+            m[i] = -INFINITY;
+            l[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < E; ++c) acc[i][c] = 0.f;
+        }
+        const int mine = (w.end - w.begin + P.slots * U - 1) / (P.slots * U);
+        const int trips = __reduce_max_sync(FULL, mine);
+        for (int it = 0; it < trips; ++it) {
+            Piece<T, VE, NV> kp[U], vp[U];
+            bool on[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const int e = w.begin + (it * U + j) * P.slots + slot;
+                const int col = e < w.end ? __ldg(P.cols + e) : -1;
+                on[j] = (uint32_t)col < (uint32_t)cols;
+                kp[j].load(kbase + (int64_t)col * P.a.k.row_stride + (int64_t)g * P.a.k.head_stride, t, P.tl, D, on[j]);
+                vp[j].load(vbase + (int64_t)col * P.a.v.row_stride + (int64_t)g * P.a.v.head_stride, t, P.tl, D, on[j]);
+            }
+            float s[U * G];
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                float k[E];
+                kp[j].get(k);
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    float x = 0.f;
+#pragma unroll
+                    for (int c = 0; c < E; ++c) x = fmaf(q[i][c], k[c], x);
+                    s[j * G + i] = x;
+                }
+            }
+            group_sum<U * G>(s, P.tl);
+            float p[U * G];
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                float top = m[i];
+#pragma unroll
+                for (int j = 0; j < U; ++j) {
+                    s[j * G + i] = on[j] ? s[j * G + i] * c2 : -INFINITY;
+                    top = fmaxf(top, s[j * G + i]);
+                }
+                const float ref = top == -INFINITY ? 0.f : top;     // nothing seen yet: all weights are zero
+                const float corr = fast_exp2(m[i] - ref);
+                m[i] = top;
+                l[i] *= corr;
+#pragma unroll
+                for (int j = 0; j < U; ++j) {
+                    p[j * G + i] = fast_exp2(s[j * G + i] - ref);
+                    l[i] += p[j * G + i];
+                }
+#pragma unroll
+                for (int c = 0; c < E; ++c) acc[i][c] *= corr;
+            }
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                float v[E];
+                vp[j].get(v);
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+#pragma unroll
+                    for (int c = 0; c < E; ++c) acc[i][c] = fmaf(p[j * G + i], v[c], acc[i][c]);
+            }
+        }
+        for (int o = P.tl; o < width; o <<= 1) {                      // join the slots of a row
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                const float mo = __shfl_xor_sync(FULL, m[i], o), lo = __shfl_xor_sync(FULL, l[i], o);
+                const float top = fmaxf(m[i], mo), ref = top == -INFINITY ? 0.f : top;
+                const float ca = fast_exp2(m[i] - ref), cb = fast_exp2(mo - ref);
+                m[i] = top;
+                l[i] = l[i] * ca + lo * cb;
+#pragma unroll
+                for (int c = 0; c < E; ++c) acc[i][c] = acc[i][c] * ca + __shfl_xor_sync(FULL, acc[i][c], o) * cb;
+            }
+        }
+        if (!w.live || slot) continue;
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const int h = h0 + i;
+            if (P.chunk_mode) {
+                float* part = P.partial + ((int64_t)w.item * P.a.q_heads + h) * (D + 2);
+                store_partial<VE, NV>(part, t, P.tl, D, acc[i]);
+                if (t == 0) {
+                    part[D] = m[i];
+                    part[D + 1] = l[i];
+                }
+            } else {
+                const bool none = l[i] == 0.f;                        // no edge left by the mask: zero row, log of an empty sum
+                const float inv = none ? 0.f : 1.f / l[i];
+#pragma unroll
+                for (int c = 0; c < E; ++c) acc[i][c] = none ? 0.f : acc[i][c] * inv;
+                store_piece<T, VE, NV>((T*)P.a.out.data + (int64_t)w.row * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride, t, P.tl, D, acc[i]);
+                if (t == 0) P.a.lse[(int64_t)w.row * P.a.q_heads + h] = none ? -INFINITY : m[i] * LN2 + logf(l[i]);
+            }
+        }
+    }
+}
+
+// One warp per (long row, query head): the chunks' sums, rescaled to the common maximum, in order.
+template <typename T> __global__ void __launch_bounds__(AT_THREADS) k_attend_forward_join(const __grid_constant__ Attend P) {
+    const int lane = threadIdx.x & 31, D = P.a.head_dim;
+    const int64_t units = (int64_t)__ldcg(P.words + 1) * P.a.q_heads, stride = (int64_t)P.a.q_heads * (D + 2);
+    for (int64_t u = (int64_t)blockIdx.x * (AT_THREADS / 32) + threadIdx.x / 32; u < units; u += (int64_t)gridDim.x * (AT_THREADS / 32)) {
+        const int4 row = P.longs[u / P.a.q_heads];
+        const int h = (int)(u % P.a.q_heads);
+        const float* part = P.partial + (int64_t)row.y * stride + (int64_t)h * (D + 2);
+        float m = -INFINITY, l = 0.f;
+        for (int c = lane; c < row.z; c += 32) m = fmaxf(m, part[c * stride + D]);
+        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, o));
+        const float ref = m == -INFINITY ? 0.f : m;
+        for (int c = lane; c < row.z; c += 32) l += part[c * stride + D + 1] * fast_exp2(part[c * stride + D] - ref);
+        for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(FULL, l, o);
+        const bool none = l == 0.f;
+        T* out = (T*)P.a.out.data + (int64_t)row.x * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride;
+        for (int col = lane; col < D; col += 32) {
+            float acc = 0.f;
+#pragma unroll 4
+            for (int c = 0; c < row.z; ++c) acc = fmaf(part[c * stride + col], fast_exp2(part[c * stride + D] - ref), acc);
+            out[col] = from_f32<T>(none ? 0.f : acc / l);
+        }
+        if (lane == 0) P.a.lse[(int64_t)row.x * P.a.q_heads + h] = none ? -INFINITY : m * LN2 + logf(l);
+    }
+}
+
+// dq, and the statistics the source-order pass needs per (destination, head).
+template <typename T, int VE, int NV, int G, int U>
+__global__ void __launch_bounds__(AT_THREADS) k_attend_dq(const __grid_constant__ Attend P) {
+    constexpr int E = VE * NV;
+    const int lane = threadIdx.x & 31, t = lane & (P.tl - 1), slot = (lane / P.tl) & (P.slots - 1);
+    const int width = P.tl * P.slots, per_block = AT_THREADS / width;
+    const int rows = P.chunk_mode ? __ldcg(P.words) : length_of(P.rows), cols = length_of(P.columns);
+    const int64_t units = (int64_t)rows * P.units_per_row;
+    const float c2 = P.a.scale * LOG2E;
+    const int D = P.a.head_dim;
+    const T* kbase = (const T*)P.a.k.data;
+    const T* vbase = (const T*)P.a.v.data;
+    for (int64_t base = (int64_t)blockIdx.x * per_block; base < units; base += (int64_t)gridDim.x * per_block) {
+        const int64_t u = base + threadIdx.x / width;
+        const Work w = find_work(P, u, units, t == 0 && slot == 0);
+        const bool in = u < units;
+        const int h0 = w.unit * G, g = h0 / (P.a.q_heads / P.a.kv_heads);
+        float q[G][E], go[G][E], acc[G][E], lse2[G], delta[G];
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            Piece<T, VE, NV> p;
+            float o[E];
+            p.load((const T*)P.a.out.data + (int64_t)w.row * P.a.out.row_stride + (int64_t)(h0 + i) * P.a.out.head_stride, t, P.tl, D, in);
+            p.get(o);
+            p.load((const T*)P.a.dout.data + (int64_t)w.row * P.a.dout.row_stride + (int64_t)(h0 + i) * P.a.dout.head_stride, t, P.tl, D, in);
+            p.get(go[i]);
+            p.load((const T*)P.a.q.data + (int64_t)w.row * P.a.q.row_stride + (int64_t)(h0 + i) * P.a.q.head_stride, t, P.tl, D, in);
+            p.get(q[i]);
+            delta[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < E; ++c) {
+                delta[i] = fmaf(go[i][c], o[c], delta[i]);
+                acc[i][c] = 0.f;
+            }
+            lse2[i] = in ? __ldg(P.a.lse + (int64_t)w.row * P.a.q_heads + h0 + i) * LOG2E : 0.f;
+        }
+        group_sum<G>(delta, P.tl);
+        if (in && !P.chunk_mode && slot == 0 && t == 0) {
+#pragma unroll
+            for (int i = 0; i < G; ++i) P.stat[(int64_t)w.row * P.a.q_heads + h0 + i] = make_float2(lse2[i], delta[i]);
+        }
+        const int mine = (w.end - w.begin + P.slots * U - 1) / (P.slots * U);
+        const int trips = __reduce_max_sync(FULL, mine);
+        for (int it = 0; it < trips; ++it) {
+            Piece<T, VE, NV> kp[U], vp[U];
+            bool on[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const int e = w.begin + (it * U + j) * P.slots + slot;
+                const int col = e < w.end ? __ldg(P.cols + e) : -1;
+                on[j] = (uint32_t)col < (uint32_t)cols;
+                kp[j].load(kbase + (int64_t)col * P.a.k.row_stride + (int64_t)g * P.a.k.head_stride, t, P.tl, D, on[j]);
+                vp[j].load(vbase + (int64_t)col * P.a.v.row_stride + (int64_t)g * P.a.v.head_stride, t, P.tl, D, on[j]);
+            }
+            float s[2 * U * G];
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                float k[E], v[E];
+                kp[j].get(k);
+                vp[j].get(v);
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    float x = 0.f, y = 0.f;
+#pragma unroll
+                    for (int c = 0; c < E; ++c) {
+                        x = fmaf(q[i][c], k[c], x);
+                        y = fmaf(go[i][c], v[c], y);
+                    }
+                    s[j * G + i] = x;
+                    s[U * G + j * G + i] = y;
+                }
+            }
+            group_sum<2 * U * G>(s, P.tl);
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                float k[E];
+                kp[j].get(k);
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    const float p = on[j] ? fast_exp2(fmaf(s[j * G + i], c2, -lse2[i])) : 0.f;
+                    const float ds = on[j] ? p * (s[U * G + j * G + i] - delta[i]) : 0.f;
+#pragma unroll
+                    for (int c = 0; c < E; ++c) acc[i][c] = fmaf(ds, k[c], acc[i][c]);
+                }
+            }
+        }
+        for (int o = P.tl; o < width; o <<= 1) {
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+#pragma unroll
+                for (int c = 0; c < E; ++c) acc[i][c] += __shfl_xor_sync(FULL, acc[i][c], o);
+        }
+        if (!w.live || slot) continue;
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const int h = h0 + i;
+            if (P.chunk_mode) {
+                store_partial<VE, NV>(P.partial + ((int64_t)w.item * P.a.q_heads + h) * D, t, P.tl, D, acc[i]);
+            } else {
+#pragma unroll
+                for (int c = 0; c < E; ++c) acc[i][c] *= P.a.scale;
+                store_piece<T, VE, NV>((T*)P.a.dq.data + (int64_t)w.row * P.a.dq.row_stride + (int64_t)h * P.a.dq.head_stride, t, P.tl, D, acc[i]);
+            }
+        }
+    }
+}
+
+// dk and dv of one (source, key/value head): over the destinations that list it, and over the query heads that share it.
+template <typename T, int VE, int NV, int G, int U>
+__global__ void __launch_bounds__(AT_THREADS) k_attend_dkv(const __grid_constant__ Attend P) {
+    constexpr int E = VE * NV;
+    const int lane = threadIdx.x & 31, t = lane & (P.tl - 1), slot = (lane / P.tl) & (P.slots - 1);
+    const int width = P.tl * P.slots, per_block = AT_THREADS / width;
+    const int rows = P.chunk_mode ? __ldcg(P.words) : length_of(P.rows), cols = length_of(P.columns);
+    const int64_t units = (int64_t)rows * P.units_per_row;
+    const float c2 = P.a.scale * LOG2E;
+    const int D = P.a.head_dim, group = P.a.q_heads / P.a.kv_heads;
+    const T* qbase = (const T*)P.a.q.data;
+    const T* gbase = (const T*)P.a.dout.data;
+    for (int64_t base = (int64_t)blockIdx.x * per_block; base < units; base += (int64_t)gridDim.x * per_block) {
+        const Work w = find_work(P, base + threadIdx.x / width, units, t == 0 && slot == 0);
+        const int g = w.unit;
+        float k[E], v[E], dk[E], dv[E];
+        {
+            Piece<T, VE, NV> p;
+            const bool any = w.live && w.end > w.begin;
+            p.load((const T*)P.a.k.data + (int64_t)w.row * P.a.k.row_stride + (int64_t)g * P.a.k.head_stride, t, P.tl, D, any);
+            p.get(k);
+            p.load((const T*)P.a.v.data + (int64_t)w.row * P.a.v.row_stride + (int64_t)g * P.a.v.head_stride, t, P.tl, D, any);
+            p.get(v);
+        }
+#pragma unroll
+        for (int c = 0; c < E; ++c) dk[c] = dv[c] = 0.f;
+        const int mine = (w.end - w.begin + P.slots * U - 1) / (P.slots * U);
+        const int trips = __reduce_max_sync(FULL, mine);
+        for (int h0 = g * group; h0 < (g + 1) * group; h0 += G) {
+            for (int it = 0; it < trips; ++it) {
+                Piece<T, VE, NV> qp[U][G], gp[U][G];
+                float2 st[U][G];
+                bool on[U];
+#pragma unroll
+                for (int j = 0; j < U; ++j) {
+                    const int e = w.begin + (it * U + j) * P.slots + slot;
+                    const int col = e < w.end ? __ldg(P.cols + e) : -1;
+                    on[j] = (uint32_t)col < (uint32_t)cols;
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        qp[j][i].load(qbase + (int64_t)col * P.a.q.row_stride + (int64_t)(h0 + i) * P.a.q.head_stride, t, P.tl, D, on[j]);
+                        gp[j][i].load(gbase + (int64_t)col * P.a.dout.row_stride + (int64_t)(h0 + i) * P.a.dout.head_stride, t, P.tl, D, on[j]);
+                        st[j][i] = on[j] ? __ldg(P.stat + (int64_t)col * P.a.q_heads + h0 + i) : make_float2(0.f, 0.f);
+                    }
+                }
+                float s[2 * U * G];
+#pragma unroll
+                for (int j = 0; j < U; ++j)
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        float q[E], go[E], x = 0.f, y = 0.f;
+                        qp[j][i].get(q);
+                        gp[j][i].get(go);
+#pragma unroll
+                        for (int c = 0; c < E; ++c) {
+                            x = fmaf(q[c], k[c], x);
+                            y = fmaf(go[c], v[c], y);
+                        }
+                        s[j * G + i] = x;
+                        s[U * G + j * G + i] = y;
+                    }
+                group_sum<2 * U * G>(s, P.tl);
+#pragma unroll
+                for (int j = 0; j < U; ++j)
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        float q[E], go[E];
+                        qp[j][i].get(q);
+                        gp[j][i].get(go);
+                        const float p = on[j] ? fast_exp2(fmaf(s[j * G + i], c2, -st[j][i].x)) : 0.f;
+                        const float ds = on[j] ? p * (s[U * G + j * G + i] - st[j][i].y) : 0.f;
+#pragma unroll
+                        for (int c = 0; c < E; ++c) {
+                            dv[c] = fmaf(p, go[c], dv[c]);
+                            dk[c] = fmaf(ds, q[c], dk[c]);
+                        }
+                    }
+            }
+        }
+        for (int o = P.tl; o < width; o <<= 1) {
+#pragma unroll
+            for (int c = 0; c < E; ++c) {
+                dk[c] += __shfl_xor_sync(FULL, dk[c], o);
+                dv[c] += __shfl_xor_sync(FULL, dv[c], o);
+            }
+        }
+        if (!w.live || slot) continue;
+        if (P.chunk_mode) {
+            float* part = P.partial + ((int64_t)w.item * P.a.kv_heads + g) * 2 * D;
+            store_partial<VE, NV>(part, t, P.tl, D, dk);
+            store_partial<VE, NV>(part + D, t, P.tl, D, dv);
+        } else {
+#pragma unroll
+            for (int c = 0; c < E; ++c) dk[c] *= P.a.scale;
+            store_piece<T, VE, NV>((T*)P.a.dk.data + (int64_t)w.row * P.a.dk.row_stride + (int64_t)g * P.a.dk.head_stride, t, P.tl, D, dk);
+            store_piece<T, VE, NV>((T*)P.a.dv.data + (int64_t)w.row * P.a.dv.row_stride + (int64_t)g * P.a.dv.head_stride, t, P.tl, D, dv);
+        }
+    }
+}
+
+// Chunk sums of long rows added in order: one warp per (row, head, 32 of its `width` values).  dq: one operand of
+// width D; dk and dv: width 2 D, the second half for dv.
+template <typename T, bool KV> __global__ void __launch_bounds__(AT_THREADS) k_attend_sum_join(const __grid_constant__ Attend P) {
+    const int lane = threadIdx.x & 31, D = P.a.head_dim;
+    const int heads = KV ? P.a.kv_heads : P.a.q_heads, width = KV ? 2 * D : D, tiles = (width + 31) / 32;
+    const int64_t units = (int64_t)__ldcg(P.words + 1) * heads * tiles, stride = (int64_t)heads * width;
+    for (int64_t u = (int64_t)blockIdx.x * (AT_THREADS / 32) + threadIdx.x / 32; u < units; u += (int64_t)gridDim.x * (AT_THREADS / 32)) {
+        const int4 row = P.longs[u / ((int64_t)heads * tiles)];
+        const int h = (int)(u / tiles % heads), col = (int)(u % tiles) * 32 + lane;
+        if (col >= width) continue;
+        const float* part = P.partial + (int64_t)row.y * stride + (int64_t)h * width + col;
+        float acc = 0.f;
+#pragma unroll 8
+        for (int c = 0; c < row.z; ++c) acc += part[c * stride];
+        const HeadView& to = !KV ? P.a.dq : (col < D ? P.a.dk : P.a.dv);
+        if (!KV || col < D) acc *= P.a.scale;
+        ((T*)to.data)[(int64_t)row.x * to.row_stride + (int64_t)h * to.head_stride + (col < D ? col : col - D)] = from_f32<T>(acc);
+    }
+}
+
+// The destination of every edge, in edge order.
+__global__ void __launch_bounds__(AT_THREADS) k_edge_rows(const int32_t* __restrict__ indptr, Count dst, int edge_bound, int32_t* __restrict__ rows) {
+    const int n = length_of(dst), lane = threadIdx.x & 31;
+    for (int64_t r = (int64_t)blockIdx.x * (AT_THREADS / 32) + threadIdx.x / 32; r < n; r += (int64_t)gridDim.x * (AT_THREADS / 32)) {
+        const int b = __ldg(indptr + r), end = __ldg(indptr + r + 1), e = end < edge_bound ? end : edge_bound;
+        for (int i = (b < 0 ? 0 : b) + lane; i < e; i += 32) rows[i] = (int32_t)r;
+    }
+}
+
+// ---------------------------------------------------------------- launches
+struct AttendLayout {
+    size_t words, items, longs, stat, partial, total;
+};
+
+static AttendLayout attend_layout(int64_t dst, int64_t edges, int32_t q_heads, int32_t head_dim) {
+    AttendLayout l{};
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
+    const int64_t chunks = 2 * (edges / AT_CHUNK) + 2;
+    l.words = take(256);
+    l.items = take((size_t)chunks * 8);
+    l.longs = take((size_t)(edges / AT_CHUNK + 1) * 16);
+    l.stat = take((size_t)dst * q_heads * 8);
+    l.partial = take((size_t)chunks * q_heads * (2 * (size_t)head_dim + 2) * 4);
+    l.total = off;
+    return l;
+}
+
+size_t reverse_workspace(int64_t edges) { return align_up((size_t)edges * 4, 256) + key_sort_bytes(edges); }
+
+size_t attention_workspace(int64_t dst, int64_t edges, int32_t q_heads, int32_t head_dim) {
+    const size_t a = attend_layout(dst, edges, q_heads, head_dim).total, b = reverse_workspace(edges);
+    return a > b ? a : b;
+}
+
+// Elements per access that the head dimension and all operands allow.
+static int wide_elems(const BlockAttention& a, std::initializer_list<const HeadView*> views) {
+    const int size = a.dtype == GS_BF16 ? 2 : 4;
+    for (int ve = 16 / size; ve >= 4; ve /= 2) {
+        bool ok = a.head_dim % ve == 0;
+        for (const HeadView* v : views)
+            ok = ok && ((uintptr_t)v->data % (ve * size)) == 0 && (v->row_stride * size) % (ve * size) == 0 && (v->head_stride * size) % (ve * size) == 0;
+        if (ok) return ve;
+    }
+    return 1;
+}
+
+static void shape_groups(Attend& P, int ve, int nv, int64_t rows, int units_per_row, int64_t row_hint) {
+    const int pieces = (P.a.head_dim + ve * nv - 1) / (ve * nv);
+    P.tl = 1;
+    while (P.tl < pieces) P.tl *= 2;
+    P.units_per_row = units_per_row;
+    P.slots = 1;
+    // several groups share a row while the rows alone do not give every SM sixteen warps and each group keeps four edges
+    while (P.tl * P.slots * 2 <= 32 && rows * units_per_row * P.tl * P.slots * 2 <= sm_count() * 16 * 32 && (row_hint == 0 || row_hint >= 8 * P.slots)) P.slots *= 2;
+}
+
+enum AttendKind { AT_FORWARD, AT_DQ, AT_DKV };
+
+template <AttendKind K, typename T, int VE, int NV, int G> static void run_attend(Attend P, int64_t rows, int64_t row_hint, cudaStream_t s) {
+    constexpr int U = VE * NV * G >= 32 ? 2 : 4;
+    const int units_per_row = K == AT_DKV ? P.a.kv_heads : P.a.q_heads / G;
+    for (int pass = 0; pass < (P.split ? 2 : 1); ++pass) {
+        P.chunk_mode = pass;
+        const int64_t n = pass ? 2 * ((int64_t)P.edge_bound / AT_CHUNK) + 2 : rows;
+        shape_groups(P, VE, NV, n, units_per_row, pass ? AT_CHUNK : row_hint);
+        const int per_block = AT_THREADS / (P.tl * P.slots);
+        int64_t blocks = (n * units_per_row + per_block - 1) / per_block;
+        const int64_t cap = sm_count() * (pass ? 16 : 64);
+        if (blocks > cap) blocks = cap;
+        const int grid = (int)limit_grid(blocks);
+        if constexpr (K == AT_FORWARD) k_attend_forward<T, VE, NV, G, U><<<grid, AT_THREADS, 0, s>>>(P);
+        else if constexpr (K == AT_DQ) k_attend_dq<T, VE, NV, G, U><<<grid, AT_THREADS, 0, s>>>(P);
+        else k_attend_dkv<T, VE, NV, G, (G > 1 ? (U > 2 ? 2 : 1) : U)><<<grid, AT_THREADS, 0, s>>>(P);
+        count_launches(1);
+    }
+    if (P.split) {
+        const int grid = (int)limit_grid(sm_count() * 2);
+        if constexpr (K == AT_FORWARD) k_attend_forward_join<T><<<grid, AT_THREADS, 0, s>>>(P);
+        else k_attend_sum_join<T, K == AT_DKV><<<grid, AT_THREADS, 0, s>>>(P);
+        count_launches(1);
+    }
+}
+
+// Query heads of one key/value head that a group takes together (they share the loads of k and v).
+template <AttendKind K, typename T, int VE, int NV> static void run_group(const Attend& P, int64_t rows, int64_t row_hint, cudaStream_t s) {
+    const int group = P.a.q_heads / P.a.kv_heads;
+    if constexpr (VE * (int)sizeof(T) == 16) {
+        if (group % 4 == 0) return run_attend<K, T, VE, NV, 4>(P, rows, row_hint, s);
+        if (group % 2 == 0) return run_attend<K, T, VE, NV, 2>(P, rows, row_hint, s);
+    }
+    run_attend<K, T, VE, NV, 1>(P, rows, row_hint, s);
+}
+
+template <AttendKind K> static cudaError_t run_kind(Attend& P, int ve, int64_t rows, int64_t row_hint, cudaStream_t s) {
+    const int D = P.a.head_dim;
+    if (P.split) {
+        const cudaError_t e = cudaMemsetAsync(P.words, 0, 8, s);
+        if (e != cudaSuccess) return e;
+    }
+    if (P.a.dtype == GS_BF16) {
+        if (ve == 8) run_group<K, bf16, 8, 1>(P, rows, row_hint, s);
+        else if (ve == 4 && D <= 128) run_group<K, bf16, 4, 1>(P, rows, row_hint, s);
+        else if (ve == 4) run_group<K, bf16, 4, 2>(P, rows, row_hint, s);
+        else if (D <= 32) run_group<K, bf16, 1, 1>(P, rows, row_hint, s);
+        else if (D <= 64) run_group<K, bf16, 1, 2>(P, rows, row_hint, s);
+        else if (D <= 128) run_group<K, bf16, 1, 4>(P, rows, row_hint, s);
+        else run_group<K, bf16, 1, 8>(P, rows, row_hint, s);
+    } else {
+        if (ve == 4 && D <= 128) run_group<K, float, 4, 1>(P, rows, row_hint, s);
+        else if (ve == 4) run_group<K, float, 4, 2>(P, rows, row_hint, s);
+        else if (D <= 32) run_group<K, float, 1, 1>(P, rows, row_hint, s);
+        else if (D <= 64) run_group<K, float, 1, 2>(P, rows, row_hint, s);
+        else if (D <= 128) run_group<K, float, 1, 4>(P, rows, row_hint, s);
+        else run_group<K, float, 1, 8>(P, rows, row_hint, s);
+    }
+    return cudaGetLastError();
+}
+
+static Attend attend_params(const BlockAttention& a, void* workspace) {
+    Attend P{};
+    P.a = a;
+    P.edge_bound = a.edge_bound;
+    const AttendLayout l = attend_layout(a.dst.bound, a.edge_bound, a.q_heads, a.head_dim);
+    char* ws = (char*)workspace;
+    P.words = (int32_t*)(ws + l.words);
+    P.items = (int2*)(ws + l.items);
+    P.longs = (int4*)(ws + l.longs);
+    P.partial = (float*)(ws + l.partial);
+    P.stat = (float2*)(ws + l.stat);
+    return P;
+}
+
+cudaError_t launch_attention_forward(const BlockAttention& a, void* workspace, cudaStream_t s) {
+    Attend P = attend_params(a, workspace);
+    P.starts = a.indptr;
+    P.cols = a.indices;
+    P.rows = a.dst;
+    P.columns = a.src;
+    P.split = (a.max_row == 0 || a.max_row > AT_CHUNK) && a.edge_bound > AT_CHUNK;
+    return run_kind<AT_FORWARD>(P, wide_elems(a, {&a.q, &a.k, &a.v, &a.out}), a.dst.bound, a.max_row, s);
+}
+
+cudaError_t launch_attention_backward(const BlockAttention& a, const int32_t* rev_indptr, const int32_t* rev_dst, void* workspace, cudaStream_t s) {
+    Attend P = attend_params(a, workspace);
+    const int ve = wide_elems(a, {&a.q, &a.k, &a.v, &a.out, &a.dout, &a.dq, &a.dk, &a.dv});
+    P.starts = a.indptr;
+    P.cols = a.indices;
+    P.rows = a.dst;
+    P.columns = a.src;
+    P.split = (a.max_row == 0 || a.max_row > AT_CHUNK) && a.edge_bound > AT_CHUNK;
+    cudaError_t e = run_kind<AT_DQ>(P, ve, a.dst.bound, a.max_row, s);
+    if (e != cudaSuccess) return e;
+    P.starts = rev_indptr;
+    P.cols = rev_dst;
+    P.rows = a.src;
+    P.columns = a.dst;
+    P.split = a.edge_bound > AT_CHUNK;
+    return run_kind<AT_DKV>(P, ve, a.src.bound, 0, s);
+}
+
+cudaError_t launch_block_reverse(const int32_t* indptr, const int32_t* indices, Count dst, Count src, Count edges, int32_t* rev_indptr,
+                                 int32_t* rev_dst, void* workspace, cudaStream_t s) {
+    int32_t* rows = (int32_t*)workspace;
+    int64_t blocks = ((int64_t)dst.bound + AT_THREADS / 32 - 1) / (AT_THREADS / 32);
+    if (blocks > sm_count() * 32) blocks = sm_count() * 32;
+    k_edge_rows<<<(int)limit_grid(blocks), AT_THREADS, 0, s>>>(indptr, dst, edges.bound, rows);
+    count_launches(1);
+    const unsigned long long* sorted = nullptr;
+    cudaError_t e = launch_key_sort(indices, rows, edges, src.bound, (char*)workspace + align_up((size_t)edges.bound * 4, 256), &sorted, s);
+    if (e != cudaSuccess) return e;
+    e = launch_row_starts(sorted, edges, src, rev_indptr, s);
+    if (e != cudaSuccess) return e;
+    return launch_payloads(sorted, edges, rev_dst, s);
+}
+
+}  // namespace gs

@@ -54,4 +54,27 @@ struct EmbedGrad {
 size_t embedding_workspace(int64_t n_bound, int64_t table_rows, int32_t dim);
 cudaError_t launch_embedding_grad(const EmbedGrad& p, void* workspace, cudaStream_t s);
 
+// ---- attention over a block ----
+struct HeadView {           // [rows][heads][head_dim], strides in elements, the last one 1
+    void* data;
+    int64_t row_stride, head_stride;
+};
+struct BlockAttention {
+    const int32_t* indptr;
+    const int32_t* indices;
+    Count dst, src;
+    int32_t edge_bound, max_row;
+    gs_dtype dtype;
+    int32_t q_heads, kv_heads, head_dim;
+    float scale;
+    HeadView q, k, v, out, dout, dq, dk, dv;
+    float* lse;             // [dst][q_heads]
+};
+size_t attention_workspace(int64_t dst, int64_t edges, int32_t q_heads, int32_t head_dim);
+size_t reverse_workspace(int64_t edges);
+cudaError_t launch_attention_forward(const BlockAttention& a, void* workspace, cudaStream_t s);
+cudaError_t launch_attention_backward(const BlockAttention& a, const int32_t* rev_indptr, const int32_t* rev_dst, void* workspace, cudaStream_t s);
+cudaError_t launch_block_reverse(const int32_t* indptr, const int32_t* indices, Count dst, Count src, Count edges, int32_t* rev_indptr,
+                                 int32_t* rev_dst, void* workspace, cudaStream_t s);
+
 }  // namespace gs

@@ -52,6 +52,50 @@ gs_status embedding_grad(EmbedGrad g, bool sparse, void* ws, size_t ws_bytes, cu
     return GS_OK;
 }
 
+gs_status check_block(const gs_block* b) {
+    if (!b) return set_error(GS_ERR_ARG, "block is NULL");
+    if (b->max_dst < 0 || b->max_src < 0 || b->max_edges < 0 || b->max_edges >= (1 << 30)) return set_error(GS_ERR_ARG, "a size of the block is out of range");
+    if (!b->d_indptr || (b->max_edges > 0 && !b->d_indices)) return set_error(GS_ERR_ARG, "the block has no arrays");
+    const int given = (b->d_num_dst != nullptr) + (b->d_num_src != nullptr) + (b->d_num_edges != nullptr);
+    if (given != 0 && given != 3) return set_error(GS_ERR_ARG, "the block's device counts are given all together or not at all");
+    if (!aligned_to(b->d_indptr, 4) || !aligned_to(b->d_indices, 4) || !aligned_to(b->d_num_dst, 4) || !aligned_to(b->d_num_src, 4) || !aligned_to(b->d_num_edges, 4))
+        return set_error(GS_ERR_ALIGN, "misaligned block array");
+    return GS_OK;
+}
+
+gs_status check_heads(const char* name, const gs_heads* h, int64_t rows, int32_t heads, int32_t dim, gs_dtype t, HeadView* out) {
+    if (!h || (!h->d_data && rows > 0)) return set_error(GS_ERR_ARG, "%s is NULL", name);
+    if ((heads > 1 && h->head_stride < dim) || (rows > 1 && h->row_stride < dim)) return set_error(GS_ERR_ARG, "%s: a stride is smaller than head_dim", name);
+    if (!aligned_to(h->d_data, size_of(t))) return set_error(GS_ERR_ALIGN, "%s is misaligned", name);
+    *out = HeadView{h->d_data, h->row_stride, h->head_stride};
+    return GS_OK;
+}
+
+#define GS_TRY(call)                          \
+    do {                                      \
+        const gs_status s__ = (call);         \
+        if (s__ != GS_OK) return s__;         \
+    } while (0)
+
+gs_status check_attention(const gs_block* b, int32_t max_row, gs_dtype t, int32_t q_heads, int32_t kv_heads, int32_t dim, BlockAttention* a) {
+    GS_TRY(check_block(b));
+    if (!known(t)) return set_error(GS_ERR_ARG, "unknown dtype %d", (int)t);
+    if (max_row < 0) return set_error(GS_ERR_ARG, "max_row is negative");
+    if (dim < 1 || dim > 256) return set_error(GS_ERR_ARG, "head_dim %d outside [1, 256]", dim);
+    if (q_heads < 1 || q_heads > 1024 || kv_heads < 1 || q_heads % kv_heads) return set_error(GS_ERR_ARG, "q_heads %d, kv_heads %d: 1 to 1024, the second a divisor of the first", q_heads, kv_heads);
+    a->indptr = b->d_indptr;
+    a->indices = b->d_indices;
+    a->dst = Count{b->d_num_dst, b->max_dst};
+    a->src = Count{b->d_num_src, b->max_src};
+    a->edge_bound = b->max_edges;
+    a->max_row = max_row;
+    a->dtype = t;
+    a->q_heads = q_heads;
+    a->kv_heads = kv_heads;
+    a->head_dim = dim;
+    return GS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -98,6 +142,72 @@ gs_status gs_embedding_backward_sparse(const void* d_dout, gs_dtype dout_dtype, 
     EmbedGrad g{d_dout, d_grad, d_ids, Count{d_count_or_null, count_bound}, table_rows, dout_ld, grad_ld, dim,
                 dout_dtype, grad_dtype, scale, d_rows, d_num_rows};
     return embedding_grad(g, true, d_workspace, workspace_bytes, (cudaStream_t)stream);
+}
+
+gs_status gs_block_attention_workspace_bytes(int32_t max_dst, int32_t max_edges, int32_t q_heads, int32_t head_dim, size_t* bytes) {
+    if (!bytes) return set_error(GS_ERR_ARG, "bytes is NULL");
+    if (max_dst < 0 || max_edges < 0 || max_edges >= (1 << 30)) return set_error(GS_ERR_ARG, "a size of the block is out of range");
+    if (q_heads < 1 || q_heads > 1024 || head_dim < 1 || head_dim > 256) return set_error(GS_ERR_ARG, "q_heads outside [1, 1024] or head_dim outside [1, 256]");
+    *bytes = attention_workspace(max_dst, max_edges, q_heads, head_dim);
+    return GS_OK;
+}
+
+gs_status gs_block_attention_forward(const gs_block* block, int32_t max_row, gs_dtype dtype, int32_t q_heads, int32_t kv_heads,
+                                     int32_t head_dim, float scale, const gs_heads* q, const gs_heads* k, const gs_heads* v,
+                                     const gs_heads* out, float* d_lse, void* d_workspace, size_t workspace_bytes, void* stream) {
+    BlockAttention a{};
+    GS_TRY(check_attention(block, max_row, dtype, q_heads, kv_heads, head_dim, &a));
+    a.scale = scale;
+    GS_TRY(check_heads("q", q, block->max_dst, q_heads, head_dim, dtype, &a.q));
+    GS_TRY(check_heads("k", k, block->max_src, kv_heads, head_dim, dtype, &a.k));
+    GS_TRY(check_heads("v", v, block->max_src, kv_heads, head_dim, dtype, &a.v));
+    GS_TRY(check_heads("out", out, block->max_dst, q_heads, head_dim, dtype, &a.out));
+    if (block->max_dst == 0) return GS_OK;
+    if (!d_lse) return set_error(GS_ERR_ARG, "d_lse is NULL");
+    if (!aligned_to(d_lse, 4)) return set_error(GS_ERR_ALIGN, "d_lse is misaligned");
+    a.lse = d_lse;
+    GS_TRY(check_workspace(d_workspace, workspace_bytes, attention_workspace(block->max_dst, block->max_edges, q_heads, head_dim)));
+    GS_TRAIN_CUDA(launch_attention_forward(a, d_workspace, (cudaStream_t)stream));
+    return GS_OK;
+}
+
+gs_status gs_block_reverse(const gs_block* block, int32_t* d_rev_indptr, int32_t* d_rev_dst, void* d_workspace,
+                           size_t workspace_bytes, void* stream) {
+    GS_TRY(check_block(block));
+    if (!d_rev_indptr || (!d_rev_dst && block->max_edges > 0)) return set_error(GS_ERR_ARG, "NULL argument");
+    if (!aligned_to(d_rev_indptr, 4) || !aligned_to(d_rev_dst, 4)) return set_error(GS_ERR_ALIGN, "misaligned argument");
+    if (block->max_src == ((int32_t)0x7FFFFFFF)) return set_error(GS_ERR_ARG, "a size of the block is out of range");
+    GS_TRY(check_workspace(d_workspace, workspace_bytes, reverse_workspace(block->max_edges)));
+    // without a device count the edges end where the last row does
+    const int32_t* d_edges = block->d_num_edges ? block->d_num_edges : block->d_indptr + block->max_dst;
+    GS_TRAIN_CUDA(launch_block_reverse(block->d_indptr, block->d_indices, Count{block->d_num_dst, block->max_dst},
+                                       Count{block->d_num_src, block->max_src}, Count{d_edges, block->max_edges}, d_rev_indptr, d_rev_dst,
+                                       d_workspace, (cudaStream_t)stream));
+    return GS_OK;
+}
+
+gs_status gs_block_attention_backward(const gs_block* block, int32_t max_row, const int32_t* d_rev_indptr, const int32_t* d_rev_dst,
+                                      gs_dtype dtype, int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale,
+                                      const gs_heads* q, const gs_heads* k, const gs_heads* v, const gs_heads* out,
+                                      const float* d_lse, const gs_heads* dout, const gs_heads* dq, const gs_heads* dk,
+                                      const gs_heads* dv, void* d_workspace, size_t workspace_bytes, void* stream) {
+    BlockAttention a{};
+    GS_TRY(check_attention(block, max_row, dtype, q_heads, kv_heads, head_dim, &a));
+    a.scale = scale;
+    GS_TRY(check_heads("q", q, block->max_dst, q_heads, head_dim, dtype, &a.q));
+    GS_TRY(check_heads("k", k, block->max_src, kv_heads, head_dim, dtype, &a.k));
+    GS_TRY(check_heads("v", v, block->max_src, kv_heads, head_dim, dtype, &a.v));
+    GS_TRY(check_heads("out", out, block->max_dst, q_heads, head_dim, dtype, &a.out));
+    GS_TRY(check_heads("dout", dout, block->max_dst, q_heads, head_dim, dtype, &a.dout));
+    GS_TRY(check_heads("dq", dq, block->max_dst, q_heads, head_dim, dtype, &a.dq));
+    GS_TRY(check_heads("dk", dk, block->max_src, kv_heads, head_dim, dtype, &a.dk));
+    GS_TRY(check_heads("dv", dv, block->max_src, kv_heads, head_dim, dtype, &a.dv));
+    if (!d_rev_indptr || (!d_rev_dst && block->max_edges > 0) || (!d_lse && block->max_dst > 0)) return set_error(GS_ERR_ARG, "NULL argument");
+    if (!aligned_to(d_rev_indptr, 4) || !aligned_to(d_rev_dst, 4) || !aligned_to(d_lse, 4)) return set_error(GS_ERR_ALIGN, "misaligned argument");
+    a.lse = const_cast<float*>(d_lse);
+    GS_TRY(check_workspace(d_workspace, workspace_bytes, attention_workspace(block->max_dst, block->max_edges, q_heads, head_dim)));
+    GS_TRAIN_CUDA(launch_attention_backward(a, d_rev_indptr, d_rev_dst, d_workspace, (cudaStream_t)stream));
+    return GS_OK;
 }
 
 gs_status gs_train_status(void* stream) {
