@@ -527,6 +527,23 @@ gs_status gs_block_attention_backward(const gs_block* block, int32_t max_row, co
                                       const float* d_lse, const gs_heads* dout, const gs_heads* dq, const gs_heads* dk,
                                       const gs_heads* dv, void* d_workspace, size_t workspace_bytes, void* stream);
 
+/* Softmax cross entropy of `rows` hidden rows against every row of a table (classes, or all nodes of a graph),
+ * without keeping the logits z[n, v] = scale * <hidden[n], table[v]>:
+ *   lse[n] = log sum_v exp(z[n, v]),  loss[n] = lse[n] - z[n, labels[n]];  a label outside [0, vocab): loss 0, no gradient
+ * gs_xent_backward takes the upstream gradient dloss[n] and the forward's lse, recomputes the logits, and writes
+ *   dz = dloss[n] * scale * (exp(z - lse[n]) - [v == labels[n]]),  dhidden = dz table,  dtable = dz^T hidden
+ *   d_hidden [rows][hidden_ld], d_table [vocab][table_ld] of `dtype`; gradients of `grad_dtype`; loss, lse, dloss float[rows]
+ *   rows >= 0, 1 <= vocab < 2^31, 1 <= dim <= 4096
+ * f32 operands are multiplied in 32 bits.  Workspace: gs_xent_workspace_bytes, enough for either call. */
+gs_status gs_xent_workspace_bytes(int32_t rows, int64_t vocab, int32_t dim, gs_dtype dtype, size_t* bytes);
+gs_status gs_xent_forward(const void* d_hidden, int64_t hidden_ld, const void* d_table, int64_t table_ld, gs_dtype dtype,
+                          int32_t rows, int64_t vocab, int32_t dim, float scale, const int32_t* d_labels, float* d_loss,
+                          float* d_lse, void* d_workspace, size_t workspace_bytes, void* stream);
+gs_status gs_xent_backward(const void* d_hidden, int64_t hidden_ld, const void* d_table, int64_t table_ld, gs_dtype dtype,
+                           int32_t rows, int64_t vocab, int32_t dim, float scale, const int32_t* d_labels, const float* d_lse,
+                           const float* d_dloss, void* d_dhidden, int64_t dhidden_ld, void* d_dtable, int64_t dtable_ld,
+                           gs_dtype grad_dtype, void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* Synchronises `stream`; GS_ERR_CUDA if a kernel of the training operators ever gave up one of its (bounded) waits. */
 gs_status gs_train_status(void* stream);
 

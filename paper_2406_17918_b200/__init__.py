@@ -10,6 +10,7 @@ from .binding import (  # noqa: F401
     gs_sample_batch_host, gs_sample_batch_noalloc, NOALLOC_SCRATCH_BYTES, gs_batch_counts, gs_gather_features, gs_cache_read_rows, gs_gather_rows, gs_gather_rows_peer, gs_shard_bucket, gs_shard_workspace_bytes, gs_shard_sample_rows, gs_shard_status, gs_shard_extend, gs_shard_merge, gs_shard_fan_out, gs_gather_status,
     gs_cache_export, gs_cache_import, gs_sync_status, gs_batch_stats, gs_cache_profile_begin, gs_cache_profile_end, gs_cache_set_tuning, gs_debug_set_grid_cap, gs_kernel_launches, gs_alu_ceiling, gs_cache_set_dedup, GS_DEDUP_DIRECT, GS_DEDUP_HASH, GS_DEDUP_SORT, GS_DEDUP_AUTO,
     gs_embedding_lookup, gs_embedding_workspace_bytes, gs_embedding_backward, gs_embedding_backward_sparse, gs_train_status,
+    gs_xent_workspace_bytes, gs_xent_forward, gs_xent_backward,
     gs_block_attention_workspace_bytes, gs_block_attention_forward, gs_block_reverse, gs_block_attention_backward,
     gs_last_error, gs_stats_word_offset, library_path, exported_symbols, COUNTS_READBACK_BYTES,
 )

@@ -118,6 +118,9 @@ def _load():
         "gs_embedding_backward_sparse": [vp, ctypes.c_int, i64, vp, vp, i32, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_int, i64,
                                          vp, sz, vp],
         "gs_train_status": [vp],
+        "gs_xent_workspace_bytes": [i32, i64, i32, ctypes.c_int, psz],
+        "gs_xent_forward": [vp, i64, vp, i64, ctypes.c_int, i32, i64, i32, ctypes.c_float, vp, vp, vp, vp, sz, vp],
+        "gs_xent_backward": [vp, i64, vp, i64, ctypes.c_int, i32, i64, i32, ctypes.c_float, vp, vp, vp, vp, i64, vp, i64, ctypes.c_int, vp, sz, vp],
         "gs_block_attention_workspace_bytes": [i32, i32, i32, i32, psz],
         "gs_block_attention_forward": [vp, i32, ctypes.c_int, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, sz, vp],
         "gs_block_reverse": [vp, vp, vp, vp, sz, vp],
@@ -824,6 +827,59 @@ def gs_block_attention_backward(indptr: torch.Tensor, indices: torch.Tensor, rev
                                           _heads(dq, "dq", b.max_dst, hq, d, t), _heads(dk, "dk", b.max_src, hk, d, t),
                                           _heads(dv, "dv", b.max_src, hk, d, t), _ptr(workspace), workspace.numel(), _stream(stream)))
     return dq, dk, dv
+
+
+def gs_xent_workspace_bytes(rows: int, vocab: int, dim: int, dtype: torch.dtype = torch.bfloat16) -> int:
+    out = ctypes.c_size_t()
+    _check(_L.gs_xent_workspace_bytes(int(rows), int(vocab), int(dim), _dtype(dtype), ctypes.byref(out)))
+    return out.value
+
+
+def _xent_args(hidden, table, labels):
+    _rows_2d(hidden, "hidden")
+    _rows_2d(table, "table")
+    _ids_1d(labels, "labels")
+    if hidden.dtype != table.dtype or hidden.shape[1] != table.shape[1]:
+        raise TypeError("hidden and table must have one dtype and one width")
+    if labels.numel() != hidden.shape[0]:
+        raise ValueError("one label per hidden row expected")
+
+
+def _f32_rows(t, what, n):
+    if t.dtype != torch.float32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous() or t.numel() < n:
+        raise TypeError("%s must be a contiguous float32 CUDA tensor with one entry per row" % what)
+    return t
+
+
+def gs_xent_forward(hidden: torch.Tensor, table: torch.Tensor, labels: torch.Tensor, workspace: torch.Tensor, scale: float = 1.0,
+                    loss: torch.Tensor = None, lse: torch.Tensor = None, stream=None):
+    """loss[n] = lse[n] - scale <hidden[n], table[labels[n]]>, lse over all rows of the table; labels outside it: loss 0."""
+    _xent_args(hidden, table, labels)
+    n = hidden.shape[0]
+    loss = torch.empty(n, dtype=torch.float32, device=hidden.device) if loss is None else _f32_rows(loss, "loss", n)
+    lse = torch.empty(n, dtype=torch.float32, device=hidden.device) if lse is None else _f32_rows(lse, "lse", n)
+    _check(_L.gs_xent_forward(_ptr(hidden), _ld(hidden), _ptr(table), _ld(table), _dtype(hidden.dtype), n, table.shape[0], hidden.shape[1],
+                              float(scale), _ptr(labels), _ptr(loss), _ptr(lse), _ptr(workspace), workspace.numel(), _stream(stream)))
+    return loss, lse
+
+
+def gs_xent_backward(hidden: torch.Tensor, table: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                     workspace: torch.Tensor, scale: float = 1.0, dhidden: torch.Tensor = None, dtable: torch.Tensor = None,
+                     out_dtype: torch.dtype = None, stream=None):
+    """Gradients of gs_xent_forward for the upstream gradient dloss (float32, one per row).  Returns (dhidden, dtable)."""
+    _xent_args(hidden, table, labels)
+    n, d = hidden.shape
+    _f32_rows(lse, "lse", n)
+    _f32_rows(dloss, "dloss", n)
+    t = out_dtype or hidden.dtype
+    dhidden = torch.empty((n, d), dtype=t, device=hidden.device) if dhidden is None else _rows_2d(dhidden, "dhidden")
+    dtable = torch.empty(tuple(table.shape), dtype=dhidden.dtype, device=hidden.device) if dtable is None else _rows_2d(dtable, "dtable")
+    if tuple(dhidden.shape) != (n, d) or dtable.shape != table.shape or dhidden.dtype != dtable.dtype:
+        raise ValueError("dhidden / dtable must have the shapes of hidden / table and one dtype")
+    _check(_L.gs_xent_backward(_ptr(hidden), _ld(hidden), _ptr(table), _ld(table), _dtype(hidden.dtype), n, table.shape[0], d, float(scale),
+                               _ptr(labels), _ptr(lse), _ptr(dloss), _ptr(dhidden), _ld(dhidden), _ptr(dtable), _ld(dtable),
+                               _dtype(dhidden.dtype), _ptr(workspace), workspace.numel(), _stream(stream)))
+    return dhidden, dtable
 
 
 def gs_train_status(stream=None):

@@ -1,5 +1,6 @@
 // Host-side descriptors of the training operators: embedding rows, attention over blocks, softmax over a table's rows.
 #pragma once
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -76,5 +77,35 @@ cudaError_t launch_attention_forward(const BlockAttention& a, void* workspace, c
 cudaError_t launch_attention_backward(const BlockAttention& a, const int32_t* rev_indptr, const int32_t* rev_dst, void* workspace, cudaStream_t s);
 cudaError_t launch_block_reverse(const int32_t* indptr, const int32_t* indices, Count dst, Count src, Count edges, int32_t* rev_indptr,
                                  int32_t* rev_dst, void* workspace, cudaStream_t s);
+
+// ---- softmax cross entropy against every row of a table ----
+struct Xent {
+    const void* hidden;
+    const void* table;
+    int64_t hidden_ld, table_ld, vocab;
+    gs_dtype dtype;
+    int32_t rows, dim;
+    float scale;
+    const int32_t* labels;
+    float* loss;            // forward
+    float* lse_out;
+    const float* lse;       // backward
+    const float* dloss;
+    void* dhidden;
+    void* dtable;
+    int64_t dhidden_ld, dtable_ld;
+    gs_dtype grad_dtype;
+#ifdef __CUDACC__
+    __device__ void store(void* to, int64_t at, float x) const {
+        if (grad_dtype == GS_BF16) static_cast<__nv_bfloat16*>(to)[at] = __float2bfloat16_rn(x);
+        else static_cast<float*>(to)[at] = x;
+    }
+    __device__ void store_dhidden(int64_t r, int c, float x) const { store(dhidden, r * dhidden_ld + c, x); }
+    __device__ void store_dtable(int64_t r, int c, float x) const { store(dtable, r * dtable_ld + c, x); }
+#endif
+};
+size_t xent_workspace(const Xent& a);      // sizes and dtype only
+cudaError_t launch_xent_forward(const Xent& a, void* workspace, cudaStream_t s);
+cudaError_t launch_xent_backward(const Xent& a, void* workspace, cudaStream_t s);
 
 }  // namespace gs

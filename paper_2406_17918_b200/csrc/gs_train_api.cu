@@ -96,6 +96,19 @@ gs_status check_attention(const gs_block* b, int32_t max_row, gs_dtype t, int32_
     return GS_OK;
 }
 
+gs_status check_xent(const Xent& a, const void* ws, size_t ws_bytes) {
+    if (!known(a.dtype)) return set_error(GS_ERR_ARG, "unknown dtype %d", (int)a.dtype);
+    if (a.rows < 0) return set_error(GS_ERR_ARG, "rows is negative");
+    if (a.vocab < 1 || a.vocab >= ((int64_t)1 << 31)) return set_error(GS_ERR_ARG, "vocab outside [1, 2^31)");
+    if (a.dim < 1 || a.dim > 4096) return set_error(GS_ERR_ARG, "dim %d outside [1, 4096]", a.dim);
+    if (!a.table || (a.rows > 0 && (!a.hidden || !a.labels))) return set_error(GS_ERR_ARG, "NULL argument");
+    if (a.hidden_ld < a.dim || a.table_ld < a.dim) return set_error(GS_ERR_ARG, "a row pitch is smaller than dim");
+    if (!aligned_to(a.hidden, size_of(a.dtype)) || !aligned_to(a.table, size_of(a.dtype)) || !aligned_to(a.labels, 4))
+        return set_error(GS_ERR_ALIGN, "misaligned argument");
+    if (a.rows == 0) return GS_OK;
+    return check_workspace(ws, ws_bytes, xent_workspace(a));
+}
+
 }  // namespace
 
 extern "C" {
@@ -207,6 +220,54 @@ gs_status gs_block_attention_backward(const gs_block* block, int32_t max_row, co
     a.lse = const_cast<float*>(d_lse);
     GS_TRY(check_workspace(d_workspace, workspace_bytes, attention_workspace(block->max_dst, block->max_edges, q_heads, head_dim)));
     GS_TRAIN_CUDA(launch_attention_backward(a, d_rev_indptr, d_rev_dst, d_workspace, (cudaStream_t)stream));
+    return GS_OK;
+}
+
+gs_status gs_xent_workspace_bytes(int32_t rows, int64_t vocab, int32_t dim, gs_dtype dtype, size_t* bytes) {
+    if (!bytes) return set_error(GS_ERR_ARG, "bytes is NULL");
+    if (!known(dtype) || rows < 0 || vocab < 1 || vocab >= ((int64_t)1 << 31) || dim < 1 || dim > 4096) return set_error(GS_ERR_ARG, "a size or the dtype is out of range");
+    Xent a{};
+    a.rows = rows;
+    a.vocab = vocab;
+    a.dim = dim;
+    a.dtype = dtype;
+    *bytes = xent_workspace(a);
+    return GS_OK;
+}
+
+gs_status gs_xent_forward(const void* d_hidden, int64_t hidden_ld, const void* d_table, int64_t table_ld, gs_dtype dtype,
+                          int32_t rows, int64_t vocab, int32_t dim, float scale, const int32_t* d_labels, float* d_loss,
+                          float* d_lse, void* d_workspace, size_t workspace_bytes, void* stream) {
+    Xent a{};
+    a.hidden = d_hidden; a.hidden_ld = hidden_ld; a.table = d_table; a.table_ld = table_ld; a.dtype = dtype;
+    a.rows = rows; a.vocab = vocab; a.dim = dim; a.scale = scale; a.labels = d_labels; a.loss = d_loss; a.lse_out = d_lse;
+    GS_TRY(check_xent(a, d_workspace, workspace_bytes));
+    if (rows == 0) return GS_OK;
+    if (!d_loss || !d_lse) return set_error(GS_ERR_ARG, "NULL argument");
+    if (!aligned_to(d_loss, 4) || !aligned_to(d_lse, 4)) return set_error(GS_ERR_ALIGN, "misaligned argument");
+    GS_TRAIN_CUDA(launch_xent_forward(a, d_workspace, (cudaStream_t)stream));
+    return GS_OK;
+}
+
+gs_status gs_xent_backward(const void* d_hidden, int64_t hidden_ld, const void* d_table, int64_t table_ld, gs_dtype dtype,
+                           int32_t rows, int64_t vocab, int32_t dim, float scale, const int32_t* d_labels, const float* d_lse,
+                           const float* d_dloss, void* d_dhidden, int64_t dhidden_ld, void* d_dtable, int64_t dtable_ld,
+                           gs_dtype grad_dtype, void* d_workspace, size_t workspace_bytes, void* stream) {
+    Xent a{};
+    a.hidden = d_hidden; a.hidden_ld = hidden_ld; a.table = d_table; a.table_ld = table_ld; a.dtype = dtype;
+    a.rows = rows; a.vocab = vocab; a.dim = dim; a.scale = scale; a.labels = d_labels; a.lse = d_lse; a.dloss = d_dloss;
+    a.dhidden = d_dhidden; a.dhidden_ld = dhidden_ld; a.dtable = d_dtable; a.dtable_ld = dtable_ld; a.grad_dtype = grad_dtype;
+    GS_TRY(check_xent(a, d_workspace, workspace_bytes));
+    if (!known(grad_dtype)) return set_error(GS_ERR_ARG, "unknown dtype %d", (int)grad_dtype);
+    if (!d_dtable || (rows > 0 && (!d_dhidden || !d_lse || !d_dloss))) return set_error(GS_ERR_ARG, "NULL argument");
+    if (dhidden_ld < dim || dtable_ld < dim) return set_error(GS_ERR_ARG, "a row pitch is smaller than dim");
+    if (!aligned_to(d_dhidden, size_of(grad_dtype)) || !aligned_to(d_dtable, size_of(grad_dtype)) || !aligned_to(d_lse, 4) || !aligned_to(d_dloss, 4))
+        return set_error(GS_ERR_ALIGN, "misaligned argument");
+    if (rows == 0) {
+        GS_TRAIN_CUDA(cudaMemset2DAsync(d_dtable, (size_t)dtable_ld * size_of(grad_dtype), 0, (size_t)dim * size_of(grad_dtype), (size_t)vocab, (cudaStream_t)stream));
+        return GS_OK;
+    }
+    GS_TRAIN_CUDA(launch_xent_backward(a, d_workspace, (cudaStream_t)stream));
     return GS_OK;
 }
 

@@ -1,0 +1,32 @@
+// How the softmax-over-a-table kernels divide their work.
+#pragma once
+#include <stdint.h>
+
+namespace gs {
+
+// A grid of tiles_x by tiles_y output tiles, walked with y fastest, cut into `parts` equal runs: run c covers the
+// tiles [start(c), start(c + 1)) of the flattened grid.  A run that does not hold a whole row of tiles leaves a
+// partial result for that row: the run that starts inside row i in slot 2c, a run that starts at or before row i
+// and ends inside it in slot 2c + 1.
+struct Runs {
+    int64_t tiles_x, tiles_y, parts;
+    __host__ __device__ int64_t total() const { return tiles_x * tiles_y; }
+    __host__ __device__ int64_t start(int64_t c) const { return total() * c / parts; }
+    // The run that holds flattened tile t.
+    __host__ __device__ int64_t run_of(int64_t t) const {
+        int64_t c = t * parts / total();
+        while (c + 1 < parts && start(c + 1) <= t) ++c;
+        while (c > 0 && start(c) > t) --c;
+        return c;
+    }
+    __host__ __device__ int64_t slot(int64_t c, int64_t row) const { return start(c) > row * tiles_y ? 2 * c : 2 * c + 1; }
+};
+
+inline Runs make_runs(int64_t x, int64_t tile_x, int64_t y, int64_t tile_y, int64_t parts) {
+    Runs r{(x + tile_x - 1) / tile_x, (y + tile_y - 1) / tile_y, parts};
+    if (r.parts > r.total()) r.parts = r.total();
+    if (r.parts < 1) r.parts = 1;
+    return r;
+}
+
+}  // namespace gs
