@@ -533,8 +533,9 @@ gs_status gs_block_attention_backward(const gs_block* block, int32_t max_row, co
  * gs_xent_backward takes the upstream gradient dloss[n] and the forward's lse, recomputes the logits, and writes
  *   dz = dloss[n] * scale * (exp(z - lse[n]) - [v == labels[n]]),  dhidden = dz table,  dtable = dz^T hidden
  *   d_hidden [rows][hidden_ld], d_table [vocab][table_ld] of `dtype`; gradients of `grad_dtype`; loss, lse, dloss float[rows]
- *   rows >= 0, 1 <= vocab < 2^31, 1 <= dim <= 4096
- * f32 operands are multiplied in 32 bits.  Workspace: gs_xent_workspace_bytes, enough for either call. */
+ *   0 <= rows < 2^31 - 256, 1 <= vocab < 2^31 - 256, 1 <= dim <= 4096
+ * f32 operands are multiplied in 32 bits.  bf16 operands with dim <= 256 (and, where dim is a multiple of 8, bases and
+ * pitches on 16 bytes) use the tensor cores: f32 sums, and dz rounded to bf16 for the second product.  Workspace: gs_xent_workspace_bytes, enough for either call. */
 gs_status gs_xent_workspace_bytes(int32_t rows, int64_t vocab, int32_t dim, gs_dtype dtype, size_t* bytes);
 gs_status gs_xent_forward(const void* d_hidden, int64_t hidden_ld, const void* d_table, int64_t table_ld, gs_dtype dtype,
                           int32_t rows, int64_t vocab, int32_t dim, float scale, const int32_t* d_labels, float* d_loss,

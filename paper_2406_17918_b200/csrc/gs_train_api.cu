@@ -1,5 +1,6 @@
 // The C ABI of the training operators: argument checks and launches.
 #include "gs_train.h"
+#include "gs_xent.h"
 
 using namespace gs;
 
@@ -7,6 +8,7 @@ namespace {
 
 bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 bool known(gs_dtype t) { return t == GS_F32 || t == GS_BF16; }
+constexpr int64_t XENT_MAX_VOCAB = ((int64_t)1 << 31) - 257;   // row numbers of whole tiles stay below 2^31
 size_t size_of(gs_dtype t) { return t == GS_BF16 ? 2 : 4; }
 
 gs_status cuda_error(cudaError_t e, const char* what) { return set_error(GS_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e)); }
@@ -98,8 +100,8 @@ gs_status check_attention(const gs_block* b, int32_t max_row, gs_dtype t, int32_
 
 gs_status check_xent(const Xent& a, const void* ws, size_t ws_bytes) {
     if (!known(a.dtype)) return set_error(GS_ERR_ARG, "unknown dtype %d", (int)a.dtype);
-    if (a.rows < 0) return set_error(GS_ERR_ARG, "rows is negative");
-    if (a.vocab < 1 || a.vocab >= ((int64_t)1 << 31)) return set_error(GS_ERR_ARG, "vocab outside [1, 2^31)");
+    if (a.rows < 0 || a.rows > XENT_MAX_VOCAB) return set_error(GS_ERR_ARG, "rows outside [0, 2^31 - 256)");
+    if (a.vocab < 1 || a.vocab > XENT_MAX_VOCAB) return set_error(GS_ERR_ARG, "vocab outside [1, 2^31 - 256)");
     if (a.dim < 1 || a.dim > 4096) return set_error(GS_ERR_ARG, "dim %d outside [1, 4096]", a.dim);
     if (!a.table || (a.rows > 0 && (!a.hidden || !a.labels))) return set_error(GS_ERR_ARG, "NULL argument");
     if (a.hidden_ld < a.dim || a.table_ld < a.dim) return set_error(GS_ERR_ARG, "a row pitch is smaller than dim");
@@ -225,7 +227,7 @@ gs_status gs_block_attention_backward(const gs_block* block, int32_t max_row, co
 
 gs_status gs_xent_workspace_bytes(int32_t rows, int64_t vocab, int32_t dim, gs_dtype dtype, size_t* bytes) {
     if (!bytes) return set_error(GS_ERR_ARG, "bytes is NULL");
-    if (!known(dtype) || rows < 0 || vocab < 1 || vocab >= ((int64_t)1 << 31) || dim < 1 || dim > 4096) return set_error(GS_ERR_ARG, "a size or the dtype is out of range");
+    if (!known(dtype) || rows < 0 || vocab < 1 || vocab > XENT_MAX_VOCAB || dim < 1 || dim > 4096) return set_error(GS_ERR_ARG, "a size or the dtype is out of range");
     Xent a{};
     a.rows = rows;
     a.vocab = vocab;
@@ -275,6 +277,9 @@ gs_status gs_train_status(void* stream) {
     int sort = 0;
     GS_TRAIN_CUDA(train_gave_up((cudaStream_t)stream, &sort));
     if (sort) return set_error(GS_ERR_CUDA, "a sort gave up waiting for an earlier tile");
+    int xent = 0;
+    GS_TRAIN_CUDA(xent_gave_up((cudaStream_t)stream, &xent));
+    if (xent) return set_error(GS_ERR_CUDA, "a softmax kernel gave up waiting for a copy or a product");
     return GS_OK;
 }
 

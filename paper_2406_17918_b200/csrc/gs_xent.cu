@@ -6,8 +6,9 @@
 // time.  The backward pass recomputes them from lse, once for dh (a tile of hidden rows stays, the table streams by)
 // and once for dw (a tile of table rows stays, the hidden rows stream by): 8 N V d operations, no atomics.
 //
-// k_xent_simt serves both directions: x are the rows that stay, y the rows that stream.  Products in 32 bits on
-// the CUDA cores: exact enough for f32 operands, which the tensor cores' types are not.
+// bf16 operands of up to 256 columns go to the tensor cores (gs_xent_tc.cu).  k_xent_simt takes the rest, f32 above
+// all, with products in 32 bits on the CUDA cores: exact enough for f32 operands, which the tensor cores' types are
+// not.  It serves both directions: x are the rows that stay, y the rows that stream.
 #include "gs_device.cuh"
 #include "gs_train.cuh"
 #include "gs_train.h"
@@ -189,13 +190,13 @@ __global__ void __launch_bounds__(XS_THREADS) k_xent_simt(const __grid_constant_
 }
 
 // lse and loss of every row from the runs' statistics.
-__global__ void __launch_bounds__(256) k_xent_finish(Xent a, Runs runs, int tile, const float2* __restrict__ stats, const float* __restrict__ picked) {
+__global__ void __launch_bounds__(256) k_xent_finish(Xent a, Runs runs, int tile, int per, const float2* __restrict__ stats, const float* __restrict__ picked) {
     for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < a.rows; n += (int64_t)gridDim.x * 256) {
         const int64_t i = n / tile;
         const int64_t c0 = runs.run_of(i * runs.tiles_y), c1 = runs.run_of((i + 1) * runs.tiles_y - 1);
         float m = -INFINITY, l = 0.f;
-        for (int64_t c = c0; c <= c1; ++c) {
-            const float2 s = stats[(c + i) * tile + n % tile];
+        for (int64_t c = (c0 + i) * per; c < (c1 + i + 1) * per; ++c) {      // `per` entries of a run, in order
+            const float2 s = stats[c * tile + n % tile];
             const float top = fmaxf(m, s.x), ref = top == -INFINITY ? 0.f : top;
             l = l * xe_exp2(m - ref) + s.y * xe_exp2(s.x - ref);
             m = top;
@@ -238,7 +239,10 @@ static size_t simt_workspace(const Xent& a) {
     return fwd > bwd ? fwd : bwd;
 }
 
-size_t xent_workspace(const Xent& a) { return align_up(simt_workspace(a), 256); }
+size_t xent_workspace(const Xent& a) {
+    const size_t simt = simt_workspace(a), tc = a.dtype == GS_BF16 && a.dim <= XENT_TC_MAX_DIM ? xent_tc_workspace(a) : 0;
+    return align_up(simt > tc ? simt : tc, 256);
+}
 
 template <typename T, XentMode M> static void run_simt(XentSimt& P, cudaStream_t s) {
     const int cols = M == XE_FORWARD ? 1 : (P.a.dim + XS_COLS - 1) / XS_COLS;
@@ -253,7 +257,24 @@ template <XentMode M> static void run_join(const Xent& a, const Runs& runs, int 
     count_launches(1);
 }
 
+cudaError_t launch_xent_join(const Xent& a, bool hidden, const Runs& runs, int tile, int pitch, const float* partial, cudaStream_t s) {
+    if (hidden) run_join<XE_DHIDDEN>(a, runs, tile, pitch, partial, s);
+    else run_join<XE_DTABLE>(a, runs, tile, pitch, partial, s);
+    return cudaGetLastError();
+}
+
 cudaError_t launch_xent_forward(const Xent& a, void* workspace, cudaStream_t s) {
+    const int64_t finish = limit_grid((a.rows + 255) / 256);
+    if (xent_tc_takes(a)) {
+        Runs runs;
+        const float2* stats;
+        const float* picked;
+        const cudaError_t e = launch_xent_tc_forward(a, workspace, &runs, &stats, &picked, s);
+        if (e != cudaSuccess) return e;
+        k_xent_finish<<<(int)finish, 256, 0, s>>>(a, runs, XENT_TC_TILE, 2, stats, picked);
+        count_launches(1);
+        return cudaGetLastError();
+    }
     XentSimt P{};
     P.a = a;
     P.runs = simt_runs(a.rows, a.vocab);
@@ -261,13 +282,13 @@ cudaError_t launch_xent_forward(const Xent& a, void* workspace, cudaStream_t s) 
     P.picked = (float*)((char*)workspace + align_up((size_t)(P.runs.parts + P.runs.tiles_x) * XS_TILE * 8, 256));
     if (a.dtype == GS_BF16) run_simt<bf16, XE_FORWARD>(P, s);
     else run_simt<float, XE_FORWARD>(P, s);
-    const int64_t blocks = (a.rows + 255) / 256;
-    k_xent_finish<<<(int)limit_grid(blocks), 256, 0, s>>>(a, P.runs, XS_TILE, P.stats, P.picked);
+    k_xent_finish<<<(int)finish, 256, 0, s>>>(a, P.runs, XS_TILE, 1, P.stats, P.picked);
     count_launches(1);
     return cudaGetLastError();
 }
 
 cudaError_t launch_xent_backward(const Xent& a, void* workspace, cudaStream_t s) {
+    if (xent_tc_takes(a)) return launch_xent_tc_backward(a, workspace, s);
     XentSimt P{};
     P.a = a;
     P.partial = (float*)workspace;

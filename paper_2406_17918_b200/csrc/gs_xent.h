@@ -1,5 +1,7 @@
 // How the softmax-over-a-table kernels divide their work.
 #pragma once
+#include <cuda_runtime.h>
+#include <stddef.h>
 #include <stdint.h>
 
 namespace gs {
@@ -28,5 +30,16 @@ inline Runs make_runs(int64_t x, int64_t tile_x, int64_t y, int64_t tile_y, int6
     if (r.parts < 1) r.parts = 1;
     return r;
 }
+
+constexpr int XENT_TC_TILE = 128;       // rows of either operand per tile of the tensor-core kernels
+constexpr int XENT_TC_MAX_DIM = 256;    // a gradient tile of 128 rows and S of two units fill the 512 columns of tensor memory
+
+struct Xent;
+bool xent_tc_takes(const Xent& a);
+size_t xent_tc_workspace(const Xent& a);
+cudaError_t launch_xent_tc_forward(const Xent& a, void* workspace, Runs* runs, const float2** stats, const float** picked, cudaStream_t s);
+cudaError_t launch_xent_tc_backward(const Xent& a, void* workspace, cudaStream_t s);
+cudaError_t launch_xent_join(const Xent& a, bool hidden, const Runs& runs, int tile, int pitch, const float* partial, cudaStream_t s);
+cudaError_t xent_gave_up(cudaStream_t s, int* h_flag);
 
 }  // namespace gs

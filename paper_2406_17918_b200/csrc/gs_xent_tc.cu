@@ -1,0 +1,575 @@
+// Softmax cross entropy against a table on the tensor cores: bf16 operands of up to 256 columns.
+//
+// A block keeps a tile of 128 rows of x in shared memory (hidden rows for the forward pass and dh, table rows for dw)
+// and lets tiles of 128 rows of y stream by (TMA, 128-byte swizzle).  Unit u of a block:
+//   S = X Y^T (tcgen05, 128 x 128, f32 in tensor memory)  ->  a softmax warpgroup turns S into statistics, or into
+//   Z = dz in bf16 that overwrites S in tensor memory     ->  O += Z Y, the same shared-memory tile of Y as the second
+// operand, read along its other dimension.  Rounding Z to bf16 costs 2^-9 of each term, about what the gradient's own
+// rounding to bf16 does.  Roles: one thread issues the loads, one the products, two warpgroups (one thread per row of x)
+// take the units alternately, so that S of unit u + 1 is multiplied while unit u is exponentiated.  The products of
+// unit u + 2 may overwrite S of unit u without a wait: they are issued after the product that read Z of unit u.
+// Work is cut into equal runs of units, one per SM; a row of tiles shared by runs is joined from f32 partials.
+#include <atomic>
+
+#include "gs_device.cuh"
+#include "gs_tc.cuh"
+#include "gs_train.cuh"
+#include "gs_train.h"
+#include "gs_xent.h"
+
+namespace gs {
+
+constexpr int XT = XENT_TC_TILE;
+constexpr int XT_THREADS = 384;            // 4 warps of roles, 2 softmax warpgroups
+constexpr int XT_CHUNK = XT * 128;         // bytes of a tile's 64 columns
+constexpr int XT_MAX_STAGES = 8;
+constexpr float XT_LOG2E = 1.4426950408889634f;
+
+__device__ int g_xent_gave_up;
+
+__device__ __forceinline__ float xt_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+struct XentTc {
+    Xent a;
+    Runs runs;
+    int nx, ny;
+    int chunks, ksteps, on;      // 64-column pieces of a row, 16-column steps, columns of O (a multiple of 16)
+    int stages, xbufs, obufs;
+    float2* stats;               // forward: [parts + tiles_x][2][XT]
+    float* picked;
+    float* partial;              // backward: [2 parts][XT][on]
+};
+
+// The block's runs, cut at rows of tiles.
+struct Segments {
+    const Runs& r;
+    int64_t run, t, end;
+    int step;
+    __device__ Segments(const Runs& runs, int first, int step_) : r(runs), run(first), step(step_) {
+        t = run < r.parts ? r.start(run) : 0;
+        end = run < r.parts ? r.start(run + 1) : 0;
+    }
+    // Next segment: row xi, tiles [y0, y0 + n) of it; false when the block is done.
+    __device__ bool next(int64_t& run_out, int64_t& xi, int& y0, int& n) {
+        while (t >= end) {
+            run += step;
+            if (run >= r.parts) return false;
+            t = r.start(run);
+            end = r.start(run + 1);
+        }
+        xi = t / r.tiles_y;
+        const int64_t last = (xi + 1) * r.tiles_y < end ? (xi + 1) * r.tiles_y : end;
+        y0 = (int)(t - xi * r.tiles_y);
+        n = (int)(last - t);
+        t = last;
+        run_out = run;
+        return true;
+    }
+};
+
+// 16 columns of a gradient row (fewer at its end), in 16-byte pieces where the address allows.
+__device__ __forceinline__ void store_columns(void* to, gs_dtype t, int64_t at, const float (&f)[16], int left) {
+    if (t == GS_BF16) {
+        bf16* p = static_cast<bf16*>(to) + at;
+        if (left >= 16 && ((uintptr_t)p & 15) == 0) return store_vec<bf16, 16>(p, f);
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (j < left) p[j] = from_f32<bf16>(f[j]);
+    } else {
+        float* p = static_cast<float*>(to) + at;
+        if (left >= 16 && ((uintptr_t)p & 15) == 0) return store_vec<float, 16>(p, f);
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (j < left) p[j] = f[j];
+    }
+}
+
+enum { TC_FORWARD = 0, TC_DHIDDEN = 1, TC_DTABLE = 2 };
+
+template <int M>
+__global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant__ XentTc P, const __grid_constant__ CUtensorMap xmap,
+                                                           const __grid_constant__ CUtensorMap ymap) {
+    extern __shared__ unsigned char tiles[];
+    __shared__ __align__(8) unsigned long long bars[2 * XT_MAX_STAGES + 17];
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile int s_stop;
+    constexpr int COLS = M == TC_DTABLE ? XT : 4;
+    __shared__ __align__(16) float col_lse[8][COLS], col_g[8][COLS];   // dw: of the unit's hidden rows, a copy per softmax warp
+    __shared__ __align__(16) int col_label[8][COLS];
+    constexpr int SBUFS = M == TC_FORWARD ? 4 : 2;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t tile_bytes = (uint32_t)P.chunks * XT_CHUNK;
+    const uint32_t xbase = (tc::smem_addr(tiles) + 1023) & ~1023u, ring = xbase + P.xbufs * tile_bytes;
+    const uint32_t b0 = tc::smem_addr(bars);
+    auto full = [&](int i) { return b0 + 8 * i; };
+    auto empty = [&](int i) { return b0 + 8 * (XT_MAX_STAGES + i); };
+    const uint32_t b1 = b0 + 16 * XT_MAX_STAGES;
+    auto s_full = [&](int i) { return b1 + 8 * i; };         // 4: S of a unit is in tensor memory
+    auto p_full = [&](int i) { return b1 + 32 + 8 * i; };    // 4: Z is written (forward: S may be overwritten)
+    auto x_full = [&](int i) { return b1 + 64 + 8 * i; };    // 2
+    auto x_free = [&](int i) { return b1 + 80 + 8 * i; };    // 2
+    auto o_full = [&](int i) { return b1 + 96 + 8 * i; };    // 2
+    auto o_free = [&](int i) { return b1 + 112 + 8 * i; };   // 2
+    const uint32_t drained = b1 + 128;
+
+    if (threadIdx.x == 0) {
+        s_stop = 0;
+        for (int i = 0; i < P.stages; ++i) {
+            tc::mbar_init(full(i), 1);
+            tc::mbar_init(empty(i), 1);
+        }
+        for (int i = 0; i < 4; ++i) {
+            tc::mbar_init(s_full(i), 1);
+            tc::mbar_init(p_full(i), 128);
+        }
+        for (int i = 0; i < 2; ++i) {
+            tc::mbar_init(x_full(i), 1);
+            tc::mbar_init(x_free(i), 1);
+            tc::mbar_init(o_full(i), 1);
+            tc::mbar_init(o_free(i), 256);
+        }
+        tc::mbar_init(drained, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 2) tc::tmem_alloc(tc::smem_addr(&s_tmem), 512);
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = s_tmem;
+    Segments seg(P.runs, blockIdx.x, gridDim.x);
+    int64_t run, xi;
+    int y0, n;
+
+    if (warp == 0) {
+        if (lane == 0) {                                   // ---- loads
+            int st = 0, issued = 0, segs = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            while (ok && seg.next(run, xi, y0, n)) {
+                const int xb = segs % P.xbufs;
+                if (segs >= P.xbufs) ok = tc::mbar_wait(x_free(xb), (uint32_t)(segs / P.xbufs - 1) & 1, &s_stop);
+                if (!ok) break;
+                tc::mbar_expect(x_full(xb), tile_bytes);
+                for (int c = 0; c < P.chunks; ++c) tc::tma_load(xbase + xb * tile_bytes + c * XT_CHUNK, &xmap, c * 64, (int)(xi * XT), x_full(xb));
+                ++segs;
+                for (int i = 0; i < n; ++i) {
+                    if (issued >= P.stages) ok = tc::mbar_wait(empty(st), ph ^ 1, &s_stop);
+                    if (!ok) break;
+                    tc::mbar_expect(full(st), tile_bytes);
+                    for (int c = 0; c < P.chunks; ++c) tc::tma_load(ring + st * tile_bytes + c * XT_CHUNK, &ymap, c * 64, (y0 + i) * XT, full(st));
+                    ++issued;
+                    if (++st == P.stages) {
+                        st = 0;
+                        ph ^= 1;
+                    }
+                }
+            }
+            if (!ok) atomicExch(&g_xent_gave_up, 1);
+            // no copy may be in flight when the block ends, whatever became of the other roles
+            const long long begin = clock64();
+            for (int j = issued > P.stages ? issued - P.stages : 0; j < issued; ++j)
+                while (!tc::mbar_try(full(j % P.stages), (uint32_t)(j / P.stages) & 1) && clock64() - begin < tc::WAIT_CLOCKS) {}
+            for (int j = segs > P.xbufs ? segs - P.xbufs : 0; j < segs; ++j)
+                while (!tc::mbar_try(x_full(j % P.xbufs), (uint32_t)(j / P.xbufs) & 1) && clock64() - begin < tc::WAIT_CLOCKS) {}
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {                                   // ---- products
+            const uint32_t si = tc::instruction(XT, false), oi = tc::instruction(P.on, true);
+            int st = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            int64_t u = 0;
+            // the unit whose second product is still to be issued
+            bool pending = false, p_first = false, p_last = false;
+            int p_st = 0, p_ob = 0, p_seg = 0;
+            auto second = [&](int64_t pu) {
+                const int b = (int)(pu & 1);
+                ok = ok && tc::mbar_wait(p_full(b), (uint32_t)(pu >> 1) & 1, &s_stop);
+                if (ok && p_first && p_seg >= P.obufs) ok = tc::mbar_wait(o_free(p_ob), (uint32_t)(p_seg / P.obufs - 1) & 1, &s_stop);
+                if (!ok) return;
+                tc::fence_after();
+                const uint32_t o = tmem + 256 + p_ob * 128, z = tmem + b * XT;
+                for (int k = 0; k < XT / 16; ++k)
+                    tc::mma_ts(o, z + k * 8, tc::operand(ring + p_st * tile_bytes + k * 2048, XT_CHUNK, 1024), oi, !(p_first && k == 0));
+                tc::commit(empty(p_st));
+                if (p_last) tc::commit(o_full(p_ob));
+                pending = false;
+            };
+            for (int s = 0; ok && seg.next(run, xi, y0, n); ++s) {
+                const int xb = s % P.xbufs;
+                ok = tc::mbar_wait(x_full(xb), (uint32_t)(s / P.xbufs) & 1, &s_stop);
+                for (int i = 0; i < n && ok; ++i, ++u) {
+                    ok = tc::mbar_wait(full(st), ph, &s_stop);
+                    const int b = (int)(u % SBUFS);
+                    if (M == TC_FORWARD && u >= SBUFS) ok = ok && tc::mbar_wait(p_full(b), (uint32_t)(u / SBUFS - 1) & 1, &s_stop);
+                    if (!ok) break;
+                    tc::fence_after();
+                    for (int k = 0; k < P.ksteps; ++k) {
+                        const uint32_t off = (k >> 2) * XT_CHUNK + (k & 3) * 32;
+                        tc::mma_ss(tmem + b * XT, tc::operand(xbase + xb * tile_bytes + off, 16, 1024), tc::operand(ring + st * tile_bytes + off, 16, 1024), si, k > 0);
+                    }
+                    tc::commit(s_full(b));
+                    if (i + 1 == n) tc::commit(x_free(xb));
+                    if (M == TC_FORWARD) {
+                        tc::commit(empty(st));
+                    } else {
+                        if (pending) second(u - 1);
+                        pending = true;
+                        p_first = i == 0;
+                        p_last = i + 1 == n;
+                        p_st = st;
+                        p_seg = s;
+                        p_ob = s % P.obufs;
+                    }
+                    if (++st == P.stages) {
+                        st = 0;
+                        ph ^= 1;
+                    }
+                }
+            }
+            if (M != TC_FORWARD && ok && pending) second(u - 1);
+            if (!ok) {
+                atomicExch(&g_xent_gave_up, 1);
+                // products already issued still write tensor memory: wait for them before it is freed
+                tc::commit(drained);
+                const long long begin = clock64();
+                while (!tc::mbar_try(drained, 0) && clock64() - begin < tc::WAIT_CLOCKS) {}
+            }
+        }
+    } else if (warp >= 4) {                                // ---- softmax
+        const int wg = (warp >> 2) - 1, sw = warp - 4, row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 lanes of tensor memory
+        const float c2 = P.a.scale * XT_LOG2E;
+        bool ok = true;
+        int64_t u = 0;
+        for (int s = 0; ok && seg.next(run, xi, y0, n); ++s) {
+            const int64_t x = xi * XT + row;
+            float lse2 = 0.f, m = -INFINITY, l = 0.f;
+            int label = -1;
+            if (M != TC_DTABLE && x < P.nx) {
+                const int lab = __ldg(P.a.labels + x);
+                label = lab >= 0 && lab < P.a.vocab ? lab : -1;
+                if (M == TC_DHIDDEN) lse2 = __ldg(P.a.lse + x) * XT_LOG2E;
+            }
+            for (int i = 0; i < n && ok; ++i, ++u) {
+                if ((int)(u & 1) != wg) continue;
+                const int b = (int)(u % SBUFS), ybase = (y0 + i) * XT;
+                if (M == TC_DTABLE) {                      // lse, upstream gradient and label of the unit's hidden rows
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int h = ybase + j * 32 + lane, lab = h < P.ny ? __ldg(P.a.labels + h) : -1;
+                        const bool valid = lab >= 0 && lab < P.a.vocab;
+                        col_label[sw][j * 32 + lane] = valid ? lab : -1;
+                        col_lse[sw][j * 32 + lane] = h < P.ny ? __ldg(P.a.lse + h) * XT_LOG2E : 0.f;
+                        col_g[sw][j * 32 + lane] = valid ? __ldg(P.a.dloss + h) * P.a.scale : 0.f;
+                    }
+                    __syncwarp();
+                }
+                ok = tc::mbar_wait(s_full(b), (uint32_t)(u / SBUFS) & 1, &s_stop);
+                ok = __all_sync(FULL, ok);
+                if (!ok) break;
+                tc::fence_after();
+                const uint32_t sa = tmem + b * XT + lanes;
+                uint32_t r[2][32];
+                tc::ld32(sa, r[0]);
+                tc::wait_ld(r[0]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t (&q)[32] = r[c & 1];
+                    if (c < 3) tc::ld32(sa + 32 * (c + 1), r[(c + 1) & 1]);
+                    const int col = ybase + c * 32;
+                    float f[32];
+                    if (M == TC_FORWARD) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(q[j]) * c2;
+                        if (col + 32 > P.ny) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (col + j >= P.ny) f[j] = -INFINITY;
+                        }
+                        if (__any_sync(FULL, label >= col && label < col + 32)) {
+                            float z = 0.f;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (col + j == label) z = f[j];
+                            if (label >= col && label < col + 32) P.picked[x] = z;
+                            __syncwarp();
+                        }
+                        float top = m;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) top = fmaxf(top, f[j]);
+                        const float ref = top == -INFINITY ? 0.f : top;
+                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sum[j & 3] += xt_exp2(f[j] - ref);
+                        l = l * xt_exp2(m - ref) + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+                        m = top;
+                    } else {
+                        if (M == TC_DHIDDEN) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) f[j] = xt_exp2(fmaf(__uint_as_float(q[j]), c2, -lse2));
+                            if (__any_sync(FULL, label >= col && label < col + 32)) {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j)
+                                    if (col + j == label) f[j] -= 1.f;
+                            }
+                            if (col + 32 > P.ny) {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j)
+                                    if (col + j >= P.ny) f[j] = 0.f;
+                            }
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; j += 4) {
+                                const float4 ls = *reinterpret_cast<const float4*>(&col_lse[sw][c * 32 + j]);
+                                f[j] = xt_exp2(fmaf(__uint_as_float(q[j]), c2, -ls.x));
+                                f[j + 1] = xt_exp2(fmaf(__uint_as_float(q[j + 1]), c2, -ls.y));
+                                f[j + 2] = xt_exp2(fmaf(__uint_as_float(q[j + 2]), c2, -ls.z));
+                                f[j + 3] = xt_exp2(fmaf(__uint_as_float(q[j + 3]), c2, -ls.w));
+                            }
+                            const int x_warp = (int)(xi * XT) + (warp & 3) * 32;
+                            const int lab = col_label[sw][c * 32 + lane] - x_warp;
+                            if (__any_sync(FULL, lab >= 0 && lab < 32)) {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j)
+                                    if (__shfl_sync(FULL, lab, j) == lane) f[j] -= 1.f;
+                            }
+#pragma unroll
+                            for (int j = 0; j < 32; j += 4) {
+                                const float4 g = *reinterpret_cast<const float4*>(&col_g[sw][c * 32 + j]);
+                                f[j] *= g.x;
+                                f[j + 1] *= g.y;
+                                f[j + 2] *= g.z;
+                                f[j + 3] *= g.w;
+                            }
+                        }
+                        uint32_t z[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) z[j] = pack_bf16(f[2 * j], f[2 * j + 1]);
+                        if (c < 3) tc::wait_ld(r[(c + 1) & 1]);    // the next columns are read before Z overwrites more of S
+                        tc::st16(sa + 16 * c, z);
+                    }
+                    if (M == TC_FORWARD && c < 3) tc::wait_ld(r[(c + 1) & 1]);
+                }
+                if (M != TC_FORWARD) tc::wait_st();
+                tc::fence_before();
+                tc::mbar_arrive(p_full(b));
+            }
+            if (!ok) break;
+            if (M == TC_FORWARD) {
+                P.stats[((run + xi) * 2 + wg) * XT + row] = make_float2(m, l);
+                continue;
+            }
+            // ---- the segment's sum
+            const int ob = s % P.obufs;
+            ok = tc::mbar_wait(o_full(ob), (uint32_t)(s / P.obufs) & 1, &s_stop);
+            ok = __all_sync(FULL, ok);
+            if (!ok) break;
+            tc::fence_after();
+            const bool whole = y0 == 0 && n == P.runs.tiles_y;
+            float factor = 1.f;
+            if (M == TC_DHIDDEN) factor = label >= 0 ? __ldg(P.a.dloss + x) * P.a.scale : 0.f;
+            const bool zero = M == TC_DHIDDEN && factor == 0.f;
+            float* part = P.partial + (P.runs.slot(run, xi) * XT + row) * P.on;
+            for (int c = wg * 16; c < P.on; c += 32) {
+                uint32_t q[16];
+                __syncwarp();
+                tc::ld16(tmem + 256 + ob * 128 + lanes + c, q);
+                tc::wait_ld(q);
+                float f[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) f[j] = zero ? 0.f : __uint_as_float(q[j]) * factor;
+                if (x < P.nx) {
+                    if (!whole) store_vec<float, 16>(part + c, f);
+                    else if (M == TC_DHIDDEN) store_columns(P.a.dhidden, P.a.grad_dtype, x * P.a.dhidden_ld + c, f, P.a.dim - c);
+                    else store_columns(P.a.dtable, P.a.grad_dtype, x * P.a.dtable_ld + c, f, P.a.dim - c);
+                }
+            }
+            tc::fence_before();
+            tc::mbar_arrive(o_free(ob));
+        }
+        if (!ok && lane == 0) atomicExch(&g_xent_gave_up, 1);
+    }
+    __syncwarp();
+    tc::fence_before();
+    __syncthreads();
+    if (warp == 2) {
+        tc::fence_after();
+        tc::tmem_free(tmem, 512);
+    }
+}
+
+// Rows repacked to a pitch that tile loads can address (a multiple of 16 bytes).
+__global__ void __launch_bounds__(256) k_xent_pack(const bf16* __restrict__ src, int64_t ld, int64_t rows, int dim, int pitch, bf16* __restrict__ dst) {
+    const int64_t total = rows * (pitch / 2);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / (pitch / 2);
+        const int c = (int)(i - r * (pitch / 2)) * 2;
+        const bf16* p = src + r * ld + c;
+        const bf16 lo = c < dim ? p[0] : from_f32<bf16>(0.f), hi = c + 1 < dim ? p[1] : from_f32<bf16>(0.f);
+        reinterpret_cast<__nv_bfloat162*>(dst)[i] = __nv_bfloat162(lo, hi);
+    }
+}
+
+// ---------------------------------------------------------------- launches
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static EncodeTiled encode_tiled() {
+    static std::atomic<EncodeTiled> found{nullptr};
+    EncodeTiled f = found.load(std::memory_order_relaxed);
+    if (!f) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) return nullptr;
+        f = (EncodeTiled)p;
+        found.store(f, std::memory_order_relaxed);
+    }
+    return f;
+}
+
+// Rows of `dim` bf16, tiles of 64 columns by 128 rows; what lies outside reads as zero.
+static cudaError_t row_map(CUtensorMap* map, const void* base, int64_t rows, int dim, int64_t ld) {
+    const EncodeTiled f = encode_tiled();
+    if (!f) return cudaErrorSymbolNotFound;
+    const cuuint64_t dims[2] = {(cuuint64_t)dim, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t box[2] = {64, XT}, step[2] = {1, 1};
+    return f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? cudaSuccess
+               : cudaErrorInvalidValue;
+}
+
+static bool tile_rows_ok(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && (ld * 2) % 16 == 0; }
+static int packed_pitch(int dim) { return (dim + 7) / 8 * 8; }
+
+bool xent_tc_takes(const Xent& a) {
+    if (a.dtype != GS_BF16 || a.dim > XENT_TC_MAX_DIM) return false;
+    return a.dim % 8 != 0 || (tile_rows_ok(a.hidden, a.hidden_ld) && tile_rows_ok(a.table, a.table_ld));
+}
+
+struct TcLayout {
+    size_t hidden, table, rest, total;
+};
+
+static TcLayout tc_layout(const Xent& a) {
+    TcLayout l{};
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
+    if (a.dim % 8) {                       // operands that tile loads may not be able to address are copied
+        l.hidden = take((size_t)a.rows * packed_pitch(a.dim) * 2);
+        l.table = take((size_t)a.vocab * packed_pitch(a.dim) * 2);
+    }
+    l.rest = off;
+    const int64_t parts = sm_count(), tx = (a.rows + XT - 1) / XT;
+    const size_t fwd = align_up((size_t)(parts + tx) * 2 * XT * 8, 256) + align_up((size_t)a.rows * 4, 256);
+    const size_t bwd = (size_t)2 * parts * XT * ((a.dim + 15) / 16 * 16) * 4;
+    take(fwd > bwd ? fwd : bwd);
+    l.total = off;
+    return l;
+}
+
+size_t xent_tc_workspace(const Xent& a) { return tc_layout(a).total; }
+
+cudaError_t xent_gave_up(cudaStream_t s, int* h_flag) {
+    cudaError_t e = cudaMemcpyFromSymbolAsync(h_flag, g_xent_gave_up, sizeof(int), 0, cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    return e;
+}
+
+struct Operands {
+    const void* hidden;
+    const void* table;
+    int64_t hidden_ld, table_ld;
+    char* rest;
+};
+
+static cudaError_t prepare_operands(const Xent& a, void* workspace, Operands* o, cudaStream_t s) {
+    const TcLayout l = tc_layout(a);
+    char* ws = (char*)workspace;
+    *o = Operands{a.hidden, a.table, a.hidden_ld, a.table_ld, ws + l.rest};
+    const int pitch = packed_pitch(a.dim);
+    auto pack = [&](const void* src, int64_t ld, int64_t rows, char* dst) {
+        int64_t blocks = (rows * (pitch / 2) + 255) / 256;
+        if (blocks > sm_count() * 32) blocks = sm_count() * 32;
+        k_xent_pack<<<(int)limit_grid(blocks), 256, 0, s>>>((const bf16*)src, ld, rows, a.dim, pitch, (bf16*)dst);
+        count_launches(1);
+    };
+    if (!tile_rows_ok(a.hidden, a.hidden_ld)) {
+        pack(a.hidden, a.hidden_ld, a.rows, ws + l.hidden);
+        o->hidden = ws + l.hidden;
+        o->hidden_ld = pitch;
+    }
+    if (!tile_rows_ok(a.table, a.table_ld)) {
+        pack(a.table, a.table_ld, a.vocab, ws + l.table);
+        o->table = ws + l.table;
+        o->table_ld = pitch;
+    }
+    return cudaGetLastError();
+}
+
+template <int M> static cudaError_t run_tc(const Xent& a, const Operands& o, XentTc& P, cudaStream_t s) {
+    constexpr bool ON_X = M != TC_DTABLE;
+    P.a = a;
+    P.nx = ON_X ? a.rows : (int)a.vocab;
+    P.ny = ON_X ? (int)a.vocab : a.rows;
+    P.runs = make_runs(P.nx, XT, P.ny, XT, sm_count());
+    P.chunks = (a.dim + 63) / 64;
+    P.ksteps = (a.dim + 15) / 16;
+    P.on = P.ksteps * 16;
+    const int tile = P.chunks * XT_CHUNK;
+    P.xbufs = P.chunks <= 2 ? 2 : 1;
+    P.stages = (192 << 10) / tile - P.xbufs;
+    if (P.stages > XT_MAX_STAGES) P.stages = XT_MAX_STAGES;
+    P.obufs = P.on <= 128 ? 2 : 1;
+    CUtensorMap hm, tm;
+    cudaError_t e = row_map(&hm, o.hidden, a.rows, a.dim, o.hidden_ld);
+    if (e == cudaSuccess) e = row_map(&tm, o.table, a.vocab, a.dim, o.table_ld);
+    if (e != cudaSuccess) return e;
+    // at least 120 KB, so that an SM holds one block: a block takes all of the tensor memory
+    int smem = (P.xbufs + P.stages) * tile + 1024;
+    if (smem < (120 << 10)) smem = 120 << 10;
+    e = cudaFuncSetAttribute(k_xent_tc<M>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    k_xent_tc<M><<<(int)limit_grid(P.runs.parts), XT_THREADS, smem, s>>>(P, ON_X ? hm : tm, ON_X ? tm : hm);
+    count_launches(1);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_xent_tc_forward(const Xent& a, void* workspace, Runs* runs, const float2** stats, const float** picked, cudaStream_t s) {
+    Operands o;
+    cudaError_t e = prepare_operands(a, workspace, &o, s);
+    if (e != cudaSuccess) return e;
+    XentTc P{};
+    const int64_t tx = (a.rows + XT - 1) / XT;
+    P.stats = (float2*)o.rest;
+    P.picked = (float*)(o.rest + align_up((size_t)(sm_count() + tx) * 2 * XT * 8, 256));
+    e = run_tc<TC_FORWARD>(a, o, P, s);
+    *runs = P.runs;
+    *stats = P.stats;
+    *picked = P.picked;
+    return e;
+}
+
+cudaError_t launch_xent_tc_backward(const Xent& a, void* workspace, cudaStream_t s) {
+    Operands o;
+    cudaError_t e = prepare_operands(a, workspace, &o, s);
+    if (e != cudaSuccess) return e;
+    XentTc P{};
+    P.partial = (float*)o.rest;
+    e = run_tc<TC_DHIDDEN>(a, o, P, s);
+    if (e != cudaSuccess) return e;
+    e = launch_xent_join(a, true, P.runs, XT, P.on, P.partial, s);
+    if (e != cudaSuccess) return e;
+    e = run_tc<TC_DTABLE>(a, o, P, s);
+    if (e != cudaSuccess) return e;
+    return launch_xent_join(a, false, P.runs, XT, P.on, P.partial, s);
+}
+
+}  // namespace gs
