@@ -500,11 +500,11 @@ gs_status gs_embedding_backward_sparse(const void* d_dout, gs_dtype dout_dtype, 
  *   block      a block of gs_sample_batch, or one the caller fills: max_* are the sizes, d_num_* device scalars with
  *              the actual ones, or NULL (the sizes are exact; all three together)
  *   max_row    an upper bound on the edges of one destination (the fan-out, for a sampled block), or 0 if it is not
- *              known: rows above 256 edges are then split over the device.  A longer row than promised is slower,
+ *              known: rows above 128 edges are then split over the device.  A longer row than promised is slower,
  *              not wrong.
  *   gs_heads   [rows][heads][head_dim] of `dtype`, head_dim contiguous, strides in elements (a slice of a fused
  *              projection is fine); q, out, dout, dq have the destinations' rows and q_heads, k, v, dk, dv the
- *              sources' rows and kv_heads (a divisor of q_heads); 1 <= head_dim <= 256, q_heads <= 1024
+ *              sources' rows and kv_heads (a divisor of q_heads); 1 <= head_dim <= 256, q_heads <= 128
  *   d_lse      float[max_dst][q_heads]
  * gs_block_reverse turns the block's edges to source order, once for all layers that use the block: the
  * destinations of source j, ascending, are d_rev_dst[d_rev_indptr[j] .. d_rev_indptr[j+1]) (int32[max_src + 1] and

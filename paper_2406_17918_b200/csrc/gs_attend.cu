@@ -20,7 +20,7 @@
 namespace gs {
 
 constexpr int AT_THREADS = 256;
-constexpr int AT_CHUNK = 256;
+constexpr int AT_CHUNK = 128;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float fast_exp2(float x) {
@@ -29,6 +29,8 @@ __device__ __forceinline__ float fast_exp2(float x) {
     return y;
 }
 
+enum AttendKind { AT_FORWARD, AT_DQ, AT_DKV };
+
 struct Attend {
     BlockAttention a;
     const int32_t* starts;      // row offsets and columns: the block's, or the reversed block's
@@ -36,6 +38,7 @@ struct Attend {
     Count rows, columns;
     int edge_bound;
     int tl, slots, units_per_row;
+    int tiles;                  // ring kernels: warp-sized tiles of units a warp takes at a time
     int split;                  // rows above AT_CHUNK edges go to the chunk list
     int chunk_mode;             // this launch works through the chunk list
     int32_t* words;             // [0] chunks, [1] long rows
@@ -523,6 +526,12 @@ template <typename T, bool KV> __global__ void __launch_bounds__(AT_THREADS) k_a
     }
 }
 
+}  // namespace gs
+
+#include "gs_attend_ring.cuh"
+
+namespace gs {
+
 // The destination of every edge, in edge order.
 __global__ void __launch_bounds__(AT_THREADS) k_edge_rows(const int32_t* __restrict__ indptr, Count dst, int edge_bound, int32_t* __restrict__ rows) {
     const int n = length_of(dst), lane = threadIdx.x & 31;
@@ -564,7 +573,8 @@ static int wide_elems(const BlockAttention& a, std::initializer_list<const HeadV
     for (int ve = 16 / size; ve >= 4; ve /= 2) {
         bool ok = a.head_dim % ve == 0;
         for (const HeadView* v : views)
-            ok = ok && ((uintptr_t)v->data % (ve * size)) == 0 && (v->row_stride * size) % (ve * size) == 0 && (v->head_stride * size) % (ve * size) == 0;
+            ok = ok && ((uintptr_t)v->data % (ve * size)) == 0 && (v->row_stride * size) % (ve * size) == 0 && (v->head_stride * size) % (ve * size) == 0 &&
+                 v->row_stride * size < ((int64_t)1 << 32) && v->head_stride * size < ((int64_t)1 << 32);
         if (ok) return ve;
     }
     return 1;
@@ -579,8 +589,6 @@ static void shape_groups(Attend& P, int ve, int nv, int64_t rows, int units_per_
     // several groups share a row while the rows alone do not give every SM sixteen warps and each group keeps four edges
     while (P.tl * P.slots * 2 <= 32 && rows * units_per_row * P.tl * P.slots * 2 <= sm_count() * 16 * 32 && (row_hint == 0 || row_hint >= 8 * P.slots)) P.slots *= 2;
 }
-
-enum AttendKind { AT_FORWARD, AT_DQ, AT_DKV };
 
 template <AttendKind K, typename T, int VE, int NV, int G> static void run_attend(Attend P, int64_t rows, int64_t row_hint, cudaStream_t s) {
     constexpr int U = VE * NV * G >= 32 ? 2 : 4;
@@ -607,14 +615,48 @@ template <AttendKind K, typename T, int VE, int NV, int G> static void run_atten
     }
 }
 
-// Query heads of one key/value head that a group takes together (they share the loads of k and v).
-template <AttendKind K, typename T, int VE, int NV> static void run_group(const Attend& P, int64_t rows, int64_t row_hint, cudaStream_t s) {
-    const int group = P.a.q_heads / P.a.kv_heads;
-    if constexpr (VE * (int)sizeof(T) == 16) {
-        if (group % 4 == 0) return run_attend<K, T, VE, NV, 4>(P, rows, row_hint, s);
-        if (group % 2 == 0) return run_attend<K, T, VE, NV, 2>(P, rows, row_hint, s);
+// The ring kernels: edge batches through shared memory.
+template <AttendKind K, typename T, int VE, int NV, int G> static cudaError_t run_ring(Attend P, int64_t rows, cudaStream_t s) {
+    constexpr int U = K == AT_DKV ? (G == 4 ? 1 : 2) : 4;
+    constexpr int smem = RING_WARPS * RingShape<K, T, VE, NV, G, U>::WARP;
+    auto kernel = k_attend_ring<K, T, VE, NV, G, U>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    P.units_per_row = K == AT_DKV ? P.a.kv_heads : P.a.q_heads / G;
+    const int pieces = (P.a.head_dim + VE * NV - 1) / (VE * NV);
+    P.tl = 1;
+    while (P.tl < pieces) P.tl *= 2;
+    const int gpw = 32 / P.tl;
+    const int64_t resident = sm_count() * RING_WARPS * ((220 << 10) / smem);
+    for (int pass = 0; pass < (P.split ? 2 : 1); ++pass) {
+        P.chunk_mode = pass;
+        const int64_t n = pass ? 2 * ((int64_t)P.edge_bound / AT_CHUNK) + 2 : rows;
+        const int64_t tiles = (n * P.units_per_row + gpw - 1) / gpw;
+        // rows: about four rounds of all resident warps, as far as a warp's row offsets go; chunks are long enough alone
+        int64_t per = pass ? 1 : tiles / (resident * 4);
+        const int64_t most = (int64_t)(RING_ROWS - 2) * P.units_per_row / gpw;
+        per = per > most ? most : per;
+        P.tiles = (int)(per < 1 ? 1 : per);
+        int64_t blocks = (tiles + (int64_t)P.tiles * RING_WARPS - 1) / ((int64_t)P.tiles * RING_WARPS);
+        const int64_t cap = pass ? resident / RING_WARPS * 2 : (int64_t)1 << 30;
+        kernel<<<(int)limit_grid(blocks > cap ? cap : blocks), RING_WARPS * 32, smem, s>>>(P);
+        count_launches(1);
     }
-    run_attend<K, T, VE, NV, 1>(P, rows, row_hint, s);
+    if (P.split) {
+        const int grid = (int)limit_grid(sm_count() * 2);
+        if constexpr (K == AT_FORWARD) k_attend_forward_join<T><<<grid, AT_THREADS, 0, s>>>(P);
+        else k_attend_sum_join<T, K == AT_DKV><<<grid, AT_THREADS, 0, s>>>(P);
+        count_launches(1);
+    }
+    return cudaGetLastError();
+}
+
+// Query heads of one key/value head that a group takes together (they share the loads of k and v).
+template <AttendKind K, typename T, int VE, int NV> static cudaError_t ring_group(const Attend& P, int64_t rows, cudaStream_t s) {
+    const int group = P.a.q_heads / P.a.kv_heads;
+    if (group % 4 == 0) return run_ring<K, T, VE, NV, 4>(P, rows, s);
+    if (group % 2 == 0) return run_ring<K, T, VE, NV, 2>(P, rows, s);
+    return run_ring<K, T, VE, NV, 1>(P, rows, s);
 }
 
 template <AttendKind K> static cudaError_t run_kind(Attend& P, int ve, int64_t rows, int64_t row_hint, cudaStream_t s) {
@@ -623,21 +665,22 @@ template <AttendKind K> static cudaError_t run_kind(Attend& P, int ve, int64_t r
         const cudaError_t e = cudaMemsetAsync(P.words, 0, 8, s);
         if (e != cudaSuccess) return e;
     }
+    // pieces of 16 or 8 bytes: the ring kernels; else one element at a time
     if (P.a.dtype == GS_BF16) {
-        if (ve == 8) run_group<K, bf16, 8, 1>(P, rows, row_hint, s);
-        else if (ve == 4 && D <= 128) run_group<K, bf16, 4, 1>(P, rows, row_hint, s);
-        else if (ve == 4) run_group<K, bf16, 4, 2>(P, rows, row_hint, s);
-        else if (D <= 32) run_group<K, bf16, 1, 1>(P, rows, row_hint, s);
-        else if (D <= 64) run_group<K, bf16, 1, 2>(P, rows, row_hint, s);
-        else if (D <= 128) run_group<K, bf16, 1, 4>(P, rows, row_hint, s);
-        else run_group<K, bf16, 1, 8>(P, rows, row_hint, s);
+        if (ve == 8) return ring_group<K, bf16, 8, 1>(P, rows, s);
+        if (ve == 4 && D <= 128) return ring_group<K, bf16, 4, 1>(P, rows, s);
+        if (ve == 4) return ring_group<K, bf16, 4, 2>(P, rows, s);
+        if (D <= 32) run_attend<K, bf16, 1, 1, 1>(P, rows, row_hint, s);
+        else if (D <= 64) run_attend<K, bf16, 1, 2, 1>(P, rows, row_hint, s);
+        else if (D <= 128) run_attend<K, bf16, 1, 4, 1>(P, rows, row_hint, s);
+        else run_attend<K, bf16, 1, 8, 1>(P, rows, row_hint, s);
     } else {
-        if (ve == 4 && D <= 128) run_group<K, float, 4, 1>(P, rows, row_hint, s);
-        else if (ve == 4) run_group<K, float, 4, 2>(P, rows, row_hint, s);
-        else if (D <= 32) run_group<K, float, 1, 1>(P, rows, row_hint, s);
-        else if (D <= 64) run_group<K, float, 1, 2>(P, rows, row_hint, s);
-        else if (D <= 128) run_group<K, float, 1, 4>(P, rows, row_hint, s);
-        else run_group<K, float, 1, 8>(P, rows, row_hint, s);
+        if (ve == 4 && D <= 128) return ring_group<K, float, 4, 1>(P, rows, s);
+        if (ve == 4) return ring_group<K, float, 4, 2>(P, rows, s);
+        if (D <= 32) run_attend<K, float, 1, 1, 1>(P, rows, row_hint, s);
+        else if (D <= 64) run_attend<K, float, 1, 2, 1>(P, rows, row_hint, s);
+        else if (D <= 128) run_attend<K, float, 1, 4, 1>(P, rows, row_hint, s);
+        else run_attend<K, float, 1, 8, 1>(P, rows, row_hint, s);
     }
     return cudaGetLastError();
 }

@@ -1,0 +1,498 @@
+// Attention over a block with operands on 16- or 8-byte pieces: the edges stream through shared memory.
+//
+// A group of tl lanes owns one (row, head) unit at a time and walks through its units batch by batch (up to U edges of
+// one row).  Every lane copies exactly the pieces it will use itself into slots of its own (cp.async, zero-filled where
+// an edge is masked), RING_DEPTH batches ahead, and the column indices one batch earlier still: the gathers of the next
+// batches are in flight across row boundaries while one is computed, they hold no registers, and no barrier is needed
+// because no lane reads another's copies.  Rows' own operands (q; q, dout, out; k, v) ride in their first batch.
+// Latency is hidden with 8 to 14 warps per SM, so what is left to save is instructions: pairs of values go through
+// packed 32-bit operations, addresses are one multiply-add per copy, and masked edges take the same path as others.
+#pragma once
+#include "gs_train.cuh"
+
+namespace gs {
+
+constexpr int RING_SLOTS = 3;            // batches of copies per lane
+constexpr int RING_DEPTH = RING_SLOTS - 1;
+constexpr int RING_WARPS = 2;            // warps per block
+constexpr int RING_ROWS = 64;            // rows whose offsets a warp holds at a time
+
+template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int n) {   // n bytes, the rest zero
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    else if constexpr (BYTES == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+
+// Two 32-bit values in one 64-bit register pair.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void split(f32x2 x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+template <int N> __device__ __forceinline__ float dot2(const f32x2 (&a)[N], const f32x2 (&b)[N]) {
+    f32x2 s = mul2(a[0], b[0]);
+#pragma unroll
+    for (int i = 1; i < N; ++i) s = fma2(a[i], b[i], s);
+    float lo, hi;
+    split(s, lo, hi);
+    return lo + hi;
+}
+template <int N> __device__ __forceinline__ void axpy2(float p, const f32x2 (&x)[N], f32x2 (&acc)[N]) {
+    const f32x2 pp = pair(p, p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) acc[i] = fma2(pp, x[i], acc[i]);
+}
+template <int N> __device__ __forceinline__ void scale2(float p, f32x2 (&x)[N]) {
+    const f32x2 pp = pair(p, p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = mul2(pp, x[i]);
+}
+template <int N> __device__ __forceinline__ void unpair(const f32x2 (&x)[N], float (&y)[2 * N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) split(x[i], y[2 * i], y[2 * i + 1]);
+}
+
+// The sums over the tl lanes of a group, in every lane; straight code for the usual widths.
+template <int N, int TL> __device__ __forceinline__ void group_sum_of(float (&x)[N]) {
+#pragma unroll
+    for (int o = 1; o < TL; o <<= 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(FULL, x[i], o);
+    }
+}
+template <int N> __device__ __forceinline__ void ring_sum(float (&x)[N], int tl) {
+    if (tl == 4) group_sum_of<N, 4>(x);
+    else if (tl == 2) group_sum_of<N, 2>(x);
+    else if (tl == 8) group_sum_of<N, 8>(x);
+    else group_sum<N>(x, tl);
+}
+
+template <AttendKind K, typename T, int VE, int NV, int G, int U> struct RingShape {
+    static constexpr int PB = (int)sizeof(T) * VE;                                 // bytes of a piece
+    static constexpr int EDGE = (K == AT_DKV ? 2 * NV * G : 2 * NV);               // pieces per edge
+    static constexpr int ROW = K == AT_FORWARD ? NV * G : (K == AT_DQ ? 3 * NV * G : 2 * NV);
+    static constexpr int PIECES = (U * EDGE + ROW) * 32 * PB;
+    static constexpr int STAT = K == AT_DKV ? U * G * 32 * 8 : (K == AT_DQ ? G * 32 * 4 : 0);
+    static constexpr int SLOT = PIECES + STAT;
+    static constexpr int WARP = RING_SLOTS * SLOT + RING_ROWS * 16;
+};
+
+template <AttendKind K, typename T, int VE, int NV, int G, int U>
+__global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_constant__ Attend P) {
+    using S = RingShape<K, T, VE, NV, G, U>;
+    constexpr int E = VE * NV, N2 = E / 2, PB = S::PB, SZ = (int)sizeof(T);
+    extern __shared__ __align__(16) unsigned char ring_smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned char* mine = ring_smem + (size_t)warp * S::WARP;
+    int4* rows_s = reinterpret_cast<int4*>(mine + RING_SLOTS * S::SLOT);           // begin, end, row, item (or -1: listed as long)
+    const uint32_t mine_a = (uint32_t)__cvta_generic_to_shared(mine);
+    const int tl = P.tl, t = lane & (tl - 1), gi = lane / tl, gpw = 32 / tl, upr = P.units_per_row;
+    const int rows = P.chunk_mode ? __ldcg(P.words) : length_of(P.rows), cols = length_of(P.columns);
+    const int64_t units = (int64_t)rows * upr;
+    const float c2 = P.a.scale * LOG2E;
+    const int D = P.a.head_dim, group = P.a.q_heads / P.a.kv_heads;
+    const int passes = K == AT_DKV ? group / G : 1;                                 // walks over a row's edges
+    const HeadView& av = K == AT_DKV ? P.a.q : P.a.k;                               // the edges' two operands
+    const HeadView& bv = K == AT_DKV ? P.a.dout : P.a.v;
+    const uint32_t astep = (uint32_t)av.row_stride * SZ, bstep = (uint32_t)bv.row_stride * SZ;   // below 2^32 by the choice of kernel
+    const uint32_t ahead_step = (uint32_t)av.head_stride * SZ, bhead_step = (uint32_t)bv.head_stride * SZ;
+    const char* abase = (const char*)av.data + t * PB;
+    const char* bbase = (const char*)bv.data + t * PB;
+    int size[NV];                                                                   // bytes of this lane's pieces: 0 behind the row's end
+#pragma unroll
+    for (int n = 0; n < NV; ++n) size[n] = (t + n * tl) * VE < D ? PB : 0;
+    enum : uint32_t { LIVE = 1, FIRST = 2, LAST = 4, HEAD = 8 };                    // a batch: flags | edges << 4 | local row << 8 | head << 16 | walk << 24
+
+    // a warp takes P.tiles tiles of gpw consecutive units at a time
+    const int64_t span = (int64_t)P.tiles * gpw;
+    for (int64_t u0 = ((int64_t)blockIdx.x * RING_WARPS + warp) * span; u0 < units; u0 += (int64_t)gridDim.x * RING_WARPS * span) {
+        const int r0 = (int)(u0 / upr), off = (int)(u0 - (int64_t)r0 * upr);
+        const int left = (int)(units - u0 < span ? units - u0 : span);
+        const int nrows = (off + left + upr - 1) / upr;                             // at most RING_ROWS by the choice of P.tiles
+        __syncwarp();
+        for (int i = lane; i < nrows; i += 32) {
+            int row = r0 + i, item = 0, first = 0;
+            if (P.chunk_mode) {
+                const int2 it = P.items[row];
+                item = row;
+                row = it.x;
+                first = it.y * AT_CHUNK;
+            }
+            int b = __ldg(P.starts + row), e = __ldg(P.starts + row + 1);
+            b = b < 0 ? 0 : b;
+            e = e > P.edge_bound ? P.edge_bound : e;
+            if (e < b) e = b;
+            if (P.chunk_mode) {
+                b += first;
+                e = b + AT_CHUNK < e ? b + AT_CHUNK : e;
+            } else if (P.split && e - b > AT_CHUNK) {
+                // listed once: by the warp that holds the row's first unit
+                if (i > 0 || off == 0) list_long_row(P, row, e - b);
+                e = b;
+                item = -1;
+            }
+            rows_s[i] = make_int4(b, e, row, item);
+        }
+        __syncwarp();
+
+        // ---- the producer's position: unit, row, walk and next edge of this group
+        int lu = gi, e_next = 0, e_end = 0, pass = 0, lr = 0, head = 0;
+        bool fresh = true, walk = true;
+        const char* ap = abase;                              // this lane's first piece in row 0 of the edges' operands
+        const char* bp = bbase;
+        uint32_t next = 0;
+        int idx[U];                                // the batch whose indices are on their way
+        auto fetch = [&]() {
+            next = 0;
+#pragma unroll
+            for (int j = 0; j < U; ++j) idx[j] = -1;
+            if (lu >= left) return;
+            if (fresh) {
+                const int v = off + lu;
+                lr = upr == 1 ? v : v / upr;
+                head = v - lr * upr;
+                const int4 r = rows_s[lr];
+                e_next = r.x;
+                e_end = r.y;
+                pass = 0;
+                next = FIRST;
+                fresh = false;
+                walk = true;
+            }
+            if (walk) next |= HEAD;
+            walk = false;
+            const int32_t* c = P.cols + e_next;
+#pragma unroll
+            for (int j = 0; j < U; ++j)
+                if (e_next + j < e_end) idx[j] = __ldg(c + j);
+            next |= LIVE | (uint32_t)lr << 8 | (uint32_t)head << 16 | (uint32_t)pass << 24;
+            e_next += U;
+            if (e_next >= e_end) {
+                if (K == AT_DKV && passes > 1 && ++pass < passes && e_end > rows_s[lr].x) {
+                    e_next = rows_s[lr].x;
+                    walk = true;
+                } else {
+                    next |= LAST;
+                    lu += gpw;
+                    fresh = true;
+                }
+            }
+        };
+        // the copies of the batch whose indices have arrived; returns its description
+        int h0 = 0;
+        auto issue = [&](int slot) -> uint32_t {
+            uint32_t batch = next;
+            const uint32_t base = mine_a + slot * S::SLOT, lp = base + lane * PB;
+            const int hd = (batch >> 16) & 255;
+            if (batch & HEAD) {
+                h0 = K == AT_DKV ? hd * group + (int)(batch >> 24) * G : hd * G;
+                const int he = K == AT_DKV ? h0 : (group == G ? hd : h0 / group);
+                ap = abase + (uint64_t)he * ahead_step;
+                bp = bbase + (uint64_t)he * bhead_step;
+            }
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const bool on = (uint32_t)idx[j] < (uint32_t)cols;
+                const uint32_t col = on ? idx[j] : 0;
+                batch |= on ? 16u << j : 0u;
+                const char* a = ap + (uint64_t)col * astep;
+                const char* b = bp + (uint64_t)col * bstep;
+#pragma unroll
+                for (int i = 0; i < (K == AT_DKV ? G : 1); ++i)
+#pragma unroll
+                    for (int n = 0; n < NV; ++n) {
+                        const uint32_t to = lp + (uint32_t)(j * S::EDGE + i * 2 * NV + n) * 32 * PB;
+                        const int sz = on ? size[n] : 0;
+                        const uint32_t off_n = sz ? n * tl * PB : 0;
+                        copy_async<PB>(to, a + i * ahead_step + off_n, sz);
+                        copy_async<PB>(to + NV * 32 * PB, b + i * bhead_step + off_n, sz);
+                    }
+                if (K == AT_DKV) {
+#pragma unroll
+                    for (int i = 0; i < G; ++i)
+                        copy_async<8>(base + S::PIECES + ((j * G + i) * 32 + lane) * 8, P.stat + (uint64_t)col * P.a.q_heads + h0 + i, on ? 8 : 0);
+                }
+            }
+            if (batch & FIRST) {
+                const int4 r = rows_s[(batch >> 8) & 255];
+                const bool any = K != AT_DKV || r.y > r.x;
+                auto rowcopy = [&](const HeadView& v, int h, int piece) {
+                    const char* p = (const char*)v.data + ((int64_t)r.z * v.row_stride + (int64_t)h * v.head_stride) * SZ;
+#pragma unroll
+                    for (int n = 0; n < NV; ++n)
+                        copy_async<PB>(lp + (uint32_t)(U * S::EDGE + piece + n) * 32 * PB, size[n] ? p + (t + n * tl) * PB : p, any ? size[n] : 0);
+                };
+                if (K == AT_DKV) {
+                    rowcopy(P.a.k, hd, 0);
+                    rowcopy(P.a.v, hd, NV);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        rowcopy(P.a.q, h0 + i, i * NV);
+                        if (K == AT_DQ) {
+                            rowcopy(P.a.dout, h0 + i, (G + i) * NV);
+                            rowcopy(P.a.out, h0 + i, (2 * G + i) * NV);
+                            copy_async<4>(base + S::PIECES + (i * 32 + lane) * 4, P.a.lse + (int64_t)r.z * P.a.q_heads + h0 + i, 4);
+                        }
+                    }
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            return batch;
+        };
+        auto pieces = [&](int slot, int p, f32x2 (&x)[N2]) {
+#pragma unroll
+            for (int n = 0; n < NV; ++n) {
+                Raw<T, VE> r;
+                float y[VE];
+                r.w = *reinterpret_cast<const typename Raw<T, VE>::word*>(mine + slot * S::SLOT + (size_t)(p + n) * 32 * PB + lane * PB);
+                unpack<T, VE>(r, y);
+#pragma unroll
+                for (int c = 0; c < VE / 2; ++c) x[n * VE / 2 + c] = pair(y[2 * c], y[2 * c + 1]);
+            }
+        };
+
+        // what a unit keeps from batch to batch
+        constexpr int NX = K == AT_DKV ? 1 : G, NA = K == AT_DKV ? 2 : G;
+        f32x2 x0[NX][N2], x1[K == AT_FORWARD ? 1 : NX][K == AT_FORWARD ? 1 : N2];   // q; q, dout; k, v
+        f32x2 acc[NA][N2];                                                           // out; dq; dk, dv
+        float m[G], l[G];                                                            // running maximum and sum; lse (base 2), delta
+#pragma unroll
+        for (int i = 0; i < NX; ++i)
+#pragma unroll
+            for (int c = 0; c < N2; ++c) {
+                x0[i][c] = 0;
+                if constexpr (K != AT_FORWARD) x1[i][c] = 0;
+            }
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+            for (int c = 0; c < N2; ++c) acc[i][c] = 0;
+#pragma unroll
+        for (int i = 0; i < G; ++i) m[i] = l[i] = 0.f;
+
+        uint32_t batches[RING_DEPTH];
+        fetch();
+#pragma unroll
+        for (int s = 0; s < RING_DEPTH; ++s) {
+            batches[s] = issue(s);
+            fetch();
+        }
+        int slot = 0, ahead = RING_DEPTH;
+        while (__any_sync(FULL, batches[0] & LIVE)) {
+            const uint32_t batch = batches[0];
+#pragma unroll
+            for (int s = 0; s + 1 < RING_DEPTH; ++s) batches[s] = batches[s + 1];
+            batches[RING_DEPTH - 1] = issue(ahead);
+            fetch();
+            asm volatile("cp.async.wait_group %0;" ::"n"(RING_DEPTH) : "memory");
+            const int h = (batch >> 16) & 255;
+            auto on = [&](int j) { return (batch >> (4 + j)) & 1; };
+            if constexpr (K == AT_FORWARD) {
+                if (batch & FIRST) {
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        pieces(slot, U * S::EDGE + i * NV, x0[i]);
+                        m[i] = -INFINITY;
+                        l[i] = 0.f;
+#pragma unroll
+                        for (int c = 0; c < N2; ++c) acc[i][c] = 0;
+                    }
+                }
+                float s[U * G];
+#pragma unroll
+                for (int j = 0; j < U; ++j) {
+                    f32x2 k[N2];
+                    pieces(slot, j * S::EDGE, k);
+#pragma unroll
+                    for (int i = 0; i < G; ++i) s[j * G + i] = dot2(x0[i], k);
+                }
+                ring_sum<U * G>(s, tl);
+                float p[U * G];
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    float top = m[i];
+#pragma unroll
+                    for (int j = 0; j < U; ++j) {
+                        s[j * G + i] = on(j) ? s[j * G + i] * c2 : -INFINITY;
+                        top = fmaxf(top, s[j * G + i]);
+                    }
+                    const float ref = top == -INFINITY ? 0.f : top;
+                    const float corr = fast_exp2(m[i] - ref);
+                    m[i] = top;
+                    l[i] *= corr;
+#pragma unroll
+                    for (int j = 0; j < U; ++j) {
+                        p[j * G + i] = fast_exp2(s[j * G + i] - ref);
+                        l[i] += p[j * G + i];
+                    }
+                    scale2(corr, acc[i]);
+                }
+#pragma unroll
+                for (int j = 0; j < U; ++j) {
+                    f32x2 v[N2];
+                    pieces(slot, j * S::EDGE + NV, v);
+#pragma unroll
+                    for (int i = 0; i < G; ++i) axpy2(p[j * G + i], v, acc[i]);
+                }
+                if (batch & LAST) {
+                    const int4 rw = rows_s[(batch >> 8) & 255];
+                    if (rw.w >= 0) {
+#pragma unroll
+                        for (int i = 0; i < G; ++i) {
+                            const int hh = h * G + i;
+                            float o[E];
+                            unpair(acc[i], o);
+                            if (P.chunk_mode) {
+                                float* part = P.partial + ((int64_t)rw.w * P.a.q_heads + hh) * (D + 2);
+                                store_partial<VE, NV>(part, t, tl, D, o);
+                                if (t == 0) {
+                                    part[D] = m[i];
+                                    part[D + 1] = l[i];
+                                }
+                            } else {
+                                const bool none = l[i] == 0.f;
+                                const float inv = none ? 0.f : 1.f / l[i];
+#pragma unroll
+                                for (int c = 0; c < E; ++c) o[c] = none ? 0.f : o[c] * inv;
+                                store_piece<T, VE, NV>((T*)P.a.out.data + (int64_t)rw.z * P.a.out.row_stride + (int64_t)hh * P.a.out.head_stride, t, tl, D, o);
+                                if (t == 0) P.a.lse[(int64_t)rw.z * P.a.q_heads + hh] = none ? -INFINITY : m[i] * LN2 + logf(l[i]);
+                            }
+                        }
+                    }
+                }
+            } else if constexpr (K == AT_DQ) {
+                if (__any_sync(FULL, batch & FIRST)) {
+                    float delta[G];
+#pragma unroll
+                    for (int i = 0; i < G; ++i) delta[i] = 0.f;
+                    if (batch & FIRST) {
+#pragma unroll
+                        for (int i = 0; i < G; ++i) {
+                            f32x2 o[N2];
+                            pieces(slot, U * S::EDGE + i * NV, x0[i]);
+                            pieces(slot, U * S::EDGE + (G + i) * NV, x1[i]);
+                            pieces(slot, U * S::EDGE + (2 * G + i) * NV, o);
+                            m[i] = *reinterpret_cast<const float*>(mine + slot * S::SLOT + S::PIECES + (i * 32 + lane) * 4) * LOG2E;
+                            delta[i] = dot2(x1[i], o);
+#pragma unroll
+                            for (int c = 0; c < N2; ++c) acc[i][c] = 0;
+                        }
+                    }
+                    __syncwarp();
+                    ring_sum<G>(delta, tl);
+                    if (batch & FIRST) {
+                        const int row = rows_s[(batch >> 8) & 255].z;
+#pragma unroll
+                        for (int i = 0; i < G; ++i) {
+                            l[i] = delta[i];
+                            if (!P.chunk_mode && t == 0) P.stat[(int64_t)row * P.a.q_heads + h * G + i] = make_float2(m[i], l[i]);
+                        }
+                    }
+                    __syncwarp();
+                }
+                float s[2 * U * G];
+#pragma unroll
+                for (int j = 0; j < U; ++j) {
+                    f32x2 k[N2], v[N2];
+                    pieces(slot, j * S::EDGE, k);
+                    pieces(slot, j * S::EDGE + NV, v);
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        s[j * G + i] = dot2(x0[i], k);
+                        s[U * G + j * G + i] = dot2(x1[i], v);
+                    }
+                }
+                ring_sum<2 * U * G>(s, tl);
+#pragma unroll
+                for (int j = 0; j < U; ++j) {
+                    f32x2 k[N2];
+                    pieces(slot, j * S::EDGE, k);
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        const float ds = on(j) ? fast_exp2(fmaf(s[j * G + i], c2, -m[i])) * (s[U * G + j * G + i] - l[i]) : 0.f;
+                        axpy2(ds, k, acc[i]);
+                    }
+                }
+                if (batch & LAST) {
+                    const int4 rw = rows_s[(batch >> 8) & 255];
+                    if (rw.w >= 0) {
+#pragma unroll
+                        for (int i = 0; i < G; ++i) {
+                            const int hh = h * G + i;
+                            if (!P.chunk_mode) scale2(P.a.scale, acc[i]);
+                            float o[E];
+                            unpair(acc[i], o);
+                            if (P.chunk_mode) store_partial<VE, NV>(P.partial + ((int64_t)rw.w * P.a.q_heads + hh) * D, t, tl, D, o);
+                            else store_piece<T, VE, NV>((T*)P.a.dq.data + (int64_t)rw.z * P.a.dq.row_stride + (int64_t)hh * P.a.dq.head_stride, t, tl, D, o);
+                        }
+                    }
+                }
+            } else {
+                if (batch & FIRST) {
+                    pieces(slot, U * S::EDGE, x0[0]);
+                    pieces(slot, U * S::EDGE + NV, x1[0]);
+#pragma unroll
+                    for (int c = 0; c < N2; ++c) acc[0][c] = acc[1][c] = 0;
+                }
+                float s[2 * U * G];
+                f32x2 q[U][G][N2], go[U][G][N2];
+#pragma unroll
+                for (int j = 0; j < U; ++j)
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        pieces(slot, j * S::EDGE + i * 2 * NV, q[j][i]);
+                        pieces(slot, j * S::EDGE + i * 2 * NV + NV, go[j][i]);
+                        s[j * G + i] = dot2(q[j][i], x0[0]);
+                        s[U * G + j * G + i] = dot2(go[j][i], x1[0]);
+                    }
+                ring_sum<2 * U * G>(s, tl);
+#pragma unroll
+                for (int j = 0; j < U; ++j)
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        const float2 st = *reinterpret_cast<const float2*>(mine + slot * S::SLOT + S::PIECES + ((j * G + i) * 32 + lane) * 8);
+                        const float p = on(j) ? fast_exp2(fmaf(s[j * G + i], c2, -st.x)) : 0.f;
+                        const float ds = on(j) ? p * (s[U * G + j * G + i] - st.y) : 0.f;
+                        axpy2(p, go[j][i], acc[1]);
+                        axpy2(ds, q[j][i], acc[0]);
+                    }
+                if (batch & LAST) {
+                    const int4 rw = rows_s[(batch >> 8) & 255];
+                    if (rw.w >= 0) {
+                        if (!P.chunk_mode) scale2(P.a.scale, acc[0]);
+                        float dk[E], dv[E];
+                        unpair(acc[0], dk);
+                        unpair(acc[1], dv);
+                        if (P.chunk_mode) {
+                            float* part = P.partial + ((int64_t)rw.w * P.a.kv_heads + h) * 2 * D;
+                            store_partial<VE, NV>(part, t, tl, D, dk);
+                            store_partial<VE, NV>(part + D, t, tl, D, dv);
+                        } else {
+                            store_piece<T, VE, NV>((T*)P.a.dk.data + (int64_t)rw.z * P.a.dk.row_stride + (int64_t)h * P.a.dk.head_stride, t, tl, D, dk);
+                            store_piece<T, VE, NV>((T*)P.a.dv.data + (int64_t)rw.z * P.a.dv.row_stride + (int64_t)h * P.a.dv.head_stride, t, tl, D, dv);
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            slot = slot + 1 == RING_SLOTS ? 0 : slot + 1;
+            ahead = ahead + 1 == RING_SLOTS ? 0 : ahead + 1;
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+}
+
+}  // namespace gs

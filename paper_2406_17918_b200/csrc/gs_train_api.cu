@@ -84,7 +84,7 @@ gs_status check_attention(const gs_block* b, int32_t max_row, gs_dtype t, int32_
     if (!known(t)) return set_error(GS_ERR_ARG, "unknown dtype %d", (int)t);
     if (max_row < 0) return set_error(GS_ERR_ARG, "max_row is negative");
     if (dim < 1 || dim > 256) return set_error(GS_ERR_ARG, "head_dim %d outside [1, 256]", dim);
-    if (q_heads < 1 || q_heads > 1024 || kv_heads < 1 || q_heads % kv_heads) return set_error(GS_ERR_ARG, "q_heads %d, kv_heads %d: 1 to 1024, the second a divisor of the first", q_heads, kv_heads);
+    if (q_heads < 1 || q_heads > 128 || kv_heads < 1 || q_heads % kv_heads) return set_error(GS_ERR_ARG, "q_heads %d, kv_heads %d: 1 to 128, the second a divisor of the first", q_heads, kv_heads);
     a->indptr = b->d_indptr;
     a->indices = b->d_indices;
     a->dst = Count{b->d_num_dst, b->max_dst};
@@ -162,7 +162,7 @@ gs_status gs_embedding_backward_sparse(const void* d_dout, gs_dtype dout_dtype, 
 gs_status gs_block_attention_workspace_bytes(int32_t max_dst, int32_t max_edges, int32_t q_heads, int32_t head_dim, size_t* bytes) {
     if (!bytes) return set_error(GS_ERR_ARG, "bytes is NULL");
     if (max_dst < 0 || max_edges < 0 || max_edges >= (1 << 30)) return set_error(GS_ERR_ARG, "a size of the block is out of range");
-    if (q_heads < 1 || q_heads > 1024 || head_dim < 1 || head_dim > 256) return set_error(GS_ERR_ARG, "q_heads outside [1, 1024] or head_dim outside [1, 256]");
+    if (q_heads < 1 || q_heads > 128 || head_dim < 1 || head_dim > 256) return set_error(GS_ERR_ARG, "q_heads outside [1, 128] or head_dim outside [1, 256]");
     *bytes = attention_workspace(max_dst, max_edges, q_heads, head_dim);
     return GS_OK;
 }
