@@ -88,6 +88,13 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
     asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
                  ::"r"(d), "r"(a), "l"(b), "r"(inst), "r"((uint32_t)add) : "memory");
 }
+// One lane of a converged warp.  Roles of one thread are written for the whole warp, with this around the
+// instructions proper: the operands then are uniform values, which the instructions take without a detour.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(p));
+    return p != 0;
+}
 
 // 32 (16) consecutive columns of this warp's 32 lanes, one lane per thread.
 __device__ __forceinline__ void ld32(uint32_t addr, uint32_t (&r)[32]) {

@@ -210,22 +210,23 @@ __global__ void __launch_bounds__(256) k_xent_finish(Xent a, Runs runs, int tile
 }
 
 // Rows of tiles that several runs share: their partial sums in order.  Block (c, .) takes the row in which run c is
-// the first to start inside.
+// the first to start inside: the run before it left slot 2c - 1, the runs c, c + 1, .. up to the row's end 2c, 2c + 2, ..
 template <XentMode M> __global__ void __launch_bounds__(256) k_xent_join(Xent a, Runs runs, int tile, int pitch, const float* __restrict__ partial) {
     const int nx = M == XE_DHIDDEN ? a.rows : (int)a.vocab;
     for (int64_t c = 1 + blockIdx.x; c < runs.parts; c += gridDim.x) {
         const int64_t t = runs.start(c), i = t / runs.tiles_y;
         if (t == i * runs.tiles_y || runs.start(c - 1) > i * runs.tiles_y) continue;
         const int64_t c1 = runs.run_of((i + 1) * runs.tiles_y - 1);
-        for (int e = blockIdx.y * 256 + threadIdx.x; e < tile * a.dim; e += gridDim.y * 256) {
-            const int r = e / a.dim, col = e - r * a.dim;
-            if (i * tile + r >= nx) break;
-            float acc = 0.f;
-#pragma unroll 4
-            for (int64_t k = c - 1; k <= c1; ++k) acc += __ldcg(partial + (runs.slot(k, i) * tile + r) * pitch + col);
-            if (M == XE_DHIDDEN) a.store_dhidden(i * tile + r, col, acc);
-            else a.store_dtable(i * tile + r, col, acc);
-        }
+        const int e = blockIdx.y * 256 + threadIdx.x, r = e / pitch, col = e - r * pitch;
+        if (r >= tile || i * tile + r >= nx || col >= a.dim) continue;
+        const float* p = partial + ((2 * c - 1) * tile + r) * pitch + col;
+        const int64_t step = (int64_t)tile * pitch;
+        float acc = __ldcg(p);
+        p += step;
+#pragma unroll 8
+        for (int64_t k = c; k <= c1; ++k, p += 2 * step) acc += __ldcg(p);
+        if (M == XE_DHIDDEN) a.store_dhidden(i * tile + r, col, acc);
+        else a.store_dtable(i * tile + r, col, acc);
     }
 }
 
@@ -252,7 +253,7 @@ template <typename T, XentMode M> static void run_simt(XentSimt& P, cudaStream_t
 
 template <XentMode M> static void run_join(const Xent& a, const Runs& runs, int tile, int pitch, const float* partial, cudaStream_t s) {
     if (runs.parts < 2) return;
-    const int by = (tile * a.dim + 1023) / 1024;
+    const int by = (tile * pitch + 255) / 256;
     k_xent_join<M><<<dim3((unsigned)limit_grid(runs.parts - 1), (unsigned)by), 256, 0, s>>>(a, runs, tile, pitch, partial);
     count_launches(1);
 }
@@ -271,7 +272,7 @@ cudaError_t launch_xent_forward(const Xent& a, void* workspace, cudaStream_t s) 
         const float* picked;
         const cudaError_t e = launch_xent_tc_forward(a, workspace, &runs, &stats, &picked, s);
         if (e != cudaSuccess) return e;
-        k_xent_finish<<<(int)finish, 256, 0, s>>>(a, runs, XENT_TC_TILE, 2, stats, picked);
+        k_xent_finish<<<(int)finish, 256, 0, s>>>(a, runs, XENT_TC_TILE, XENT_TC_STATS, stats, picked);
         count_launches(1);
         return cudaGetLastError();
     }

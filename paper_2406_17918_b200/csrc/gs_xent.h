@@ -32,6 +32,7 @@ inline Runs make_runs(int64_t x, int64_t tile_x, int64_t y, int64_t tile_y, int6
 }
 
 constexpr int XENT_TC_TILE = 128;       // rows of either operand per tile of the tensor-core kernels
+constexpr int XENT_TC_STATS = 4;        // entries of forward statistics per run and row of tiles
 constexpr int XENT_TC_MAX_DIM = 256;    // a gradient tile of 128 rows and S of two units fill the 512 columns of tensor memory
 
 struct Xent;

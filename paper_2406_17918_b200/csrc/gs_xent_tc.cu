@@ -20,7 +20,7 @@
 namespace gs {
 
 constexpr int XT = XENT_TC_TILE;
-constexpr int XT_THREADS = 384;            // 4 warps of roles, 2 softmax warpgroups
+constexpr int XT_THREADS = 640;            // 4 warps of roles, 4 softmax warpgroups: two per unit, 64 columns each
 constexpr int XT_CHUNK = XT * 128;         // bytes of a tile's 64 columns
 constexpr int XT_MAX_STAGES = 8;
 constexpr float XT_LOG2E = 1.4426950408889634f;
@@ -33,13 +33,52 @@ __device__ __forceinline__ float xt_exp2(float x) {
     return y;
 }
 
+// 2^x for x <= 0 by the multiply-add units, two at a time: x = n + f with n the nearest integer (taken from the low bits
+// of x + 1.5 * 2^23), 2^f by a polynomial on [-1/2, 1/2] (minimax in relative error with the constant 1 fixed, found by
+// reweighted least squares: 1.9e-7 with degree 5, 2.9e-6 with degree 4), 2^n from its exponent bits.  x is cut at -126; NaN
+// passes through.  The special-function units give 16 exponentials per clock and SM; every third pair or so comes from here.
+template <int DEGREE> __device__ __forceinline__ f32x2 exp2_by_fma(f32x2 x) {
+    constexpr float C5[5] = {0.6931470036506653f, 0.24022242426872253f, 0.05550733581185341f, 0.009671512991189957f, 0.001326472731307149f};
+    constexpr float C4[4] = {0.6931241750717163f, 0.24024099111557007f, 0.055906426161527634f, 0.009582852944731712f};
+    float lo, hi;
+    split(x, lo, hi);
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(lo) : "f"(-126.f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(hi) : "f"(-126.f));
+    x = pair(lo, hi);
+    const f32x2 magic = pair(12583039.f, 12583039.f), minus = pair(-12583039.f, -12583039.f), one = pair(1.f, 1.f), neg = pair(-1.f, -1.f);
+    const f32x2 r = add2(x, magic);                       // 1.5 * 2^23 + 127 + n
+    const f32x2 f = fma2(add2(r, minus), neg, x);
+    f32x2 p;
+    if constexpr (DEGREE == 5) {
+        p = pair(C5[4], C5[4]);
+#pragma unroll
+        for (int i = 3; i >= 0; --i) p = fma2(p, f, pair(C5[i], C5[i]));
+    } else {
+        p = pair(C4[3], C4[3]);
+#pragma unroll
+        for (int i = 2; i >= 0; --i) p = fma2(p, f, pair(C4[i], C4[i]));
+    }
+    p = fma2(p, f, one);
+    split(r, lo, hi);
+    return mul2(p, pair(__uint_as_float(__float_as_uint(lo) << 23), __uint_as_float(__float_as_uint(hi) << 23)));
+}
+
+// 2^x of pair j of 16: the share of the multiply-add units is 6 of 16 pairs forward, 4 of 16 backward (there the
+// tensor cores set the pace).
+template <bool FORWARD> __device__ __forceinline__ f32x2 exp2_pair(f32x2 x, int j) {
+    if (FORWARD ? (j % 8 == 1 || j % 8 == 4 || j % 8 == 6) : j % 4 == 1) return exp2_by_fma<FORWARD ? 5 : 4>(x);
+    float lo, hi;
+    split(x, lo, hi);
+    return pair(xt_exp2(lo), xt_exp2(hi));
+}
+
 struct XentTc {
     Xent a;
     Runs runs;
     int nx, ny;
-    int chunks, ksteps, on;      // 64-column pieces of a row, 16-column steps, columns of O (a multiple of 16)
-    int stages, xbufs, obufs;
-    float2* stats;               // forward: [parts + tiles_x][2][XT]
+    int on;                      // columns of O: dim rounded up to 16
+    int stages;
+    float2* stats;               // forward: [parts + tiles_x][XENT_TC_STATS][XT]
     float* picked;
     float* partial;              // backward: [2 parts][XT][on]
 };
@@ -90,20 +129,33 @@ __device__ __forceinline__ void store_columns(void* to, gs_dtype t, int64_t at, 
 
 enum { TC_FORWARD = 0, TC_DHIDDEN = 1, TC_DTABLE = 2 };
 
-template <int M>
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float r;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// CHUNKS: 64-column pieces of a row, known at compile time so that the issuing warp's code is straight.
+template <int M, int CHUNKS>
 __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant__ XentTc P, const __grid_constant__ CUtensorMap xmap,
                                                            const __grid_constant__ CUtensorMap ymap) {
     extern __shared__ unsigned char tiles[];
     __shared__ __align__(8) unsigned long long bars[2 * XT_MAX_STAGES + 17];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_stop;
-    constexpr int COLS = M == TC_DTABLE ? XT : 4;
-    __shared__ __align__(16) float col_lse[8][COLS], col_g[8][COLS];   // dw: of the unit's hidden rows, a copy per softmax warp
-    __shared__ __align__(16) int col_label[8][COLS];
+    constexpr int COLS = M == TC_DTABLE ? XT / 2 : 4;
+    __shared__ __align__(16) float col_lse[16][COLS], col_g[16][COLS];   // dw: -lse (base 2) and gradient of the unit's hidden rows, a copy per softmax warp
+    __shared__ __align__(16) int col_label[16][COLS];
     constexpr int SBUFS = M == TC_FORWARD ? 4 : 2;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tile_bytes = (uint32_t)P.chunks * XT_CHUNK;
-    const uint32_t xbase = (tc::smem_addr(tiles) + 1023) & ~1023u, ring = xbase + P.xbufs * tile_bytes;
+    const int warp = __shfl_sync(FULL, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    constexpr uint32_t tile_bytes = CHUNKS * XT_CHUNK;
+    constexpr int OBUFS = CHUNKS <= 2 ? 2 : 1, XBUFS = CHUNKS <= 2 ? 2 : 1;
+    const uint32_t xbase = (tc::smem_addr(tiles) + 1023) & ~1023u, ring = xbase + XBUFS * tile_bytes;
     const uint32_t b0 = tc::smem_addr(bars);
     auto full = [&](int i) { return b0 + 8 * i; };
     auto empty = [&](int i) { return b0 + 8 * (XT_MAX_STAGES + i); };
@@ -124,13 +176,13 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
         }
         for (int i = 0; i < 4; ++i) {
             tc::mbar_init(s_full(i), 1);
-            tc::mbar_init(p_full(i), 128);
+            tc::mbar_init(p_full(i), 256);
         }
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(x_full(i), 1);
             tc::mbar_init(x_free(i), 1);
             tc::mbar_init(o_full(i), 1);
-            tc::mbar_init(o_free(i), 256);
+            tc::mbar_init(o_free(i), 512);
         }
         tc::mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -140,28 +192,34 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    const uint32_t tmem = s_tmem;
+    const uint32_t tmem = __shfl_sync(FULL, s_tmem, 0);
     Segments seg(P.runs, blockIdx.x, gridDim.x);
     int64_t run, xi;
     int y0, n;
 
     if (warp == 0) {
-        if (lane == 0) {                                   // ---- loads
+        {                                                  // ---- loads
             int st = 0, issued = 0, segs = 0;
             uint32_t ph = 0;
             bool ok = true;
             while (ok && seg.next(run, xi, y0, n)) {
-                const int xb = segs % P.xbufs;
-                if (segs >= P.xbufs) ok = tc::mbar_wait(x_free(xb), (uint32_t)(segs / P.xbufs - 1) & 1, &s_stop);
+                const int xb = segs % XBUFS;
+                if (segs >= XBUFS) ok = __all_sync(FULL, tc::mbar_wait(x_free(xb), (uint32_t)(segs / XBUFS - 1) & 1, &s_stop));
                 if (!ok) break;
-                tc::mbar_expect(x_full(xb), tile_bytes);
-                for (int c = 0; c < P.chunks; ++c) tc::tma_load(xbase + xb * tile_bytes + c * XT_CHUNK, &xmap, c * 64, (int)(xi * XT), x_full(xb));
+                if (tc::elect_one()) {
+                    tc::mbar_expect(x_full(xb), tile_bytes);
+                    for (int c = 0; c < CHUNKS; ++c) tc::tma_load(xbase + xb * tile_bytes + c * XT_CHUNK, &xmap, c * 64, (int)(xi * XT), x_full(xb));
+                }
+                __syncwarp();
                 ++segs;
                 for (int i = 0; i < n; ++i) {
-                    if (issued >= P.stages) ok = tc::mbar_wait(empty(st), ph ^ 1, &s_stop);
+                    if (issued >= P.stages) ok = __all_sync(FULL, tc::mbar_wait(empty(st), ph ^ 1, &s_stop));
                     if (!ok) break;
-                    tc::mbar_expect(full(st), tile_bytes);
-                    for (int c = 0; c < P.chunks; ++c) tc::tma_load(ring + st * tile_bytes + c * XT_CHUNK, &ymap, c * 64, (y0 + i) * XT, full(st));
+                    if (tc::elect_one()) {
+                        tc::mbar_expect(full(st), tile_bytes);
+                        for (int c = 0; c < CHUNKS; ++c) tc::tma_load(ring + st * tile_bytes + c * XT_CHUNK, &ymap, c * 64, (y0 + i) * XT, full(st));
+                    }
+                    __syncwarp();
                     ++issued;
                     if (++st == P.stages) {
                         st = 0;
@@ -174,80 +232,93 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
             const long long begin = clock64();
             for (int j = issued > P.stages ? issued - P.stages : 0; j < issued; ++j)
                 while (!tc::mbar_try(full(j % P.stages), (uint32_t)(j / P.stages) & 1) && clock64() - begin < tc::WAIT_CLOCKS) {}
-            for (int j = segs > P.xbufs ? segs - P.xbufs : 0; j < segs; ++j)
-                while (!tc::mbar_try(x_full(j % P.xbufs), (uint32_t)(j / P.xbufs) & 1) && clock64() - begin < tc::WAIT_CLOCKS) {}
+            for (int j = segs > XBUFS ? segs - XBUFS : 0; j < segs; ++j)
+                while (!tc::mbar_try(x_full(j % XBUFS), (uint32_t)(j / XBUFS) & 1) && clock64() - begin < tc::WAIT_CLOCKS) {}
         }
-    } else if (warp == 1) {
-        if (lane == 0) {                                   // ---- products
-            const uint32_t si = tc::instruction(XT, false), oi = tc::instruction(P.on, true);
-            int st = 0;
-            uint32_t ph = 0;
-            bool ok = true;
-            int64_t u = 0;
-            // the unit whose second product is still to be issued
-            bool pending = false, p_first = false, p_last = false;
-            int p_st = 0, p_ob = 0, p_seg = 0;
-            auto second = [&](int64_t pu) {
-                const int b = (int)(pu & 1);
-                ok = ok && tc::mbar_wait(p_full(b), (uint32_t)(pu >> 1) & 1, &s_stop);
-                if (ok && p_first && p_seg >= P.obufs) ok = tc::mbar_wait(o_free(p_ob), (uint32_t)(p_seg / P.obufs - 1) & 1, &s_stop);
-                if (!ok) return;
-                tc::fence_after();
-                const uint32_t o = tmem + 256 + p_ob * 128, z = tmem + b * XT;
-                for (int k = 0; k < XT / 16; ++k)
-                    tc::mma_ts(o, z + k * 8, tc::operand(ring + p_st * tile_bytes + k * 2048, XT_CHUNK, 1024), oi, !(p_first && k == 0));
+    } else if (warp == 1) {                                // ---- products
+        const uint32_t si = tc::instruction(XT, false), oi = tc::instruction(P.on, true);
+        const uint64_t xd = tc::operand(xbase, 16, 1024), yd = tc::operand(ring, 16, 1024), zd = tc::operand(ring, XT_CHUNK, 1024);
+        const uint32_t tile_step = tile_bytes >> 4;        // in the operands' units of 16 bytes
+        int st = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        uint32_t u = 0;
+        // the unit whose second product is still to be issued
+        bool pending = false, p_first = false, p_last = false;
+        int p_st = 0, p_ob = 0, p_seg = 0;
+        auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(FULL, tc::mbar_wait(bar, parity, &s_stop)); };
+        auto second = [&](uint32_t pu) {
+            const int b = (int)(pu & 1);
+            wait(p_full(b), (uint32_t)(pu >> 1) & 1);
+            if (p_first && p_seg >= OBUFS) wait(o_free(p_ob), (uint32_t)(p_seg / OBUFS - 1) & 1);
+            if (!ok) return;
+            tc::fence_after();
+            const uint32_t o = tmem + 256 + p_ob * 128, z = tmem + b * XT;
+            const uint64_t d = zd + (uint32_t)p_st * tile_step;
+            if (tc::elect_one()) {
+#pragma unroll
+                for (int k = 0; k < XT / 16; ++k)          // Z lies in two halves, each over the columns of S it came from
+                    tc::mma_ts(o, z + (k < 4 ? 0 : 32) + k * 8, d + k * 128, oi, !(p_first && k == 0));
                 tc::commit(empty(p_st));
                 if (p_last) tc::commit(o_full(p_ob));
-                pending = false;
-            };
-            for (int s = 0; ok && seg.next(run, xi, y0, n); ++s) {
-                const int xb = s % P.xbufs;
-                ok = tc::mbar_wait(x_full(xb), (uint32_t)(s / P.xbufs) & 1, &s_stop);
-                for (int i = 0; i < n && ok; ++i, ++u) {
-                    ok = tc::mbar_wait(full(st), ph, &s_stop);
-                    const int b = (int)(u % SBUFS);
-                    if (M == TC_FORWARD && u >= SBUFS) ok = ok && tc::mbar_wait(p_full(b), (uint32_t)(u / SBUFS - 1) & 1, &s_stop);
-                    if (!ok) break;
-                    tc::fence_after();
-                    for (int k = 0; k < P.ksteps; ++k) {
-                        const uint32_t off = (k >> 2) * XT_CHUNK + (k & 3) * 32;
-                        tc::mma_ss(tmem + b * XT, tc::operand(xbase + xb * tile_bytes + off, 16, 1024), tc::operand(ring + st * tile_bytes + off, 16, 1024), si, k > 0);
-                    }
+            }
+            __syncwarp();
+            pending = false;
+        };
+        for (int s = 0; ok && seg.next(run, xi, y0, n); ++s) {
+            const int xb = s % XBUFS;
+            wait(x_full(xb), (uint32_t)(s / XBUFS) & 1);
+            for (int i = 0; i < n && ok; ++i, ++u) {
+                wait(full(st), ph);
+                const int b = (int)(u % SBUFS);
+                if (M == TC_FORWARD && u >= SBUFS) wait(p_full(b), (uint32_t)(u / SBUFS - 1) & 1);
+                if (!ok) break;
+                tc::fence_after();
+                const uint64_t a = xd + (uint32_t)xb * tile_step, y = yd + (uint32_t)st * tile_step;
+                const uint32_t d = tmem + b * XT;
+                if (tc::elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < CHUNKS * 4; ++k)       // columns behind dim are zero in both operands
+                        tc::mma_ss(d, a + (k >> 2) * (XT_CHUNK >> 4) + (k & 3) * 2, y + (k >> 2) * (XT_CHUNK >> 4) + (k & 3) * 2, si, k > 0);
                     tc::commit(s_full(b));
                     if (i + 1 == n) tc::commit(x_free(xb));
-                    if (M == TC_FORWARD) {
-                        tc::commit(empty(st));
-                    } else {
-                        if (pending) second(u - 1);
-                        pending = true;
-                        p_first = i == 0;
-                        p_last = i + 1 == n;
-                        p_st = st;
-                        p_seg = s;
-                        p_ob = s % P.obufs;
-                    }
-                    if (++st == P.stages) {
-                        st = 0;
-                        ph ^= 1;
-                    }
+                    if (M == TC_FORWARD) tc::commit(empty(st));
+                }
+                __syncwarp();
+                if (M != TC_FORWARD) {
+                    if (pending) second(u - 1);
+                    pending = true;
+                    p_first = i == 0;
+                    p_last = i + 1 == n;
+                    p_st = st;
+                    p_seg = s;
+                    p_ob = s % OBUFS;
+                }
+                if (++st == P.stages) {
+                    st = 0;
+                    ph ^= 1;
                 }
             }
-            if (M != TC_FORWARD && ok && pending) second(u - 1);
-            if (!ok) {
+        }
+        if (M != TC_FORWARD && ok && pending) second(u - 1);
+        if (!ok) {
+            // products already issued still write tensor memory: wait for them before it is freed
+            if (tc::elect_one()) {
                 atomicExch(&g_xent_gave_up, 1);
-                // products already issued still write tensor memory: wait for them before it is freed
                 tc::commit(drained);
-                const long long begin = clock64();
-                while (!tc::mbar_try(drained, 0) && clock64() - begin < tc::WAIT_CLOCKS) {}
             }
+            __syncwarp();
+            const long long begin = clock64();
+            while (!tc::mbar_try(drained, 0) && clock64() - begin < tc::WAIT_CLOCKS) {}
         }
     } else if (warp >= 4) {                                // ---- softmax
-        const int wg = (warp >> 2) - 1, sw = warp - 4, row = (warp & 3) * 32 + lane;
+        const int sw = warp - 4, wg = sw >> 2, half = wg & 1, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 lanes of tensor memory
         const float c2 = P.a.scale * XT_LOG2E;
         bool ok = true;
-        int64_t u = 0;
-        for (int s = 0; ok && seg.next(run, xi, y0, n); ++s) {
+        uint32_t u = 0;
+        int segment = 0;
+        while (ok && seg.next(run, xi, y0, n)) {
             const int64_t x = xi * XT + row;
             float lse2 = 0.f, m = -INFINITY, l = 0.f;
             int label = -1;
@@ -257,16 +328,16 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                 if (M == TC_DHIDDEN) lse2 = __ldg(P.a.lse + x) * XT_LOG2E;
             }
             for (int i = 0; i < n && ok; ++i, ++u) {
-                if ((int)(u & 1) != wg) continue;
-                const int b = (int)(u % SBUFS), ybase = (y0 + i) * XT;
+                if ((int)(u & 1) != wg >> 1) continue;
+                const int b = (int)(u % SBUFS), ybase = (y0 + i) * XT + half * 64;
                 if (M == TC_DTABLE) {                      // lse, upstream gradient and label of the unit's hidden rows
                     __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
+                    for (int j = 0; j < 2; ++j) {
                         const int h = ybase + j * 32 + lane, lab = h < P.ny ? __ldg(P.a.labels + h) : -1;
                         const bool valid = lab >= 0 && lab < P.a.vocab;
                         col_label[sw][j * 32 + lane] = valid ? lab : -1;
-                        col_lse[sw][j * 32 + lane] = h < P.ny ? __ldg(P.a.lse + h) * XT_LOG2E : 0.f;
+                        col_lse[sw][j * 32 + lane] = h < P.ny ? __ldg(P.a.lse + h) * -XT_LOG2E : 0.f;
                         col_g[sw][j * 32 + lane] = valid ? __ldg(P.a.dloss + h) * P.a.scale : 0.f;
                     }
                     __syncwarp();
@@ -275,100 +346,126 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                 ok = __all_sync(FULL, ok);
                 if (!ok) break;
                 tc::fence_after();
-                const uint32_t sa = tmem + b * XT + lanes;
-                uint32_t r[2][32];
-                tc::ld32(sa, r[0]);
-                tc::wait_ld(r[0]);
+                const uint32_t sa = tmem + b * XT + half * 64 + lanes;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t (&q)[32] = r[c & 1];
-                    if (c < 3) tc::ld32(sa + 32 * (c + 1), r[(c + 1) & 1]);
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t q[32];
+                    tc::ld32(sa + 32 * c, q);
+                    tc::wait_ld(q);
                     const int col = ybase + c * 32;
-                    float f[32];
+                    f32x2 f[16];
                     if (M == TC_FORWARD) {
+                        if (c == 1) {                      // S is in registers: the buffer may be overwritten
+                            tc::fence_before();
+                            tc::mbar_arrive(p_full(b));
+                        }
+                        float cc = c2;
+                        if (col + 32 > P.ny) {             // behind the table's last row
+                            cc = 1.f;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(q[j]) * c2;
-                        if (col + 32 > P.ny) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (col + j >= P.ny) f[j] = -INFINITY;
+                            for (int j = 0; j < 32; ++j) q[j] = col + j < P.ny ? __float_as_uint(__uint_as_float(q[j]) * c2) : 0xFF800000u;
                         }
                         if (__any_sync(FULL, label >= col && label < col + 32)) {
                             float z = 0.f;
 #pragma unroll
                             for (int j = 0; j < 32; ++j)
-                                if (col + j == label) z = f[j];
+                                if (col + j == label) z = __uint_as_float(q[j]) * cc;
                             if (label >= col && label < col + 32) P.picked[x] = z;
                             __syncwarp();
                         }
-                        float top = m;
+                        float e[4];                        // the largest product with cc comes from the largest or the smallest S
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) top = fmaxf(top, f[j]);
-                        const float ref = top == -INFINITY ? 0.f : top;
-                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                        for (int j = 0; j < 4; ++j) e[j] = __uint_as_float(q[j]);
+                        if (cc >= 0.f) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) sum[j & 3] += xt_exp2(f[j] - ref);
-                        l = l * xt_exp2(m - ref) + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+                            for (int j = 4; j < 32; j += 8)
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) e[k] = j < 28 ? max3(e[k], __uint_as_float(q[j + k]), __uint_as_float(q[(j + k + 4) & 31])) : fmaxf(e[k], __uint_as_float(q[j + k]));
+                            e[0] = fmaxf(max3(e[0], e[1], e[2]), e[3]);
+                        } else {
+#pragma unroll
+                            for (int j = 4; j < 32; j += 8)
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) e[k] = j < 28 ? min3(e[k], __uint_as_float(q[j + k]), __uint_as_float(q[(j + k + 4) & 31])) : fminf(e[k], __uint_as_float(q[j + k]));
+                            e[0] = fminf(min3(e[0], e[1], e[2]), e[3]);
+                        }
+                        const float top = fmaxf(m, e[0] * cc), ref = top == -INFINITY ? 0.f : top;
+                        const f32x2 c22 = pair(cc, cc), r2 = pair(-ref, -ref);
+                        f32x2 sum[2] = {0, 0};
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            sum[j & 1] = add2(sum[j & 1], exp2_pair<true>(fma2(pair(__uint_as_float(q[2 * j]), __uint_as_float(q[2 * j + 1])), c22, r2), j));
+                        float lo, hi;
+                        split(add2(sum[0], sum[1]), lo, hi);
+                        l = l * xt_exp2(m - ref) + (lo + hi);
                         m = top;
                     } else {
+                        const f32x2 c22 = pair(c2, c2);
                         if (M == TC_DHIDDEN) {
+                            const f32x2 r2 = pair(-lse2, -lse2);
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) f[j] = xt_exp2(fmaf(__uint_as_float(q[j]), c2, -lse2));
+                            for (int j = 0; j < 16; ++j)
+                                f[j] = exp2_pair<false>(fma2(pair(__uint_as_float(q[2 * j]), __uint_as_float(q[2 * j + 1])), c22, r2), j);
                             if (__any_sync(FULL, label >= col && label < col + 32)) {
 #pragma unroll
-                                for (int j = 0; j < 32; ++j)
-                                    if (col + j == label) f[j] -= 1.f;
+                                for (int j = 0; j < 16; ++j)
+                                    f[j] = add2(f[j], pair(col + 2 * j == label ? -1.f : 0.f, col + 2 * j + 1 == label ? -1.f : 0.f));
                             }
                             if (col + 32 > P.ny) {
 #pragma unroll
-                                for (int j = 0; j < 32; ++j)
-                                    if (col + j >= P.ny) f[j] = 0.f;
+                                for (int j = 0; j < 16; ++j) {
+                                    float lo, hi;
+                                    split(f[j], lo, hi);
+                                    f[j] = pair(col + 2 * j < P.ny ? lo : 0.f, col + 2 * j + 1 < P.ny ? hi : 0.f);
+                                }
                             }
                         } else {
 #pragma unroll
-                            for (int j = 0; j < 32; j += 4) {
-                                const float4 ls = *reinterpret_cast<const float4*>(&col_lse[sw][c * 32 + j]);
-                                f[j] = xt_exp2(fmaf(__uint_as_float(q[j]), c2, -ls.x));
-                                f[j + 1] = xt_exp2(fmaf(__uint_as_float(q[j + 1]), c2, -ls.y));
-                                f[j + 2] = xt_exp2(fmaf(__uint_as_float(q[j + 2]), c2, -ls.z));
-                                f[j + 3] = xt_exp2(fmaf(__uint_as_float(q[j + 3]), c2, -ls.w));
+                            for (int j = 0; j < 16; j += 2) {
+                                const float4 ls = *reinterpret_cast<const float4*>(&col_lse[sw][c * 32 + 2 * j]);
+                                f[j] = exp2_pair<false>(fma2(pair(__uint_as_float(q[2 * j]), __uint_as_float(q[2 * j + 1])), c22, pair(ls.x, ls.y)), j);
+                                f[j + 1] = exp2_pair<false>(fma2(pair(__uint_as_float(q[2 * j + 2]), __uint_as_float(q[2 * j + 3])), c22, pair(ls.z, ls.w)), j + 1);
                             }
-                            const int x_warp = (int)(xi * XT) + (warp & 3) * 32;
-                            const int lab = col_label[sw][c * 32 + lane] - x_warp;
+                            const int lab = col_label[sw][c * 32 + lane] - ((int)(xi * XT) + (warp & 3) * 32);
                             if (__any_sync(FULL, lab >= 0 && lab < 32)) {
 #pragma unroll
-                                for (int j = 0; j < 32; ++j)
-                                    if (__shfl_sync(FULL, lab, j) == lane) f[j] -= 1.f;
+                                for (int j = 0; j < 16; ++j) {
+                                    const int a = __shfl_sync(FULL, lab, 2 * j), d = __shfl_sync(FULL, lab, 2 * j + 1);
+                                    f[j] = add2(f[j], pair(a == lane ? -1.f : 0.f, d == lane ? -1.f : 0.f));
+                                }
                             }
 #pragma unroll
-                            for (int j = 0; j < 32; j += 4) {
-                                const float4 g = *reinterpret_cast<const float4*>(&col_g[sw][c * 32 + j]);
-                                f[j] *= g.x;
-                                f[j + 1] *= g.y;
-                                f[j + 2] *= g.z;
-                                f[j + 3] *= g.w;
+                            for (int j = 0; j < 16; j += 2) {
+                                const float4 g = *reinterpret_cast<const float4*>(&col_g[sw][c * 32 + 2 * j]);
+                                f[j] = mul2(f[j], pair(g.x, g.y));
+                                f[j + 1] = mul2(f[j + 1], pair(g.z, g.w));
                             }
                         }
                         uint32_t z[16];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) z[j] = pack_bf16(f[2 * j], f[2 * j + 1]);
-                        if (c < 3) tc::wait_ld(r[(c + 1) & 1]);    // the next columns are read before Z overwrites more of S
-                        tc::st16(sa + 16 * c, z);
+                        for (int j = 0; j < 16; ++j) {
+                            float lo, hi;
+                            split(f[j], lo, hi);
+                            z[j] = pack_bf16(lo, hi);
+                        }
+                        __syncwarp();
+                        tc::st16(sa + 16 * c, z);           // over columns of S that this warp has read
                     }
-                    if (M == TC_FORWARD && c < 3) tc::wait_ld(r[(c + 1) & 1]);
                 }
-                if (M != TC_FORWARD) tc::wait_st();
-                tc::fence_before();
-                tc::mbar_arrive(p_full(b));
+                if (M != TC_FORWARD) {
+                    tc::wait_st();
+                    tc::fence_before();
+                    tc::mbar_arrive(p_full(b));
+                }
             }
             if (!ok) break;
             if (M == TC_FORWARD) {
-                P.stats[((run + xi) * 2 + wg) * XT + row] = make_float2(m, l);
+                P.stats[((run + xi) * XENT_TC_STATS + wg) * XT + row] = make_float2(m, l);
                 continue;
             }
             // ---- the segment's sum
-            const int ob = s % P.obufs;
-            ok = tc::mbar_wait(o_full(ob), (uint32_t)(s / P.obufs) & 1, &s_stop);
+            const int s = segment++, ob = s % OBUFS;
+            ok = tc::mbar_wait(o_full(ob), (uint32_t)(s / OBUFS) & 1, &s_stop);
             ok = __all_sync(FULL, ok);
             if (!ok) break;
             tc::fence_after();
@@ -377,7 +474,7 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
             if (M == TC_DHIDDEN) factor = label >= 0 ? __ldg(P.a.dloss + x) * P.a.scale : 0.f;
             const bool zero = M == TC_DHIDDEN && factor == 0.f;
             float* part = P.partial + (P.runs.slot(run, xi) * XT + row) * P.on;
-            for (int c = wg * 16; c < P.on; c += 32) {
+            for (int c = wg * 16; c < P.on; c += 64) {
                 uint32_t q[16];
                 __syncwarp();
                 tc::ld16(tmem + 256 + ob * 128 + lanes + c, q);
@@ -468,7 +565,7 @@ static TcLayout tc_layout(const Xent& a) {
     }
     l.rest = off;
     const int64_t parts = sm_count(), tx = (a.rows + XT - 1) / XT;
-    const size_t fwd = align_up((size_t)(parts + tx) * 2 * XT * 8, 256) + align_up((size_t)a.rows * 4, 256);
+    const size_t fwd = align_up((size_t)(parts + tx) * XENT_TC_STATS * XT * 8, 256) + align_up((size_t)a.rows * 4, 256);
     const size_t bwd = (size_t)2 * parts * XT * ((a.dim + 15) / 16 * 16) * 4;
     take(fwd > bwd ? fwd : bwd);
     l.total = off;
@@ -520,24 +617,21 @@ template <int M> static cudaError_t run_tc(const Xent& a, const Operands& o, Xen
     P.nx = ON_X ? a.rows : (int)a.vocab;
     P.ny = ON_X ? (int)a.vocab : a.rows;
     P.runs = make_runs(P.nx, XT, P.ny, XT, sm_count());
-    P.chunks = (a.dim + 63) / 64;
-    P.ksteps = (a.dim + 15) / 16;
-    P.on = P.ksteps * 16;
-    const int tile = P.chunks * XT_CHUNK;
-    P.xbufs = P.chunks <= 2 ? 2 : 1;
-    P.stages = (192 << 10) / tile - P.xbufs;
+    const int chunks = (a.dim + 63) / 64, tile = chunks * XT_CHUNK, xbufs = chunks <= 2 ? 2 : 1;
+    P.on = (a.dim + 15) / 16 * 16;
+    P.stages = (192 << 10) / tile - xbufs;
     if (P.stages > XT_MAX_STAGES) P.stages = XT_MAX_STAGES;
-    P.obufs = P.on <= 128 ? 2 : 1;
     CUtensorMap hm, tm;
     cudaError_t e = row_map(&hm, o.hidden, a.rows, a.dim, o.hidden_ld);
     if (e == cudaSuccess) e = row_map(&tm, o.table, a.vocab, a.dim, o.table_ld);
     if (e != cudaSuccess) return e;
     // at least 120 KB, so that an SM holds one block: a block takes all of the tensor memory
-    int smem = (P.xbufs + P.stages) * tile + 1024;
+    int smem = (xbufs + P.stages) * tile + 1024;
     if (smem < (120 << 10)) smem = 120 << 10;
-    e = cudaFuncSetAttribute(k_xent_tc<M>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    auto kernel = chunks == 1 ? k_xent_tc<M, 1> : (chunks == 2 ? k_xent_tc<M, 2> : (chunks == 3 ? k_xent_tc<M, 3> : k_xent_tc<M, 4>));
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    k_xent_tc<M><<<(int)limit_grid(P.runs.parts), XT_THREADS, smem, s>>>(P, ON_X ? hm : tm, ON_X ? tm : hm);
+    kernel<<<(int)limit_grid(P.runs.parts), XT_THREADS, smem, s>>>(P, ON_X ? hm : tm, ON_X ? tm : hm);
     count_launches(1);
     return cudaGetLastError();
 }
@@ -549,7 +643,7 @@ cudaError_t launch_xent_tc_forward(const Xent& a, void* workspace, Runs* runs, c
     XentTc P{};
     const int64_t tx = (a.rows + XT - 1) / XT;
     P.stats = (float2*)o.rest;
-    P.picked = (float*)(o.rest + align_up((size_t)(sm_count() + tx) * 2 * XT * 8, 256));
+    P.picked = (float*)(o.rest + align_up((size_t)(sm_count() + tx) * XENT_TC_STATS * XT * 8, 256));
     e = run_tc<TC_FORWARD>(a, o, P, s);
     *runs = P.runs;
     *stats = P.stats;
