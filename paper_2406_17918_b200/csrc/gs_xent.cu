@@ -189,49 +189,57 @@ __global__ void __launch_bounds__(XS_THREADS) k_xent_simt(const __grid_constant_
     }
 }
 
-// lse and loss of every row from the runs' statistics.
+// lse and loss of every row from the runs' statistics: a warp per row, its lanes over the entries.
 __global__ void __launch_bounds__(256) k_xent_finish(Xent a, Runs runs, int tile, int per, const float2* __restrict__ stats, const float* __restrict__ picked) {
-    for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < a.rows; n += (int64_t)gridDim.x * 256) {
+    const int lane = threadIdx.x & 31;
+    for (int64_t n = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; n < a.rows; n += (int64_t)gridDim.x * 8) {
         const int64_t i = n / tile;
         const int64_t c0 = runs.run_of(i * runs.tiles_y), c1 = runs.run_of((i + 1) * runs.tiles_y - 1);
         float m = -INFINITY, l = 0.f;
-        for (int64_t c = (c0 + i) * per; c < (c1 + i + 1) * per; ++c) {      // `per` entries of a run, in order
+        for (int64_t c = (c0 + i) * per + lane; c < (c1 + i + 1) * per; c += 32) {      // `per` entries of a run
             const float2 s = stats[c * tile + n % tile];
             const float top = fmaxf(m, s.x), ref = top == -INFINITY ? 0.f : top;
             l = l * xe_exp2(m - ref) + s.y * xe_exp2(s.x - ref);
             m = top;
         }
-        const int lab = a.labels[n];
-        const bool valid = lab >= 0 && lab < a.vocab;
-        const float log2l = log2f(l);
-        a.lse_out[n] = (m + log2l) * XE_LN2;
-        a.loss[n] = valid ? ((m - picked[n]) + log2l) * XE_LN2 : 0.f;
+        for (int o = 16; o; o >>= 1) {
+            const float mo = __shfl_xor_sync(FULL, m, o), lo = __shfl_xor_sync(FULL, l, o);
+            const float top = fmaxf(m, mo), ref = top == -INFINITY ? 0.f : top;
+            l = l * xe_exp2(m - ref) + lo * xe_exp2(mo - ref);
+            m = top;
+        }
+        if (lane == 0) {
+            const int lab = a.labels[n];
+            const bool valid = lab >= 0 && lab < a.vocab;
+            const float log2l = log2f(l);
+            a.lse_out[n] = (m + log2l) * XE_LN2;
+            a.loss[n] = valid ? ((m - picked[n]) + log2l) * XE_LN2 : 0.f;
+        }
     }
 }
 
-// Rows of tiles that several runs share: their partial sums in order.  Block (c, .) takes the row in which run c is
-// the first to start inside: the run before it left slot 2c - 1, the runs c, c + 1, .. up to the row's end 2c, 2c + 2, ..
-template <XentMode M> __global__ void __launch_bounds__(256) k_xent_join(Xent a, Runs runs, int tile, int pitch, const float* __restrict__ partial) {
-    const int nx = M == XE_DHIDDEN ? a.rows : (int)a.vocab;
-    for (int64_t c = 1 + blockIdx.x; c < runs.parts; c += gridDim.x) {
-        const int64_t t = runs.start(c), i = t / runs.tiles_y;
-        if (t == i * runs.tiles_y || runs.start(c - 1) > i * runs.tiles_y) continue;
-        const int64_t c1 = runs.run_of((i + 1) * runs.tiles_y - 1);
-        const int e = blockIdx.y * 256 + threadIdx.x, r = e / pitch, col = e - r * pitch;
-        if (r >= tile || i * tile + r >= nx || col >= a.dim) continue;
-        const float* p = partial + ((2 * c - 1) * tile + r) * pitch + col;
-        const int64_t step = (int64_t)tile * pitch;
+// Rows of tiles that several runs share: their partial sums in order.  The run before the first that starts inside, c,
+// left slot 2c - 1, the runs c, c + 1, .. up to the row's end 2c, 2c + 2, ..
+template <XentMode M> __global__ void __launch_bounds__(256) k_xent_join(Xent a, const __grid_constant__ JoinList list, int tile, int pitch, const float* __restrict__ partial) {
+    const JoinList::Entry j = list.e[blockIdx.x];
+    const int64_t nx = M == XE_DHIDDEN ? a.rows : a.vocab, x0 = (int64_t)j.row * tile, step = (int64_t)tile * pitch;
+    const int rows = nx - x0 < tile ? (int)(nx - x0) : tile;
+    for (int e = blockIdx.y * 256 + threadIdx.x; e < rows * pitch; e += gridDim.y * 256) {
+        const int r = e / pitch, col = e - r * pitch;
+        if (col >= a.dim) continue;
+        const float* p = partial + (2 * (int64_t)j.first - 1) * step + e;
         float acc = __ldcg(p);
         p += step;
 #pragma unroll 8
-        for (int64_t k = c; k <= c1; ++k, p += 2 * step) acc += __ldcg(p);
-        if (M == XE_DHIDDEN) a.store_dhidden(i * tile + r, col, acc);
-        else a.store_dtable(i * tile + r, col, acc);
+        for (int k = 0; k < j.runs; ++k, p += 2 * step) acc += __ldcg(p);
+        if (M == XE_DHIDDEN) a.store_dhidden(x0 + r, col, acc);
+        else a.store_dtable(x0 + r, col, acc);
     }
 }
 
 // ---------------------------------------------------------------- launches
-static Runs simt_runs(int64_t x, int64_t y) { return make_runs(x, XS_TILE, y, XS_TILE, sm_count() * 2); }
+static int64_t simt_parts() { return sm_count() * 2 < MAX_JOINS ? sm_count() * 2 : MAX_JOINS; }
+static Runs simt_runs(int64_t x, int64_t y) { return make_runs(x, XS_TILE, y, XS_TILE, simt_parts()); }
 
 static size_t simt_workspace(const Xent& a) {
     const Runs f = simt_runs(a.rows, a.vocab), t = simt_runs(a.vocab, a.rows);
@@ -252,9 +260,13 @@ template <typename T, XentMode M> static void run_simt(XentSimt& P, cudaStream_t
 }
 
 template <XentMode M> static void run_join(const Xent& a, const Runs& runs, int tile, int pitch, const float* partial, cudaStream_t s) {
-    if (runs.parts < 2) return;
-    const int by = (tile * pitch + 255) / 256;
-    k_xent_join<M><<<dim3((unsigned)limit_grid(runs.parts - 1), (unsigned)by), 256, 0, s>>>(a, runs, tile, pitch, partial);
+    JoinList list;
+    const int n = list_joins(runs, &list);
+    if (!n) return;
+    // few shared rows: spread each over many blocks
+    int64_t by = (tile * pitch + 255) / 256, few = sm_count() * 8 / n + 1;
+    if (by > few) by = few;
+    k_xent_join<M><<<dim3((unsigned)n, (unsigned)by), 256, 0, s>>>(a, list, tile, pitch, partial);
     count_launches(1);
 }
 
@@ -265,7 +277,7 @@ cudaError_t launch_xent_join(const Xent& a, bool hidden, const Runs& runs, int t
 }
 
 cudaError_t launch_xent_forward(const Xent& a, void* workspace, cudaStream_t s) {
-    const int64_t finish = limit_grid((a.rows + 255) / 256);
+    const int64_t finish = limit_grid((a.rows + 7) / 8 < sm_count() * 8 ? (a.rows + 7) / 8 : sm_count() * 8);
     if (xent_tc_takes(a)) {
         Runs runs;
         const float2* stats;

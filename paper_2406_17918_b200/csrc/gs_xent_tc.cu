@@ -23,6 +23,7 @@ constexpr int XT = XENT_TC_TILE;
 constexpr int XT_THREADS = 640;            // 4 warps of roles, 4 softmax warpgroups: two per unit, 64 columns each
 constexpr int XT_CHUNK = XT * 128;         // bytes of a tile's 64 columns
 constexpr int XT_MAX_STAGES = 8;
+constexpr int XT_SHORT_ROWS = 16;          // rows of fewer tiles than this get two O
 constexpr float XT_LOG2E = 1.4426950408889634f;
 
 __device__ int g_xent_gave_up;
@@ -63,10 +64,12 @@ template <int DEGREE> __device__ __forceinline__ f32x2 exp2_by_fma(f32x2 x) {
     return mul2(p, pair(__uint_as_float(__float_as_uint(lo) << 23), __uint_as_float(__float_as_uint(hi) << 23)));
 }
 
-// 2^x of pair j of 16: the share of the multiply-add units is 6 of 16 pairs forward, 4 of 16 backward (there the
-// tensor cores set the pace).
+// 2^x of pair j of 16: the multiply-add units take 4 of 16 pairs forward, 2 of 16 backward (there the tensor cores set
+// the pace).  Measured at 8,192 x 169,343 x 128: forward 369 us with 4, 387 with 5, 396 with 6 pairs, 443 with none;
+// backward 1,083 us with 2, 1,078 with none (64 columns: 902 and 969), 1,098 with 4.
+constexpr int FMA_PAIRS_FORWARD = 0x2222, FMA_PAIRS_BACKWARD = 0x0202;
 template <bool FORWARD> __device__ __forceinline__ f32x2 exp2_pair(f32x2 x, int j) {
-    if (FORWARD ? (j % 8 == 1 || j % 8 == 4 || j % 8 == 6) : j % 4 == 1) return exp2_by_fma<FORWARD ? 5 : 4>(x);
+    if (((FORWARD ? FMA_PAIRS_FORWARD : FMA_PAIRS_BACKWARD) >> j) & 1) return exp2_by_fma<FORWARD ? 5 : 4>(x);
     float lo, hi;
     split(x, lo, hi);
     return pair(xt_exp2(lo), xt_exp2(hi));
@@ -78,10 +81,15 @@ struct XentTc {
     int nx, ny;
     int on;                      // columns of O: dim rounded up to 16
     int stages;
+    int sbufs, obufs;            // buffers of S and of O in tensor memory: O(i) starts at column 128 sbufs + i * on_pitch
+    int on_pitch;
     float2* stats;               // forward: [parts + tiles_x][XENT_TC_STATS][XT]
     float* picked;
     float* partial;              // backward: [2 parts][XT][on]
+    const float* row_info;       // dw: [tiles of hidden rows][3][XT]: -lse (base 2), upstream gradient times scale, label
 };
+constexpr int XT_INFO = 3 * XT * 4;        // bytes of a tile's row_info
+constexpr int XT_STAGING = 16 * 32 * 16 * 2; // bytes in which the softmax warps turn rows of bf16 that are not on 16 bytes
 
 // The block's runs, cut at rows of tiles.
 struct Segments {
@@ -129,6 +137,16 @@ __device__ __forceinline__ void store_columns(void* to, gs_dtype t, int64_t at, 
 
 enum { TC_FORWARD = 0, TC_DHIDDEN = 1, TC_DTABLE = 2 };
 
+__device__ __forceinline__ float4 shared_f4(uint32_t a) {
+    float4 r;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(r.x), "=f"(r.y), "=f"(r.z), "=f"(r.w) : "r"(a));
+    return r;
+}
+__device__ __forceinline__ int shared_i(uint32_t a) {
+    int r;
+    asm volatile("ld.shared.s32 %0, [%1];" : "=r"(r) : "r"(a));
+    return r;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -145,17 +163,16 @@ template <int M, int CHUNKS>
 __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant__ XentTc P, const __grid_constant__ CUtensorMap xmap,
                                                            const __grid_constant__ CUtensorMap ymap) {
     extern __shared__ unsigned char tiles[];
-    __shared__ __align__(8) unsigned long long bars[2 * XT_MAX_STAGES + 17];
+    __shared__ __align__(8) unsigned long long bars[2 * XT_MAX_STAGES + 22];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_stop;
-    constexpr int COLS = M == TC_DTABLE ? XT / 2 : 4;
-    __shared__ __align__(16) float col_lse[16][COLS], col_g[16][COLS];   // dw: -lse (base 2) and gradient of the unit's hidden rows, a copy per softmax warp
-    __shared__ __align__(16) int col_label[16][COLS];
-    constexpr int SBUFS = M == TC_FORWARD ? 4 : 2;
+    const int SBUFS = M == TC_FORWARD ? 4 : P.sbufs;
     const int warp = __shfl_sync(FULL, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     constexpr uint32_t tile_bytes = CHUNKS * XT_CHUNK;
-    constexpr int OBUFS = CHUNKS <= 2 ? 2 : 1, XBUFS = CHUNKS <= 2 ? 2 : 1;
+    constexpr int XBUFS = CHUNKS <= 2 ? 2 : 1;
     const uint32_t xbase = (tc::smem_addr(tiles) + 1023) & ~1023u, ring = xbase + XBUFS * tile_bytes;
+    const uint32_t info = ring + P.stages * tile_bytes;      // dw: row_info of the stages' tiles
+    const uint32_t staging = info + (M == TC_DTABLE ? P.stages * XT_INFO : 0);
     const uint32_t b0 = tc::smem_addr(bars);
     auto full = [&](int i) { return b0 + 8 * i; };
     auto empty = [&](int i) { return b0 + 8 * (XT_MAX_STAGES + i); };
@@ -166,7 +183,8 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
     auto x_free = [&](int i) { return b1 + 80 + 8 * i; };    // 2
     auto o_full = [&](int i) { return b1 + 96 + 8 * i; };    // 2
     auto o_free = [&](int i) { return b1 + 112 + 8 * i; };   // 2
-    const uint32_t drained = b1 + 128;
+    auto z_free = [&](int i) { return b1 + 128 + 8 * i; };   // 4: Z of a unit has been multiplied (backward)
+    auto drained = [&](int i) { return b1 + 160 + 8 * i; };  // 2: the products of a role that gives up
 
     if (threadIdx.x == 0) {
         s_stop = 0;
@@ -177,6 +195,7 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
         for (int i = 0; i < 4; ++i) {
             tc::mbar_init(s_full(i), 1);
             tc::mbar_init(p_full(i), 256);
+            tc::mbar_init(z_free(i), 1);
         }
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(x_full(i), 1);
@@ -184,7 +203,8 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
             tc::mbar_init(o_full(i), 1);
             tc::mbar_init(o_free(i), 512);
         }
-        tc::mbar_init(drained, 1);
+        tc::mbar_init(drained(0), 1);
+        tc::mbar_init(drained(1), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -193,6 +213,16 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
     __syncthreads();
     tc::fence_after();
     const uint32_t tmem = __shfl_sync(FULL, s_tmem, 0);
+    // A role that gives up: its products still write tensor memory, which must not be freed under them.
+    auto drain = [&](uint32_t bar) {
+        if (tc::elect_one()) {
+            atomicExch(&g_xent_gave_up, 1);
+            tc::commit(bar);
+        }
+        __syncwarp();
+        const long long begin = clock64();
+        while (!tc::mbar_try(bar, 0) && clock64() - begin < tc::WAIT_CLOCKS) {}
+    };
     Segments seg(P.runs, blockIdx.x, gridDim.x);
     int64_t run, xi;
     int y0, n;
@@ -216,7 +246,8 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                     if (issued >= P.stages) ok = __all_sync(FULL, tc::mbar_wait(empty(st), ph ^ 1, &s_stop));
                     if (!ok) break;
                     if (tc::elect_one()) {
-                        tc::mbar_expect(full(st), tile_bytes);
+                        tc::mbar_expect(full(st), tile_bytes + (M == TC_DTABLE ? XT_INFO : 0));
+                        if (M == TC_DTABLE) tc::bulk_load(info + st * XT_INFO, P.row_info + (int64_t)(y0 + i) * (XT_INFO / 4), XT_INFO, full(st));
                         for (int c = 0; c < CHUNKS; ++c) tc::tma_load(ring + st * tile_bytes + c * XT_CHUNK, &ymap, c * 64, (y0 + i) * XT, full(st));
                     }
                     __syncwarp();
@@ -235,43 +266,21 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
             for (int j = segs > XBUFS ? segs - XBUFS : 0; j < segs; ++j)
                 while (!tc::mbar_try(x_full(j % XBUFS), (uint32_t)(j / XBUFS) & 1) && clock64() - begin < tc::WAIT_CLOCKS) {}
         }
-    } else if (warp == 1) {                                // ---- products
-        const uint32_t si = tc::instruction(XT, false), oi = tc::instruction(P.on, true);
-        const uint64_t xd = tc::operand(xbase, 16, 1024), yd = tc::operand(ring, 16, 1024), zd = tc::operand(ring, XT_CHUNK, 1024);
-        const uint32_t tile_step = tile_bytes >> 4;        // in the operands' units of 16 bytes
-        int st = 0;
-        uint32_t ph = 0;
-        bool ok = true;
-        uint32_t u = 0;
-        // the unit whose second product is still to be issued
-        bool pending = false, p_first = false, p_last = false;
-        int p_st = 0, p_ob = 0, p_seg = 0;
+    } else if (warp == 1) {                                // ---- first products: S
+        const uint32_t inst = tc::instruction(XT, false);
+        const uint64_t xd = tc::operand(xbase, 16, 1024), yd = tc::operand(ring, 16, 1024);
+        constexpr uint32_t tile_step = tile_bytes >> 4;    // in the operands' units of 16 bytes
+        int st = 0, b = 0, segs = 0;
+        uint32_t ph = 0, bph = 0;
+        bool ok = true, reuse = false;
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(FULL, tc::mbar_wait(bar, parity, &s_stop)); };
-        auto second = [&](uint32_t pu) {
-            const int b = (int)(pu & 1);
-            wait(p_full(b), (uint32_t)(pu >> 1) & 1);
-            if (p_first && p_seg >= OBUFS) wait(o_free(p_ob), (uint32_t)(p_seg / OBUFS - 1) & 1);
-            if (!ok) return;
-            tc::fence_after();
-            const uint32_t o = tmem + 256 + p_ob * 128, z = tmem + b * XT;
-            const uint64_t d = zd + (uint32_t)p_st * tile_step;
-            if (tc::elect_one()) {
-#pragma unroll
-                for (int k = 0; k < XT / 16; ++k)          // Z lies in two halves, each over the columns of S it came from
-                    tc::mma_ts(o, z + (k < 4 ? 0 : 32) + k * 8, d + k * 128, oi, !(p_first && k == 0));
-                tc::commit(empty(p_st));
-                if (p_last) tc::commit(o_full(p_ob));
-            }
-            __syncwarp();
-            pending = false;
-        };
-        for (int s = 0; ok && seg.next(run, xi, y0, n); ++s) {
-            const int xb = s % XBUFS;
-            wait(x_full(xb), (uint32_t)(s / XBUFS) & 1);
-            for (int i = 0; i < n && ok; ++i, ++u) {
+        while (ok && seg.next(run, xi, y0, n)) {
+            const int xb = segs % XBUFS;
+            wait(x_full(xb), (uint32_t)(segs / XBUFS) & 1);
+            ++segs;
+            for (int i = 0; i < n; ++i) {
                 wait(full(st), ph);
-                const int b = (int)(u % SBUFS);
-                if (M == TC_FORWARD && u >= SBUFS) wait(p_full(b), (uint32_t)(u / SBUFS - 1) & 1);
+                if (reuse) wait(M == TC_FORWARD ? p_full(b) : z_free(b), bph ^ 1);
                 if (!ok) break;
                 tc::fence_after();
                 const uint64_t a = xd + (uint32_t)xb * tile_step, y = yd + (uint32_t)st * tile_step;
@@ -279,45 +288,74 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                 if (tc::elect_one()) {
 #pragma unroll
                     for (int k = 0; k < CHUNKS * 4; ++k)       // columns behind dim are zero in both operands
-                        tc::mma_ss(d, a + (k >> 2) * (XT_CHUNK >> 4) + (k & 3) * 2, y + (k >> 2) * (XT_CHUNK >> 4) + (k & 3) * 2, si, k > 0);
+                        tc::mma_ss(d, a + (k >> 2) * (XT_CHUNK >> 4) + (k & 3) * 2, y + (k >> 2) * (XT_CHUNK >> 4) + (k & 3) * 2, inst, k > 0);
                     tc::commit(s_full(b));
                     if (i + 1 == n) tc::commit(x_free(xb));
                     if (M == TC_FORWARD) tc::commit(empty(st));
                 }
                 __syncwarp();
-                if (M != TC_FORWARD) {
-                    if (pending) second(u - 1);
-                    pending = true;
-                    p_first = i == 0;
-                    p_last = i + 1 == n;
-                    p_st = st;
-                    p_seg = s;
-                    p_ob = s % OBUFS;
-                }
                 if (++st == P.stages) {
                     st = 0;
                     ph ^= 1;
                 }
+                if (++b == SBUFS) {
+                    b = 0;
+                    bph ^= 1;
+                    reuse = true;
+                }
             }
         }
-        if (M != TC_FORWARD && ok && pending) second(u - 1);
-        if (!ok) {
-            // products already issued still write tensor memory: wait for them before it is freed
-            if (tc::elect_one()) {
-                atomicExch(&g_xent_gave_up, 1);
-                tc::commit(drained);
+        if (!ok) drain(drained(0));
+    } else if (warp == 3 && M != TC_FORWARD) {             // ---- second products: O
+        const uint32_t inst = tc::instruction(P.on, true);
+        const uint64_t zd = tc::operand(ring, XT_CHUNK, 1024);
+        constexpr uint32_t tile_step = tile_bytes >> 4;
+        int st = 0, b = 0, ob = 0, segs = 0;
+        uint32_t ph = 0, bph = 0, oph = 1;                 // oph: parity of the use of O before this one; the first use waits for none
+        bool ok = true;
+        auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(FULL, tc::mbar_wait(bar, parity, &s_stop)); };
+        while (ok && seg.next(run, xi, y0, n)) {
+            const uint32_t o = tmem + SBUFS * XT + ob * P.on_pitch;
+            for (int i = 0; i < n; ++i) {
+                wait(full(st), ph);                        // long complete: the tile must be visible to this thread too
+                wait(p_full(b), bph);
+                if (i == 0 && segs >= P.obufs) wait(o_free(ob), oph);
+                if (!ok) break;
+                tc::fence_after();
+                const uint32_t z = tmem + b * XT;
+                const uint64_t y = zd + (uint32_t)st * tile_step;
+                if (tc::elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < XT / 16; ++k)      // Z lies in two halves, each over the columns of S it came from
+                        tc::mma_ts(o, z + (k < 4 ? 0 : 32) + k * 8, y + k * 128, inst, i > 0 || k > 0);
+                    tc::commit(empty(st));
+                    tc::commit(z_free(b));
+                    if (i + 1 == n) tc::commit(o_full(ob));
+                }
+                __syncwarp();
+                if (++st == P.stages) {
+                    st = 0;
+                    ph ^= 1;
+                }
+                if (++b == SBUFS) {
+                    b = 0;
+                    bph ^= 1;
+                }
             }
-            __syncwarp();
-            const long long begin = clock64();
-            while (!tc::mbar_try(drained, 0) && clock64() - begin < tc::WAIT_CLOCKS) {}
+            ++segs;
+            if (++ob == P.obufs) {
+                ob = 0;
+                oph ^= 1;
+            }
         }
+        if (!ok) drain(drained(1));
     } else if (warp >= 4) {                                // ---- softmax
         const int sw = warp - 4, wg = sw >> 2, half = wg & 1, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 lanes of tensor memory
         const float c2 = P.a.scale * XT_LOG2E;
         bool ok = true;
-        uint32_t u = 0;
-        int segment = 0;
+        uint32_t ph = 0, bph = 0, oph = 0;
+        int st = 0, b = 0, ob = 0, mine = wg >> 1;             // mine: 0 at this pair's units
         while (ok && seg.next(run, xi, y0, n)) {
             const int64_t x = xi * XT + row;
             float lse2 = 0.f, m = -INFINITY, l = 0.f;
@@ -327,22 +365,18 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                 label = lab >= 0 && lab < P.a.vocab ? lab : -1;
                 if (M == TC_DHIDDEN) lse2 = __ldg(P.a.lse + x) * XT_LOG2E;
             }
-            for (int i = 0; i < n && ok; ++i, ++u) {
-                if ((int)(u & 1) != wg >> 1) continue;
-                const int b = (int)(u % SBUFS), ybase = (y0 + i) * XT + half * 64;
-                if (M == TC_DTABLE) {                      // lse, upstream gradient and label of the unit's hidden rows
-                    __syncwarp();
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int h = ybase + j * 32 + lane, lab = h < P.ny ? __ldg(P.a.labels + h) : -1;
-                        const bool valid = lab >= 0 && lab < P.a.vocab;
-                        col_label[sw][j * 32 + lane] = valid ? lab : -1;
-                        col_lse[sw][j * 32 + lane] = h < P.ny ? __ldg(P.a.lse + h) * -XT_LOG2E : 0.f;
-                        col_g[sw][j * 32 + lane] = valid ? __ldg(P.a.dloss + h) * P.a.scale : 0.f;
+            for (int i = 0; i < n && ok; ++i, mine ^= 1, st = st + 1 == P.stages ? 0 : st + 1, ph ^= st == 0, b = b + 1 == SBUFS ? 0 : b + 1, bph ^= b == 0) {
+                if (mine) continue;
+                const int ybase = (y0 + i) * XT + half * 64;
+                const uint32_t cols = info + st * XT_INFO + half * 64 * 4;      // dw: row_info of this warp's columns
+                if (M == TC_DTABLE) {
+                    ok = tc::mbar_wait(full(st), ph, &s_stop);
+                    if (!__all_sync(FULL, ok)) {
+                        ok = false;
+                        break;
                     }
-                    __syncwarp();
                 }
-                ok = tc::mbar_wait(s_full(b), (uint32_t)(u / SBUFS) & 1, &s_stop);
+                ok = tc::mbar_wait(s_full(b), bph, &s_stop);
                 ok = __all_sync(FULL, ok);
                 if (!ok) break;
                 tc::fence_after();
@@ -422,11 +456,11 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                         } else {
 #pragma unroll
                             for (int j = 0; j < 16; j += 2) {
-                                const float4 ls = *reinterpret_cast<const float4*>(&col_lse[sw][c * 32 + 2 * j]);
+                                const float4 ls = shared_f4(cols + (c * 32 + 2 * j) * 4);
                                 f[j] = exp2_pair<false>(fma2(pair(__uint_as_float(q[2 * j]), __uint_as_float(q[2 * j + 1])), c22, pair(ls.x, ls.y)), j);
                                 f[j + 1] = exp2_pair<false>(fma2(pair(__uint_as_float(q[2 * j + 2]), __uint_as_float(q[2 * j + 3])), c22, pair(ls.z, ls.w)), j + 1);
                             }
-                            const int lab = col_label[sw][c * 32 + lane] - ((int)(xi * XT) + (warp & 3) * 32);
+                            const int lab = shared_i(cols + (2 * XT + c * 32 + lane) * 4) - ((int)(xi * XT) + (warp & 3) * 32);
                             if (__any_sync(FULL, lab >= 0 && lab < 32)) {
 #pragma unroll
                                 for (int j = 0; j < 16; ++j) {
@@ -436,7 +470,7 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                             }
 #pragma unroll
                             for (int j = 0; j < 16; j += 2) {
-                                const float4 g = *reinterpret_cast<const float4*>(&col_g[sw][c * 32 + 2 * j]);
+                                const float4 g = shared_f4(cols + (XT + c * 32 + 2 * j) * 4);
                                 f[j] = mul2(f[j], pair(g.x, g.y));
                                 f[j + 1] = mul2(f[j + 1], pair(g.z, g.w));
                             }
@@ -464,8 +498,7 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                 continue;
             }
             // ---- the segment's sum
-            const int s = segment++, ob = s % OBUFS;
-            ok = tc::mbar_wait(o_full(ob), (uint32_t)(s / OBUFS) & 1, &s_stop);
+            ok = tc::mbar_wait(o_full(ob), oph, &s_stop);
             ok = __all_sync(FULL, ok);
             if (!ok) break;
             tc::fence_after();
@@ -474,22 +507,45 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
             if (M == TC_DHIDDEN) factor = label >= 0 ? __ldg(P.a.dloss + x) * P.a.scale : 0.f;
             const bool zero = M == TC_DHIDDEN && factor == 0.f;
             float* part = P.partial + (P.runs.slot(run, xi) * XT + row) * P.on;
+            void* grad = M == TC_DHIDDEN ? P.a.dhidden : P.a.dtable;
+            const int64_t grad_ld = M == TC_DHIDDEN ? P.a.dhidden_ld : P.a.dtable_ld;
+            const bool staged = P.a.grad_dtype == GS_BF16 && (((uintptr_t)grad & 15) != 0 || (grad_ld & 7) != 0);
             for (int c = wg * 16; c < P.on; c += 64) {
                 uint32_t q[16];
                 __syncwarp();
-                tc::ld16(tmem + 256 + ob * 128 + lanes + c, q);
+                tc::ld16(tmem + SBUFS * XT + ob * P.on_pitch + lanes + c, q);
                 tc::wait_ld(q);
                 float f[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) f[j] = zero ? 0.f : __uint_as_float(q[j]) * factor;
-                if (x < P.nx) {
-                    if (!whole) store_vec<float, 16>(part + c, f);
-                    else if (M == TC_DHIDDEN) store_columns(P.a.dhidden, P.a.grad_dtype, x * P.a.dhidden_ld + c, f, P.a.dim - c);
-                    else store_columns(P.a.dtable, P.a.grad_dtype, x * P.a.dtable_ld + c, f, P.a.dim - c);
+                if (!whole) {
+                    if (x < P.nx) store_vec<float, 16>(part + c, f);
+                } else if (staged) {
+                    // rows of bf16 that start anywhere: through shared memory, two rows of 16 columns per store
+                    const uint32_t to = staging + sw * 1024 + lane * 32;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(pack_bf16(f[0], f[1])), "r"(pack_bf16(f[2], f[3])), "r"(pack_bf16(f[4], f[5])), "r"(pack_bf16(f[6], f[7])) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16), "r"(pack_bf16(f[8], f[9])), "r"(pack_bf16(f[10], f[11])), "r"(pack_bf16(f[12], f[13])), "r"(pack_bf16(f[14], f[15])) : "memory");
+                    __syncwarp();
+                    const int64_t x_warp = x - lane;
+                    const bool in = c + (lane & 15) < P.a.dim;
+#pragma unroll
+                    for (int r = 0; r < 32; r += 2) {
+                        const int rr = r + (lane >> 4);
+                        uint16_t v;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(staging + sw * 1024 + rr * 32 + (lane & 15) * 2) : "memory");
+                        if (in && x_warp + rr < P.nx) static_cast<uint16_t*>(grad)[(x_warp + rr) * grad_ld + c + (lane & 15)] = v;
+                    }
+                    __syncwarp();
+                } else if (x < P.nx) {
+                    store_columns(grad, P.a.grad_dtype, x * grad_ld + c, f, P.a.dim - c);
                 }
             }
             tc::fence_before();
             tc::mbar_arrive(o_free(ob));
+            if (++ob == P.obufs) {
+                ob = 0;
+                oph ^= 1;
+            }
         }
         if (!ok && lane == 0) atomicExch(&g_xent_gave_up, 1);
     }
@@ -502,15 +558,34 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
     }
 }
 
-// Rows repacked to a pitch that tile loads can address (a multiple of 16 bytes).
-__global__ void __launch_bounds__(256) k_xent_pack(const bf16* __restrict__ src, int64_t ld, int64_t rows, int dim, int pitch, bf16* __restrict__ dst) {
-    const int64_t total = rows * (pitch / 2);
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / (pitch / 2);
-        const int c = (int)(i - r * (pitch / 2)) * 2;
+// What the dw kernel needs of the hidden rows, tile by tile (rows behind the last have no gradient).
+__global__ void __launch_bounds__(XT) k_xent_row_info(Xent a, float* __restrict__ info) {
+    for (int64_t t = blockIdx.x; t * XT < a.rows; t += gridDim.x) {
+        const int64_t n = t * XT + threadIdx.x;
+        const int lab = n < a.rows ? a.labels[n] : -1;
+        const bool valid = lab >= 0 && lab < a.vocab;
+        float* p = info + t * 3 * XT + threadIdx.x;
+        p[0] = n < a.rows ? a.lse[n] * -XT_LOG2E : 0.f;
+        p[XT] = valid ? a.dloss[n] * a.scale : 0.f;
+        reinterpret_cast<int*>(p)[2 * XT] = valid ? lab : -1;
+    }
+}
+
+// Rows repacked to a pitch that tile loads can address (a multiple of 16 bytes): 8 columns per thread, read in units of U.
+template <typename U> __global__ void __launch_bounds__(256) k_xent_pack(const bf16* __restrict__ src, int64_t ld, int64_t rows, int dim, int pitch, bf16* __restrict__ dst) {
+    constexpr int PER = sizeof(U) / 2;
+    const int per_row = pitch / 8, rows_per_block = 256 / per_row;
+    const int r_in = threadIdx.x / per_row, c = (threadIdx.x - r_in * per_row) * 8;
+    if (r_in >= rows_per_block) return;
+    for (int64_t r = (int64_t)blockIdx.x * rows_per_block + r_in; r < rows; r += (int64_t)gridDim.x * rows_per_block) {
         const bf16* p = src + r * ld + c;
-        const bf16 lo = c < dim ? p[0] : from_f32<bf16>(0.f), hi = c + 1 < dim ? p[1] : from_f32<bf16>(0.f);
-        reinterpret_cast<__nv_bfloat162*>(dst)[i] = __nv_bfloat162(lo, hi);
+        union {
+            U u[8 / PER];
+            uint4 w;
+        } v;
+#pragma unroll
+        for (int j = 0; j < 8 / PER; ++j) v.u[j] = c + j * PER < dim ? __ldcs(reinterpret_cast<const U*>(p) + j) : U{};
+        *reinterpret_cast<uint4*>(dst + r * pitch + c) = v.w;
     }
 }
 
@@ -566,7 +641,7 @@ static TcLayout tc_layout(const Xent& a) {
     l.rest = off;
     const int64_t parts = sm_count(), tx = (a.rows + XT - 1) / XT;
     const size_t fwd = align_up((size_t)(parts + tx) * XENT_TC_STATS * XT * 8, 256) + align_up((size_t)a.rows * 4, 256);
-    const size_t bwd = (size_t)2 * parts * XT * ((a.dim + 15) / 16 * 16) * 4;
+    const size_t bwd = align_up((size_t)2 * parts * XT * ((a.dim + 15) / 16 * 16) * 4, 256) + (size_t)tx * XT_INFO;
     take(fwd > bwd ? fwd : bwd);
     l.total = off;
     return l;
@@ -593,9 +668,14 @@ static cudaError_t prepare_operands(const Xent& a, void* workspace, Operands* o,
     *o = Operands{a.hidden, a.table, a.hidden_ld, a.table_ld, ws + l.rest};
     const int pitch = packed_pitch(a.dim);
     auto pack = [&](const void* src, int64_t ld, int64_t rows, char* dst) {
-        int64_t blocks = (rows * (pitch / 2) + 255) / 256;
+        const int rows_per_block = 256 / (pitch / 8);
+        int64_t blocks = (rows + rows_per_block - 1) / rows_per_block;
         if (blocks > sm_count() * 32) blocks = sm_count() * 32;
-        k_xent_pack<<<(int)limit_grid(blocks), 256, 0, s>>>((const bf16*)src, ld, rows, a.dim, pitch, (bf16*)dst);
+        const uint64_t all = (uint64_t)(uintptr_t)src | (uint64_t)ld * 2 | (uint64_t)a.dim * 2;
+        const int grid = (int)limit_grid(blocks);
+        if (all % 8 == 0) k_xent_pack<uint2><<<grid, 256, 0, s>>>((const bf16*)src, ld, rows, a.dim, pitch, (bf16*)dst);
+        else if (all % 4 == 0) k_xent_pack<uint32_t><<<grid, 256, 0, s>>>((const bf16*)src, ld, rows, a.dim, pitch, (bf16*)dst);
+        else k_xent_pack<uint16_t><<<grid, 256, 0, s>>>((const bf16*)src, ld, rows, a.dim, pitch, (bf16*)dst);
         count_launches(1);
     };
     if (!tile_rows_ok(a.hidden, a.hidden_ld)) {
@@ -619,6 +699,16 @@ template <int M> static cudaError_t run_tc(const Xent& a, const Operands& o, Xen
     P.runs = make_runs(P.nx, XT, P.ny, XT, sm_count());
     const int chunks = (a.dim + 63) / 64, tile = chunks * XT_CHUNK, xbufs = chunks <= 2 ? 2 : 1;
     P.on = (a.dim + 15) / 16 * 16;
+    // 512 columns of tensor memory: three S and one or two O of up to 128 (64) columns, or two S and one O of up to 256.
+    // With few units per row of tiles a second O pays more than a third S: the next row's products need not wait for
+    // the store of this one's.
+    P.on_pitch = chunks == 1 ? 64 : 128;
+    P.sbufs = chunks <= 2 ? 3 : 2;
+    P.obufs = chunks == 1 ? 2 : 1;
+    if (chunks == 2 && P.runs.tiles_y < XT_SHORT_ROWS) {
+        P.sbufs = 2;
+        P.obufs = 2;
+    }
     P.stages = (192 << 10) / tile - xbufs;
     if (P.stages > XT_MAX_STAGES) P.stages = XT_MAX_STAGES;
     CUtensorMap hm, tm;
@@ -626,7 +716,7 @@ template <int M> static cudaError_t run_tc(const Xent& a, const Operands& o, Xen
     if (e == cudaSuccess) e = row_map(&tm, o.table, a.vocab, a.dim, o.table_ld);
     if (e != cudaSuccess) return e;
     // at least 120 KB, so that an SM holds one block: a block takes all of the tensor memory
-    int smem = (xbufs + P.stages) * tile + 1024;
+    int smem = (xbufs + P.stages) * tile + 1024 + (M == TC_DTABLE ? P.stages * XT_INFO : 0) + (M == TC_FORWARD ? 0 : XT_STAGING);
     if (smem < (120 << 10)) smem = 120 << 10;
     auto kernel = chunks == 1 ? k_xent_tc<M, 1> : (chunks == 2 ? k_xent_tc<M, 2> : (chunks == 3 ? k_xent_tc<M, 3> : k_xent_tc<M, 4>));
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -657,6 +747,10 @@ cudaError_t launch_xent_tc_backward(const Xent& a, void* workspace, cudaStream_t
     if (e != cudaSuccess) return e;
     XentTc P{};
     P.partial = (float*)o.rest;
+    float* row_info = (float*)(o.rest + align_up((size_t)2 * sm_count() * XT * ((a.dim + 15) / 16 * 16) * 4, 256));
+    P.row_info = row_info;
+    k_xent_row_info<<<(int)limit_grid((a.rows + XT - 1) / XT), XT, 0, s>>>(a, row_info);
+    count_launches(1);
     e = run_tc<TC_DHIDDEN>(a, o, P, s);
     if (e != cudaSuccess) return e;
     e = launch_xent_join(a, true, P.runs, XT, P.on, P.partial, s);
