@@ -80,16 +80,19 @@ struct XentTc {
     Runs runs;
     int nx, ny;
     int on;                      // columns of O: dim rounded up to 16
-    int stages;
+    int stages, xbufs;           // tiles of y and of x in shared memory
     int sbufs, obufs;            // buffers of S and of O in tensor memory: O(i) starts at column 128 sbufs + i * on_pitch
     int on_pitch;
+    int out, out_pitch;          // backward: OUT_*, bytes between the staged rows
     float2* stats;               // forward: [parts + tiles_x][XENT_TC_STATS][XT]
     float* picked;
     float* partial;              // backward: [2 parts][XT][on]
     const float* row_info;       // dw: [tiles of hidden rows][3][XT]: -lse (base 2), upstream gradient times scale, label
 };
 constexpr int XT_INFO = 3 * XT * 4;        // bytes of a tile's row_info
-constexpr int XT_STAGING = 16 * 32 * 16 * 2; // bytes in which the softmax warps turn rows of bf16 that are not on 16 bytes
+// How a finished tile of bf16 gradients leaves: lane by lane; or through shared memory and then by bulk copies, a row each
+// (rows on 16 bytes) or the whole tile at once (rows without gaps, wherever they start).
+enum { OUT_DIRECT = 0, OUT_ROWS = 1, OUT_TILE = 2 };
 
 // The block's runs, cut at rows of tiles.
 struct Segments {
@@ -163,14 +166,13 @@ template <int M, int CHUNKS>
 __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant__ XentTc P, const __grid_constant__ CUtensorMap xmap,
                                                            const __grid_constant__ CUtensorMap ymap) {
     extern __shared__ unsigned char tiles[];
-    __shared__ __align__(8) unsigned long long bars[2 * XT_MAX_STAGES + 22];
+    __shared__ __align__(8) unsigned long long bars[2 * XT_MAX_STAGES + 24];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_stop;
     const int SBUFS = M == TC_FORWARD ? 4 : P.sbufs;
     const int warp = __shfl_sync(FULL, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     constexpr uint32_t tile_bytes = CHUNKS * XT_CHUNK;
-    constexpr int XBUFS = CHUNKS <= 2 ? 2 : 1;
-    const uint32_t xbase = (tc::smem_addr(tiles) + 1023) & ~1023u, ring = xbase + XBUFS * tile_bytes;
+    const uint32_t xbase = (tc::smem_addr(tiles) + 1023) & ~1023u, ring = xbase + P.xbufs * tile_bytes;
     const uint32_t info = ring + P.stages * tile_bytes;      // dw: row_info of the stages' tiles
     const uint32_t staging = info + (M == TC_DTABLE ? P.stages * XT_INFO : 0);
     const uint32_t b0 = tc::smem_addr(bars);
@@ -184,6 +186,7 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
     auto o_full = [&](int i) { return b1 + 96 + 8 * i; };    // 2
     auto o_free = [&](int i) { return b1 + 112 + 8 * i; };   // 2
     auto z_free = [&](int i) { return b1 + 128 + 8 * i; };   // 4: Z of a unit has been multiplied (backward)
+    const uint32_t staged = b1 + 176, unstaged = b1 + 184;   // the tile is in shared memory; its copies have read it
     auto drained = [&](int i) { return b1 + 160 + 8 * i; };  // 2: the products of a role that gives up
 
     if (threadIdx.x == 0) {
@@ -203,6 +206,8 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
             tc::mbar_init(o_full(i), 1);
             tc::mbar_init(o_free(i), 512);
         }
+        tc::mbar_init(staged, 512);
+        tc::mbar_init(unstaged, 32);
         tc::mbar_init(drained(0), 1);
         tc::mbar_init(drained(1), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -213,6 +218,8 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
     __syncthreads();
     tc::fence_after();
     const uint32_t tmem = __shfl_sync(FULL, s_tmem, 0);
+    // a whole tile of 128 rows can leave in one copy; its last, shorter neighbour goes lane by lane
+    auto stages_tile = [&](int64_t i) { return P.out == OUT_ROWS || (P.out == OUT_TILE && (i + 1) * XT <= P.nx); };
     // A role that gives up: its products still write tensor memory, which must not be freed under them.
     auto drain = [&](uint32_t bar) {
         if (tc::elect_one()) {
@@ -233,8 +240,8 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
             uint32_t ph = 0;
             bool ok = true;
             while (ok && seg.next(run, xi, y0, n)) {
-                const int xb = segs % XBUFS;
-                if (segs >= XBUFS) ok = __all_sync(FULL, tc::mbar_wait(x_free(xb), (uint32_t)(segs / XBUFS - 1) & 1, &s_stop));
+                const int xb = segs % P.xbufs;
+                if (segs >= P.xbufs) ok = __all_sync(FULL, tc::mbar_wait(x_free(xb), (uint32_t)(segs / P.xbufs - 1) & 1, &s_stop));
                 if (!ok) break;
                 if (tc::elect_one()) {
                     tc::mbar_expect(x_full(xb), tile_bytes);
@@ -263,8 +270,8 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
             const long long begin = clock64();
             for (int j = issued > P.stages ? issued - P.stages : 0; j < issued; ++j)
                 while (!tc::mbar_try(full(j % P.stages), (uint32_t)(j / P.stages) & 1) && clock64() - begin < tc::WAIT_CLOCKS) {}
-            for (int j = segs > XBUFS ? segs - XBUFS : 0; j < segs; ++j)
-                while (!tc::mbar_try(x_full(j % XBUFS), (uint32_t)(j / XBUFS) & 1) && clock64() - begin < tc::WAIT_CLOCKS) {}
+            for (int j = segs > P.xbufs ? segs - P.xbufs : 0; j < segs; ++j)
+                while (!tc::mbar_try(x_full(j % P.xbufs), (uint32_t)(j / P.xbufs) & 1) && clock64() - begin < tc::WAIT_CLOCKS) {}
         }
     } else if (warp == 1) {                                // ---- first products: S
         const uint32_t inst = tc::instruction(XT, false);
@@ -275,8 +282,8 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
         bool ok = true, reuse = false;
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(FULL, tc::mbar_wait(bar, parity, &s_stop)); };
         while (ok && seg.next(run, xi, y0, n)) {
-            const int xb = segs % XBUFS;
-            wait(x_full(xb), (uint32_t)(segs / XBUFS) & 1);
+            const int xb = segs % P.xbufs;
+            wait(x_full(xb), (uint32_t)(segs / P.xbufs) & 1);
             ++segs;
             for (int i = 0; i < n; ++i) {
                 wait(full(st), ph);
@@ -349,13 +356,106 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
             }
         }
         if (!ok) drain(drained(1));
+    } else if (warp == 2 && M != TC_FORWARD && P.out != OUT_DIRECT) {       // ---- copies of finished tiles
+        bool ok = true;
+        uint32_t parity = 0;
+        char* grad = (char*)(M == TC_DHIDDEN ? P.a.dhidden : P.a.dtable);
+        const int64_t ld = (M == TC_DHIDDEN ? P.a.dhidden_ld : P.a.dtable_ld) * 2;
+        while (ok && seg.next(run, xi, y0, n)) {
+            if (y0 != 0 || n != P.runs.tiles_y || !stages_tile(xi)) continue;
+            ok = __all_sync(FULL, tc::mbar_wait(staged, parity, &s_stop));
+            if (!ok) break;
+            parity ^= 1;
+            if (P.out == OUT_ROWS) {
+                for (int r = lane; r < XT && xi * XT + r < P.nx; r += 32) tc::bulk_store(grad + (xi * XT + r) * ld, staging + r * P.out_pitch, P.a.dim * 2);
+            } else if (lane == 0) {
+                tc::bulk_store(grad + xi * XT * ld, staging, XT * P.a.dim * 2);
+            }
+            tc::bulk_commit();
+            tc::bulk_wait_read();
+            tc::mbar_arrive(unstaged);
+        }
+        tc::bulk_wait_all();
+        if (!ok && lane == 0) atomicExch(&g_xent_gave_up, 1);
     } else if (warp >= 4) {                                // ---- softmax
         const int sw = warp - 4, wg = sw >> 2, half = wg & 1, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 lanes of tensor memory
         const float c2 = P.a.scale * XT_LOG2E;
         bool ok = true;
         uint32_t ph = 0, bph = 0, oph = 0;
-        int st = 0, b = 0, ob = 0, mine = wg >> 1;             // mine: 0 at this pair's units
+        int st = 0, b = 0, ob = 0, mine = wg >> 1, tiles_out = 0;   // mine: 0 at this pair's units
+        // The sum of a finished segment.  It is taken after the first unit of the next one, when the last products have long ended.
+        bool pending = false, whole = false;
+        int64_t e_run = 0, e_xi = 0;
+        auto epilogue = [&]() {
+            pending = false;
+            const int64_t x = e_xi * XT + row;
+            ok = tc::mbar_wait(o_full(ob), oph, &s_stop);
+            ok = __all_sync(FULL, ok);
+            if (!ok) return;
+            tc::fence_after();
+            float factor = 1.f;
+            if (M == TC_DHIDDEN && x < P.nx) {
+                const int lab = __ldg(P.a.labels + x);
+                factor = lab >= 0 && lab < P.a.vocab ? __ldg(P.a.dloss + x) * P.a.scale : 0.f;
+            }
+            const bool zero = M == TC_DHIDDEN && factor == 0.f;
+            float* part = P.partial + (P.runs.slot(e_run, e_xi) * XT + row) * P.on;
+            void* grad = M == TC_DHIDDEN ? P.a.dhidden : P.a.dtable;
+            const int64_t grad_ld = M == TC_DHIDDEN ? P.a.dhidden_ld : P.a.dtable_ld;
+            const bool stage = whole && stages_tile(e_xi);
+            if (stage && tiles_out > 0) {                  // the copies of the tile before must have read the rows
+                ok = __all_sync(FULL, tc::mbar_wait(unstaged, (uint32_t)(tiles_out - 1) & 1, &s_stop));
+                if (!ok) return;
+            }
+            tiles_out += stage;
+            for (int c = wg * 16; c < P.on; c += 64) {
+                uint32_t q[16];
+                __syncwarp();
+                tc::ld16(tmem + SBUFS * XT + ob * P.on_pitch + lanes + c, q);
+                tc::wait_ld(q);
+                float f[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) f[j] = zero ? 0.f : __uint_as_float(q[j]) * factor;
+                if (!whole) {
+                    if (x < P.nx) store_vec<float, 16>(part + c, f);
+                } else if (stage) {
+                    const uint32_t to = staging + row * P.out_pitch + c * 2;
+                    uint32_t w[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] = pack_bf16(f[2 * j], f[2 * j + 1]);
+                    if (P.out == OUT_ROWS) {
+                        if (c < P.a.dim) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                        if (c + 8 < P.a.dim) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+                    } else {
+                        const int left = P.a.dim - c;
+                        if (P.a.dim % 2 == 0) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (2 * j < left) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + 4 * j), "r"(w[j]) : "memory");
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                if (2 * j < left) asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + 4 * j), "h"((uint16_t)w[j]) : "memory");
+                                if (2 * j + 1 < left) asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + 4 * j + 2), "h"((uint16_t)(w[j] >> 16)) : "memory");
+                            }
+                        }
+                    }
+                } else if (x < P.nx) {
+                    store_columns(grad, P.a.grad_dtype, x * grad_ld + c, f, P.a.dim - c);
+                }
+            }
+            tc::fence_before();
+            tc::mbar_arrive(o_free(ob));
+            if (stage) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // the copy engine sees the rows
+                tc::mbar_arrive(staged);
+            }
+            if (++ob == P.obufs) {
+                ob = 0;
+                oph ^= 1;
+            }
+        };
         while (ok && seg.next(run, xi, y0, n)) {
             const int64_t x = xi * XT + row;
             float lse2 = 0.f, m = -INFINITY, l = 0.f;
@@ -490,6 +590,7 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                     tc::wait_st();
                     tc::fence_before();
                     tc::mbar_arrive(p_full(b));
+                    if (pending) epilogue();
                 }
             }
             if (!ok) break;
@@ -497,56 +598,13 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                 P.stats[((run + xi) * XENT_TC_STATS + wg) * XT + row] = make_float2(m, l);
                 continue;
             }
-            // ---- the segment's sum
-            ok = tc::mbar_wait(o_full(ob), oph, &s_stop);
-            ok = __all_sync(FULL, ok);
-            if (!ok) break;
-            tc::fence_after();
-            const bool whole = y0 == 0 && n == P.runs.tiles_y;
-            float factor = 1.f;
-            if (M == TC_DHIDDEN) factor = label >= 0 ? __ldg(P.a.dloss + x) * P.a.scale : 0.f;
-            const bool zero = M == TC_DHIDDEN && factor == 0.f;
-            float* part = P.partial + (P.runs.slot(run, xi) * XT + row) * P.on;
-            void* grad = M == TC_DHIDDEN ? P.a.dhidden : P.a.dtable;
-            const int64_t grad_ld = M == TC_DHIDDEN ? P.a.dhidden_ld : P.a.dtable_ld;
-            const bool staged = P.a.grad_dtype == GS_BF16 && (((uintptr_t)grad & 15) != 0 || (grad_ld & 7) != 0);
-            for (int c = wg * 16; c < P.on; c += 64) {
-                uint32_t q[16];
-                __syncwarp();
-                tc::ld16(tmem + SBUFS * XT + ob * P.on_pitch + lanes + c, q);
-                tc::wait_ld(q);
-                float f[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) f[j] = zero ? 0.f : __uint_as_float(q[j]) * factor;
-                if (!whole) {
-                    if (x < P.nx) store_vec<float, 16>(part + c, f);
-                } else if (staged) {
-                    // rows of bf16 that start anywhere: through shared memory, two rows of 16 columns per store
-                    const uint32_t to = staging + sw * 1024 + lane * 32;
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(pack_bf16(f[0], f[1])), "r"(pack_bf16(f[2], f[3])), "r"(pack_bf16(f[4], f[5])), "r"(pack_bf16(f[6], f[7])) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16), "r"(pack_bf16(f[8], f[9])), "r"(pack_bf16(f[10], f[11])), "r"(pack_bf16(f[12], f[13])), "r"(pack_bf16(f[14], f[15])) : "memory");
-                    __syncwarp();
-                    const int64_t x_warp = x - lane;
-                    const bool in = c + (lane & 15) < P.a.dim;
-#pragma unroll
-                    for (int r = 0; r < 32; r += 2) {
-                        const int rr = r + (lane >> 4);
-                        uint16_t v;
-                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(staging + sw * 1024 + rr * 32 + (lane & 15) * 2) : "memory");
-                        if (in && x_warp + rr < P.nx) static_cast<uint16_t*>(grad)[(x_warp + rr) * grad_ld + c + (lane & 15)] = v;
-                    }
-                    __syncwarp();
-                } else if (x < P.nx) {
-                    store_columns(grad, P.a.grad_dtype, x * grad_ld + c, f, P.a.dim - c);
-                }
-            }
-            tc::fence_before();
-            tc::mbar_arrive(o_free(ob));
-            if (++ob == P.obufs) {
-                ob = 0;
-                oph ^= 1;
-            }
+            if (pending) epilogue();
+            pending = true;
+            whole = y0 == 0 && n == P.runs.tiles_y;
+            e_run = run;
+            e_xi = xi;
         }
+        if (M != TC_FORWARD && ok && pending) epilogue();
         if (!ok && lane == 0) atomicExch(&g_xent_gave_up, 1);
     }
     __syncwarp();
@@ -697,7 +755,9 @@ template <int M> static cudaError_t run_tc(const Xent& a, const Operands& o, Xen
     P.nx = ON_X ? a.rows : (int)a.vocab;
     P.ny = ON_X ? (int)a.vocab : a.rows;
     P.runs = make_runs(P.nx, XT, P.ny, XT, sm_count());
-    const int chunks = (a.dim + 63) / 64, tile = chunks * XT_CHUNK, xbufs = chunks <= 2 ? 2 : 1;
+    const int chunks = (a.dim + 63) / 64, tile = chunks * XT_CHUNK;
+    const bool short_rows = P.runs.tiles_y < XT_SHORT_ROWS;
+    P.xbufs = chunks == 1 || (chunks == 2 && (M == TC_FORWARD || short_rows)) ? 2 : 1;
     P.on = (a.dim + 15) / 16 * 16;
     // 512 columns of tensor memory: three S and one or two O of up to 128 (64) columns, or two S and one O of up to 256.
     // With few units per row of tiles a second O pays more than a third S: the next row's products need not wait for
@@ -705,18 +765,28 @@ template <int M> static cudaError_t run_tc(const Xent& a, const Operands& o, Xen
     P.on_pitch = chunks == 1 ? 64 : 128;
     P.sbufs = chunks <= 2 ? 3 : 2;
     P.obufs = chunks == 1 ? 2 : 1;
-    if (chunks == 2 && P.runs.tiles_y < XT_SHORT_ROWS) {
+    if (chunks == 2 && short_rows) {
         P.sbufs = 2;
         P.obufs = 2;
     }
-    P.stages = (192 << 10) / tile - xbufs;
+    // shared memory: X, the ring of Y, row info, and rows on their way out where X and three or more tiles of Y leave room
+    int staging = 0;
+    if (M != TC_FORWARD && chunks <= 2 && a.grad_dtype == GS_BF16) {
+        const void* grad = M == TC_DHIDDEN ? a.dhidden : a.dtable;
+        const int64_t ld = M == TC_DHIDDEN ? a.dhidden_ld : a.dtable_ld;
+        if (tile_rows_ok(grad, ld) && a.dim % 8 == 0) P.out = OUT_ROWS;
+        else if (((uintptr_t)grad & 15) == 0 && ld == a.dim) P.out = OUT_TILE;
+        P.out_pitch = a.dim * 2 + (P.out == OUT_ROWS ? 16 : 0);      // 16 bytes apart: neighbouring rows in different banks
+        if (P.out != OUT_DIRECT) staging = XT * P.out_pitch;
+    }
+    P.stages = ((M == TC_FORWARD ? 192 : 216) * 1024 - staging) / (tile + (M == TC_DTABLE ? XT_INFO : 0)) - P.xbufs;
     if (P.stages > XT_MAX_STAGES) P.stages = XT_MAX_STAGES;
     CUtensorMap hm, tm;
     cudaError_t e = row_map(&hm, o.hidden, a.rows, a.dim, o.hidden_ld);
     if (e == cudaSuccess) e = row_map(&tm, o.table, a.vocab, a.dim, o.table_ld);
     if (e != cudaSuccess) return e;
     // at least 120 KB, so that an SM holds one block: a block takes all of the tensor memory
-    int smem = (xbufs + P.stages) * tile + 1024 + (M == TC_DTABLE ? P.stages * XT_INFO : 0) + (M == TC_FORWARD ? 0 : XT_STAGING);
+    int smem = (P.xbufs + P.stages) * tile + 1024 + (M == TC_DTABLE ? P.stages * XT_INFO : 0) + staging;
     if (smem < (120 << 10)) smem = 120 << 10;
     auto kernel = chunks == 1 ? k_xent_tc<M, 1> : (chunks == 2 ? k_xent_tc<M, 2> : (chunks == 3 ? k_xent_tc<M, 3> : k_xent_tc<M, 4>));
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
