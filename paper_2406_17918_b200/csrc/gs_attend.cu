@@ -50,7 +50,7 @@ struct Attend {
 
 __device__ __forceinline__ int length_of(const Count& c) {
     if (!c.d_n) return c.bound;
-    const int n = __ldg(c.d_n);
+    const int n = __ldcg(c.d_n);
     return n < 0 ? 0 : (n > c.bound ? c.bound : n);
 }
 
@@ -532,12 +532,13 @@ template <typename T, bool KV> __global__ void __launch_bounds__(AT_THREADS) k_a
 
 namespace gs {
 
-// The destination of every edge, in edge order.
+// The destination of every edge, in edge order: 8 lanes per row.
 __global__ void __launch_bounds__(AT_THREADS) k_edge_rows(const int32_t* __restrict__ indptr, Count dst, int edge_bound, int32_t* __restrict__ rows) {
-    const int n = length_of(dst), lane = threadIdx.x & 31;
-    for (int64_t r = (int64_t)blockIdx.x * (AT_THREADS / 32) + threadIdx.x / 32; r < n; r += (int64_t)gridDim.x * (AT_THREADS / 32)) {
+    chain_wait();
+    const int n = length_of(dst), t = threadIdx.x & 7;
+    for (int64_t r = (int64_t)blockIdx.x * (AT_THREADS / 8) + threadIdx.x / 8; r < n; r += (int64_t)gridDim.x * (AT_THREADS / 8)) {
         const int b = __ldg(indptr + r), end = __ldg(indptr + r + 1), e = end < edge_bound ? end : edge_bound;
-        for (int i = (b < 0 ? 0 : b) + lane; i < e; i += 32) rows[i] = (int32_t)r;
+        for (int i = (b < 0 ? 0 : b) + t; i < e; i += 8) rows[i] = (int32_t)r;
     }
 }
 
@@ -560,7 +561,7 @@ static AttendLayout attend_layout(int64_t dst, int64_t edges, int32_t q_heads, i
     return l;
 }
 
-size_t reverse_workspace(int64_t edges) { return align_up((size_t)edges * 4, 256) + key_sort_bytes(edges); }
+size_t reverse_workspace(int64_t edges) { return 2 * align_up((size_t)edges * 4, 256) + key_sort_bytes(edges); }
 
 size_t attention_workspace(int64_t dst, int64_t edges, int32_t q_heads, int32_t head_dim) {
     const size_t a = attend_layout(dst, edges, q_heads, head_dim).total, b = reverse_workspace(edges);
@@ -729,17 +730,15 @@ cudaError_t launch_attention_backward(const BlockAttention& a, const int32_t* re
 
 cudaError_t launch_block_reverse(const int32_t* indptr, const int32_t* indices, Count dst, Count src, Count edges, int32_t* rev_indptr,
                                  int32_t* rev_dst, void* workspace, cudaStream_t s) {
+    const size_t list = align_up((size_t)edges.bound * 4, 256);
     int32_t* rows = (int32_t*)workspace;
-    int64_t blocks = ((int64_t)dst.bound + AT_THREADS / 32 - 1) / (AT_THREADS / 32);
+    uint32_t* keys = (uint32_t*)((char*)workspace + list);
+    int64_t blocks = ((int64_t)dst.bound + AT_THREADS / 8 - 1) / (AT_THREADS / 8);
     if (blocks > sm_count() * 32) blocks = sm_count() * 32;
-    k_edge_rows<<<(int)limit_grid(blocks), AT_THREADS, 0, s>>>(indptr, dst, edges.bound, rows);
-    count_launches(1);
-    const unsigned long long* sorted = nullptr;
-    cudaError_t e = launch_key_sort(indices, rows, edges, src.bound, (char*)workspace + align_up((size_t)edges.bound * 4, 256), &sorted, s);
-    if (e != cudaSuccess) return e;
-    e = launch_row_starts(sorted, edges, src, rev_indptr, s);
-    if (e != cudaSuccess) return e;
-    return launch_payloads(sorted, edges, rev_dst, s);
+    cudaError_t e = launch_train(k_edge_rows, blocks, AT_THREADS, 0, s, indptr, dst, (int)edges.bound, rows);
+    if (e == cudaSuccess) e = launch_key_sort(indices, rows, edges, src.bound, (char*)workspace + 2 * list, keys, rev_dst, s);
+    if (e == cudaSuccess) e = launch_row_starts(keys, edges, src, rev_indptr, s);
+    return e;
 }
 
 }  // namespace gs

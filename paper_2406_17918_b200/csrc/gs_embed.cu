@@ -15,7 +15,7 @@ constexpr int EL_ROWS = 4;      // rows in flight per thread of the lookup
 
 __device__ __forceinline__ int list_length(const Count& c) {
     if (!c.d_n) return c.bound;
-    const int n = __ldg(c.d_n);
+    const int n = __ldcg(c.d_n);      // may be the work of the kernel before
     return n < 0 ? 0 : (n > c.bound ? c.bound : n);
 }
 
@@ -102,13 +102,14 @@ cudaError_t launch_embedding_lookup(const EmbedLookup& p, cudaStream_t s) {
 // ---------------------------------------------------------------- gradient
 constexpr int ES_CHUNK = 256;       // entries of one run summed by one group of lanes
 constexpr int ES_UNROLL = 4;        // rows in flight per lane
+constexpr int ES_ROWS = 4;          // rows a group of lanes takes at a time
 constexpr int ES_THREADS = 256;
 constexpr int HEAD_TILE = 1024;
 
 struct RunSum {
     EmbedGrad g;
-    const unsigned long long* sorted;
-    const int32_t* starts;          // row r's entries are sorted[starts[r] .. starts[r + 1])
+    const int32_t* order;           // positions in the order of their ids
+    const int32_t* starts;          // row r's entries are order[starts[r] .. starts[r + 1])
     Count rows;                     // dense: the table's rows; sparse: the runs (device) of at most n
     int tl;                         // lanes per row (power of two)
     int32_t* words;                 // [0] chunks, [1] long rows
@@ -127,7 +128,7 @@ __device__ __forceinline__ void run_sum(const RunSum& P, int b, int e, int col, 
     for (; k + ES_UNROLL <= e; k += ES_UNROLL) {
         Raw<Tin, VE> v[ES_UNROLL];
 #pragma unroll
-        for (int j = 0; j < ES_UNROLL; ++j) v[j] = load_raw_stream<Tin, VE>(dout + (int64_t)(uint32_t)__ldg(P.sorted + k + j) * P.g.dout_ld);
+        for (int j = 0; j < ES_UNROLL; ++j) v[j] = load_raw_stream<Tin, VE>(dout + (int64_t)__ldcg(P.order + k + j) * P.g.dout_ld);
 #pragma unroll
         for (int j = 0; j < ES_UNROLL; ++j) {
             float x[VE];
@@ -138,48 +139,76 @@ __device__ __forceinline__ void run_sum(const RunSum& P, int b, int e, int col, 
     }
     for (; k < e; ++k) {
         float x[VE];
-        unpack<Tin, VE>(load_raw_stream<Tin, VE>(dout + (int64_t)(uint32_t)__ldg(P.sorted + k) * P.g.dout_ld), x);
+        unpack<Tin, VE>(load_raw_stream<Tin, VE>(dout + (int64_t)__ldcg(P.order + k) * P.g.dout_ld), x);
 #pragma unroll
         for (int i = 0; i < VE; ++i) acc[i] += x[i];
     }
 }
 
+// Most rows have one entry or none, so a group of lanes takes ES_ROWS neighbouring rows at a time: their offsets, first
+// positions and first rows are each in flight together.
 template <typename Tin, typename Tout, int VE>
 __global__ void __launch_bounds__(ES_THREADS) k_run_sum(RunSum P) {
+    chain_wait();
     const int rows = list_length(P.rows), bound = P.rows.bound;
-    const int units = P.g.dim / VE, lane = threadIdx.x & 31, t = lane & (P.tl - 1);
+    const int units = P.g.dim / VE, t = threadIdx.x & (P.tl - 1);
     const int per_block = ES_THREADS / P.tl;
+    const Tin* dout = (const Tin*)P.g.dout;
     Tout* grad = (Tout*)P.g.grad;
-    for (int64_t r = (int64_t)blockIdx.x * per_block + threadIdx.x / P.tl; r < bound; r += (int64_t)gridDim.x * per_block) {
-        const int b = r < rows ? __ldg(P.starts + r) : 0, e = r < rows ? __ldg(P.starts + r + 1) : 0;
-        if (e - b > ES_CHUNK) {
-            if (t == 0) {
-                const int nc = (e - b + ES_CHUNK - 1) / ES_CHUNK;
-                const int first = atomicAdd(P.words, nc);
-                P.longs[atomicAdd(P.words + 1, 1)] = make_int4((int)r, first, nc, 0);
-                for (int c = 0; c < nc; ++c) P.items[first + c] = make_int2((int)r, c);
+    for (int64_t r = ((int64_t)blockIdx.x * per_block + threadIdx.x / P.tl) * ES_ROWS; r < bound; r += (int64_t)gridDim.x * per_block * ES_ROWS) {
+        int b[ES_ROWS + 1], first[ES_ROWS];
+#pragma unroll
+        for (int j = 0; j <= ES_ROWS; ++j) b[j] = __ldcg(P.starts + (r + j < rows ? r + j : rows));      // behind the last row: empty
+#pragma unroll
+        for (int j = 0; j < ES_ROWS; ++j) first[j] = b[j + 1] > b[j] ? __ldcg(P.order + b[j]) : -1;
+        bool listed[ES_ROWS];
+#pragma unroll
+        for (int j = 0; j < ES_ROWS; ++j) {
+            const int len = b[j + 1] - b[j];
+            listed[j] = len > ES_CHUNK;
+            if (listed[j] && t == 0) {
+                const int nc = (len + ES_CHUNK - 1) / ES_CHUNK;
+                const int at = atomicAdd(P.words, nc);
+                P.longs[atomicAdd(P.words + 1, 1)] = make_int4((int)(r + j), at, nc, 0);
+                for (int c = 0; c < nc; ++c) P.items[at + c] = make_int2((int)(r + j), c);
             }
-            continue;
         }
         for (int u = t; u < units; u += P.tl) {
-            float acc[VE];
-            run_sum<Tin, VE>(P, b, e, u * VE, acc);
+            Raw<Tin, VE> v[ES_ROWS];
 #pragma unroll
-            for (int i = 0; i < VE; ++i) acc[i] = e > b ? acc[i] * P.g.scale : 0.f;
-            store_vec<Tout, VE>(grad + r * P.g.grad_ld + (int64_t)u * VE, acc);
+            for (int j = 0; j < ES_ROWS; ++j)
+                v[j] = first[j] >= 0 && !listed[j] ? load_raw_stream<Tin, VE>(dout + (int64_t)first[j] * P.g.dout_ld + (int64_t)u * VE) : zero_raw<Tin, VE>();
+#pragma unroll
+            for (int j = 0; j < ES_ROWS; ++j) {
+                if (r + j >= bound || listed[j]) continue;
+                float acc[VE];
+                unpack<Tin, VE>(v[j], acc);
+                if (b[j + 1] - b[j] > 1) {
+                    float more[VE];
+                    run_sum<Tin, VE>(P, b[j] + 1, b[j + 1], u * VE, more);
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) acc[i] += more[i];
+                }
+                if (first[j] >= 0) {
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) acc[i] *= P.g.scale;
+                }
+                store_vec<Tout, VE>(grad + (r + j) * P.g.grad_ld + (int64_t)u * VE, acc);
+            }
         }
     }
 }
 
 template <typename Tin, int VE>
 __global__ void __launch_bounds__(ES_THREADS) k_run_chunks(RunSum P) {
+    chain_wait();
     const int chunks = __ldcg(P.words);
     const int units = P.g.dim / VE, t = threadIdx.x & (P.tl - 1);
     const int per_block = ES_THREADS / P.tl;
     for (int64_t c = (int64_t)blockIdx.x * per_block + threadIdx.x / P.tl; c < chunks; c += (int64_t)gridDim.x * per_block) {
         const int2 it = P.items[c];
-        const int b = __ldg(P.starts + it.x) + it.y * ES_CHUNK;
-        const int end = __ldg(P.starts + it.x + 1), e = b + ES_CHUNK < end ? b + ES_CHUNK : end;
+        const int b = __ldcg(P.starts + it.x) + it.y * ES_CHUNK;
+        const int end = __ldcg(P.starts + it.x + 1), e = b + ES_CHUNK < end ? b + ES_CHUNK : end;
         for (int u = t; u < units; u += P.tl) {
             float acc[VE];
             run_sum<Tin, VE>(P, b, e, u * VE, acc);
@@ -194,6 +223,7 @@ template <typename Tout>
 __global__ void __launch_bounds__(ES_THREADS) k_run_join(RunSum P) {
     constexpr int W = ES_THREADS / 32;
     __shared__ float share[W][32];
+    chain_wait();
     const int longs = __ldcg(P.words + 1), lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     const int ctiles = (P.g.dim + 31) / 32;
     Tout* grad = (Tout*)P.g.grad;
@@ -218,16 +248,17 @@ __global__ void __launch_bounds__(ES_THREADS) k_run_join(RunSum P) {
 }
 
 // Heads of runs of equal ids per tile of the sorted list ...
-__global__ void __launch_bounds__(HEAD_TILE) k_head_counts(const unsigned long long* __restrict__ sorted, Count nc, uint32_t limit,
+__global__ void __launch_bounds__(HEAD_TILE) k_head_counts(const uint32_t* __restrict__ keys, Count nc, uint32_t limit,
                                                            int32_t* __restrict__ tile_heads) {
+    chain_wait();
     const int n = list_length(nc);
     const int tiles = (nc.bound + HEAD_TILE - 1) / HEAD_TILE;
     for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int64_t i = (int64_t)tile * HEAD_TILE + threadIdx.x;
         bool head = false;
         if (i < n) {
-            const uint32_t k = (uint32_t)(__ldg(sorted + i) >> 32);
-            head = k < limit && (i == 0 || (uint32_t)(__ldg(sorted + i - 1) >> 32) != k);
+            const uint32_t k = __ldcg(keys + i);
+            head = k < limit && (i == 0 || __ldcg(keys + i - 1) != k);
         }
         const int c = __syncthreads_count(head);
         if (threadIdx.x == 0) tile_heads[tile] = c;
@@ -235,10 +266,11 @@ __global__ void __launch_bounds__(HEAD_TILE) k_head_counts(const unsigned long l
 }
 
 // ... and the list of runs: id and first entry of each; -1 behind the last one.
-__global__ void __launch_bounds__(HEAD_TILE) k_head_list(const unsigned long long* __restrict__ sorted, Count nc, uint32_t limit,
+__global__ void __launch_bounds__(HEAD_TILE) k_head_list(const uint32_t* __restrict__ keys, Count nc, uint32_t limit,
                                                          const int32_t* __restrict__ tile_heads, int32_t* __restrict__ rows,
                                                          int32_t* __restrict__ starts, int32_t* __restrict__ d_num_rows) {
     __shared__ int warp_sums[33];
+    chain_wait();
     const int n = list_length(nc);
     const int tiles = (nc.bound + HEAD_TILE - 1) / HEAD_TILE;
     for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
@@ -255,9 +287,9 @@ __global__ void __launch_bounds__(HEAD_TILE) k_head_list(const unsigned long lon
         bool head = false, valid = false;
         uint32_t k = 0;
         if (i < n) {
-            k = (uint32_t)(__ldg(sorted + i) >> 32);
+            k = __ldcg(keys + i);
             valid = k < limit;
-            head = valid && (i == 0 || (uint32_t)(__ldg(sorted + i - 1) >> 32) != k);
+            head = valid && (i == 0 || __ldcg(keys + i - 1) != k);
         }
         const int at = before + block_exclusive_scan<HEAD_TILE>(head ? 1 : 0, warp_sums, &total);
         if (head) {
@@ -265,7 +297,7 @@ __global__ void __launch_bounds__(HEAD_TILE) k_head_list(const unsigned long lon
             starts[at] = (int32_t)i;
         }
         // the end of the last run: where the valid entries end
-        if (valid && (i + 1 == n || (uint32_t)(__ldg(sorted + i + 1) >> 32) >= limit)) starts[runs] = (int32_t)i + 1;
+        if (valid && (i + 1 == n || __ldcg(keys + i + 1) >= limit)) starts[runs] = (int32_t)i + 1;
         if (i >= runs && i < nc.bound) rows[i] = -1;
         if (tile == 0 && threadIdx.x == 0) {
             *d_num_rows = runs;
@@ -276,7 +308,7 @@ __global__ void __launch_bounds__(HEAD_TILE) k_head_list(const unsigned long lon
 }
 
 struct EmbedLayout {
-    size_t sort, starts, words, items, longs, partial, total;
+    size_t sort, keys, order, starts, words, items, longs, partial, total;
     int64_t chunks, long_rows;
 };
 
@@ -285,6 +317,8 @@ static EmbedLayout embed_layout(int64_t n, int64_t table_rows, int32_t dim) {
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
     l.sort = take(key_sort_bytes(n));
+    l.keys = take((size_t)n * 4);
+    l.order = take((size_t)n * 4);
     const int64_t rows = (table_rows > n ? table_rows : n) + 1;       // dense: per table row; sparse: per run
     l.starts = take((size_t)rows * 4);
     l.words = take(256 + ((size_t)n / HEAD_TILE + 1) * 4);
@@ -299,28 +333,27 @@ static EmbedLayout embed_layout(int64_t n, int64_t table_rows, int32_t dim) {
 
 size_t embedding_workspace(int64_t n, int64_t table_rows, int32_t dim) { return embed_layout(n, table_rows, dim).total; }
 
-template <typename Tin, typename Tout, int VE> static void run_sum_t(RunSum& P, cudaStream_t s) {
+template <typename Tin, typename Tout, int VE> static cudaError_t run_sum_t(RunSum& P, cudaStream_t s) {
     const int units = P.g.dim / VE;
     P.tl = 1;
     while (P.tl < 32 && P.tl < units) P.tl *= 2;
-    const int per_block = ES_THREADS / P.tl;
+    const int per_block = ES_THREADS / P.tl * ES_ROWS;
     int64_t blocks = ((int64_t)P.rows.bound + per_block - 1) / per_block;
     if (blocks > sm_count() * 256) blocks = sm_count() * 256;
-    k_run_sum<Tin, Tout, VE><<<(int)limit_grid(blocks), ES_THREADS, 0, s>>>(P);
-    count_launches(1);
-    if (P.g.n.bound <= ES_CHUNK) return;           // no run can be longer than a chunk
-    k_run_chunks<Tin, VE><<<(int)limit_grid(sm_count() * 8), ES_THREADS, 0, s>>>(P);
-    k_run_join<Tout><<<(int)limit_grid(sm_count() * 4), ES_THREADS, 0, s>>>(P);
-    count_launches(2);
+    cudaError_t e = launch_train(k_run_sum<Tin, Tout, VE>, blocks, ES_THREADS, 0, s, P);
+    if (P.g.n.bound <= ES_CHUNK || e != cudaSuccess) return e;           // no run can be longer than a chunk
+    e = launch_train(k_run_chunks<Tin, VE>, sm_count() * 8, ES_THREADS, 0, s, P);
+    if (e == cudaSuccess) e = launch_train(k_run_join<Tout>, sm_count() * 4, ES_THREADS, 0, s, P);
+    return e;
 }
 
-template <typename Tin, typename Tout> static void run_sum_tt(RunSum& P, int ve, cudaStream_t s) {
+template <typename Tin, typename Tout> static cudaError_t run_sum_tt(RunSum& P, int ve, cudaStream_t s) {
     if constexpr (sizeof(Tin) == 2) {
         if (ve == 8) return run_sum_t<Tin, Tout, 8>(P, s);
     }
     if (ve == 4) return run_sum_t<Tin, Tout, 4>(P, s);
     if (ve == 2) return run_sum_t<Tin, Tout, 2>(P, s);
-    run_sum_t<Tin, Tout, 1>(P, s);
+    return run_sum_t<Tin, Tout, 1>(P, s);
 }
 
 cudaError_t launch_embedding_grad(const EmbedGrad& g, void* workspace, cudaStream_t s) {
@@ -328,36 +361,36 @@ cudaError_t launch_embedding_grad(const EmbedGrad& g, void* workspace, cudaStrea
     char* ws = (char*)workspace;
     RunSum P{};
     P.g = g;
-    cudaError_t e = launch_key_sort(g.ids, nullptr, g.n, g.table_rows, ws + l.sort, &P.sorted, s);
-    if (e != cudaSuccess) return e;
-    int32_t* starts = (int32_t*)(ws + l.starts);
-    P.starts = starts;
     P.words = (int32_t*)(ws + l.words);
     P.items = (int2*)(ws + l.items);
     P.longs = (int4*)(ws + l.longs);
     P.partial = (float*)(ws + l.partial);
-    e = cudaMemsetAsync(P.words, 0, 8, s);
+    uint32_t* keys = (uint32_t*)(ws + l.keys);
+    int32_t* order = (int32_t*)(ws + l.order);
+    int32_t* starts = (int32_t*)(ws + l.starts);
+    P.order = order;
+    P.starts = starts;
+    cudaError_t e = cudaMemsetAsync(P.words, 0, 8, s);
+    if (e == cudaSuccess) e = launch_key_sort(g.ids, nullptr, g.n, g.table_rows, ws + l.sort, keys, order, s);
     if (e != cudaSuccess) return e;
     if (g.rows) {
         int32_t* heads = P.words + 64;
         const int64_t tiles = ((int64_t)g.n.bound + HEAD_TILE - 1) / HEAD_TILE;
-        const int grid = (int)limit_grid(tiles < sm_count() * 2 ? tiles : sm_count() * 2);
-        k_head_counts<<<grid, HEAD_TILE, 0, s>>>(P.sorted, g.n, (uint32_t)g.table_rows, heads);
-        k_head_list<<<grid, HEAD_TILE, 0, s>>>(P.sorted, g.n, (uint32_t)g.table_rows, heads, g.rows, starts, g.d_num_rows);
-        count_launches(2);
+        const int64_t grid = tiles < sm_count() * 2 ? tiles : sm_count() * 2;
+        e = launch_train(k_head_counts, grid, HEAD_TILE, 0, s, keys, g.n, (uint32_t)g.table_rows, heads);
+        if (e == cudaSuccess) e = launch_train(k_head_list, grid, HEAD_TILE, 0, s, keys, g.n, (uint32_t)g.table_rows, heads, g.rows, starts, g.d_num_rows);
         P.rows = Count{g.d_num_rows, g.n.bound};
     } else {
         P.rows = Count{nullptr, (int32_t)g.table_rows};
-        e = launch_row_starts(P.sorted, g.n, P.rows, starts, s);
-        if (e != cudaSuccess) return e;
+        e = launch_row_starts(keys, g.n, P.rows, starts, s);
     }
+    if (e != cudaSuccess) return e;
     const int in = bytes_of(g.dout_dtype), out = bytes_of(g.grad_dtype);
     const int ve = unit_elems(g.dout, g.dout_ld, in, g.grad, g.grad_ld, out, g.dim);
-    if (in == 4 && out == 4) run_sum_tt<float, float>(P, ve, s);
-    else if (in == 4) run_sum_tt<float, bf16>(P, ve, s);
-    else if (out == 4) run_sum_tt<bf16, float>(P, ve, s);
-    else run_sum_tt<bf16, bf16>(P, ve, s);
-    return cudaGetLastError();
+    if (in == 4 && out == 4) return run_sum_tt<float, float>(P, ve, s);
+    if (in == 4) return run_sum_tt<float, bf16>(P, ve, s);
+    if (out == 4) return run_sum_tt<bf16, float>(P, ve, s);
+    return run_sum_tt<bf16, bf16>(P, ve, s);
 }
 
 }  // namespace gs

@@ -30,7 +30,9 @@ struct KeySort {
     int32_t* ticket;         // [4]
     uint32_t* state;         // this pass: [tiles][256]: 2 flag bits, 30 bits of count
     const unsigned long long* src;
-    unsigned long long* dst;
+    unsigned long long* dst;      // passes before the last: key << 32 | payload
+    uint32_t* out_keys;           // last pass
+    int32_t* out_payload;
 };
 
 __device__ __forceinline__ int count_of(const Count& c) {
@@ -44,23 +46,42 @@ __device__ __forceinline__ uint32_t clamp_key(int32_t k, uint32_t limit) {
 }
 
 __device__ __forceinline__ unsigned long long first_word(const KeySort& P, int i) {
-    return ((unsigned long long)clamp_key(__ldg(P.keys + i), P.key_limit) << 32) | (uint32_t)(P.payload ? __ldg(P.payload + i) : i);
+    return ((unsigned long long)clamp_key(__ldg(P.keys + i), P.key_limit) << 32) | (uint32_t)(P.payload ? __ldcg(P.payload + i) : i);
 }
 
 __global__ void __launch_bounds__(KS_THREADS) k_key_hist(KeySort P) {
+    constexpr int U = 4;
     __shared__ int h[4][256];
+    chain_wait();
     const int n = count_of(P.n);
     for (int i = threadIdx.x; i < 1024; i += KS_THREADS) (&h[0][0])[i] = 0;
     __syncthreads();
-    for (int64_t i = (int64_t)blockIdx.x * KS_THREADS + threadIdx.x; i < n; i += (int64_t)gridDim.x * KS_THREADS) {
-        const uint32_t k = clamp_key(__ldg(P.keys + i), P.key_limit);
-        for (int p = 0; p < P.passes; ++p) atomicAdd(&h[p][(k >> (8 * p)) & 255u], 1);
+    for (int64_t i = (int64_t)blockIdx.x * KS_THREADS * U + threadIdx.x; i < n; i += (int64_t)gridDim.x * KS_THREADS * U) {
+        uint32_t k[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) k[j] = i + j * KS_THREADS < n ? clamp_key(__ldg(P.keys + i + j * KS_THREADS), P.key_limit) : 0xFFFFFFFFu;
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            if (i + j * KS_THREADS < n)
+                for (int p = 0; p < P.passes; ++p) atomicAdd(&h[p][(k[j] >> (8 * p)) & 255u], 1);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 256 * P.passes; i += KS_THREADS) {
         const int c = (&h[0][0])[i];
         if (c) atomicAdd(P.hist + i, c);
     }
+}
+
+// Lanes whose digit equals this lane's, from one ballot per bit (a match instruction takes time for every distinct
+// digit in the warp: 2 M keys, 50 us a pass).
+__device__ __forceinline__ uint32_t same_digit(uint32_t d) {
+    uint32_t same = FULL;
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+        const uint32_t set = __ballot_sync(FULL, (d >> b) & 1u);
+        same &= (d >> b) & 1u ? set : ~set;
+    }
+    return same;
 }
 
 // Ranks a warp's keys round by round: rank[r] = keys of the same digit before this one in the warp's share,
@@ -70,21 +91,23 @@ __device__ __forceinline__ void rank_rounds(const unsigned long long (&key)[ROUN
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) {
         const uint32_t d = (uint32_t)(key[r] >> shift) & 255u;
-        const uint32_t same = __match_any_sync(FULL, d);
-        rank[r] = cnt[d] + __popc(same & lanemask_lt());
+        const uint32_t same = same_digit(d), before = __popc(same & lanemask_lt());
+        const int base = cnt[d];
+        rank[r] = base + before;
         __syncwarp();
-        if ((same & lanemask_lt()) == 0) cnt[d] += __popc(same);
+        if (before == 0) cnt[d] = base + __popc(same);
         __syncwarp();
     }
 }
 
-__global__ void __launch_bounds__(KS_THREADS) k_key_pass(KeySort P, int first) {
+__global__ void __launch_bounds__(KS_THREADS, 3) k_key_pass(KeySort P, int first, int last) {
     __shared__ unsigned long long pairs[KS_TILE];
     __shared__ int cnt[KS_WARPS][256];
     __shared__ int local_start[256];     // first place of a digit inside the tile
     __shared__ int out_base[256];        // output position of the tile's pair j of digit d is out_base[d] + j
     __shared__ int warp_sums[33];
     __shared__ int s_tile;
+    chain_wait();
     const int n = count_of(P.n);
     const int tiles = (int)(((int64_t)n + KS_TILE - 1) / KS_TILE);
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, d = threadIdx.x;
@@ -146,7 +169,13 @@ __global__ void __launch_bounds__(KS_THREADS) k_key_pass(KeySort P, int first) {
         for (int j = threadIdx.x; j < KS_TILE; j += KS_THREADS) {
             const unsigned long long w = pairs[j];
             const int64_t at = (int64_t)out_base[(uint32_t)(w >> P.shift) & 255u] + j;
-            if (at >= 0 && at < n) P.dst[at] = w;
+            if (at < 0 || at >= n) continue;
+            if (last) {
+                P.out_keys[at] = (uint32_t)(w >> 32);
+                P.out_payload[at] = (int32_t)(uint32_t)w;
+            } else {
+                P.dst[at] = w;
+            }
         }
     }
 }
@@ -158,6 +187,7 @@ __global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P) 
     int* cnt = reinterpret_cast<int*>(small_pairs + KS_SMALL);
     __shared__ int start[256];
     __shared__ int warp_sums[33];
+    chain_wait();
     const int n = count_of(P.n);
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     unsigned long long key[R];
@@ -197,7 +227,10 @@ __global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P) 
         }
         __syncthreads();
     }
-    for (int j = threadIdx.x; j < n; j += KS_SMALL_THREADS) P.dst[j] = small_pairs[j];
+    for (int j = threadIdx.x; j < n; j += KS_SMALL_THREADS) {
+        P.out_keys[j] = (uint32_t)(small_pairs[j] >> 32);
+        P.out_payload[j] = (int32_t)(uint32_t)small_pairs[j];
+    }
 }
 
 static int64_t ks_tiles(int64_t n) { return (n + KS_TILE - 1) / KS_TILE; }
@@ -207,28 +240,26 @@ size_t key_sort_bytes(int64_t n) {
 }
 
 cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n, int64_t key_limit, void* workspace,
-                            const unsigned long long** sorted, cudaStream_t s) {
+                            uint32_t* out_keys, int32_t* out_payload, cudaStream_t s) {
     KeySort P{};
     P.keys = keys;
     P.payload = payload;
     P.n = n;
     P.key_limit = (uint32_t)key_limit;
+    P.out_keys = out_keys;
+    P.out_payload = out_payload;
     int bits = 1;
     while (bits < 32 && (key_limit >> bits)) ++bits;
     P.passes = (bits + 7) / 8;
+    if (n.bound <= KS_SMALL) {
+        constexpr int smem = KS_SMALL * 8 + (KS_SMALL_THREADS / 32) * 256 * 4;
+        const cudaError_t e = cudaFuncSetAttribute(k_key_sort_small, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        return launch_train(k_key_sort_small, 1, KS_SMALL_THREADS, smem, s, P);
+    }
     const size_t buf = align_up((size_t)n.bound * 8, 256);
     unsigned long long* a = (unsigned long long*)workspace;
     unsigned long long* b = (unsigned long long*)((char*)workspace + buf);
-    if (n.bound <= KS_SMALL) {
-        constexpr int smem = KS_SMALL * 8 + (KS_SMALL_THREADS / 32) * 256 * 4;
-        cudaError_t e = cudaFuncSetAttribute(k_key_sort_small, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
-        P.dst = a;
-        k_key_sort_small<<<1, KS_SMALL_THREADS, smem, s>>>(P);
-        *sorted = a;
-        count_launches(1);
-        return cudaGetLastError();
-    }
     const int64_t tiles = ks_tiles(n.bound);
     int32_t* words = (int32_t*)((char*)workspace + 2 * buf);
     int32_t* hist = words;
@@ -237,71 +268,76 @@ cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n
     cudaError_t e = cudaMemsetAsync(words, 0, (1028 + (size_t)tiles * 256 * P.passes) * 4, s);
     if (e != cudaSuccess) return e;
     P.hist = hist;
-    k_key_hist<<<(int)limit_grid(tiles < sm_count() * 4 ? tiles : sm_count() * 4), KS_THREADS, 0, s>>>(P);
-    for (int p = 0; p < P.passes; ++p) {
+    int64_t grid = (n.bound + KS_THREADS * 4 - 1) / (KS_THREADS * 4);
+    if (grid > sm_count() * 8) grid = sm_count() * 8;
+    e = launch_train(k_key_hist, grid, KS_THREADS, 0, s, P);
+    grid = tiles < sm_count() * 3 ? tiles : sm_count() * 3;
+    for (int p = 0; p < P.passes && e == cudaSuccess; ++p) {
         P.shift = 32 + 8 * p;
         P.hist = hist + 256 * p;
         P.ticket = ticket + p;
         P.state = state + (size_t)tiles * 256 * p;
         P.src = (p & 1) ? a : b;
         P.dst = (p & 1) ? b : a;
-        const int64_t grid = tiles < sm_count() * 4 ? tiles : sm_count() * 4;
-        k_key_pass<<<(int)limit_grid(grid), KS_THREADS, 0, s>>>(P, p == 0);
+        e = launch_train(k_key_pass, grid, KS_THREADS, 0, s, P, (int)(p == 0), (int)(p + 1 == P.passes));
     }
-    *sorted = (P.passes & 1) ? a : b;
-    count_launches(1 + P.passes);
-    return cudaGetLastError();
+    return e;
 }
 
 // ---------------------------------------------------------------- row offsets of the sorted list
-__device__ __forceinline__ int lower_bound_key(const unsigned long long* sorted, int lo, int hi, uint32_t key) {
+__device__ __forceinline__ int lower_bound_key(const uint32_t* keys, int lo, int hi, uint32_t key) {
     while (lo < hi) {
         const int mid = (int)(((unsigned)lo + (unsigned)hi) >> 1);
-        if ((uint32_t)(__ldg(sorted + mid) >> 32) < key) lo = mid + 1;
+        if (__ldca(keys + mid) < key) lo = mid + 1;
         else hi = mid;
     }
     return lo;
 }
 
-constexpr int RS_ROWS = 256;
+// The same by a whole warp: 32 probes per step.
+__device__ __forceinline__ int lower_bound_warp(const uint32_t* keys, int n, uint32_t key) {
+    int lo = 0, hi = n;                                    // the answer lies in [lo, hi]
+    const int lane = threadIdx.x & 31;
+    while (lo < hi) {
+        const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+        const uint32_t less = __ballot_sync(FULL, at < hi && __ldcg(keys + at) < key);   // a prefix of the lanes
+        const int k = __popc(less);
+        if (k == 0) return lo;
+        hi = k < 32 && lo + k * step < hi ? lo + k * step : hi;
+        lo = lo + (k - 1) * step + 1;
+    }
+    return lo;
+}
 
-// A block finds the range of its 256 rows first, so that the rows' own searches stay in a narrow window.
-__global__ void __launch_bounds__(RS_ROWS) k_row_starts(const unsigned long long* __restrict__ sorted, Count nc, Count rc,
-                                                        int32_t* __restrict__ starts) {
+constexpr int RS_THREADS = 256, RS_ROWS = 1024;
+
+// A block finds the range of its rows first, so that the rows' own searches stay in a narrow window.
+__global__ void __launch_bounds__(RS_THREADS) k_row_starts(const uint32_t* __restrict__ keys, Count nc, Count rc, int32_t* __restrict__ starts) {
     __shared__ int range[2];
+    chain_wait();
     const int n = count_of(nc);
     const int64_t rows = (int64_t)count_of(rc) + 1;      // one more than the rows: the end of the last
     for (int64_t r0 = (int64_t)blockIdx.x * RS_ROWS; r0 < rows; r0 += (int64_t)gridDim.x * RS_ROWS) {
-        if (threadIdx.x < 2) {
-            const int64_t r = r0 + (threadIdx.x ? RS_ROWS : 0);
-            range[threadIdx.x] = lower_bound_key(sorted, 0, n, (uint32_t)r);
+        __syncthreads();
+        if (threadIdx.x < 64) {
+            const int64_t r = r0 + (threadIdx.x >= 32 ? RS_ROWS : 0);
+            const int at = lower_bound_warp(keys, n, (uint32_t)r);
+            if ((threadIdx.x & 31) == 0) range[threadIdx.x >> 5] = at;
         }
         __syncthreads();
-        const int64_t r = r0 + threadIdx.x;
-        if (r < rows) starts[r] = lower_bound_key(sorted, range[0], range[1], (uint32_t)r);
-        __syncthreads();
+        const int lo = range[0], hi = range[1];
+#pragma unroll
+        for (int j = 0; j < RS_ROWS / RS_THREADS; ++j) {
+            const int64_t r = r0 + j * RS_THREADS + threadIdx.x;
+            if (r < rows) starts[r] = lower_bound_key(keys, lo, hi, (uint32_t)r);
+        }
     }
 }
 
-cudaError_t launch_row_starts(const unsigned long long* sorted, Count n, Count rows, int32_t* starts, cudaStream_t s) {
+cudaError_t launch_row_starts(const uint32_t* keys, Count n, Count rows, int32_t* starts, cudaStream_t s) {
     int64_t blocks = ((int64_t)rows.bound + 1 + RS_ROWS - 1) / RS_ROWS;
-    if (blocks > sm_count() * 64) blocks = sm_count() * 64;
-    k_row_starts<<<(int)limit_grid(blocks), RS_ROWS, 0, s>>>(sorted, n, rows, starts);
-    count_launches(1);
-    return cudaGetLastError();
-}
-
-__global__ void __launch_bounds__(256) k_payloads(const unsigned long long* __restrict__ sorted, Count nc, int32_t* __restrict__ out) {
-    const int n = count_of(nc);
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) out[i] = (int32_t)(uint32_t)__ldcs(sorted + i);
-}
-
-cudaError_t launch_payloads(const unsigned long long* sorted, Count n, int32_t* payloads, cudaStream_t s) {
-    int64_t blocks = ((int64_t)n.bound + 255) / 256;
-    if (blocks > sm_count() * 16) blocks = sm_count() * 16;
-    k_payloads<<<(int)limit_grid(blocks), 256, 0, s>>>(sorted, n, payloads);
-    count_launches(1);
-    return cudaGetLastError();
+    if (blocks > sm_count() * 32) blocks = sm_count() * 32;
+    return launch_train(k_row_starts, blocks, RS_THREADS, 0, s, keys, n, rows, starts);
 }
 
 cudaError_t train_gave_up(cudaStream_t s, int* h_sort) {

@@ -15,16 +15,30 @@ struct Count {
     int32_t bound;
 };
 
-// ---- stable sort of (key, payload) pairs; result: key << 32 | payload, ascending keys, equal keys in input order ----
+// Kernels of a call are set up while their predecessor drains; each begins with chain_wait().
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_train(void (*kernel)(KArgs...), int64_t grid, int block, size_t smem, cudaStream_t s, Args... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)limit_grid(grid));
+    cfg.blockDim = dim3((unsigned)block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    count_launches(1);
+    return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+
+// ---- stable sort of (key, payload) pairs by key: ascending keys, equal keys in input order ----
 size_t key_sort_bytes(int64_t n_bound);
 // Keys outside [0, key_limit) take the value key_limit and end behind all others.  payload NULL: the position.
-// The sorted words are left in *sorted (inside the workspace), which stays valid until the workspace is used again.
 cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n, int64_t key_limit, void* workspace,
-                            const unsigned long long** sorted, cudaStream_t s);
-// starts[r] = number of sorted words with key < r, r = 0 .. rows (rows from the device if rows.d_n is set).
-cudaError_t launch_row_starts(const unsigned long long* sorted, Count n, Count rows, int32_t* starts, cudaStream_t s);
-// payloads[i] = low word of sorted[i]
-cudaError_t launch_payloads(const unsigned long long* sorted, Count n, int32_t* payloads, cudaStream_t s);
+                            uint32_t* out_keys, int32_t* out_payload, cudaStream_t s);
+// starts[r] = number of sorted keys < r, r = 0 .. rows (rows from the device if rows.d_n is set).
+cudaError_t launch_row_starts(const uint32_t* keys, Count n, Count rows, int32_t* starts, cudaStream_t s);
 cudaError_t train_gave_up(cudaStream_t s, int* h_sort);
 
 // ---- embedding rows ----
