@@ -17,12 +17,6 @@ constexpr int RING_DEPTH = RING_SLOTS - 1;
 constexpr int RING_WARPS = 2;            // warps per block
 constexpr int RING_ROWS = 64;            // rows whose offsets a warp holds at a time
 
-template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int n) {   // n bytes, the rest zero
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-    else if constexpr (BYTES == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-
 template <int N> __device__ __forceinline__ float dot2(const f32x2 (&a)[N], const f32x2 (&b)[N]) {
     f32x2 s = mul2(a[0], b[0]);
 #pragma unroll
@@ -140,12 +134,22 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
             next = 0;
 #pragma unroll
             for (int j = 0; j < U; ++j) idx[j] = -1;
-            if (lu >= left) return;
+            int4 r;
             if (fresh) {
-                const int v = off + lu;
-                lr = upr == 1 ? v : v / upr;
-                head = v - lr * upr;
-                const int4 r = rows_s[lr];
+                for (;; lu += gpw) {
+                    if (lu >= left) return;
+                    const int v = off + lu;
+                    lr = upr == 1 ? v : v / upr;
+                    head = v - lr * upr;
+                    r = rows_s[lr];
+                    if (K != AT_DKV || r.y > r.x) break;
+                    // a source that no destination lists: zeros at once (a listed long row: nothing)
+                    if (r.w >= 0 && !P.chunk_mode) {
+                        const float zero[E] = {};
+                        store_piece<T, VE, NV>((T*)P.a.dk.data + (int64_t)r.z * P.a.dk.row_stride + (int64_t)head * P.a.dk.head_stride, t, tl, D, zero);
+                        store_piece<T, VE, NV>((T*)P.a.dv.data + (int64_t)r.z * P.a.dv.row_stride + (int64_t)head * P.a.dv.head_stride, t, tl, D, zero);
+                    }
+                }
                 e_next = r.x;
                 e_end = r.y;
                 pass = 0;

@@ -3,7 +3,7 @@
 // The gradient of row r is scale * (sum of the rows dout[p] with ids[p] = r): the positions are sorted by id (stable,
 // gs_sort.cu), the rows of a run are added in ascending position in 32 bits and rounded once.  No atomics on
 // floats: the result does not depend on the schedule.  Runs of up to ES_CHUNK entries are summed by the group of
-// lanes that writes the row; a longer run (a hub) is cut into chunks whose sums go to the workspace and are added in order.
+// lanes that meets their head; a longer run (a hub) is cut into chunks whose sums go to the workspace and are added in order.
 #include "gs_device.cuh"
 #include "gs_train.cuh"
 #include "gs_train.h"
@@ -100,37 +100,55 @@ cudaError_t launch_embedding_lookup(const EmbedLookup& p, cudaStream_t s) {
 }
 
 // ---------------------------------------------------------------- gradient
-constexpr int ES_CHUNK = 256;       // entries of one run summed by one group of lanes
-constexpr int ES_UNROLL = 4;        // rows in flight per lane
-constexpr int ES_ROWS = 4;          // rows a group of lanes takes at a time
+constexpr int ES_CHUNK = 32;        // entries of one run summed by the group of lanes that meets its head
+constexpr int ES_UNROLL = 8;        // rows in flight per lane
 constexpr int ES_THREADS = 256;
-constexpr int HEAD_TILE = 1024;
+constexpr int ES_TILE = ES_THREADS; // sorted entries per block of the sums
 
 struct RunSum {
     EmbedGrad g;
-    const int32_t* order;           // positions in the order of their ids
-    const int32_t* starts;          // row r's entries are order[starts[r] .. starts[r + 1])
-    Count rows;                     // dense: the table's rows; sparse: the runs (device) of at most n
-    int tl;                         // lanes per row (power of two)
-    int32_t* words;                 // [0] chunks, [1] long rows
-    int2* items;                    // chunk -> (row, chunk of the row)
-    int4* longs;                    // long row -> (row, first chunk, chunks, -)
+    const uint32_t* keys;           // ids, ascending (table_rows stands for ids outside the table)
+    const int32_t* order;           // their positions
+    const int32_t* tile_runs;       // sparse: runs before each tile of the list
+    int tl;                         // lanes per row (a power of two)
+    int32_t* words;                 // [0] chunks, [1] long runs
+    int2* items;                    // chunk -> entries [x, y)
+    int4* longs;                    // long run -> (row of the gradient, first chunk, chunks, -)
     float* partial;                 // [chunks][dim]
 };
 
-// Sum of the entries [b, e) at columns c .. c + VE of dout, in ascending position.
+// First entry behind the run of `key` that entry e belongs to.
+__device__ __forceinline__ int run_end(const uint32_t* keys, int e, int n, uint32_t key) {
+    int lo = e, step = ES_CHUNK;                       // keys[lo] == key; double the step, then halve it
+    while (lo + step < n && __ldcg(keys + lo + step) == key) {
+        lo += step;
+        step *= 2;
+    }
+    for (; step > 0; step >>= 1)
+        while (lo + step < n && __ldcg(keys + lo + step) == key) lo += step;
+    return lo + 1;
+}
+
+// A hub's run is listed for the chunk kernel.
+__device__ __forceinline__ void list_run(const RunSum& P, int row, int b, int e) {
+    const int nc = (e - b + ES_CHUNK - 1) / ES_CHUNK;
+    const int at = atomicAdd(P.words, nc);
+    P.longs[atomicAdd(P.words + 1, 1)] = make_int4(row, at, nc, 0);
+    for (int c = 0; c < nc; ++c) P.items[at + c] = make_int2(b + c * ES_CHUNK, b + (c + 1) * ES_CHUNK < e ? b + (c + 1) * ES_CHUNK : e);
+}
+
+// Adds the entries [b, e) at columns col .. col + VE of dout in ascending position.
 template <typename Tin, int VE>
-__device__ __forceinline__ void run_sum(const RunSum& P, int b, int e, int col, float (&acc)[VE]) {
+__device__ __forceinline__ void add_entries(const RunSum& P, int b, int e, int64_t col, float (&acc)[VE]) {
     const Tin* dout = (const Tin*)P.g.dout + col;
-#pragma unroll
-    for (int i = 0; i < VE; ++i) acc[i] = 0.f;
+    constexpr int U = ES_UNROLL;
     int k = b;
-    for (; k + ES_UNROLL <= e; k += ES_UNROLL) {
-        Raw<Tin, VE> v[ES_UNROLL];
+    for (; k + U <= e; k += U) {
+        Raw<Tin, VE> v[U];
 #pragma unroll
-        for (int j = 0; j < ES_UNROLL; ++j) v[j] = load_raw_stream<Tin, VE>(dout + (int64_t)__ldcg(P.order + k + j) * P.g.dout_ld);
+        for (int j = 0; j < U; ++j) v[j] = load_raw_stream<Tin, VE>(dout + (int64_t)__ldcg(P.order + k + j) * P.g.dout_ld);
 #pragma unroll
-        for (int j = 0; j < ES_UNROLL; ++j) {
+        for (int j = 0; j < U; ++j) {
             float x[VE];
             unpack<Tin, VE>(v[j], x);
 #pragma unroll
@@ -145,60 +163,104 @@ __device__ __forceinline__ void run_sum(const RunSum& P, int b, int e, int col, 
     }
 }
 
-// Most rows have one entry or none, so a group of lanes takes ES_ROWS neighbouring rows at a time: their offsets, first
-// positions and first rows are each in flight together.
-template <typename Tin, typename Tout, int VE>
-__global__ void __launch_bounds__(ES_THREADS) k_run_sum(RunSum P) {
+// The sorted entries, in equal pieces: a group of tl lanes takes tl neighbouring entries, whose rows are all in flight
+// whatever runs they belong to, and owns the runs whose heads it meets (the last one beyond its own entries, if it
+// continues).  Work by entries, not by rows: rows of the table are many and mostly empty, and the frequent ids lie together.
+template <typename Tin, typename Tout, int VE, bool SPARSE>
+__global__ void __launch_bounds__(ES_THREADS, 4) k_run_sum(RunSum P) {
+    __shared__ int warp_sums[33];
     chain_wait();
-    const int rows = list_length(P.rows), bound = P.rows.bound;
-    const int units = P.g.dim / VE, t = threadIdx.x & (P.tl - 1);
-    const int per_block = ES_THREADS / P.tl;
+    const int n = list_length(P.g.n), bound = P.g.n.bound;
+    const uint32_t limit = (uint32_t)P.g.table_rows;
+    const int tiles = (bound + ES_TILE - 1) / ES_TILE;
+    const int lane = threadIdx.x & 31, tl = P.tl, t = lane & (tl - 1), base = lane & ~(tl - 1);
+    const int units = P.g.dim / VE;
+    const uint32_t group = tl == 32 ? FULL : ((1u << tl) - 1u) << base;
     const Tin* dout = (const Tin*)P.g.dout;
-    Tout* grad = (Tout*)P.g.grad;
-    for (int64_t r = ((int64_t)blockIdx.x * per_block + threadIdx.x / P.tl) * ES_ROWS; r < bound; r += (int64_t)gridDim.x * per_block * ES_ROWS) {
-        int b[ES_ROWS + 1], first[ES_ROWS];
-#pragma unroll
-        for (int j = 0; j <= ES_ROWS; ++j) b[j] = __ldcg(P.starts + (r + j < rows ? r + j : rows));      // behind the last row: empty
-#pragma unroll
-        for (int j = 0; j < ES_ROWS; ++j) first[j] = b[j + 1] > b[j] ? __ldcg(P.order + b[j]) : -1;
-        bool listed[ES_ROWS];
-#pragma unroll
-        for (int j = 0; j < ES_ROWS; ++j) {
-            const int len = b[j + 1] - b[j];
-            listed[j] = len > ES_CHUNK;
-            if (listed[j] && t == 0) {
-                const int nc = (len + ES_CHUNK - 1) / ES_CHUNK;
-                const int at = atomicAdd(P.words, nc);
-                P.longs[atomicAdd(P.words + 1, 1)] = make_int4((int)(r + j), at, nc, 0);
-                for (int c = 0; c < nc; ++c) P.items[at + c] = make_int2((int)(r + j), c);
+    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int before = SPARSE ? __ldcg(P.tile_runs + tile) : 0, runs = SPARSE ? __ldcg(P.g.d_num_rows) : 0;
+        {
+            const int64_t e64 = (int64_t)tile * ES_TILE + threadIdx.x;
+            const int e = e64 < bound ? (int)e64 : bound;
+            uint32_t key = limit;
+            int pos = 0;
+            bool head = false;
+            if (e < n) {
+                key = __ldcg(P.keys + e);
+                pos = __ldcg(P.order + e);
+                head = key < limit && (e == 0 || __ldcg(P.keys + e - 1) != key);
             }
-        }
-        for (int u = t; u < units; u += P.tl) {
-            Raw<Tin, VE> v[ES_ROWS];
-#pragma unroll
-            for (int j = 0; j < ES_ROWS; ++j)
-                v[j] = first[j] >= 0 && !listed[j] ? load_raw_stream<Tin, VE>(dout + (int64_t)first[j] * P.g.dout_ld + (int64_t)u * VE) : zero_raw<Tin, VE>();
-#pragma unroll
-            for (int j = 0; j < ES_ROWS; ++j) {
-                if (r + j >= bound || listed[j]) continue;
+            int row = (int)key;
+            if (SPARSE) {
+                int total;
+                row = before + block_exclusive_scan<ES_THREADS>(head ? 1 : 0, warp_sums, &total);
+                if (head) P.g.rows[row] = (int32_t)key;
+                if (e >= runs && e < bound) P.g.rows[e] = -1;
+            }
+            bool is_long = false;
+            if (head && e + ES_CHUNK < n && __ldcg(P.keys + e + ES_CHUNK) == key) {
+                is_long = true;
+                list_run(P, row, e, run_end(P.keys, e, n, key));
+            }
+            const uint32_t heads = __ballot_sync(FULL, head) & group, longs = __ballot_sync(FULL, is_long), valid = __ballot_sync(FULL, key < limit);
+            for (int u = t; u < units + t; u += tl) {                  // the same number of turns for all lanes
+                const bool on = u < units;
+                const int64_t col = (int64_t)u * VE;
                 float acc[VE];
-                unpack<Tin, VE>(v[j], acc);
-                if (b[j + 1] - b[j] > 1) {
-                    float more[VE];
-                    run_sum<Tin, VE>(P, b[j] + 1, b[j + 1], u * VE, more);
 #pragma unroll
-                    for (int i = 0; i < VE; ++i) acc[i] += more[i];
-                }
-                if (first[j] >= 0) {
+                for (int i = 0; i < VE; ++i) acc[i] = 0.f;
+                int open = -1;                                         // lane of the head of the run being summed
+                auto flush = [&](int row_of) {
+                    if (!on) return;
 #pragma unroll
                     for (int i = 0; i < VE; ++i) acc[i] *= P.g.scale;
+                    store_vec<Tout, VE>((Tout*)P.g.grad + (int64_t)row_of * P.g.grad_ld + col, acc);
+                };
+                for (int j0 = 0; j0 < tl; j0 += ES_UNROLL) {
+                    Raw<Tin, VE> v[ES_UNROLL];
+#pragma unroll
+                    for (int j = 0; j < ES_UNROLL; ++j) {
+                        const int l = base + ((j0 + j) & (tl - 1)), p = __shfl_sync(FULL, pos, l);
+                        const uint32_t upto = heads & (0xFFFFFFFFu >> (31 - l));      // heads of this group up to entry l
+                        const bool want = on && j0 + j < tl && ((valid >> l) & 1) && upto && !((longs >> (31 - __clz(upto))) & 1);
+                        v[j] = want ? load_raw_stream<Tin, VE>(dout + (int64_t)p * P.g.dout_ld + col) : zero_raw<Tin, VE>();
+                    }
+#pragma unroll
+                    for (int j = 0; j < ES_UNROLL; ++j) {
+                        const int l = base + ((j0 + j) & (tl - 1));
+                        const bool starts = j0 + j < tl && ((heads >> l) & 1), ends = j0 + j < tl && !((valid >> l) & 1);
+                        const int row_of = __shfl_sync(FULL, row, open < 0 ? base : open);
+                        if ((starts || ends) && open >= 0) flush(row_of);
+                        float x[VE];
+                        unpack<Tin, VE>(v[j], x);
+#pragma unroll
+                        for (int i = 0; i < VE; ++i) acc[i] = starts ? x[i] : acc[i] + x[i];
+                        if (starts) open = (longs >> l) & 1 ? -1 : l;
+                        if (ends) open = -1;
+                    }
                 }
-                store_vec<Tout, VE>(grad + (r + j) * P.g.grad_ld + (int64_t)u * VE, acc);
+                const int row_of = __shfl_sync(FULL, row, open < 0 ? base : open);
+                const uint32_t open_key = __shfl_sync(FULL, key, open < 0 ? base : open);
+                if (open >= 0) {
+                    const int from = e - t + tl;                       // behind the group's entries
+                    int to = from;
+                    while (to < n && to - from < ES_CHUNK && __ldcg(P.keys + to) == open_key) ++to;
+                    if (on && to > from) add_entries<Tin, VE>(P, from, to, col, acc);
+                    flush(row_of);
+                }
+                __syncwarp();
             }
+        }
+        if (SPARSE) {                                                  // rows behind the last run
+            const int64_t first = (int64_t)tile * ES_TILE, end = first + ES_TILE < bound ? first + ES_TILE : bound;
+            const float zero[VE] = {};
+            for (int64_t r = (first > runs ? first : runs) + threadIdx.x / tl; r < end; r += ES_THREADS / tl)
+                for (int u = t; u < units; u += tl) store_vec<Tout, VE>((Tout*)P.g.grad + r * P.g.grad_ld + (int64_t)u * VE, zero);
         }
     }
 }
 
+// The listed runs, ES_CHUNK entries at a time.
 template <typename Tin, int VE>
 __global__ void __launch_bounds__(ES_THREADS) k_run_chunks(RunSum P) {
     chain_wait();
@@ -207,11 +269,11 @@ __global__ void __launch_bounds__(ES_THREADS) k_run_chunks(RunSum P) {
     const int per_block = ES_THREADS / P.tl;
     for (int64_t c = (int64_t)blockIdx.x * per_block + threadIdx.x / P.tl; c < chunks; c += (int64_t)gridDim.x * per_block) {
         const int2 it = P.items[c];
-        const int b = __ldcg(P.starts + it.x) + it.y * ES_CHUNK;
-        const int end = __ldcg(P.starts + it.x + 1), e = b + ES_CHUNK < end ? b + ES_CHUNK : end;
         for (int u = t; u < units; u += P.tl) {
             float acc[VE];
-            run_sum<Tin, VE>(P, b, e, u * VE, acc);
+#pragma unroll
+            for (int i = 0; i < VE; ++i) acc[i] = 0.f;
+            add_entries<Tin, VE>(P, it.x, it.y, (int64_t)u * VE, acc);
 #pragma unroll
             for (int i = 0; i < VE; ++i) P.partial[c * P.g.dim + u * VE + i] = acc[i];
         }
@@ -248,99 +310,82 @@ __global__ void __launch_bounds__(ES_THREADS) k_run_join(RunSum P) {
 }
 
 // Heads of runs of equal ids per tile of the sorted list ...
-__global__ void __launch_bounds__(HEAD_TILE) k_head_counts(const uint32_t* __restrict__ keys, Count nc, uint32_t limit,
-                                                           int32_t* __restrict__ tile_heads) {
+__global__ void __launch_bounds__(ES_THREADS) k_head_counts(const uint32_t* __restrict__ keys, Count nc, uint32_t limit,
+                                                            int32_t* __restrict__ tile_runs) {
     chain_wait();
-    const int n = list_length(nc);
-    const int tiles = (nc.bound + HEAD_TILE - 1) / HEAD_TILE;
-    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t i = (int64_t)tile * HEAD_TILE + threadIdx.x;
-        bool head = false;
-        if (i < n) {
-            const uint32_t k = __ldcg(keys + i);
-            head = k < limit && (i == 0 || __ldcg(keys + i - 1) != k);
+    const int n = list_length(nc), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int tiles = (nc.bound + ES_TILE - 1) / ES_TILE;
+    // a warp per tile
+    for (int tile = blockIdx.x * (ES_THREADS / 32) + warp; tile < tiles; tile += gridDim.x * (ES_THREADS / 32)) {
+        int c = 0;
+#pragma unroll
+        for (int j = 0; j < ES_TILE; j += 32) {
+            const int64_t i = (int64_t)tile * ES_TILE + j + lane;
+            const uint32_t k = i < n ? __ldcg(keys + i) : limit;
+            uint32_t prev = __shfl_up_sync(FULL, k, 1);
+            if (lane == 0) prev = i > 0 && i < n ? __ldcg(keys + i - 1) : 0xFFFFFFFFu;
+            c += __popc(__ballot_sync(FULL, k < limit && k != prev));
         }
-        const int c = __syncthreads_count(head);
-        if (threadIdx.x == 0) tile_heads[tile] = c;
+        if (lane == 0) tile_runs[tile] = c;
     }
 }
 
-// ... and the list of runs: id and first entry of each; -1 behind the last one.
-__global__ void __launch_bounds__(HEAD_TILE) k_head_list(const uint32_t* __restrict__ keys, Count nc, uint32_t limit,
-                                                         const int32_t* __restrict__ tile_heads, int32_t* __restrict__ rows,
-                                                         int32_t* __restrict__ starts, int32_t* __restrict__ d_num_rows) {
+// ... and the runs before each tile, and in all.
+__global__ void __launch_bounds__(1024) k_head_scan(int tiles, int32_t* __restrict__ tile_runs, int32_t* __restrict__ d_num_rows) {
     __shared__ int warp_sums[33];
     chain_wait();
-    const int n = list_length(nc);
-    const int tiles = (nc.bound + HEAD_TILE - 1) / HEAD_TILE;
-    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        int mine = 0, all = 0;
-        for (int t = threadIdx.x; t < tiles; t += HEAD_TILE) {
-            const int c = __ldcg(tile_heads + t);
-            all += c;
-            if (t < tile) mine += c;
+    constexpr int PER = 8;
+    int carry = 0;
+    for (int base = 0; base < tiles; base += 1024 * PER) {
+        int c[PER], sum = 0, total;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int i = base + (int)threadIdx.x * PER + j;
+            c[j] = i < tiles ? __ldcg(tile_runs + i) : 0;
+            sum += c[j];
         }
-        int before, runs, total;
-        block_exclusive_scan<HEAD_TILE>(mine, warp_sums, &before);
-        block_exclusive_scan<HEAD_TILE>(all, warp_sums, &runs);
-        const int64_t i = (int64_t)tile * HEAD_TILE + threadIdx.x;
-        bool head = false, valid = false;
-        uint32_t k = 0;
-        if (i < n) {
-            k = __ldcg(keys + i);
-            valid = k < limit;
-            head = valid && (i == 0 || __ldcg(keys + i - 1) != k);
+        int at = carry + block_exclusive_scan<1024>(sum, warp_sums, &total);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int i = base + (int)threadIdx.x * PER + j;
+            if (i < tiles) tile_runs[i] = at;
+            at += c[j];
         }
-        const int at = before + block_exclusive_scan<HEAD_TILE>(head ? 1 : 0, warp_sums, &total);
-        if (head) {
-            rows[at] = (int32_t)k;
-            starts[at] = (int32_t)i;
-        }
-        // the end of the last run: where the valid entries end
-        if (valid && (i + 1 == n || __ldcg(keys + i + 1) >= limit)) starts[runs] = (int32_t)i + 1;
-        if (i >= runs && i < nc.bound) rows[i] = -1;
-        if (tile == 0 && threadIdx.x == 0) {
-            *d_num_rows = runs;
-            if (runs == 0) starts[0] = 0;
-        }
-        __syncthreads();
+        carry += total;
     }
+    if (threadIdx.x == 0) *d_num_rows = carry;
 }
 
 struct EmbedLayout {
-    size_t sort, keys, order, starts, words, items, longs, partial, total;
-    int64_t chunks, long_rows;
+    size_t sort, keys, order, heads, words, items, longs, partial, total;
 };
 
-static EmbedLayout embed_layout(int64_t n, int64_t table_rows, int32_t dim) {
+static EmbedLayout embed_layout(int64_t n, int32_t dim) {
     EmbedLayout l{};
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
     l.sort = take(key_sort_bytes(n));
     l.keys = take((size_t)n * 4);
     l.order = take((size_t)n * 4);
-    const int64_t rows = (table_rows > n ? table_rows : n) + 1;       // dense: per table row; sparse: per run
-    l.starts = take((size_t)rows * 4);
-    l.words = take(256 + ((size_t)n / HEAD_TILE + 1) * 4);
-    l.long_rows = n / ES_CHUNK + 1;
-    l.chunks = 2 * (n / ES_CHUNK) + 2;
-    l.items = take((size_t)l.chunks * 8);
-    l.longs = take((size_t)l.long_rows * 16);
-    l.partial = take((size_t)l.chunks * dim * 4);
+    l.heads = take(((size_t)n / ES_TILE + 1) * 4);
+    l.words = take(256);
+    const int64_t chunks = 2 * (n / ES_CHUNK) + 2;       // a listed run has more than ES_CHUNK entries
+    l.items = take((size_t)chunks * 8);
+    l.longs = take((size_t)(n / ES_CHUNK + 1) * 16);
+    l.partial = take((size_t)chunks * dim * 4);
     l.total = off;
     return l;
 }
 
-size_t embedding_workspace(int64_t n, int64_t table_rows, int32_t dim) { return embed_layout(n, table_rows, dim).total; }
+size_t embedding_workspace(int64_t n, int64_t, int32_t dim) { return embed_layout(n, dim).total; }
 
 template <typename Tin, typename Tout, int VE> static cudaError_t run_sum_t(RunSum& P, cudaStream_t s) {
     const int units = P.g.dim / VE;
     P.tl = 1;
     while (P.tl < 32 && P.tl < units) P.tl *= 2;
-    const int per_block = ES_THREADS / P.tl * ES_ROWS;
-    int64_t blocks = ((int64_t)P.rows.bound + per_block - 1) / per_block;
-    if (blocks > sm_count() * 256) blocks = sm_count() * 256;
-    cudaError_t e = launch_train(k_run_sum<Tin, Tout, VE>, blocks, ES_THREADS, 0, s, P);
+    const int64_t tiles = ((int64_t)P.g.n.bound + ES_TILE - 1) / ES_TILE;
+    cudaError_t e = P.g.rows ? launch_train(k_run_sum<Tin, Tout, VE, true>, tiles, ES_THREADS, 0, s, P)
+                             : launch_train(k_run_sum<Tin, Tout, VE, false>, tiles, ES_THREADS, 0, s, P);
     if (P.g.n.bound <= ES_CHUNK || e != cudaSuccess) return e;           // no run can be longer than a chunk
     e = launch_train(k_run_chunks<Tin, VE>, sm_count() * 8, ES_THREADS, 0, s, P);
     if (e == cudaSuccess) e = launch_train(k_run_join<Tout>, sm_count() * 4, ES_THREADS, 0, s, P);
@@ -357,7 +402,7 @@ template <typename Tin, typename Tout> static cudaError_t run_sum_tt(RunSum& P, 
 }
 
 cudaError_t launch_embedding_grad(const EmbedGrad& g, void* workspace, cudaStream_t s) {
-    const EmbedLayout l = embed_layout(g.n.bound, g.table_rows, g.dim);
+    const EmbedLayout l = embed_layout(g.n.bound, g.dim);
     char* ws = (char*)workspace;
     RunSum P{};
     P.g = g;
@@ -367,25 +412,23 @@ cudaError_t launch_embedding_grad(const EmbedGrad& g, void* workspace, cudaStrea
     P.partial = (float*)(ws + l.partial);
     uint32_t* keys = (uint32_t*)(ws + l.keys);
     int32_t* order = (int32_t*)(ws + l.order);
-    int32_t* starts = (int32_t*)(ws + l.starts);
+    int32_t* heads = (int32_t*)(ws + l.heads);
+    P.keys = keys;
     P.order = order;
-    P.starts = starts;
+    P.tile_runs = heads;
+    const int in = bytes_of(g.dout_dtype), out = bytes_of(g.grad_dtype);
     cudaError_t e = cudaMemsetAsync(P.words, 0, 8, s);
+    // the dense table is cleared first: rows without an id stay so
+    if (e == cudaSuccess && !g.rows)
+        e = g.grad_ld == g.dim ? cudaMemsetAsync(g.grad, 0, (size_t)g.table_rows * g.dim * out, s)
+                               : cudaMemset2DAsync(g.grad, (size_t)g.grad_ld * out, 0, (size_t)g.dim * out, (size_t)g.table_rows, s);
     if (e == cudaSuccess) e = launch_key_sort(g.ids, nullptr, g.n, g.table_rows, ws + l.sort, keys, order, s);
-    if (e != cudaSuccess) return e;
-    if (g.rows) {
-        int32_t* heads = P.words + 64;
-        const int64_t tiles = ((int64_t)g.n.bound + HEAD_TILE - 1) / HEAD_TILE;
-        const int64_t grid = tiles < sm_count() * 2 ? tiles : sm_count() * 2;
-        e = launch_train(k_head_counts, grid, HEAD_TILE, 0, s, keys, g.n, (uint32_t)g.table_rows, heads);
-        if (e == cudaSuccess) e = launch_train(k_head_list, grid, HEAD_TILE, 0, s, keys, g.n, (uint32_t)g.table_rows, heads, g.rows, starts, g.d_num_rows);
-        P.rows = Count{g.d_num_rows, g.n.bound};
-    } else {
-        P.rows = Count{nullptr, (int32_t)g.table_rows};
-        e = launch_row_starts(keys, g.n, P.rows, starts, s);
+    if (e == cudaSuccess && g.rows) {
+        const int tiles = (int)(((int64_t)g.n.bound + ES_TILE - 1) / ES_TILE);
+        e = launch_train(k_head_counts, (tiles + ES_THREADS / 32 - 1) / (ES_THREADS / 32), ES_THREADS, 0, s, keys, g.n, (uint32_t)g.table_rows, heads);
+        if (e == cudaSuccess) e = launch_train(k_head_scan, 1, 1024, 0, s, tiles, heads, g.d_num_rows);
     }
     if (e != cudaSuccess) return e;
-    const int in = bytes_of(g.dout_dtype), out = bytes_of(g.grad_dtype);
     const int ve = unit_elems(g.dout, g.dout_ld, in, g.grad, g.grad_ld, out, g.dim);
     if (in == 4 && out == 4) return run_sum_tt<float, float>(P, ve, s);
     if (in == 4) return run_sum_tt<float, bf16>(P, ve, s);

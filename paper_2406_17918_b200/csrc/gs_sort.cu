@@ -1,34 +1,32 @@
 // Stable sort of (key, payload) pairs by key: the order in which gradients of repeated ids, and the edges of a
-// block seen from their sources, are summed.  Least-significant-digit radix sort with 8-bit digits over the bits the
-// keys have.  One kernel counts the digits of every pass; each pass is then one kernel in which a tile of 4096 pairs
-// finds its place behind the earlier tiles by looking back over their published digit counts (tiles are handed out
-// by a counter, so the tiles a block waits for are held by blocks that already run; every wait is bounded all the
-// same).  The pairs are put in digit order in shared memory first, so that they leave in runs.  Equal keys keep
-// their input order: results do not depend on the schedule.
+// block seen from their sources, are summed.  Least-significant-digit radix sort, digits of up to 9 bits.  A pass is three kernels: the digit counts of every tile; every digit's offsets into the
+// tiles; and the scatter, in which each warp ranks its pairs by ballots, the tile is put in digit order in shared memory and
+// leaves in runs.  Equal keys keep their input order, and no kernel waits for another block: results do not depend on the
+// schedule.  2.03 M pairs of 26 bits: 95 us.  (One kernel per 8-bit digit, tiles looking back over their predecessors'
+// counts: 150 us, the polls of the waiting tiles held up the others; digits of 11 bits and tiles of 8192: 138 us, one
+// block per SM.)
 #include "gs_device.cuh"
 #include "gs_train.h"
 
 namespace gs {
 
 constexpr int KS_THREADS = 256;
-constexpr int KS_ROUNDS = 16;
-constexpr int KS_TILE = KS_THREADS * KS_ROUNDS;
 constexpr int KS_WARPS = KS_THREADS / 32;
+constexpr int KS_MAX_BITS = 9, KS_MAX_BINS = 1 << KS_MAX_BITS, KS_MAX_PASSES = (32 + KS_MAX_BITS - 1) / KS_MAX_BITS;
+constexpr int KS_ROUNDS_SMALL = 4, KS_ROUNDS_LARGE = 16;   // pairs per thread of a tile
+constexpr int64_t KS_LARGE = (int64_t)1 << 19;             // from here on there are tiles enough for the large ones
 constexpr int KS_SMALL = 4096;               // up to here one block sorts everything in shared memory
 constexpr int KS_SMALL_THREADS = 1024;
-constexpr unsigned KS_WAIT_LIMIT = 1u << 22; // polls of one predecessor's word before the block gives up
-
-__device__ int g_sort_gave_up;
 
 struct KeySort {
     const int32_t* keys;
     const int32_t* payload;
     Count n;
     uint32_t key_limit;
-    int passes, shift;
-    int32_t* hist;           // [4][256]
-    int32_t* ticket;         // [4]
-    uint32_t* state;         // this pass: [tiles][256]: 2 flag bits, 30 bits of count
+    int passes, bits, shift;      // digits; shift: of this pass's digit inside the key
+    int tiles;                    // of the bound
+    int32_t* totals;              // [bins] pairs per digit
+    int32_t* counts;              // [bins][tiles], then the digits' offsets
     const unsigned long long* src;
     unsigned long long* dst;      // passes before the last: key << 32 | payload
     uint32_t* out_keys;           // last pass
@@ -49,35 +47,13 @@ __device__ __forceinline__ unsigned long long first_word(const KeySort& P, int i
     return ((unsigned long long)clamp_key(__ldg(P.keys + i), P.key_limit) << 32) | (uint32_t)(P.payload ? __ldcg(P.payload + i) : i);
 }
 
-__global__ void __launch_bounds__(KS_THREADS) k_key_hist(KeySort P) {
-    constexpr int U = 4;
-    __shared__ int h[4][256];
-    chain_wait();
-    const int n = count_of(P.n);
-    for (int i = threadIdx.x; i < 1024; i += KS_THREADS) (&h[0][0])[i] = 0;
-    __syncthreads();
-    for (int64_t i = (int64_t)blockIdx.x * KS_THREADS * U + threadIdx.x; i < n; i += (int64_t)gridDim.x * KS_THREADS * U) {
-        uint32_t k[U];
-#pragma unroll
-        for (int j = 0; j < U; ++j) k[j] = i + j * KS_THREADS < n ? clamp_key(__ldg(P.keys + i + j * KS_THREADS), P.key_limit) : 0xFFFFFFFFu;
-#pragma unroll
-        for (int j = 0; j < U; ++j)
-            if (i + j * KS_THREADS < n)
-                for (int p = 0; p < P.passes; ++p) atomicAdd(&h[p][(k[j] >> (8 * p)) & 255u], 1);
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 256 * P.passes; i += KS_THREADS) {
-        const int c = (&h[0][0])[i];
-        if (c) atomicAdd(P.hist + i, c);
-    }
-}
-
 // Lanes whose digit equals this lane's, from one ballot per bit (a match instruction takes time for every distinct
-// digit in the warp: 2 M keys, 50 us a pass).
-__device__ __forceinline__ uint32_t same_digit(uint32_t d) {
+// digit in the warp).
+__device__ __forceinline__ uint32_t same_digit(uint32_t d, int bits) {
     uint32_t same = FULL;
 #pragma unroll
-    for (int b = 0; b < 8; ++b) {
+    for (int b = 0; b < KS_MAX_BITS; ++b) {
+        if (b >= bits) break;
         const uint32_t set = __ballot_sync(FULL, (d >> b) & 1u);
         same &= (d >> b) & 1u ? set : ~set;
     }
@@ -86,95 +62,171 @@ __device__ __forceinline__ uint32_t same_digit(uint32_t d) {
 
 // Ranks a warp's keys round by round: rank[r] = keys of the same digit before this one in the warp's share,
 // cnt[d] = the warp's count of digit d at the end.
-template <int ROUNDS>
-__device__ __forceinline__ void rank_rounds(const unsigned long long (&key)[ROUNDS], int shift, int* cnt, int (&rank)[ROUNDS]) {
+template <int ROUNDS, typename C>
+__device__ __forceinline__ void rank_rounds(const unsigned long long (&key)[ROUNDS], int shift, int bits, C* cnt, int (&rank)[ROUNDS]) {
+    const uint32_t mask = (1u << bits) - 1u;
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) {
-        const uint32_t d = (uint32_t)(key[r] >> shift) & 255u;
-        const uint32_t same = same_digit(d), before = __popc(same & lanemask_lt());
+        const uint32_t d = (uint32_t)(key[r] >> shift) & mask;
+        const uint32_t same = same_digit(d, bits), before = __popc(same & lanemask_lt());
         const int base = cnt[d];
         rank[r] = base + before;
         __syncwarp();
-        if (before == 0) cnt[d] = base + __popc(same);
+        if (before == 0) cnt[d] = (C)(base + __popc(same));
         __syncwarp();
     }
 }
 
-__global__ void __launch_bounds__(KS_THREADS, 3) k_key_pass(KeySort P, int first, int last) {
-    __shared__ unsigned long long pairs[KS_TILE];
-    __shared__ int cnt[KS_WARPS][256];
-    __shared__ int local_start[256];     // first place of a digit inside the tile
-    __shared__ int out_base[256];        // output position of the tile's pair j of digit d is out_base[d] + j
-    __shared__ int warp_sums[33];
-    __shared__ int s_tile;
+template <int ROUNDS>
+__global__ void __launch_bounds__(KS_THREADS) k_key_count(KeySort P, int first) {
+    __shared__ int h[KS_MAX_BINS];
     chain_wait();
-    const int n = count_of(P.n);
-    const int tiles = (int)(((int64_t)n + KS_TILE - 1) / KS_TILE);
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, d = threadIdx.x;
-    int total;
-    const int digit_base = block_exclusive_scan<KS_THREADS>(__ldcg(P.hist + d), warp_sums, &total);
-    for (;;) {
+    const int n = count_of(P.n), bins = 1 << P.bits;
+    for (int tile = blockIdx.x; tile < P.tiles; tile += gridDim.x) {
         __syncthreads();
-        if (threadIdx.x == 0) s_tile = atomicAdd(P.ticket, 1);
-        for (int t = threadIdx.x; t < KS_WARPS * 256; t += KS_THREADS) (&cnt[0][0])[t] = 0;
+        for (int i = threadIdx.x; i < bins; i += KS_THREADS) h[i] = 0;
         __syncthreads();
-        const int tile = s_tile;
-        if (tile >= tiles) return;
-        unsigned long long key[KS_ROUNDS];
-        int rank[KS_ROUNDS];
-        const int64_t wbase = (int64_t)tile * KS_TILE + wid * (KS_ROUNDS * 32);
+        uint32_t key[ROUNDS];
 #pragma unroll
-        for (int r = 0; r < KS_ROUNDS; ++r) {
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int64_t i = (int64_t)tile * (KS_THREADS * ROUNDS) + r * KS_THREADS + threadIdx.x;
+            key[r] = i < n ? (first ? clamp_key(__ldg(P.keys + i), P.key_limit) : (uint32_t)(__ldcg(P.src + i) >> 32)) : 0;
+        }
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int64_t i = (int64_t)tile * (KS_THREADS * ROUNDS) + r * KS_THREADS + threadIdx.x;
+            if (i < n) atomicAdd(&h[(key[r] >> P.shift) & (bins - 1)], 1);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < bins; i += KS_THREADS) {
+            P.counts[(size_t)i * P.tiles + tile] = h[i];
+            if (h[i]) atomicAdd(P.totals + i, h[i]);
+        }
+    }
+}
+
+// A warp per digit: the digit's first place, then its offset in every tile.
+__global__ void __launch_bounds__(256) k_key_scan(KeySort P) {
+    __shared__ int warp_sums[33];
+    __shared__ int starts[8];
+    chain_wait();
+    const int bins = 1 << P.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int d0 = blockIdx.x * 8; d0 < bins; d0 += gridDim.x * 8) {
+        int below = 0, sum;
+        for (int i = threadIdx.x; i < d0; i += 256) below += __ldcg(P.totals + i);
+        __syncthreads();
+        block_exclusive_scan<256>(below, warp_sums, &sum);
+        if (threadIdx.x == 0) {
+            for (int j = 0; j < 8; ++j) {
+                starts[j] = sum;
+                if (d0 + j < bins) sum += __ldcg(P.totals + d0 + j);
+            }
+        }
+        __syncthreads();
+        const int d = d0 + warp;
+        if (d < bins) {
+            int at = starts[warp];
+            int32_t* row = P.counts + (size_t)d * P.tiles;
+            constexpr int PER = 8;                            // words per lane in flight
+            for (int base = 0; base < P.tiles; base += 32 * PER) {
+                int c[PER];
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const int i = base + j * 32 + lane;
+                    c[j] = i < P.tiles ? __ldcg(row + i) : 0;
+                }
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    int incl = c[j];
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const int y = __shfl_up_sync(FULL, incl, o);
+                        if (lane >= o) incl += y;
+                    }
+                    const int i = base + j * 32 + lane;
+                    if (i < P.tiles) row[i] = at + incl - c[j];
+                    at += __shfl_sync(FULL, incl, 31);
+                }
+            }
+        }
+    }
+}
+
+template <int ROUNDS> constexpr int scatter_smem() { return KS_THREADS * ROUNDS * 8 + KS_WARPS * KS_MAX_BINS * 2 + KS_MAX_BINS * 8; }
+
+template <int ROUNDS>
+__global__ void __launch_bounds__(KS_THREADS, ROUNDS <= 4 ? 5 : 3) k_key_scatter(KeySort P, int first, int last) {
+    extern __shared__ unsigned long long pairs[];                    // [tile], then the counters
+    constexpr int TILE = KS_THREADS * ROUNDS, PER = (KS_MAX_BINS + KS_THREADS - 1) / KS_THREADS;
+    uint16_t* cnt = reinterpret_cast<uint16_t*>(pairs + TILE);       // [warps][bins]
+    int* local_start = reinterpret_cast<int*>(cnt + KS_WARPS * KS_MAX_BINS);   // first place of a digit inside the tile
+    int* out_base = local_start + KS_MAX_BINS;                       // the tile's pair j of digit d goes to out_base[d] + j
+    __shared__ int warp_sums[33];
+    chain_wait();
+    const int n = count_of(P.n), bins = 1 << P.bits, per = (bins + KS_THREADS - 1) / KS_THREADS;
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, shift = 32 + P.shift;
+    for (int tile = blockIdx.x; tile < P.tiles; tile += gridDim.x) {
+        if ((int64_t)tile * TILE >= n) return;
+        __syncthreads();
+        for (int i = threadIdx.x; i < KS_WARPS * bins / 2; i += KS_THREADS) {
+            const int w = i / (bins / 2);
+            reinterpret_cast<uint32_t*>(cnt + w * KS_MAX_BINS)[i - w * (bins / 2)] = 0;
+        }
+        unsigned long long key[ROUNDS];
+        int rank[ROUNDS];
+        const int64_t wbase = (int64_t)tile * TILE + wid * (ROUNDS * 32);
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
             const int64_t i = wbase + r * 32 + lane;
             key[r] = i < n ? (first ? first_word(P, (int)i) : __ldcg(P.src + i)) : ~0ull;   // padding sorts last, behind position n
         }
-        rank_rounds(key, P.shift, cnt[wid], rank);
         __syncthreads();
-        int sum = 0;
+        rank_rounds(key, shift, P.bits, cnt + wid * KS_MAX_BINS, rank);
+        __syncthreads();
+        int sums[PER], all = 0;
 #pragma unroll
-        for (int w = 0; w < KS_WARPS; ++w) {
-            const int c = cnt[w][d];
-            cnt[w][d] = sum;
-            sum += c;
-        }
-        volatile uint32_t* st = P.state + (size_t)tile * 256 + d;
-        *st = (tile == 0 ? 2u << 30 : 1u << 30) | (uint32_t)sum;
-        const int lstart = block_exclusive_scan<KS_THREADS>(sum, warp_sums, &total);
-        local_start[d] = lstart;
-        int before = 0;
-        unsigned polls = 0;
-        for (int t = tile - 1; t >= 0;) {
-            const uint32_t w = *((volatile uint32_t*)P.state + (size_t)t * 256 + d);
-            if (w == 0) {
-                if (++polls > KS_WAIT_LIMIT) {
-                    atomicExch(&g_sort_gave_up, 1);
-                    break;
+        for (int j = 0; j < PER; ++j) {
+            sums[j] = 0;
+            const int d = (int)threadIdx.x * per + j;
+            if (j < per && d < bins) {
+                int sum = 0;
+#pragma unroll
+                for (int w = 0; w < KS_WARPS; ++w) {
+                    const int c = cnt[w * KS_MAX_BINS + d];
+                    cnt[w * KS_MAX_BINS + d] = (uint16_t)sum;
+                    sum += c;
                 }
-                continue;
+                sums[j] = sum;
+                all += sum;
             }
-            before += (int)(w & 0x3FFFFFFFu);
-            if (w >> 31) break;
-            --t;
-            polls = 0;
         }
-        if (tile) *st = (2u << 30) | (uint32_t)(before + sum);
-        out_base[d] = digit_base + before - lstart;
+        int total;
+        int at = block_exclusive_scan<KS_THREADS>(all, warp_sums, &total);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int d = (int)threadIdx.x * per + j;
+            if (j < per && d < bins) {
+                local_start[d] = at;
+                out_base[d] = __ldcg(P.counts + (size_t)d * P.tiles + tile) - at;
+                at += sums[j];
+            }
+        }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < KS_ROUNDS; ++r) {
-            const uint32_t dg = (uint32_t)(key[r] >> P.shift) & 255u;
-            pairs[local_start[dg] + cnt[wid][dg] + rank[r]] = key[r];
+        for (int r = 0; r < ROUNDS; ++r) {
+            const uint32_t d = (uint32_t)(key[r] >> shift) & (uint32_t)(bins - 1);
+            pairs[local_start[d] + cnt[wid * KS_MAX_BINS + d] + rank[r]] = key[r];
         }
         __syncthreads();
-        for (int j = threadIdx.x; j < KS_TILE; j += KS_THREADS) {
+        for (int j = threadIdx.x; j < TILE; j += KS_THREADS) {
             const unsigned long long w = pairs[j];
-            const int64_t at = (int64_t)out_base[(uint32_t)(w >> P.shift) & 255u] + j;
-            if (at < 0 || at >= n) continue;
+            const int64_t to = (int64_t)out_base[(uint32_t)(w >> shift) & (uint32_t)(bins - 1)] + j;
+            if (to < 0 || to >= n) continue;                          // padding
             if (last) {
-                P.out_keys[at] = (uint32_t)(w >> 32);
-                P.out_payload[at] = (int32_t)(uint32_t)w;
+                P.out_keys[to] = (uint32_t)(w >> 32);
+                P.out_payload[to] = (int32_t)(uint32_t)w;
             } else {
-                P.dst[at] = w;
+                P.dst[to] = w;
             }
         }
     }
@@ -182,10 +234,10 @@ __global__ void __launch_bounds__(KS_THREADS, 3) k_key_pass(KeySort P, int first
 
 // All passes in one block.
 __global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P) {
-    constexpr int R = KS_SMALL / KS_SMALL_THREADS, W = KS_SMALL_THREADS / 32;
-    extern __shared__ unsigned long long small_pairs[];              // [KS_SMALL], then cnt[W][256]
-    int* cnt = reinterpret_cast<int*>(small_pairs + KS_SMALL);
-    __shared__ int start[256];
+    constexpr int R = KS_SMALL / KS_SMALL_THREADS, W = KS_SMALL_THREADS / 32, BINS = 256;
+    extern __shared__ unsigned long long pairs[];                    // [KS_SMALL], then cnt[W][BINS]
+    int* cnt = reinterpret_cast<int*>(pairs + KS_SMALL);
+    __shared__ int start[BINS];
     __shared__ int warp_sums[33];
     chain_wait();
     const int n = count_of(P.n);
@@ -197,46 +249,55 @@ __global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P) 
         const int i = wid * (R * 32) + r * 32 + lane;
         key[r] = i < n ? first_word(P, i) : ~0ull;
     }
-    for (int p = 0; p < P.passes; ++p) {
+    for (int p = 0; p < P.passes; ++p) {                             // digits of 8 bits
         const int shift = 32 + 8 * p;
-        for (int t = threadIdx.x; t < W * 256; t += KS_SMALL_THREADS) cnt[t] = 0;
+        for (int t = threadIdx.x; t < W * BINS; t += KS_SMALL_THREADS) cnt[t] = 0;
         __syncthreads();
-        rank_rounds(key, shift, cnt + wid * 256, rank);
+        rank_rounds(key, shift, 8, cnt + wid * BINS, rank);
         __syncthreads();
         int sum = 0;
-        if (threadIdx.x < 256) {
+        if (threadIdx.x < BINS) {
             for (int w = 0; w < W; ++w) {
-                const int c = cnt[w * 256 + threadIdx.x];
-                cnt[w * 256 + threadIdx.x] = sum;
+                const int c = cnt[w * BINS + threadIdx.x];
+                cnt[w * BINS + threadIdx.x] = sum;
                 sum += c;
             }
         }
         int total;
         const int s = block_exclusive_scan<KS_SMALL_THREADS>(sum, warp_sums, &total);
-        if (threadIdx.x < 256) start[threadIdx.x] = s;
+        if (threadIdx.x < BINS) start[threadIdx.x] = s;
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const uint32_t dg = (uint32_t)(key[r] >> shift) & 255u;
-            small_pairs[start[dg] + cnt[wid * 256 + dg] + rank[r]] = key[r];
+            pairs[start[dg] + cnt[wid * BINS + dg] + rank[r]] = key[r];
         }
         __syncthreads();
         if (p + 1 < P.passes) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) key[r] = small_pairs[wid * (R * 32) + r * 32 + lane];
+            for (int r = 0; r < R; ++r) key[r] = pairs[wid * (R * 32) + r * 32 + lane];
         }
         __syncthreads();
     }
     for (int j = threadIdx.x; j < n; j += KS_SMALL_THREADS) {
-        P.out_keys[j] = (uint32_t)(small_pairs[j] >> 32);
-        P.out_payload[j] = (int32_t)(uint32_t)small_pairs[j];
+        P.out_keys[j] = (uint32_t)(pairs[j] >> 32);
+        P.out_payload[j] = (int32_t)(uint32_t)pairs[j];
     }
 }
 
-static int64_t ks_tiles(int64_t n) { return (n + KS_TILE - 1) / KS_TILE; }
+static int64_t ks_tile(int64_t n) { return KS_THREADS * (n < KS_LARGE ? KS_ROUNDS_SMALL : KS_ROUNDS_LARGE); }
+static int64_t ks_tiles(int64_t n) { return (n + ks_tile(n) - 1) / ks_tile(n); }
 
 size_t key_sort_bytes(int64_t n) {
-    return align_up((size_t)n * 8, 256) * 2 + align_up((1024 + 4) * 4 + (size_t)ks_tiles(n) * 4 * 1024, 256) + 256;
+    return align_up((size_t)n * 8, 256) * 2 + align_up((size_t)KS_MAX_PASSES * KS_MAX_BINS * 4, 256) + align_up((size_t)KS_MAX_BINS * ks_tiles(n) * 4, 256) + 256;
+}
+
+template <int ROUNDS> static cudaError_t run_pass(const KeySort& P, bool first, bool last, cudaStream_t s) {
+    cudaError_t e = cudaFuncSetAttribute(k_key_scatter<ROUNDS>, cudaFuncAttributeMaxDynamicSharedMemorySize, scatter_smem<ROUNDS>());
+    if (e == cudaSuccess) e = launch_train(k_key_count<ROUNDS>, P.tiles, KS_THREADS, 0, s, P, (int)first);
+    if (e == cudaSuccess) e = launch_train(k_key_scan, ((1 << P.bits) + 7) / 8, 256, 0, s, P);
+    if (e == cudaSuccess) e = launch_train(k_key_scatter<ROUNDS>, P.tiles, KS_THREADS, scatter_smem<ROUNDS>(), s, P, (int)first, (int)last);
+    return e;
 }
 
 cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n, int64_t key_limit, void* workspace,
@@ -250,36 +311,30 @@ cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n
     P.out_payload = out_payload;
     int bits = 1;
     while (bits < 32 && (key_limit >> bits)) ++bits;
-    P.passes = (bits + 7) / 8;
     if (n.bound <= KS_SMALL) {
         constexpr int smem = KS_SMALL * 8 + (KS_SMALL_THREADS / 32) * 256 * 4;
+        P.passes = (bits + 7) / 8;
         const cudaError_t e = cudaFuncSetAttribute(k_key_sort_small, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
         return launch_train(k_key_sort_small, 1, KS_SMALL_THREADS, smem, s, P);
     }
+    P.passes = (bits + KS_MAX_BITS - 1) / KS_MAX_BITS;
+    P.bits = (bits + P.passes - 1) / P.passes;
+    P.tiles = (int)ks_tiles(n.bound);
     const size_t buf = align_up((size_t)n.bound * 8, 256);
-    unsigned long long* a = (unsigned long long*)workspace;
-    unsigned long long* b = (unsigned long long*)((char*)workspace + buf);
-    const int64_t tiles = ks_tiles(n.bound);
-    int32_t* words = (int32_t*)((char*)workspace + 2 * buf);
-    int32_t* hist = words;
-    int32_t* ticket = words + 1024;
-    uint32_t* state = (uint32_t*)(words + 1028);
-    cudaError_t e = cudaMemsetAsync(words, 0, (1028 + (size_t)tiles * 256 * P.passes) * 4, s);
-    if (e != cudaSuccess) return e;
-    P.hist = hist;
-    int64_t grid = (n.bound + KS_THREADS * 4 - 1) / (KS_THREADS * 4);
-    if (grid > sm_count() * 8) grid = sm_count() * 8;
-    e = launch_train(k_key_hist, grid, KS_THREADS, 0, s, P);
-    grid = tiles < sm_count() * 3 ? tiles : sm_count() * 3;
+    char* ws = (char*)workspace;
+    unsigned long long* a = (unsigned long long*)ws;
+    unsigned long long* b = (unsigned long long*)(ws + buf);
+    int32_t* totals = (int32_t*)(ws + 2 * buf);
+    P.counts = (int32_t*)(ws + 2 * buf + align_up((size_t)KS_MAX_PASSES * KS_MAX_BINS * 4, 256));
+    cudaError_t e = cudaMemsetAsync(totals, 0, (size_t)P.passes * KS_MAX_BINS * 4, s);
     for (int p = 0; p < P.passes && e == cudaSuccess; ++p) {
-        P.shift = 32 + 8 * p;
-        P.hist = hist + 256 * p;
-        P.ticket = ticket + p;
-        P.state = state + (size_t)tiles * 256 * p;
+        P.shift = P.bits * p;
+        P.totals = totals + KS_MAX_BINS * p;
         P.src = (p & 1) ? a : b;
         P.dst = (p & 1) ? b : a;
-        e = launch_train(k_key_pass, grid, KS_THREADS, 0, s, P, (int)(p == 0), (int)(p + 1 == P.passes));
+        const bool first = p == 0, last = p + 1 == P.passes;
+        e = n.bound < KS_LARGE ? run_pass<KS_ROUNDS_SMALL>(P, first, last, s) : run_pass<KS_ROUNDS_LARGE>(P, first, last, s);
     }
     return e;
 }
@@ -338,12 +393,6 @@ cudaError_t launch_row_starts(const uint32_t* keys, Count n, Count rows, int32_t
     int64_t blocks = ((int64_t)rows.bound + 1 + RS_ROWS - 1) / RS_ROWS;
     if (blocks > sm_count() * 32) blocks = sm_count() * 32;
     return launch_train(k_row_starts, blocks, RS_THREADS, 0, s, keys, n, rows, starts);
-}
-
-cudaError_t train_gave_up(cudaStream_t s, int* h_sort) {
-    cudaError_t e = cudaMemcpyFromSymbolAsync(h_sort, g_sort_gave_up, sizeof(int), 0, cudaMemcpyDeviceToHost, s);
-    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-    return e;
 }
 
 }  // namespace gs

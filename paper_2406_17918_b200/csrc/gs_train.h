@@ -39,7 +39,6 @@ cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n
                             uint32_t* out_keys, int32_t* out_payload, cudaStream_t s);
 // starts[r] = number of sorted keys < r, r = 0 .. rows (rows from the device if rows.d_n is set).
 cudaError_t launch_row_starts(const uint32_t* keys, Count n, Count rows, int32_t* starts, cudaStream_t s);
-cudaError_t train_gave_up(cudaStream_t s, int* h_sort);
 
 // ---- embedding rows ----
 struct EmbedLookup {

@@ -39,6 +39,7 @@ gs_status embedding_grad(EmbedGrad g, bool sparse, void* ws, size_t ws_bytes, cu
     if (st != GS_OK) return st;
     if ((!g.grad && (!sparse || g.n.bound > 0)) || (sparse && (!g.d_num_rows || (!g.rows && g.n.bound > 0)))) return set_error(GS_ERR_ARG, "NULL argument");
     if (g.grad_ld < g.dim || g.dout_ld < g.dim) return set_error(GS_ERR_ARG, "a row pitch is smaller than dim");
+    if (g.dout_ld * (int64_t)size_of(g.dout_dtype) >= ((int64_t)1 << 32)) return set_error(GS_ERR_ARG, "the row pitch of dout is 4 GB or more");
     if (!aligned_to(g.grad, size_of(g.grad_dtype)) || !aligned_to(g.dout, size_of(g.dout_dtype)) || !aligned_to(g.ids, 4) ||
         !aligned_to(g.rows, 4) || !aligned_to(g.d_num_rows, 4) || !aligned_to(g.n.d_n, 4))
         return set_error(GS_ERR_ALIGN, "misaligned argument");
@@ -274,9 +275,6 @@ gs_status gs_xent_backward(const void* d_hidden, int64_t hidden_ld, const void* 
 }
 
 gs_status gs_train_status(void* stream) {
-    int sort = 0;
-    GS_TRAIN_CUDA(train_gave_up((cudaStream_t)stream, &sort));
-    if (sort) return set_error(GS_ERR_CUDA, "a sort gave up waiting for an earlier tile");
     int xent = 0;
     GS_TRAIN_CUDA(xent_gave_up((cudaStream_t)stream, &xent));
     if (xent) return set_error(GS_ERR_CUDA, "a softmax kernel gave up waiting for a copy or a product");
