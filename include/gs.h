@@ -500,7 +500,7 @@ gs_status gs_embedding_backward_sparse(const void* d_dout, gs_dtype dout_dtype, 
  *   block      a block of gs_sample_batch, or one the caller fills: max_* are the sizes, d_num_* device scalars with
  *              the actual ones, or NULL (the sizes are exact; all three together)
  *   max_row    an upper bound on the edges of one destination (the fan-out, for a sampled block), or 0 if it is not
- *              known: rows above 128 edges are then split over the device.  A longer row than promised is slower,
+ *              known: rows above 64 edges are then split over the device.  A longer row than promised is slower,
  *              not wrong.
  *   gs_heads   [rows][heads][head_dim] of `dtype`, head_dim contiguous, strides in elements (a slice of a fused
  *              projection is fine); q, out, dout, dq have the destinations' rows and q_heads, k, v, dk, dv the

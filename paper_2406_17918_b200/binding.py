@@ -43,10 +43,6 @@ class _CBlockBuffers(ctypes.Structure):
                 ("d_indices", ctypes.c_void_p), ("indices_capacity", ctypes.c_int64)]
 
 
-class _CHeads(ctypes.Structure):
-    _fields_ = [("d_data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
-
-
 NOALLOC_SCRATCH_BYTES = 64 << 20
 
 
@@ -639,7 +635,21 @@ def gs_cache_set_dedup(cache: Cache, method: int):
 
 
 # ---------------------------------------------------------------- training operators
+# Small calls are bound by this file: addresses and streams go to the library as plain integers, and the strided
+# operands of a call as one array.
 _DTYPE = {torch.float32: GS_F32, torch.bfloat16: GS_BF16}
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _on(stream, t: torch.Tensor):
+    """The stream's handle; by default the current one of the tensor's device."""
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(t.get_device()) if _raw_stream is not None else torch.cuda.current_stream(t.device).cuda_stream
 
 
 def _dtype(t: torch.dtype) -> int:
@@ -650,13 +660,14 @@ def _dtype(t: torch.dtype) -> int:
 
 
 def _rows_2d(t: torch.Tensor, what: str) -> torch.Tensor:
-    if not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    stride = t.stride()
+    if len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1) or not t.is_cuda:
         raise TypeError("%s must be a row-major 2-D CUDA tensor" % what)
     return t
 
 
 def _ids_1d(t: torch.Tensor, what: str) -> torch.Tensor:
-    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous():
+    if t.dtype is not torch.int32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous():
         raise TypeError("%s must be a contiguous 1-D int32 CUDA tensor" % what)
     return t
 
@@ -678,9 +689,9 @@ def gs_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1
         _rows_2d(out, "out")
         if out.shape[0] < ids.numel() or out.shape[1] != table.shape[1]:
             raise ValueError("out must be [len(ids), dim]")
-    _check(_L.gs_embedding_lookup(_ptr(table), _dtype(table.dtype), table.shape[0], table.shape[1], _ld(table), _ptr(ids),
-                                  _ptr(count), ids.numel(), float(scale), _ptr(out), _dtype(out.dtype), _ld(out),
-                                  _stream(stream)))
+    _check(_L.gs_embedding_lookup(_addr(table), _dtype(table.dtype), table.shape[0], table.shape[1], _ld(table), _addr(ids),
+                                  _addr(count), ids.numel(), float(scale), _addr(out), _dtype(out.dtype), _ld(out),
+                                  _on(stream, out)))
     return out
 
 
@@ -708,9 +719,9 @@ def gs_embedding_backward(dout: torch.Tensor, ids: torch.Tensor, table_rows: int
         _rows_2d(out, "out")
         if tuple(out.shape) != (int(table_rows), dout.shape[1]):
             raise ValueError("out must be [table_rows, dim]")
-    _check(_L.gs_embedding_backward(_ptr(dout), _dtype(dout.dtype), _ld(dout), _ptr(ids), _ptr(count), ids.numel(),
-                                    int(table_rows), dout.shape[1], float(scale), _ptr(out), _dtype(out.dtype), _ld(out),
-                                    _ptr(workspace), workspace.numel(), _stream(stream)))
+    _check(_L.gs_embedding_backward(_addr(dout), _dtype(dout.dtype), _ld(dout), _addr(ids), _addr(count), ids.numel(),
+                                    int(table_rows), dout.shape[1], float(scale), _addr(out), _dtype(out.dtype), _ld(out),
+                                    _addr(workspace), workspace.numel(), _on(stream, workspace)))
     return out
 
 
@@ -731,29 +742,31 @@ def gs_embedding_backward_sparse(dout: torch.Tensor, ids: torch.Tensor, table_ro
     _rows_2d(grad, "grad")
     if rows.numel() < n or grad.shape[0] < n or grad.shape[1] != d:
         raise ValueError("rows / grad must hold one entry per id")
-    _check(_L.gs_embedding_backward_sparse(_ptr(dout), _dtype(dout.dtype), _ld(dout), _ptr(ids), _ptr(count), n, int(table_rows), d,
-                                           float(scale), _ptr(rows), _ptr(num_rows), _ptr(grad), _dtype(grad.dtype), _ld(grad),
-                                           _ptr(workspace), workspace.numel(), _stream(stream)))
+    _check(_L.gs_embedding_backward_sparse(_addr(dout), _dtype(dout.dtype), _ld(dout), _addr(ids), _addr(count), n, int(table_rows), d,
+                                           float(scale), _addr(rows), _addr(num_rows), _addr(grad), _dtype(grad.dtype), _ld(grad),
+                                           _addr(workspace), workspace.numel(), _on(stream, workspace)))
     return rows, num_rows, grad
 
 
 def _csr_block(indptr, indices, num_src, counts):
     _ids_1d(indptr, "indptr")
     _ids_1d(indices, "indices")
-    b = _CBlock()
-    b.max_dst, b.max_src, b.max_edges = indptr.numel() - 1, int(num_src), indices.numel()
-    b.d_indptr, b.d_indices = indptr.data_ptr(), indices.data_ptr()
-    if counts is not None:
-        b.d_num_dst, b.d_num_src, b.d_num_edges = (c.data_ptr() for c in counts)
-    return b
+    nd, ns, ne = (None, None, None) if counts is None else (c.data_ptr() for c in counts)
+    return _CBlock(indptr.numel() - 1, int(num_src), indices.numel(), nd, ns, ne, indptr.data_ptr(), indices.data_ptr())
 
 
-def _heads(t, what, rows, heads, dim, dtype):
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != dim or \
-            (t.stride(2) != 1 and dim > 1):
-        raise TypeError("%s must be a CUDA tensor [%d, %d, %d] of %s with a contiguous last dimension" % (what, rows, heads, dim, dtype))
-    return ctypes.byref(_CHeads(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), dim),
-                                t.stride(1) if heads > 1 else dim))
+def _heads(dtype, *operands):
+    """gs_heads of (tensor, name, rows, heads, head_dim), one behind the other; returns (array, addresses)."""
+    words = []
+    for t, what, rows, heads, dim in operands:
+        shape, stride = t.shape, t.stride()
+        if t.dtype is not dtype or len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != dim or not t.is_cuda or \
+                (stride[2] != 1 and dim > 1):
+            raise TypeError("%s must be a CUDA tensor [%d, %d, %d] of %s with a contiguous last dimension" % (what, rows, heads, dim, dtype))
+        words += (t.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], dim), stride[1] if heads > 1 else dim)
+    array = (ctypes.c_int64 * len(words))(*words)
+    at = ctypes.addressof(array)
+    return array, [at + 24 * i for i in range(len(operands))]
 
 
 def gs_block_attention_workspace_bytes(num_dst: int, num_src: int, num_edges: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
@@ -781,11 +794,11 @@ def gs_block_attention_forward(indptr: torch.Tensor, indices: torch.Tensor, q: t
         lse = torch.empty((n, hq), dtype=torch.float32, device=q.device)
     elif lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape[0] < b.max_dst or lse.shape[1] != hq:
         raise TypeError("lse must be a contiguous float32 tensor [dst, q_heads]")
+    keep, (pq, pk, pv, po) = _heads(q.dtype, (q, "q", b.max_dst, hq, d), (k, "k", b.max_src, hk, d), (v, "v", b.max_src, hk, d),
+                                    (out, "out", b.max_dst, hq, d))
     _check(_L.gs_block_attention_forward(ctypes.byref(b), int(max_row), _dtype(q.dtype), hq, hk, d,
-                                         d ** -0.5 if scale is None else float(scale), _heads(q, "q", b.max_dst, hq, d, q.dtype),
-                                         _heads(k, "k", b.max_src, hk, d, q.dtype), _heads(v, "v", b.max_src, hk, d, q.dtype),
-                                         _heads(out, "out", b.max_dst, hq, d, q.dtype), _ptr(lse), _ptr(workspace), workspace.numel(),
-                                         _stream(stream)))
+                                         d ** -0.5 if scale is None else float(scale), pq, pk, pv, po, _addr(lse), _addr(workspace),
+                                         workspace.numel(), _on(stream, workspace)))
     return out, lse
 
 
@@ -799,7 +812,7 @@ def gs_block_reverse(indptr: torch.Tensor, indices: torch.Tensor, num_src: int, 
         rev_dst = torch.empty(b.max_edges, dtype=torch.int32, device=indptr.device)
     if _ids_1d(rev_indptr, "rev_indptr").numel() < b.max_src + 1 or _ids_1d(rev_dst, "rev_dst").numel() < b.max_edges:
         raise ValueError("rev_indptr / rev_dst are too small")
-    _check(_L.gs_block_reverse(ctypes.byref(b), _ptr(rev_indptr), _ptr(rev_dst), _ptr(workspace), workspace.numel(), _stream(stream)))
+    _check(_L.gs_block_reverse(ctypes.byref(b), _addr(rev_indptr), _addr(rev_dst), _addr(workspace), workspace.numel(), _on(stream, workspace)))
     return rev_indptr, rev_dst
 
 
@@ -820,12 +833,12 @@ def gs_block_attention_backward(indptr: torch.Tensor, indices: torch.Tensor, rev
     dk = torch.empty((k.shape[0], hk, d), dtype=q.dtype, device=q.device) if dk is None else dk
     dv = torch.empty((v.shape[0], hk, d), dtype=q.dtype, device=q.device) if dv is None else dv
     t = q.dtype
-    _check(_L.gs_block_attention_backward(ctypes.byref(b), int(max_row), _ptr(rev_indptr), _ptr(rev_dst), _dtype(t), hq, hk, d,
-                                          d ** -0.5 if scale is None else float(scale), _heads(q, "q", b.max_dst, hq, d, t),
-                                          _heads(k, "k", b.max_src, hk, d, t), _heads(v, "v", b.max_src, hk, d, t),
-                                          _heads(out, "out", b.max_dst, hq, d, t), _ptr(lse), _heads(dout, "dout", b.max_dst, hq, d, t),
-                                          _heads(dq, "dq", b.max_dst, hq, d, t), _heads(dk, "dk", b.max_src, hk, d, t),
-                                          _heads(dv, "dv", b.max_src, hk, d, t), _ptr(workspace), workspace.numel(), _stream(stream)))
+    keep, (pq, pk, pv, po, pdo, pdq, pdk, pdv) = _heads(
+        t, (q, "q", b.max_dst, hq, d), (k, "k", b.max_src, hk, d), (v, "v", b.max_src, hk, d), (out, "out", b.max_dst, hq, d),
+        (dout, "dout", b.max_dst, hq, d), (dq, "dq", b.max_dst, hq, d), (dk, "dk", b.max_src, hk, d), (dv, "dv", b.max_src, hk, d))
+    _check(_L.gs_block_attention_backward(ctypes.byref(b), int(max_row), _addr(rev_indptr), _addr(rev_dst), _dtype(t), hq, hk, d,
+                                          d ** -0.5 if scale is None else float(scale), pq, pk, pv, po, _addr(lse), pdo, pdq, pdk, pdv,
+                                          _addr(workspace), workspace.numel(), _on(stream, workspace)))
     return dq, dk, dv
 
 
@@ -858,8 +871,8 @@ def gs_xent_forward(hidden: torch.Tensor, table: torch.Tensor, labels: torch.Ten
     n = hidden.shape[0]
     loss = torch.empty(n, dtype=torch.float32, device=hidden.device) if loss is None else _f32_rows(loss, "loss", n)
     lse = torch.empty(n, dtype=torch.float32, device=hidden.device) if lse is None else _f32_rows(lse, "lse", n)
-    _check(_L.gs_xent_forward(_ptr(hidden), _ld(hidden), _ptr(table), _ld(table), _dtype(hidden.dtype), n, table.shape[0], hidden.shape[1],
-                              float(scale), _ptr(labels), _ptr(loss), _ptr(lse), _ptr(workspace), workspace.numel(), _stream(stream)))
+    _check(_L.gs_xent_forward(_addr(hidden), _ld(hidden), _addr(table), _ld(table), _dtype(hidden.dtype), n, table.shape[0], hidden.shape[1],
+                              float(scale), _addr(labels), _addr(loss), _addr(lse), _addr(workspace), workspace.numel(), _on(stream, workspace)))
     return loss, lse
 
 
@@ -876,12 +889,12 @@ def gs_xent_backward(hidden: torch.Tensor, table: torch.Tensor, labels: torch.Te
     dtable = torch.empty(tuple(table.shape), dtype=dhidden.dtype, device=hidden.device) if dtable is None else _rows_2d(dtable, "dtable")
     if tuple(dhidden.shape) != (n, d) or dtable.shape != table.shape or dhidden.dtype != dtable.dtype:
         raise ValueError("dhidden / dtable must have the shapes of hidden / table and one dtype")
-    _check(_L.gs_xent_backward(_ptr(hidden), _ld(hidden), _ptr(table), _ld(table), _dtype(hidden.dtype), n, table.shape[0], d, float(scale),
-                               _ptr(labels), _ptr(lse), _ptr(dloss), _ptr(dhidden), _ld(dhidden), _ptr(dtable), _ld(dtable),
-                               _dtype(dhidden.dtype), _ptr(workspace), workspace.numel(), _stream(stream)))
+    _check(_L.gs_xent_backward(_addr(hidden), _ld(hidden), _addr(table), _ld(table), _dtype(hidden.dtype), n, table.shape[0], d, float(scale),
+                               _addr(labels), _addr(lse), _addr(dloss), _addr(dhidden), _ld(dhidden), _addr(dtable), _ld(dtable),
+                               _dtype(dhidden.dtype), _addr(workspace), workspace.numel(), _on(stream, workspace)))
     return dhidden, dtable
 
 
 def gs_train_status(stream=None):
     """Synchronises; raises if a kernel of the training operators ever gave up waiting."""
-    _check(_L.gs_train_status(_stream(stream)))
+    _check(_L.gs_train_status((torch.cuda.current_stream() if stream is None else stream).cuda_stream))

@@ -20,7 +20,7 @@
 namespace gs {
 
 constexpr int AT_THREADS = 256;
-constexpr int AT_CHUNK = 128;
+constexpr int AT_CHUNK = 64;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float fast_exp2(float x) {
@@ -273,29 +273,46 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_forward(const __grid_cons
     }
 }
 
-// One warp per (long row, query head): the chunks' sums, rescaled to the common maximum, in order.
+// One block per (long row, query head): the chunks' sums rescaled to the common maximum; each warp adds a contiguous share of
+// the chunks, the shares are added in order.
 template <typename T> __global__ void __launch_bounds__(AT_THREADS) k_attend_forward_join(const __grid_constant__ Attend P) {
-    const int lane = threadIdx.x & 31, D = P.a.head_dim;
+    constexpr int W = AT_THREADS / 32;
+    __shared__ float s_m[W], s_l[W], s_acc[W][256];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = P.a.head_dim;
     const int64_t units = (int64_t)__ldcg(P.words + 1) * P.a.q_heads, stride = (int64_t)P.a.q_heads * (D + 2);
-    for (int64_t u = (int64_t)blockIdx.x * (AT_THREADS / 32) + threadIdx.x / 32; u < units; u += (int64_t)gridDim.x * (AT_THREADS / 32)) {
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
         const int4 row = P.longs[u / P.a.q_heads];
         const int h = (int)(u % P.a.q_heads);
         const float* part = P.partial + (int64_t)row.y * stride + (int64_t)h * (D + 2);
+        const int per = (row.z + W - 1) / W, c0 = warp * per, c1 = c0 + per < row.z ? c0 + per : row.z;
         float m = -INFINITY, l = 0.f;
-        for (int c = lane; c < row.z; c += 32) m = fmaxf(m, part[c * stride + D]);
+        for (int c = c0 + lane; c < c1; c += 32) m = fmaxf(m, part[c * stride + D]);
         for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, o));
+        __syncthreads();                                       // the previous unit's sums are read
+        if (lane == 0) s_m[warp] = m;
+        __syncthreads();
+        for (int w = 0; w < W; ++w) m = fmaxf(m, s_m[w]);
         const float ref = m == -INFINITY ? 0.f : m;
-        for (int c = lane; c < row.z; c += 32) l += part[c * stride + D + 1] * fast_exp2(part[c * stride + D] - ref);
+        for (int c = c0 + lane; c < c1; c += 32) l += part[c * stride + D + 1] * fast_exp2(part[c * stride + D] - ref);
         for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(FULL, l, o);
-        const bool none = l == 0.f;
-        T* out = (T*)P.a.out.data + (int64_t)row.x * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride;
+        if (lane == 0) s_l[warp] = l;
         for (int col = lane; col < D; col += 32) {
             float acc = 0.f;
 #pragma unroll 4
-            for (int c = 0; c < row.z; ++c) acc = fmaf(part[c * stride + col], fast_exp2(part[c * stride + D] - ref), acc);
+            for (int c = c0; c < c1; ++c) acc = fmaf(part[c * stride + col], fast_exp2(part[c * stride + D] - ref), acc);
+            s_acc[warp][col] = acc;
+        }
+        __syncthreads();
+        l = 0.f;
+        for (int w = 0; w < W; ++w) l += s_l[w];
+        const bool none = l == 0.f;
+        T* out = (T*)P.a.out.data + (int64_t)row.x * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride;
+        for (int col = threadIdx.x; col < D; col += AT_THREADS) {
+            float acc = 0.f;
+            for (int w = 0; w < W; ++w) acc += s_acc[w][col];
             out[col] = from_f32<T>(none ? 0.f : acc / l);
         }
-        if (lane == 0) P.a.lse[(int64_t)row.x * P.a.q_heads + h] = none ? -INFINITY : m * LN2 + logf(l);
+        if (threadIdx.x == 0) P.a.lse[(int64_t)row.x * P.a.q_heads + h] = none ? -INFINITY : m * LN2 + logf(l);
     }
 }
 
@@ -506,23 +523,34 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_dkv(const __grid_constant
     }
 }
 
-// Chunk sums of long rows added in order: one warp per (row, head, 32 of its `width` values).  dq: one operand of
-// width D; dk and dv: width 2 D, the second half for dv.
+// Chunk sums of long rows added in order: one block per (row, head), its warps over shares of the chunks.  dq: one operand
+// of width D; dk and dv: width 2 D, the second half for dv.
 template <typename T, bool KV> __global__ void __launch_bounds__(AT_THREADS) k_attend_sum_join(const __grid_constant__ Attend P) {
-    const int lane = threadIdx.x & 31, D = P.a.head_dim;
-    const int heads = KV ? P.a.kv_heads : P.a.q_heads, width = KV ? 2 * D : D, tiles = (width + 31) / 32;
-    const int64_t units = (int64_t)__ldcg(P.words + 1) * heads * tiles, stride = (int64_t)heads * width;
-    for (int64_t u = (int64_t)blockIdx.x * (AT_THREADS / 32) + threadIdx.x / 32; u < units; u += (int64_t)gridDim.x * (AT_THREADS / 32)) {
-        const int4 row = P.longs[u / ((int64_t)heads * tiles)];
-        const int h = (int)(u / tiles % heads), col = (int)(u % tiles) * 32 + lane;
-        if (col >= width) continue;
-        const float* part = P.partial + (int64_t)row.y * stride + (int64_t)h * width + col;
-        float acc = 0.f;
-#pragma unroll 8
-        for (int c = 0; c < row.z; ++c) acc += part[c * stride];
-        const HeadView& to = !KV ? P.a.dq : (col < D ? P.a.dk : P.a.dv);
-        if (!KV || col < D) acc *= P.a.scale;
-        ((T*)to.data)[(int64_t)row.x * to.row_stride + (int64_t)h * to.head_stride + (col < D ? col : col - D)] = from_f32<T>(acc);
+    constexpr int W = AT_THREADS / 32;
+    __shared__ float s_acc[W][512];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = P.a.head_dim;
+    const int heads = KV ? P.a.kv_heads : P.a.q_heads, width = KV ? 2 * D : D;
+    const int64_t units = (int64_t)__ldcg(P.words + 1) * heads, stride = (int64_t)heads * width;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int4 row = P.longs[u / heads];
+        const int h = (int)(u % heads);
+        const float* part = P.partial + (int64_t)row.y * stride + (int64_t)h * width;
+        const int per = (row.z + W - 1) / W, c0 = warp * per, c1 = c0 + per < row.z ? c0 + per : row.z;
+        __syncthreads();                                       // the previous unit's sums are read
+        for (int col = lane; col < width; col += 32) {
+            float acc = 0.f;
+#pragma unroll 4
+            for (int c = c0; c < c1; ++c) acc += part[c * stride + col];
+            s_acc[warp][col] = acc;
+        }
+        __syncthreads();
+        for (int col = threadIdx.x; col < width; col += AT_THREADS) {
+            float acc = 0.f;
+            for (int w = 0; w < W; ++w) acc += s_acc[w][col];
+            const HeadView& to = !KV ? P.a.dq : (col < D ? P.a.dk : P.a.dv);
+            if (!KV || col < D) acc *= P.a.scale;
+            ((T*)to.data)[(int64_t)row.x * to.row_stride + (int64_t)h * to.head_stride + (col < D ? col : col - D)] = from_f32<T>(acc);
+        }
     }
 }
 
@@ -575,7 +603,7 @@ static int wide_elems(const BlockAttention& a, std::initializer_list<const HeadV
         bool ok = a.head_dim % ve == 0;
         for (const HeadView* v : views)
             ok = ok && ((uintptr_t)v->data % (ve * size)) == 0 && (v->row_stride * size) % (ve * size) == 0 && (v->head_stride * size) % (ve * size) == 0 &&
-                 v->row_stride * size < ((int64_t)1 << 32) && v->head_stride * size < ((int64_t)1 << 32);
+                 v->row_stride * size < ((int64_t)1 << 32) && v->head_stride * size * a.q_heads < ((int64_t)1 << 31);
         if (ok) return ve;
     }
     return 1;
@@ -609,7 +637,7 @@ template <AttendKind K, typename T, int VE, int NV, int G> static void run_atten
         count_launches(1);
     }
     if (P.split) {
-        const int grid = (int)limit_grid(sm_count() * 2);
+        const int grid = (int)limit_grid(sm_count() * 8);
         if constexpr (K == AT_FORWARD) k_attend_forward_join<T><<<grid, AT_THREADS, 0, s>>>(P);
         else k_attend_sum_join<T, K == AT_DKV><<<grid, AT_THREADS, 0, s>>>(P);
         count_launches(1);
@@ -633,7 +661,7 @@ template <AttendKind K, typename T, int VE, int NV, int G> static cudaError_t ru
         P.chunk_mode = pass;
         const int64_t n = pass ? 2 * ((int64_t)P.edge_bound / AT_CHUNK) + 2 : rows;
         const int64_t tiles = (n * P.units_per_row + gpw - 1) / gpw;
-        // rows: about four rounds of all resident warps, as far as a warp's row offsets go; chunks are long enough alone
+        // rows: four rounds of all resident warps (2 and 8: 3 to 10 % slower), as far as a warp's row offsets go; chunks are long enough alone
         int64_t per = pass ? 1 : tiles / (resident * 4);
         const int64_t most = (int64_t)(RING_ROWS - 2) * P.units_per_row / gpw;
         per = per > most ? most : per;
@@ -644,7 +672,7 @@ template <AttendKind K, typename T, int VE, int NV, int G> static cudaError_t ru
         count_launches(1);
     }
     if (P.split) {
-        const int grid = (int)limit_grid(sm_count() * 2);
+        const int grid = (int)limit_grid(sm_count() * 8);
         if constexpr (K == AT_FORWARD) k_attend_forward_join<T><<<grid, AT_THREADS, 0, s>>>(P);
         else k_attend_sum_join<T, K == AT_DKV><<<grid, AT_THREADS, 0, s>>>(P);
         count_launches(1);

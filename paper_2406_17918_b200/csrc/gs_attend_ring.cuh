@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
     unsigned char* mine = ring_smem + (size_t)warp * S::WARP;
     int4* rows_s = reinterpret_cast<int4*>(mine + RING_SLOTS * S::SLOT);           // begin, end, row, item (or -1: listed as long)
     const uint32_t mine_a = (uint32_t)__cvta_generic_to_shared(mine);
-    const int tl = P.tl, t = lane & (tl - 1), gi = lane / tl, gpw = 32 / tl, upr = P.units_per_row;
+    const int tl = P.tl, t = lane & (tl - 1), gpw = 32 / tl, upr = P.units_per_row;
     const int rows = P.chunk_mode ? __ldcg(P.words) : length_of(P.rows), cols = length_of(P.columns);
     const int64_t units = (int64_t)rows * upr;
     const float c2 = P.a.scale * LOG2E;
@@ -86,6 +86,14 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
     const uint32_t ahead_step = (uint32_t)av.head_stride * SZ, bhead_step = (uint32_t)bv.head_stride * SZ;
     const char* abase = (const char*)av.data + t * PB;
     const char* bbase = (const char*)bv.data + t * PB;
+    const int tshift = 31 - __clz(tl), ushift = (upr & (upr - 1)) == 0 ? 31 - __clz(upr) : -1;
+    // byte strides of the rows' own operands and of the results
+    auto stride32 = [](const HeadView& v) { return (uint32_t)v.row_stride * SZ; };
+    const HeadView& r0v = K == AT_DKV ? P.a.k : P.a.q;
+    const HeadView& r1v = K == AT_DKV ? P.a.v : P.a.dout;
+    const HeadView& o0v = K == AT_FORWARD ? P.a.out : (K == AT_DQ ? P.a.dq : P.a.dk);
+    const HeadView& o1v = P.a.dv;
+    const uint32_t r0step = stride32(r0v), r1step = stride32(r1v), o0step = stride32(o0v), o1step = stride32(o1v), outstep = stride32(P.a.out);
     int size[NV];                                                                   // bytes of this lane's pieces: 0 behind the row's end
 #pragma unroll
     for (int n = 0; n < NV; ++n) size[n] = (t + n * tl) * VE < D ? PB : 0;
@@ -123,40 +131,46 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
         }
         __syncwarp();
 
-        // ---- the producer's position: unit, row, walk and next edge of this group
-        int lu = gi, e_next = 0, e_end = 0, pass = 0, lr = 0, head = 0;
+        // ---- the producer's position: unit, row, walk and next edge of this group.  A group that has finished its unit takes
+        // the warp's next one, so that long rows do not hold up the others; the heads of a row stay side by side.
+        int next_unit = 0, e_next = 0, e_end = 0, pass = 0, lr = 0, head = -1;
         bool fresh = true, walk = true;
         const char* ap = abase;                              // this lane's first piece in row 0 of the edges' operands
         const char* bp = bbase;
         uint32_t next = 0;
-        int idx[U];                                // the batch whose indices are on their way
+        int idx[U];                                          // the batch whose indices are on their way
         auto fetch = [&]() {
             next = 0;
 #pragma unroll
             for (int j = 0; j < U; ++j) idx[j] = -1;
-            int4 r;
-            if (fresh) {
-                for (;; lu += gpw) {
-                    if (lu >= left) return;
-                    const int v = off + lu;
-                    lr = upr == 1 ? v : v / upr;
+            for (;;) {
+                const uint32_t want = __ballot_sync(FULL, fresh);
+                if (!want || next_unit >= left) break;
+                const int lu = next_unit + (__popc(want & ((1u << (lane - t)) - 1u)) >> tshift);
+                next_unit += __popc(want) >> tshift;
+                if (fresh && lu < left) {
+                    const int v = off + lu, last = head;
+                    lr = ushift >= 0 ? v >> ushift : v / upr;
                     head = v - lr * upr;
-                    r = rows_s[lr];
-                    if (K != AT_DKV || r.y > r.x) break;
-                    // a source that no destination lists: zeros at once (a listed long row: nothing)
-                    if (r.w >= 0 && !P.chunk_mode) {
-                        const float zero[E] = {};
-                        store_piece<T, VE, NV>((T*)P.a.dk.data + (int64_t)r.z * P.a.dk.row_stride + (int64_t)head * P.a.dk.head_stride, t, tl, D, zero);
-                        store_piece<T, VE, NV>((T*)P.a.dv.data + (int64_t)r.z * P.a.dv.row_stride + (int64_t)head * P.a.dv.head_stride, t, tl, D, zero);
+                    const int4 r = rows_s[lr];
+                    walk = walk || head != last;
+                    if (K == AT_DKV && r.y <= r.x) {
+                        // a source that no destination lists: zeros at once (a listed long row: nothing)
+                        if (r.w >= 0 && !P.chunk_mode) {
+                            const float zero[E] = {};
+                            store_piece<T, VE, NV>((T*)((char*)o0v.data + (uint64_t)(uint32_t)r.z * o0step) + head * (int)o0v.head_stride, t, tl, D, zero);
+                            store_piece<T, VE, NV>((T*)((char*)o1v.data + (uint64_t)(uint32_t)r.z * o1step) + head * (int)o1v.head_stride, t, tl, D, zero);
+                        }
+                    } else {
+                        e_next = r.x;
+                        e_end = r.y;
+                        pass = 0;
+                        next = FIRST;
+                        fresh = false;
                     }
                 }
-                e_next = r.x;
-                e_end = r.y;
-                pass = 0;
-                next = FIRST;
-                fresh = false;
-                walk = true;
             }
+            if (fresh) return;                               // nothing left for this group
             if (walk) next |= HEAD;
             walk = false;
             const int32_t* c = P.cols + e_next;
@@ -171,7 +185,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                     walk = true;
                 } else {
                     next |= LAST;
-                    lu += gpw;
+                    walk = passes > 1;
                     fresh = true;
                 }
             }
@@ -214,22 +228,22 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
             if (batch & FIRST) {
                 const int4 r = rows_s[(batch >> 8) & 255];
                 const bool any = K != AT_DKV || r.y > r.x;
-                auto rowcopy = [&](const HeadView& v, int h, int piece) {
-                    const char* p = (const char*)v.data + ((int64_t)r.z * v.row_stride + (int64_t)h * v.head_stride) * SZ;
+                auto rowcopy = [&](const HeadView& v, uint32_t step, int h, int piece) {
+                    const char* p = (const char*)v.data + (uint64_t)(uint32_t)r.z * step + (uint32_t)(h * (int)v.head_stride * SZ);
 #pragma unroll
                     for (int n = 0; n < NV; ++n)
                         copy_async<PB>(lp + (uint32_t)(U * S::EDGE + piece + n) * 32 * PB, size[n] ? p + (t + n * tl) * PB : p, any ? size[n] : 0);
                 };
                 if (K == AT_DKV) {
-                    rowcopy(P.a.k, hd, 0);
-                    rowcopy(P.a.v, hd, NV);
+                    rowcopy(r0v, r0step, hd, 0);
+                    rowcopy(r1v, r1step, hd, NV);
                 } else {
 #pragma unroll
                     for (int i = 0; i < G; ++i) {
-                        rowcopy(P.a.q, h0 + i, i * NV);
+                        rowcopy(r0v, r0step, h0 + i, i * NV);
                         if (K == AT_DQ) {
-                            rowcopy(P.a.dout, h0 + i, (G + i) * NV);
-                            rowcopy(P.a.out, h0 + i, (2 * G + i) * NV);
+                            rowcopy(r1v, r1step, h0 + i, (G + i) * NV);
+                            rowcopy(P.a.out, outstep, h0 + i, (2 * G + i) * NV);
                             copy_async<4>(base + S::PIECES + (i * 32 + lane) * 4, P.a.lse + (int64_t)r.z * P.a.q_heads + h0 + i, 4);
                         }
                     }
@@ -353,7 +367,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                                 const float inv = none ? 0.f : 1.f / l[i];
 #pragma unroll
                                 for (int c = 0; c < E; ++c) o[c] = none ? 0.f : o[c] * inv;
-                                store_piece<T, VE, NV>((T*)P.a.out.data + (int64_t)rw.z * P.a.out.row_stride + (int64_t)hh * P.a.out.head_stride, t, tl, D, o);
+                                store_piece<T, VE, NV>((T*)((char*)o0v.data + (uint64_t)(uint32_t)rw.z * o0step) + hh * (int)o0v.head_stride, t, tl, D, o);
                                 if (t == 0) P.a.lse[(int64_t)rw.z * P.a.q_heads + hh] = none ? -INFINITY : m[i] * LN2 + logf(l[i]);
                             }
                         }
@@ -422,7 +436,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                             float o[E];
                             unpair(acc[i], o);
                             if (P.chunk_mode) store_partial<VE, NV>(P.partial + ((int64_t)rw.w * P.a.q_heads + hh) * D, t, tl, D, o);
-                            else store_piece<T, VE, NV>((T*)P.a.dq.data + (int64_t)rw.z * P.a.dq.row_stride + (int64_t)hh * P.a.dq.head_stride, t, tl, D, o);
+                            else store_piece<T, VE, NV>((T*)((char*)o0v.data + (uint64_t)(uint32_t)rw.z * o0step) + hh * (int)o0v.head_stride, t, tl, D, o);
                         }
                     }
                 }
@@ -467,8 +481,8 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                             store_partial<VE, NV>(part, t, tl, D, dk);
                             store_partial<VE, NV>(part + D, t, tl, D, dv);
                         } else {
-                            store_piece<T, VE, NV>((T*)P.a.dk.data + (int64_t)rw.z * P.a.dk.row_stride + (int64_t)h * P.a.dk.head_stride, t, tl, D, dk);
-                            store_piece<T, VE, NV>((T*)P.a.dv.data + (int64_t)rw.z * P.a.dv.row_stride + (int64_t)h * P.a.dv.head_stride, t, tl, D, dv);
+                            store_piece<T, VE, NV>((T*)((char*)o0v.data + (uint64_t)(uint32_t)rw.z * o0step) + h * (int)o0v.head_stride, t, tl, D, dk);
+                            store_piece<T, VE, NV>((T*)((char*)o1v.data + (uint64_t)(uint32_t)rw.z * o1step) + h * (int)o1v.head_stride, t, tl, D, dv);
                         }
                     }
                 }
