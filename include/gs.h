@@ -507,9 +507,9 @@ gs_status gs_embedding_backward_sparse(const void* d_dout, gs_dtype dout_dtype, 
  *              sources' rows and kv_heads (a divisor of q_heads); 1 <= head_dim <= 256, q_heads <= 128
  *   d_lse      float[max_dst][q_heads]
  * gs_block_reverse turns the block's edges to source order, once for all layers that use the block: the
- * destinations of source j, ascending, are d_rev_dst[d_rev_indptr[j] .. d_rev_indptr[j+1]) (int32[max_src + 1] and
- * int32[max_edges]; masked edges are left out).  The backward pass recomputes the probabilities from lse and sums dk
- * and dv in that order; dq, dk and dv are written for every row of their counts (zeros where nothing contributes).
+ * destinations of source j, ascending, are d_rev_dst[d_rev_indptr[j] .. d_rev_indptr[j+1]), and d_rev_edge holds the
+ * edges they came from (int32[max_src + 1] and twice int32[max_edges]; masked edges are left out).  The backward pass
+ * recomputes the probabilities from lse and sums dk and dv in that order; dq, dk and dv are written for every row of their counts (zeros where nothing contributes).
  * Workspace: gs_block_attention_workspace_bytes, enough for any of the three calls. */
 typedef struct {
     void* d_data;
@@ -519,10 +519,10 @@ gs_status gs_block_attention_workspace_bytes(int32_t max_dst, int32_t max_edges,
 gs_status gs_block_attention_forward(const gs_block* block, int32_t max_row, gs_dtype dtype, int32_t q_heads, int32_t kv_heads,
                                      int32_t head_dim, float scale, const gs_heads* q, const gs_heads* k, const gs_heads* v,
                                      const gs_heads* out, float* d_lse, void* d_workspace, size_t workspace_bytes, void* stream);
-gs_status gs_block_reverse(const gs_block* block, int32_t* d_rev_indptr, int32_t* d_rev_dst, void* d_workspace,
+gs_status gs_block_reverse(const gs_block* block, int32_t* d_rev_indptr, int32_t* d_rev_dst, int32_t* d_rev_edge, void* d_workspace,
                            size_t workspace_bytes, void* stream);
 gs_status gs_block_attention_backward(const gs_block* block, int32_t max_row, const int32_t* d_rev_indptr, const int32_t* d_rev_dst,
-                                      gs_dtype dtype, int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale,
+                                      const int32_t* d_rev_edge, gs_dtype dtype, int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale,
                                       const gs_heads* q, const gs_heads* k, const gs_heads* v, const gs_heads* out,
                                       const float* d_lse, const gs_heads* dout, const gs_heads* dq, const gs_heads* dk,
                                       const gs_heads* dv, void* d_workspace, size_t workspace_bytes, void* stream);

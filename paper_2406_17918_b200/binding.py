@@ -119,8 +119,8 @@ def _load():
         "gs_xent_backward": [vp, i64, vp, i64, ctypes.c_int, i32, i64, i32, ctypes.c_float, vp, vp, vp, vp, i64, vp, i64, ctypes.c_int, vp, sz, vp],
         "gs_block_attention_workspace_bytes": [i32, i32, i32, i32, psz],
         "gs_block_attention_forward": [vp, i32, ctypes.c_int, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, sz, vp],
-        "gs_block_reverse": [vp, vp, vp, vp, sz, vp],
-        "gs_block_attention_backward": [vp, i32, vp, vp, ctypes.c_int, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+        "gs_block_reverse": [vp, vp, vp, vp, vp, sz, vp],
+        "gs_block_attention_backward": [vp, i32, vp, vp, vp, ctypes.c_int, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                         vp, sz, vp],
     }
     for name, args in sig.items():
@@ -803,17 +803,21 @@ def gs_block_attention_forward(indptr: torch.Tensor, indices: torch.Tensor, q: t
 
 
 def gs_block_reverse(indptr: torch.Tensor, indices: torch.Tensor, num_src: int, workspace: torch.Tensor, rev_indptr: torch.Tensor = None,
-                     rev_dst: torch.Tensor = None, counts=None, stream=None):
-    """The block in source order: (int32[num_src + 1] offsets, int32[edges] destinations), masked edges left out."""
+                     rev_dst: torch.Tensor = None, rev_edge: torch.Tensor = None, counts=None, stream=None):
+    """The block in source order: (int32[num_src + 1] offsets, int32[edges] destinations, int32[edges] edges they came
+    from), masked edges left out."""
     b = _csr_block(indptr, indices, num_src, counts)
     if rev_indptr is None:
         rev_indptr = torch.empty(b.max_src + 1, dtype=torch.int32, device=indptr.device)
     if rev_dst is None:
         rev_dst = torch.empty(b.max_edges, dtype=torch.int32, device=indptr.device)
-    if _ids_1d(rev_indptr, "rev_indptr").numel() < b.max_src + 1 or _ids_1d(rev_dst, "rev_dst").numel() < b.max_edges:
-        raise ValueError("rev_indptr / rev_dst are too small")
-    _check(_L.gs_block_reverse(ctypes.byref(b), _addr(rev_indptr), _addr(rev_dst), _addr(workspace), workspace.numel(), _on(stream, workspace)))
-    return rev_indptr, rev_dst
+    if rev_edge is None:
+        rev_edge = torch.empty(b.max_edges, dtype=torch.int32, device=indptr.device)
+    if _ids_1d(rev_indptr, "rev_indptr").numel() < b.max_src + 1 or _ids_1d(rev_dst, "rev_dst").numel() < b.max_edges or \
+            _ids_1d(rev_edge, "rev_edge").numel() < b.max_edges:
+        raise ValueError("rev_indptr / rev_dst / rev_edge are too small")
+    _check(_L.gs_block_reverse(ctypes.byref(b), _addr(rev_indptr), _addr(rev_dst), _addr(rev_edge), _addr(workspace), workspace.numel(), _on(stream, workspace)))
+    return rev_indptr, rev_dst, rev_edge
 
 
 def gs_block_attention_backward(indptr: torch.Tensor, indices: torch.Tensor, reverse, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -824,8 +828,9 @@ def gs_block_attention_backward(indptr: torch.Tensor, indices: torch.Tensor, rev
     n, hq, d = q.shape
     hk = k.shape[1]
     b = _csr_block(indptr, indices, k.shape[0], counts)
-    rev_indptr, rev_dst = reverse
-    if _ids_1d(rev_indptr, "rev_indptr").numel() < b.max_src + 1 or _ids_1d(rev_dst, "rev_dst").numel() < b.max_edges:
+    rev_indptr, rev_dst, rev_edge = reverse
+    if _ids_1d(rev_indptr, "rev_indptr").numel() < b.max_src + 1 or _ids_1d(rev_dst, "rev_dst").numel() < b.max_edges or \
+            _ids_1d(rev_edge, "rev_edge").numel() < b.max_edges:
         raise ValueError("reverse belongs to another block")
     if lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.shape[0] < b.max_dst or lse.shape[1] != hq:
         raise TypeError("lse must be a contiguous float32 tensor [dst, q_heads]")
@@ -836,7 +841,7 @@ def gs_block_attention_backward(indptr: torch.Tensor, indices: torch.Tensor, rev
     keep, (pq, pk, pv, po, pdo, pdq, pdk, pdv) = _heads(
         t, (q, "q", b.max_dst, hq, d), (k, "k", b.max_src, hk, d), (v, "v", b.max_src, hk, d), (out, "out", b.max_dst, hq, d),
         (dout, "dout", b.max_dst, hq, d), (dq, "dq", b.max_dst, hq, d), (dk, "dk", b.max_src, hk, d), (dv, "dv", b.max_src, hk, d))
-    _check(_L.gs_block_attention_backward(ctypes.byref(b), int(max_row), _addr(rev_indptr), _addr(rev_dst), _dtype(t), hq, hk, d,
+    _check(_L.gs_block_attention_backward(ctypes.byref(b), int(max_row), _addr(rev_indptr), _addr(rev_dst), _addr(rev_edge), _dtype(t), hq, hk, d,
                                           d ** -0.5 if scale is None else float(scale), pq, pk, pv, po, _addr(lse), pdo, pdq, pdk, pdv,
                                           _addr(workspace), workspace.numel(), _on(stream, workspace)))
     return dq, dk, dv

@@ -3,7 +3,9 @@
 // For destination i, query head h, key/value head g(h) and the edges j of row i:
 //   s = scale q_ih . k_jg,  lse_ih = log sum_j exp s,  o_ih = sum_j p v_jg,  p = exp(s - lse_ih);
 //   delta = do . o,  ds = p (do . v - delta) scale,  dq_i = sum_j ds k_j,  dk_j = sum_i ds q_i,  dv_j = sum_i p do_i.
-// One pass over the edges each: the forward keeps a running maximum and sum, the backward recomputes p from lse.
+// The forward keeps a running maximum and sum.  The backward recomputes p from lse in the pass that sums dq; the ring kernels
+// leave p and ds there, 8 bytes per edge and head, for the pass in source order, which then needs neither k nor v
+// (4.36 M edges of 4 heads of 32: 848 us with the dot products taken again).
 //
 // Every edge gathers whole rows, so the kernels are bound by the gathered bytes: a group of tl lanes holds one
 // (row, head) with one wide load per lane and operand, U edges are in flight per group, and groups of one row's heads are
@@ -45,7 +47,9 @@ struct Attend {
     int2* items;                // chunk -> (row, chunk of the row)
     int4* longs;                // long row -> (row, first chunk, chunks, -)
     float* partial;
-    float2* stat;               // [dst][q heads]: lse in base 2, delta
+    float2* stat;               // [dst][q heads]: lse in base 2, delta (one-element kernels)
+    float2* pd;                 // [edges][q heads]: p and ds before the scale, from the dq pass (ring kernels)
+    const int32_t* edges;       // source-order pass: the edge each column came from
 };
 
 __device__ __forceinline__ int length_of(const Count& c) {
@@ -570,9 +574,24 @@ __global__ void __launch_bounds__(AT_THREADS) k_edge_rows(const int32_t* __restr
     }
 }
 
+// The destinations in the order of the sorted edges.
+__global__ void __launch_bounds__(AT_THREADS) k_edge_gather(Count edges, const int32_t* __restrict__ edge, const int32_t* __restrict__ rows, int32_t* __restrict__ out) {
+    constexpr int U = 4;
+    chain_wait();
+    const int n = length_of(edges);
+    for (int64_t i = (int64_t)blockIdx.x * AT_THREADS * U + threadIdx.x; i < n; i += (int64_t)gridDim.x * AT_THREADS * U) {
+        int e[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) e[j] = i + j * AT_THREADS < n ? __ldcg(edge + i + j * AT_THREADS) : 0;
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            if (i + j * AT_THREADS < n) out[i + j * AT_THREADS] = __ldcg(rows + e[j]);
+    }
+}
+
 // ---------------------------------------------------------------- launches
 struct AttendLayout {
-    size_t words, items, longs, stat, partial, total;
+    size_t words, items, longs, stat, pd, partial, total;
 };
 
 static AttendLayout attend_layout(int64_t dst, int64_t edges, int32_t q_heads, int32_t head_dim) {
@@ -584,6 +603,7 @@ static AttendLayout attend_layout(int64_t dst, int64_t edges, int32_t q_heads, i
     l.items = take((size_t)chunks * 8);
     l.longs = take((size_t)(edges / AT_CHUNK + 1) * 16);
     l.stat = take((size_t)dst * q_heads * 8);
+    l.pd = take((size_t)edges * q_heads * 8);
     l.partial = take((size_t)chunks * q_heads * (2 * (size_t)head_dim + 2) * 4);
     l.total = off;
     return l;
@@ -646,7 +666,7 @@ template <AttendKind K, typename T, int VE, int NV, int G> static void run_atten
 
 // The ring kernels: edge batches through shared memory.
 template <AttendKind K, typename T, int VE, int NV, int G> static cudaError_t run_ring(Attend P, int64_t rows, cudaStream_t s) {
-    constexpr int U = K == AT_DKV ? (G == 4 ? 1 : 2) : 4;
+    constexpr int U = K == AT_DKV ? 2 : 4;       // edges per batch: sampled rows have tens, sources two or three (4 there: 8 % slower)
     constexpr int smem = RING_WARPS * RingShape<K, T, VE, NV, G, U>::WARP;
     auto kernel = k_attend_ring<K, T, VE, NV, G, U>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -725,6 +745,7 @@ static Attend attend_params(const BlockAttention& a, void* workspace) {
     P.longs = (int4*)(ws + l.longs);
     P.partial = (float*)(ws + l.partial);
     P.stat = (float2*)(ws + l.stat);
+    P.pd = (float2*)(ws + l.pd);
     return P;
 }
 
@@ -738,7 +759,8 @@ cudaError_t launch_attention_forward(const BlockAttention& a, void* workspace, c
     return run_kind<AT_FORWARD>(P, wide_elems(a, {&a.q, &a.k, &a.v, &a.out}), a.dst.bound, a.max_row, s);
 }
 
-cudaError_t launch_attention_backward(const BlockAttention& a, const int32_t* rev_indptr, const int32_t* rev_dst, void* workspace, cudaStream_t s) {
+cudaError_t launch_attention_backward(const BlockAttention& a, const int32_t* rev_indptr, const int32_t* rev_dst, const int32_t* rev_edge,
+                                      void* workspace, cudaStream_t s) {
     Attend P = attend_params(a, workspace);
     const int ve = wide_elems(a, {&a.q, &a.k, &a.v, &a.out, &a.dout, &a.dq, &a.dk, &a.dv});
     P.starts = a.indptr;
@@ -750,6 +772,7 @@ cudaError_t launch_attention_backward(const BlockAttention& a, const int32_t* re
     if (e != cudaSuccess) return e;
     P.starts = rev_indptr;
     P.cols = rev_dst;
+    P.edges = rev_edge;
     P.rows = a.src;
     P.columns = a.dst;
     P.split = a.edge_bound > AT_CHUNK;
@@ -757,15 +780,18 @@ cudaError_t launch_attention_backward(const BlockAttention& a, const int32_t* re
 }
 
 cudaError_t launch_block_reverse(const int32_t* indptr, const int32_t* indices, Count dst, Count src, Count edges, int32_t* rev_indptr,
-                                 int32_t* rev_dst, void* workspace, cudaStream_t s) {
+                                 int32_t* rev_dst, int32_t* rev_edge, void* workspace, cudaStream_t s) {
     const size_t list = align_up((size_t)edges.bound * 4, 256);
     int32_t* rows = (int32_t*)workspace;
     uint32_t* keys = (uint32_t*)((char*)workspace + list);
     int64_t blocks = ((int64_t)dst.bound + AT_THREADS / 8 - 1) / (AT_THREADS / 8);
     if (blocks > sm_count() * 32) blocks = sm_count() * 32;
     cudaError_t e = launch_train(k_edge_rows, blocks, AT_THREADS, 0, s, indptr, dst, (int)edges.bound, rows);
-    if (e == cudaSuccess) e = launch_key_sort(indices, rows, edges, src.bound, (char*)workspace + 2 * list, keys, rev_dst, s);
+    if (e == cudaSuccess) e = launch_key_sort(indices, nullptr, edges, src.bound, (char*)workspace + 2 * list, keys, rev_edge, s);
     if (e == cudaSuccess) e = launch_row_starts(keys, edges, src, rev_indptr, s);
+    blocks = ((int64_t)edges.bound + AT_THREADS * 4 - 1) / (AT_THREADS * 4);
+    if (blocks > sm_count() * 16) blocks = sm_count() * 16;
+    if (e == cudaSuccess) e = launch_train(k_edge_gather, blocks, AT_THREADS, 0, s, edges, rev_edge, rows, rev_dst);
     return e;
 }
 

@@ -4,7 +4,7 @@
 // one row).  Every lane copies exactly the pieces it will use itself into slots of its own (cp.async, zero-filled where
 // an edge is masked), RING_DEPTH batches ahead, and the column indices one batch earlier still: the gathers of the next
 // batches are in flight across row boundaries while one is computed, they hold no registers, and no barrier is needed
-// because no lane reads another's copies.  Rows' own operands (q; q, dout, out; k, v) ride in their first batch.
+// because no lane reads another's copies.  Rows' own operands (q; q, dout, out) ride in their first batch.
 // Latency is hidden with 8 to 14 warps per SM, so what is left to save is instructions: pairs of values go through
 // packed 32-bit operations, addresses are one multiply-add per copy, and masked edges take the same path as others.
 #pragma once
@@ -58,7 +58,7 @@ template <int N> __device__ __forceinline__ void ring_sum(float (&x)[N], int tl)
 template <AttendKind K, typename T, int VE, int NV, int G, int U> struct RingShape {
     static constexpr int PB = (int)sizeof(T) * VE;                                 // bytes of a piece
     static constexpr int EDGE = (K == AT_DKV ? 2 * NV * G : 2 * NV);               // pieces per edge
-    static constexpr int ROW = K == AT_FORWARD ? NV * G : (K == AT_DQ ? 3 * NV * G : 2 * NV);
+    static constexpr int ROW = K == AT_FORWARD ? NV * G : (K == AT_DQ ? 3 * NV * G : 0);
     static constexpr int PIECES = (U * EDGE + ROW) * 32 * PB;
     static constexpr int STAT = K == AT_DKV ? U * G * 32 * 8 : (K == AT_DQ ? G * 32 * 4 : 0);
     static constexpr int SLOT = PIECES + STAT;
@@ -89,8 +89,8 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
     const int tshift = 31 - __clz(tl), ushift = (upr & (upr - 1)) == 0 ? 31 - __clz(upr) : -1;
     // byte strides of the rows' own operands and of the results
     auto stride32 = [](const HeadView& v) { return (uint32_t)v.row_stride * SZ; };
-    const HeadView& r0v = K == AT_DKV ? P.a.k : P.a.q;
-    const HeadView& r1v = K == AT_DKV ? P.a.v : P.a.dout;
+    const HeadView& r0v = P.a.q;
+    const HeadView& r1v = P.a.dout;
     const HeadView& o0v = K == AT_FORWARD ? P.a.out : (K == AT_DQ ? P.a.dq : P.a.dk);
     const HeadView& o1v = P.a.dv;
     const uint32_t r0step = stride32(r0v), r1step = stride32(r1v), o0step = stride32(o0v), o1step = stride32(o1v), outstep = stride32(P.a.out);
@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
         const char* ap = abase;                              // this lane's first piece in row 0 of the edges' operands
         const char* bp = bbase;
         uint32_t next = 0;
-        int idx[U];                                          // the batch whose indices are on their way
+        int idx[U], edge[U];                                 // the batch whose indices are on their way; dkv: its edges, dq: the first
         auto fetch = [&]() {
             next = 0;
 #pragma unroll
@@ -176,7 +176,11 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
             const int32_t* c = P.cols + e_next;
 #pragma unroll
             for (int j = 0; j < U; ++j)
-                if (e_next + j < e_end) idx[j] = __ldg(c + j);
+                if (e_next + j < e_end) {
+                    idx[j] = __ldg(c + j);
+                    if (K == AT_DKV) edge[j] = __ldg(P.edges + e_next + j);
+                }
+            if (K == AT_DQ) edge[0] = e_next;
             next |= LIVE | (uint32_t)lr << 8 | (uint32_t)head << 16 | (uint32_t)pass << 24;
             e_next += U;
             if (e_next >= e_end) {
@@ -204,7 +208,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
             }
 #pragma unroll
             for (int j = 0; j < U; ++j) {
-                const bool on = (uint32_t)idx[j] < (uint32_t)cols;
+                const bool on = (uint32_t)idx[j] < (uint32_t)cols && (K != AT_DKV || (uint32_t)edge[j] < (uint32_t)P.edge_bound);
                 const uint32_t col = on ? idx[j] : 0;
                 batch |= on ? 16u << j : 0u;
                 const char* a = ap + (uint64_t)col * astep;
@@ -222,30 +226,24 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                 if (K == AT_DKV) {
 #pragma unroll
                     for (int i = 0; i < G; ++i)
-                        copy_async<8>(base + S::PIECES + ((j * G + i) * 32 + lane) * 8, P.stat + (uint64_t)col * P.a.q_heads + h0 + i, on ? 8 : 0);
+                        copy_async<8>(base + S::PIECES + ((j * G + i) * 32 + lane) * 8, P.pd + (uint64_t)(on ? edge[j] : 0) * P.a.q_heads + h0 + i, on ? 8 : 0);
                 }
             }
-            if (batch & FIRST) {
+            if (K != AT_DKV && (batch & FIRST)) {
                 const int4 r = rows_s[(batch >> 8) & 255];
-                const bool any = K != AT_DKV || r.y > r.x;
                 auto rowcopy = [&](const HeadView& v, uint32_t step, int h, int piece) {
                     const char* p = (const char*)v.data + (uint64_t)(uint32_t)r.z * step + (uint32_t)(h * (int)v.head_stride * SZ);
 #pragma unroll
                     for (int n = 0; n < NV; ++n)
-                        copy_async<PB>(lp + (uint32_t)(U * S::EDGE + piece + n) * 32 * PB, size[n] ? p + (t + n * tl) * PB : p, any ? size[n] : 0);
+                        copy_async<PB>(lp + (uint32_t)(U * S::EDGE + piece + n) * 32 * PB, size[n] ? p + (t + n * tl) * PB : p, size[n]);
                 };
-                if (K == AT_DKV) {
-                    rowcopy(r0v, r0step, hd, 0);
-                    rowcopy(r1v, r1step, hd, NV);
-                } else {
 #pragma unroll
-                    for (int i = 0; i < G; ++i) {
-                        rowcopy(r0v, r0step, h0 + i, i * NV);
-                        if (K == AT_DQ) {
-                            rowcopy(r1v, r1step, h0 + i, (G + i) * NV);
-                            rowcopy(P.a.out, outstep, h0 + i, (2 * G + i) * NV);
-                            copy_async<4>(base + S::PIECES + (i * 32 + lane) * 4, P.a.lse + (int64_t)r.z * P.a.q_heads + h0 + i, 4);
-                        }
+                for (int i = 0; i < G; ++i) {
+                    rowcopy(r0v, r0step, h0 + i, i * NV);
+                    if (K == AT_DQ) {
+                        rowcopy(r1v, r1step, h0 + i, (G + i) * NV);
+                        rowcopy(P.a.out, outstep, h0 + i, (2 * G + i) * NV);
+                        copy_async<4>(base + S::PIECES + (i * 32 + lane) * 4, P.a.lse + (int64_t)r.z * P.a.q_heads + h0 + i, 4);
                     }
                 }
             }
@@ -266,16 +264,18 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
 
         // what a unit keeps from batch to batch
         constexpr int NX = K == AT_DKV ? 1 : G, NA = K == AT_DKV ? 2 : G;
-        f32x2 x0[NX][N2], x1[K == AT_FORWARD ? 1 : NX][K == AT_FORWARD ? 1 : N2];   // q; q, dout; k, v
+        f32x2 x0[K == AT_DKV ? 1 : NX][K == AT_DKV ? 1 : N2], x1[K == AT_DQ ? NX : 1][K == AT_DQ ? N2 : 1];   // q; q, dout
         f32x2 acc[NA][N2];                                                           // out; dq; dk, dv
         float m[G], l[G];                                                            // running maximum and sum; lse (base 2), delta
+        if constexpr (K != AT_DKV) {
 #pragma unroll
-        for (int i = 0; i < NX; ++i)
+            for (int i = 0; i < NX; ++i)
 #pragma unroll
-            for (int c = 0; c < N2; ++c) {
-                x0[i][c] = 0;
-                if constexpr (K != AT_FORWARD) x1[i][c] = 0;
-            }
+                for (int c = 0; c < N2; ++c) {
+                    x0[i][c] = 0;
+                    if constexpr (K == AT_DQ) x1[i][c] = 0;
+                }
+        }
 #pragma unroll
         for (int i = 0; i < NA; ++i)
 #pragma unroll
@@ -284,18 +284,25 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
         for (int i = 0; i < G; ++i) m[i] = l[i] = 0.f;
 
         uint32_t batches[RING_DEPTH];
+        int first_edge[K == AT_DQ ? RING_DEPTH : 1];         // dq: where p and ds of a batch's edges go
         fetch();
 #pragma unroll
         for (int s = 0; s < RING_DEPTH; ++s) {
             batches[s] = issue(s);
+            if (K == AT_DQ) first_edge[s] = edge[0];
             fetch();
         }
         int slot = 0, ahead = RING_DEPTH;
         while (__any_sync(FULL, batches[0] & LIVE)) {
             const uint32_t batch = batches[0];
+            const int my_edge = first_edge[0];
 #pragma unroll
-            for (int s = 0; s + 1 < RING_DEPTH; ++s) batches[s] = batches[s + 1];
+            for (int s = 0; s + 1 < RING_DEPTH; ++s) {
+                batches[s] = batches[s + 1];
+                if (K == AT_DQ) first_edge[s] = first_edge[s + 1];
+            }
             batches[RING_DEPTH - 1] = issue(ahead);
+            if (K == AT_DQ) first_edge[RING_DEPTH - 1] = edge[0];
             fetch();
             asm volatile("cp.async.wait_group %0;" ::"n"(RING_DEPTH) : "memory");
             const int h = (batch >> 16) & 255;
@@ -422,8 +429,10 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                     pieces(slot, j * S::EDGE, k);
 #pragma unroll
                     for (int i = 0; i < G; ++i) {
-                        const float ds = on(j) ? fast_exp2(fmaf(s[j * G + i], c2, -m[i])) * (s[U * G + j * G + i] - l[i]) : 0.f;
+                        const float p = on(j) ? fast_exp2(fmaf(s[j * G + i], c2, -m[i])) : 0.f;
+                        const float ds = on(j) ? p * (s[U * G + j * G + i] - l[i]) : 0.f;
                         axpy2(ds, k, acc[i]);
+                        if (on(j) && t == 0) P.pd[(int64_t)(my_edge + j) * P.a.q_heads + h * G + i] = make_float2(p, ds);
                     }
                 }
                 if (batch & LAST) {
@@ -442,32 +451,19 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                 }
             } else {
                 if (batch & FIRST) {
-                    pieces(slot, U * S::EDGE, x0[0]);
-                    pieces(slot, U * S::EDGE + NV, x1[0]);
 #pragma unroll
                     for (int c = 0; c < N2; ++c) acc[0][c] = acc[1][c] = 0;
                 }
-                float s[2 * U * G];
-                f32x2 q[U][G][N2], go[U][G][N2];
 #pragma unroll
                 for (int j = 0; j < U; ++j)
 #pragma unroll
-                    for (int i = 0; i < G; ++i) {
-                        pieces(slot, j * S::EDGE + i * 2 * NV, q[j][i]);
-                        pieces(slot, j * S::EDGE + i * 2 * NV + NV, go[j][i]);
-                        s[j * G + i] = dot2(q[j][i], x0[0]);
-                        s[U * G + j * G + i] = dot2(go[j][i], x1[0]);
-                    }
-                ring_sum<2 * U * G>(s, tl);
-#pragma unroll
-                for (int j = 0; j < U; ++j)
-#pragma unroll
-                    for (int i = 0; i < G; ++i) {
-                        const float2 st = *reinterpret_cast<const float2*>(mine + slot * S::SLOT + S::PIECES + ((j * G + i) * 32 + lane) * 8);
-                        const float p = on(j) ? fast_exp2(fmaf(s[j * G + i], c2, -st.x)) : 0.f;
-                        const float ds = on(j) ? p * (s[U * G + j * G + i] - st.y) : 0.f;
-                        axpy2(p, go[j][i], acc[1]);
-                        axpy2(ds, q[j][i], acc[0]);
+                    for (int i = 0; i < G; ++i) {            // what is not an edge was filled with zeros
+                        f32x2 q[N2], go[N2];
+                        pieces(slot, j * S::EDGE + i * 2 * NV, q);
+                        pieces(slot, j * S::EDGE + i * 2 * NV + NV, go);
+                        const float2 pd = *reinterpret_cast<const float2*>(mine + slot * S::SLOT + S::PIECES + ((j * G + i) * 32 + lane) * 8);
+                        axpy2(pd.x, go, acc[1]);
+                        axpy2(pd.y, q, acc[0]);
                     }
                 if (batch & LAST) {
                     const int4 rw = rows_s[(batch >> 8) & 255];

@@ -87,9 +87,10 @@ struct BlockAttention {
 size_t attention_workspace(int64_t dst, int64_t edges, int32_t q_heads, int32_t head_dim);
 size_t reverse_workspace(int64_t edges);
 cudaError_t launch_attention_forward(const BlockAttention& a, void* workspace, cudaStream_t s);
-cudaError_t launch_attention_backward(const BlockAttention& a, const int32_t* rev_indptr, const int32_t* rev_dst, void* workspace, cudaStream_t s);
+cudaError_t launch_attention_backward(const BlockAttention& a, const int32_t* rev_indptr, const int32_t* rev_dst, const int32_t* rev_edge,
+                                      void* workspace, cudaStream_t s);
 cudaError_t launch_block_reverse(const int32_t* indptr, const int32_t* indices, Count dst, Count src, Count edges, int32_t* rev_indptr,
-                                 int32_t* rev_dst, void* workspace, cudaStream_t s);
+                                 int32_t* rev_dst, int32_t* rev_edge, void* workspace, cudaStream_t s);
 
 // ---- softmax cross entropy against every row of a table ----
 struct Xent {

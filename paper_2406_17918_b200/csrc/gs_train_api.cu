@@ -187,23 +187,23 @@ gs_status gs_block_attention_forward(const gs_block* block, int32_t max_row, gs_
     return GS_OK;
 }
 
-gs_status gs_block_reverse(const gs_block* block, int32_t* d_rev_indptr, int32_t* d_rev_dst, void* d_workspace,
+gs_status gs_block_reverse(const gs_block* block, int32_t* d_rev_indptr, int32_t* d_rev_dst, int32_t* d_rev_edge, void* d_workspace,
                            size_t workspace_bytes, void* stream) {
     GS_TRY(check_block(block));
-    if (!d_rev_indptr || (!d_rev_dst && block->max_edges > 0)) return set_error(GS_ERR_ARG, "NULL argument");
-    if (!aligned_to(d_rev_indptr, 4) || !aligned_to(d_rev_dst, 4)) return set_error(GS_ERR_ALIGN, "misaligned argument");
+    if (!d_rev_indptr || ((!d_rev_dst || !d_rev_edge) && block->max_edges > 0)) return set_error(GS_ERR_ARG, "NULL argument");
+    if (!aligned_to(d_rev_indptr, 4) || !aligned_to(d_rev_dst, 4) || !aligned_to(d_rev_edge, 4)) return set_error(GS_ERR_ALIGN, "misaligned argument");
     if (block->max_src == ((int32_t)0x7FFFFFFF)) return set_error(GS_ERR_ARG, "a size of the block is out of range");
     GS_TRY(check_workspace(d_workspace, workspace_bytes, reverse_workspace(block->max_edges)));
     // without a device count the edges end where the last row does
     const int32_t* d_edges = block->d_num_edges ? block->d_num_edges : block->d_indptr + block->max_dst;
     GS_TRAIN_CUDA(launch_block_reverse(block->d_indptr, block->d_indices, Count{block->d_num_dst, block->max_dst},
-                                       Count{block->d_num_src, block->max_src}, Count{d_edges, block->max_edges}, d_rev_indptr, d_rev_dst,
+                                       Count{block->d_num_src, block->max_src}, Count{d_edges, block->max_edges}, d_rev_indptr, d_rev_dst, d_rev_edge,
                                        d_workspace, (cudaStream_t)stream));
     return GS_OK;
 }
 
 gs_status gs_block_attention_backward(const gs_block* block, int32_t max_row, const int32_t* d_rev_indptr, const int32_t* d_rev_dst,
-                                      gs_dtype dtype, int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale,
+                                      const int32_t* d_rev_edge, gs_dtype dtype, int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale,
                                       const gs_heads* q, const gs_heads* k, const gs_heads* v, const gs_heads* out,
                                       const float* d_lse, const gs_heads* dout, const gs_heads* dq, const gs_heads* dk,
                                       const gs_heads* dv, void* d_workspace, size_t workspace_bytes, void* stream) {
@@ -218,11 +218,11 @@ gs_status gs_block_attention_backward(const gs_block* block, int32_t max_row, co
     GS_TRY(check_heads("dq", dq, block->max_dst, q_heads, head_dim, dtype, &a.dq));
     GS_TRY(check_heads("dk", dk, block->max_src, kv_heads, head_dim, dtype, &a.dk));
     GS_TRY(check_heads("dv", dv, block->max_src, kv_heads, head_dim, dtype, &a.dv));
-    if (!d_rev_indptr || (!d_rev_dst && block->max_edges > 0) || (!d_lse && block->max_dst > 0)) return set_error(GS_ERR_ARG, "NULL argument");
-    if (!aligned_to(d_rev_indptr, 4) || !aligned_to(d_rev_dst, 4) || !aligned_to(d_lse, 4)) return set_error(GS_ERR_ALIGN, "misaligned argument");
+    if (!d_rev_indptr || ((!d_rev_dst || !d_rev_edge) && block->max_edges > 0) || (!d_lse && block->max_dst > 0)) return set_error(GS_ERR_ARG, "NULL argument");
+    if (!aligned_to(d_rev_indptr, 4) || !aligned_to(d_rev_dst, 4) || !aligned_to(d_rev_edge, 4) || !aligned_to(d_lse, 4)) return set_error(GS_ERR_ALIGN, "misaligned argument");
     a.lse = const_cast<float*>(d_lse);
     GS_TRY(check_workspace(d_workspace, workspace_bytes, attention_workspace(block->max_dst, block->max_edges, q_heads, head_dim)));
-    GS_TRAIN_CUDA(launch_attention_backward(a, d_rev_indptr, d_rev_dst, d_workspace, (cudaStream_t)stream));
+    GS_TRAIN_CUDA(launch_attention_backward(a, d_rev_indptr, d_rev_dst, d_rev_edge, d_workspace, (cudaStream_t)stream));
     return GS_OK;
 }
 
