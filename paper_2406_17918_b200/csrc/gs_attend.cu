@@ -669,7 +669,8 @@ template <AttendKind K, typename T, int VE, int NV, int G> static cudaError_t ru
     constexpr int U = K == AT_DKV ? 2 : 4;       // edges per batch: sampled rows have tens, sources two or three (4 there: 8 % slower)
     constexpr int smem = RING_WARPS * RingShape<K, T, VE, NV, G, U>::WARP;
     auto kernel = k_attend_ring<K, T, VE, NV, G, U>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static std::atomic<uint64_t> allowed{0};
+    cudaError_t e = allow_smem(kernel, smem, allowed);
     if (e != cudaSuccess) return e;
     P.units_per_row = K == AT_DKV ? P.a.kv_heads : P.a.q_heads / G;
     const int pieces = (P.a.head_dim + VE * NV - 1) / (VE * NV);
@@ -787,7 +788,7 @@ cudaError_t launch_block_reverse(const int32_t* indptr, const int32_t* indices, 
     int64_t blocks = ((int64_t)dst.bound + AT_THREADS / 8 - 1) / (AT_THREADS / 8);
     if (blocks > sm_count() * 32) blocks = sm_count() * 32;
     cudaError_t e = launch_train(k_edge_rows, blocks, AT_THREADS, 0, s, indptr, dst, (int)edges.bound, rows);
-    if (e == cudaSuccess) e = launch_key_sort(indices, nullptr, edges, src.bound, (char*)workspace + 2 * list, keys, rev_edge, s);
+    if (e == cudaSuccess) e = launch_key_sort(indices, nullptr, edges, src.bound, (char*)workspace + 2 * list, keys, rev_edge, nullptr, 0, s);
     if (e == cudaSuccess) e = launch_row_starts(keys, edges, src, rev_indptr, s);
     blocks = ((int64_t)edges.bound + AT_THREADS * 4 - 1) / (AT_THREADS * 4);
     if (blocks > sm_count() * 16) blocks = sm_count() * 16;

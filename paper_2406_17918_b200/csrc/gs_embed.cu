@@ -417,12 +417,12 @@ cudaError_t launch_embedding_grad(const EmbedGrad& g, void* workspace, cudaStrea
     P.order = order;
     P.tile_runs = heads;
     const int in = bytes_of(g.dout_dtype), out = bytes_of(g.grad_dtype);
-    cudaError_t e = cudaMemsetAsync(P.words, 0, 8, s);
+    cudaError_t e = cudaSuccess;
     // the dense table is cleared first: rows without an id stay so
-    if (e == cudaSuccess && !g.rows)
+    if (!g.rows)
         e = g.grad_ld == g.dim ? cudaMemsetAsync(g.grad, 0, (size_t)g.table_rows * g.dim * out, s)
                                : cudaMemset2DAsync(g.grad, (size_t)g.grad_ld * out, 0, (size_t)g.dim * out, (size_t)g.table_rows, s);
-    if (e == cudaSuccess) e = launch_key_sort(g.ids, nullptr, g.n, g.table_rows, ws + l.sort, keys, order, s);
+    if (e == cudaSuccess) e = launch_key_sort(g.ids, nullptr, g.n, g.table_rows, ws + l.sort, keys, order, P.words, 2, s);
     if (e == cudaSuccess && g.rows) {
         const int tiles = (int)(((int64_t)g.n.bound + ES_TILE - 1) / ES_TILE);
         e = launch_train(k_head_counts, (tiles + ES_THREADS / 32 - 1) / (ES_THREADS / 32), ES_THREADS, 0, s, keys, g.n, (uint32_t)g.table_rows, heads);

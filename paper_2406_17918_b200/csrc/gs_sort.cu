@@ -31,6 +31,8 @@ struct KeySort {
     unsigned long long* dst;      // passes before the last: key << 32 | payload
     uint32_t* out_keys;           // last pass
     int32_t* out_payload;
+    int32_t* zero;                // words that the first kernel clears for the caller
+    int zero_words;
 };
 
 __device__ __forceinline__ int count_of(const Count& c) {
@@ -82,6 +84,8 @@ __global__ void __launch_bounds__(KS_THREADS) k_key_count(KeySort P, int first) 
     __shared__ int h[KS_MAX_BINS];
     chain_wait();
     const int n = count_of(P.n), bins = 1 << P.bits;
+    if (first && blockIdx.x == 0)
+        for (int i = threadIdx.x; i < P.zero_words; i += KS_THREADS) P.zero[i] = 0;
     for (int tile = blockIdx.x; tile < P.tiles; tile += gridDim.x) {
         __syncthreads();
         for (int i = threadIdx.x; i < bins; i += KS_THREADS) h[i] = 0;
@@ -241,6 +245,7 @@ __global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P) 
     __shared__ int warp_sums[33];
     chain_wait();
     const int n = count_of(P.n);
+    for (int i = threadIdx.x; i < P.zero_words; i += KS_SMALL_THREADS) P.zero[i] = 0;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     unsigned long long key[R];
     int rank[R];
@@ -293,7 +298,8 @@ size_t key_sort_bytes(int64_t n) {
 }
 
 template <int ROUNDS> static cudaError_t run_pass(const KeySort& P, bool first, bool last, cudaStream_t s) {
-    cudaError_t e = cudaFuncSetAttribute(k_key_scatter<ROUNDS>, cudaFuncAttributeMaxDynamicSharedMemorySize, scatter_smem<ROUNDS>());
+    static std::atomic<uint64_t> allowed{0};
+    cudaError_t e = allow_smem(k_key_scatter<ROUNDS>, scatter_smem<ROUNDS>(), allowed);
     if (e == cudaSuccess) e = launch_train(k_key_count<ROUNDS>, P.tiles, KS_THREADS, 0, s, P, (int)first);
     if (e == cudaSuccess) e = launch_train(k_key_scan, ((1 << P.bits) + 7) / 8, 256, 0, s, P);
     if (e == cudaSuccess) e = launch_train(k_key_scatter<ROUNDS>, P.tiles, KS_THREADS, scatter_smem<ROUNDS>(), s, P, (int)first, (int)last);
@@ -301,7 +307,7 @@ template <int ROUNDS> static cudaError_t run_pass(const KeySort& P, bool first, 
 }
 
 cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n, int64_t key_limit, void* workspace,
-                            uint32_t* out_keys, int32_t* out_payload, cudaStream_t s) {
+                            uint32_t* out_keys, int32_t* out_payload, int32_t* zero, int zero_words, cudaStream_t s) {
     KeySort P{};
     P.keys = keys;
     P.payload = payload;
@@ -309,12 +315,15 @@ cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n
     P.key_limit = (uint32_t)key_limit;
     P.out_keys = out_keys;
     P.out_payload = out_payload;
+    P.zero = zero;
+    P.zero_words = zero_words;
     int bits = 1;
     while (bits < 32 && (key_limit >> bits)) ++bits;
     if (n.bound <= KS_SMALL) {
         constexpr int smem = KS_SMALL * 8 + (KS_SMALL_THREADS / 32) * 256 * 4;
         P.passes = (bits + 7) / 8;
-        const cudaError_t e = cudaFuncSetAttribute(k_key_sort_small, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        static std::atomic<uint64_t> allowed{0};
+        const cudaError_t e = allow_smem(k_key_sort_small, smem, allowed);
         if (e != cudaSuccess) return e;
         return launch_train(k_key_sort_small, 1, KS_SMALL_THREADS, smem, s, P);
     }

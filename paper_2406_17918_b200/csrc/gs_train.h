@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "gs_internal.h"
 
 namespace gs {
@@ -32,11 +34,24 @@ inline cudaError_t launch_train(void (*kernel)(KArgs...), int64_t grid, int bloc
     return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
 }
 
+// Allows `kernel` that much dynamic shared memory, once per device.
+template <typename F> inline cudaError_t allow_smem(F* kernel, int bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev >= 0 && dev < 64 ? (uint64_t)1 << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
 // ---- stable sort of (key, payload) pairs by key: ascending keys, equal keys in input order ----
 size_t key_sort_bytes(int64_t n_bound);
 // Keys outside [0, key_limit) take the value key_limit and end behind all others.  payload NULL: the position.
+// `zero_words` int32 words at `zero` (or none) are cleared on the way, before the last kernel of the sort.
 cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n, int64_t key_limit, void* workspace,
-                            uint32_t* out_keys, int32_t* out_payload, cudaStream_t s);
+                            uint32_t* out_keys, int32_t* out_payload, int32_t* zero, int zero_words, cudaStream_t s);
 // starts[r] = number of sorted keys < r, r = 0 .. rows (rows from the device if rows.d_n is set).
 cudaError_t launch_row_starts(const uint32_t* keys, Count n, Count rows, int32_t* starts, cudaStream_t s);
 

@@ -191,13 +191,14 @@ __global__ void __launch_bounds__(XS_THREADS) k_xent_simt(const __grid_constant_
 
 // lse and loss of every row from the runs' statistics: a warp per row, its lanes over the entries.
 __global__ void __launch_bounds__(256) k_xent_finish(Xent a, Runs runs, int tile, int per, const float2* __restrict__ stats, const float* __restrict__ picked) {
+    chain_wait();
     const int lane = threadIdx.x & 31;
     for (int64_t n = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; n < a.rows; n += (int64_t)gridDim.x * 8) {
         const int64_t i = n / tile;
         const int64_t c0 = runs.run_of(i * runs.tiles_y), c1 = runs.run_of((i + 1) * runs.tiles_y - 1);
         float m = -INFINITY, l = 0.f;
         for (int64_t c = (c0 + i) * per + lane; c < (c1 + i + 1) * per; c += 32) {      // `per` entries of a run
-            const float2 s = stats[c * tile + n % tile];
+            const float2 s = __ldcg(stats + c * tile + n % tile);
             const float top = fmaxf(m, s.x), ref = top == -INFINITY ? 0.f : top;
             l = l * xe_exp2(m - ref) + s.y * xe_exp2(s.x - ref);
             m = top;
@@ -213,7 +214,7 @@ __global__ void __launch_bounds__(256) k_xent_finish(Xent a, Runs runs, int tile
             const bool valid = lab >= 0 && lab < a.vocab;
             const float log2l = log2f(l);
             a.lse_out[n] = (m + log2l) * XE_LN2;
-            a.loss[n] = valid ? ((m - picked[n]) + log2l) * XE_LN2 : 0.f;
+            a.loss[n] = valid ? ((m - __ldcg(picked + n)) + log2l) * XE_LN2 : 0.f;
         }
     }
 }
@@ -221,6 +222,7 @@ __global__ void __launch_bounds__(256) k_xent_finish(Xent a, Runs runs, int tile
 // Rows of tiles that several runs share: their partial sums in order.  The run before the first that starts inside, c,
 // left slot 2c - 1, the runs c, c + 1, .. up to the row's end 2c, 2c + 2, ..
 template <XentMode M> __global__ void __launch_bounds__(256) k_xent_join(Xent a, const __grid_constant__ JoinList list, int tile, int pitch, const float* __restrict__ partial) {
+    chain_wait();
     const JoinList::Entry j = list.e[blockIdx.x];
     const int64_t nx = M == XE_DHIDDEN ? a.rows : a.vocab, x0 = (int64_t)j.row * tile, step = (int64_t)tile * pitch;
     const int rows = nx - x0 < tile ? (int)(nx - x0) : tile;
@@ -266,7 +268,16 @@ template <XentMode M> static void run_join(const Xent& a, const Runs& runs, int 
     // few shared rows: spread each over many blocks
     int64_t by = (tile * pitch + 255) / 256, few = sm_count() * 8 / n + 1;
     if (by > few) by = few;
-    k_xent_join<M><<<dim3((unsigned)n, (unsigned)by), 256, 0, s>>>(a, list, tile, pitch, partial);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)n, (unsigned)by);
+    cfg.blockDim = dim3(256);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    cudaLaunchKernelEx(&cfg, k_xent_join<M>, a, list, tile, pitch, partial);
     count_launches(1);
 }
 
@@ -284,9 +295,7 @@ cudaError_t launch_xent_forward(const Xent& a, void* workspace, cudaStream_t s) 
         const float* picked;
         const cudaError_t e = launch_xent_tc_forward(a, workspace, &runs, &stats, &picked, s);
         if (e != cudaSuccess) return e;
-        k_xent_finish<<<(int)finish, 256, 0, s>>>(a, runs, XENT_TC_TILE, XENT_TC_STATS, stats, picked);
-        count_launches(1);
-        return cudaGetLastError();
+        return launch_train(k_xent_finish, finish, 256, 0, s, a, runs, XENT_TC_TILE, XENT_TC_STATS, stats, picked);
     }
     XentSimt P{};
     P.a = a;

@@ -214,6 +214,7 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 2) tc::tmem_alloc(tc::smem_addr(&s_tmem), 512);
+    chain_wait();                                          // what is set up above may overlap the kernel before
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
@@ -618,6 +619,7 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
 
 // What the dw kernel needs of the hidden rows, tile by tile (rows behind the last have no gradient).
 __global__ void __launch_bounds__(XT) k_xent_row_info(Xent a, float* __restrict__ info) {
+    chain_wait();
     for (int64_t t = blockIdx.x; t * XT < a.rows; t += gridDim.x) {
         const int64_t n = t * XT + threadIdx.x;
         const int lab = n < a.rows ? a.labels[n] : -1;
@@ -632,6 +634,7 @@ __global__ void __launch_bounds__(XT) k_xent_row_info(Xent a, float* __restrict_
 // Rows repacked to a pitch that tile loads can address (a multiple of 16 bytes): 8 columns per thread, read in units of U.
 template <typename U> __global__ void __launch_bounds__(256) k_xent_pack(const bf16* __restrict__ src, int64_t ld, int64_t rows, int dim, int pitch, bf16* __restrict__ dst) {
     constexpr int PER = sizeof(U) / 2;
+    chain_wait();
     const int per_row = pitch / 8, rows_per_block = 256 / per_row;
     const int r_in = threadIdx.x / per_row, c = (threadIdx.x - r_in * per_row) * 8;
     if (r_in >= rows_per_block) return;
@@ -718,23 +721,28 @@ struct Operands {
     const void* table;
     int64_t hidden_ld, table_ld;
     char* rest;
+    CUtensorMap hidden_map, table_map;
 };
 
 static cudaError_t prepare_operands(const Xent& a, void* workspace, Operands* o, cudaStream_t s) {
     const TcLayout l = tc_layout(a);
     char* ws = (char*)workspace;
-    *o = Operands{a.hidden, a.table, a.hidden_ld, a.table_ld, ws + l.rest};
+    o->hidden = a.hidden;
+    o->table = a.table;
+    o->hidden_ld = a.hidden_ld;
+    o->table_ld = a.table_ld;
+    o->rest = ws + l.rest;
+    cudaError_t e = cudaSuccess;
     const int pitch = packed_pitch(a.dim);
     auto pack = [&](const void* src, int64_t ld, int64_t rows, char* dst) {
         const int rows_per_block = 256 / (pitch / 8);
         int64_t blocks = (rows + rows_per_block - 1) / rows_per_block;
         if (blocks > sm_count() * 32) blocks = sm_count() * 32;
         const uint64_t all = (uint64_t)(uintptr_t)src | (uint64_t)ld * 2 | (uint64_t)a.dim * 2;
-        const int grid = (int)limit_grid(blocks);
-        if (all % 8 == 0) k_xent_pack<uint2><<<grid, 256, 0, s>>>((const bf16*)src, ld, rows, a.dim, pitch, (bf16*)dst);
-        else if (all % 4 == 0) k_xent_pack<uint32_t><<<grid, 256, 0, s>>>((const bf16*)src, ld, rows, a.dim, pitch, (bf16*)dst);
-        else k_xent_pack<uint16_t><<<grid, 256, 0, s>>>((const bf16*)src, ld, rows, a.dim, pitch, (bf16*)dst);
-        count_launches(1);
+        if (e != cudaSuccess) return;
+        if (all % 8 == 0) e = launch_train(k_xent_pack<uint2>, blocks, 256, 0, s, (const bf16*)src, ld, rows, a.dim, pitch, (bf16*)dst);
+        else if (all % 4 == 0) e = launch_train(k_xent_pack<uint32_t>, blocks, 256, 0, s, (const bf16*)src, ld, rows, a.dim, pitch, (bf16*)dst);
+        else e = launch_train(k_xent_pack<uint16_t>, blocks, 256, 0, s, (const bf16*)src, ld, rows, a.dim, pitch, (bf16*)dst);
     };
     if (!tile_rows_ok(a.hidden, a.hidden_ld)) {
         pack(a.hidden, a.hidden_ld, a.rows, ws + l.hidden);
@@ -746,7 +754,9 @@ static cudaError_t prepare_operands(const Xent& a, void* workspace, Operands* o,
         o->table = ws + l.table;
         o->table_ld = pitch;
     }
-    return cudaGetLastError();
+    if (e == cudaSuccess) e = row_map(&o->hidden_map, o->hidden, a.rows, a.dim, o->hidden_ld);
+    if (e == cudaSuccess) e = row_map(&o->table_map, o->table, a.vocab, a.dim, o->table_ld);
+    return e;
 }
 
 template <int M> static cudaError_t run_tc(const Xent& a, const Operands& o, XentTc& P, cudaStream_t s) {
@@ -781,19 +791,14 @@ template <int M> static cudaError_t run_tc(const Xent& a, const Operands& o, Xen
     }
     P.stages = ((M == TC_FORWARD ? 192 : 216) * 1024 - staging) / (tile + (M == TC_DTABLE ? XT_INFO : 0)) - P.xbufs;
     if (P.stages > XT_MAX_STAGES) P.stages = XT_MAX_STAGES;
-    CUtensorMap hm, tm;
-    cudaError_t e = row_map(&hm, o.hidden, a.rows, a.dim, o.hidden_ld);
-    if (e == cudaSuccess) e = row_map(&tm, o.table, a.vocab, a.dim, o.table_ld);
-    if (e != cudaSuccess) return e;
     // at least 120 KB, so that an SM holds one block: a block takes all of the tensor memory
     int smem = (P.xbufs + P.stages) * tile + 1024 + (M == TC_DTABLE ? P.stages * XT_INFO : 0) + staging;
     if (smem < (120 << 10)) smem = 120 << 10;
     auto kernel = chunks == 1 ? k_xent_tc<M, 1> : (chunks == 2 ? k_xent_tc<M, 2> : (chunks == 3 ? k_xent_tc<M, 3> : k_xent_tc<M, 4>));
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static std::atomic<uint64_t> allowed[4];
+    const cudaError_t e = allow_smem(kernel, 226 << 10, allowed[chunks - 1]);
     if (e != cudaSuccess) return e;
-    kernel<<<(int)limit_grid(P.runs.parts), XT_THREADS, smem, s>>>(P, ON_X ? hm : tm, ON_X ? tm : hm);
-    count_launches(1);
-    return cudaGetLastError();
+    return launch_train(kernel, P.runs.parts, XT_THREADS, smem, s, P, ON_X ? o.hidden_map : o.table_map, ON_X ? o.table_map : o.hidden_map);
 }
 
 cudaError_t launch_xent_tc_forward(const Xent& a, void* workspace, Runs* runs, const float2** stats, const float** picked, cudaStream_t s) {
@@ -819,9 +824,8 @@ cudaError_t launch_xent_tc_backward(const Xent& a, void* workspace, cudaStream_t
     P.partial = (float*)o.rest;
     float* row_info = (float*)(o.rest + align_up((size_t)2 * sm_count() * XT * ((a.dim + 15) / 16 * 16) * 4, 256));
     P.row_info = row_info;
-    k_xent_row_info<<<(int)limit_grid((a.rows + XT - 1) / XT), XT, 0, s>>>(a, row_info);
-    count_launches(1);
-    e = run_tc<TC_DHIDDEN>(a, o, P, s);
+    e = launch_train(k_xent_row_info, (a.rows + XT - 1) / XT, XT, 0, s, a, row_info);
+    if (e == cudaSuccess) e = run_tc<TC_DHIDDEN>(a, o, P, s);
     if (e != cudaSuccess) return e;
     e = launch_xent_join(a, true, P.runs, XT, P.on, P.partial, s);
     if (e != cudaSuccess) return e;
