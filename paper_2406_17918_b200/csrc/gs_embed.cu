@@ -111,6 +111,7 @@ struct RunSum {
     const int32_t* order;           // their positions
     const int32_t* tile_runs;       // sparse: runs before each tile of the list
     int tl;                         // lanes per row (a power of two)
+    int seg;                        // sorted entries per group, at most tl
     int32_t* words;                 // [0] chunks, [1] long runs
     int2* items;                    // chunk -> entries [x, y)
     int4* longs;                    // long run -> (row of the gradient, first chunk, chunks, -)
@@ -163,21 +164,25 @@ __device__ __forceinline__ void add_entries(const RunSum& P, int b, int e, int64
     }
 }
 
-// The sorted entries, in equal pieces: a group of tl lanes takes tl neighbouring entries, whose rows are all in flight
+// The sorted entries, in equal pieces: a group of tl lanes takes `seg` neighbouring entries, whose rows are all in flight
 // whatever runs they belong to, and owns the runs whose heads it meets (the last one beyond its own entries, if it
 // continues).  Work by entries, not by rows: rows of the table are many and mostly empty, and the frequent ids lie together.
+// A block takes ES_THREADS / tl * seg entries: all of a tile of ES_THREADS when seg = tl, fewer of it where there are too
+// few entries to fill the device that way.
 template <typename Tin, typename Tout, int VE, bool SPARSE>
 __global__ void __launch_bounds__(ES_THREADS, 4) k_run_sum(RunSum P) {
     __shared__ int warp_sums[33];
+    __shared__ int s_key[ES_THREADS], s_pos[ES_THREADS], s_row[ES_THREADS];
+    __shared__ unsigned char s_flag[ES_THREADS];            // 1: head, 2: of a listed run, 4: an entry with an id
     chain_wait();
     const int n = list_length(P.g.n), bound = P.g.n.bound;
     const uint32_t limit = (uint32_t)P.g.table_rows;
     const int tiles = (bound + ES_TILE - 1) / ES_TILE;
-    const int lane = threadIdx.x & 31, tl = P.tl, t = lane & (tl - 1), base = lane & ~(tl - 1);
+    const int tl = P.tl, t = threadIdx.x & (tl - 1), seg = P.seg, parts = tl / seg;      // blocks per tile
     const int units = P.g.dim / VE;
-    const uint32_t group = tl == 32 ? FULL : ((1u << tl) - 1u) << base;
     const Tin* dout = (const Tin*)P.g.dout;
-    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    for (int64_t bt = blockIdx.x; bt < (int64_t)tiles * parts; bt += gridDim.x) {
+        const int tile = (int)(bt / parts), part = (int)(bt - (int64_t)tile * parts);
         const int before = SPARSE ? __ldcg(P.tile_runs + tile) : 0, runs = SPARSE ? __ldcg(P.g.d_num_rows) : 0;
         {
             const int64_t e64 = (int64_t)tile * ES_TILE + threadIdx.x;
@@ -194,67 +199,72 @@ __global__ void __launch_bounds__(ES_THREADS, 4) k_run_sum(RunSum P) {
             if (SPARSE) {
                 int total;
                 row = before + block_exclusive_scan<ES_THREADS>(head ? 1 : 0, warp_sums, &total);
-                if (head) P.g.rows[row] = (int32_t)key;
-                if (e >= runs && e < bound) P.g.rows[e] = -1;
+                if (part == 0) {
+                    if (head) P.g.rows[row] = (int32_t)key;
+                    if (e >= runs && e < bound) P.g.rows[e] = -1;
+                }
             }
-            bool is_long = false;
-            if (head && e + ES_CHUNK < n && __ldcg(P.keys + e + ES_CHUNK) == key) {
-                is_long = true;
-                list_run(P, row, e, run_end(P.keys, e, n, key));
-            }
-            const uint32_t heads = __ballot_sync(FULL, head) & group, longs = __ballot_sync(FULL, is_long), valid = __ballot_sync(FULL, key < limit);
-            for (int u = t; u < units + t; u += tl) {                  // the same number of turns for all lanes
-                const bool on = u < units;
-                const int64_t col = (int64_t)u * VE;
-                float acc[VE];
+            const bool listed = head && e + ES_CHUNK < n && __ldcg(P.keys + e + ES_CHUNK) == key;
+            if (listed && part == 0) list_run(P, row, e, run_end(P.keys, e, n, key));
+            __syncthreads();
+            s_key[threadIdx.x] = (int)key;
+            s_pos[threadIdx.x] = pos;
+            s_row[threadIdx.x] = row;
+            s_flag[threadIdx.x] = (head ? 1 : 0) | (listed ? 2 : 0) | (key < limit ? 4 : 0);
+            __syncthreads();
+        }
+        // this group's entries of the tile: seg of them, the parts of a tile interleaved
+        const int first = (part * (ES_THREADS / tl) + threadIdx.x / tl) * seg;
+        for (int u = t; u < units; u += tl) {
+            const int64_t col = (int64_t)u * VE;
+            float acc[VE];
 #pragma unroll
-                for (int i = 0; i < VE; ++i) acc[i] = 0.f;
-                int open = -1;                                         // lane of the head of the run being summed
-                auto flush = [&](int row_of) {
-                    if (!on) return;
+            for (int i = 0; i < VE; ++i) acc[i] = 0.f;
+            int open = -1;                                             // entry of the head of the run being summed
+            auto flush = [&]() {
 #pragma unroll
-                    for (int i = 0; i < VE; ++i) acc[i] *= P.g.scale;
-                    store_vec<Tout, VE>((Tout*)P.g.grad + (int64_t)row_of * P.g.grad_ld + col, acc);
-                };
-                for (int j0 = 0; j0 < tl; j0 += ES_UNROLL) {
-                    Raw<Tin, VE> v[ES_UNROLL];
+                for (int i = 0; i < VE; ++i) acc[i] *= P.g.scale;
+                store_vec<Tout, VE>((Tout*)P.g.grad + (int64_t)s_row[open] * P.g.grad_ld + col, acc);
+                open = -1;
+            };
+            bool skip = true;                                          // entries of a run met before, or listed
+            for (int j0 = 0; j0 < seg; j0 += ES_UNROLL) {
+                Raw<Tin, VE> v[ES_UNROLL];
+                bool mine = !skip;
 #pragma unroll
-                    for (int j = 0; j < ES_UNROLL; ++j) {
-                        const int l = base + ((j0 + j) & (tl - 1)), p = __shfl_sync(FULL, pos, l);
-                        const uint32_t upto = heads & (0xFFFFFFFFu >> (31 - l));      // heads of this group up to entry l
-                        const bool want = on && j0 + j < tl && ((valid >> l) & 1) && upto && !((longs >> (31 - __clz(upto))) & 1);
-                        v[j] = want ? load_raw_stream<Tin, VE>(dout + (int64_t)p * P.g.dout_ld + col) : zero_raw<Tin, VE>();
-                    }
+                for (int j = 0; j < ES_UNROLL; ++j) {
+                    const int l = first + j0 + j, flag = j0 + j < seg ? s_flag[l] : 0;
+                    if (flag & 1) mine = !(flag & 2);
+                    v[j] = mine && (flag & 4) ? load_raw_stream<Tin, VE>(dout + (int64_t)s_pos[l] * P.g.dout_ld + col) : zero_raw<Tin, VE>();
+                }
 #pragma unroll
-                    for (int j = 0; j < ES_UNROLL; ++j) {
-                        const int l = base + ((j0 + j) & (tl - 1));
-                        const bool starts = j0 + j < tl && ((heads >> l) & 1), ends = j0 + j < tl && !((valid >> l) & 1);
-                        const int row_of = __shfl_sync(FULL, row, open < 0 ? base : open);
-                        if ((starts || ends) && open >= 0) flush(row_of);
-                        float x[VE];
-                        unpack<Tin, VE>(v[j], x);
+                for (int j = 0; j < ES_UNROLL; ++j) {
+                    const int l = first + j0 + j, flag = j0 + j < seg ? s_flag[l] : 4;
+                    const bool starts = flag & 1;
+                    if ((starts || !(flag & 4)) && open >= 0) flush();
+                    float x[VE];
+                    unpack<Tin, VE>(v[j], x);
 #pragma unroll
-                        for (int i = 0; i < VE; ++i) acc[i] = starts ? x[i] : acc[i] + x[i];
-                        if (starts) open = (longs >> l) & 1 ? -1 : l;
-                        if (ends) open = -1;
+                    for (int i = 0; i < VE; ++i) acc[i] = starts ? x[i] : acc[i] + x[i];
+                    if (starts) {
+                        skip = flag & 2;
+                        open = skip ? -1 : l;
                     }
                 }
-                const int row_of = __shfl_sync(FULL, row, open < 0 ? base : open);
-                const uint32_t open_key = __shfl_sync(FULL, key, open < 0 ? base : open);
-                if (open >= 0) {
-                    const int from = e - t + tl;                       // behind the group's entries
-                    int to = from;
-                    while (to < n && to - from < ES_CHUNK && __ldcg(P.keys + to) == open_key) ++to;
-                    if (on && to > from) add_entries<Tin, VE>(P, from, to, col, acc);
-                    flush(row_of);
-                }
-                __syncwarp();
+            }
+            if (open >= 0) {
+                const int from = tile * ES_TILE + first + seg;         // behind the group's entries
+                const uint32_t key = (uint32_t)s_key[open];
+                int to = from;
+                while (to < n && to - from < ES_CHUNK && __ldcg(P.keys + to) == key) ++to;
+                if (to > from) add_entries<Tin, VE>(P, from, to, col, acc);
+                flush();
             }
         }
         if (SPARSE) {                                                  // rows behind the last run
-            const int64_t first = (int64_t)tile * ES_TILE, end = first + ES_TILE < bound ? first + ES_TILE : bound;
+            const int64_t f0 = (int64_t)tile * ES_TILE, end = f0 + ES_TILE < bound ? f0 + ES_TILE : bound;
             const float zero[VE] = {};
-            for (int64_t r = (first > runs ? first : runs) + threadIdx.x / tl; r < end; r += ES_THREADS / tl)
+            for (int64_t r = (f0 > runs ? f0 : runs) + part * (ES_THREADS / tl) + threadIdx.x / tl; r < end; r += (ES_THREADS / tl) * parts)
                 for (int u = t; u < units; u += tl) store_vec<Tout, VE>((Tout*)P.g.grad + r * P.g.grad_ld + (int64_t)u * VE, zero);
         }
     }
@@ -383,7 +393,12 @@ template <typename Tin, typename Tout, int VE> static cudaError_t run_sum_t(RunS
     const int units = P.g.dim / VE;
     P.tl = 1;
     while (P.tl < 32 && P.tl < units) P.tl *= 2;
-    const int64_t tiles = ((int64_t)P.g.n.bound + ES_TILE - 1) / ES_TILE;
+    int64_t tiles = ((int64_t)P.g.n.bound + ES_TILE - 1) / ES_TILE;
+    P.seg = P.tl;
+    while (P.seg > 4 && tiles < sm_count() * 4) {        // four blocks per SM, as long as a group keeps four entries
+        P.seg /= 2;
+        tiles *= 2;
+    }
     cudaError_t e = P.g.rows ? launch_train(k_run_sum<Tin, Tout, VE, true>, tiles, ES_THREADS, 0, s, P)
                              : launch_train(k_run_sum<Tin, Tout, VE, false>, tiles, ES_THREADS, 0, s, P);
     if (P.g.n.bound <= ES_CHUNK || e != cudaSuccess) return e;           // no run can be longer than a chunk
@@ -419,10 +434,13 @@ cudaError_t launch_embedding_grad(const EmbedGrad& g, void* workspace, cudaStrea
     const int in = bytes_of(g.dout_dtype), out = bytes_of(g.grad_dtype);
     cudaError_t e = cudaSuccess;
     // the dense table is cleared first: rows without an id stay so
-    if (!g.rows)
-        e = g.grad_ld == g.dim ? cudaMemsetAsync(g.grad, 0, (size_t)g.table_rows * g.dim * out, s)
-                               : cudaMemset2DAsync(g.grad, (size_t)g.grad_ld * out, 0, (size_t)g.dim * out, (size_t)g.table_rows, s);
-    if (e == cudaSuccess) e = launch_key_sort(g.ids, nullptr, g.n, g.table_rows, ws + l.sort, keys, order, P.words, 2, s);
+    Fill fill{};
+    if (!g.rows) {
+        const size_t bytes = (size_t)g.table_rows * g.dim * out;
+        if (g.grad_ld == g.dim && (uintptr_t)g.grad % 16 == 0 && bytes % 16 == 0) fill = Fill{(uint4*)g.grad, (int64_t)(bytes / 16)};
+        else e = cudaMemset2DAsync(g.grad, (size_t)g.grad_ld * out, 0, (size_t)g.dim * out, (size_t)g.table_rows, s);
+    }
+    if (e == cudaSuccess) e = launch_key_sort(g.ids, nullptr, g.n, g.table_rows, ws + l.sort, keys, order, P.words, 2, fill, s);
     if (e == cudaSuccess && g.rows) {
         const int tiles = (int)(((int64_t)g.n.bound + ES_TILE - 1) / ES_TILE);
         e = launch_train(k_head_counts, (tiles + ES_THREADS / 32 - 1) / (ES_THREADS / 32), ES_THREADS, 0, s, keys, g.n, (uint32_t)g.table_rows, heads);

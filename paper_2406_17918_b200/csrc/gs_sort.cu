@@ -5,6 +5,8 @@
 // schedule.  2.03 M pairs of 26 bits: 95 us.  (One kernel per 8-bit digit, tiles looking back over their predecessors'
 // counts: 150 us, the polls of the waiting tiles held up the others; digits of 11 bits and tiles of 8192: 138 us, one
 // block per SM.)
+#include <cooperative_groups.h>
+
 #include "gs_device.cuh"
 #include "gs_train.h"
 
@@ -17,6 +19,9 @@ constexpr int KS_ROUNDS_SMALL = 4, KS_ROUNDS_LARGE = 16;   // pairs per thread o
 constexpr int64_t KS_LARGE = (int64_t)1 << 19;             // from here on there are tiles enough for the large ones
 constexpr int KS_SMALL = 4096;               // up to here one block sorts everything in shared memory
 constexpr int KS_SMALL_THREADS = 1024;
+constexpr int KC_BLOCKS = 8;                 // up to KC_MAX pairs a cluster of blocks sorts in its shared memory
+constexpr int KC_ROUNDS = 8, KC_TILE = 1024 * KC_ROUNDS, KC_MAX = KC_BLOCKS * KC_TILE;
+constexpr int KC_BITS = 9, KC_BINS = 1 << KC_BITS;
 
 struct KeySort {
     const int32_t* keys;
@@ -236,14 +241,24 @@ __global__ void __launch_bounds__(KS_THREADS, ROUNDS <= 4 ? 5 : 3) k_key_scatter
     }
 }
 
-// All passes in one block.
-__global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P) {
+// The rest of the grid clears memory for the caller meanwhile: a sort of so few pairs keeps a few SMs busy.
+__device__ __forceinline__ void fill_zero(const Fill& f, int block, int blocks) {
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < f.pieces; i += (int64_t)blocks * blockDim.x) __stcs(f.p + i, zero);
+}
+
+// All passes in one block; the others clear memory.
+__global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P, Fill f) {
     constexpr int R = KS_SMALL / KS_SMALL_THREADS, W = KS_SMALL_THREADS / 32, BINS = 256;
     extern __shared__ unsigned long long pairs[];                    // [KS_SMALL], then cnt[W][BINS]
     int* cnt = reinterpret_cast<int*>(pairs + KS_SMALL);
     __shared__ int start[BINS];
     __shared__ int warp_sums[33];
     chain_wait();
+    if (blockIdx.x > 0) {
+        fill_zero(f, blockIdx.x - 1, gridDim.x - 1);
+        return;
+    }
     const int n = count_of(P.n);
     for (int i = threadIdx.x; i < P.zero_words; i += KS_SMALL_THREADS) P.zero[i] = 0;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
@@ -290,6 +305,88 @@ __global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P) 
     }
 }
 
+__global__ void __launch_bounds__(KS_SMALL_THREADS) k_fill(Fill f) {
+    chain_wait();
+    fill_zero(f, blockIdx.x, gridDim.x);
+}
+
+// All passes in one cluster: every block ranks its share, the blocks read one another's digit counts, and every pair goes
+// straight to its place in the shared memory of the block that holds it next.
+__global__ void __cluster_dims__(KC_BLOCKS, 1, 1) __launch_bounds__(1024) k_key_sort_cluster(KeySort P, Fill f) {
+    namespace cg = cooperative_groups;
+    constexpr int W = 32;
+    extern __shared__ unsigned long long pairs[];                    // two buffers of KC_TILE, then the counters
+    uint16_t* cnt = reinterpret_cast<uint16_t*>(pairs + 2 * KC_TILE);           // [W][KC_BINS]
+    int* totals = reinterpret_cast<int*>(cnt + W * KC_BINS);         // this block's pairs per digit
+    int* place = totals + KC_BINS;                                   // first place of this block's pairs of a digit
+    __shared__ int warp_sums[33];
+    chain_wait();
+    if (blockIdx.x >= KC_BLOCKS) {                                   // whole clusters
+        fill_zero(f, blockIdx.x - KC_BLOCKS, gridDim.x - KC_BLOCKS);
+        return;
+    }
+    cg::cluster_group cluster = cg::this_cluster();
+    const int n = count_of(P.n), me = blockIdx.x, bins = 1 << P.bits;
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    if (me == 0)
+        for (int i = threadIdx.x; i < P.zero_words; i += 1024) P.zero[i] = 0;
+    unsigned long long key[KC_ROUNDS];
+    int rank[KC_ROUNDS];
+#pragma unroll
+    for (int r = 0; r < KC_ROUNDS; ++r) {
+        const int i = me * KC_TILE + wid * (KC_ROUNDS * 32) + r * 32 + lane;
+        key[r] = i < n ? first_word(P, i) : ~0ull;                   // padding sorts last, behind position n
+    }
+    for (int p = 0; p < P.passes; ++p) {
+        const int shift = 32 + P.bits * p;
+        unsigned long long* to = pairs + (p & 1) * KC_TILE;
+        for (int i = threadIdx.x; i < W * KC_BINS / 2; i += 1024) reinterpret_cast<uint32_t*>(cnt)[i] = 0;
+        __syncthreads();
+        rank_rounds(key, shift, P.bits, cnt + wid * KC_BINS, rank);
+        __syncthreads();
+        if (threadIdx.x < bins) {
+            int sum = 0;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const int c = cnt[w * KC_BINS + threadIdx.x];
+                cnt[w * KC_BINS + threadIdx.x] = (uint16_t)sum;
+                sum += c;
+            }
+            totals[threadIdx.x] = sum;
+        }
+        cluster.sync();                                              // the counts are there; the last pass's pairs are read
+        int before = 0, all = 0, total;
+        if (threadIdx.x < bins) {
+#pragma unroll
+            for (int c = 0; c < KC_BLOCKS; ++c) {
+                const int t = cluster.map_shared_rank(totals, c)[threadIdx.x];
+                if (c < me) before += t;
+                all += t;
+            }
+        }
+        const int start = block_exclusive_scan<1024>(all, warp_sums, &total);
+        if (threadIdx.x < bins) place[threadIdx.x] = start + before;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < KC_ROUNDS; ++r) {
+            const uint32_t d = (uint32_t)(key[r] >> shift) & (uint32_t)(bins - 1);
+            const int at = place[d] + cnt[wid * KC_BINS + d] + rank[r];
+            cluster.map_shared_rank(to, at / KC_TILE)[at % KC_TILE] = key[r];
+        }
+        cluster.sync();                                              // all pairs have arrived, all counts are read
+#pragma unroll
+        for (int r = 0; r < KC_ROUNDS; ++r) key[r] = to[wid * (KC_ROUNDS * 32) + r * 32 + lane];
+    }
+#pragma unroll
+    for (int r = 0; r < KC_ROUNDS; ++r) {
+        const int i = me * KC_TILE + wid * (KC_ROUNDS * 32) + r * 32 + lane;
+        if (i < n) {
+            P.out_keys[i] = (uint32_t)(key[r] >> 32);
+            P.out_payload[i] = (int32_t)(uint32_t)key[r];
+        }
+    }
+}
+
 static int64_t ks_tile(int64_t n) { return KS_THREADS * (n < KS_LARGE ? KS_ROUNDS_SMALL : KS_ROUNDS_LARGE); }
 static int64_t ks_tiles(int64_t n) { return (n + ks_tile(n) - 1) / ks_tile(n); }
 
@@ -307,7 +404,7 @@ template <int ROUNDS> static cudaError_t run_pass(const KeySort& P, bool first, 
 }
 
 cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n, int64_t key_limit, void* workspace,
-                            uint32_t* out_keys, int32_t* out_payload, int32_t* zero, int zero_words, cudaStream_t s) {
+                            uint32_t* out_keys, int32_t* out_payload, int32_t* zero, int zero_words, Fill fill, cudaStream_t s) {
     KeySort P{};
     P.keys = keys;
     P.payload = payload;
@@ -319,14 +416,30 @@ cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n
     P.zero_words = zero_words;
     int bits = 1;
     while (bits < 32 && (key_limit >> bits)) ++bits;
-    if (n.bound <= KS_SMALL) {
+    // blocks that clear memory beside the sort: enough for all SMs, each with a few kilobytes at least
+    int64_t fillers = fill.pieces / 4096;
+    if (fillers > sm_count() - KC_BLOCKS) fillers = sm_count() - KC_BLOCKS;
+    fillers = (fillers + (fill.pieces > 0)) / KC_BLOCKS * KC_BLOCKS + (fill.pieces > 0 ? KC_BLOCKS : 0);
+    cudaError_t e = cudaSuccess;
+    if (n.bound > KS_SMALL && n.bound <= KC_MAX && limit_grid(KC_BLOCKS + fillers) == KC_BLOCKS + fillers) {
+        constexpr int smem = 2 * KC_TILE * 8 + 32 * KC_BINS * 2 + 2 * KC_BINS * 4;
+        static std::atomic<uint64_t> allowed{0};
+        P.passes = (bits + KC_BITS - 1) / KC_BITS;
+        P.bits = (bits + P.passes - 1) / P.passes;
+        e = allow_smem(k_key_sort_cluster, smem, allowed);
+        if (e != cudaSuccess) return e;
+        return launch_train(k_key_sort_cluster, KC_BLOCKS + fillers, 1024, smem, s, P, fill);
+    }
+    if (n.bound <= KS_SMALL && limit_grid(1 + fillers) == 1 + fillers) {
         constexpr int smem = KS_SMALL * 8 + (KS_SMALL_THREADS / 32) * 256 * 4;
         P.passes = (bits + 7) / 8;
         static std::atomic<uint64_t> allowed{0};
-        const cudaError_t e = allow_smem(k_key_sort_small, smem, allowed);
+        e = allow_smem(k_key_sort_small, smem, allowed);
         if (e != cudaSuccess) return e;
-        return launch_train(k_key_sort_small, 1, KS_SMALL_THREADS, smem, s, P);
+        return launch_train(k_key_sort_small, 1 + fillers, KS_SMALL_THREADS, smem, s, P, fill);
     }
+    if (fill.pieces > 0) e = launch_train(k_fill, fillers, KS_SMALL_THREADS, 0, s, fill);
+    if (e != cudaSuccess) return e;
     P.passes = (bits + KS_MAX_BITS - 1) / KS_MAX_BITS;
     P.bits = (bits + P.passes - 1) / P.passes;
     P.tiles = (int)ks_tiles(n.bound);
@@ -336,7 +449,7 @@ cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n
     unsigned long long* b = (unsigned long long*)(ws + buf);
     int32_t* totals = (int32_t*)(ws + 2 * buf);
     P.counts = (int32_t*)(ws + 2 * buf + align_up((size_t)KS_MAX_PASSES * KS_MAX_BINS * 4, 256));
-    cudaError_t e = cudaMemsetAsync(totals, 0, (size_t)P.passes * KS_MAX_BINS * 4, s);
+    e = cudaMemsetAsync(totals, 0, (size_t)P.passes * KS_MAX_BINS * 4, s);
     for (int p = 0; p < P.passes && e == cudaSuccess; ++p) {
         P.shift = P.bits * p;
         P.totals = totals + KS_MAX_BINS * p;

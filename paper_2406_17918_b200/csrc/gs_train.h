@@ -46,12 +46,18 @@ template <typename F> inline cudaError_t allow_smem(F* kernel, int bytes, std::a
     return e;
 }
 
+// Memory to be cleared, in 16-byte pieces.
+struct Fill {
+    uint4* p;
+    int64_t pieces;
+};
+
 // ---- stable sort of (key, payload) pairs by key: ascending keys, equal keys in input order ----
 size_t key_sort_bytes(int64_t n_bound);
 // Keys outside [0, key_limit) take the value key_limit and end behind all others.  payload NULL: the position.
-// `zero_words` int32 words at `zero` (or none) are cleared on the way, before the last kernel of the sort.
+// `zero_words` int32 words at `zero` (or none) and `fill` are cleared on the way.
 cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n, int64_t key_limit, void* workspace,
-                            uint32_t* out_keys, int32_t* out_payload, int32_t* zero, int zero_words, cudaStream_t s);
+                            uint32_t* out_keys, int32_t* out_payload, int32_t* zero, int zero_words, Fill fill, cudaStream_t s);
 // starts[r] = number of sorted keys < r, r = 0 .. rows (rows from the device if rows.d_n is set).
 cudaError_t launch_row_starts(const uint32_t* keys, Count n, Count rows, int32_t* starts, cudaStream_t s);
 
