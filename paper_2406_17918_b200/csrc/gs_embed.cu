@@ -275,17 +275,42 @@ template <typename Tin, int VE>
 __global__ void __launch_bounds__(ES_THREADS) k_run_chunks(RunSum P) {
     chain_wait();
     const int chunks = __ldcg(P.words);
-    const int units = P.g.dim / VE, t = threadIdx.x & (P.tl - 1);
+    constexpr int CHUNK_UNROLL = 16;
+    const int units = P.g.dim / VE, t = threadIdx.x & (P.tl - 1), base = threadIdx.x & 31 & ~(P.tl - 1);
+    const uint32_t group = P.tl == 32 ? FULL : ((1u << P.tl) - 1u) << base;
     const int per_block = ES_THREADS / P.tl;
     for (int64_t c = (int64_t)blockIdx.x * per_block + threadIdx.x / P.tl; c < chunks; c += (int64_t)gridDim.x * per_block) {
         const int2 it = P.items[c];
-        for (int u = t; u < units; u += P.tl) {
+        const Tin* dout = (const Tin*)P.g.dout;
+        // positions by lane, tl at a time, then as many rows in flight as fit
+        for (int u = t; u < units + t; u += P.tl) {                   // the same number of turns for all lanes of the group
+            const int64_t col = (int64_t)u * VE;
+            const bool on = u < units;
             float acc[VE];
 #pragma unroll
             for (int i = 0; i < VE; ++i) acc[i] = 0.f;
-            add_entries<Tin, VE>(P, it.x, it.y, (int64_t)u * VE, acc);
+            for (int b = it.x; b < it.y; b += P.tl) {
+                const int pos = b + t < it.y ? __ldcg(P.order + b + t) : 0;
+                for (int j0 = 0; j0 < P.tl && b + j0 < it.y; j0 += CHUNK_UNROLL) {
+                    Raw<Tin, VE> v[CHUNK_UNROLL];
 #pragma unroll
-            for (int i = 0; i < VE; ++i) P.partial[c * P.g.dim + u * VE + i] = acc[i];
+                    for (int j = 0; j < CHUNK_UNROLL; ++j) {
+                        const int p = __shfl_sync(group, pos, base + ((j0 + j) & (P.tl - 1)));
+                        v[j] = on && j0 + j < P.tl && b + j0 + j < it.y ? load_raw_stream<Tin, VE>(dout + (int64_t)p * P.g.dout_ld + col) : zero_raw<Tin, VE>();
+                    }
+#pragma unroll
+                    for (int j = 0; j < CHUNK_UNROLL; ++j) {
+                        float x[VE];
+                        unpack<Tin, VE>(v[j], x);
+#pragma unroll
+                        for (int i = 0; i < VE; ++i) acc[i] += x[i];
+                    }
+                }
+            }
+            if (on) {
+#pragma unroll
+                for (int i = 0; i < VE; ++i) P.partial[c * P.g.dim + u * VE + i] = acc[i];
+            }
         }
     }
 }

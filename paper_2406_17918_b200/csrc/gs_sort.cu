@@ -249,9 +249,9 @@ __device__ __forceinline__ void fill_zero(const Fill& f, int block, int blocks) 
 
 // All passes in one block; the others clear memory.
 __global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P, Fill f) {
-    constexpr int R = KS_SMALL / KS_SMALL_THREADS, W = KS_SMALL_THREADS / 32, BINS = 256;
+    constexpr int R = KS_SMALL / KS_SMALL_THREADS, W = KS_SMALL_THREADS / 32, BINS = KC_BINS;
     extern __shared__ unsigned long long pairs[];                    // [KS_SMALL], then cnt[W][BINS]
-    int* cnt = reinterpret_cast<int*>(pairs + KS_SMALL);
+    uint16_t* cnt = reinterpret_cast<uint16_t*>(pairs + KS_SMALL);
     __shared__ int start[BINS];
     __shared__ int warp_sums[33];
     chain_wait();
@@ -269,17 +269,19 @@ __global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P, 
         const int i = wid * (R * 32) + r * 32 + lane;
         key[r] = i < n ? first_word(P, i) : ~0ull;
     }
-    for (int p = 0; p < P.passes; ++p) {                             // digits of 8 bits
-        const int shift = 32 + 8 * p;
-        for (int t = threadIdx.x; t < W * BINS; t += KS_SMALL_THREADS) cnt[t] = 0;
+    const uint32_t mask = (1u << P.bits) - 1u;
+    for (int p = 0; p < P.passes; ++p) {
+        const int shift = 32 + P.bits * p;
+        for (int t = threadIdx.x; t < W * BINS / 2; t += KS_SMALL_THREADS) reinterpret_cast<uint32_t*>(cnt)[t] = 0;
         __syncthreads();
-        rank_rounds(key, shift, 8, cnt + wid * BINS, rank);
+        rank_rounds(key, shift, P.bits, cnt + wid * BINS, rank);
         __syncthreads();
         int sum = 0;
         if (threadIdx.x < BINS) {
+#pragma unroll
             for (int w = 0; w < W; ++w) {
                 const int c = cnt[w * BINS + threadIdx.x];
-                cnt[w * BINS + threadIdx.x] = sum;
+                cnt[w * BINS + threadIdx.x] = (uint16_t)sum;
                 sum += c;
             }
         }
@@ -289,7 +291,7 @@ __global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P, 
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const uint32_t dg = (uint32_t)(key[r] >> shift) & 255u;
+            const uint32_t dg = (uint32_t)(key[r] >> shift) & mask;
             pairs[start[dg] + cnt[wid * BINS + dg] + rank[r]] = key[r];
         }
         __syncthreads();
@@ -354,8 +356,19 @@ __global__ void __cluster_dims__(KC_BLOCKS, 1, 1) __launch_bounds__(1024) k_key_
             }
             totals[threadIdx.x] = sum;
         }
+        // in digit order first, so that neighbouring threads send runs, not single pairs, to the other blocks
+        const int mine = threadIdx.x < bins ? totals[threadIdx.x] : 0;
+        int total;
+        const int local = block_exclusive_scan<1024>(mine, warp_sums, &total);
+        if (threadIdx.x < bins) place[threadIdx.x] = local;
         cluster.sync();                                              // the counts are there; the last pass's pairs are read
-        int before = 0, all = 0, total;
+        unsigned long long* staged = pairs + (~p & 1) * KC_TILE;
+#pragma unroll
+        for (int r = 0; r < KC_ROUNDS; ++r) {
+            const uint32_t d = (uint32_t)(key[r] >> shift) & (uint32_t)(bins - 1);
+            staged[place[d] + cnt[wid * KC_BINS + d] + rank[r]] = key[r];
+        }
+        int before = 0, all = 0;
         if (threadIdx.x < bins) {
 #pragma unroll
             for (int c = 0; c < KC_BLOCKS; ++c) {
@@ -365,13 +378,14 @@ __global__ void __cluster_dims__(KC_BLOCKS, 1, 1) __launch_bounds__(1024) k_key_
             }
         }
         const int start = block_exclusive_scan<1024>(all, warp_sums, &total);
-        if (threadIdx.x < bins) place[threadIdx.x] = start + before;
+        if (threadIdx.x < bins) place[threadIdx.x] = start + before - local;
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < KC_ROUNDS; ++r) {
-            const uint32_t d = (uint32_t)(key[r] >> shift) & (uint32_t)(bins - 1);
-            const int at = place[d] + cnt[wid * KC_BINS + d] + rank[r];
-            cluster.map_shared_rank(to, at / KC_TILE)[at % KC_TILE] = key[r];
+            const int j = r * 1024 + threadIdx.x;
+            const unsigned long long w = staged[j];
+            const int at = place[(uint32_t)(w >> shift) & (uint32_t)(bins - 1)] + j;
+            cluster.map_shared_rank(to, at / KC_TILE)[at % KC_TILE] = w;
         }
         cluster.sync();                                              // all pairs have arrived, all counts are read
 #pragma unroll
@@ -431,8 +445,9 @@ cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n
         return launch_train(k_key_sort_cluster, KC_BLOCKS + fillers, 1024, smem, s, P, fill);
     }
     if (n.bound <= KS_SMALL && limit_grid(1 + fillers) == 1 + fillers) {
-        constexpr int smem = KS_SMALL * 8 + (KS_SMALL_THREADS / 32) * 256 * 4;
-        P.passes = (bits + 7) / 8;
+        constexpr int smem = KS_SMALL * 8 + (KS_SMALL_THREADS / 32) * KC_BINS * 2;
+        P.passes = (bits + KC_BITS - 1) / KC_BITS;
+        P.bits = (bits + P.passes - 1) / P.passes;
         static std::atomic<uint64_t> allowed{0};
         e = allow_smem(k_key_sort_small, smem, allowed);
         if (e != cudaSuccess) return e;
