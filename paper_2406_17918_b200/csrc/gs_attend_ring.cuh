@@ -5,14 +5,14 @@
 // an edge is masked), RING_DEPTH batches ahead, and the column indices one batch earlier still: the gathers of the next
 // batches are in flight across row boundaries while one is computed, they hold no registers, and no barrier is needed
 // because no lane reads another's copies.  Rows' own operands (q; q, dout, out) ride in their first batch.
-// Latency is hidden with 8 to 14 warps per SM, so what is left to save is instructions: pairs of values go through
+// Latency is hidden with 16 to 21 warps per SM, so what is left to save is instructions: pairs of values go through
 // packed 32-bit operations, addresses are one multiply-add per copy, and masked edges take the same path as others.
 #pragma once
 #include "gs_train.cuh"
 
 namespace gs {
 
-constexpr int RING_SLOTS = 3;            // batches of copies per lane
+constexpr int RING_SLOTS = 2;            // batches of copies per lane: 346 us with 2, 390 with 3, 492 with 4 (fewer warps fit)
 constexpr int RING_DEPTH = RING_SLOTS - 1;
 constexpr int RING_WARPS = 2;            // warps per block
 constexpr int RING_ROWS = 64;            // rows whose offsets a warp holds at a time
