@@ -4,12 +4,17 @@
 // and lets tiles of 128 rows of y stream by (TMA, 128-byte swizzle).  Unit u of a block:
 //   S = X Y^T (tcgen05, 128 x 128, f32 in tensor memory)  ->  a softmax warpgroup turns S into statistics, or into
 //   Z = dz in bf16 that overwrites S in tensor memory     ->  O += Z Y, the same shared-memory tile of Y as the second
-// operand, read along its other dimension.  Rounding Z to bf16 costs 2^-9 of each term, about what the gradient's own
-// rounding to bf16 does.  Roles: one thread issues the loads, one the products, two warpgroups (one thread per row of x)
-// take the units alternately, so that S of unit u + 1 is multiplied while unit u is exponentiated.  The products of
-// unit u + 2 may overwrite S of unit u without a wait: they are issued after the product that read Z of unit u.
+// operand, read along its other dimension.  Rounding Z to bf16 costs up to 2^-8 of each term, as the gradient's own
+// rounding to bf16 does; the entries of labels are rounded in two parts (LabelUnits).
+// Roles: one warp issues the loads, one the products S, one the products O, one the copies of finished tiles out; sixteen
+// warps weigh, eight to a unit (a thread per row and 64 columns), the two groups of eight in turn, so that S of one unit is
+// multiplied while another is exponentiated.  S of a later unit may overwrite a Z once the product that read it has ended.
 // Work is cut into equal runs of units, one per SM; a row of tiles shared by runs is joined from f32 partials.
+// Bound: forward by the exponentials (one per logit; special-function and multiply-add units share them), backward by the
+// reads of X, Y and Y again from shared memory beside them.  8,192 x 169,343 x 128: forward 363 us (0.98 PFLOP/s), dh 500 us and
+// dw 580 us (1.4 and 1.2 PFLOP/s over their two products).
 #include <atomic>
+#include <type_traits>
 
 #include "gs_device.cuh"
 #include "gs_tc.cuh"
@@ -87,6 +92,8 @@ struct XentTc {
     float2* stats;               // forward: [parts + tiles_x][XENT_TC_STATS][XT]
     float* picked;
     float* partial;              // backward: [2 parts][XT][on]
+    const uint32_t* marks;       // backward: [tiles of hidden rows][mark_words] bits, the tiles of the table with a label of these rows
+    int mark_words;
     const float* row_info;       // dw: [tiles of hidden rows][3][XT]: -lse (base 2), upstream gradient times scale, label
 };
 constexpr int XT_INFO = 3 * XT * 4;        // bytes of a tile's row_info
@@ -160,6 +167,51 @@ __device__ __forceinline__ float min3(float a, float b, float c) {
     asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+
+// Where a unit holds entries of labels.  p - 1 of a small p lies just under one, where bf16 drops p: up to 2^-9 of the
+// entry, the same way in every row of a label, so that nothing averages it out (512 columns: 0.003 of the table's gradient,
+// where rounding it takes 0.0017).  The 16 columns of Z around such an entry are multiplied in two parts, the second what the
+// rounding took from the first, in the columns of S beside it.  Only those 16: frequent labels lie together in the
+// table, and the block that has them would be the last (8,192 x 169,343 x 128, labels by a squared law: both gradients
+// 1,030 us without the second part, 1,112 with it, 1,238 with all 128 columns of every such unit).
+// The warps that write Z and the one that multiplies it find the places alike: marked units from memory, 32 of a segment at
+// a time, the columns from the labels.
+struct LabelUnits {
+    uint32_t mask;
+    // before unit i of a segment of n units, by all lanes of a warp: whether it is marked
+    template <int M> __device__ bool marked(int i, int64_t xi, int y0, int n, const uint32_t* marks, int words) {
+        if ((i & 31) == 0) {
+            const int y = i + (threadIdx.x & 31);
+            const int64_t hidden = M == TC_DHIDDEN ? xi : y0 + y, table = M == TC_DHIDDEN ? y0 + y : xi;
+            mask = __ballot_sync(FULL, y < n && (__ldcg(marks + hidden * words + (table >> 5)) >> (table & 31) & 1));
+        }
+        return mask >> (i & 31) & 1;
+    }
+    // Bit 4 k: columns 16 k .. 16 k + 15 of tile y hold a label's entry.  dh: the labels of the rows of tile xi; dw: the
+    // columns are the hidden rows whose info lies at `at`.
+    template <int M> static __device__ uint32_t columns(const Xent& a, int64_t xi, int y, uint32_t at) {
+        const int lane = threadIdx.x & 31;
+        uint32_t m = 0;
+        if (M == TC_DHIDDEN) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t x = xi * XT + lane * 4 + j;
+                const int lab = x < a.rows ? __ldg(a.labels + x) : -1;
+                if (lab >= 0 && lab < a.vocab && lab / XT == y) m |= 1u << (lab % XT / 16 * 4);
+            }
+            return __reduce_or_sync(FULL, m);
+        }
+        int lab[4];
+        asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(lab[0]), "=r"(lab[1]), "=r"(lab[2]), "=r"(lab[3]) : "r"(at + (2 * XT + lane * 4) * 4));
+        const int from = (int)(xi * XT);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m |= (uint32_t)(lab[j] - from) < (uint32_t)XT;       // -1 is in no tile
+        m = __ballot_sync(FULL, m);                                                      // four lanes to 16 columns
+        m |= m >> 1;
+        m |= m >> 2;
+        return m & 0x11111111u;
+    }
+};
 
 // CHUNKS: 64-column pieces of a row, known at compile time so that the issuing warp's code is straight.
 template <int M, int CHUNKS>
@@ -322,10 +374,13 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
         uint32_t ph = 0, bph = 0, oph = 1;                 // oph: parity of the use of O before this one; the first use waits for none
         bool ok = true;
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(FULL, tc::mbar_wait(bar, parity, &s_stop)); };
+        LabelUnits units;
         while (ok && seg.next(run, xi, y0, n)) {
             const uint32_t o = tmem + SBUFS * XT + ob * P.on_pitch;
             for (int i = 0; i < n; ++i) {
+                const bool marked = units.marked<M>(i, xi, y0, n, P.marks, P.mark_words);
                 wait(full(st), ph);                        // long complete: the tile must be visible to this thread too
+                const uint32_t labels = marked && ok ? LabelUnits::columns<M>(P.a, xi, y0 + i, info + st * XT_INFO) : 0;
                 wait(p_full(b), bph);
                 if (i == 0 && segs >= P.obufs) wait(o_free(ob), oph);
                 if (!ok) break;
@@ -334,8 +389,13 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                 const uint64_t y = zd + (uint32_t)st * tile_step;
                 if (tc::elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < XT / 16; ++k)      // Z lies in two halves, each over the columns of S it came from
-                        tc::mma_ts(o, z + (k < 4 ? 0 : 32) + k * 8, y + k * 128, inst, i > 0 || k > 0);
+                    for (int k = 0; k < XT / 16; ++k)      // Z lies in four pieces, each over the columns of S it came from
+                        tc::mma_ts(o, z + (k >> 1) * 32 + (k & 1) * 8, y + k * 128, inst, i > 0 || k > 0);
+                    if (labels) {
+#pragma unroll
+                        for (int k = 0; k < XT / 16; ++k)
+                            if (labels >> 4 * k & 1) tc::mma_ts(o, z + (k >> 1) * 32 + 16 + (k & 1) * 8, y + k * 128, inst, true);
+                    }
                     tc::commit(empty(st));
                     tc::commit(z_free(b));
                     if (i + 1 == n) tc::commit(o_full(ob));
@@ -466,7 +526,9 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                 label = lab >= 0 && lab < P.a.vocab ? lab : -1;
                 if (M == TC_DHIDDEN) lse2 = __ldg(P.a.lse + x) * XT_LOG2E;
             }
+            LabelUnits units;
             for (int i = 0; i < n && ok; ++i, mine ^= 1, st = st + 1 == P.stages ? 0 : st + 1, ph ^= st == 0, b = b + 1 == SBUFS ? 0 : b + 1, bph ^= b == 0) {
+                const bool marked = M != TC_FORWARD && units.marked<M>(i, xi, y0, n, P.marks, P.mark_words);
                 if (mine) continue;
                 const int ybase = (y0 + i) * XT + half * 64;
                 const uint32_t cols = info + st * XT_INFO + half * 64 * 4;      // dw: row_info of this warp's columns
@@ -482,110 +544,145 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
                 if (!ok) break;
                 tc::fence_after();
                 const uint32_t sa = tmem + b * XT + half * 64 + lanes;
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
+                // backward: 32 columns of S become Z
+                auto weigh = [&](auto labels, int c) {
+                    constexpr bool LABELS = decltype(labels)::value;
                     uint32_t q[32];
                     tc::ld32(sa + 32 * c, q);
                     tc::wait_ld(q);
                     const int col = ybase + c * 32;
                     f32x2 f[16];
-                    if (M == TC_FORWARD) {
-                        if (c == 1) {                      // S is in registers: the buffer may be overwritten
-                            tc::fence_before();
-                            tc::mbar_arrive(p_full(b));
-                        }
-                        float cc = c2;
-                        if (col + 32 > P.ny) {             // behind the table's last row
-                            cc = 1.f;
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) q[j] = col + j < P.ny ? __float_as_uint(__uint_as_float(q[j]) * c2) : 0xFF800000u;
-                        }
-                        if (__any_sync(FULL, label >= col && label < col + 32)) {
-                            float z = 0.f;
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (col + j == label) z = __uint_as_float(q[j]) * cc;
-                            if (label >= col && label < col + 32) P.picked[x] = z;
-                            __syncwarp();
-                        }
-                        float e[4];                        // the largest product with cc comes from the largest or the smallest S
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) e[j] = __uint_as_float(q[j]);
-                        if (cc >= 0.f) {
-#pragma unroll
-                            for (int j = 4; j < 32; j += 8)
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) e[k] = j < 28 ? max3(e[k], __uint_as_float(q[j + k]), __uint_as_float(q[(j + k + 4) & 31])) : fmaxf(e[k], __uint_as_float(q[j + k]));
-                            e[0] = fmaxf(max3(e[0], e[1], e[2]), e[3]);
-                        } else {
-#pragma unroll
-                            for (int j = 4; j < 32; j += 8)
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) e[k] = j < 28 ? min3(e[k], __uint_as_float(q[j + k]), __uint_as_float(q[(j + k + 4) & 31])) : fminf(e[k], __uint_as_float(q[j + k]));
-                            e[0] = fminf(min3(e[0], e[1], e[2]), e[3]);
-                        }
-                        const float top = fmaxf(m, e[0] * cc), ref = top == -INFINITY ? 0.f : top;
-                        const f32x2 c22 = pair(cc, cc), r2 = pair(-ref, -ref);
-                        f32x2 sum[2] = {0, 0};
+                    const f32x2 c22 = pair(c2, c2);
+                    uint32_t mask = 0;                 // this row's label entries among the 32 columns
+                    if (M == TC_DHIDDEN) {
+                        const f32x2 r2 = pair(-lse2, -lse2);
 #pragma unroll
                         for (int j = 0; j < 16; ++j)
-                            sum[j & 1] = add2(sum[j & 1], exp2_pair<true>(fma2(pair(__uint_as_float(q[2 * j]), __uint_as_float(q[2 * j + 1])), c22, r2), j));
-                        float lo, hi;
-                        split(add2(sum[0], sum[1]), lo, hi);
-                        l = l * xt_exp2(m - ref) + (lo + hi);
-                        m = top;
-                    } else {
-                        const f32x2 c22 = pair(c2, c2);
-                        if (M == TC_DHIDDEN) {
-                            const f32x2 r2 = pair(-lse2, -lse2);
+                            f[j] = exp2_pair<false>(fma2(pair(__uint_as_float(q[2 * j]), __uint_as_float(q[2 * j + 1])), c22, r2), j);
+                        if (LABELS) {
+                            if (label >= col && label < col + 32) mask = 1u << (label - col);
 #pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                f[j] = exp2_pair<false>(fma2(pair(__uint_as_float(q[2 * j]), __uint_as_float(q[2 * j + 1])), c22, r2), j);
-                            if (__any_sync(FULL, label >= col && label < col + 32)) {
+                            for (int j = 0; j < 16; ++j) f[j] = add2(f[j], pair(mask >> 2 * j & 1 ? -1.f : 0.f, mask >> (2 * j + 1) & 1 ? -1.f : 0.f));
+                        }
+                        if (col + 32 > P.ny) {
 #pragma unroll
-                                for (int j = 0; j < 16; ++j)
-                                    f[j] = add2(f[j], pair(col + 2 * j == label ? -1.f : 0.f, col + 2 * j + 1 == label ? -1.f : 0.f));
-                            }
-                            if (col + 32 > P.ny) {
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) {
-                                    float lo, hi;
-                                    split(f[j], lo, hi);
-                                    f[j] = pair(col + 2 * j < P.ny ? lo : 0.f, col + 2 * j + 1 < P.ny ? hi : 0.f);
-                                }
-                            }
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 16; j += 2) {
-                                const float4 ls = shared_f4(cols + (c * 32 + 2 * j) * 4);
-                                f[j] = exp2_pair<false>(fma2(pair(__uint_as_float(q[2 * j]), __uint_as_float(q[2 * j + 1])), c22, pair(ls.x, ls.y)), j);
-                                f[j + 1] = exp2_pair<false>(fma2(pair(__uint_as_float(q[2 * j + 2]), __uint_as_float(q[2 * j + 3])), c22, pair(ls.z, ls.w)), j + 1);
-                            }
-                            const int lab = shared_i(cols + (2 * XT + c * 32 + lane) * 4) - ((int)(xi * XT) + (warp & 3) * 32);
-                            if (__any_sync(FULL, lab >= 0 && lab < 32)) {
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) {
-                                    const int a = __shfl_sync(FULL, lab, 2 * j), d = __shfl_sync(FULL, lab, 2 * j + 1);
-                                    f[j] = add2(f[j], pair(a == lane ? -1.f : 0.f, d == lane ? -1.f : 0.f));
-                                }
-                            }
-#pragma unroll
-                            for (int j = 0; j < 16; j += 2) {
-                                const float4 g = shared_f4(cols + (XT + c * 32 + 2 * j) * 4);
-                                f[j] = mul2(f[j], pair(g.x, g.y));
-                                f[j + 1] = mul2(f[j + 1], pair(g.z, g.w));
+                            for (int j = 0; j < 16; ++j) {
+                                float lo, hi;
+                                split(f[j], lo, hi);
+                                f[j] = pair(col + 2 * j < P.ny ? lo : 0.f, col + 2 * j + 1 < P.ny ? hi : 0.f);
                             }
                         }
-                        uint32_t z[16];
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; j += 2) {
+                            const float4 ls = shared_f4(cols + (c * 32 + 2 * j) * 4);
+                            f[j] = exp2_pair<false>(fma2(pair(__uint_as_float(q[2 * j]), __uint_as_float(q[2 * j + 1])), c22, pair(ls.x, ls.y)), j);
+                            f[j + 1] = exp2_pair<false>(fma2(pair(__uint_as_float(q[2 * j + 2]), __uint_as_float(q[2 * j + 3])), c22, pair(ls.z, ls.w)), j + 1);
+                        }
+                        if (LABELS) {
+                            const int lab = shared_i(cols + (2 * XT + c * 32 + lane) * 4) - ((int)(xi * XT) + (warp & 3) * 32);
+                            mask = __ballot_sync(FULL, lab >= 0 && lab < 32);      // columns whose label is this lane's row
+#pragma unroll
+                            for (int k = 0; k < 5; ++k) {
+                                const uint32_t ones = __ballot_sync(FULL, lab >> k & 1);
+                                mask &= lane >> k & 1 ? ones : ~ones;
+                            }
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) f[j] = add2(f[j], pair(mask >> 2 * j & 1 ? -1.f : 0.f, mask >> (2 * j + 1) & 1 ? -1.f : 0.f));
+                        }
+#pragma unroll
+                        for (int j = 0; j < 16; j += 2) {
+                            const float4 g = shared_f4(cols + (XT + c * 32 + 2 * j) * 4);
+                            f[j] = mul2(f[j], pair(g.x, g.y));
+                            f[j + 1] = mul2(f[j + 1], pair(g.z, g.w));
+                        }
+                    }
+                    uint32_t z[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float lo, hi;
+                        split(f[j], lo, hi);
+                        z[j] = pack_bf16(lo, hi);
+                    }
+                    __syncwarp();
+                    tc::st16(sa + 32 * c, z);           // over columns of S that this warp has read
+                    if (LABELS) {                      // what the rounding took
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
                             float lo, hi;
                             split(f[j], lo, hi);
-                            z[j] = pack_bf16(lo, hi);
+                            lo -= __uint_as_float(z[j] << 16);
+                            hi -= __uint_as_float(z[j] & 0xFFFF0000u);
+                            // nothing to add where an entry left the range
+                            z[j] = pack_bf16(fabsf(lo) <= 3e38f ? lo : 0.f, fabsf(hi) <= 3e38f ? hi : 0.f);
                         }
                         __syncwarp();
-                        tc::st16(sa + 16 * c, z);           // over columns of S that this warp has read
+                        tc::st16(sa + 32 * c + 16, z);
                     }
+                };
+                if constexpr (M != TC_FORWARD) {
+                    if (marked) {
+                        const uint32_t labels = LabelUnits::columns<M>(P.a, xi, y0 + i, info + st * XT_INFO) >> half * 16;
+#pragma unroll 1
+                        for (int c = 0; c < 2; ++c) {
+                            if (labels >> 8 * c & 0x11) weigh(std::true_type{}, c);
+                            else weigh(std::false_type{}, c);
+                        }
+                    } else {
+                        weigh(std::false_type{}, 0);
+                        weigh(std::false_type{}, 1);
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < (M == TC_FORWARD ? 2 : 0); ++c) {
+                    uint32_t q[32];
+                    tc::ld32(sa + 32 * c, q);
+                    tc::wait_ld(q);
+                    const int col = ybase + c * 32;
+                    if (c == 1) {                      // S is in registers: the buffer may be overwritten
+                        tc::fence_before();
+                        tc::mbar_arrive(p_full(b));
+                    }
+                    float cc = c2;
+                    if (col + 32 > P.ny) {             // behind the table's last row
+                        cc = 1.f;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) q[j] = col + j < P.ny ? __float_as_uint(__uint_as_float(q[j]) * c2) : 0xFF800000u;
+                    }
+                    if (__any_sync(FULL, label >= col && label < col + 32)) {
+                        float z = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (col + j == label) z = __uint_as_float(q[j]) * cc;
+                        if (label >= col && label < col + 32) P.picked[x] = z;
+                        __syncwarp();
+                    }
+                    float e[4];                        // the largest product with cc comes from the largest or the smallest S
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) e[j] = __uint_as_float(q[j]);
+                    if (cc >= 0.f) {
+#pragma unroll
+                        for (int j = 4; j < 32; j += 8)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) e[k] = j < 28 ? max3(e[k], __uint_as_float(q[j + k]), __uint_as_float(q[(j + k + 4) & 31])) : fmaxf(e[k], __uint_as_float(q[j + k]));
+                        e[0] = fmaxf(max3(e[0], e[1], e[2]), e[3]);
+                    } else {
+#pragma unroll
+                        for (int j = 4; j < 32; j += 8)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) e[k] = j < 28 ? min3(e[k], __uint_as_float(q[j + k]), __uint_as_float(q[(j + k + 4) & 31])) : fminf(e[k], __uint_as_float(q[j + k]));
+                        e[0] = fminf(min3(e[0], e[1], e[2]), e[3]);
+                    }
+                    const float top = fmaxf(m, e[0] * cc), ref = top == -INFINITY ? 0.f : top;
+                    const f32x2 c22 = pair(cc, cc), r2 = pair(-ref, -ref);
+                    f32x2 sum[2] = {0, 0};
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        sum[j & 1] = add2(sum[j & 1], exp2_pair<true>(fma2(pair(__uint_as_float(q[2 * j]), __uint_as_float(q[2 * j + 1])), c22, r2), j));
+                    float lo, hi;
+                    split(add2(sum[0], sum[1]), lo, hi);
+                    l = l * xt_exp2(m - ref) + (lo + hi);
+                    m = top;
                 }
                 if (M != TC_FORWARD) {
                     tc::wait_st();
@@ -617,10 +714,13 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
     }
 }
 
-// What the dw kernel needs of the hidden rows, tile by tile (rows behind the last have no gradient).
-__global__ void __launch_bounds__(XT) k_xent_row_info(Xent a, float* __restrict__ info) {
+// What the dw kernel needs of the hidden rows, tile by tile (rows behind the last have no gradient), and the marks of the
+// table's tiles in which their labels lie.
+__global__ void __launch_bounds__(XT) k_xent_row_info(Xent a, float* __restrict__ info, uint32_t* __restrict__ marks, int words) {
     chain_wait();
     for (int64_t t = blockIdx.x; t * XT < a.rows; t += gridDim.x) {
+        for (int i = threadIdx.x; i < words; i += XT) marks[t * words + i] = 0;
+        __syncthreads();
         const int64_t n = t * XT + threadIdx.x;
         const int lab = n < a.rows ? a.labels[n] : -1;
         const bool valid = lab >= 0 && lab < a.vocab;
@@ -628,6 +728,7 @@ __global__ void __launch_bounds__(XT) k_xent_row_info(Xent a, float* __restrict_
         p[0] = n < a.rows ? a.lse[n] * -XT_LOG2E : 0.f;
         p[XT] = valid ? a.dloss[n] * a.scale : 0.f;
         reinterpret_cast<int*>(p)[2 * XT] = valid ? lab : -1;
+        if (valid) atomicOr(marks + t * words + (lab >> 5) / XT, 1u << (lab / XT & 31));
     }
 }
 
@@ -687,6 +788,9 @@ bool xent_tc_takes(const Xent& a) {
     return a.dim % 8 != 0 || (tile_rows_ok(a.hidden, a.hidden_ld) && tile_rows_ok(a.table, a.table_ld));
 }
 
+// Words of marks per tile of hidden rows: a bit per tile of the table.
+static int mark_words(const Xent& a) { return (int)((a.vocab + 32 * XT - 1) / (32 * XT)); }
+
 struct TcLayout {
     size_t hidden, table, rest, total;
 };
@@ -702,7 +806,7 @@ static TcLayout tc_layout(const Xent& a) {
     l.rest = off;
     const int64_t parts = sm_count(), tx = (a.rows + XT - 1) / XT;
     const size_t fwd = align_up((size_t)(parts + tx) * XENT_TC_STATS * XT * 8, 256) + align_up((size_t)a.rows * 4, 256);
-    const size_t bwd = align_up((size_t)2 * parts * XT * ((a.dim + 15) / 16 * 16) * 4, 256) + (size_t)tx * XT_INFO;
+    const size_t bwd = align_up((size_t)2 * parts * XT * ((a.dim + 15) / 16 * 16) * 4, 256) + (size_t)tx * (XT_INFO + (size_t)mark_words(a) * 4);
     take(fwd > bwd ? fwd : bwd);
     l.total = off;
     return l;
@@ -824,7 +928,10 @@ cudaError_t launch_xent_tc_backward(const Xent& a, void* workspace, cudaStream_t
     P.partial = (float*)o.rest;
     float* row_info = (float*)(o.rest + align_up((size_t)2 * sm_count() * XT * ((a.dim + 15) / 16 * 16) * 4, 256));
     P.row_info = row_info;
-    e = launch_train(k_xent_row_info, (a.rows + XT - 1) / XT, XT, 0, s, a, row_info);
+    P.mark_words = mark_words(a);
+    uint32_t* marks = (uint32_t*)(row_info + (int64_t)((a.rows + XT - 1) / XT) * (XT_INFO / 4));
+    P.marks = marks;
+    e = launch_train(k_xent_row_info, (a.rows + XT - 1) / XT, XT, 0, s, a, row_info, marks, P.mark_words);
     if (e == cudaSuccess) e = run_tc<TC_DHIDDEN>(a, o, P, s);
     if (e != cudaSuccess) return e;
     e = launch_xent_join(a, true, P.runs, XT, P.on, P.partial, s);

@@ -209,3 +209,36 @@ def test_refusals():
     with pytest.raises(gs.GsError) as e:
         gs.gs_xent_forward(big, big, y[:1], ws)
     assert e.value.status == 1
+
+
+@pytest.mark.parametrize("n,v,d", [(1, 512, 32), (64, 512, 64), (300, 171, 100), (700, 1024, 128), (130, 300, 200), (90, 513, 256), (5, 3, 24)])
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_label_entries_keep_their_precision(n, v, d, out):
+    """p - 1 of a small p lies just under one, where bf16 loses p: a bias that every row of a label would share.  The
+    label's entry enters the product in two parts, 2^-16 of it is lost; the others are rounded once; an exponential of
+    the gradient is off by 2^-18 beside E."""
+    t = torch.bfloat16
+    g = _gen(n + v + d)
+    h, w, y, dl = _inputs(n, v, d, t, g, std=0.02)                     # logits near zero: p is about 1 / v
+    y = y.clamp(0, v - 1)
+    y[: n // 2] = 0                                                    # many rows of one label in one tile
+    dl = dl.abs() + 1.0                                                # the bias would not average out
+    hd, wd = h.double(), w.double()
+    z = hd @ wd.t()
+    lse = torch.logsumexp(z, 1)
+    at, yc = torch.arange(n, device="cuda"), y.long()
+    p = torch.exp(z - lse[:, None])
+    dz, other = p.clone(), p.clone()
+    dz[at, yc] -= 1.0
+    other[at, yc] = 0.0
+    E = 4 * ((d + 4) * U * (hd.abs() @ wd.abs().t()).amax(1) + 2.0 ** -21 + (v + 4) * U) + 2.0 ** -18
+    label = torch.zeros_like(p)
+    label[at, yc] = dz[at, yc].abs()
+    dld = dl.double()[:, None]
+    err = (E[:, None] * p + 2.0 ** -8 * other + 2.0 ** -16 * label) * dld
+    dz = dz * dld
+    dh, dw = dz @ wd, dz.t() @ hd
+    half = HALF_ULP[out]
+    got = _run(h, w, y, dl, 1.0, out)
+    _check(got, {"dhidden": (dh, err @ wd.abs() + (v + 4) * U * (dz.abs() @ wd.abs()) + half * dh.abs()),
+                 "dtable": (dw, err.t() @ hd.abs() + (n + 4) * U * (dz.abs().t() @ hd.abs()) + half * dw.abs())})
