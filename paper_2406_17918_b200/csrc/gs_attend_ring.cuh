@@ -401,12 +401,8 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                     __syncwarp();
                     ring_sum<G>(delta, tl);
                     if (batch & FIRST) {
-                        const int row = rows_s[(batch >> 8) & 255].z;
 #pragma unroll
-                        for (int i = 0; i < G; ++i) {
-                            l[i] = delta[i];
-                            if (!P.chunk_mode && t == 0) P.stat[(int64_t)row * P.a.q_heads + h * G + i] = make_float2(m[i], l[i]);
-                        }
+                        for (int i = 0; i < G; ++i) l[i] = delta[i];
                     }
                     __syncwarp();
                 }

@@ -1,5 +1,6 @@
 // Stable sort of (key, payload) pairs by key: the order in which gradients of repeated ids, and the edges of a
-// block seen from their sources, are summed.  Least-significant-digit radix sort, digits of up to 9 bits.  A pass is three kernels: the digit counts of every tile; every digit's offsets into the
+// block seen from their sources, are summed.  Least-significant-digit radix sort, digits of up to 9 bits.  A pass is three
+// kernels: the digit counts of every tile; every digit's offsets into the
 // tiles; and the scatter, in which each warp ranks its pairs by ballots, the tile is put in digit order in shared memory and
 // leaves in runs.  Equal keys keep their input order, and no kernel waits for another block: results do not depend on the
 // schedule.  2.03 M pairs of 26 bits: 95 us.  (One kernel per 8-bit digit, tiles looking back over their predecessors'
@@ -245,6 +246,7 @@ __global__ void __launch_bounds__(KS_THREADS, ROUNDS <= 4 ? 5 : 3) k_key_scatter
 __device__ __forceinline__ void fill_zero(const Fill& f, int block, int blocks) {
     const uint4 zero = make_uint4(0, 0, 0, 0);
     for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < f.pieces; i += (int64_t)blocks * blockDim.x) __stcs(f.p + i, zero);
+    if (block == 0 && (int)threadIdx.x < f.tail) reinterpret_cast<char*>(f.p + f.pieces)[threadIdx.x] = 0;
 }
 
 // All passes in one block; the others clear memory.
@@ -312,7 +314,7 @@ __global__ void __launch_bounds__(KS_SMALL_THREADS) k_fill(Fill f) {
     fill_zero(f, blockIdx.x, gridDim.x);
 }
 
-// All passes in one cluster: every block ranks its share, the blocks read one another's digit counts, and every pair goes
+// All passes in one cluster (40,961 ids of 18 bits: 33 us, the clearing of 87 MB beside it; bound by the ballots of the ranks): every block ranks its share, the blocks read one another's digit counts, and every pair goes
 // straight to its place in the shared memory of the block that holds it next.
 __global__ void __cluster_dims__(KC_BLOCKS, 1, 1) __launch_bounds__(1024) k_key_sort_cluster(KeySort P, Fill f) {
     namespace cg = cooperative_groups;

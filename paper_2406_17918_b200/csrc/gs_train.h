@@ -46,10 +46,11 @@ template <typename F> inline cudaError_t allow_smem(F* kernel, int bytes, std::a
     return e;
 }
 
-// Memory to be cleared, in 16-byte pieces.
+// Memory to be cleared: 16-byte pieces (none: nothing) and fewer than 16 bytes behind them.
 struct Fill {
     uint4* p;
     int64_t pieces;
+    int tail;
 };
 
 // ---- stable sort of (key, payload) pairs by key: ascending keys, equal keys in input order ----
