@@ -11,8 +11,8 @@
 // multiplied while another is exponentiated.  S of a later unit may overwrite a Z once the product that read it has ended.
 // Work is cut into equal runs of units, one per SM; a row of tiles shared by runs is joined from f32 partials.
 // Bound: forward by the exponentials (one per logit; special-function and multiply-add units share them), backward by the
-// reads of X, Y and Y again from shared memory beside them.  8,192 x 169,343 x 128: forward 363 us (0.98 PFLOP/s), dh 500 us and
-// dw 580 us (1.4 and 1.2 PFLOP/s over their two products).
+// reads of X, Y and Y again from shared memory beside them.  8,192 x 169,343 x 128: forward 363 us (0.98 PFLOP/s), dh 516 us and
+// dw 589 us (1.4 and 1.2 PFLOP/s over their two products).
 #include <atomic>
 #include <type_traits>
 
