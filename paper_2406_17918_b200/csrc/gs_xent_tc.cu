@@ -885,6 +885,8 @@ template <int M> static cudaError_t run_tc(const Xent& a, const Operands& o, Xen
     }
     // shared memory: X, the ring of Y, row info, and rows on their way out where X and three or more tiles of Y leave room
     int staging = 0;
+    P.out = OUT_DIRECT;                    // each gradient by its own address and pitch
+    P.out_pitch = 0;
     if (M != TC_FORWARD && chunks <= 2 && a.grad_dtype == GS_BF16) {
         const void* grad = M == TC_DHIDDEN ? a.dhidden : a.dtable;
         const int64_t ld = M == TC_DHIDDEN ? a.dhidden_ld : a.dtable_ld;
