@@ -652,6 +652,15 @@ def _on(stream, t: torch.Tensor):
     return _raw_stream(t.get_device()) if _raw_stream is not None else torch.cuda.current_stream(t.device).cuda_stream
 
 
+def _new(shape, dtype, like: torch.Tensor, stream) -> torch.Tensor:
+    """An output that the caller did not bring: memory of the stream the call runs on, so that nothing queued on another
+    stream for the memory's last owner can still write to it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
 def _dtype(t: torch.dtype) -> int:
     code = _DTYPE.get(t)
     if code is None:
@@ -684,7 +693,7 @@ def gs_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1
     _rows_2d(table, "table")
     _ids_1d(ids, "ids")
     if out is None:
-        out = torch.empty((ids.numel(), table.shape[1]), dtype=out_dtype or table.dtype, device=table.device)
+        out = _new((ids.numel(), table.shape[1]), out_dtype or table.dtype, table, stream)
     else:
         _rows_2d(out, "out")
         if out.shape[0] < ids.numel() or out.shape[1] != table.shape[1]:
@@ -714,7 +723,7 @@ def gs_embedding_backward(dout: torch.Tensor, ids: torch.Tensor, table_rows: int
     """Gradient of the whole table: row r = scale * sum of dout[p] over ids[p] == r, zeros elsewhere."""
     _embedding_grad_args(dout, ids)
     if out is None:
-        out = torch.empty((int(table_rows), dout.shape[1]), dtype=out_dtype or dout.dtype, device=dout.device)
+        out = _new((int(table_rows), dout.shape[1]), out_dtype or dout.dtype, dout, stream)
     else:
         _rows_2d(out, "out")
         if tuple(out.shape) != (int(table_rows), dout.shape[1]):
@@ -733,11 +742,11 @@ def gs_embedding_backward_sparse(dout: torch.Tensor, ids: torch.Tensor, table_ro
     _embedding_grad_args(dout, ids)
     n, d = ids.numel(), dout.shape[1]
     if rows is None:
-        rows = torch.empty(n, dtype=torch.int32, device=dout.device)
+        rows = _new(n, torch.int32, dout, stream)
     if num_rows is None:
-        num_rows = torch.empty(1, dtype=torch.int32, device=dout.device)
+        num_rows = _new(1, torch.int32, dout, stream)
     if grad is None:
-        grad = torch.empty((n, d), dtype=out_dtype or dout.dtype, device=dout.device)
+        grad = _new((n, d), out_dtype or dout.dtype, dout, stream)
     _ids_1d(rows, "rows")
     _rows_2d(grad, "grad")
     if rows.numel() < n or grad.shape[0] < n or grad.shape[1] != d:
@@ -789,9 +798,9 @@ def gs_block_attention_forward(indptr: torch.Tensor, indices: torch.Tensor, q: t
         raise ValueError("q has fewer rows than the block has destinations")
     b = _csr_block(indptr, indices, k.shape[0], counts)
     if out is None:
-        out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
+        out = _new((n, hq, d), q.dtype, q, stream)
     if lse is None:
-        lse = torch.empty((n, hq), dtype=torch.float32, device=q.device)
+        lse = _new((n, hq), torch.float32, q, stream)
     elif lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape[0] < b.max_dst or lse.shape[1] != hq:
         raise TypeError("lse must be a contiguous float32 tensor [dst, q_heads]")
     keep, (pq, pk, pv, po) = _heads(q.dtype, (q, "q", b.max_dst, hq, d), (k, "k", b.max_src, hk, d), (v, "v", b.max_src, hk, d),
@@ -808,11 +817,11 @@ def gs_block_reverse(indptr: torch.Tensor, indices: torch.Tensor, num_src: int, 
     from), masked edges left out."""
     b = _csr_block(indptr, indices, num_src, counts)
     if rev_indptr is None:
-        rev_indptr = torch.empty(b.max_src + 1, dtype=torch.int32, device=indptr.device)
+        rev_indptr = _new(b.max_src + 1, torch.int32, indptr, stream)
     if rev_dst is None:
-        rev_dst = torch.empty(b.max_edges, dtype=torch.int32, device=indptr.device)
+        rev_dst = _new(b.max_edges, torch.int32, indptr, stream)
     if rev_edge is None:
-        rev_edge = torch.empty(b.max_edges, dtype=torch.int32, device=indptr.device)
+        rev_edge = _new(b.max_edges, torch.int32, indptr, stream)
     if _ids_1d(rev_indptr, "rev_indptr").numel() < b.max_src + 1 or _ids_1d(rev_dst, "rev_dst").numel() < b.max_edges or \
             _ids_1d(rev_edge, "rev_edge").numel() < b.max_edges:
         raise ValueError("rev_indptr / rev_dst / rev_edge are too small")
@@ -834,9 +843,9 @@ def gs_block_attention_backward(indptr: torch.Tensor, indices: torch.Tensor, rev
         raise ValueError("reverse belongs to another block")
     if lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.shape[0] < b.max_dst or lse.shape[1] != hq:
         raise TypeError("lse must be a contiguous float32 tensor [dst, q_heads]")
-    dq = torch.empty((n, hq, d), dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty((k.shape[0], hk, d), dtype=q.dtype, device=q.device) if dk is None else dk
-    dv = torch.empty((v.shape[0], hk, d), dtype=q.dtype, device=q.device) if dv is None else dv
+    dq = _new((n, hq, d), q.dtype, q, stream) if dq is None else dq
+    dk = _new((k.shape[0], hk, d), q.dtype, q, stream) if dk is None else dk
+    dv = _new((v.shape[0], hk, d), q.dtype, q, stream) if dv is None else dv
     t = q.dtype
     keep, (pq, pk, pv, po, pdo, pdq, pdk, pdv) = _heads(
         t, (q, "q", b.max_dst, hq, d), (k, "k", b.max_src, hk, d), (v, "v", b.max_src, hk, d), (out, "out", b.max_dst, hq, d),
@@ -874,8 +883,8 @@ def gs_xent_forward(hidden: torch.Tensor, table: torch.Tensor, labels: torch.Ten
     """loss[n] = lse[n] - scale <hidden[n], table[labels[n]]>, lse over all rows of the table; labels outside it: loss 0."""
     _xent_args(hidden, table, labels)
     n = hidden.shape[0]
-    loss = torch.empty(n, dtype=torch.float32, device=hidden.device) if loss is None else _f32_rows(loss, "loss", n)
-    lse = torch.empty(n, dtype=torch.float32, device=hidden.device) if lse is None else _f32_rows(lse, "lse", n)
+    loss = _new(n, torch.float32, hidden, stream) if loss is None else _f32_rows(loss, "loss", n)
+    lse = _new(n, torch.float32, hidden, stream) if lse is None else _f32_rows(lse, "lse", n)
     _check(_L.gs_xent_forward(_addr(hidden), _ld(hidden), _addr(table), _ld(table), _dtype(hidden.dtype), n, table.shape[0], hidden.shape[1],
                               float(scale), _addr(labels), _addr(loss), _addr(lse), _addr(workspace), workspace.numel(), _on(stream, workspace)))
     return loss, lse
@@ -890,8 +899,8 @@ def gs_xent_backward(hidden: torch.Tensor, table: torch.Tensor, labels: torch.Te
     _f32_rows(lse, "lse", n)
     _f32_rows(dloss, "dloss", n)
     t = out_dtype or hidden.dtype
-    dhidden = torch.empty((n, d), dtype=t, device=hidden.device) if dhidden is None else _rows_2d(dhidden, "dhidden")
-    dtable = torch.empty(tuple(table.shape), dtype=dhidden.dtype, device=hidden.device) if dtable is None else _rows_2d(dtable, "dtable")
+    dhidden = _new((n, d), t, hidden, stream) if dhidden is None else _rows_2d(dhidden, "dhidden")
+    dtable = _new(tuple(table.shape), dhidden.dtype, hidden, stream) if dtable is None else _rows_2d(dtable, "dtable")
     if tuple(dhidden.shape) != (n, d) or dtable.shape != table.shape or dhidden.dtype != dtable.dtype:
         raise ValueError("dhidden / dtable must have the shapes of hidden / table and one dtype")
     _check(_L.gs_xent_backward(_addr(hidden), _ld(hidden), _addr(table), _ld(table), _dtype(hidden.dtype), n, table.shape[0], d, float(scale),
