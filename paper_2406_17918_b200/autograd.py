@@ -1,7 +1,9 @@
 """The training operators as differentiable PyTorch functions.
 
 Thin ``torch.autograd.Function`` wrappers over the library's calls: what is saved, recomputed and returned is what the
-C ABI documents (``include/gs.h``).  Workspaces come from PyTorch's caching allocator for the length of a call.
+C ABI documents (``include/gs.h``).  Workspaces come from PyTorch's caching allocator for the length of a call.  Arrays
+at their bounds (``count``, ``counts``, more query rows than the block has destinations): rows behind the actual sizes are
+zeros, in results and in gradients.
 """
 from __future__ import annotations
 

@@ -7,6 +7,7 @@ tensors (torch is used for device memory and streams only); the binding passes t
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import re
 
@@ -652,13 +653,16 @@ def _on(stream, t: torch.Tensor):
     return _raw_stream(t.get_device()) if _raw_stream is not None else torch.cuda.current_stream(t.device).cuda_stream
 
 
-def _new(shape, dtype, like: torch.Tensor, stream) -> torch.Tensor:
+def _new(shape, dtype, like: torch.Tensor, stream, rest=None) -> torch.Tensor:
     """An output that the caller did not bring: memory of the stream the call runs on, so that nothing queued on another
-    stream for the memory's last owner can still write to it."""
-    if stream is None:
+    stream for the memory's last owner can still write to it.  `rest`: what rows that the kernels do not write hold, where
+    there may be such rows (an array at its bound, whose length only the device knows)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _new(shape, dtype, like, None, rest)
+    if rest is None:
         return torch.empty(shape, dtype=dtype, device=like.device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
+    return torch.full(shape, rest, dtype=dtype, device=like.device)
 
 
 def _dtype(t: torch.dtype) -> int:
@@ -689,11 +693,11 @@ def _ld(t: torch.Tensor) -> int:
 def gs_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: torch.Tensor = None,
                         out_dtype: torch.dtype = None, count: torch.Tensor = None, stream=None) -> torch.Tensor:
     """out[p] = scale * table[ids[p]]; ids outside the table give rows of zeros.  `count`: a 0-d int32 CUDA tensor
-    with the list's length (`ids` is then the bound)."""
+    with the list's length (`ids` is then the bound; rows behind it are zeros, or left as they are in a given `out`)."""
     _rows_2d(table, "table")
     _ids_1d(ids, "ids")
     if out is None:
-        out = _new((ids.numel(), table.shape[1]), out_dtype or table.dtype, table, stream)
+        out = _new((ids.numel(), table.shape[1]), out_dtype or table.dtype, table, stream, None if count is None else 0)
     else:
         _rows_2d(out, "out")
         if out.shape[0] < ids.numel() or out.shape[1] != table.shape[1]:
@@ -791,16 +795,18 @@ def gs_block_attention_forward(indptr: torch.Tensor, indices: torch.Tensor, q: t
     """Attention of a block's destinations (q: [dst, q_heads, head_dim]) over their sources (k, v: [src, kv_heads,
     head_dim]); indptr, indices: the block's int32 arrays; an index outside [0, src) is masked.  `scale` defaults to
     1 / sqrt(head_dim); `max_row`: an upper bound on a row's edges (the fan-out) if one is known; `counts`: the
-    device scalars of Block.counts_device() when the arrays are only bounds.  Returns (out, lse)."""
+    device scalars of Block.counts_device() when the arrays are only bounds.  Returns (out, lse); rows of q that the block
+    does not have get zeros and -inf, or are left as they are in given arrays."""
     n, hq, d = q.shape
     hk = k.shape[1]
     if indptr.numel() - 1 > n:
         raise ValueError("q has fewer rows than the block has destinations")
     b = _csr_block(indptr, indices, k.shape[0], counts)
+    exact = counts is None and n == b.max_dst
     if out is None:
-        out = _new((n, hq, d), q.dtype, q, stream)
+        out = _new((n, hq, d), q.dtype, q, stream, None if exact else 0)
     if lse is None:
-        lse = _new((n, hq), torch.float32, q, stream)
+        lse = _new((n, hq), torch.float32, q, stream, None if exact else -math.inf)
     elif lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape[0] < b.max_dst or lse.shape[1] != hq:
         raise TypeError("lse must be a contiguous float32 tensor [dst, q_heads]")
     keep, (pq, pk, pv, po) = _heads(q.dtype, (q, "q", b.max_dst, hq, d), (k, "k", b.max_src, hk, d), (v, "v", b.max_src, hk, d),
@@ -833,7 +839,8 @@ def gs_block_attention_backward(indptr: torch.Tensor, indices: torch.Tensor, rev
                                 out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor, workspace: torch.Tensor, scale: float = None,
                                 max_row: int = 0, dq: torch.Tensor = None, dk: torch.Tensor = None, dv: torch.Tensor = None, counts=None,
                                 stream=None):
-    """Gradients of gs_block_attention_forward; `reverse` is what gs_block_reverse returned.  Returns (dq, dk, dv)."""
+    """Gradients of gs_block_attention_forward; `reverse` is what gs_block_reverse returned.  Returns (dq, dk, dv); rows that
+    the block does not have get zeros, or are left as they are in given arrays."""
     n, hq, d = q.shape
     hk = k.shape[1]
     b = _csr_block(indptr, indices, k.shape[0], counts)
@@ -843,9 +850,10 @@ def gs_block_attention_backward(indptr: torch.Tensor, indices: torch.Tensor, rev
         raise ValueError("reverse belongs to another block")
     if lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.shape[0] < b.max_dst or lse.shape[1] != hq:
         raise TypeError("lse must be a contiguous float32 tensor [dst, q_heads]")
-    dq = _new((n, hq, d), q.dtype, q, stream) if dq is None else dq
-    dk = _new((k.shape[0], hk, d), q.dtype, q, stream) if dk is None else dk
-    dv = _new((v.shape[0], hk, d), q.dtype, q, stream) if dv is None else dv
+    rest = lambda rows, bound: None if counts is None and rows == bound else 0  # noqa: E731
+    dq = _new((n, hq, d), q.dtype, q, stream, rest(n, b.max_dst)) if dq is None else dq
+    dk = _new((k.shape[0], hk, d), q.dtype, q, stream, rest(k.shape[0], b.max_src)) if dk is None else dk
+    dv = _new((v.shape[0], hk, d), q.dtype, q, stream, rest(v.shape[0], b.max_src)) if dv is None else dv
     t = q.dtype
     keep, (pq, pk, pv, po, pdo, pdq, pdk, pdv) = _heads(
         t, (q, "q", b.max_dst, hq, d), (k, "k", b.max_src, hk, d), (v, "v", b.max_src, hk, d), (out, "out", b.max_dst, hq, d),
