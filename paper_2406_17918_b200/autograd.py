@@ -3,9 +3,11 @@
 Thin ``torch.autograd.Function`` wrappers over the library's calls: what is saved, recomputed and returned is what the
 C ABI documents (``include/gs.h``).  Workspaces come from PyTorch's caching allocator for the length of a call.  Arrays
 at their bounds (``count``, ``counts``, more query rows than the block has destinations): rows behind the actual sizes are
-zeros, in results and in gradients.
+zeros, in results and in gradients.  The gradients are not differentiable: second derivatives raise an error.
 """
 from __future__ import annotations
+
+import functools
 
 import torch
 
@@ -18,6 +20,32 @@ def _workspace(nbytes: int, like: torch.Tensor) -> torch.Tensor:
     return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
 
 
+class _NotTwice(torch.autograd.Function):
+    """A gradient that depends on `on`, which it cannot be differentiated by."""
+
+    @staticmethod
+    def forward(ctx, grad, *on):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the training operators have first derivatives only: a gradient taken with create_graph=True was differentiated")
+
+
+def _first_order(backward):
+    """With create_graph, the gradients of `backward` are tied to all that they depend on, saved operands included
+    (once_differentiable looks at the incoming gradients alone), so that a second derivative is an error and not zero."""
+
+    @functools.wraps(backward)
+    def checked(ctx, *incoming):
+        with torch.no_grad():
+            grads = backward(ctx, *incoming)
+        on = [t for t in (*incoming, *ctx.saved_tensors) if t is not None and t.requires_grad] if torch.is_grad_enabled() else []
+        return tuple(g if g is None else _NotTwice.apply(g, *on) for g in grads) if on else grads
+
+    return checked
+
+
 class _Embedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, table, ids, scale, out_dtype, count):
@@ -26,6 +54,7 @@ class _Embedding(torch.autograd.Function):
         return gs.gs_embedding_lookup(table, ids, scale=scale, out_dtype=out_dtype, count=count)
 
     @staticmethod
+    @_first_order
     def backward(ctx, dout):
         ids, count = ctx.saved_tensors
         rows, dim = ctx.shape
@@ -50,6 +79,7 @@ class _BlockAttention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @_first_order
     def backward(ctx, dout):
         q, k, v, indptr, indices, out, lse = ctx.saved_tensors
         n, heads, dim = q.shape
@@ -76,6 +106,7 @@ class _TableCrossEntropy(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @_first_order
     def backward(ctx, dloss):
         hidden, table, labels, lse = ctx.saved_tensors
         ws = _workspace(gs.gs_xent_workspace_bytes(hidden.shape[0], table.shape[0], hidden.shape[1], hidden.dtype), hidden)
