@@ -499,6 +499,8 @@ gs_status gs_embedding_backward_sparse(const void* d_dout, gs_dtype dout_dtype, 
  * edge gets out = 0, lse = -inf and has no part in any gradient.
  *   block      a block of gs_sample_batch, or one the caller fills: max_* are the sizes, d_num_* device scalars with
  *              the actual ones, or NULL (the sizes are exact; all three together)
+ *              The edges are those of the rows: what lies before indptr[0] or behind the last offset has no part
+ *              (indptr + a, with the whole array of indices, is the part of a block from destination a on).
  *   max_row    an upper bound on the edges of one destination (the fan-out, for a sampled block), or 0 if it is not
  *              known: rows above 64 edges are then split over the device.  A longer row than promised is slower,
  *              not wrong.

@@ -829,7 +829,8 @@ cudaError_t launch_block_reverse(const int32_t* indptr, const int32_t* indices, 
     int64_t blocks = ((int64_t)dst.bound + AT_THREADS / 8 - 1) / (AT_THREADS / 8);
     if (blocks > sm_count() * 32) blocks = sm_count() * 32;
     cudaError_t e = launch_train(k_edge_rows, blocks, AT_THREADS, 0, s, indptr, dst, (int)edges.bound, rows);
-    if (e == cudaSuccess) e = launch_key_sort(indices, nullptr, edges, src.bound, (char*)workspace + 2 * list, keys, rev_edge, nullptr, 0, Fill{}, s);
+    // edges before the first row's offset or behind the last row belong to no destination
+    if (e == cudaSuccess) e = launch_key_sort(indices, nullptr, edges, Rows{indptr, dst}, src.bound, (char*)workspace + 2 * list, keys, rev_edge, nullptr, 0, Fill{}, s);
     if (e != cudaSuccess) return e;
     blocks = ((int64_t)edges.bound + AT_THREADS * 4) / (AT_THREADS * 4);
     if (blocks > sm_count() * 16) blocks = sm_count() * 16;

@@ -483,7 +483,7 @@ cudaError_t launch_embedding_grad(const EmbedGrad& g, void* workspace, cudaStrea
         if (g.grad_ld == g.dim && (uintptr_t)g.grad % 16 == 0 && bytes >= 16) fill = Fill{(uint4*)g.grad, (int64_t)(bytes / 16), (int)(bytes % 16)};
         else e = cudaMemset2DAsync(g.grad, (size_t)g.grad_ld * out, 0, (size_t)g.dim * out, (size_t)g.table_rows, s);
     }
-    if (e == cudaSuccess) e = launch_key_sort(g.ids, nullptr, g.n, g.table_rows, ws + l.sort, keys, order, P.words, 2, fill, s);
+    if (e == cudaSuccess) e = launch_key_sort(g.ids, nullptr, g.n, Rows{}, g.table_rows, ws + l.sort, keys, order, P.words, 2, fill, s);
     if (e == cudaSuccess && g.rows) {
         const int tiles = (int)(((int64_t)g.n.bound + ES_TILE - 1) / ES_TILE);
         e = launch_train(k_head_counts, (tiles + ES_THREADS / 32 - 1) / (ES_THREADS / 32), ES_THREADS, 0, s, keys, g.n, (uint32_t)g.table_rows, heads);

@@ -28,6 +28,7 @@ struct KeySort {
     const int32_t* keys;
     const int32_t* payload;
     Count n;
+    Rows within;                  // positions outside these rows take the value key_limit too
     uint32_t key_limit;
     int passes, bits, shift;      // digits; shift: of this pass's digit inside the key
     int tiles;                    // of the bound
@@ -51,8 +52,18 @@ __device__ __forceinline__ uint32_t clamp_key(int32_t k, uint32_t limit) {
     return (uint32_t)k < limit ? (uint32_t)k : limit;
 }
 
-__device__ __forceinline__ unsigned long long first_word(const KeySort& P, int i) {
-    return ((unsigned long long)clamp_key(__ldg(P.keys + i), P.key_limit) << 32) | (uint32_t)(P.payload ? __ldcg(P.payload + i) : i);
+// The positions [x, y) that the rows hold.
+__device__ __forceinline__ int2 span_of(const Rows& r) {
+    if (!r.offsets) return make_int2(0, 0x7FFFFFFF);
+    return make_int2(__ldcg(r.offsets), __ldcg(r.offsets + count_of(r.n)));
+}
+
+__device__ __forceinline__ uint32_t first_key(const KeySort& P, int2 span, int i) {
+    return i >= span.x && i < span.y ? clamp_key(__ldg(P.keys + i), P.key_limit) : P.key_limit;
+}
+
+__device__ __forceinline__ unsigned long long first_word(const KeySort& P, int2 span, int i) {
+    return ((unsigned long long)first_key(P, span, i) << 32) | (uint32_t)(P.payload ? __ldcg(P.payload + i) : i);
 }
 
 // Lanes whose digit equals this lane's, from one ballot per bit (a match instruction takes time for every distinct
@@ -90,6 +101,7 @@ __global__ void __launch_bounds__(KS_THREADS) k_key_count(KeySort P, int first) 
     __shared__ int h[KS_MAX_BINS];
     chain_wait();
     const int n = count_of(P.n), bins = 1 << P.bits;
+    const int2 span = span_of(P.within);
     if (first && blockIdx.x == 0)
         for (int i = threadIdx.x; i < P.zero_words; i += KS_THREADS) P.zero[i] = 0;
     for (int tile = blockIdx.x; tile < P.tiles; tile += gridDim.x) {
@@ -100,7 +112,7 @@ __global__ void __launch_bounds__(KS_THREADS) k_key_count(KeySort P, int first) 
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
             const int64_t i = (int64_t)tile * (KS_THREADS * ROUNDS) + r * KS_THREADS + threadIdx.x;
-            key[r] = i < n ? (first ? clamp_key(__ldg(P.keys + i), P.key_limit) : (uint32_t)(__ldcg(P.src + i) >> 32)) : 0;
+            key[r] = i < n ? (first ? first_key(P, span, (int)i) : (uint32_t)(__ldcg(P.src + i) >> 32)) : 0;
         }
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
@@ -174,6 +186,7 @@ __global__ void __launch_bounds__(KS_THREADS, ROUNDS <= 4 ? 5 : 3) k_key_scatter
     __shared__ int warp_sums[33];
     chain_wait();
     const int n = count_of(P.n), bins = 1 << P.bits, per = (bins + KS_THREADS - 1) / KS_THREADS;
+    const int2 span = span_of(P.within);
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, shift = 32 + P.shift;
     for (int tile = blockIdx.x; tile < P.tiles; tile += gridDim.x) {
         if ((int64_t)tile * TILE >= n) return;
@@ -188,7 +201,7 @@ __global__ void __launch_bounds__(KS_THREADS, ROUNDS <= 4 ? 5 : 3) k_key_scatter
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
             const int64_t i = wbase + r * 32 + lane;
-            key[r] = i < n ? (first ? first_word(P, (int)i) : __ldcg(P.src + i)) : ~0ull;   // padding sorts last, behind position n
+            key[r] = i < n ? (first ? first_word(P, span, (int)i) : __ldcg(P.src + i)) : ~0ull;   // padding sorts last, behind position n
         }
         __syncthreads();
         rank_rounds(key, shift, P.bits, cnt + wid * KS_MAX_BINS, rank);
@@ -262,6 +275,7 @@ __global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P, 
         return;
     }
     const int n = count_of(P.n);
+    const int2 span = span_of(P.within);
     for (int i = threadIdx.x; i < P.zero_words; i += KS_SMALL_THREADS) P.zero[i] = 0;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     unsigned long long key[R];
@@ -269,7 +283,7 @@ __global__ void __launch_bounds__(KS_SMALL_THREADS) k_key_sort_small(KeySort P, 
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int i = wid * (R * 32) + r * 32 + lane;
-        key[r] = i < n ? first_word(P, i) : ~0ull;
+        key[r] = i < n ? first_word(P, span, i) : ~0ull;
     }
     const uint32_t mask = (1u << P.bits) - 1u;
     for (int p = 0; p < P.passes; ++p) {
@@ -331,6 +345,7 @@ __global__ void __cluster_dims__(KC_BLOCKS, 1, 1) __launch_bounds__(1024) k_key_
     }
     cg::cluster_group cluster = cg::this_cluster();
     const int n = count_of(P.n), me = blockIdx.x, bins = 1 << P.bits;
+    const int2 span = span_of(P.within);
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     if (me == 0)
         for (int i = threadIdx.x; i < P.zero_words; i += 1024) P.zero[i] = 0;
@@ -339,7 +354,7 @@ __global__ void __cluster_dims__(KC_BLOCKS, 1, 1) __launch_bounds__(1024) k_key_
 #pragma unroll
     for (int r = 0; r < KC_ROUNDS; ++r) {
         const int i = me * KC_TILE + wid * (KC_ROUNDS * 32) + r * 32 + lane;
-        key[r] = i < n ? first_word(P, i) : ~0ull;                   // padding sorts last, behind position n
+        key[r] = i < n ? first_word(P, span, i) : ~0ull;                   // padding sorts last, behind position n
     }
     for (int p = 0; p < P.passes; ++p) {
         const int shift = 32 + P.bits * p;
@@ -419,12 +434,13 @@ template <int ROUNDS> static cudaError_t run_pass(const KeySort& P, bool first, 
     return e;
 }
 
-cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n, int64_t key_limit, void* workspace,
+cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n, Rows within, int64_t key_limit, void* workspace,
                             uint32_t* out_keys, int32_t* out_payload, int32_t* zero, int zero_words, Fill fill, cudaStream_t s) {
     KeySort P{};
     P.keys = keys;
     P.payload = payload;
     P.n = n;
+    P.within = within;
     P.key_limit = (uint32_t)key_limit;
     P.out_keys = out_keys;
     P.out_payload = out_payload;

@@ -17,6 +17,12 @@ struct Count {
     int32_t bound;
 };
 
+// Rows of a list by their offsets; NULL: none, the list as a whole.
+struct Rows {
+    const int32_t* offsets;
+    Count n;
+};
+
 // Kernels of a call are set up while their predecessor drains; each begins with chain_wait().
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_train(void (*kernel)(KArgs...), int64_t grid, int block, size_t smem, cudaStream_t s, Args... args) {
@@ -55,9 +61,10 @@ struct Fill {
 
 // ---- stable sort of (key, payload) pairs by key: ascending keys, equal keys in input order ----
 size_t key_sort_bytes(int64_t n_bound);
-// Keys outside [0, key_limit) take the value key_limit and end behind all others.  payload NULL: the position.
+// Keys outside [0, key_limit), and those at positions outside the rows of `within`, take the value key_limit and end behind all
+// others.  payload NULL: the position.
 // `zero_words` int32 words at `zero` (or none) and `fill` are cleared on the way.
-cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n, int64_t key_limit, void* workspace,
+cudaError_t launch_key_sort(const int32_t* keys, const int32_t* payload, Count n, Rows within, int64_t key_limit, void* workspace,
                             uint32_t* out_keys, int32_t* out_payload, int32_t* zero, int zero_words, Fill fill, cudaStream_t s);
 // starts[r] = number of sorted keys < r, r = 0 .. rows (rows from the device if rows.d_n is set).
 cudaError_t launch_row_starts(const uint32_t* keys, Count n, Count rows, int32_t* starts, cudaStream_t s);
