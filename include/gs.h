@@ -496,7 +496,8 @@ gs_status gs_embedding_backward_sparse(const void* d_dout, gs_dtype dout_dtype, 
  * g = h * kv_heads / q_heads, and the edges e = indptr[i] .. indptr[i+1) with source j = indices[e]:
  *   s_e = scale * <q[i,h], k[j,g]>,  lse[i,h] = log sum_e exp(s_e),  out[i,h] = sum_e exp(s_e - lse[i,h]) v[j,g]
  * An edge whose index is outside [0, num_src) is masked (its rows are not read); a destination without an unmasked
- * edge gets out = 0, lse = -inf and has no part in any gradient.
+ * edge, or whose scores are all -inf, gets out = 0, lse = -inf and has no part in any gradient.  An edge whose score is
+ * -inf among others has probability 0 and no part in the gradients.
  *   block      a block of gs_sample_batch, or one the caller fills: max_* are the sizes, d_num_* device scalars with
  *              the actual ones, or NULL (the sizes are exact; all three together)
  *              The edges are those of the rows: what lies before indptr[0] or behind the last offset has no part

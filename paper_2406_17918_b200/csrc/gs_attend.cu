@@ -17,6 +17,7 @@
 // 4.36 M edges of 4 heads of 32, bf16 (512 bytes gathered per edge): forward 330 us (6.8 TB/s gathered), dq 412 us, dk and dv
 // 564 us, the reversed block 245 us.
 #include <initializer_list>
+#include <type_traits>
 
 #include "gs_device.cuh"
 #include "gs_train.cuh"
@@ -34,6 +35,12 @@ __device__ __forceinline__ float fast_exp2(float x) {
     return y;
 }
 
+// lse in base 2, as the backward passes take it.  A row whose scores are all -inf has lse = -inf like a masked one and no
+// part in any gradient: +inf instead makes its probabilities exp(-inf) = 0.  An edge of probability zero has no part in a
+// sum, not even one of 0 times the infinity that made its score; looking at every edge for it takes 4 to 16 %, so it is done
+// where a sum came out not finite.
+__device__ __forceinline__ float backward_lse(float lse) { return lse == -INFINITY ? INFINITY : lse * LOG2E; }
+
 enum AttendKind { AT_FORWARD, AT_DQ, AT_DKV };
 
 struct Attend {
@@ -45,8 +52,10 @@ struct Attend {
     int tl, slots, units_per_row;
     int tiles;                  // ring kernels: warp-sized tiles of units a warp takes at a time
     int split;                  // rows above AT_CHUNK edges go to the chunk list
+    int dst_split;              // the same of the dq pass, for the pass behind it
     int chunk_mode;             // this launch works through the chunk list
     int32_t* words;             // [0] chunks, [1] long rows
+    int32_t* look;              // set by the dq pass if there are edges of probability zero to look for (ring kernels)
     int2* items;                // chunk -> (row, chunk of the row)
     int4* longs;                // long row -> (row, first chunk, chunks, -)
     float* partial;
@@ -359,7 +368,7 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_dq(const __grid_constant_
                 delta[i] = fmaf(go[i][c], o[c], delta[i]);
                 acc[i][c] = 0.f;
             }
-            lse2[i] = in ? __ldg(P.a.lse + (int64_t)w.row * P.a.q_heads + h0 + i) * LOG2E : 0.f;
+            lse2[i] = in ? backward_lse(__ldg(P.a.lse + (int64_t)w.row * P.a.q_heads + h0 + i)) : 0.f;
         }
         group_sum<G>(delta, P.tl);
         if (in && !P.chunk_mode && slot == 0 && t == 0) {
@@ -368,48 +377,64 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_dq(const __grid_constant_
         }
         const int mine = (w.end - w.begin + P.slots * U - 1) / (P.slots * U);
         const int trips = __reduce_max_sync(FULL, mine);
-        for (int it = 0; it < trips; ++it) {
-            Piece<T, VE, NV> kp[U], vp[U];
-            bool on[U];
+        auto walk = [&](auto look) {
+            for (int it = 0; it < trips; ++it) {
+                Piece<T, VE, NV> kp[U], vp[U];
+                bool on[U];
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const int e = w.begin + (it * U + j) * P.slots + slot;
-                const int col = e < w.end ? __ldg(P.cols + e) : -1;
-                on[j] = (uint32_t)col < (uint32_t)cols;
-                kp[j].load(kbase + (int64_t)col * P.a.k.row_stride + (int64_t)g * P.a.k.head_stride, t, P.tl, D, on[j]);
-                vp[j].load(vbase + (int64_t)col * P.a.v.row_stride + (int64_t)g * P.a.v.head_stride, t, P.tl, D, on[j]);
-            }
-            float s[2 * U * G];
+                for (int j = 0; j < U; ++j) {
+                    const int e = w.begin + (it * U + j) * P.slots + slot;
+                    const int col = e < w.end ? __ldg(P.cols + e) : -1;
+                    on[j] = (uint32_t)col < (uint32_t)cols;
+                    kp[j].load(kbase + (int64_t)col * P.a.k.row_stride + (int64_t)g * P.a.k.head_stride, t, P.tl, D, on[j]);
+                    vp[j].load(vbase + (int64_t)col * P.a.v.row_stride + (int64_t)g * P.a.v.head_stride, t, P.tl, D, on[j]);
+                }
+                float s[2 * U * G];
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
-                float k[E], v[E];
-                kp[j].get(k);
-                vp[j].get(v);
+                for (int j = 0; j < U; ++j) {
+                    float k[E], v[E];
+                    kp[j].get(k);
+                    vp[j].get(v);
 #pragma unroll
-                for (int i = 0; i < G; ++i) {
-                    float x = 0.f, y = 0.f;
+                    for (int i = 0; i < G; ++i) {
+                        float x = 0.f, y = 0.f;
 #pragma unroll
-                    for (int c = 0; c < E; ++c) {
-                        x = fmaf(q[i][c], k[c], x);
-                        y = fmaf(go[i][c], v[c], y);
+                        for (int c = 0; c < E; ++c) {
+                            x = fmaf(q[i][c], k[c], x);
+                            y = fmaf(go[i][c], v[c], y);
+                        }
+                        s[j * G + i] = x;
+                        s[U * G + j * G + i] = y;
                     }
-                    s[j * G + i] = x;
-                    s[U * G + j * G + i] = y;
+                }
+                group_sum<2 * U * G>(s, P.tl);
+#pragma unroll
+                for (int j = 0; j < U; ++j) {
+                    float k[E];
+                    kp[j].get(k);
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        const float p = on[j] ? fast_exp2(fmaf(s[j * G + i], c2, -lse2[i])) : 0.f;
+                        const float ds = on[j] ? p * (s[U * G + j * G + i] - delta[i]) : 0.f;
+                        if (decltype(look)::value && p == 0.f) continue;
+#pragma unroll
+                        for (int c = 0; c < E; ++c) acc[i][c] = fmaf(ds, k[c], acc[i][c]);
+                    }
                 }
             }
-            group_sum<2 * U * G>(s, P.tl);
+        };
+        walk(std::false_type{});
+        bool finite = true;
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
-                float k[E];
-                kp[j].get(k);
+        for (int i = 0; i < G; ++i)
 #pragma unroll
-                for (int i = 0; i < G; ++i) {
-                    const float p = on[j] ? fast_exp2(fmaf(s[j * G + i], c2, -lse2[i])) : 0.f;
-                    const float ds = on[j] ? p * (s[U * G + j * G + i] - delta[i]) : 0.f;
+            for (int c = 0; c < E; ++c) finite = finite && acc[i][c] * 0.f == 0.f;
+        if (!__all_sync(FULL, finite)) {                              // once more, without the edges of probability zero
 #pragma unroll
-                    for (int c = 0; c < E; ++c) acc[i][c] = fmaf(ds, k[c], acc[i][c]);
-                }
-            }
+            for (int i = 0; i < G; ++i)
+#pragma unroll
+                for (int c = 0; c < E; ++c) acc[i][c] = 0.f;
+            walk(std::true_type{});
         }
         for (int o = P.tl; o < width; o <<= 1) {
 #pragma unroll
@@ -460,56 +485,68 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_dkv(const __grid_constant
         for (int c = 0; c < E; ++c) dk[c] = dv[c] = 0.f;
         const int mine = (w.end - w.begin + P.slots * U - 1) / (P.slots * U);
         const int trips = __reduce_max_sync(FULL, mine);
-        for (int h0 = g * group; h0 < (g + 1) * group; h0 += G) {
-            for (int it = 0; it < trips; ++it) {
-                Piece<T, VE, NV> qp[U][G], gp[U][G];
-                float2 st[U][G];
-                bool on[U];
+        auto walk = [&](auto look) {
+            for (int h0 = g * group; h0 < (g + 1) * group; h0 += G) {
+                for (int it = 0; it < trips; ++it) {
+                    Piece<T, VE, NV> qp[U][G], gp[U][G];
+                    float2 st[U][G];
+                    bool on[U];
 #pragma unroll
-                for (int j = 0; j < U; ++j) {
-                    const int e = w.begin + (it * U + j) * P.slots + slot;
-                    const int col = e < w.end ? __ldg(P.cols + e) : -1;
-                    on[j] = (uint32_t)col < (uint32_t)cols;
+                    for (int j = 0; j < U; ++j) {
+                        const int e = w.begin + (it * U + j) * P.slots + slot;
+                        const int col = e < w.end ? __ldg(P.cols + e) : -1;
+                        on[j] = (uint32_t)col < (uint32_t)cols;
 #pragma unroll
-                    for (int i = 0; i < G; ++i) {
-                        qp[j][i].load(qbase + (int64_t)col * P.a.q.row_stride + (int64_t)(h0 + i) * P.a.q.head_stride, t, P.tl, D, on[j]);
-                        gp[j][i].load(gbase + (int64_t)col * P.a.dout.row_stride + (int64_t)(h0 + i) * P.a.dout.head_stride, t, P.tl, D, on[j]);
-                        st[j][i] = on[j] ? __ldg(P.stat + (int64_t)col * P.a.q_heads + h0 + i) : make_float2(0.f, 0.f);
+                        for (int i = 0; i < G; ++i) {
+                            qp[j][i].load(qbase + (int64_t)col * P.a.q.row_stride + (int64_t)(h0 + i) * P.a.q.head_stride, t, P.tl, D, on[j]);
+                            gp[j][i].load(gbase + (int64_t)col * P.a.dout.row_stride + (int64_t)(h0 + i) * P.a.dout.head_stride, t, P.tl, D, on[j]);
+                            st[j][i] = on[j] ? __ldg(P.stat + (int64_t)col * P.a.q_heads + h0 + i) : make_float2(0.f, 0.f);
+                        }
                     }
+                    float s[2 * U * G];
+#pragma unroll
+                    for (int j = 0; j < U; ++j)
+#pragma unroll
+                        for (int i = 0; i < G; ++i) {
+                            float q[E], go[E], x = 0.f, y = 0.f;
+                            qp[j][i].get(q);
+                            gp[j][i].get(go);
+#pragma unroll
+                            for (int c = 0; c < E; ++c) {
+                                x = fmaf(q[c], k[c], x);
+                                y = fmaf(go[c], v[c], y);
+                            }
+                            s[j * G + i] = x;
+                            s[U * G + j * G + i] = y;
+                        }
+                    group_sum<2 * U * G>(s, P.tl);
+#pragma unroll
+                    for (int j = 0; j < U; ++j)
+#pragma unroll
+                        for (int i = 0; i < G; ++i) {
+                            float q[E], go[E];
+                            qp[j][i].get(q);
+                            gp[j][i].get(go);
+                            const float p = on[j] ? fast_exp2(fmaf(s[j * G + i], c2, -st[j][i].x)) : 0.f;
+                            const float ds = on[j] ? p * (s[U * G + j * G + i] - st[j][i].y) : 0.f;
+                            if (decltype(look)::value && p == 0.f) continue;
+#pragma unroll
+                            for (int c = 0; c < E; ++c) {
+                                dv[c] = fmaf(p, go[c], dv[c]);
+                                dk[c] = fmaf(ds, q[c], dk[c]);
+                            }
+                        }
                 }
-                float s[2 * U * G];
-#pragma unroll
-                for (int j = 0; j < U; ++j)
-#pragma unroll
-                    for (int i = 0; i < G; ++i) {
-                        float q[E], go[E], x = 0.f, y = 0.f;
-                        qp[j][i].get(q);
-                        gp[j][i].get(go);
-#pragma unroll
-                        for (int c = 0; c < E; ++c) {
-                            x = fmaf(q[c], k[c], x);
-                            y = fmaf(go[c], v[c], y);
-                        }
-                        s[j * G + i] = x;
-                        s[U * G + j * G + i] = y;
-                    }
-                group_sum<2 * U * G>(s, P.tl);
-#pragma unroll
-                for (int j = 0; j < U; ++j)
-#pragma unroll
-                    for (int i = 0; i < G; ++i) {
-                        float q[E], go[E];
-                        qp[j][i].get(q);
-                        gp[j][i].get(go);
-                        const float p = on[j] ? fast_exp2(fmaf(s[j * G + i], c2, -st[j][i].x)) : 0.f;
-                        const float ds = on[j] ? p * (s[U * G + j * G + i] - st[j][i].y) : 0.f;
-#pragma unroll
-                        for (int c = 0; c < E; ++c) {
-                            dv[c] = fmaf(p, go[c], dv[c]);
-                            dk[c] = fmaf(ds, q[c], dk[c]);
-                        }
-                    }
             }
+        };
+        walk(std::false_type{});
+        bool finite = true;
+#pragma unroll
+        for (int c = 0; c < E; ++c) finite = finite && dk[c] * 0.f == 0.f && dv[c] * 0.f == 0.f;
+        if (!__all_sync(FULL, finite)) {                              // once more, without the edges of probability zero
+#pragma unroll
+            for (int c = 0; c < E; ++c) dk[c] = dv[c] = 0.f;
+            walk(std::true_type{});
         }
         for (int o = P.tl; o < width; o <<= 1) {
 #pragma unroll
@@ -532,6 +569,82 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_dkv(const __grid_constant
     }
 }
 
+// The ring kernels have no second walk over a row's edges.  Their dq pass says whether there may be edges of probability
+// zero to leave out, in a sum that is not finite or a row without weights; the elements that came out not finite are then
+// taken again behind the source-order pass, from p and ds, without those edges and else in the same order.
+struct Again {
+    const Attend& P;
+    // The sum over the edges [b, e), in chunks as the passes take them; part(b, e): over some of them in a row.
+    template <typename F> __device__ float sum(int b, int e, bool split, F part) const {
+        constexpr int W = AT_THREADS / 32;
+        if (!split || e - b <= AT_CHUNK) return part(b, e);
+        const int nc = (e - b + AT_CHUNK - 1) / AT_CHUNK, per = (nc + W - 1) / W;
+        float all = 0.f;
+        for (int c0 = 0; c0 < nc && all == all; c0 += per) {
+            float share = 0.f;
+            for (int c = c0; c < c0 + per && c < nc && share == share; ++c) share += part(b + c * AT_CHUNK, b + (c + 1) * AT_CHUNK < e ? b + (c + 1) * AT_CHUNK : e);
+            all += share;
+        }
+        return all;
+    }
+    template <typename T> __device__ float dq(int b, int e, int h, int col) const {
+        const HeadView& k = P.a.k;
+        const T* from = (const T*)k.data + (int64_t)(h / (P.a.q_heads / P.a.kv_heads)) * k.head_stride + col;
+        const int cols = length_of(P.a.src);
+        return sum(b, e, P.dst_split, [&](int b, int e) {
+            float acc = 0.f;
+            for (int i = b; i < e && acc == acc; ++i) {              // NaN stays
+                const int j = __ldg(P.a.indices + i);
+                if ((uint32_t)j >= (uint32_t)cols) continue;
+                const float2 pd = __ldg(P.pd + (int64_t)i * P.a.q_heads + h);
+                if (pd.x != 0.f) acc = fmaf(pd.y, to_f32(from[(int64_t)j * k.row_stride]), acc);
+            }
+            return acc;
+        }) * P.a.scale;
+    }
+    template <typename T> __device__ float kv(int b, int e, int g, int col, bool dv) const {
+        const HeadView& x = dv ? P.a.dout : P.a.q;
+        const int group = P.a.q_heads / P.a.kv_heads, walk = group % 4 == 0 ? 4 : (group % 2 == 0 ? 2 : 1), cols = length_of(P.a.dst);
+        const float s = sum(b, e, P.split, [&](int b, int e) {
+            float acc = 0.f;
+            for (int h0 = g * group; h0 < (g + 1) * group; h0 += walk)
+                for (int i = b; i < e && acc == acc; ++i) {
+                    const int row = __ldg(P.cols + i), edge = __ldg(P.edges + i);
+                    if ((uint32_t)row >= (uint32_t)cols || (uint32_t)edge >= (uint32_t)P.edge_bound) continue;
+                    for (int h = h0; h < h0 + walk; ++h) {
+                        const float2 pd = __ldg(P.pd + (int64_t)edge * P.a.q_heads + h);
+                        if (pd.x != 0.f) acc = fmaf(dv ? pd.x : pd.y, to_f32(((const T*)x.data)[(int64_t)row * x.row_stride + (int64_t)h * x.head_stride + col]), acc);
+                    }
+                }
+            return acc;
+        });
+        return dv ? s : s * P.a.scale;
+    }
+    // Offsets of a row within the edges.
+    __device__ int2 range(const int32_t* starts, int row) const {
+        const int b = __ldg(starts + row), e = __ldg(starts + row + 1), b1 = b < 0 ? 0 : b, e1 = e > P.edge_bound ? P.edge_bound : e;
+        return make_int2(b1, e1 < b1 ? b1 : e1);
+    }
+    // The rows of a gradient, a warp per (row, head); without `longs`, those of chunks are looked at where they are joined.
+    template <typename T, typename F> __device__ void rows(const HeadView& v, const int32_t* starts, int n, int heads, bool longs, F again) const {
+        const int lane = threadIdx.x & 31;
+        for (int64_t u = ((int64_t)blockIdx.x * AT_THREADS + threadIdx.x) / 32; u < (int64_t)n * heads; u += (int64_t)gridDim.x * AT_THREADS / 32) {
+            const int row = (int)(u / heads), h = (int)(u - (int64_t)row * heads);
+            const int2 r = range(starts, row);
+            if (!longs && r.y - r.x > AT_CHUNK) continue;
+            T* x = (T*)v.data + (int64_t)row * v.row_stride + (int64_t)h * v.head_stride;
+            for (int col = lane; col < P.a.head_dim; col += 32)
+                if (to_f32(x[col]) * 0.f != 0.f) x[col] = from_f32<T>(again(r.x, r.y, h, col));
+        }
+    }
+    template <typename T> __device__ void all() const {
+        const int n = length_of(P.a.dst), src = length_of(P.a.src);
+        rows<T>(P.a.dq, P.a.indptr, n, P.a.q_heads, true, [&](int b, int e, int h, int col) { return dq<T>(b, e, h, col); });
+        rows<T>(P.a.dk, P.starts, src, P.a.kv_heads, !P.split, [&](int b, int e, int h, int col) { return kv<T>(b, e, h, col, false); });
+        rows<T>(P.a.dv, P.starts, src, P.a.kv_heads, !P.split, [&](int b, int e, int h, int col) { return kv<T>(b, e, h, col, true); });
+    }
+};
+
 // Chunk sums of long rows added in order: one block per (row, head), its warps over shares of the chunks.  dq: one operand
 // of width D; dk and dv: width 2 D, the second half for dv.
 template <typename T, bool KV> __global__ void __launch_bounds__(AT_THREADS) k_attend_sum_join(const __grid_constant__ Attend P) {
@@ -540,6 +653,9 @@ template <typename T, bool KV> __global__ void __launch_bounds__(AT_THREADS) k_a
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = P.a.head_dim;
     const int heads = KV ? P.a.kv_heads : P.a.q_heads, width = KV ? 2 * D : D;
     const int64_t units = (int64_t)__ldcg(P.words + 1) * heads, stride = (int64_t)heads * width;
+    const Again again{P};
+    const bool look = KV && __ldcg(P.look) != 0;
+    if (look) again.all<T>();
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
         const int4 row = P.longs[u / heads];
         const int h = (int)(u % heads);
@@ -558,6 +674,10 @@ template <typename T, bool KV> __global__ void __launch_bounds__(AT_THREADS) k_a
             for (int w = 0; w < W; ++w) acc += s_acc[w][col];
             const HeadView& to = !KV ? P.a.dq : (col < D ? P.a.dk : P.a.dv);
             if (!KV || col < D) acc *= P.a.scale;
+            if (look && acc * 0.f != 0.f) {
+                const int2 r = again.range(P.starts, row.x);
+                acc = again.kv<T>(r.x, r.y, h, col < D ? col : col - D, col >= D);
+            }
             ((T*)to.data)[(int64_t)row.x * to.row_stride + (int64_t)h * to.head_stride + (col < D ? col : col - D)] = from_f32<T>(acc);
         }
     }
@@ -733,8 +853,8 @@ template <AttendKind K, typename T, int VE, int NV, int G> static cudaError_t ru
         kernel<<<(int)limit_grid(blocks > cap ? cap : blocks), RING_WARPS * 32, smem, s>>>(P);
         count_launches(1);
     }
-    if (P.split) {
-        const int grid = (int)limit_grid(sm_count() * 8);
+    if (P.split || K == AT_DKV) {                             // behind the source-order pass also what has to be taken again
+        const int grid = (int)limit_grid(sm_count() * (K == AT_DKV ? 4 : 8));
         if constexpr (K == AT_FORWARD) k_attend_forward_join<T><<<grid, AT_THREADS, 0, s>>>(P);
         else k_attend_sum_join<T, K == AT_DKV><<<grid, AT_THREADS, 0, s>>>(P);
         count_launches(1);
@@ -752,10 +872,6 @@ template <AttendKind K, typename T, int VE, int NV> static cudaError_t ring_grou
 
 template <AttendKind K> static cudaError_t run_kind(Attend& P, int ve, int64_t rows, int64_t row_hint, cudaStream_t s) {
     const int D = P.a.head_dim;
-    if (P.split) {
-        const cudaError_t e = cudaMemsetAsync(P.words, 0, 8, s);
-        if (e != cudaSuccess) return e;
-    }
     // pieces of 16 or 8 bytes: the ring kernels; else one element at a time
     if (P.a.dtype == GS_BF16) {
         if (ve == 8) return ring_group<K, bf16, 8, 1>(P, rows, s);
@@ -798,6 +914,8 @@ cudaError_t launch_attention_forward(const BlockAttention& a, void* workspace, c
     P.rows = a.dst;
     P.columns = a.src;
     P.split = (a.max_row == 0 || a.max_row > AT_CHUNK) && a.edge_bound > AT_CHUNK;
+    const cudaError_t e = P.split ? cudaMemsetAsync(P.words, 0, 8, s) : cudaSuccess;
+    if (e != cudaSuccess) return e;
     return run_kind<AT_FORWARD>(P, wide_elems(a, {&a.q, &a.k, &a.v, &a.out}), a.dst.bound, a.max_row, s);
 }
 
@@ -810,8 +928,14 @@ cudaError_t launch_attention_backward(const BlockAttention& a, const int32_t* re
     P.rows = a.dst;
     P.columns = a.src;
     P.split = (a.max_row == 0 || a.max_row > AT_CHUNK) && a.edge_bound > AT_CHUNK;
-    cudaError_t e = run_kind<AT_DQ>(P, ve, a.dst.bound, a.max_row, s);
+    // the words of both passes, cleared at once
+    int32_t* kv_words = P.words + 2;
+    P.look = P.words + 4;
+    cudaError_t e = cudaMemsetAsync(P.words, 0, 5 * 4, s);
+    if (e == cudaSuccess) e = run_kind<AT_DQ>(P, ve, a.dst.bound, a.max_row, s);
     if (e != cudaSuccess) return e;
+    P.words = kv_words;
+    P.dst_split = P.split;
     P.starts = rev_indptr;
     P.cols = rev_dst;
     P.edges = rev_edge;

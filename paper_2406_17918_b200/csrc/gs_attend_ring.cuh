@@ -40,6 +40,16 @@ template <int N> __device__ __forceinline__ void unpair(const f32x2 (&x)[N], flo
     for (int i = 0; i < N; ++i) split(x[i], y[2 * i], y[2 * i + 1]);
 }
 
+// No element is infinite or NaN: a product with zero is zero.
+template <int N> __device__ __forceinline__ bool all_finite(const f32x2 (&x)[N]) {
+    f32x2 z = mul2(x[0], pair(0.f, 0.f));
+#pragma unroll
+    for (int i = 1; i < N; ++i) z = fma2(x[i], pair(0.f, 0.f), z);
+    float lo, hi;
+    split(z, lo, hi);
+    return lo + hi == 0.f;
+}
+
 // The sums over the tl lanes of a group, in every lane; straight code for the usual widths.
 template <int N, int TL> __device__ __forceinline__ void group_sum_of(float (&x)[N]) {
 #pragma unroll
@@ -97,7 +107,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
     int size[NV];                                                                   // bytes of this lane's pieces: 0 behind the row's end
 #pragma unroll
     for (int n = 0; n < NV; ++n) size[n] = (t + n * tl) * VE < D ? PB : 0;
-    enum : uint32_t { LIVE = 1, FIRST = 2, LAST = 4, HEAD = 8 };                    // a batch: flags | edges << 4 | local row << 8 | head << 16 | walk << 24
+    enum : uint32_t { LIVE = 1, FIRST = 2, LAST = 4, HEAD = 8, EDGES = 15 << 4 };                    // a batch: flags | edges << 4 | local row << 8 | head << 16 | walk << 24
 
     // a warp takes P.tiles tiles of gpw consecutive units at a time
     const int64_t span = (int64_t)P.tiles * gpw;
@@ -392,7 +402,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                             pieces(slot, U * S::EDGE + i * NV, x0[i]);
                             pieces(slot, U * S::EDGE + (G + i) * NV, x1[i]);
                             pieces(slot, U * S::EDGE + (2 * G + i) * NV, o);
-                            m[i] = *reinterpret_cast<const float*>(mine + slot * S::SLOT + S::PIECES + (i * 32 + lane) * 4) * LOG2E;
+                            m[i] = backward_lse(*reinterpret_cast<const float*>(mine + slot * S::SLOT + S::PIECES + (i * 32 + lane) * 4));
                             delta[i] = dot2(x1[i], o);
 #pragma unroll
                             for (int c = 0; c < N2; ++c) acc[i][c] = 0;
@@ -406,6 +416,9 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                     }
                     __syncwarp();
                 }
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+                    if (m[i] == INFINITY && (batch & EDGES)) *P.look = 1;       // edges, but no weights
                 float s[2 * U * G];
 #pragma unroll
                 for (int j = 0; j < U; ++j) {
@@ -437,6 +450,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
 #pragma unroll
                         for (int i = 0; i < G; ++i) {
                             const int hh = h * G + i;
+                            if (!all_finite(acc[i])) *P.look = 1;
                             if (!P.chunk_mode) scale2(P.a.scale, acc[i]);
                             float o[E];
                             unpair(acc[i], o);
