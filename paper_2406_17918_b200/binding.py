@@ -685,6 +685,22 @@ def _ids_1d(t: torch.Tensor, what: str) -> torch.Tensor:
     return t
 
 
+def _counter(t: torch.Tensor, what: str):
+    """Address of a device scalar (None: there is none)."""
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or not t.is_cuda or t.numel() < 1:
+        raise TypeError("%s must be an int32 CUDA tensor of one element" % what)
+    return t.data_ptr()
+
+
+def _workspace(t: torch.Tensor):
+    """(address, bytes) of a call's workspace."""
+    if t.dtype is not torch.uint8 or not t.is_cuda or not t.is_contiguous():
+        raise TypeError("workspace must be a contiguous uint8 CUDA tensor")
+    return t.data_ptr(), t.numel()
+
+
 def _ld(t: torch.Tensor) -> int:
     """Row pitch; a single row may carry any stride."""
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
@@ -703,7 +719,7 @@ def gs_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1
         if out.shape[0] < ids.numel() or out.shape[1] != table.shape[1]:
             raise ValueError("out must be [len(ids), dim]")
     _check(_L.gs_embedding_lookup(_addr(table), _dtype(table.dtype), table.shape[0], table.shape[1], _ld(table), _addr(ids),
-                                  _addr(count), ids.numel(), float(scale), _addr(out), _dtype(out.dtype), _ld(out),
+                                  _counter(count, "count"), ids.numel(), float(scale), _addr(out), _dtype(out.dtype), _ld(out),
                                   _on(stream, out)))
     return out
 
@@ -732,9 +748,9 @@ def gs_embedding_backward(dout: torch.Tensor, ids: torch.Tensor, table_rows: int
         _rows_2d(out, "out")
         if tuple(out.shape) != (int(table_rows), dout.shape[1]):
             raise ValueError("out must be [table_rows, dim]")
-    _check(_L.gs_embedding_backward(_addr(dout), _dtype(dout.dtype), _ld(dout), _addr(ids), _addr(count), ids.numel(),
+    _check(_L.gs_embedding_backward(_addr(dout), _dtype(dout.dtype), _ld(dout), _addr(ids), _counter(count, "count"), ids.numel(),
                                     int(table_rows), dout.shape[1], float(scale), _addr(out), _dtype(out.dtype), _ld(out),
-                                    _addr(workspace), workspace.numel(), _on(stream, workspace)))
+                                    *_workspace(workspace), _on(stream, workspace)))
     return out
 
 
@@ -755,16 +771,16 @@ def gs_embedding_backward_sparse(dout: torch.Tensor, ids: torch.Tensor, table_ro
     _rows_2d(grad, "grad")
     if rows.numel() < n or grad.shape[0] < n or grad.shape[1] != d:
         raise ValueError("rows / grad must hold one entry per id")
-    _check(_L.gs_embedding_backward_sparse(_addr(dout), _dtype(dout.dtype), _ld(dout), _addr(ids), _addr(count), n, int(table_rows), d,
-                                           float(scale), _addr(rows), _addr(num_rows), _addr(grad), _dtype(grad.dtype), _ld(grad),
-                                           _addr(workspace), workspace.numel(), _on(stream, workspace)))
+    _check(_L.gs_embedding_backward_sparse(_addr(dout), _dtype(dout.dtype), _ld(dout), _addr(ids), _counter(count, "count"), n, int(table_rows), d,
+                                           float(scale), _addr(rows), _counter(num_rows, "num_rows"), _addr(grad), _dtype(grad.dtype), _ld(grad),
+                                           *_workspace(workspace), _on(stream, workspace)))
     return rows, num_rows, grad
 
 
 def _csr_block(indptr, indices, num_src, counts):
     _ids_1d(indptr, "indptr")
     _ids_1d(indices, "indices")
-    nd, ns, ne = (None, None, None) if counts is None else (c.data_ptr() for c in counts)
+    nd, ns, ne = (None, None, None) if counts is None else (_counter(c, "each of counts") for c in counts)
     return _CBlock(indptr.numel() - 1, int(num_src), indices.numel(), nd, ns, ne, indptr.data_ptr(), indices.data_ptr())
 
 
@@ -807,13 +823,12 @@ def gs_block_attention_forward(indptr: torch.Tensor, indices: torch.Tensor, q: t
         out = _new((n, hq, d), q.dtype, q, stream, None if exact else 0)
     if lse is None:
         lse = _new((n, hq), torch.float32, q, stream, None if exact else -math.inf)
-    elif lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape[0] < b.max_dst or lse.shape[1] != hq:
+    elif lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.shape[0] < b.max_dst or lse.shape[1] != hq:
         raise TypeError("lse must be a contiguous float32 tensor [dst, q_heads]")
     keep, (pq, pk, pv, po) = _heads(q.dtype, (q, "q", b.max_dst, hq, d), (k, "k", b.max_src, hk, d), (v, "v", b.max_src, hk, d),
                                     (out, "out", b.max_dst, hq, d))
     _check(_L.gs_block_attention_forward(ctypes.byref(b), int(max_row), _dtype(q.dtype), hq, hk, d,
-                                         d ** -0.5 if scale is None else float(scale), pq, pk, pv, po, _addr(lse), _addr(workspace),
-                                         workspace.numel(), _on(stream, workspace)))
+                                         d ** -0.5 if scale is None else float(scale), pq, pk, pv, po, _addr(lse), *_workspace(workspace), _on(stream, workspace)))
     return out, lse
 
 
@@ -831,7 +846,7 @@ def gs_block_reverse(indptr: torch.Tensor, indices: torch.Tensor, num_src: int, 
     if _ids_1d(rev_indptr, "rev_indptr").numel() < b.max_src + 1 or _ids_1d(rev_dst, "rev_dst").numel() < b.max_edges or \
             _ids_1d(rev_edge, "rev_edge").numel() < b.max_edges:
         raise ValueError("rev_indptr / rev_dst / rev_edge are too small")
-    _check(_L.gs_block_reverse(ctypes.byref(b), _addr(rev_indptr), _addr(rev_dst), _addr(rev_edge), _addr(workspace), workspace.numel(), _on(stream, workspace)))
+    _check(_L.gs_block_reverse(ctypes.byref(b), _addr(rev_indptr), _addr(rev_dst), _addr(rev_edge), *_workspace(workspace), _on(stream, workspace)))
     return rev_indptr, rev_dst, rev_edge
 
 
@@ -860,7 +875,7 @@ def gs_block_attention_backward(indptr: torch.Tensor, indices: torch.Tensor, rev
         (dout, "dout", b.max_dst, hq, d), (dq, "dq", b.max_dst, hq, d), (dk, "dk", b.max_src, hk, d), (dv, "dv", b.max_src, hk, d))
     _check(_L.gs_block_attention_backward(ctypes.byref(b), int(max_row), _addr(rev_indptr), _addr(rev_dst), _addr(rev_edge), _dtype(t), hq, hk, d,
                                           d ** -0.5 if scale is None else float(scale), pq, pk, pv, po, _addr(lse), pdo, pdq, pdk, pdv,
-                                          _addr(workspace), workspace.numel(), _on(stream, workspace)))
+                                          *_workspace(workspace), _on(stream, workspace)))
     return dq, dk, dv
 
 
@@ -894,7 +909,7 @@ def gs_xent_forward(hidden: torch.Tensor, table: torch.Tensor, labels: torch.Ten
     loss = _new(n, torch.float32, hidden, stream) if loss is None else _f32_rows(loss, "loss", n)
     lse = _new(n, torch.float32, hidden, stream) if lse is None else _f32_rows(lse, "lse", n)
     _check(_L.gs_xent_forward(_addr(hidden), _ld(hidden), _addr(table), _ld(table), _dtype(hidden.dtype), n, table.shape[0], hidden.shape[1],
-                              float(scale), _addr(labels), _addr(loss), _addr(lse), _addr(workspace), workspace.numel(), _on(stream, workspace)))
+                              float(scale), _addr(labels), _addr(loss), _addr(lse), *_workspace(workspace), _on(stream, workspace)))
     return loss, lse
 
 
@@ -913,7 +928,7 @@ def gs_xent_backward(hidden: torch.Tensor, table: torch.Tensor, labels: torch.Te
         raise ValueError("dhidden / dtable must have the shapes of hidden / table and one dtype")
     _check(_L.gs_xent_backward(_addr(hidden), _ld(hidden), _addr(table), _ld(table), _dtype(hidden.dtype), n, table.shape[0], d, float(scale),
                                _addr(labels), _addr(lse), _addr(dloss), _addr(dhidden), _ld(dhidden), _addr(dtable), _ld(dtable),
-                               _dtype(dhidden.dtype), _addr(workspace), workspace.numel(), _on(stream, workspace)))
+                               _dtype(dhidden.dtype), *_workspace(workspace), _on(stream, workspace)))
     return dhidden, dtable
 
 
