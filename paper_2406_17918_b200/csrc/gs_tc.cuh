@@ -26,17 +26,17 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     return done != 0;
 }
 
-// Waits for the phase with this parity to complete; gives up (false) once `stop` is set or after about two seconds,
-// and then sets `stop`, so that every role of the block leaves its loop.
+// Waits for the phase with this parity to complete; gives up (false) once `stop` is set or after `limit` clocks (about two
+// seconds), and then sets `stop`, so that every role of the block leaves its loop.
 constexpr long long WAIT_CLOCKS = 4000000000ll;
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* stop) {
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* stop, long long limit = WAIT_CLOCKS) {
     if (mbar_try(bar, parity)) return true;
     const long long begin = clock64();
     for (;;) {
         for (int i = 0; i < 64; ++i)
             if (mbar_try(bar, parity)) return true;
         if (*stop) return false;
-        if (clock64() - begin > WAIT_CLOCKS) {
+        if (clock64() - begin > limit) {
             *stop = 1;
             return false;
         }

@@ -29,6 +29,7 @@ constexpr int XT_THREADS = 640;            // 4 warps of roles, 4 softmax warpgr
 constexpr int XT_CHUNK = XT * 128;         // bytes of a tile's 64 columns
 constexpr int XT_MAX_STAGES = 8;
 constexpr int XT_SHORT_ROWS = 16;          // rows of fewer tiles than this get two O
+constexpr long long XT_UNIT_CLOCKS = 1000000;   // more than five hundred times what a unit takes
 constexpr float XT_LOG2E = 1.4426950408889634f;
 
 __device__ int g_xent_gave_up;
@@ -422,9 +423,13 @@ __global__ void __launch_bounds__(XT_THREADS, 1) k_xent_tc(const __grid_constant
         uint32_t parity = 0;
         char* grad = (char*)(M == TC_DHIDDEN ? P.a.dhidden : P.a.dtable);
         const int64_t ld = (M == TC_DHIDDEN ? P.a.dhidden_ld : P.a.dtable_ld) * 2;
+        long long units = 0;                               // since the last finished tile
         while (ok && seg.next(run, xi, y0, n)) {
+            units += n;
             if (y0 != 0 || n != P.runs.tiles_y || !stages_tile(xi)) continue;
-            ok = __all_sync(FULL, tc::mbar_wait(staged, parity, &s_stop));
+            // the other roles wait for units, this one for whole rows of them: a table of 320 M rows takes over two seconds
+            ok = __all_sync(FULL, tc::mbar_wait(staged, parity, &s_stop, tc::WAIT_CLOCKS + units * XT_UNIT_CLOCKS));
+            units = 0;
             if (!ok) break;
             parity ^= 1;
             if (P.out == OUT_ROWS) {
