@@ -76,11 +76,11 @@ def train(config: str = "tiny", steps: int = 50, lr: float = 0.02, log=print):
         loss = model.loss(hidden, neighbour_targets(graph, seeds, rng)).mean()
         optimizer.zero_grad(set_to_none=True)
         loss.backward()
+        gs.gs_train_status()                                 # synchronises; no step on gradients that a kernel did not finish
         optimizer.step()
         history.append(float(loss.detach()))
         if step % 10 == 0 or step + 1 == steps:
             log("step %4d  input nodes %6d  loss %.4f" % (step, n[hops], history[-1]))
-    gs.gs_train_status()
     return history
 
 

@@ -548,7 +548,10 @@ gs_status gs_xent_backward(const void* d_hidden, int64_t hidden_ld, const void* 
                            const float* d_dloss, void* d_dhidden, int64_t dhidden_ld, void* d_dtable, int64_t dtable_ld,
                            gs_dtype grad_dtype, void* d_workspace, size_t workspace_bytes, void* stream);
 
-/* Synchronises `stream`; GS_ERR_CUDA if a kernel of the training operators ever gave up one of its (bounded) waits. */
+/* Synchronises `stream`; GS_ERR_CUDA if a kernel of the training operators ever gave up one of its (bounded) waits.  Such a
+ * kernel leaves its results partly unwritten, and the call that launched it has long returned GS_OK: gs_xent_forward's and
+ * gs_xent_backward's results for bf16 operands hold only if this passes after them (before a step is kept, say).  Once set,
+ * the state stays for the process. */
 gs_status gs_train_status(void* stream);
 
 /* Number of kernels this library has launched in the calling process (monotonic). */

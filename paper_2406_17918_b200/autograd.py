@@ -115,5 +115,6 @@ class _TableCrossEntropy(torch.autograd.Function):
 
 
 def table_cross_entropy(hidden: torch.Tensor, table: torch.Tensor, labels: torch.Tensor, scale: float = 1.0):
-    """Cross entropy per row of softmax(scale * hidden table^T); labels outside the table give 0 and no gradient."""
+    """Cross entropy per row of softmax(scale * hidden table^T); labels outside the table give 0 and no gradient.  Results of
+    bf16 operands hold if ``gs_train_status()`` passes after them (it synchronises: call it where a step is kept anyway)."""
     return _TableCrossEntropy.apply(hidden, table, labels, float(scale))

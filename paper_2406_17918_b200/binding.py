@@ -933,5 +933,6 @@ def gs_xent_backward(hidden: torch.Tensor, table: torch.Tensor, labels: torch.Te
 
 
 def gs_train_status(stream=None):
-    """Synchronises; raises if a kernel of the training operators ever gave up waiting."""
+    """Synchronises; raises if a kernel of the training operators ever gave up waiting, and so left results partly unwritten:
+    call it before they are kept."""
     _check(_L.gs_train_status((torch.cuda.current_stream() if stream is None else stream).cuda_stream))
