@@ -535,6 +535,7 @@ gs_status gs_block_attention_backward(const gs_block* block, int32_t max_row, co
  *   lse[n] = log sum_v exp(z[n, v]),  loss[n] = lse[n] - z[n, labels[n]];  a label outside [0, vocab): loss 0, no gradient
  * gs_xent_backward takes the upstream gradient dloss[n] and the forward's lse, recomputes the logits, and writes
  *   dz = dloss[n] * scale * (exp(z - lse[n]) - [v == labels[n]]),  dhidden = dz table,  dtable = dz^T hidden
+ * A row without a valid label has no part in the gradients, whatever its hidden row holds (rows behind a batch's size, say).
  *   d_hidden [rows][hidden_ld], d_table [vocab][table_ld] of `dtype`; gradients of `grad_dtype`; loss, lse, dloss float[rows]
  *   0 <= rows < 2^31 - 256, 1 <= vocab < 2^31 - 256, 1 <= dim <= 4096
  * f32 operands are multiplied in 32 bits.  bf16 operands with dim <= 256 (and, where dim is a multiple of 8, bases and

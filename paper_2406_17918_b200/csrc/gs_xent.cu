@@ -146,7 +146,9 @@ __global__ void __launch_bounds__(XS_THREADS) k_xent_simt(const __grid_constant_
                         float* yc = &xs[0][0];                         // [16][132], over xs
                         for (int i = threadIdx.x; i < 16 * XS_COLS; i += XS_THREADS) {
                             const int r = i / XS_COLS, c = i % XS_COLS;
-                            yc[r * (XS_COLS + 4) + c] = y0 + k0 + r < ny && col0 + c < d ? to_f32(Y[(int64_t)(y0 + k0 + r) * yld + col0 + c]) : 0.f;
+                            // a hidden row without a label may hold anything: zeros
+                            const bool on = y0 + k0 + r < ny && col0 + c < d && (ON_X || s_label[k0 + r] >= 0);
+                            yc[r * (XS_COLS + 4) + c] = on ? to_f32(Y[(int64_t)(y0 + k0 + r) * yld + col0 + c]) : 0.f;
                         }
                         __syncthreads();
 #pragma unroll
