@@ -41,6 +41,15 @@ __device__ __forceinline__ float fast_exp2(float x) {
 // where a sum came out not finite.
 __device__ __forceinline__ float backward_lse(float lse) { return lse == -INFINITY ? INFINITY : lse * LOG2E; }
 
+// delta = do . o is taken from `out`, which a caller of bf16 holds rounded: off by up to 2^-9 of sum |do||o|, which ds of a
+// row of few edges, or of one probability near 1, does not bear (2.5 times the error of dq and dk at 179 rows of mostly one to three
+// edges).  The dq pass therefore also sums r = sum p (dp - delta), which is 0 for the right delta, and sum p k, and corrects
+// itself: dq = sum p (dp - delta) k - r sum p k.  The pass behind it adds r to delta (the "shift").  262,144 rows of 4 x 32: dq 410 ->
+// 457 us, dk and dv 552 -> 606 (ds rewritten at a row's end instead: 609 and 552).  f32: nothing to correct.
+template <typename T> constexpr bool rounded_out = sizeof(T) == 2;
+// Floats of a chunk's part of dq, per head: the sum; and sum p k and r.
+template <typename T> __device__ __forceinline__ int dq_part(int dim) { return rounded_out<T> ? 2 * dim + 1 : dim; }
+
 enum AttendKind { AT_FORWARD, AT_DQ, AT_DKV };
 
 struct Attend {
@@ -60,6 +69,7 @@ struct Attend {
     int4* longs;                // long row -> (row, first chunk, chunks, -)
     float* partial;
     float2* stat;               // [dst][q heads]: lse in base 2, delta (one-element kernels)
+    float* shift;               // [dst][q heads]: what is missing in the dq pass's delta (ring kernels; else NULL)
     float2* pd;                 // [edges][q heads]: p and ds before the scale, from the dq pass (ring kernels)
     const int32_t* edges;       // source-order pass: the edge each column came from
 };
@@ -351,7 +361,9 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_dq(const __grid_constant_
         const Work w = find_work(P, u, units, t == 0 && slot == 0);
         const bool in = u < units;
         const int h0 = w.unit * G, g = h0 / (P.a.q_heads / P.a.kv_heads);
+        constexpr bool SHIFTED = rounded_out<T>;
         float q[G][E], go[G][E], acc[G][E], lse2[G], delta[G];
+        float pk[SHIFTED ? G : 1][SHIFTED ? E : 1], miss[G];
 #pragma unroll
         for (int i = 0; i < G; ++i) {
             Piece<T, VE, NV> p;
@@ -367,7 +379,9 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_dq(const __grid_constant_
             for (int c = 0; c < E; ++c) {
                 delta[i] = fmaf(go[i][c], o[c], delta[i]);
                 acc[i][c] = 0.f;
+                if constexpr (SHIFTED) pk[i][c] = 0.f;
             }
+            miss[i] = 0.f;
             lse2[i] = in ? backward_lse(__ldg(P.a.lse + (int64_t)w.row * P.a.q_heads + h0 + i)) : 0.f;
         }
         group_sum<G>(delta, P.tl);
@@ -418,7 +432,11 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_dq(const __grid_constant_
                         const float ds = on[j] ? p * (s[U * G + j * G + i] - delta[i]) : 0.f;
                         if (decltype(look)::value && p == 0.f) continue;
 #pragma unroll
-                        for (int c = 0; c < E; ++c) acc[i][c] = fmaf(ds, k[c], acc[i][c]);
+                        for (int c = 0; c < E; ++c) {
+                            acc[i][c] = fmaf(ds, k[c], acc[i][c]);
+                            if constexpr (SHIFTED) pk[i][c] = fmaf(p, k[c], pk[i][c]);
+                        }
+                        miss[i] += ds;
                     }
                 }
             }
@@ -431,26 +449,45 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_dq(const __grid_constant_
             for (int c = 0; c < E; ++c) finite = finite && acc[i][c] * 0.f == 0.f;
         if (!__all_sync(FULL, finite)) {                              // once more, without the edges of probability zero
 #pragma unroll
-            for (int i = 0; i < G; ++i)
+            for (int i = 0; i < G; ++i) {
+                miss[i] = 0.f;
 #pragma unroll
-                for (int c = 0; c < E; ++c) acc[i][c] = 0.f;
+                for (int c = 0; c < E; ++c) {
+                    acc[i][c] = 0.f;
+                    if constexpr (SHIFTED) pk[i][c] = 0.f;
+                }
+            }
             walk(std::true_type{});
         }
         for (int o = P.tl; o < width; o <<= 1) {
 #pragma unroll
-            for (int i = 0; i < G; ++i)
+            for (int i = 0; i < G; ++i) {
+                if constexpr (SHIFTED) miss[i] += __shfl_xor_sync(FULL, miss[i], o);
 #pragma unroll
-                for (int c = 0; c < E; ++c) acc[i][c] += __shfl_xor_sync(FULL, acc[i][c], o);
+                for (int c = 0; c < E; ++c) {
+                    acc[i][c] += __shfl_xor_sync(FULL, acc[i][c], o);
+                    if constexpr (SHIFTED) pk[i][c] += __shfl_xor_sync(FULL, pk[i][c], o);
+                }
+            }
         }
         if (!w.live || slot) continue;
 #pragma unroll
         for (int i = 0; i < G; ++i) {
             const int h = h0 + i;
             if (P.chunk_mode) {
-                store_partial<VE, NV>(P.partial + ((int64_t)w.item * P.a.q_heads + h) * D, t, P.tl, D, acc[i]);
+                float* part = P.partial + ((int64_t)w.item * P.a.q_heads + h) * dq_part<T>(D);
+                store_partial<VE, NV>(part, t, P.tl, D, acc[i]);
+                if constexpr (SHIFTED) {
+                    store_partial<VE, NV>(part + D, t, P.tl, D, pk[i]);
+                    if (t == 0) part[2 * D] = miss[i];
+                }
             } else {
+                if (SHIFTED && t == 0) P.stat[(int64_t)w.row * P.a.q_heads + h] = make_float2(lse2[i], delta[i] + miss[i]);
 #pragma unroll
-                for (int c = 0; c < E; ++c) acc[i][c] *= P.a.scale;
+                for (int c = 0; c < E; ++c) {
+                    if constexpr (SHIFTED) acc[i][c] = fmaf(-miss[i], pk[i][c], acc[i][c]);
+                    acc[i][c] *= P.a.scale;
+                }
                 store_piece<T, VE, NV>((T*)P.a.dq.data + (int64_t)w.row * P.a.dq.row_stride + (int64_t)h * P.a.dq.head_stride, t, P.tl, D, acc[i]);
             }
         }
@@ -587,20 +624,24 @@ struct Again {
         }
         return all;
     }
-    template <typename T> __device__ float dq(int b, int e, int h, int col) const {
+    template <typename T> __device__ float dq(int row, int b, int e, int h, int col) const {
         const HeadView& k = P.a.k;
         const T* from = (const T*)k.data + (int64_t)(h / (P.a.q_heads / P.a.kv_heads)) * k.head_stride + col;
         const int cols = length_of(P.a.src);
-        return sum(b, e, P.dst_split, [&](int b, int e) {
-            float acc = 0.f;
-            for (int i = b; i < e && acc == acc; ++i) {              // NaN stays
-                const int j = __ldg(P.a.indices + i);
-                if ((uint32_t)j >= (uint32_t)cols) continue;
-                const float2 pd = __ldg(P.pd + (int64_t)i * P.a.q_heads + h);
-                if (pd.x != 0.f) acc = fmaf(pd.y, to_f32(from[(int64_t)j * k.row_stride]), acc);
-            }
-            return acc;
-        }) * P.a.scale;
+        auto over = [&](bool pk) {                                   // sum p (dp - delta) k, or sum p k
+            return sum(b, e, P.dst_split, [&](int b, int e) {
+                float acc = 0.f;
+                for (int i = b; i < e && acc == acc; ++i) {          // NaN stays
+                    const int j = __ldg(P.a.indices + i);
+                    if ((uint32_t)j >= (uint32_t)cols) continue;
+                    const float2 pd = __ldg(P.pd + (int64_t)i * P.a.q_heads + h);
+                    if (pd.x != 0.f) acc = fmaf(pk ? pd.x : pd.y, to_f32(from[(int64_t)j * k.row_stride]), acc);
+                }
+                return acc;
+            });
+        };
+        const float acc = over(false), pk = rounded_out<T> ? over(true) : 0.f;
+        return (pk != 0.f ? fmaf(-__ldg(P.shift + (int64_t)row * P.a.q_heads + h), pk, acc) : acc) * P.a.scale;
     }
     template <typename T> __device__ float kv(int b, int e, int g, int col, bool dv) const {
         const HeadView& x = dv ? P.a.dout : P.a.q;
@@ -613,7 +654,9 @@ struct Again {
                     if ((uint32_t)row >= (uint32_t)cols || (uint32_t)edge >= (uint32_t)P.edge_bound) continue;
                     for (int h = h0; h < h0 + walk; ++h) {
                         const float2 pd = __ldg(P.pd + (int64_t)edge * P.a.q_heads + h);
-                        if (pd.x != 0.f) acc = fmaf(dv ? pd.x : pd.y, to_f32(((const T*)x.data)[(int64_t)row * x.row_stride + (int64_t)h * x.head_stride + col]), acc);
+                        if (pd.x == 0.f) continue;
+                        const float ds = rounded_out<T> ? fmaf(-pd.x, __ldg(P.shift + (int64_t)row * P.a.q_heads + h), pd.y) : pd.y;
+                        acc = fmaf(dv ? pd.x : ds, to_f32(((const T*)x.data)[(int64_t)row * x.row_stride + (int64_t)h * x.head_stride + col]), acc);
                     }
                 }
             return acc;
@@ -634,14 +677,14 @@ struct Again {
             if (!longs && r.y - r.x > AT_CHUNK) continue;
             T* x = (T*)v.data + (int64_t)row * v.row_stride + (int64_t)h * v.head_stride;
             for (int col = lane; col < P.a.head_dim; col += 32)
-                if (to_f32(x[col]) * 0.f != 0.f) x[col] = from_f32<T>(again(r.x, r.y, h, col));
+                if (to_f32(x[col]) * 0.f != 0.f) x[col] = from_f32<T>(again(row, r.x, r.y, h, col));
         }
     }
     template <typename T> __device__ void all() const {
         const int n = length_of(P.a.dst), src = length_of(P.a.src);
-        rows<T>(P.a.dq, P.a.indptr, n, P.a.q_heads, true, [&](int b, int e, int h, int col) { return dq<T>(b, e, h, col); });
-        rows<T>(P.a.dk, P.starts, src, P.a.kv_heads, !P.split, [&](int b, int e, int h, int col) { return kv<T>(b, e, h, col, false); });
-        rows<T>(P.a.dv, P.starts, src, P.a.kv_heads, !P.split, [&](int b, int e, int h, int col) { return kv<T>(b, e, h, col, true); });
+        rows<T>(P.a.dq, P.a.indptr, n, P.a.q_heads, true, [&](int row, int b, int e, int h, int col) { return dq<T>(row, b, e, h, col); });
+        rows<T>(P.a.dk, P.starts, src, P.a.kv_heads, !P.split, [&](int, int b, int e, int h, int col) { return kv<T>(b, e, h, col, false); });
+        rows<T>(P.a.dv, P.starts, src, P.a.kv_heads, !P.split, [&](int, int b, int e, int h, int col) { return kv<T>(b, e, h, col, true); });
     }
 };
 
@@ -649,9 +692,9 @@ struct Again {
 // of width D; dk and dv: width 2 D, the second half for dv.
 template <typename T, bool KV> __global__ void __launch_bounds__(AT_THREADS) k_attend_sum_join(const __grid_constant__ Attend P) {
     constexpr int W = AT_THREADS / 32;
-    __shared__ float s_acc[W][512];
+    __shared__ float s_acc[W][513];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = P.a.head_dim;
-    const int heads = KV ? P.a.kv_heads : P.a.q_heads, width = KV ? 2 * D : D;
+    const int heads = KV ? P.a.kv_heads : P.a.q_heads, width = KV ? 2 * D : dq_part<T>(D);
     const int64_t units = (int64_t)__ldcg(P.words + 1) * heads, stride = (int64_t)heads * width;
     const Again again{P};
     const bool look = KV && __ldcg(P.look) != 0;
@@ -669,6 +712,24 @@ template <typename T, bool KV> __global__ void __launch_bounds__(AT_THREADS) k_a
             s_acc[warp][col] = acc;
         }
         __syncthreads();
+        if constexpr (!KV && rounded_out<T>) {
+            float miss = 0.f;
+            for (int w = 0; w < W; ++w) miss += s_acc[w][2 * D];
+            for (int col = threadIdx.x; col < D; col += AT_THREADS) {
+                float acc = 0.f, pk = 0.f;
+                for (int w = 0; w < W; ++w) {
+                    acc += s_acc[w][col];
+                    pk += s_acc[w][D + col];
+                }
+                ((T*)P.a.dq.data)[(int64_t)row.x * P.a.dq.row_stride + (int64_t)h * P.a.dq.head_stride + col] = from_f32<T>(fmaf(-miss, pk, acc) * P.a.scale);
+            }
+            if (threadIdx.x == 0) {
+                const int64_t at = (int64_t)row.x * P.a.q_heads + h;
+                if (P.shift) P.shift[at] = miss;
+                else P.stat[at].y += miss;
+            }
+            continue;
+        }
         for (int col = threadIdx.x; col < width; col += AT_THREADS) {
             float acc = 0.f;
             for (int w = 0; w < W; ++w) acc += s_acc[w][col];
@@ -803,6 +864,7 @@ static void shape_groups(Attend& P, int ve, int nv, int64_t rows, int units_per_
 template <AttendKind K, typename T, int VE, int NV, int G> static void run_attend(Attend P, int64_t rows, int64_t row_hint, cudaStream_t s) {
     constexpr int U = VE * NV * G >= 32 ? 2 : 4;
     const int units_per_row = K == AT_DKV ? P.a.kv_heads : P.a.q_heads / G;
+    P.shift = nullptr;                                        // goes to stat
     for (int pass = 0; pass < (P.split ? 2 : 1); ++pass) {
         P.chunk_mode = pass;
         const int64_t n = pass ? 2 * ((int64_t)P.edge_bound / AT_CHUNK) + 2 : rows;
@@ -904,6 +966,7 @@ static Attend attend_params(const BlockAttention& a, void* workspace) {
     P.partial = (float*)(ws + l.partial);
     P.stat = (float2*)(ws + l.stat);
     P.pd = (float2*)(ws + l.pd);
+    P.shift = (float*)(ws + l.stat);                         // the ring kernels keep no stat
     return P;
 }
 

@@ -50,6 +50,19 @@ template <int N> __device__ __forceinline__ bool all_finite(const f32x2 (&x)[N])
     return lo + hi == 0.f;
 }
 
+// Shifts of G neighbouring heads, zeros where there is no edge.
+template <int G> __device__ __forceinline__ void load_shifts(const float* p, bool on, float* x) {
+    if constexpr (G == 4) {
+        const float4 w = on ? __ldg(reinterpret_cast<const float4*>(p)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
+    } else if constexpr (G == 2) {
+        const float2 w = on ? __ldg(reinterpret_cast<const float2*>(p)) : make_float2(0.f, 0.f);
+        x[0] = w.x; x[1] = w.y;
+    } else {
+        x[0] = on ? __ldg(p) : 0.f;
+    }
+}
+
 // The sums over the tl lanes of a group, in every lane; straight code for the usual widths.
 template <int N, int TL> __device__ __forceinline__ void group_sum_of(float (&x)[N]) {
 #pragma unroll
@@ -79,6 +92,7 @@ template <AttendKind K, typename T, int VE, int NV, int G, int U>
 __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_constant__ Attend P) {
     using S = RingShape<K, T, VE, NV, G, U>;
     constexpr int E = VE * NV, N2 = E / 2, PB = S::PB, SZ = (int)sizeof(T);
+    constexpr bool SHIFTED = rounded_out<T>;                                      // delta of the dq pass lacks P.shift
     extern __shared__ __align__(16) unsigned char ring_smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned char* mine = ring_smem + (size_t)warp * S::WARP;
@@ -206,6 +220,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
         };
         // the copies of the batch whose indices have arrived; returns its description
         int h0 = 0;
+        float shift[U * G];                                  // dkv: what the edges' destinations add to delta
         auto issue = [&](int slot) -> uint32_t {
             uint32_t batch = next;
             const uint32_t base = mine_a + slot * S::SLOT, lp = base + lane * PB;
@@ -237,6 +252,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
 #pragma unroll
                     for (int i = 0; i < G; ++i)
                         copy_async<8>(base + S::PIECES + ((j * G + i) * 32 + lane) * 8, P.pd + (uint64_t)(on ? edge[j] : 0) * P.a.q_heads + h0 + i, on ? 8 : 0);
+                    if (SHIFTED) load_shifts<G>(P.shift + (uint64_t)col * P.a.q_heads + h0, on, &shift[j * G]);
                 }
             }
             if (K != AT_DKV && (batch & FIRST)) {
@@ -277,6 +293,8 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
         f32x2 x0[K == AT_DKV ? 1 : NX][K == AT_DKV ? 1 : N2], x1[K == AT_DQ ? NX : 1][K == AT_DQ ? N2 : 1];   // q; q, dout
         f32x2 acc[NA][N2];                                                           // out; dq; dk, dv
         float m[G], l[G];                                                            // running maximum and sum; lse (base 2), delta
+        f32x2 kp[K == AT_DQ && SHIFTED ? G : 1][K == AT_DQ && SHIFTED ? N2 : 1];     // dq: sum of p k
+        float miss[G];                                                               // and of p (dp - delta): 0 but for delta's rounding
         if constexpr (K != AT_DKV) {
 #pragma unroll
             for (int i = 0; i < NX; ++i)
@@ -295,10 +313,19 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
 
         uint32_t batches[RING_DEPTH];
         int first_edge[K == AT_DQ ? RING_DEPTH : 1];         // dq: where p and ds of a batch's edges go
+        constexpr int NS = K == AT_DKV && SHIFTED ? U * G : 1;
+        float shifts[RING_DEPTH][NS];
+        auto keep_shifts = [&](int s) {
+            if constexpr (K == AT_DKV && SHIFTED) {
+#pragma unroll
+                for (int i = 0; i < NS; ++i) shifts[s][i] = shift[i];
+            }
+        };
         fetch();
 #pragma unroll
         for (int s = 0; s < RING_DEPTH; ++s) {
             batches[s] = issue(s);
+            keep_shifts(s);
             if (K == AT_DQ) first_edge[s] = edge[0];
             fetch();
         }
@@ -306,12 +333,18 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
         while (__any_sync(FULL, batches[0] & LIVE)) {
             const uint32_t batch = batches[0];
             const int my_edge = first_edge[0];
+            float my_shift[NS];
+#pragma unroll
+            for (int i = 0; i < NS; ++i) my_shift[i] = shifts[0][i];
 #pragma unroll
             for (int s = 0; s + 1 < RING_DEPTH; ++s) {
                 batches[s] = batches[s + 1];
+#pragma unroll
+                for (int i = 0; i < NS; ++i) shifts[s][i] = shifts[s + 1][i];
                 if (K == AT_DQ) first_edge[s] = first_edge[s + 1];
             }
             batches[RING_DEPTH - 1] = issue(ahead);
+            keep_shifts(RING_DEPTH - 1);
             if (K == AT_DQ) first_edge[RING_DEPTH - 1] = edge[0];
             fetch();
             asm volatile("cp.async.wait_group %0;" ::"n"(RING_DEPTH) : "memory");
@@ -406,6 +439,11 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                             delta[i] = dot2(x1[i], o);
 #pragma unroll
                             for (int c = 0; c < N2; ++c) acc[i][c] = 0;
+                            if constexpr (SHIFTED) {
+                                miss[i] = 0.f;
+#pragma unroll
+                                for (int c = 0; c < N2; ++c) kp[i][c] = 0;
+                            }
                         }
                     }
                     __syncwarp();
@@ -441,6 +479,10 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                         const float p = on(j) ? fast_exp2(fmaf(s[j * G + i], c2, -m[i])) : 0.f;
                         const float ds = on(j) ? p * (s[U * G + j * G + i] - l[i]) : 0.f;
                         axpy2(ds, k, acc[i]);
+                        if constexpr (SHIFTED) {
+                            axpy2(p, k, kp[i]);
+                            miss[i] += ds;
+                        }
                         if (on(j) && t == 0) P.pd[(int64_t)(my_edge + j) * P.a.q_heads + h * G + i] = make_float2(p, ds);
                     }
                 }
@@ -451,11 +493,25 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                         for (int i = 0; i < G; ++i) {
                             const int hh = h * G + i;
                             if (!all_finite(acc[i])) *P.look = 1;
-                            if (!P.chunk_mode) scale2(P.a.scale, acc[i]);
                             float o[E];
+                            if (P.chunk_mode) {
+                                float* part = P.partial + ((int64_t)rw.w * P.a.q_heads + hh) * dq_part<T>(D);
+                                unpair(acc[i], o);
+                                store_partial<VE, NV>(part, t, tl, D, o);
+                                if constexpr (SHIFTED) {
+                                    unpair(kp[i], o);
+                                    store_partial<VE, NV>(part + D, t, tl, D, o);
+                                    if (t == 0) part[2 * D] = miss[i];
+                                }
+                                continue;
+                            }
+                            if constexpr (SHIFTED) {
+                                axpy2(-miss[i], kp[i], acc[i]);
+                                if (t == 0) P.shift[(int64_t)rw.z * P.a.q_heads + hh] = miss[i];
+                            }
+                            scale2(P.a.scale, acc[i]);
                             unpair(acc[i], o);
-                            if (P.chunk_mode) store_partial<VE, NV>(P.partial + ((int64_t)rw.w * P.a.q_heads + hh) * D, t, tl, D, o);
-                            else store_piece<T, VE, NV>((T*)((char*)o0v.data + (uint64_t)(uint32_t)rw.z * o0step) + hh * (int)o0v.head_stride, t, tl, D, o);
+                            store_piece<T, VE, NV>((T*)((char*)o0v.data + (uint64_t)(uint32_t)rw.z * o0step) + hh * (int)o0v.head_stride, t, tl, D, o);
                         }
                     }
                 }
@@ -473,7 +529,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32) k_attend_ring(const __grid_co
                         pieces(slot, j * S::EDGE + i * 2 * NV + NV, go);
                         const float2 pd = *reinterpret_cast<const float2*>(mine + slot * S::SLOT + S::PIECES + ((j * G + i) * 32 + lane) * 8);
                         axpy2(pd.x, go, acc[1]);
-                        axpy2(pd.y, q, acc[0]);
+                        axpy2(SHIFTED ? fmaf(-pd.x, my_shift[SHIFTED ? j * G + i : 0], pd.y) : pd.y, q, acc[0]);
                     }
                 if (batch & LAST) {
                     const int4 rw = rows_s[(batch >> 8) & 255];
