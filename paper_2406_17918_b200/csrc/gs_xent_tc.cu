@@ -28,7 +28,6 @@ constexpr int XT = XENT_TC_TILE;
 constexpr int XT_THREADS = 640;            // 4 warps of roles, 4 softmax warpgroups: two per unit, 64 columns each
 constexpr int XT_CHUNK = XT * 128;         // bytes of a tile's 64 columns
 constexpr int XT_MAX_STAGES = 8;
-constexpr int XT_SHORT_ROWS = 16;          // rows of fewer tiles than this get two O
 constexpr long long XT_UNIT_CLOCKS = 1000000;   // more than five hundred times what a unit takes
 constexpr float XT_LOG2E = 1.4426950408889634f;
 
@@ -902,19 +901,14 @@ template <int M> static cudaError_t run_tc(const Xent& a, const Operands& o, Xen
     P.ny = ON_X ? (int)a.vocab : a.rows;
     P.runs = make_runs(P.nx, XT, P.ny, XT, sm_count());
     const int chunks = (a.dim + 63) / 64, tile = chunks * XT_CHUNK;
-    const bool short_rows = P.runs.tiles_y < XT_SHORT_ROWS;
-    P.xbufs = chunks == 1 || (chunks == 2 && (M == TC_FORWARD || short_rows)) ? 2 : 1;
+    P.xbufs = chunks == 1 || (chunks == 2 && M == TC_FORWARD) ? 2 : 1;
     P.on = (a.dim + 15) / 16 * 16;
-    // 512 columns of tensor memory: three S and one or two O of up to 128 (64) columns, or two S and one O of up to 256.
-    // With few units per row of tiles a second O pays more than a third S: the next row's products need not wait for
-    // the store of this one's.
+    // 512 columns of tensor memory: three S and one O of up to 128 columns (two of up to 64), or two S and one O of up to
+    // 256.  Two S and two O of 128 columns, whose next row's products need not wait for the store of this one's: dw of
+    // 169,343 x 128 with 128 hidden rows 56.4 | 57.2 us, but 512 rows 67.0 | 65.9, 1,024 rows 94.5 | 85.9, 8,192 rows 582 | 503.
     P.on_pitch = chunks == 1 ? 64 : 128;
     P.sbufs = chunks <= 2 ? 3 : 2;
     P.obufs = chunks == 1 ? 2 : 1;
-    if (chunks == 2 && short_rows) {
-        P.sbufs = 2;
-        P.obufs = 2;
-    }
     // shared memory: X, the ring of Y, row info, and rows on their way out where X and three or more tiles of Y leave room
     int staging = 0;
     P.out = OUT_DIRECT;                    // each gradient by its own address and pitch
