@@ -463,9 +463,10 @@ gs_status gs_alu_ceiling(int32_t what, int32_t milliseconds, void* stream, doubl
  * What a training step does with a batch: the rows of the input nodes (gs_gather_features for fixed features,
  * gs_embedding_lookup for learned ones), attention of every hop's destinations over their sampled neighbours, a
  * softmax over classes or over all nodes; and the gradients of each.  The calls are independent of the caches and
- * can be used with any arrays.  Types are GS_F32 and GS_BF16; sums, softmax statistics and gradients are kept in
- * 32 bits and rounded once, to the output's type.  No floating-point atomics: a call's result does not depend on
- * scheduling.  Workspaces are 256-byte aligned, owned by the caller, and hold nothing between calls. */
+ * can be used with any arrays.  Types are GS_F32 and GS_BF16; sums and softmax statistics are kept in 32 bits and
+ * rounded once, to the output's type (and, for bf16 operands of the cross entropy, dz to bf16 on the way: see there).
+ * No floating-point atomics: a call's result does not depend on scheduling.  Workspaces are 256-byte aligned, owned by
+ * the caller, and hold nothing between calls. */
 
 /* out[p, :] = scale * table[ids[p], :] for p < count; an id outside [0, table_rows) gives a row of zeros.
  *   d_table  [table_rows][table_ld] of table_dtype, table_ld >= dim (elements); table_rows < 2^31
@@ -512,7 +513,8 @@ gs_status gs_embedding_backward_sparse(const void* d_dout, gs_dtype dout_dtype, 
  * gs_block_reverse turns the block's edges to source order, once for all layers that use the block: the
  * destinations of source j, ascending, are d_rev_dst[d_rev_indptr[j] .. d_rev_indptr[j+1]), and d_rev_edge holds the
  * edges they came from (int32[max_src + 1] and twice int32[max_edges]; masked edges are left out).  The backward pass
- * recomputes the probabilities from lse and sums dk and dv in that order; dq, dk and dv are written for every row of their counts (zeros where nothing contributes).
+ * recomputes the probabilities from lse and sums dk and dv in that order; dq, dk and dv are
+ * written for every row of their counts (zeros where nothing contributes), and not behind them.
  * Workspace: gs_block_attention_workspace_bytes, enough for any of the three calls. */
 typedef struct {
     void* d_data;
@@ -539,7 +541,8 @@ gs_status gs_block_attention_backward(const gs_block* block, int32_t max_row, co
  *   d_hidden [rows][hidden_ld], d_table [vocab][table_ld] of `dtype`; gradients of `grad_dtype`; loss, lse, dloss float[rows]
  *   0 <= rows < 2^31 - 256, 1 <= vocab < 2^31 - 256, 1 <= dim <= 4096
  * f32 operands are multiplied in 32 bits.  bf16 operands with dim <= 256 (and, where dim is a multiple of 8, bases and
- * pitches on 16 bytes) use the tensor cores: f32 sums, and dz rounded to bf16 for the second product.  Workspace: gs_xent_workspace_bytes, enough for either call. */
+ * pitches on 16 bytes) use the tensor cores: f32 sums, and dz rounded to bf16 for the second product (the labels' entries
+ * in two parts, 2^-16).  All others are multiplied on the CUDA cores, at a small part of that speed.  Workspace: gs_xent_workspace_bytes, enough for either call. */
 gs_status gs_xent_workspace_bytes(int32_t rows, int64_t vocab, int32_t dim, gs_dtype dtype, size_t* bytes);
 gs_status gs_xent_forward(const void* d_hidden, int64_t hidden_ld, const void* d_table, int64_t table_ld, gs_dtype dtype,
                           int32_t rows, int64_t vocab, int32_t dim, float scale, const int32_t* d_labels, float* d_loss,

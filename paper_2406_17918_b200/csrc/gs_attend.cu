@@ -5,7 +5,7 @@
 //   delta = do . o,  ds = p (do . v - delta) scale,  dq_i = sum_j ds k_j,  dk_j = sum_i ds q_i,  dv_j = sum_i p do_i.
 // The forward keeps a running maximum and sum.  The backward recomputes p from lse in the pass that sums dq; the ring kernels
 // leave p and ds there, 8 bytes per edge and head, for the pass in source order, which then needs neither k nor v
-// (4.36 M edges of 4 heads of 32: 564 us, 848 with the dot products taken again).
+// (4.36 M edges of 4 heads of 32: 605 us, 848 with the dot products taken again).
 //
 // Every edge gathers whole rows, so the kernels are bound by the gathered bytes: a group of tl lanes holds one
 // (row, head) with one wide load per lane and operand, U edges are in flight per group, and groups of one row's heads are
@@ -14,8 +14,8 @@
 // A row longer than AT_CHUNK edges (hubs) is cut into chunks; the chunks' results are joined in order.
 // Operands in pieces of 16 or 8 bytes go to the ring kernels (gs_attend_ring.cuh); the kernels of this file take one element
 // at a time, whatever the alignment and the head dimension, and let `slots` groups share a row when rows are too few.
-// 4.36 M edges of 4 heads of 32, bf16 (512 bytes gathered per edge): forward 330 us (6.8 TB/s gathered), dq 412 us, dk and dv
-// 564 us, the reversed block 245 us.
+// 4.36 M edges of 4 heads of 32, bf16 (512 bytes gathered per edge): forward 347 us (6.4 TB/s gathered), dq 458 us, dk and dv
+// 605 us, the reversed block 218 us.
 #include <initializer_list>
 #include <type_traits>
 
@@ -41,11 +41,11 @@ __device__ __forceinline__ float fast_exp2(float x) {
 // where a sum came out not finite.
 __device__ __forceinline__ float backward_lse(float lse) { return lse == -INFINITY ? INFINITY : lse * LOG2E; }
 
-// delta = do . o is taken from `out`, which a caller of bf16 holds rounded: off by up to 2^-9 of sum |do||o|, which ds of a
-// row of few edges, or of one probability near 1, does not bear (2.5 times the error of dq and dk at 179 rows of mostly one to three
-// edges).  The dq pass therefore also sums r = sum p (dp - delta), which is 0 for the right delta, and sum p k, and corrects
-// itself: dq = sum p (dp - delta) k - r sum p k.  The pass behind it adds r to delta (the "shift").  262,144 rows of 4 x 32: dq 410 ->
-// 457 us, dk and dv 552 -> 606 (ds rewritten at a row's end instead: 609 and 552).  f32: nothing to correct.
+// delta = do . o is taken from `out`, which a caller of bf16 holds rounded: off by up to 2^-8 of sum |do||o|, which ds of a
+// row of few edges, or of one probability near 1, does not bear (2.5 times the error of dq and dk at 179 rows of mostly one
+// to three edges).  The dq pass therefore also sums r = sum p (dp - delta), which is 0 for the right delta, and sum p k, and corrects
+// itself: dq = sum p (dp - delta) k - r sum p k.  The pass behind it adds r to delta (the "shift").  262,144 rows of 4 x 32:
+// dq 410 -> 457 us, dk and dv 552 -> 606 (ds rewritten at a row's end instead: 609 and 552).  f32: nothing to correct.
 template <typename T> constexpr bool rounded_out = sizeof(T) == 2;
 // Floats of a chunk's part of dq, per head: the sum; and sum p k and r.
 template <typename T> __device__ __forceinline__ int dq_part(int dim) { return rounded_out<T> ? 2 * dim + 1 : dim; }

@@ -11,8 +11,8 @@
 // multiplied while another is exponentiated.  S of a later unit may overwrite a Z once the product that read it has ended.
 // Work is cut into equal runs of units, one per SM; a row of tiles shared by runs is joined from f32 partials.
 // Bound: forward by the exponentials (one per logit; special-function and multiply-add units share them), backward by the
-// reads of X, Y and Y again from shared memory beside them.  8,192 x 169,343 x 128: forward 363 us (0.98 PFLOP/s), dh 516 us and
-// dw 589 us (1.4 and 1.2 PFLOP/s over their two products).
+// reads of X, Y and Y again from shared memory beside them.  8,192 x 169,343 x 128: forward 357 us (0.99 PFLOP/s), dh 481 us and
+// dw 571 us (1.5 and 1.2 PFLOP/s over their two products).
 #include <atomic>
 #include <type_traits>
 
@@ -70,8 +70,8 @@ template <int DEGREE> __device__ __forceinline__ f32x2 exp2_by_fma(f32x2 x) {
 }
 
 // 2^x of pair j of 16: the multiply-add units take 4 of 16 pairs forward, 2 of 16 backward (there the tensor cores set
-// the pace).  Measured at 8,192 x 169,343 x 128: forward 369 us with 4, 387 with 5, 396 with 6 pairs, 443 with none;
-// backward 1,083 us with 2, 1,078 with none (64 columns: 902 and 969), 1,098 with 4.
+// the pace).  Measured side by side at 8,192 x 169,343 x 128 (an earlier forward, 369 us): forward 369 us with 4, 387 with 5,
+// 396 with 6 pairs, 443 with none; backward 1,083 us with 2, 1,078 with none (64 columns: 902 and 969), 1,098 with 4.
 constexpr int FMA_PAIRS_FORWARD = 0x2222, FMA_PAIRS_BACKWARD = 0x0202;
 template <bool FORWARD> __device__ __forceinline__ f32x2 exp2_pair(f32x2 x, int j) {
     if (((FORWARD ? FMA_PAIRS_FORWARD : FMA_PAIRS_BACKWARD) >> j) & 1) return exp2_by_fma<FORWARD ? 5 : 4>(x);
