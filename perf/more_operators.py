@@ -309,10 +309,9 @@ def _own_run(s):
         values = gs.gs_coded_read(coded, num_rows=c["rows"], out_dtype=torch.bfloat16)
         return dict(values=values, hidden=hidden) if c["residual"] else dict(values=values)
     if op == "cache":
-        ws = _workspace(s, lambda: gs.gs_coded_write_workspace_bytes(c["written"]))
         if "cache" not in s:
             s["cache"] = gs.CodedRows(s["codes"], s["scales"], c["head_dim"], c["block"])
-        gs.gs_coded_write(s["cache"], s["new"], ws, ids=s["ids"])
+        gs.gs_coded_write(s["cache"], s["new"], ids=s["ids"])
         return dict(values=gs.gs_coded_read(s["cache"], ids=s["wanted"], out_dtype=_TYPES[c["type"]]), scales=s["scales"])
     if op == "serve":
         ws = _workspace(s, lambda: gs.gs_coded_attention_workspace_bytes(c["dst"], s["indices"].numel(), c["heads"], c["head_dim"]))
