@@ -552,6 +552,85 @@ gs_status gs_xent_backward(const void* d_hidden, int64_t hidden_ld, const void* 
                            const float* d_dloss, void* d_dhidden, int64_t dhidden_ld, void* d_dtable, int64_t dtable_ld,
                            gs_dtype grad_dtype, void* d_workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Around an attention layer: norms, rows kept in 8 bits, attention over them, the norm of all gradients.
+ * Types, sums, strides, workspaces, device counts and the order of results are as for the training operators above. */
+
+/* Root-mean-square norm of rows [rows][dim], 1 <= dim <= 8192, with the addition of a residual before it:
+ *   h = x + residual, rounded to `dtype` (h = x without a residual);  out = weight h / sqrt(mean(h^2) + eps)
+ * d_weight_or_null [dim] of weight_dtype (NULL: ones); eps >= 0.  d_hidden_or_null receives h, which the backward pass takes; it may
+ * be the array of x or of the residual, and d_out that of x, at the same pitch.  d_count_or_null: as for gs_gather_features;
+ * rows behind the count are left as they are.
+ * gs_rms_norm_coded writes the result in 8 bits instead (gs_coded below): row p to row p of `out`, which has scales of its own for
+ * every row (block 1) and heads * head_dim == dim: a scale per group of head_dim columns.
+ * gs_rms_norm_backward takes h, the gradient dout of out and, if h is used elsewhere, the gradient dhidden that arrives there:
+ *   dx = dhidden + the gradient through the norm (it is the residual's gradient too);  dweight[c] = sum over rows, or NULL
+ * dx may be the array of dhidden or of dout.  Workspace: gs_rms_norm_workspace_bytes. */
+typedef struct {
+    void* d_codes;            /* [rows][row_stride] e4m3, head h from byte h * pitch on, pitch = head_dim rounded up to 16 */
+    uint8_t* d_scales;        /* [ceil(rows / block)][scale_stride], head h's at h */
+    int64_t rows, row_stride, scale_stride;
+    int32_t heads, head_dim, block;
+} gs_coded;
+gs_status gs_rms_norm_workspace_bytes(int32_t rows, int32_t dim, size_t* bytes);
+gs_status gs_rms_norm_forward(const void* d_x, int64_t x_ld, const void* d_residual_or_null, int64_t residual_ld, gs_dtype dtype,
+                              const void* d_weight_or_null, gs_dtype weight_dtype, const int32_t* d_count_or_null, int32_t rows,
+                              int32_t dim, float eps, void* d_hidden_or_null, int64_t hidden_ld, void* d_out, int64_t out_ld, void* stream);
+gs_status gs_rms_norm_coded(const void* d_x, int64_t x_ld, const void* d_residual_or_null, int64_t residual_ld, gs_dtype dtype,
+                            const void* d_weight_or_null, gs_dtype weight_dtype, const int32_t* d_count_or_null, int32_t rows,
+                            int32_t dim, float eps, void* d_hidden_or_null, int64_t hidden_ld, const gs_coded* out, void* stream);
+gs_status gs_rms_norm_backward(const void* d_hidden, int64_t hidden_ld, const void* d_dout, int64_t dout_ld,
+                               const void* d_dhidden_or_null, int64_t dhidden_ld, gs_dtype dtype, const void* d_weight_or_null,
+                               gs_dtype weight_dtype, const int32_t* d_count_or_null, int32_t rows, int32_t dim, float eps, void* d_dx,
+                               int64_t dx_ld, void* d_dweight_or_null, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Rows in 8 bits (gs_coded): key and value rows of nodes, say, kept for serving.  A value is code * 2^(scale - 127), code of e4m3
+ * (4 exponent and 3 mantissa bits, largest 448, no infinities), scale a byte for each block of `block` consecutive rows (a power of
+ * two, 1 to 64) and head.  A block's scale is the smallest with |x| <= 448 * 2^(scale - 127) for the finite values written to
+ * it; infinities and NaN become NaN.  Storage that holds zeros is a valid store of zero rows.  d_codes is aligned to 16 bytes,
+ * row_stride a multiple of 16 and at least heads * pitch; a range of heads of a store is a store (d_codes + h * pitch, d_scales + h).
+ *   gs_coded_write  rows[p] (gs_heads of `dtype`, strides in elements) goes to row d_ids[p], or first + p if d_ids is NULL.  An id
+ *                   outside the store is skipped; of the positions with one id the last counts.  Where other rows of a block
+ *                   stay, its scale does not fall, and their codes are requantised if it rises (exact, but for values that
+ *                   fall below 2^-6 of it); a block whose rows are all written starts afresh.  The bytes between head_dim and pitch
+ *                   are written as zeros.  d_claims (only with d_ids): int32[rows + (block > 1 ? ceil(rows / block) : 0)], the
+ *                   caller's, all -1 before the first call and after each; calls that share it do not overlap.
+ *   gs_coded_read   out[p] = row d_ids[p], or first + p; an id outside the store gives zeros.
+ * d_count_or_null, count_bound: as for gs_gather_features. */
+gs_status gs_coded_write(const gs_coded* to, gs_dtype dtype, const gs_heads* rows, const int32_t* d_ids_or_null, int64_t first,
+                         const int32_t* d_count_or_null, int32_t count_bound, int32_t* d_claims, void* stream);
+gs_status gs_coded_read(const gs_coded* from, const int32_t* d_ids_or_null, int64_t first, const int32_t* d_count_or_null,
+                        int32_t count_bound, gs_dtype dtype, const gs_heads* out, void* stream);
+
+/* gs_block_attention_forward with keys and values held in 8 bits: source j's are row d_rows[j] of k and v, or row j if d_rows is
+ * NULL (max_src is then at most k->rows).  An edge whose source or row does not exist is masked.  k and v have one number of rows,
+ * heads and block size and may be parts of one store; q and out are of `dtype`.
+ * Workspace: gs_coded_attention_workspace_bytes. */
+gs_status gs_coded_attention_workspace_bytes(int32_t max_edges, int32_t q_heads, int32_t head_dim, size_t* bytes);
+gs_status gs_coded_attention_forward(const gs_block* block, const int32_t* d_rows_or_null, int32_t max_row, gs_dtype dtype,
+                                     int32_t q_heads, int32_t head_dim, float scale, const gs_heads* q, const gs_coded* k,
+                                     const gs_coded* v, const gs_heads* out, float* d_lse, void* d_workspace, size_t workspace_bytes,
+                                     void* stream);
+
+/* The norm over n gradients, norm = sqrt(sum of all squares), and their scaling by min(1, max_norm / (norm + 1e-6)):
+ *   gs_grad_norm  writes *d_norm
+ *   gs_grad_clip  also writes d_out of every gradient (d_grad itself: in place; nothing is written where the factor is 1)
+ * A gradient is elems contiguous numbers of `dtype`, in any order; with d_rows only its first *d_rows * row_elems count (the touched
+ * rows of gs_embedding_backward_sparse), and what lies behind is neither read nor written.  A norm that is infinite or NaN gives the
+ * factor that this formula gives.  n <= 65536; results do not overlap one another or other gradients.
+ * Workspace: gs_grad_workspace_bytes(n). */
+typedef struct {
+    const void* d_grad;
+    void* d_out;                    /* gs_grad_clip */
+    int64_t elems;
+    const int32_t* d_rows_or_null;
+    int64_t row_elems;
+    gs_dtype dtype;
+} gs_grad;
+gs_status gs_grad_workspace_bytes(int32_t n, size_t* bytes);
+gs_status gs_grad_norm(const gs_grad* grads, int32_t n, float* d_norm, void* d_workspace, size_t workspace_bytes, void* stream);
+gs_status gs_grad_clip(const gs_grad* grads, int32_t n, float max_norm, float* d_norm_or_null, void* d_workspace,
+                       size_t workspace_bytes, void* stream);
+
 /* Synchronises `stream`; GS_ERR_CUDA if a kernel of the training operators ever gave up one of its (bounded) waits.  Such a
  * kernel leaves its results partly unwritten, and the call that launched it has long returned GS_OK: gs_xent_forward's and
  * gs_xent_backward's results for bf16 operands hold only if this passes after them (before a step is kept, say).  Once set,

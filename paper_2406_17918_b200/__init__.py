@@ -12,5 +12,8 @@ from .binding import (  # noqa: F401
     gs_embedding_lookup, gs_embedding_workspace_bytes, gs_embedding_backward, gs_embedding_backward_sparse, gs_train_status,
     gs_xent_workspace_bytes, gs_xent_forward, gs_xent_backward,
     gs_block_attention_workspace_bytes, gs_block_attention_forward, gs_block_reverse, gs_block_attention_backward,
+    gs_rms_norm_workspace_bytes, gs_rms_norm_forward, gs_rms_norm_coded, gs_rms_norm_backward,
+    CodedRows, gs_coded_rows, gs_coded_write, gs_coded_read, gs_coded_attention_workspace_bytes, gs_coded_attention_forward,
+    gs_grad_workspace_bytes, gs_grad_norm, gs_grad_clip,
     gs_last_error, gs_stats_word_offset, library_path, exported_symbols, COUNTS_READBACK_BYTES,
 )

@@ -13,7 +13,7 @@ import torch
 
 from . import binding as gs
 
-__all__ = ["embedding", "block_attention", "table_cross_entropy"]
+__all__ = ["embedding", "block_attention", "rms_norm", "table_cross_entropy"]
 
 
 def _workspace(nbytes: int, like: torch.Tensor) -> torch.Tensor:
@@ -118,3 +118,29 @@ def table_cross_entropy(hidden: torch.Tensor, table: torch.Tensor, labels: torch
     """Cross entropy per row of softmax(scale * hidden table^T); labels outside the table give 0 and no gradient.  Results of
     bf16 operands hold if ``gs_train_status()`` passes after them (it synchronises: call it where a step is kept anyway)."""
     return _TableCrossEntropy.apply(hidden, table, labels, float(scale))
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps, count):
+        ctx.set_materialize_grads(False)
+        out, hidden = gs.gs_rms_norm_forward(x, weight, residual=residual, eps=eps, count=count)
+        ctx.save_for_backward(hidden, weight, count)
+        ctx.eps, ctx.with_residual = eps, residual is not None
+        return (out, hidden) if residual is not None else out
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, dout, dhidden=None):
+        hidden, weight, count = ctx.saved_tensors
+        if dout is None:                                     # the norm's result has no part in what is differentiated
+            dout = torch.zeros_like(hidden)
+        ws = _workspace(gs.gs_rms_norm_workspace_bytes(*hidden.shape), hidden)
+        dx, dweight = gs.gs_rms_norm_backward(hidden, dout.contiguous(), ws, weight=weight, dhidden=None if dhidden is None else dhidden.contiguous(),
+                                              eps=ctx.eps, count=count)
+        return dx, dweight, dx if ctx.with_residual else None, None, None
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor = None, residual: torch.Tensor = None, eps: float = 1e-6, count: torch.Tensor = None):
+    """weight * h / sqrt(mean(h^2) + eps) for the rows of h = x + residual.  With a residual returns (that, h), both differentiable."""
+    return _RmsNorm.apply(x, weight, residual, float(eps), count)

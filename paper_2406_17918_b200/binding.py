@@ -123,6 +123,17 @@ def _load():
         "gs_block_reverse": [vp, vp, vp, vp, vp, sz, vp],
         "gs_block_attention_backward": [vp, i32, vp, vp, vp, ctypes.c_int, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                         vp, sz, vp],
+        "gs_rms_norm_workspace_bytes": [i32, i32, psz],
+        "gs_rms_norm_forward": [vp, i64, vp, i64, ctypes.c_int, vp, ctypes.c_int, vp, i32, i32, ctypes.c_float, vp, i64, vp, i64, vp],
+        "gs_rms_norm_coded": [vp, i64, vp, i64, ctypes.c_int, vp, ctypes.c_int, vp, i32, i32, ctypes.c_float, vp, i64, vp, vp],
+        "gs_rms_norm_backward": [vp, i64, vp, i64, vp, i64, ctypes.c_int, vp, ctypes.c_int, vp, i32, i32, ctypes.c_float, vp, i64, vp, vp, sz, vp],
+        "gs_coded_write": [vp, ctypes.c_int, vp, vp, i64, vp, i32, vp, vp],
+        "gs_coded_read": [vp, vp, i64, vp, i32, ctypes.c_int, vp, vp],
+        "gs_coded_attention_workspace_bytes": [i32, i32, i32, psz],
+        "gs_coded_attention_forward": [vp, vp, i32, ctypes.c_int, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, sz, vp],
+        "gs_grad_workspace_bytes": [i32, psz],
+        "gs_grad_norm": [vp, i32, vp, vp, sz, vp],
+        "gs_grad_clip": [vp, i32, ctypes.c_float, vp, vp, sz, vp],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -936,3 +947,269 @@ def gs_train_status(stream=None):
     """Synchronises; raises if a kernel of the training operators ever gave up waiting, and so left results partly unwritten:
     call it before they are kept."""
     _check(_L.gs_train_status((torch.cuda.current_stream() if stream is None else stream).cuda_stream))
+
+
+# ---------------------------------------------------------------- around an attention layer: norms, rows in 8 bits, gradient clipping
+def _one_device(*tensors):
+    """All operands of a call are memory of one GPU: the call's."""
+    device = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("the operands are on different devices")
+    return device
+
+
+def _run(device, fn, *args):
+    """The call, on the operands' device."""
+    if device == torch.cuda.current_device():
+        _check(fn(*args))
+        return
+    with torch.cuda.device(device):
+        _check(fn(*args))
+
+
+def _norm_rows(t, what, like):
+    _rows_2d(t, what)
+    if t.dtype is not like.dtype or t.shape != like.shape:
+        raise TypeError("%s must have the dtype and shape of the normalised rows" % what)
+    return t
+
+
+def _norm_weight(weight, dim):
+    if weight is None:
+        return None, GS_F32
+    if weight.dim() != 1 or weight.shape[0] != dim or not weight.is_cuda or not weight.is_contiguous():
+        raise TypeError("weight must be a contiguous CUDA tensor [%d]" % dim)
+    return weight.data_ptr(), _dtype(weight.dtype)
+
+
+def _opt(t):
+    """(address, row pitch) of an operand that may be missing."""
+    return (None, 0) if t is None else (t.data_ptr(), _ld(t))
+
+
+def gs_rms_norm_workspace_bytes(rows: int, dim: int) -> int:
+    """Bytes for gs_rms_norm_backward of so many rows."""
+    out = ctypes.c_size_t()
+    _check(_L.gs_rms_norm_workspace_bytes(int(rows), int(dim), ctypes.byref(out)))
+    return out.value
+
+
+def _norm_inputs(x, weight, residual, hidden, stream, count):
+    _rows_2d(x, "x")
+    if residual is not None:
+        _norm_rows(residual, "residual", x)
+        hidden = _new(tuple(x.shape), x.dtype, x, stream, None if count is None else 0) if hidden is None else _norm_rows(hidden, "hidden", x)
+    elif hidden is not None:
+        _norm_rows(hidden, "hidden", x)
+    return hidden, _norm_weight(weight, x.shape[1])
+
+
+def gs_rms_norm_forward(x: torch.Tensor, weight: torch.Tensor = None, residual: torch.Tensor = None, eps: float = 1e-6, out: torch.Tensor = None,
+                        hidden: torch.Tensor = None, count: torch.Tensor = None, stream=None):
+    """h = x + residual; out = weight * h / sqrt(mean(h^2) + eps), row by row.  Returns (out, h); h is x itself without a residual.
+    `hidden` (h) may be x or residual, `out` may be x.  `count`: a 0-d int32 CUDA tensor with the number of rows (x is then the
+    bound; rows behind it are zeros, or left as they are in given arrays)."""
+    hidden, (w, wt) = _norm_inputs(x, weight, residual, hidden, stream, count)
+    out = _new(tuple(x.shape), x.dtype, x, stream, None if count is None else 0) if out is None else _norm_rows(out, "out", x)
+    device = _one_device(x, weight, residual, hidden, out, count)
+    _run(device, _L.gs_rms_norm_forward, _addr(x), _ld(x), *_opt(residual), _dtype(x.dtype), w, wt, _counter(count, "count"), x.shape[0], x.shape[1], float(eps),
+         *_opt(hidden), _addr(out), _ld(out), _on(stream, x))
+    return out, x if hidden is None else hidden
+
+
+def gs_rms_norm_coded(x: torch.Tensor, out: "CodedRows", weight: torch.Tensor = None, residual: torch.Tensor = None, eps: float = 1e-6,
+                      hidden: torch.Tensor = None, count: torch.Tensor = None, stream=None):
+    """gs_rms_norm_forward with the result in 8 bits: row p of `out` (a store with block 1 and heads * head_dim = dim).  Returns (out, h)."""
+    hidden, (w, wt) = _norm_inputs(x, weight, residual, hidden, stream, count)
+    device = _one_device(x, weight, residual, hidden, out.codes, count)
+    _run(device, _L.gs_rms_norm_coded, _addr(x), _ld(x), *_opt(residual), _dtype(x.dtype), w, wt, _counter(count, "count"), x.shape[0], x.shape[1], float(eps),
+         *_opt(hidden), out.address, _on(stream, x))
+    return out, x if hidden is None else hidden
+
+
+def gs_rms_norm_backward(hidden: torch.Tensor, dout: torch.Tensor, workspace: torch.Tensor, weight: torch.Tensor = None, dhidden: torch.Tensor = None,
+                         eps: float = 1e-6, dx: torch.Tensor = None, dweight: torch.Tensor = None, count: torch.Tensor = None, stream=None):
+    """Gradients of gs_rms_norm_forward for what it normalised.  `dhidden`: the gradient that arrives at h itself.  Returns (dx,
+    dweight); dx is the residual's gradient too, dweight None without a weight.  `dx` may be dhidden or dout."""
+    _rows_2d(hidden, "hidden")
+    _norm_rows(dout, "dout", hidden)
+    if dhidden is not None:
+        _norm_rows(dhidden, "dhidden", hidden)
+    w, wt = _norm_weight(weight, hidden.shape[1])
+    dx = _new(tuple(hidden.shape), hidden.dtype, hidden, stream, None if count is None else 0) if dx is None else _norm_rows(dx, "dx", hidden)
+    if weight is None:
+        if dweight is not None:
+            raise ValueError("there is no weight")
+    elif dweight is None:
+        dweight = _new(hidden.shape[1], weight.dtype, hidden, stream)
+    elif dweight.dtype is not weight.dtype or _norm_weight(dweight, hidden.shape[1])[0] is None:
+        raise TypeError("dweight must have the dtype of weight")
+    device = _one_device(hidden, dout, workspace, weight, dhidden, dx, dweight, count)
+    _run(device, _L.gs_rms_norm_backward, _addr(hidden), _ld(hidden), _addr(dout), _ld(dout), *_opt(dhidden), _dtype(hidden.dtype), w, wt, _counter(count, "count"),
+         hidden.shape[0], hidden.shape[1], float(eps), _addr(dx), _ld(dx), _addr(dweight), *_workspace(workspace), _on(stream, workspace))
+    return dx, dweight
+
+
+class _CCoded(ctypes.Structure):
+    _fields_ = [("d_codes", ctypes.c_void_p), ("d_scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("scale_stride", ctypes.c_int64), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32)]
+
+
+class CodedRows:
+    """Rows in 8 bits over two caller-owned tensors (see gs_coded in include/gs.h): codes [rows, heads, pitch] (float8_e4m3fn or
+    uint8; pitch = head_dim rounded up to 16) and scales uint8 [ceil(rows / block), heads].  Tensors of zeros are a store of zero
+    rows.  A store holds an int32 per row and block beside them, for writes by id; two of those on one store may not overlap."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, head_dim: int, block: int = 1):
+        head_dim, block = int(head_dim), int(block)
+        if block < 1 or block > 64 or block & (block - 1):
+            raise ValueError("block must be a power of two from 1 to 64")
+        pitch = (head_dim + 15) // 16 * 16
+        if codes.dtype not in (torch.float8_e4m3fn, torch.uint8) or not codes.is_cuda or codes.dim() != 3 or head_dim < 1 or codes.shape[2] != pitch or \
+                codes.stride(2) != 1 or (codes.shape[1] > 1 and codes.stride(1) != pitch):
+            raise TypeError("codes must be a CUDA tensor [rows, heads, %d] of float8_e4m3fn or uint8, heads one behind the other" % pitch)
+        rows, heads = codes.shape[0], codes.shape[1]
+        if scales.dtype != torch.uint8 or tuple(scales.shape) != ((rows + block - 1) // block, heads) or (heads > 1 and scales.stride(1) != 1):
+            raise TypeError("scales must be a uint8 tensor [ceil(rows / block), heads]")
+        device = _one_device(codes, scales)
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("a store cannot be made while a graph is captured")
+        claims = torch.full((rows + (scales.shape[0] if block > 1 else 0),), -1, dtype=torch.int32, device=torch.device("cuda", device))
+        self._set(codes, scales, head_dim, block, claims)
+
+    def _set(self, codes, scales, head_dim, block, claims):
+        self.codes, self.scales, self.claims = codes, scales, claims
+        self.rows, self.num_heads, self.head_dim, self.block = codes.shape[0], codes.shape[1], head_dim, block
+        stride = codes.stride(0) if self.rows > 1 else self.num_heads * codes.shape[2]
+        self._c = _CCoded(codes.data_ptr(), scales.data_ptr(), self.rows, stride, scales.stride(0) if scales.shape[0] > 1 else self.num_heads,
+                          self.num_heads, head_dim, block)
+        self.address = ctypes.addressof(self._c)
+
+    def heads(self, first: int, end: int) -> "CodedRows":
+        """The heads [first, end) as a store over the same memory (keys and values of one cache, say)."""
+        if not 0 <= first < end <= self.num_heads:
+            raise ValueError("heads [%d, %d) of %d" % (first, end, self.num_heads))
+        part = object.__new__(CodedRows)
+        part._set(self.codes[:, first:end], self.scales[:, first:end], self.head_dim, self.block, self.claims)
+        return part
+
+
+def gs_coded_rows(rows: int, heads: int, head_dim: int, block: int = 16, device=None) -> CodedRows:
+    """A store of `rows` zero rows."""
+    device = torch.device("cuda") if device is None else device
+    codes = torch.zeros((int(rows), int(heads), (int(head_dim) + 15) // 16 * 16), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+    return CodedRows(codes, torch.zeros(((int(rows) + int(block) - 1) // int(block), int(heads)), dtype=torch.uint8, device=device), head_dim, block)
+
+
+def gs_coded_write(to: CodedRows, rows: torch.Tensor, ids: torch.Tensor = None, first: int = 0, count: torch.Tensor = None, stream=None) -> CodedRows:
+    """rows[p] ([n, heads, head_dim], float32 or bfloat16) into row ids[p] of the store, or first + p.  Ids outside the store are
+    skipped, of equal ids the last counts.  `count`: the device's number of rows (n is then the bound)."""
+    n = rows.shape[0] if ids is None else _ids_1d(ids, "ids").numel()
+    keep, (p,) = _heads(rows.dtype, (rows, "rows", n, to.num_heads, to.head_dim))
+    device = _one_device(to.codes, rows, ids, count)
+    _run(device, _L.gs_coded_write, to.address, _dtype(rows.dtype), p, _addr(ids), int(first), _counter(count, "count"), n, _addr(to.claims), _on(stream, to.codes))
+    return to
+
+
+def gs_coded_read(store: CodedRows, ids: torch.Tensor = None, first: int = 0, num_rows: int = None, out: torch.Tensor = None,
+                  out_dtype: torch.dtype = torch.bfloat16, count: torch.Tensor = None, stream=None) -> torch.Tensor:
+    """out[p] = row ids[p] of the store, or first + p for p < num_rows (default: to its end); ids outside it give zeros."""
+    n = _ids_1d(ids, "ids").numel() if ids is not None else (store.rows - int(first) if num_rows is None else int(num_rows))
+    if n < 0:
+        raise ValueError("no rows from %d on" % first)
+    if out is None:
+        out = _new((n, store.num_heads, store.head_dim), out_dtype, store.codes, stream, None if count is None else 0)
+    keep, (p,) = _heads(out.dtype, (out, "out", n, store.num_heads, store.head_dim))
+    device = _one_device(store.codes, ids, out, count)
+    _run(device, _L.gs_coded_read, store.address, _addr(ids), int(first), _counter(count, "count"), n, _dtype(out.dtype), p, _on(stream, store.codes))
+    return out
+
+
+def gs_coded_attention_workspace_bytes(num_dst: int, num_edges: int, q_heads: int, head_dim: int) -> int:
+    """Bytes for gs_coded_attention_forward on such a block."""
+    out = ctypes.c_size_t()
+    _check(_L.gs_coded_attention_workspace_bytes(int(num_edges), int(q_heads), int(head_dim), ctypes.byref(out)))
+    return out.value
+
+
+def gs_coded_attention_forward(indptr: torch.Tensor, indices: torch.Tensor, q: torch.Tensor, k: CodedRows, v: CodedRows, workspace: torch.Tensor,
+                               rows: torch.Tensor = None, scale: float = None, max_row: int = 0, out: torch.Tensor = None, lse: torch.Tensor = None,
+                               counts=None, stream=None):
+    """gs_block_attention_forward with keys and values in 8 bits (k, v: stores, or parts of one).  `rows`: the store's row of every
+    source of the block (its input nodes, say); without it a source is its row.  Returns (out, lse)."""
+    n, hq, d = q.shape
+    if indptr.numel() - 1 > n:
+        raise ValueError("q has fewer rows than the block has destinations")
+    b = _csr_block(indptr, indices, k.rows if rows is None else _ids_1d(rows, "rows").numel(), counts)
+    exact = counts is None and n == b.max_dst
+    if out is None:
+        out = _new((n, hq, d), q.dtype, q, stream, None if exact else 0)
+    if lse is None:
+        lse = _new((n, hq), torch.float32, q, stream, None if exact else -math.inf)
+    elif lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.dim() != 2 or lse.shape[0] < b.max_dst or lse.shape[1] != hq:
+        raise TypeError("lse must be a contiguous float32 tensor [dst, q_heads]")
+    keep, (pq, po) = _heads(q.dtype, (q, "q", b.max_dst, hq, d), (out, "out", b.max_dst, hq, d))
+    device = _one_device(q, indptr, indices, k.codes, v.codes, workspace, rows, out, lse, *(() if counts is None else counts))
+    _run(device, _L.gs_coded_attention_forward, ctypes.byref(b), _addr(rows), int(max_row), _dtype(q.dtype), hq, d, d ** -0.5 if scale is None else float(scale),
+         pq, k.address, v.address, po, _addr(lse), *_workspace(workspace), _on(stream, workspace))
+    return out, lse
+
+
+def _dense(t: torch.Tensor, what: str) -> torch.Tensor:
+    """A tensor whose elements fill its memory without gaps, in any order of dimensions."""
+    if not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % what)
+    if not t.is_contiguous():
+        at = 1
+        for stride, size in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
+            if stride != at:
+                raise TypeError("%s has gaps or overlaps in memory" % what)
+            at *= size
+    return t
+
+
+def gs_grad_workspace_bytes(num_grads: int) -> int:
+    out = ctypes.c_size_t()
+    _check(_L.gs_grad_workspace_bytes(int(num_grads), ctypes.byref(out)))
+    return out.value
+
+
+def _grad_list(grads, out, counts):
+    """gs_grad of every gradient, six words each."""
+    if out is not None and len(out) != len(grads) or counts is not None and len(counts) != len(grads):
+        raise ValueError("one result and one count per gradient expected")
+    words = []
+    for i, g in enumerate(grads):
+        o = g if out is None else out[i]
+        c = None if counts is None else counts[i]
+        _dense(g, "each gradient")
+        if o is not g and (o.dtype is not g.dtype or o.shape != g.shape or o.stride() != g.stride() or not o.is_cuda):
+            raise TypeError("a result must have the dtype, shape and strides of its gradient")
+        if c is not None and (g.dim() < 1 or not g.is_contiguous()):
+            raise TypeError("a gradient with a count must be a contiguous tensor of rows")
+        n = g.numel()
+        words += (g.data_ptr(), o.data_ptr(), n, _counter(c, "each of counts") or 0, 0 if c is None or not n else n // g.shape[0], _dtype(g.dtype))
+    return (ctypes.c_int64 * max(1, len(words)))(*words)
+
+
+def gs_grad_norm(grads, workspace: torch.Tensor, norm: torch.Tensor = None, counts=None, stream=None) -> torch.Tensor:
+    """The norm over all numbers of a list of gradients, as float32[1] on the device.  `counts`: for each gradient None, or the
+    device's number of its rows that count (as gs_embedding_backward_sparse returns it)."""
+    grads = list(grads)
+    norm = _new(1, torch.float32, workspace, stream) if norm is None else _f32_rows(norm, "norm", 1)
+    device = _one_device(workspace, norm, *grads, *(counts or ()))
+    words = _grad_list(grads, None, counts)
+    _run(device, _L.gs_grad_norm, ctypes.addressof(words), len(grads), _addr(norm), *_workspace(workspace), _on(stream, workspace))
+    return norm
+
+
+def gs_grad_clip(grads, max_norm: float, workspace: torch.Tensor, out=None, norm: torch.Tensor = None, counts=None, stream=None) -> torch.Tensor:
+    """Scales a list of gradients by min(1, max_norm / (norm + 1e-6)), in place or into the list `out`, and returns their norm before
+    that.  `counts`: as for gs_grad_norm; rows behind a count are left as they are.  Nothing waits for the device."""
+    grads = list(grads)
+    norm = _new(1, torch.float32, workspace, stream) if norm is None else _f32_rows(norm, "norm", 1)
+    device = _one_device(workspace, norm, *grads, *(out or ()), *(counts or ()))
+    words = _grad_list(grads, out, counts)
+    _run(device, _L.gs_grad_clip, ctypes.addressof(words), len(grads), float(max_norm), _addr(norm), *_workspace(workspace), _on(stream, workspace))
+    return norm

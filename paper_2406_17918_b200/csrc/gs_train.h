@@ -151,4 +151,86 @@ size_t xent_workspace(const Xent& a);      // sizes and dtype only
 cudaError_t launch_xent_forward(const Xent& a, void* workspace, cudaStream_t s);
 cudaError_t launch_xent_backward(const Xent& a, void* workspace, cudaStream_t s);
 
+// ---- rows in 8 bits ----
+struct CodedView {
+    uint8_t* codes;         // [rows][row_stride], head h at h * pitch
+    uint8_t* scales;        // [blocks][scale_stride]
+    int64_t rows, row_stride, scale_stride;
+    int32_t heads, head_dim, pitch, shift;    // blocks of 1 << shift rows
+};
+struct CodedWrite {
+    CodedView to;
+    HeadView in;
+    gs_dtype dtype;
+    const int32_t* ids;     // NULL: the rows from `first` on
+    int64_t first;
+    Count n;
+    int32_t* claims;
+    int tl, head_tiles, take;
+};
+cudaError_t launch_coded_write(const CodedWrite& p, cudaStream_t s);
+struct CodedRead {
+    CodedView from;
+    HeadView out;
+    gs_dtype dtype;
+    const int32_t* ids;
+    int64_t first;
+    Count n;
+    int tl;
+};
+cudaError_t launch_coded_read(const CodedRead& p, cudaStream_t s);
+
+// ---- attention over such rows ----
+struct CodedAttention {
+    const int32_t* indptr;
+    const int32_t* indices;
+    const int32_t* row_of;  // NULL: a source is its row
+    Count dst, src;
+    int32_t edge_bound, max_row;
+    gs_dtype dtype;
+    int32_t q_heads, kv_heads, head_dim;
+    float scale;
+    HeadView q, out;
+    CodedView k, v;
+    float* lse;
+};
+size_t coded_attention_workspace(int64_t edges, int32_t q_heads, int32_t head_dim);
+cudaError_t launch_coded_attention(const CodedAttention& a, void* workspace, cudaStream_t s);
+
+// ---- root-mean-square norm ----
+struct RmsNorm {
+    const void* x;          // backward: what was normalised
+    const void* residual;   // backward: the gradient that comes along the residual path
+    const void* dout;       // backward
+    const void* weight;
+    void* hidden;
+    void* out;              // backward: dx
+    void* dweight;
+    int64_t x_ld, residual_ld, dout_ld, hidden_ld, out_ld;
+    gs_dtype dtype, weight_dtype;
+    Count n;
+    int32_t dim;
+    float eps;
+    CodedView coded;        // output in 8 bits
+    int tl;
+};
+constexpr int NORM_MAX_DIM = 8192;      // 512 threads of 16 elements
+size_t norm_workspace(int64_t rows, int32_t dim);
+cudaError_t launch_norm_forward(const RmsNorm& p, bool coded, cudaStream_t s);
+cudaError_t launch_norm_backward(const RmsNorm& p, void* workspace, cudaStream_t s);
+
+// ---- the norm over many gradients ----
+struct GradTensor {
+    const void* grad;
+    void* out;              // clipping: where the scaled gradient goes (grad itself: in place)
+    const int32_t* d_rows;  // NULL: all of it; else the rows of row_elems that count
+    int64_t elems;
+    int64_t row_elems;
+    gs_dtype dtype;
+    int32_t first_tile;
+};
+size_t grad_workspace(int32_t tensors);
+// norm: the global norm, on the device.  clip: `out` of every tensor gets the scaled gradient.
+cudaError_t launch_grad_norm(const GradTensor* tensors, int32_t n, bool clip, float max_norm, float* norm, void* workspace, cudaStream_t s);
+
 }  // namespace gs

@@ -1,30 +1,12 @@
 // The C ABI of the training operators: argument checks and launches.
-#include "gs_train.h"
+#include "gs_train_args.h"
 #include "gs_xent.h"
 
 using namespace gs;
 
 namespace {
 
-bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
-bool known(gs_dtype t) { return t == GS_F32 || t == GS_BF16; }
 constexpr int64_t XENT_MAX_VOCAB = ((int64_t)1 << 31) - 257;   // row numbers of whole tiles stay below 2^31
-size_t size_of(gs_dtype t) { return t == GS_BF16 ? 2 : 4; }
-
-gs_status cuda_error(cudaError_t e, const char* what) { return set_error(GS_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e)); }
-
-#define GS_TRAIN_CUDA(call)                                     \
-    do {                                                        \
-        const cudaError_t e__ = (call);                         \
-        if (e__ != cudaSuccess) return cuda_error(e__, #call);  \
-    } while (0)
-
-gs_status check_workspace(const void* ws, size_t have, size_t need) {
-    if (!ws) return set_error(GS_ERR_ARG, "workspace is NULL");
-    if (!aligned_to(ws, 256)) return set_error(GS_ERR_ALIGN, "workspace is not 256-byte aligned");
-    if (have < need) return set_error(GS_ERR_WORKSPACE, "workspace holds %zu bytes, %zu are needed", have, need);
-    return GS_OK;
-}
 
 gs_status check_table(int64_t rows, int32_t dim) {
     if (rows < 1 || rows >= ((int64_t)1 << 31)) return set_error(GS_ERR_ARG, "table_rows outside [1, 2^31)");
@@ -54,31 +36,6 @@ gs_status embedding_grad(EmbedGrad g, bool sparse, void* ws, size_t ws_bytes, cu
     GS_TRAIN_CUDA(launch_embedding_grad(g, ws, s));
     return GS_OK;
 }
-
-gs_status check_block(const gs_block* b) {
-    if (!b) return set_error(GS_ERR_ARG, "block is NULL");
-    if (b->max_dst < 0 || b->max_src < 0 || b->max_edges < 0 || b->max_edges >= (1 << 30)) return set_error(GS_ERR_ARG, "a size of the block is out of range");
-    if (!b->d_indptr || (b->max_edges > 0 && !b->d_indices)) return set_error(GS_ERR_ARG, "the block has no arrays");
-    const int given = (b->d_num_dst != nullptr) + (b->d_num_src != nullptr) + (b->d_num_edges != nullptr);
-    if (given != 0 && given != 3) return set_error(GS_ERR_ARG, "the block's device counts are given all together or not at all");
-    if (!aligned_to(b->d_indptr, 4) || !aligned_to(b->d_indices, 4) || !aligned_to(b->d_num_dst, 4) || !aligned_to(b->d_num_src, 4) || !aligned_to(b->d_num_edges, 4))
-        return set_error(GS_ERR_ALIGN, "misaligned block array");
-    return GS_OK;
-}
-
-gs_status check_heads(const char* name, const gs_heads* h, int64_t rows, int32_t heads, int32_t dim, gs_dtype t, HeadView* out) {
-    if (!h || (!h->d_data && rows > 0)) return set_error(GS_ERR_ARG, "%s is NULL", name);
-    if ((heads > 1 && h->head_stride < dim) || (rows > 1 && h->row_stride < dim)) return set_error(GS_ERR_ARG, "%s: a stride is smaller than head_dim", name);
-    if (!aligned_to(h->d_data, size_of(t))) return set_error(GS_ERR_ALIGN, "%s is misaligned", name);
-    *out = HeadView{h->d_data, h->row_stride, h->head_stride};
-    return GS_OK;
-}
-
-#define GS_TRY(call)                          \
-    do {                                      \
-        const gs_status s__ = (call);         \
-        if (s__ != GS_OK) return s__;         \
-    } while (0)
 
 gs_status check_attention(const gs_block* b, int32_t max_row, gs_dtype t, int32_t q_heads, int32_t kv_heads, int32_t dim, BlockAttention* a) {
     GS_TRY(check_block(b));
