@@ -1059,7 +1059,7 @@ class _CCoded(ctypes.Structure):
 class CodedRows:
     """Rows in 8 bits over two caller-owned tensors (see gs_coded in include/gs.h): codes [rows, heads, pitch] (float8_e4m3fn or
     uint8; pitch = head_dim rounded up to 16) and scales uint8 [ceil(rows / block), heads].  Tensors of zeros are a store of zero
-    rows.  A store holds an int32 per row and block beside them, for writes by id; two of those on one store may not overlap."""
+    rows.  A store holds an int32 per row and two per block beside them, for writes by id; two of those on one store may not overlap."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, head_dim: int, block: int = 1):
         head_dim, block = int(head_dim), int(block)
@@ -1075,7 +1075,7 @@ class CodedRows:
         device = _one_device(codes, scales)
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("a store cannot be made while a graph is captured")
-        claims = torch.full((rows + (scales.shape[0] if block > 1 else 0),), -1, dtype=torch.int32, device=torch.device("cuda", device))
+        claims = torch.full((rows + (2 * scales.shape[0] + 2 if block > 1 else 0),), -1, dtype=torch.int32, device=torch.device("cuda", device))
         self._set(codes, scales, head_dim, block, claims)
 
     def _set(self, codes, scales, head_dim, block, claims):

@@ -17,12 +17,12 @@ namespace gs {
 
 constexpr int CA_THREADS = 128;
 constexpr int CA_LONG = 64;          // rows of more edges go to the chunk list
-constexpr int CA_CHUNK = 256;        // edges of a chunk
+constexpr int CA_CHUNK = 128;        // edges of a chunk
 constexpr float CA_LOG2E = 1.4426950408889634f, CA_LN2 = 0.6931471805599453f;
 
 struct CodedAttend {
     CodedAttention a;
-    int tl, slots, units_per_row;
+    int tl, slots, units_per_row, unit_shift;
     int wide;                        // q and out in whole pieces
     int split, chunk_mode;
     int32_t* words;                  // [0] chunks, [1] long rows
@@ -46,12 +46,12 @@ __device__ __forceinline__ int list_length(const Count& c) {
 // VE codes as VE / 2 pairs.
 template <int VE> struct Codes {
     uint32_t w[VE / 4];
-    __device__ __forceinline__ void load(const uint8_t* p, bool on) {
+    __device__ __forceinline__ void take(const unsigned char* p) {
         if constexpr (VE == 16) {
-            const uint4 x = on ? __ldg(reinterpret_cast<const uint4*>(p)) : make_uint4(0, 0, 0, 0);
+            const uint4 x = *reinterpret_cast<const uint4*>(p);
             w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
         } else {
-            const uint2 x = on ? __ldg(reinterpret_cast<const uint2*>(p)) : make_uint2(0, 0);
+            const uint2 x = *reinterpret_cast<const uint2*>(p);
             w[0] = x.x; w[1] = x.y;
         }
     }
@@ -108,145 +108,232 @@ template <typename T, int VE> __device__ __forceinline__ void store_out(T* row, 
     }
 }
 
-template <typename T, int VE, int G, int U> __global__ void __launch_bounds__(CA_THREADS) k_coded_attend(const __grid_constant__ CodedAttend P) {
+// What a warp works on at a time: a set of units, one to each group of lanes (or to `slots` groups), over the same number of batches.
+struct CodedUnits {
+    int r, row, unit, begin, end;    // r: the row, or the chunk
+    bool live;
+};
+
+__device__ __forceinline__ CodedUnits find_units(const CodedAttend& P, int64_t u, int64_t units, int part, int parts) {
+    CodedUnits w;
+    w.live = u < units;
+    w.r = w.row = w.unit = w.begin = w.end = 0;
+    if (!w.live) return w;
+    if (P.unit_shift >= 0) w.r = (int)(u >> P.unit_shift);
+    else w.r = units >> 31 ? (int)(u / P.units_per_row) : (int)((uint32_t)u / (uint32_t)P.units_per_row);
+    w.unit = (int)(u - (int64_t)w.r * P.units_per_row);
+    w.row = w.r;
+    int skip = 0;
+    if (P.chunk_mode) {
+        const int2 it = P.items[w.r];
+        w.row = it.x;
+        skip = it.y * CA_CHUNK;
+    }
+    int b = __ldg(P.a.indptr + w.row), e = __ldg(P.a.indptr + w.row + 1);
+    b = b < 0 ? 0 : b;
+    e = e > P.a.edge_bound ? P.a.edge_bound : e;
+    if (e < b) e = b;
+    if (P.chunk_mode) {
+        w.begin = b + skip;
+        w.end = w.begin + CA_CHUNK < e ? w.begin + CA_CHUNK : e;
+    } else if (P.split && e - b > CA_LONG) {
+        if (w.unit == 0) {                                   // listed once, by the lanes of the row's first unit
+            const int nc = (e - b + CA_CHUNK - 1) / CA_CHUNK, lanes = parts - 1;
+            const uint32_t mask = parts == 32 ? FULL : ((1u << parts) - 1u) << (threadIdx.x & 31 & ~lanes);
+            int first = 0;
+            if (part == 0) {
+                first = atomicAdd(P.words, nc);
+                P.longs[atomicAdd(P.words + 1, 1)] = make_int4(w.row, first, nc, 0);
+            }
+            first = __shfl_sync(mask, first, threadIdx.x & 31 & ~lanes);
+            for (int c = part; c < nc; c += parts) P.items[first + c] = make_int2(w.row, c);
+        }
+        w.live = false;
+    } else {
+        w.begin = b;
+        w.end = e;
+    }
+    return w;
+}
+
+// The batches of a warp's sets are one stream: the codes of a batch are on their way to slots of the lane's own in shared memory
+// (zeros where there is no edge) while the batch before is worked on, the rows of the next one are looked up, and the next set's
+// offsets and query rows are fetched when its first batch is.  No lane reads what another has copied: no barriers.
+template <typename T, int VE, int G, int U> __global__ void __launch_bounds__(CA_THREADS, G == 1 ? 4 : 3) k_coded_attend(const __grid_constant__ CodedAttend P) {
     constexpr int N2 = VE / 2;
+    constexpr int SLOT = U * 2 * VE * 32;                    // bytes of a batch's copies, per warp
+    extern __shared__ __align__(16) unsigned char ca_smem[];
     chain_wait();
     const int lane = threadIdx.x & 31, tl = P.tl, t = lane & (tl - 1), slot = (lane / tl) & (P.slots - 1);
-    const int width = tl * P.slots, per_block = CA_THREADS / width;
+    const int width = tl * P.slots, per_warp = 32 / width;
     const int rows = P.chunk_mode ? __ldcg(P.words) : list_length(P.a.dst), cols = list_length(P.a.src);
     const int64_t units = (int64_t)rows * P.units_per_row;
+    const int64_t step = (int64_t)gridDim.x * (CA_THREADS / 32) * per_warp;
     const float c2 = P.a.scale * CA_LOG2E;
-    const int D = P.a.head_dim, c0 = t * VE;
-    const bool held = c0 < P.a.k.pitch;                      // this lane has a piece of the codes
-    for (int64_t base = (int64_t)blockIdx.x * per_block; base < units; base += (int64_t)gridDim.x * per_block) {
-        const int64_t u = base + threadIdx.x / width;
-        bool live = u < units;
-        const int r = live ? (int)(u / P.units_per_row) : 0, unit = live ? (int)(u - (int64_t)r * P.units_per_row) : 0;
-        int row = r, begin = 0, end = 0;
-        if (live) {
-            int skip = 0;
-            if (P.chunk_mode) {
-                const int2 it = P.items[r];
-                row = it.x;
-                skip = it.y * CA_CHUNK;
-            }
-            int b = __ldg(P.a.indptr + row), e = __ldg(P.a.indptr + row + 1);
-            b = b < 0 ? 0 : b;
-            e = e > P.a.edge_bound ? P.a.edge_bound : e;
-            if (e < b) e = b;
-            if (P.chunk_mode) {
-                begin = b + skip;
-                end = begin + CA_CHUNK < e ? begin + CA_CHUNK : e;
-            } else if (P.split && e - b > CA_LONG) {
-                if (unit == 0 && t == 0 && slot == 0) {      // listed once, from the row's first unit
-                    const int nc = (e - b + CA_CHUNK - 1) / CA_CHUNK, first = atomicAdd(P.words, nc);
-                    P.longs[atomicAdd(P.words + 1, 1)] = make_int4(row, first, nc, 0);
-                    for (int c = 0; c < nc; ++c) P.items[first + c] = make_int2(row, c);
-                }
-                live = false;
-            } else {
-                begin = b;
-                end = e;
-            }
+    const int D = P.a.head_dim, c0 = t * VE, group = P.a.q_heads / P.a.kv_heads;
+    const int held = c0 < P.a.k.pitch ? VE : 0;              // this lane has a piece of the codes
+    const uint32_t kstep = (uint32_t)P.a.k.row_stride, vstep = (uint32_t)P.a.v.row_stride, ksstep = (uint32_t)P.a.k.scale_stride, vsstep = (uint32_t)P.a.v.scale_stride;
+    unsigned char* mine = ca_smem + (threadIdx.x >> 5) * 2 * SLOT + lane * VE;
+    const uint32_t mine_a = (uint32_t)__cvta_generic_to_shared(mine);
+
+    // ---- ahead: the set whose batches are being fetched
+    int64_t base = ((int64_t)blockIdx.x * (CA_THREADS / 32) + (threadIdx.x >> 5)) * per_warp;
+    CodedUnits w = find_units(P, base + lane / width, units, lane & (width - 1), width);
+    const uint8_t* kbase = nullptr;
+    const uint8_t* vbase = nullptr;
+    const uint8_t* ksbase = nullptr;
+    const uint8_t* vsbase = nullptr;
+    f32x2 qn[G][N2];
+    int trips = 0, it = 0;
+    int next[U];                                             // the rows of the batch that is fetched next, -1 where there is none
+    auto begin_set = [&]() {
+        const int h0 = w.unit * G, g = h0 / group;
+        kbase = P.a.k.codes + (int64_t)g * P.a.k.pitch + (held ? c0 : 0);
+        vbase = P.a.v.codes + (int64_t)g * P.a.v.pitch + (held ? c0 : 0);
+        ksbase = P.a.k.scales + g;
+        vsbase = P.a.v.scales + g;
+        const int n = (w.end - w.begin + P.slots * U - 1) / (P.slots * U);
+        trips = __reduce_max_sync(FULL, n < 1 ? 1 : n);
+        it = 0;
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+            load_piece<T, VE>((const T*)P.a.q.data + (int64_t)w.row * P.a.q.row_stride + (int64_t)(h0 + i) * P.a.q.head_stride, c0, D, P.wide, w.live, qn[i]);
+    };
+    auto look = [&]() {
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int e = w.begin + (it * U + j) * P.slots + slot;
+            int col = e < w.end ? __ldg(P.a.indices + e) : -1;
+            if ((uint32_t)col >= (uint32_t)cols) col = -1;
+            if (P.a.row_of && col >= 0) col = __ldg(P.a.row_of + col);
+            next[j] = (uint32_t)col < (uint32_t)P.a.k.rows ? col : -1;
         }
-        const int h0 = unit * G, g = h0 / (P.a.q_heads / P.a.kv_heads);
-        const uint8_t* kbase = P.a.k.codes + (int64_t)g * P.a.k.pitch + c0;
-        const uint8_t* vbase = P.a.v.codes + (int64_t)g * P.a.v.pitch + c0;
-        f32x2 q[G][N2], acc[G][N2];
-        float m[G], l[G];
+    };
+    uint32_t ks[U], vs[U], on = 0;                           // of the batch on its way
+    auto issue = [&](int s) {
+        on = 0;
 #pragma unroll
-        for (int i = 0; i < G; ++i) {
-            load_piece<T, VE>((const T*)P.a.q.data + (int64_t)row * P.a.q.row_stride + (int64_t)(h0 + i) * P.a.q.head_stride, c0, D, P.wide, live, q[i]);
-            m[i] = -INFINITY;
-            l[i] = 0.f;
-#pragma unroll
-            for (int c = 0; c < N2; ++c) acc[i][c] = 0;
+        for (int j = 0; j < U; ++j) {
+            const bool is = next[j] >= 0;
+            const uint32_t at = is ? (uint32_t)next[j] : 0u, b = at >> P.a.k.shift;
+            const int bytes = is ? held : 0;
+            copy_async<VE>(mine_a + s * SLOT + j * 2 * VE * 32, kbase + (uint64_t)at * kstep, bytes);
+            copy_async<VE>(mine_a + s * SLOT + (j * 2 + 1) * VE * 32, vbase + (uint64_t)at * vstep, bytes);
+            ks[j] = is ? __ldg(ksbase + (uint64_t)b * ksstep) : 0u;
+            vs[j] = is ? __ldg(vsbase + (uint64_t)b * vsstep) : 0u;
+            on |= is ? 1u << j : 0u;
         }
-        const int step = P.slots * U;
-        const int trips = __reduce_max_sync(FULL, (end - begin + step - 1) / step);
-        // the cache rows of a batch's edges, -1 where there is none
-        auto look = [&](int it, int (&at)[U]) {
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    bool more = base < units;
+    if (!more) return;
+    begin_set();
+    look();
+    issue(0);
+
+    f32x2 q[G][N2], acc[G][N2];
+    float m[G], l[G];
+    int s = 0;
+    while (more) {
+        const bool first = it == 0, last = it + 1 == trips;
+        const CodedUnits cur = w;
+        const uint32_t my_on = on;
+        uint32_t my_ks[U], my_vs[U];
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const int e = begin + (it * U + j) * P.slots + slot;
-                int col = e < end ? __ldg(P.a.indices + e) : -1;
-                if ((uint32_t)col >= (uint32_t)cols) col = -1;
-                if (P.a.row_of && col >= 0) col = __ldg(P.a.row_of + col);
-                at[j] = (uint32_t)col < (uint64_t)P.a.k.rows ? col : -1;
-            }
-        };
-        int next[U];
-        look(0, next);
-        for (int it = 0; it < trips; ++it) {
-            int at[U];
-            Codes<VE> kc[U], vc[U];
-            uint32_t ks[U], vs[U];
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                at[j] = next[j];
-                const bool on = at[j] >= 0;
-                const int64_t b = at[j] >> P.a.k.shift;
-                kc[j].load(kbase + (int64_t)at[j] * P.a.k.row_stride, on && held);
-                vc[j].load(vbase + (int64_t)at[j] * P.a.v.row_stride, on && held);
-                ks[j] = on ? __ldg(P.a.k.scales + b * P.a.k.scale_stride + g) : 0u;
-                vs[j] = on ? __ldg(P.a.v.scales + b * P.a.v.scale_stride + g) : 0u;
-            }
-            look(it + 1, next);
-            float s[U * G];
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                f32x2 k[N2];
-                kc[j].get(k);
-#pragma unroll
-                for (int i = 0; i < G; ++i) {
-                    f32x2 x = mul2(q[i][0], k[0]);
-#pragma unroll
-                    for (int c = 1; c < N2; ++c) x = fma2(q[i][c], k[c], x);
-                    float lo, hi;
-                    split(x, lo, hi);
-                    s[j * G + i] = lo + hi;
-                }
-            }
-            for (int o = 1; o < tl; o <<= 1) {
-#pragma unroll
-                for (int x = 0; x < U * G; ++x) s[x] += __shfl_xor_sync(FULL, s[x], o);
-            }
-            float p[U * G];
+        for (int j = 0; j < U; ++j) {
+            my_ks[j] = ks[j];
+            my_vs[j] = vs[j];
+        }
+        if (first) {
 #pragma unroll
             for (int i = 0; i < G; ++i) {
-                float top = m[i];
+                m[i] = -INFINITY;
+                l[i] = 0.f;
 #pragma unroll
-                for (int j = 0; j < U; ++j) {
-                    s[j * G + i] = at[j] >= 0 ? s[j * G + i] * scale_of(ks[j]) * c2 : -INFINITY;
-                    top = fmaxf(top, s[j * G + i]);
-                }
-                const float ref = top == -INFINITY ? 0.f : top;     // nothing seen yet: all weights are zero
-                const float corr = exp2_fast(m[i] - ref);
-                m[i] = top;
-                l[i] *= corr;
-#pragma unroll
-                for (int j = 0; j < U; ++j) {
-                    p[j * G + i] = exp2_fast(s[j * G + i] - ref);
-                    l[i] += p[j * G + i];
-                }
-                const f32x2 cc = pair(corr, corr);
-#pragma unroll
-                for (int c = 0; c < N2; ++c) acc[i][c] = mul2(cc, acc[i][c]);
-            }
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                f32x2 v[N2];
-                vc[j].get(v);
-                const float sv = scale_of(vs[j]);
-#pragma unroll
-                for (int i = 0; i < G; ++i) {
-                    const float w = p[j * G + i] * sv;
-                    const f32x2 ww = pair(w, w);
-#pragma unroll
-                    for (int c = 0; c < N2; ++c) acc[i][c] = fma2(ww, v[c], acc[i][c]);
+                for (int c = 0; c < N2; ++c) {
+                    q[i][c] = qn[i][c];
+                    acc[i][c] = 0;
                 }
             }
         }
+        // what comes next: this set's next batch, or the next set's first
+        ++it;
+        if (last) {
+            base += step;
+            more = base < units;
+            if (more) {
+                w = find_units(P, base + lane / width, units, lane & (width - 1), width);
+                begin_set();
+            }
+        }
+        if (more) {
+            look();
+            issue(s ^ 1);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+        } else {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        }
+        const unsigned char* from = mine + s * SLOT;
+        s ^= 1;
+        float sc[U * G];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            Codes<VE> kc;
+            f32x2 k[N2];
+            kc.take(from + j * 2 * VE * 32);
+            kc.get(k);
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                f32x2 x = mul2(q[i][0], k[0]);
+#pragma unroll
+                for (int c = 1; c < N2; ++c) x = fma2(q[i][c], k[c], x);
+                float lo, hi;
+                split(x, lo, hi);
+                sc[j * G + i] = lo + hi;
+            }
+        }
+        for (int o = 1; o < tl; o <<= 1) {
+#pragma unroll
+            for (int x = 0; x < U * G; ++x) sc[x] += __shfl_xor_sync(FULL, sc[x], o);
+        }
+        float p[U * G];
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            float top = m[i];
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                sc[j * G + i] = my_on >> j & 1 ? sc[j * G + i] * scale_of(my_ks[j]) * c2 : -INFINITY;
+                top = fmaxf(top, sc[j * G + i]);
+            }
+            const float ref = top == -INFINITY ? 0.f : top;         // nothing seen yet: all weights are zero
+            const float corr = exp2_fast(m[i] - ref);
+            m[i] = top;
+            l[i] *= corr;
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                p[j * G + i] = exp2_fast(sc[j * G + i] - ref);
+                l[i] += p[j * G + i];
+            }
+            const f32x2 cc = pair(corr, corr);
+#pragma unroll
+            for (int c = 0; c < N2; ++c) acc[i][c] = mul2(cc, acc[i][c]);
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            Codes<VE> vc;
+            f32x2 v[N2];
+            vc.take(from + (j * 2 + 1) * VE * 32);
+            vc.get(v);
+            const float sv = scale_of(my_vs[j]);
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                const float x = p[j * G + i] * sv;
+                const f32x2 xx = pair(x, x);
+#pragma unroll
+                for (int c = 0; c < N2; ++c) acc[i][c] = fma2(xx, v[c], acc[i][c]);
+            }
+        }
+        if (!last) continue;
         for (int o = tl; o < width; o <<= 1) {                        // join the slots of a row
 #pragma unroll
             for (int i = 0; i < G; ++i) {
@@ -260,15 +347,15 @@ template <typename T, int VE, int G, int U> __global__ void __launch_bounds__(CA
                 for (int c = 0; c < N2; ++c) acc[i][c] = fma2(aa, acc[i][c], mul2(bb, __shfl_xor_sync(FULL, acc[i][c], o)));
             }
         }
-        if (!live || slot) continue;
+        if (!cur.live || slot) continue;
 #pragma unroll
         for (int i = 0; i < G; ++i) {
-            const int h = h0 + i;
+            const int h = cur.unit * G + i;
             float y[VE];
 #pragma unroll
             for (int c = 0; c < N2; ++c) split(acc[i][c], y[2 * c], y[2 * c + 1]);
             if (P.chunk_mode) {
-                float* part = P.partial + ((int64_t)r * P.a.q_heads + h) * (D + 2);
+                float* part = P.partial + ((int64_t)cur.r * P.a.q_heads + h) * (D + 2);
 #pragma unroll
                 for (int c = 0; c < VE; ++c)
                     if (c0 + c < D) part[c0 + c] = y[c];
@@ -281,8 +368,8 @@ template <typename T, int VE, int G, int U> __global__ void __launch_bounds__(CA
                 const float inv = none ? 0.f : 1.f / l[i];
 #pragma unroll
                 for (int c = 0; c < VE; ++c) y[c] = none ? 0.f : y[c] * inv;
-                store_out<T, VE>((T*)P.a.out.data + (int64_t)row * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride, c0, D, P.wide, y);
-                if (t == 0) P.a.lse[(int64_t)row * P.a.q_heads + h] = none ? -INFINITY : m[i] * CA_LN2 + logf(l[i]);
+                store_out<T, VE>((T*)P.a.out.data + (int64_t)cur.row * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride, c0, D, P.wide, y);
+                if (t == 0) P.a.lse[(int64_t)cur.row * P.a.q_heads + h] = none ? -INFINITY : m[i] * CA_LN2 + logf(l[i]);
             }
         }
     }
@@ -290,8 +377,8 @@ template <typename T, int VE, int G, int U> __global__ void __launch_bounds__(CA
 
 // One block per (long row, query head): the chunks' sums rescaled to the common maximum; each warp adds a contiguous share of the
 // chunks, the shares are added in order.
-template <typename T> __global__ void __launch_bounds__(256) k_coded_attend_join(const __grid_constant__ CodedAttend P) {
-    constexpr int W = 8;
+template <typename T> __global__ void __launch_bounds__(1024) k_coded_attend_join(const __grid_constant__ CodedAttend P) {
+    constexpr int W = 32;
     __shared__ float s_m[W], s_l[W], s_acc[W][256];
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = P.a.head_dim;
@@ -301,35 +388,43 @@ template <typename T> __global__ void __launch_bounds__(256) k_coded_attend_join
         const int h = (int)(u % P.a.q_heads);
         const float* part = P.partial + (int64_t)row.y * stride + (int64_t)h * (D + 2);
         const int per = (row.z + W - 1) / W, c0 = warp * per, c1 = c0 + per < row.z ? c0 + per : row.z;
-        float m = -INFINITY, l = 0.f;
+        // relative to this warp's own maximum first: nobody waits for the others' chunks
+        float m = -INFINITY, l = 0.f, acc[8] = {};
         for (int c = c0 + lane; c < c1; c += 32) m = fmaxf(m, part[c * stride + D]);
         for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, o));
-        __syncthreads();                                       // the previous unit's sums are read
-        if (lane == 0) s_m[warp] = m;
-        __syncthreads();
-        for (int w = 0; w < W; ++w) m = fmaxf(m, s_m[w]);
         const float ref = m == -INFINITY ? 0.f : m;
-        for (int c = c0 + lane; c < c1; c += 32) l += part[c * stride + D + 1] * exp2_fast(part[c * stride + D] - ref);
-        for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(FULL, l, o);
-        if (lane == 0) s_l[warp] = l;
-        for (int col = lane; col < D; col += 32) {
-            float acc = 0.f;
-#pragma unroll 4
-            for (int c = c0; c < c1; ++c) acc = fmaf(part[c * stride + col], exp2_fast(part[c * stride + D] - ref), acc);
-            s_acc[warp][col] = acc;
+#pragma unroll 8
+        for (int c = c0; c < c1; ++c) {
+            const float* x = part + c * stride;
+            const float scale = exp2_fast(x[D] - ref);
+            l = fmaf(x[D + 1], scale, l);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k * 32 + lane < D) acc[k] = fmaf(x[k * 32 + lane], scale, acc[k]);
         }
+        __syncthreads();                                       // the previous unit's sums are read
+        if (lane == 0) {
+            s_m[warp] = m;
+            s_l[warp] = l;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k * 32 + lane < D) s_acc[warp][k * 32 + lane] = acc[k];
         __syncthreads();
+        float top = -INFINITY;
+        for (int w = 0; w < W; ++w) top = fmaxf(top, s_m[w]);
+        const float all = top == -INFINITY ? 0.f : top;
         l = 0.f;
-        for (int w = 0; w < W; ++w) l += s_l[w];
+        for (int w = 0; w < W; ++w) l = fmaf(s_l[w], exp2_fast(s_m[w] - all), l);
         const bool none = l == 0.f;
         const float inv = none ? 0.f : 1.f / l;
         T* out = (T*)P.a.out.data + (int64_t)row.x * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride;
-        for (int col = threadIdx.x; col < D; col += 256) {
-            float acc = 0.f;
-            for (int w = 0; w < W; ++w) acc += s_acc[w][col];
-            out[col] = from_f32<T>(none ? 0.f : acc * inv);
+        for (int col = threadIdx.x; col < D; col += 1024) {
+            float sum = 0.f;
+            for (int w = 0; w < W; ++w) sum = fmaf(s_acc[w][col], exp2_fast(s_m[w] - all), sum);
+            out[col] = from_f32<T>(none ? 0.f : sum * inv);
         }
-        if (threadIdx.x == 0) P.a.lse[(int64_t)row.x * P.a.q_heads + h] = none ? -INFINITY : m * CA_LN2 + logf(l);
+        if (threadIdx.x == 0) P.a.lse[(int64_t)row.x * P.a.q_heads + h] = none ? -INFINITY : top * CA_LN2 + logf(l);
     }
 }
 
@@ -356,6 +451,10 @@ template <typename T, int VE, int G, int U> static cudaError_t run_coded(CodedAt
     P.tl = 1;
     while (P.tl < pieces) P.tl *= 2;
     P.units_per_row = P.a.q_heads / G;
+    P.unit_shift = -1;
+    for (int i = 0; i < 8; ++i)
+        if (P.units_per_row == 1 << i) P.unit_shift = i;
+    constexpr int smem = CA_THREADS / 32 * 2 * U * 2 * VE * 32;
     cudaError_t e = cudaSuccess;
     for (int pass = 0; pass < (P.split ? 2 : 1) && e == cudaSuccess; ++pass) {
         P.chunk_mode = pass;
@@ -366,11 +465,11 @@ template <typename T, int VE, int G, int U> static cudaError_t run_coded(CodedAt
         while (!pass && P.tl * P.slots * 2 <= 32 && n * P.units_per_row * P.tl * P.slots * 2 <= sm_count() * 16 * 32 && P.slots * U < longest) P.slots *= 2;
         const int per_block = CA_THREADS / (P.tl * P.slots);
         int64_t grid = (n * P.units_per_row + per_block - 1) / per_block;
-        const int64_t cap = sm_count() * (pass ? 16 : 64);
+        const int64_t cap = sm_count() * 16;
         if (grid > cap) grid = cap;
-        e = launch_train(k_coded_attend<T, VE, G, U>, grid, CA_THREADS, 0, s, P);
+        e = launch_train(k_coded_attend<T, VE, G, U>, grid, CA_THREADS, smem, s, P);
     }
-    if (P.split && e == cudaSuccess) e = launch_train(k_coded_attend_join<T>, sm_count() * 8, 256, 0, s, P);
+    if (P.split && e == cudaSuccess) e = launch_train(k_coded_attend_join<T>, sm_count() * 2, 1024, 0, s, P);
     return e;
 }
 
@@ -391,6 +490,7 @@ cudaError_t launch_coded_attention(const CodedAttention& a, void* workspace, cud
     P.items = (int2*)(ws + l.items);
     P.longs = (int4*)(ws + l.longs);
     P.partial = (float*)(ws + l.partial);
+    if (a.k.rows == 0) P.a.k.codes = P.a.v.codes = P.a.k.scales = P.a.v.scales = (uint8_t*)workspace;   // nothing is read: every edge is masked
     P.split = (a.max_row == 0 || a.max_row > CA_LONG) && a.edge_bound > CA_LONG;
     const int size = a.dtype == GS_BF16 ? 2 : 4, ve = 16 / size;
     auto on16 = [&](const HeadView& v) { return (uintptr_t)v.data % 16 == 0 && (v.row_stride * size) % 16 == 0 && (v.head_stride * size) % 16 == 0; };

@@ -18,13 +18,15 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
     const int b = (int)(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
     return b < 0 ? 0u : (uint32_t)b;
 }
-__device__ __forceinline__ float scale_of(uint32_t b) { return __uint_as_float(b ? b << 23 : 0x00400000u); }
+__device__ __forceinline__ float scale_of(uint32_t b) { return __uint_as_float(max(b << 23, 0x00400000u)); }
 // 2^(127 - b); bytes above 247 come from no float.
 __device__ __forceinline__ float unscale_of(uint32_t b) { return __uint_as_float(b < 254u ? (254u - b) << 23 : 0x00400000u); }
 
 // Two values to two codes, the first in the low byte; inf * 0 makes an infinity NaN, the conversion alone would make it 448.
 __device__ __forceinline__ uint32_t encode2(float x0, float x1, float unscale) {
-    const float y0 = fmaf(x0, 0.f, x0 * unscale), y1 = fmaf(x1, 0.f, x1 * unscale);
+    const f32x2 x = pair(x0, x1);
+    float y0, y1;
+    split(fma2(x, pair(0.f, 0.f), mul2(x, pair(unscale, unscale))), y0, y1);
     uint16_t r;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y1), "f"(y0));
     return r;

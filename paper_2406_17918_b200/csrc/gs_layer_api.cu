@@ -35,6 +35,8 @@ gs_status check_coded(const char* name, const gs_coded* c, CodedView* out) {
     if (c->rows > 0 && (!c->d_codes || !c->d_scales)) return set_error(GS_ERR_ARG, "%s has no arrays", name);
     if (c->row_stride % 16 || (c->rows > 1 && c->row_stride < (int64_t)c->heads * pitch)) return set_error(GS_ERR_ARG, "%s: row_stride is no multiple of 16, or too small", name);
     if (c->rows > c->block && c->scale_stride < c->heads) return set_error(GS_ERR_ARG, "%s: scale_stride is too small", name);
+    if (c->row_stride < 0 || c->row_stride >= ((int64_t)1 << 32) || c->scale_stride < 0 || c->scale_stride >= ((int64_t)1 << 32))
+        return set_error(GS_ERR_ARG, "%s: a stride is negative, or 4 GB or more", name);
     if (!aligned_to(c->d_codes, 16)) return set_error(GS_ERR_ALIGN, "%s: the codes are not 16-byte aligned", name);
     int shift = 0;
     while ((1 << shift) < c->block) ++shift;
@@ -163,6 +165,7 @@ gs_status gs_coded_write(const gs_coded* to, gs_dtype dtype, const gs_heads* row
     if (!known(dtype)) return set_error(GS_ERR_ARG, "unknown dtype %d", (int)dtype);
     GS_TRY(check_list(d_ids_or_null, first, d_count_or_null, count_bound, to->rows));
     GS_TRY(check_heads("rows", rows, count_bound, to->heads, to->head_dim, dtype, &p.in));
+    if (rows->row_stride * (int64_t)size_of(dtype) >= ((int64_t)1 << 32)) return set_error(GS_ERR_ARG, "the row pitch of rows is 4 GB or more");
     if (d_ids_or_null && !d_claims && to->rows > 0) return set_error(GS_ERR_ARG, "d_claims is NULL");
     if (!aligned_to(d_claims, 4)) return set_error(GS_ERR_ALIGN, "d_claims is misaligned");
     if (count_bound == 0 || to->rows == 0) return GS_OK;

@@ -5,10 +5,15 @@
 // Sums in 32 bits, one rounding per result.  v is recomputed by the backward pass, which has the row in hand anyway.
 //
 // Every element is read and written once, and that is the time: a row is held in registers by a group of lanes (rows of up to 32
-// pieces) or by a block, in pieces of 16 bytes where bases, pitches and the width allow, one element at a time otherwise.  dw: a
-// group keeps its columns' sums over all of its rows; blocks leave theirs in the workspace and a second kernel adds them in order.
+// pieces) or by a block, in pieces of 16 bytes.  Rows of odd widths begin anywhere within a piece: a block then takes the rows that
+// begin at one place of it (every 4th f32 row of 1,433, say), so that its threads keep their columns, and only the pieces at a
+// row's ends go one element at a time.  Arrays whose rows do not begin alike go one element at a time altogether.
+// dw: a group keeps its columns' sums over all of its rows; blocks leave theirs in the workspace and a second kernel adds them in
+// order.
 // Results in 8 bits: the largest magnitude of a group of columns is found among the lanes that hold it, by shuffles where the
 // group's pieces are a power of two and by integer maxima in shared memory otherwise.
+#include <type_traits>
+
 #include "gs_codes.cuh"
 #include "gs_device.cuh"
 #include "gs_train.h"
@@ -23,16 +28,82 @@ __device__ __forceinline__ int norm_rows(const Count& c) {
     return n < 0 ? 0 : (n > c.bound ? c.bound : n);
 }
 
-template <typename T, int VE, int NV> struct RowPart {
+// Elements in pairs for the packed 32-bit operations; rows that go one element at a time use plain floats.
+template <int VE> using El = std::conditional_t<VE == 1, float, f32x2>;
+template <int VE> constexpr int EL = VE == 1 ? 1 : VE / 2;
+__device__ __forceinline__ float v_mul(float a, float b) { return a * b; }
+__device__ __forceinline__ f32x2 v_mul(f32x2 a, f32x2 b) { return mul2(a, b); }
+__device__ __forceinline__ float v_fma(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ f32x2 v_fma(f32x2 a, f32x2 b, f32x2 c) { return fma2(a, b, c); }
+__device__ __forceinline__ float v_add(float a, float b) { return a + b; }
+__device__ __forceinline__ f32x2 v_add(f32x2 a, f32x2 b) { return add2(a, b); }
+__device__ __forceinline__ float v_sum(float a) { return a; }
+__device__ __forceinline__ float v_sum(f32x2 a) {
+    float x, y;
+    split(a, x, y);
+    return x + y;
+}
+template <int VE> __device__ __forceinline__ El<VE> v_all(float x) {
+    if constexpr (VE == 1) return x;
+    else return pair(x, x);
+}
+template <int VE> __device__ __forceinline__ void v_pack(const float (&x)[VE], El<VE> (&y)[EL<VE>]) {
+    if constexpr (VE == 1) {
+        y[0] = x[0];
+    } else {
+#pragma unroll
+        for (int i = 0; i < VE / 2; ++i) y[i] = pair(x[2 * i], x[2 * i + 1]);
+    }
+}
+template <int VE> __device__ __forceinline__ void v_unpack(const El<VE> (&y)[EL<VE>], float (&x)[VE]) {
+    if constexpr (VE == 1) {
+        x[0] = y[0];
+    } else {
+#pragma unroll
+        for (int i = 0; i < VE / 2; ++i) split(y[i], x[2 * i], x[2 * i + 1]);
+    }
+}
+
+// Where a block's rows begin: row v of its class is row v * period + cls, its first element `phase` elements behind the begin of a
+// piece (0 without EDGE).
+struct RowClass {
+    int cls, phase, n;               // n: rows of the class
+    int64_t blk, blks;
+};
+template <int VE, bool EDGE> __device__ __forceinline__ RowClass row_class(const RmsNorm& P, int n) {
+    if constexpr (!EDGE) return RowClass{0, 0, n, (int64_t)blockIdx.x, (int64_t)gridDim.x};
+    const int cls = (int)(blockIdx.x % P.period);
+    return RowClass{cls, (int)((P.phase + (int64_t)cls * P.x_ld) & (VE - 1)), n > cls ? (n - cls + P.period - 1) / P.period : 0, (int64_t)(blockIdx.x / P.period),
+                    (int64_t)(gridDim.x / P.period)};
+}
+
+template <typename T, int VE, int NV, bool EDGE> struct RowPart {
     Raw<T, VE> r[NV];
-    __device__ __forceinline__ void load(const T* row, int t, int width, int dim, bool on) {
+    __device__ __forceinline__ void load(const T* row, int t, int width, int phase, int dim, bool on) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (t + j * width) * VE;
-            r[j] = on && c < dim ? load_raw_stream<T, VE>(row + c) : zero_raw<T, VE>();
+            const int c = (t + j * width) * VE - phase;
+            if (EDGE && on && c < dim && (c < 0 || c + VE > dim)) {
+                float x[VE];
+#pragma unroll
+                for (int i = 0; i < VE; ++i) x[i] = c + i >= 0 && c + i < dim ? to_f32(row[c + i]) : 0.f;
+                set(j, x);
+            } else {
+                r[j] = on && c < dim ? load_raw_stream<T, VE>(row + c) : zero_raw<T, VE>();
+            }
         }
     }
     __device__ __forceinline__ void get(int j, float (&x)[VE]) const { unpack<T, VE>(r[j], x); }
+    __device__ __forceinline__ void pairs(int j, El<VE> (&y)[EL<VE>]) const {
+        float x[VE];
+        get(j, x);
+        v_pack<VE>(x, y);
+    }
+    __device__ __forceinline__ void set_pairs(int j, const El<VE> (&y)[EL<VE>]) {
+        float x[VE];
+        v_unpack<VE>(y, x);
+        set(j, x);
+    }
     __device__ __forceinline__ void set(int j, const float (&x)[VE]) {
         if constexpr (sizeof(T) == 4) {
             if constexpr (VE == 4) r[j].w = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
@@ -43,25 +114,35 @@ template <typename T, int VE, int NV> struct RowPart {
             r[j].w = (uint16_t)pack_bf16(x[0], 0.f);
         }
     }
-    __device__ __forceinline__ void store(T* row, int t, int width, int dim) const {
+    __device__ __forceinline__ void store(T* row, int t, int width, int phase, int dim) const {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (t + j * width) * VE;
-            if (c < dim) *reinterpret_cast<typename Raw<T, VE>::word*>(row + c) = r[j].w;
+            const int c = (t + j * width) * VE - phase;
+            if (EDGE && c < dim && (c < 0 || c + VE > dim)) {
+                float x[VE];
+                get(j, x);
+#pragma unroll
+                for (int i = 0; i < VE; ++i)
+                    if (c + i >= 0 && c + i < dim) row[c + i] = from_f32<T>(x[i]);
+            } else if (c < dim) {
+                *reinterpret_cast<typename Raw<T, VE>::word*>(row + c) = r[j].w;
+            }
         }
     }
 };
 
-template <int VE, int NV> __device__ __forceinline__ void load_weight(const RmsNorm& P, int t, int width, float (&w)[NV * VE]) {
+template <int VE, int NV> __device__ __forceinline__ void load_weight(const RmsNorm& P, int t, int width, int phase, El<VE> (&w)[NV][EL<VE>]) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
+        float x[VE];
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
-            const int c = (t + j * width) * VE + i;
-            float x = 1.f;
-            if (P.weight && c < P.dim) x = P.weight_dtype == GS_BF16 ? to_f32(static_cast<const bf16*>(P.weight)[c]) : static_cast<const float*>(P.weight)[c];
-            w[j * VE + i] = x;
+            const int c = (t + j * width) * VE + i - phase;
+            x[i] = 1.f;
+            if (P.weight && c >= 0 && c < P.dim) x[i] = P.weight_dtype == GS_BF16 ? to_f32(static_cast<const bf16*>(P.weight)[c]) : static_cast<const float*>(P.weight)[c];
         }
+        v_pack<VE>(x, w[j]);
+    }
 }
 
 // Sums over the threads of a row: a group of `width` lanes, or (BLOCK) all of the block.
@@ -95,11 +176,14 @@ __device__ __forceinline__ void store_codes(const RmsNorm& P, int64_t row, bool 
     uint32_t top[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        top[j] = 0;
+        float m = 0.f;                                       // NaN is passed over
 #pragma unroll
-        for (int i = 0; i < VE; ++i) {
-            const uint32_t m = finite_magnitude(y[j * VE + i]);
-            top[j] = m > top[j] ? m : top[j];
+        for (int i = 0; i < VE; ++i) m = fmaxf(m, fabsf(y[j * VE + i]));
+        top[j] = __float_as_uint(m);
+        if (m == INFINITY) {
+            top[j] = 0;
+#pragma unroll
+            for (int i = 0; i < VE; ++i) top[j] = max(top[j], finite_magnitude(y[j * VE + i]));
         }
     }
     const int per = hd / VE;                                 // pieces of a group of columns (VE > 1: whole ones)
@@ -108,8 +192,7 @@ __device__ __forceinline__ void store_codes(const RmsNorm& P, int64_t row, bool 
         for (int o = 1; o < per; o <<= 1) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                const uint32_t m = __shfl_xor_sync(FULL, top[j], o);
-                top[j] = m > top[j] ? m : top[j];
+                top[j] = max(top[j], __shfl_xor_sync(FULL, top[j], o));
             }
         }
     } else {
@@ -154,7 +237,7 @@ __device__ __forceinline__ void store_codes(const RmsNorm& P, int64_t row, bool 
 }
 
 // U rows of each group are in flight.
-template <typename T, int VE, int NV, int U, bool BLOCK, bool CODED>
+template <typename T, int VE, int NV, int U, bool BLOCK, bool EDGE, bool CODED>
 __global__ void __launch_bounds__(BLOCK ? 512 : NM_THREADS) k_norm_forward(const __grid_constant__ RmsNorm P) {
     constexpr int E = VE * NV;
     extern __shared__ uint32_t norm_tops[];                  // CODED: per row held
@@ -163,153 +246,197 @@ __global__ void __launch_bounds__(BLOCK ? 512 : NM_THREADS) k_norm_forward(const
     const int width = BLOCK ? (int)blockDim.x : P.tl, t = BLOCK ? (int)threadIdx.x : (int)threadIdx.x & (P.tl - 1), own = BLOCK ? 0 : threadIdx.x / width;
     const int per_block = BLOCK ? 1 : NM_THREADS / width;
     uint32_t* tops = CODED ? norm_tops + own * P.coded.heads : nullptr;
-    float w[E];
-    load_weight<VE, NV>(P, t, width, w);
-    for (int64_t base = (int64_t)blockIdx.x * per_block * U; base < n; base += (int64_t)gridDim.x * per_block * U) {
-        RowPart<T, VE, NV> x[U], r[U];
+    const RowClass C = row_class<VE, EDGE>(P, n);
+    El<VE> w[NV][EL<VE>];
+    RowPart<T, VE, NV, EDGE> x[U], r[U], xn[BLOCK ? U : 1], rn[BLOCK ? U : 1];
+    const int64_t step = C.blks * per_block * U;
+    int64_t base = C.blk * per_block * U;
+    auto row_at = [&](int64_t base, int u) { return EDGE ? (base + u * per_block + own) * P.period + C.cls : base + u * per_block + own; };
+    auto load = [&](int64_t base, auto& x, auto& r) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t row = base + u * per_block + own;
-            x[u].load((const T*)P.x + row * P.x_ld, t, width, D, row < n);
-            if (P.residual) r[u].load((const T*)P.residual + row * P.residual_ld, t, width, D, row < n);
+            const int64_t row = row_at(base, u);
+            const bool on = base < C.n && row < n;
+            x[u].load((const T*)P.x + row * P.x_ld, t, width, C.phase, D, on);
+            if (P.residual) r[u].load((const T*)P.residual + row * P.residual_ld, t, width, C.phase, D, on);
         }
+    };
+    load(base, x, r);
+    load_weight<VE, NV>(P, t, width, C.phase, w);
+    for (; base < C.n; base += step) {
+        if constexpr (BLOCK) load(base + step, xn, rn);      // few rows are held at a time: the next is on its way
         float sum[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            sum[u] = 0.f;
+            El<VE> q = v_all<VE>(0.f);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                float a[VE];
-                x[u].get(j, a);
+                El<VE> a[EL<VE>];
+                x[u].pairs(j, a);
                 if (P.residual) {
-                    float b[VE];
-                    r[u].get(j, b);
+                    El<VE> b[EL<VE>];
+                    r[u].pairs(j, b);
 #pragma unroll
-                    for (int i = 0; i < VE; ++i) a[i] += b[i];
-                    x[u].set(j, a);                          // rounded: what is normalised is what is kept
-                    x[u].get(j, a);
+                    for (int i = 0; i < EL<VE>; ++i) a[i] = v_add(a[i], b[i]);
+                    x[u].set_pairs(j, a);                    // rounded: what is normalised is what is kept
+                    x[u].pairs(j, a);
                 }
 #pragma unroll
-                for (int i = 0; i < VE; ++i) sum[u] = fmaf(a[i], a[i], sum[u]);
+                for (int i = 0; i < EL<VE>; ++i) q = v_fma(a[i], a[i], q);
             }
+            sum[u] = v_sum(q);
         }
         row_sum<BLOCK, U>(sum, width);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t row = base + u * per_block + own;
+            const int64_t row = row_at(base, u);
             const bool on = row < n;
-            const float inv = __frsqrt_rn(sum[u] / (float)D + P.eps);
-            if (on && P.hidden) x[u].store((T*)P.hidden + row * P.hidden_ld, t, width, D);
+            const El<VE> inv = v_all<VE>(__frsqrt_rn(fmaf(sum[u], P.inv_dim, P.eps)));
+            if (on && P.hidden) x[u].store((T*)P.hidden + row * P.hidden_ld, t, width, C.phase, D);
             float y[E];
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                float a[VE];
-                x[u].get(j, a);
+                El<VE> a[EL<VE>];
+                x[u].pairs(j, a);
 #pragma unroll
-                for (int i = 0; i < VE; ++i) y[j * VE + i] = a[i] * inv * w[j * VE + i];
-            }
-            if constexpr (CODED) {
-                store_codes<VE, NV, BLOCK>(P, row, on, t, width, y, tops);
-            } else if (on) {
+                for (int i = 0; i < EL<VE>; ++i) a[i] = v_mul(v_mul(a[i], inv), w[j][i]);
+                if constexpr (CODED) {
+                    float z[VE];
+                    v_unpack<VE>(a, z);
 #pragma unroll
-                for (int j = 0; j < NV; ++j) {
-                    float a[VE];
-#pragma unroll
-                    for (int i = 0; i < VE; ++i) a[i] = y[j * VE + i];
-                    r[u].set(j, a);
+                    for (int i = 0; i < VE; ++i) y[j * VE + i] = z[i];
+                } else {
+                    r[u].set_pairs(j, a);
                 }
-                r[u].store((T*)P.out + row * P.out_ld, t, width, D);
             }
+            if constexpr (CODED) store_codes<VE, NV, BLOCK>(P, row, on, t, width, y, tops);
+            else if (on) r[u].store((T*)P.out + row * P.out_ld, t, width, C.phase, D);
+        }
+        if constexpr (BLOCK) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                x[u] = xn[u];
+                r[u] = rn[u];
+            }
+        } else {
+            load(base + step, x, r);
         }
     }
 }
 
 // dw_part: [blocks][dim] sums of the rows a block took.
-template <typename T, int VE, int NV, int U, bool BLOCK>
-__global__ void __launch_bounds__(BLOCK ? 512 : NM_THREADS) k_norm_backward(const __grid_constant__ RmsNorm P, float* dw_part) {
+template <typename T, int VE, int NV, int U, bool BLOCK, bool EDGE>
+__global__ void __launch_bounds__(BLOCK ? 512 : NM_THREADS, BLOCK ? 1 : (VE * NV <= 8 ? 3 : 2)) k_norm_backward(const __grid_constant__ RmsNorm P, float* dw_part) {
     constexpr int E = VE * NV;
     extern __shared__ float norm_dw[];                       // groups: [warps][dim]
     chain_wait();
     const int n = norm_rows(P.n), D = P.dim;
     const int width = BLOCK ? (int)blockDim.x : P.tl, t = BLOCK ? (int)threadIdx.x : (int)threadIdx.x & (P.tl - 1), own = BLOCK ? 0 : threadIdx.x / width;
     const int per_block = BLOCK ? 1 : NM_THREADS / width;
-    float w[E], dw[E];
-    load_weight<VE, NV>(P, t, width, w);
-#pragma unroll
-    for (int i = 0; i < E; ++i) dw[i] = 0.f;
-    for (int64_t base = (int64_t)blockIdx.x * per_block * U; base < n; base += (int64_t)gridDim.x * per_block * U) {
-        RowPart<T, VE, NV> h[U], dy[U], dh[U];
+    const RowClass C = row_class<VE, EDGE>(P, n);
+    El<VE> w[NV][EL<VE>], dw[NV][EL<VE>];
+    RowPart<T, VE, NV, EDGE> h[U], dy[U], dh[U];             // the rows that are worked on next
+    const int64_t step = C.blks * per_block * U;
+    auto row_at = [&](int64_t base, int u) { return EDGE ? (base + u * per_block + own) * P.period + C.cls : base + u * per_block + own; };
+    auto load = [&](int64_t base) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t row = base + u * per_block + own;
-            h[u].load((const T*)P.x + row * P.x_ld, t, width, D, row < n);
-            dy[u].load((const T*)P.dout + row * P.dout_ld, t, width, D, row < n);
-            if (P.residual) dh[u].load((const T*)P.residual + row * P.residual_ld, t, width, D, row < n);
+            const int64_t row = row_at(base, u);
+            const bool on = base < C.n && row < n;
+            h[u].load((const T*)P.x + row * P.x_ld, t, width, C.phase, D, on);
+            dy[u].load((const T*)P.dout + row * P.dout_ld, t, width, C.phase, D, on);
+            if (P.residual) dh[u].load((const T*)P.residual + row * P.residual_ld, t, width, C.phase, D, on);
         }
+    };
+    load(C.blk * per_block * U);
+    load_weight<VE, NV>(P, t, width, C.phase, w);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < EL<VE>; ++i) dw[j][i] = v_all<VE>(0.f);
+    for (int64_t base = C.blk * per_block * U; base < C.n; base += step) {
+        RowPart<T, VE, NV, EDGE> hc[U], dyc[U], dhc[U];
         float sum[2 * U];                                    // sum h^2, sum g h
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            sum[2 * u] = sum[2 * u + 1] = 0.f;
+            hc[u] = h[u];
+            dyc[u] = dy[u];
+            dhc[u] = dh[u];
+            El<VE> hh = v_all<VE>(0.f), gh = v_all<VE>(0.f);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                float a[VE], b[VE];
-                h[u].get(j, a);
-                dy[u].get(j, b);
+                El<VE> a[EL<VE>], b[EL<VE>];
+                hc[u].pairs(j, a);
+                dyc[u].pairs(j, b);
 #pragma unroll
-                for (int i = 0; i < VE; ++i) {
-                    sum[2 * u] = fmaf(a[i], a[i], sum[2 * u]);
-                    sum[2 * u + 1] = fmaf(b[i] * w[j * VE + i], a[i], sum[2 * u + 1]);
+                for (int i = 0; i < EL<VE>; ++i) {
+                    hh = v_fma(a[i], a[i], hh);
+                    gh = v_fma(v_mul(b[i], w[j][i]), a[i], gh);
                 }
             }
+            sum[2 * u] = v_sum(hh);
+            sum[2 * u + 1] = v_sum(gh);
         }
+        load(base + step);                                   // on their way while these are summed and written
         row_sum<BLOCK, 2 * U>(sum, width);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t row = base + u * per_block + own;
+            const int64_t row = row_at(base, u);
             if (row >= n) continue;
-            const float inv = __frsqrt_rn(sum[2 * u] / (float)D + P.eps), mean = sum[2 * u + 1] / (float)D * inv * inv * inv;
+            const float v = __frsqrt_rn(fmaf(sum[2 * u], P.inv_dim, P.eps));
+            const El<VE> inv = v_all<VE>(v), mean = v_all<VE>(-(sum[2 * u + 1] * P.inv_dim * v * v * v));
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                float a[VE], b[VE], x[VE];
-                h[u].get(j, a);
-                dy[u].get(j, b);
-#pragma unroll
-                for (int i = 0; i < VE; ++i) {
-                    dw[j * VE + i] = fmaf(b[i], a[i] * inv, dw[j * VE + i]);
-                    x[i] = fmaf(-a[i], mean, b[i] * w[j * VE + i] * inv);
-                }
+                El<VE> a[EL<VE>], b[EL<VE>], x[EL<VE>];
+                hc[u].pairs(j, a);
+                dyc[u].pairs(j, b);
                 if (P.residual) {
-                    dh[u].get(j, b);
+                    dhc[u].pairs(j, x);
+                } else {
 #pragma unroll
-                    for (int i = 0; i < VE; ++i) x[i] += b[i];
+                    for (int i = 0; i < EL<VE>; ++i) x[i] = v_all<VE>(0.f);
                 }
-                h[u].set(j, x);
+#pragma unroll
+                for (int i = 0; i < EL<VE>; ++i) {
+                    dw[j][i] = v_fma(b[i], v_mul(a[i], inv), dw[j][i]);
+                    // the two terms of the norm's own gradient, which may cancel, before what arrives beside it
+                    x[i] = v_add(v_fma(a[i], mean, v_mul(v_mul(b[i], w[j][i]), inv)), x[i]);
+                }
+                hc[u].set_pairs(j, x);
             }
-            h[u].store((T*)P.out + row * P.out_ld, t, width, D);
+            hc[u].store((T*)P.out + row * P.out_ld, t, width, C.phase, D);
         }
     }
     if (!P.dweight) return;
+    float sums[E];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        float x[VE];
+        v_unpack<VE>(dw[j], x);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) sums[j * VE + i] = x[i];
+    }
     float* part = dw_part + (int64_t)blockIdx.x * D;
     if constexpr (BLOCK) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
-                const int c = (t + j * width) * VE + i;
-                if (c < D) part[c] = dw[j * VE + i];
+                const int c = (t + j * width) * VE + i - C.phase;
+                if (c >= 0 && c < D) part[c] = sums[j * VE + i];
             }
     } else {
         for (int o = width; o < 32; o <<= 1) {               // the groups of a warp
 #pragma unroll
-            for (int i = 0; i < E; ++i) dw[i] += __shfl_xor_sync(FULL, dw[i], o);
+            for (int i = 0; i < E; ++i) sums[i] += __shfl_xor_sync(FULL, sums[i], o);
         }
         if ((threadIdx.x & 31) < width) {
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int i = 0; i < VE; ++i) {
-                    const int c = (t + j * width) * VE + i;
-                    if (c < D) norm_dw[(threadIdx.x >> 5) * D + c] = dw[j * VE + i];
+                    const int c = (t + j * width) * VE + i - C.phase;
+                    if (c >= 0 && c < D) norm_dw[(threadIdx.x >> 5) * D + c] = sums[j * VE + i];
                 }
         }
         __syncthreads();
@@ -353,79 +480,140 @@ static int64_t norm_parts(int64_t rows) {
 }
 size_t norm_workspace(int64_t rows, int32_t dim) { return align_up((size_t)norm_parts(rows) * dim * 4, 256); }
 
-// A row's elements per thread: one to four pieces by lanes of a warp, up to 16 elements by a block.
-template <typename F> static cudaError_t norm_shape(const RmsNorm& P, int ve, F run) {
-    const int pieces = (P.dim + ve - 1) / ve;
-    if (P.dtype == GS_BF16) {
-        if (ve == 8) {
-            if (pieces <= 32) return run(bf16(), std::integral_constant<int, 8>(), std::integral_constant<int, 1>(), std::false_type());
-            if (pieces <= 64) return run(bf16(), std::integral_constant<int, 8>(), std::integral_constant<int, 2>(), std::false_type());
-            return run(bf16(), std::integral_constant<int, 8>(), std::integral_constant<int, 2>(), std::true_type());
+// How the rows of several arrays lie in memory: the elements of an access (whole pieces, or one), and, for whole pieces, after how
+// many rows they begin at the same place of a piece again.
+struct RowLayout {
+    int ve, period, phase;
+    bool edge;
+    void add(const void* p, int64_t ld, int size, int64_t rows) {
+        if (!p || ve == 1) return;
+        const int at = (int)((uintptr_t)p / size % ve), step = rows > 1 ? (int)(ld % ve) : 0;
+        if (phase < 0) {
+            phase = at;
+            turn = step;
+        } else if (at != phase || step != turn) {
+            ve = 1;
         }
-        if (pieces <= 32) return run(bf16(), std::integral_constant<int, 1>(), std::integral_constant<int, 1>(), std::false_type());
-        if (pieces <= 128) return run(bf16(), std::integral_constant<int, 1>(), std::integral_constant<int, 4>(), std::false_type());
-        return run(bf16(), std::integral_constant<int, 1>(), std::integral_constant<int, 16>(), std::true_type());
     }
-    if (ve == 4) {
-        if (pieces <= 32) return run(float(), std::integral_constant<int, 4>(), std::integral_constant<int, 1>(), std::false_type());
-        if (pieces <= 64) return run(float(), std::integral_constant<int, 4>(), std::integral_constant<int, 2>(), std::false_type());
-        return run(float(), std::integral_constant<int, 4>(), std::integral_constant<int, 4>(), std::true_type());
+    int turn;
+    void finish(int dim) {
+        period = 1;
+        if (ve > 1)
+            while (period * turn % ve) period *= 2;
+        edge = ve > 1 && (phase || turn || dim % ve);
+        if (edge && (dim + 2 * ve - 2) / ve > NORM_MAX_DIM / ve) single();   // a piece more than a block holds
     }
-    if (pieces <= 32) return run(float(), std::integral_constant<int, 1>(), std::integral_constant<int, 1>(), std::false_type());
-    if (pieces <= 128) return run(float(), std::integral_constant<int, 1>(), std::integral_constant<int, 4>(), std::false_type());
-    return run(float(), std::integral_constant<int, 1>(), std::integral_constant<int, 16>(), std::true_type());
+    void single() {
+        ve = period = 1;
+        phase = turn = 0;
+        edge = false;
+    }
+};
+
+// A row's elements per thread: one or two pieces by lanes of a warp, 8 or 16 elements by a block.
+template <typename T, int V, bool EDGE, typename F> static cudaError_t norm_width(const RmsNorm& P, F run) {
+    constexpr int FEW = 1, MORE = V > 1 ? 2 : 4, HALF = 8 / V, MOST = 16 / V;
+    const int pieces = (P.dim + (EDGE ? V - 1 : 0) + V - 1) / V;
+    auto with = [&](auto num, auto block) {
+        const int threads = (pieces + (int)num - 1) / (int)num;
+        int tl = 1;
+        if (block) tl = (threads + 31) / 32 * 32;
+        else while (tl < threads) tl *= 2;
+        return run(T(), std::integral_constant<int, V>(), num, block, std::integral_constant<bool, EDGE>(), tl);
+    };
+    if (pieces <= 32 * FEW) return with(std::integral_constant<int, FEW>(), std::false_type());
+    if (pieces <= 32 * MORE) return with(std::integral_constant<int, MORE>(), std::false_type());
+    if (pieces <= 512 * HALF) return with(std::integral_constant<int, HALF>(), std::true_type());
+    return with(std::integral_constant<int, MOST>(), std::true_type());
+}
+template <typename F> static cudaError_t norm_shape(const RmsNorm& P, const RowLayout& l, F run) {
+    if (P.dtype == GS_BF16) {
+        if (l.ve == 1) return norm_width<bf16, 1, false>(P, run);
+        return l.edge ? norm_width<bf16, 8, true>(P, run) : norm_width<bf16, 8, false>(P, run);
+    }
+    if (l.ve == 1) return norm_width<float, 1, false>(P, run);
+    return l.edge ? norm_width<float, 4, true>(P, run) : norm_width<float, 4, false>(P, run);
 }
 
-static bool whole_pieces(const RmsNorm& P, const void* p, int64_t ld, int size) { return !p || ((uintptr_t)p % 16 == 0 && (ld * size) % 16 == 0); }
-
-static int norm_width(const RmsNorm& P, int ve, int nv, bool block) {
-    const int threads = (P.dim + ve * nv - 1) / (ve * nv);
-    if (block) return (threads + 31) / 32 * 32;
-    int tl = 1;
-    while (tl < threads) tl *= 2;
-    return tl;
+// Resident blocks of a kernel on one SM, looked up once per device.
+template <typename F> static int resident_blocks(F* kernel, int threads, size_t smem, std::atomic<uint64_t>& known) {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 1;
+    const uint64_t key = ((uint64_t)(dev + 1) << 48) | ((uint64_t)threads << 32) | (smem << 8), have = known.load(std::memory_order_relaxed);
+    if ((have & ~0xFFull) == key) return (int)(have & 0xFF);
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess || n < 1) n = 1;
+    known.store(key | (uint64_t)n, std::memory_order_relaxed);
+    return n;
 }
 
 cudaError_t launch_norm_forward(const RmsNorm& p, bool coded, cudaStream_t s) {
     const int size = p.dtype == GS_BF16 ? 2 : 4;
-    int ve = 16 / size;
-    if (p.dim % ve || !whole_pieces(p, p.x, p.x_ld, size) || !whole_pieces(p, p.residual, p.residual_ld, size) || !whole_pieces(p, p.hidden, p.hidden_ld, size) ||
-        !whole_pieces(p, p.out, p.out_ld, size) || (coded && p.coded.head_dim % ve))
-        ve = 1;
-    return norm_shape(p, ve, [&](auto type, auto vec, auto num, auto block) {
+    RowLayout l{16 / size, 1, -1, false, 0};
+    const int64_t rows = p.n.bound;
+    l.add(p.x, p.x_ld, size, rows);
+    l.add(p.residual, p.residual_ld, size, rows);
+    l.add(p.hidden, p.hidden_ld, size, rows);
+    if (!coded) l.add(p.out, p.out_ld, size, rows);
+    l.finish(p.dim);
+    // columns of a piece share a scale; fewer blocks than places where rows begin (a capped grid): one element at a time
+    if ((coded && (l.edge || p.coded.head_dim % l.ve)) || limit_grid(l.period) < l.period) l.single();
+    return norm_shape(p, l, [&](auto type, auto vec, auto num, auto block, auto edge, int tl) {
         using T = decltype(type);
-        constexpr int VE = vec, NV = num, U = 2;
-        constexpr bool B = block;
+        constexpr int VE = vec, NV = num;
+        constexpr bool B = block, EDGE = edge;
+        constexpr int U = B ? 1 : 2;
         RmsNorm P = p;
-        P.tl = norm_width(p, VE, NV, B);
-        const int threads = B ? P.tl : NM_THREADS, per = (B ? 1 : NM_THREADS / P.tl) * (coded || B ? 1 : U);
-        int64_t grid = ((int64_t)p.n.bound + per - 1) / per;
-        if (grid > sm_count() * 64) grid = sm_count() * 64;
-        const size_t smem = coded ? (size_t)(B ? 1 : NM_THREADS / P.tl) * p.coded.heads * 4 : 0;
-        if (coded) return launch_train(k_norm_forward<T, VE, NV, 1, B, true>, grid, threads, smem, s, P);
-        return launch_train(k_norm_forward<T, VE, NV, (B ? 1 : U), B, false>, grid, threads, smem, s, P);
+        P.tl = tl;
+        P.period = l.period;
+        P.inv_dim = 1.f / (float)p.dim;
+        P.phase = l.phase;
+        const int threads = B ? tl : NM_THREADS, held = B ? 1 : NM_THREADS / tl;
+        auto run = [&](auto kernel, size_t smem, std::atomic<uint64_t>& known) {
+            int64_t grid = (rows + held * U - 1) / (held * U);
+            const int64_t cap = B ? sm_count() * resident_blocks(kernel, threads, smem, known) : sm_count() * 64;
+            grid = (grid + l.period - 1) / l.period * l.period;
+            grid = limit_grid(grid > cap ? cap : grid) / l.period * l.period;
+            return launch_train(kernel, grid, threads, smem, s, P);
+        };
+        static std::atomic<uint64_t> known{0}, known_coded{0};
+        if constexpr (!EDGE) {
+            if (coded) return run(k_norm_forward<T, VE, NV, U, B, false, true>, (size_t)held * p.coded.heads * 4, known_coded);
+        }
+        return run(k_norm_forward<T, VE, NV, U, B, EDGE, false>, 0, known);
     });
 }
 
 cudaError_t launch_norm_backward(const RmsNorm& p, void* workspace, cudaStream_t s) {
     const int size = p.dtype == GS_BF16 ? 2 : 4;
-    int ve = 16 / size;
-    if (p.dim % ve || !whole_pieces(p, p.x, p.x_ld, size) || !whole_pieces(p, p.residual, p.residual_ld, size) || !whole_pieces(p, p.dout, p.dout_ld, size) ||
-        !whole_pieces(p, p.out, p.out_ld, size))
-        ve = 1;
-    return norm_shape(p, ve, [&](auto type, auto vec, auto num, auto block) {
+    RowLayout l{16 / size, 1, -1, false, 0};
+    const int64_t rows = p.n.bound, most = norm_parts(rows);
+    l.add(p.x, p.x_ld, size, rows);
+    l.add(p.residual, p.residual_ld, size, rows);
+    l.add(p.dout, p.dout_ld, size, rows);
+    l.add(p.out, p.out_ld, size, rows);
+    l.finish(p.dim);
+    if (limit_grid(l.period) < l.period || most < l.period) l.single();
+    return norm_shape(p, l, [&](auto type, auto vec, auto num, auto block, auto edge, int tl) {
         using T = decltype(type);
         constexpr int VE = vec, NV = num;
-        constexpr bool B = block;
-        constexpr int U = B ? 1 : 2;
+        constexpr bool B = block, EDGE = edge;
+        constexpr int U = B || VE * NV > 4 ? 1 : 2;
         RmsNorm P = p;
-        P.tl = norm_width(p, VE, NV, B);
-        const int threads = B ? P.tl : NM_THREADS, per = (B ? 1 : NM_THREADS / P.tl) * U;
-        int64_t grid = ((int64_t)p.n.bound + per - 1) / per;
-        const int64_t most = norm_parts(p.n.bound);
-        grid = limit_grid(grid > most ? most : grid);
+        P.tl = tl;
+        P.period = l.period;
+        P.inv_dim = 1.f / (float)p.dim;
+        P.phase = l.phase;
+        const int threads = B ? tl : NM_THREADS, held = (B ? 1 : NM_THREADS / tl) * U;
+        const size_t smem = B ? 0 : (size_t)(NM_THREADS / 32) * p.dim * 4;
+        // as many blocks as are resident: each leaves its columns' sums once
+        static std::atomic<uint64_t> known{0};
+        auto kernel = k_norm_backward<T, VE, NV, U, B, EDGE>;
+        int64_t grid = (rows + held - 1) / held, cap = sm_count() * resident_blocks(kernel, threads, smem, known);
+        cap = cap < most ? cap : most;
+        grid = (grid + l.period - 1) / l.period * l.period;
+        grid = limit_grid(grid > cap ? cap : grid) / l.period * l.period;
         float* part = (float*)workspace;
-        cudaError_t e = launch_train(k_norm_backward<T, VE, NV, U, B>, grid, threads, B ? 0 : (size_t)(NM_THREADS / 32) * p.dim * 4, s, P, part);
+        cudaError_t e = launch_train(kernel, grid, threads, smem, s, P, part);
         if (e == cudaSuccess && p.dweight) e = launch_train(k_norm_dweight, (p.dim + 31) / 32, 1024, 0, s, (const float*)part, (int)grid, (int)p.dim, p.dweight, p.weight_dtype);
         return e;
     });

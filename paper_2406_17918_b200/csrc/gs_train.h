@@ -166,7 +166,7 @@ struct CodedWrite {
     int64_t first;
     Count n;
     int32_t* claims;
-    int tl, head_tiles, take;
+    int tl, head_tiles;
 };
 cudaError_t launch_coded_write(const CodedWrite& p, cudaStream_t s);
 struct CodedRead {
@@ -212,7 +212,8 @@ struct RmsNorm {
     int32_t dim;
     float eps;
     CodedView coded;        // output in 8 bits
-    int tl;
+    int tl, period, phase;
+    float inv_dim;
 };
 constexpr int NORM_MAX_DIM = 8192;      // 512 threads of 16 elements
 size_t norm_workspace(int64_t rows, int32_t dim);
