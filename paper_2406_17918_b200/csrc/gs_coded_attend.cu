@@ -377,9 +377,9 @@ template <typename T, int VE, int G, int U> __global__ void __launch_bounds__(CA
 
 // One block per (long row, query head): the chunks' sums rescaled to the common maximum; each warp adds a contiguous share of the
 // chunks, the shares are added in order.
-template <typename T> __global__ void __launch_bounds__(1024) k_coded_attend_join(const __grid_constant__ CodedAttend P) {
+template <typename T, int NK> __global__ void __launch_bounds__(1024) k_coded_attend_join(const __grid_constant__ CodedAttend P) {
     constexpr int W = 32;
-    __shared__ float s_m[W], s_l[W], s_acc[W][256];
+    __shared__ float s_m[W], s_l[W], s_acc[W][32 * NK];
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = P.a.head_dim;
     const int64_t units = (int64_t)__ldcg(P.words + 1) * P.a.q_heads, stride = (int64_t)P.a.q_heads * (D + 2);
@@ -389,7 +389,7 @@ template <typename T> __global__ void __launch_bounds__(1024) k_coded_attend_joi
         const float* part = P.partial + (int64_t)row.y * stride + (int64_t)h * (D + 2);
         const int per = (row.z + W - 1) / W, c0 = warp * per, c1 = c0 + per < row.z ? c0 + per : row.z;
         // relative to this warp's own maximum first: nobody waits for the others' chunks
-        float m = -INFINITY, l = 0.f, acc[8] = {};
+        float m = -INFINITY, l = 0.f, acc[NK] = {};
         for (int c = c0 + lane; c < c1; c += 32) m = fmaxf(m, part[c * stride + D]);
         for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, o));
         const float ref = m == -INFINITY ? 0.f : m;
@@ -399,7 +399,7 @@ template <typename T> __global__ void __launch_bounds__(1024) k_coded_attend_joi
             const float scale = exp2_fast(x[D] - ref);
             l = fmaf(x[D + 1], scale, l);
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
+            for (int k = 0; k < NK; ++k)
                 if (k * 32 + lane < D) acc[k] = fmaf(x[k * 32 + lane], scale, acc[k]);
         }
         __syncthreads();                                       // the previous unit's sums are read
@@ -408,7 +408,7 @@ template <typename T> __global__ void __launch_bounds__(1024) k_coded_attend_joi
             s_l[warp] = l;
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < NK; ++k)
             if (k * 32 + lane < D) s_acc[warp][k * 32 + lane] = acc[k];
         __syncthreads();
         float top = -INFINITY;
@@ -428,6 +428,12 @@ template <typename T> __global__ void __launch_bounds__(1024) k_coded_attend_joi
     }
 }
 
+}  // namespace gs
+
+#include "gs_coded_attend_tc.cuh"
+
+namespace gs {
+
 // ---------------------------------------------------------------- launches
 struct CodedAttendLayout {
     size_t words, items, longs, partial, total;
@@ -446,39 +452,82 @@ static CodedAttendLayout coded_attend_layout(int64_t edges, int32_t q_heads, int
 }
 size_t coded_attention_workspace(int64_t edges, int32_t q_heads, int32_t head_dim) { return coded_attend_layout(edges, q_heads, head_dim).total; }
 
-template <typename T, int VE, int G, int U> static cudaError_t run_coded(CodedAttend P, cudaStream_t s) {
-    const int pieces = P.a.k.pitch / VE;
-    P.tl = 1;
-    while (P.tl < pieces) P.tl *= 2;
-    P.units_per_row = P.a.q_heads / G;
+template <typename T> static cudaError_t launch_join(const CodedAttend& P, cudaStream_t s) {
+    const int D = P.a.head_dim;
+    if (D <= 32) return launch_train(k_coded_attend_join<T, 1>, sm_count() * 2, 1024, 0, s, P);
+    if (D <= 64) return launch_train(k_coded_attend_join<T, 2>, sm_count() * 2, 1024, 0, s, P);
+    if (D <= 128) return launch_train(k_coded_attend_join<T, 4>, sm_count() * 2, 1024, 0, s, P);
+    return launch_train(k_coded_attend_join<T, 8>, sm_count() * 2, 1024, 0, s, P);
+}
+static void set_units(CodedAttend& P, int heads) {
+    P.units_per_row = P.a.q_heads / heads;
     P.unit_shift = -1;
     for (int i = 0; i < 8; ++i)
         if (P.units_per_row == 1 << i) P.unit_shift = i;
-    constexpr int smem = CA_THREADS / 32 * 2 * U * 2 * VE * 32;
-    cudaError_t e = cudaSuccess;
-    for (int pass = 0; pass < (P.split ? 2 : 1) && e == cudaSuccess; ++pass) {
-        P.chunk_mode = pass;
-        const int64_t n = pass ? (int64_t)P.a.edge_bound / CA_LONG + 1 : P.a.dst.bound;
-        P.slots = pass ? 32 / P.tl : 1;
-        // groups share a row while the rows alone do not give every SM sixteen warps and each keeps U edges
-        const int longest = P.a.max_row == 0 || P.a.max_row > CA_LONG ? CA_LONG : P.a.max_row;
-        while (!pass && P.tl * P.slots * 2 <= 32 && n * P.units_per_row * P.tl * P.slots * 2 <= sm_count() * 16 * 32 && P.slots * U < longest) P.slots *= 2;
-        const int per_block = CA_THREADS / (P.tl * P.slots);
-        int64_t grid = (n * P.units_per_row + per_block - 1) / per_block;
-        const int64_t cap = sm_count() * 16;
-        if (grid > cap) grid = cap;
-        e = launch_train(k_coded_attend<T, VE, G, U>, grid, CA_THREADS, smem, s, P);
-    }
-    if (P.split && e == cudaSuccess) e = launch_train(k_coded_attend_join<T>, sm_count() * 2, 1024, 0, s, P);
-    return e;
 }
+static int64_t chunk_bound(const CodedAttend& P) { return (int64_t)P.a.edge_bound / CA_LONG + 1; }
 
-template <typename T> static cudaError_t coded_group(const CodedAttend& P, cudaStream_t s) {
+// One element at a time per lane: rows of up to CA_LONG edges, or chunks.
+template <typename T, int VE, int G> static cudaError_t run_coded(CodedAttend P, int chunk_mode, cudaStream_t s) {
+    constexpr int U = 4;
+    const int pieces = P.a.k.pitch / VE;
+    P.tl = 1;
+    while (P.tl < pieces) P.tl *= 2;
+    set_units(P, G);
+    constexpr int smem = CA_THREADS / 32 * 2 * U * 2 * VE * 32;
+    P.chunk_mode = chunk_mode;
+    const int64_t n = chunk_mode ? chunk_bound(P) : P.a.dst.bound;
+    P.slots = chunk_mode ? 32 / P.tl : 1;
+    // groups share a row while the rows alone do not give every SM sixteen warps and each keeps U edges
+    const int longest = P.a.max_row == 0 || P.a.max_row > CA_LONG ? CA_LONG : P.a.max_row;
+    while (!chunk_mode && P.tl * P.slots * 2 <= 32 && n * P.units_per_row * P.tl * P.slots * 2 <= sm_count() * 16 * 32 && P.slots * U < longest) P.slots *= 2;
+    const int per_block = CA_THREADS / (P.tl * P.slots);
+    int64_t grid = (n * P.units_per_row + per_block - 1) / per_block;
+    const int64_t cap = sm_count() * 16;
+    if (grid > cap) grid = cap;
+    return launch_train(k_coded_attend<T, VE, G, U>, grid, CA_THREADS, smem, s, P);
+}
+template <typename T> static cudaError_t coded_lanes(const CodedAttend& P, int chunk_mode, cudaStream_t s) {
     const int group = P.a.q_heads / P.a.kv_heads;
     // query heads that share a key/value head are taken together; what a lane holds of them stays within its registers
-    if (group % 4 == 0) return run_coded<T, 8, 4, 4>(P, s);
-    if (group % 2 == 0) return run_coded<T, 8, 2, 4>(P, s);
-    return run_coded<T, 16, 1, 4>(P, s);
+    if (group % 4 == 0) return run_coded<T, 8, 4>(P, chunk_mode, s);
+    if (group % 2 == 0) return run_coded<T, 8, 2>(P, chunk_mode, s);
+    return run_coded<T, 16, 1>(P, chunk_mode, s);
+}
+
+// On the tensor cores.
+template <int SP> static cudaError_t run_tc(CodedAttend P, int chunk_mode, cudaStream_t s) {
+    using S = TcShape<SP>;
+    auto kernel = k_coded_attend_tc<SP>;
+    static std::atomic<uint64_t> allowed{0};
+    const cudaError_t e = allow_smem(kernel, S::SMEM, allowed);
+    if (e != cudaSuccess) return e;
+    set_units(P, S::SLOTS);
+    P.chunk_mode = chunk_mode;
+    const int64_t n = chunk_mode ? chunk_bound(P) : P.a.dst.bound;
+    int64_t grid = (n * P.units_per_row + TC_WARPS - 1) / TC_WARPS;
+    const int64_t cap = sm_count() * 4;                      // what is resident
+    if (grid > cap) grid = cap;
+    return launch_train(kernel, grid, TC_WARPS * 32, S::SMEM, s, P);
+}
+static cudaError_t coded_tensor(const CodedAttend& P, int chunk_mode, cudaStream_t s) {
+    const int pieces = P.a.k.pitch / 16;
+    if (pieces <= 1) return run_tc<1>(P, chunk_mode, s);
+    if (pieces <= 2) return run_tc<2>(P, chunk_mode, s);
+    if (pieces <= 4) return run_tc<4>(P, chunk_mode, s);
+    if (pieces <= 8) return run_tc<8>(P, chunk_mode, s);
+    return run_tc<16>(P, chunk_mode, s);
+}
+template <typename T> static cudaError_t run_attention(const CodedAttend& P, cudaStream_t s) {
+    auto part = [&](int chunk_mode) {
+        if constexpr (std::is_same<T, bf16>::value)
+            if (P.a.q_heads / P.a.kv_heads % 4 == 0) return coded_tensor(P, chunk_mode, s);   // figures of both: at that kernel
+        return coded_lanes<T>(P, chunk_mode, s);
+    };
+    cudaError_t e = part(0);
+    if (P.split && e == cudaSuccess) e = part(1);
+    if (P.split && e == cudaSuccess) e = launch_join<T>(P, s);
+    return e;
 }
 
 cudaError_t launch_coded_attention(const CodedAttention& a, void* workspace, cudaStream_t s) {
@@ -499,7 +548,7 @@ cudaError_t launch_coded_attention(const CodedAttention& a, void* workspace, cud
         const cudaError_t e = cudaMemsetAsync(P.words, 0, 8, s);
         if (e != cudaSuccess) return e;
     }
-    return a.dtype == GS_BF16 ? coded_group<bf16>(P, s) : coded_group<float>(P, s);
+    return a.dtype == GS_BF16 ? run_attention<bf16>(P, s) : run_attention<float>(P, s);
 }
 
 }  // namespace gs

@@ -1,0 +1,399 @@
+// Attention over rows in 8 bits for bf16 queries, four or more of whose heads share a key head: the products on the tensor cores.
+//
+// A warp owns one (row, four query heads of one key head: the "slots") at a time and takes its edges 16 at a time.  The codes are
+// e4m3 numbers, exact as f16, and so is a bf16 query once it is scaled by a power of two (what is 2^30 below its row's largest
+// element is rounded):
+//   scores:  C[16 edges][slots] += K[16 edges][16 columns] q^T   (m16n8k16, sums in 32 bits; slot t is column 2 t, in lane t of a quad)
+//   values:  acc[slots][columns] += P[slots][16 edges] V[16 edges][8 columns]
+// P is not rounded to f16: a weight is hi + 2^-11 lo, two rows of the matrix, 22 bits of it.  The weights carry their value block's
+// scale; they are held relative to the largest weight times scale so far, as 2^14 (f16 keeps 2^-38 of that), with a maximum of its
+// own for lse.
+// What bounds it is instructions around the products (ALU 57%, issue slots 64%), not their rate, so the legacy matrix instruction
+// serves.  With fewer shared heads the other kernel needs fewer instructions.  Both measured, this : that (head groups, columns,
+// longest row): 4 x 64, 20 edges 326 : 617 us; 4 x 128, 30 edges 404 : 914; 4 x 64, 64 edges 600 : 1,674; one row of 200,011 edges 47 : 79;
+// but 2 x 32, 20 edges 314 : 258; 1 x 32, 20 edges 527 : 284; 1 x 32, one row of 200,011 edges 44 : 43.
+//
+// Rows are gathered by cp.async into TC_STAGES buffers of 16 edges a warp, TC_STAGES - 1 tiles ahead; the columns of 32 edges are read
+// one unit (a row's first) and the offsets two units ahead of the gathers.  No block barriers.  16-byte pieces are permuted within
+// 128 bytes by the edge so that every fragment is read without bank conflicts (up to 128 columns).
+#pragma once
+
+namespace gs {
+
+constexpr int TC_STAGES = 3;
+constexpr int TC_WARPS = 4;
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Rows 0 to 7 of the product are added to c; a has no others.
+__device__ __forceinline__ void mma_f16_half(float (&c)[2], uint32_t a0, uint32_t a2, uint32_t b0, uint32_t b1) {
+    float d[4];
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %5}, {%7, %8}, {%9, %10, %11, %11};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(0), "r"(a2), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(0.f));
+    c[0] = d[0];
+    c[1] = d[1];
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t codes_to_f16(uint32_t two) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
+    return h;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float f16_lo(uint32_t x) {
+    float y;
+    asm("{.reg .f16 a, b;\n\tmov.b32 {a, b}, %1;\n\tcvt.f32.f16 %0, a;}" : "=f"(y) : "r"(x));
+    return y;
+}
+// Place of byte `at` of an edge's row in a buffer of 16 edges.
+__device__ __forceinline__ int tile_byte(int edge, int at) {
+    const int c = (((edge & 1) << 1) | ((edge >> 1) & 1)) ^ ((edge >> 2 & 1) << 1), key = c << 1 | (edge & 1);
+    return (at >> 7) * 2048 + edge * 128 + ((((at >> 4) & 7) ^ key) << 4) + (at & 15);
+}
+template <int WORDS> __device__ __forceinline__ void read_words(const unsigned char* tile, int edge, int at, uint32_t (&w)[WORDS]) {
+    if constexpr (WORDS == 1) {
+        w[0] = *reinterpret_cast<const uint32_t*>(tile + tile_byte(edge, at));
+    } else if constexpr (WORDS == 2) {
+        const uint2 x = *reinterpret_cast<const uint2*>(tile + tile_byte(edge, at));
+        w[0] = x.x; w[1] = x.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < WORDS / 4; ++i) {
+            const uint4 x = *reinterpret_cast<const uint4*>(tile + tile_byte(edge, at + i * 16));
+            w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+        }
+    }
+}
+
+// SP: 16 columns each (a power of two).
+template <int SP> struct TcShape {
+    static constexpr int SLOTS = 4, ROWB = SP > 8 ? 256 : 128, TILE = 16 * ROWB, Q = SLOTS * SP * 32;
+    static constexpr int STAGE = 2 * TILE + Q, WARP = TC_STAGES * STAGE, SMEM = TC_WARPS * WARP;
+};
+
+struct TcUnit {
+    int r, row, unit, begin, end;    // r: the row, or the chunk
+    bool live;
+};
+
+template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 : (SP >= 8 ? 3 : 4)) k_coded_attend_tc(const __grid_constant__ CodedAttend P) {
+    using S = TcShape<SP>;
+    constexpr int SLOTS = S::SLOTS, L = 4 * SP, TILES = 2 * SP, PIECES = SP;
+    extern __shared__ __align__(16) unsigned char tc_smem[];
+    chain_wait();
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int rows = P.chunk_mode ? __ldcg(P.words) : list_length(P.a.dst), cols = list_length(P.a.src);
+    const int64_t units = (int64_t)rows * P.units_per_row, step = (int64_t)gridDim.x * TC_WARPS;
+    const int D = P.a.head_dim, group = P.a.q_heads / P.a.kv_heads, pitch = P.a.k.pitch;
+    const uint32_t kstep = (uint32_t)P.a.k.row_stride, vstep = (uint32_t)P.a.v.row_stride;
+    const CodedView& SV = lane < 16 ? P.a.k : P.a.v;         // whose scales this lane fetches
+    const uint32_t sstep = (uint32_t)SV.scale_stride;
+    unsigned char* mine = tc_smem + (threadIdx.x >> 5) * S::WARP;
+    const uint32_t mine_a = (uint32_t)__cvta_generic_to_shared(mine);
+
+    // ---- units: offsets two units ahead, columns one
+    int64_t u = (int64_t)blockIdx.x * TC_WARPS + (threadIdx.x >> 5);
+    if (u >= units) return;
+    auto raw_unit = [&](int64_t u) {
+        TcUnit w{0, 0, 0, 0, 0, u < units};
+        if (!w.live) return w;
+        if (P.unit_shift >= 0) w.r = (int)(u >> P.unit_shift);
+        else w.r = units >> 31 ? (int)(u / P.units_per_row) : (int)((uint32_t)u / (uint32_t)P.units_per_row);
+        w.unit = (int)(u - (int64_t)w.r * P.units_per_row);
+        w.row = w.r;
+        if (P.chunk_mode) w.row = P.items[w.r].x;
+        w.begin = __ldg(P.a.indptr + w.row);
+        w.end = __ldg(P.a.indptr + w.row + 1);
+        return w;
+    };
+    auto finish_unit = [&](TcUnit w) {
+        if (!w.live) return w;
+        w.begin = w.begin < 0 ? 0 : w.begin;
+        w.end = w.end > P.a.edge_bound ? P.a.edge_bound : w.end;
+        if (w.end < w.begin) w.end = w.begin;
+        if (P.chunk_mode) {
+            w.begin += P.items[w.r].y * CA_CHUNK;
+            w.end = w.begin + CA_CHUNK < w.end ? w.begin + CA_CHUNK : w.end;
+        } else if (P.split && w.end - w.begin > CA_LONG) {
+            if (w.unit == 0) {                               // listed once, by the warp of the row's first unit
+                const int nc = (w.end - w.begin + CA_CHUNK - 1) / CA_CHUNK;
+                int first = 0;
+                if (lane == 0) {
+                    first = atomicAdd(P.words, nc);
+                    P.longs[atomicAdd(P.words + 1, 1)] = make_int4(w.row, first, nc, 0);
+                }
+                first = __shfl_sync(FULL, first, 0);
+                for (int c = lane; c < nc; c += 32) P.items[first + c] = make_int2(w.row, c);
+            }
+            w.live = false;
+            w.end = w.begin;
+        }
+        return w;
+    };
+    auto window = [&](const TcUnit& w, int pos) { return pos + lane < w.end ? __ldg(P.a.indices + pos + lane) : -1; };
+    auto to_row = [&](int col) {
+        if ((uint32_t)col >= (uint32_t)cols) col = -1;
+        if (P.a.row_of && col >= 0) col = __ldg(P.a.row_of + col);
+        return (uint32_t)col < (uint32_t)P.a.k.rows ? col : -1;
+    };
+    TcUnit W0 = finish_unit(raw_unit(u)), W1 = finish_unit(raw_unit(u + step)), W2 = raw_unit(u + 2 * step);
+    int64_t u0 = u;                                          // the unit that is gathered
+    int pos = W0.begin, at = to_row(window(W0, pos));        // rows of 32 edges from pos & ~16 (of the unit) on
+    int next = window(W0, pos + 32), later = window(W1, W1.begin);
+    bool second = false;                                     // the tile is the later half of the window
+    bool more = true;
+
+    // ---- a tile on its way
+    struct Tile {
+        TcUnit w;
+        uint32_t on, scales;
+        bool first, last;
+    };
+    const int edges_per = 32 / (PIECES > 8 ? 8 : PIECES), piece0 = lane & (PIECES > 8 ? 7 : PIECES - 1), edge0 = lane / (PIECES > 8 ? 8 : PIECES);
+    auto issue = [&](int stage) {
+        Tile x;
+        x.w = W0;
+        x.first = pos == W0.begin;
+        const int mine_at = __shfl_sync(FULL, at, (second ? 16 : 0) + (lane & 15));
+        const bool is = pos + (lane & 15) < W0.end && mine_at >= 0;
+        const int h0 = W0.unit * SLOTS, kv0 = h0 / group;
+        x.on = __ballot_sync(FULL, is) & 0xFFFFu;
+        x.scales = 0;
+        if (is) {
+            const uint8_t* p = SV.scales + (uint64_t)((uint32_t)mine_at >> SV.shift) * sstep + kv0;
+            x.scales = __ldg(p);
+        }
+        const uint32_t base = mine_a + stage * S::STAGE;
+#pragma unroll
+        for (int i = 0; i < (16 * PIECES + 31) / 32; ++i) {
+            const int edge = PIECES > 8 ? (i >> 1) * edges_per + edge0 : i * edges_per + edge0, piece = PIECES > 8 ? piece0 + (i & 1) * 8 : piece0;
+            const int from = __shfl_sync(FULL, mine_at, edge & 15), sub = piece * 16;
+            if (edge >= 16) continue;                        // fewer pieces than lanes
+            const bool has = (x.on >> edge & 1) && sub < pitch;
+            const uint64_t row = has ? (uint32_t)from : 0u;
+            const uint32_t to = base + tile_byte(edge, piece * 16), in = has ? kv0 * pitch + sub : 0;
+            copy_async<16>(to, P.a.k.codes + row * kstep + in, has ? 16 : 0);
+            copy_async<16>(to + S::TILE, P.a.v.codes + row * vstep + in, has ? 16 : 0);
+        }
+        if (x.first && P.wide) {
+            for (int i = lane; i < SLOTS * SP * 2; i += 32) {
+                const int slot = i / (SP * 2), c = (i - slot * SP * 2) * 8;
+                const bool has = W0.live && c < D;
+                const bf16* q = (const bf16*)P.a.q.data + (has ? (int64_t)W0.row * P.a.q.row_stride + (int64_t)(h0 + slot) * P.a.q.head_stride + c : 0);
+                copy_async<16>(base + 2 * S::TILE + i * 16, q, has ? 16 : 0);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        // the next tile: of this window, of the next one, or of the next unit
+        pos += 16;
+        x.last = pos >= W0.end;
+        if (x.last) {
+            u0 += step;
+            more = u0 < units;
+            W0 = W1;
+            pos = W0.begin;
+            at = to_row(later);
+            next = window(W0, pos + 32);
+            W1 = finish_unit(W2);
+            later = window(W1, W1.begin);
+            W2 = raw_unit(u0 + 2 * step);
+            second = false;
+        } else if (second) {
+            at = to_row(next);
+            next = window(W0, pos + 32);
+            second = false;
+        } else {
+            second = true;
+        }
+        return x;
+    };
+
+    Tile queue[TC_STAGES - 1];
+    int ahead = 0;                                           // tiles on their way
+#pragma unroll
+    for (int i = 0; i < TC_STAGES - 1; ++i)
+        if (more) {
+            queue[i] = issue(i);
+            ++ahead;
+        } else {
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    int stage = 0;
+
+    // what a unit keeps: the queries' fragments (lane g, t: slot g / 2, columns t L ...), sums, maxima (lane g, t: slot t)
+    uint32_t q[SP][2];
+    float acc[TILES][2], m = 0.f, mv = 0.f, l = 0.f, qscale = 0.f;
+    const float c2 = P.a.scale * CA_LOG2E;
+    const int my_slot = g >> 1;
+    while (ahead > 0) {
+        const Tile x = queue[0];
+#pragma unroll
+        for (int i = 0; i + 1 < TC_STAGES - 1; ++i) queue[i] = queue[i + 1];
+        --ahead;
+        if (more) {
+            queue[TC_STAGES - 2] = issue(stage == 0 ? TC_STAGES - 1 : stage - 1);
+            ++ahead;
+        } else {
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(TC_STAGES - 1) : "memory");
+        __syncwarp();
+        const unsigned char* tile = mine + stage * S::STAGE;
+        stage = stage + 1 == TC_STAGES ? 0 : stage + 1;
+        const int h0 = x.w.unit * SLOTS;
+        if (x.first) {
+            m = mv = -INFINITY;
+            l = 0.f;
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) acc[i][0] = acc[i][1] = 0.f;
+            float y[L];
+            const bool has = (g & 1) == 0 && x.w.live;
+            if (P.wide) {
+                const uint32_t* w = reinterpret_cast<const uint32_t*>(tile + 2 * S::TILE + my_slot * SP * 32 + t * L * 2);
+#pragma unroll
+                for (int i = 0; i < L / 2; ++i) {
+                    const uint32_t v = has ? w[i] : 0u;
+                    y[2 * i] = bf16_lo(v);
+                    y[2 * i + 1] = bf16_hi(v);
+                }
+            } else {
+                const bf16* w = (const bf16*)P.a.q.data + (has ? (int64_t)x.w.row * P.a.q.row_stride + (int64_t)(h0 + my_slot) * P.a.q.head_stride : 0);
+#pragma unroll
+                for (int i = 0; i < L; ++i) y[i] = has && t * L + i < D ? to_f32(w[t * L + i]) : 0.f;
+            }
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < L; ++i) top = fmaxf(top, fabsf(y[i]));
+            top = fmaxf(top, __shfl_xor_sync(FULL, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(FULL, top, 2));
+            // 2^(14 - e) for a largest element of 2^e, within the range of f32
+            const int e = (int)(__float_as_uint(top) >> 23), up = e < 15 ? 253 : (e > 253 ? 15 : 268 - e);
+            const float scale = __uint_as_float((uint32_t)up << 23);
+#pragma unroll
+            for (int i = 0; i < SP; ++i) {
+                q[i][0] = pack_f16(y[4 * i] * scale, y[4 * i + 1] * scale);
+                q[i][1] = pack_f16(y[4 * i + 2] * scale, y[4 * i + 3] * scale);
+            }
+            qscale = __uint_as_float((uint32_t)(254 - __shfl_sync(FULL, up, 8 * t)) << 23) * c2;
+        }
+        // ---- scores
+        uint32_t k0[SP], k1[SP];
+        float c[4] = {0.f, 0.f, 0.f, 0.f};
+        read_words<SP>(tile, g, t * L, k0);
+        read_words<SP>(tile, g + 8, t * L, k1);
+#pragma unroll
+        for (int i = 0; i < SP; ++i) mma_f16(c, codes_to_f16(k0[i]), codes_to_f16(k1[i]), codes_to_f16(k0[i] >> 16), codes_to_f16(k1[i] >> 16), q[i][0], q[i][1]);
+        // ---- weights of slot t and the edges g and g + 8
+        const uint32_t kb0 = __shfl_sync(FULL, x.scales, g), kb1 = __shfl_sync(FULL, x.scales, g + 8);
+        const uint32_t vb0 = __shfl_sync(FULL, x.scales, g + 16), vb1 = __shfl_sync(FULL, x.scales, g + 24);
+        const float s0 = x.on >> g & 1 ? c[0] * scale_of(kb0) * qscale : -INFINITY, s1 = x.on >> (g + 8) & 1 ? c[2] * scale_of(kb1) * qscale : -INFINITY;
+        const float y0 = s0 + (float)((int)vb0 - 127), y1 = s1 + (float)((int)vb1 - 127);
+        float top = fmaxf(s0, s1), topv = fmaxf(y0, y1);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+            top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+            topv = fmaxf(topv, __shfl_xor_sync(FULL, topv, o));
+        }
+        top = fmaxf(top, m);
+        topv = fmaxf(topv, mv);
+        const float ref = top == -INFINITY ? 0.f : top, refv = topv == -INFINITY ? 0.f : topv;   // nothing seen yet: all weights are zero
+        l = fmaf(l, exp2_fast(m - ref), exp2_fast(s0 - ref) + exp2_fast(s1 - ref));
+        const float corr = exp2_fast(mv - refv), x0 = exp2_fast(y0 - refv + 14.f), x1 = exp2_fast(y1 - refv + 14.f);
+        m = top;
+        mv = topv;
+        const float hi0 = f16_lo(pack_f16(x0, 0.f)), hi1 = f16_lo(pack_f16(x1, 0.f));
+        const uint32_t a0 = transpose8(pack_f16(x0, (x0 - hi0) * 2048.f)), a2 = transpose8(pack_f16(x1, (x1 - hi1) * 2048.f));
+        if (__any_sync(FULL, corr != 1.f)) {
+            const float mul = __shfl_sync(FULL, corr, my_slot);     // lane `slot` of the first quad
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) {
+                acc[i][0] *= mul;
+                acc[i][1] *= mul;
+            }
+        }
+        // ---- values: edges 2 t, 2 t + 1, 2 t + 8, 2 t + 9, columns 2 SP g ...
+        const unsigned char* vt = tile + S::TILE;
+        const int byte = g * 2 * SP;
+        if constexpr (SP == 1) {
+            auto two = [&](int edge) { return (uint32_t)*reinterpret_cast<const uint16_t*>(vt + tile_byte(edge, byte)); };
+            const uint32_t low = __byte_perm(two(2 * t), two(2 * t + 1), 0x5140), high = __byte_perm(two(2 * t + 8), two(2 * t + 9), 0x5140);
+            mma_f16_half(acc[0], a0, a2, codes_to_f16(low), codes_to_f16(high));
+            mma_f16_half(acc[1], a0, a2, codes_to_f16(low >> 16), codes_to_f16(high >> 16));
+        } else {
+            constexpr int VW = SP / 2;
+            uint32_t v0[VW], v1[VW], v2[VW], v3[VW];
+            read_words<VW>(vt, 2 * t, byte, v0);
+            read_words<VW>(vt, 2 * t + 1, byte, v1);
+            read_words<VW>(vt, 2 * t + 8, byte, v2);
+            read_words<VW>(vt, 2 * t + 9, byte, v3);
+#pragma unroll
+            for (int i = 0; i < VW; ++i) {
+                const uint32_t la = __byte_perm(v0[i], v1[i], 0x5140), lb = __byte_perm(v0[i], v1[i], 0x7362);
+                const uint32_t ha = __byte_perm(v2[i], v3[i], 0x5140), hb = __byte_perm(v2[i], v3[i], 0x7362);
+                mma_f16_half(acc[4 * i], a0, a2, codes_to_f16(la), codes_to_f16(ha));
+                mma_f16_half(acc[4 * i + 1], a0, a2, codes_to_f16(la >> 16), codes_to_f16(ha >> 16));
+                mma_f16_half(acc[4 * i + 2], a0, a2, codes_to_f16(lb), codes_to_f16(hb));
+                mma_f16_half(acc[4 * i + 3], a0, a2, codes_to_f16(lb >> 16), codes_to_f16(hb >> 16));
+            }
+        }
+        __syncwarp();                                        // the buffer is read before it is filled again
+        if (!x.last) continue;
+        // ---- the unit's end: rows 2 slot (hi) and 2 slot + 1 (lo) of acc; a lane has columns 4 SP t ...
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(FULL, l, o);
+        const float total = __shfl_sync(FULL, l, my_slot), at_m = __shfl_sync(FULL, m, my_slot), at_mv = __shfl_sync(FULL, mv, my_slot);
+        float out[L];
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            out[i] = fmaf(__shfl_xor_sync(FULL, acc[i][0], 4), 1.f / 2048.f, acc[i][0]);
+            out[TILES + i] = fmaf(__shfl_xor_sync(FULL, acc[i][1], 4), 1.f / 2048.f, acc[i][1]);
+        }
+        if (!x.w.live || (g & 1)) continue;
+        const int h = h0 + my_slot, col = t * L;
+        const bool none = total == 0.f;                      // no edge left by the mask: zero row, log of an empty sum
+        if (P.chunk_mode) {
+            const float unit = at_m == -INFINITY ? 0.f : exp2_fast(at_mv - 14.f - at_m);
+            float* part = P.partial + ((int64_t)x.w.r * P.a.q_heads + h) * (D + 2);
+#pragma unroll
+            for (int i = 0; i < L; ++i)
+                if (col + i < D) part[col + i] = none ? 0.f : out[i] * unit;
+            if (t == 0) {
+                part[D] = at_m;
+                part[D + 1] = total;
+            }
+        } else {
+            // 2^(mv - 14 - m) / l in one factor
+            const float unit = none ? 0.f : exp2_fast(at_mv - 14.f - at_m) / total;
+            bf16* to = (bf16*)P.a.out.data + (int64_t)x.w.row * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride;
+            if (P.wide && L >= 8) {
+#pragma unroll
+                for (int i = 0; i < L / 8; ++i) {
+                    float z[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) z[j] = none ? 0.f : out[8 * i + j] * unit;
+                    if (col + 8 * i < D) store_vec<bf16, 8>(to + col + 8 * i, z);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < L; ++i)
+                    if (col + i < D) to[col + i] = from_f32<bf16>(none ? 0.f : out[i] * unit);
+            }
+            if (t == 0) P.a.lse[(int64_t)x.w.row * P.a.q_heads + h] = none ? -INFINITY : at_m * CA_LN2 + logf(total);
+        }
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
+}  // namespace gs
