@@ -10,6 +10,7 @@ import ctypes
 import math
 import os
 import re
+from array import array
 
 import torch
 
@@ -804,9 +805,9 @@ def _heads(dtype, *operands):
                 (stride[2] != 1 and dim > 1):
             raise TypeError("%s must be a CUDA tensor [%d, %d, %d] of %s with a contiguous last dimension" % (what, rows, heads, dim, dtype))
         words += (t.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], dim), stride[1] if heads > 1 else dim)
-    array = (ctypes.c_int64 * len(words))(*words)
-    at = ctypes.addressof(array)
-    return array, [at + 24 * i for i in range(len(operands))]
+    words = array("q", words)
+    at = words.buffer_info()[0]
+    return words, [at + 24 * i for i in range(len(operands))]
 
 
 def gs_block_attention_workspace_bytes(num_dst: int, num_src: int, num_edges: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
@@ -959,18 +960,32 @@ def _one_device(*tensors):
     return device
 
 
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+
+
 def _run(device, fn, *args):
     """The call, on the operands' device."""
-    if device == torch.cuda.current_device():
-        _check(fn(*args))
-        return
-    with torch.cuda.device(device):
-        _check(fn(*args))
+    if device == _current_device():
+        status = fn(*args)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args)
+    if status != 0:
+        _check(status)
+
+
+def _new_like(t: torch.Tensor, stream, rest=None) -> torch.Tensor:
+    """An output of the shape and dtype of a contiguous tensor, or of a row-major one with a pitch (see _new); without its
+    arguments to parse an allocation takes half the time."""
+    if stream is None and rest is None:
+        return torch.empty_like(t)
+    return _new(tuple(t.shape), t.dtype, t, stream, rest)
 
 
 def _norm_rows(t, what, like):
-    _rows_2d(t, what)
-    if t.dtype is not like.dtype or t.shape != like.shape:
+    stride = t.stride()
+    if len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1) or not t.is_cuda or t.dtype is not like.dtype or t.shape != like.shape:
+        _rows_2d(t, what)
         raise TypeError("%s must have the dtype and shape of the normalised rows" % what)
     return t
 
@@ -978,7 +993,7 @@ def _norm_rows(t, what, like):
 def _norm_weight(weight, dim):
     if weight is None:
         return None, GS_F32
-    if weight.dim() != 1 or weight.shape[0] != dim or not weight.is_cuda or not weight.is_contiguous():
+    if weight.shape != (dim,) or not weight.is_cuda or not weight.is_contiguous():
         raise TypeError("weight must be a contiguous CUDA tensor [%d]" % dim)
     return weight.data_ptr(), _dtype(weight.dtype)
 
@@ -999,7 +1014,7 @@ def _norm_inputs(x, weight, residual, hidden, stream, count):
     _rows_2d(x, "x")
     if residual is not None:
         _norm_rows(residual, "residual", x)
-        hidden = _new(tuple(x.shape), x.dtype, x, stream, None if count is None else 0) if hidden is None else _norm_rows(hidden, "hidden", x)
+        hidden = _new_like(x, stream, None if count is None else 0) if hidden is None else _norm_rows(hidden, "hidden", x)
     elif hidden is not None:
         _norm_rows(hidden, "hidden", x)
     return hidden, _norm_weight(weight, x.shape[1])
@@ -1011,10 +1026,11 @@ def gs_rms_norm_forward(x: torch.Tensor, weight: torch.Tensor = None, residual: 
     `hidden` (h) may be x or residual, `out` may be x.  `count`: a 0-d int32 CUDA tensor with the number of rows (x is then the
     bound; rows behind it are zeros, or left as they are in given arrays)."""
     hidden, (w, wt) = _norm_inputs(x, weight, residual, hidden, stream, count)
-    out = _new(tuple(x.shape), x.dtype, x, stream, None if count is None else 0) if out is None else _norm_rows(out, "out", x)
+    out = _new_like(x, stream, None if count is None else 0) if out is None else _norm_rows(out, "out", x)
     device = _one_device(x, weight, residual, hidden, out, count)
-    _run(device, _L.gs_rms_norm_forward, _addr(x), _ld(x), *_opt(residual), _dtype(x.dtype), w, wt, _counter(count, "count"), x.shape[0], x.shape[1], float(eps),
-         *_opt(hidden), _addr(out), _ld(out), _on(stream, x))
+    rows, dim = x.shape
+    _run(device, _L.gs_rms_norm_forward, x.data_ptr(), _ld(x), *_opt(residual), _dtype(x.dtype), w, wt, _counter(count, "count"), rows, dim, float(eps),
+         *_opt(hidden), out.data_ptr(), _ld(out), _on(stream, x))
     return out, x if hidden is None else hidden
 
 
@@ -1023,7 +1039,8 @@ def gs_rms_norm_coded(x: torch.Tensor, out: "CodedRows", weight: torch.Tensor = 
     """gs_rms_norm_forward with the result in 8 bits: row p of `out` (a store with block 1 and heads * head_dim = dim).  Returns (out, h)."""
     hidden, (w, wt) = _norm_inputs(x, weight, residual, hidden, stream, count)
     device = _one_device(x, weight, residual, hidden, out.codes, count)
-    _run(device, _L.gs_rms_norm_coded, _addr(x), _ld(x), *_opt(residual), _dtype(x.dtype), w, wt, _counter(count, "count"), x.shape[0], x.shape[1], float(eps),
+    rows, dim = x.shape
+    _run(device, _L.gs_rms_norm_coded, x.data_ptr(), _ld(x), *_opt(residual), _dtype(x.dtype), w, wt, _counter(count, "count"), rows, dim, float(eps),
          *_opt(hidden), out.address, _on(stream, x))
     return out, x if hidden is None else hidden
 
@@ -1037,17 +1054,18 @@ def gs_rms_norm_backward(hidden: torch.Tensor, dout: torch.Tensor, workspace: to
     if dhidden is not None:
         _norm_rows(dhidden, "dhidden", hidden)
     w, wt = _norm_weight(weight, hidden.shape[1])
-    dx = _new(tuple(hidden.shape), hidden.dtype, hidden, stream, None if count is None else 0) if dx is None else _norm_rows(dx, "dx", hidden)
+    dx = _new_like(hidden, stream, None if count is None else 0) if dx is None else _norm_rows(dx, "dx", hidden)
     if weight is None:
         if dweight is not None:
             raise ValueError("there is no weight")
     elif dweight is None:
-        dweight = _new(hidden.shape[1], weight.dtype, hidden, stream)
+        dweight = _new_like(weight, stream)
     elif dweight.dtype is not weight.dtype or _norm_weight(dweight, hidden.shape[1])[0] is None:
         raise TypeError("dweight must have the dtype of weight")
     device = _one_device(hidden, dout, workspace, weight, dhidden, dx, dweight, count)
-    _run(device, _L.gs_rms_norm_backward, _addr(hidden), _ld(hidden), _addr(dout), _ld(dout), *_opt(dhidden), _dtype(hidden.dtype), w, wt, _counter(count, "count"),
-         hidden.shape[0], hidden.shape[1], float(eps), _addr(dx), _ld(dx), _addr(dweight), *_workspace(workspace), _on(stream, workspace))
+    rows, dim = hidden.shape
+    _run(device, _L.gs_rms_norm_backward, hidden.data_ptr(), _ld(hidden), dout.data_ptr(), _ld(dout), *_opt(dhidden), _dtype(hidden.dtype), w, wt, _counter(count, "count"),
+         rows, dim, float(eps), dx.data_ptr(), _ld(dx), _addr(dweight), *_workspace(workspace), _on(stream, workspace))
     return dx, dweight
 
 
@@ -1144,7 +1162,7 @@ def gs_coded_attention_forward(indptr: torch.Tensor, indices: torch.Tensor, q: t
     b = _csr_block(indptr, indices, k.rows if rows is None else _ids_1d(rows, "rows").numel(), counts)
     exact = counts is None and n == b.max_dst
     if out is None:
-        out = _new((n, hq, d), q.dtype, q, stream, None if exact else 0)
+        out = _new_like(q, stream) if exact and q.is_contiguous() else _new((n, hq, d), q.dtype, q, stream, None if exact else 0)
     if lse is None:
         lse = _new((n, hq), torch.float32, q, stream, None if exact else -math.inf)
     elif lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.dim() != 2 or lse.shape[0] < b.max_dst or lse.shape[1] != hq:
@@ -1181,16 +1199,21 @@ def _grad_list(grads, out, counts):
         raise ValueError("one result and one count per gradient expected")
     words = []
     for i, g in enumerate(grads):
-        o = g if out is None else out[i]
-        c = None if counts is None else counts[i]
-        _dense(g, "each gradient")
-        if o is not g and (o.dtype is not g.dtype or o.shape != g.shape or o.stride() != g.stride() or not o.is_cuda):
-            raise TypeError("a result must have the dtype, shape and strides of its gradient")
-        if c is not None and (g.dim() < 1 or not g.is_contiguous()):
-            raise TypeError("a gradient with a count must be a contiguous tensor of rows")
-        n = g.numel()
-        words += (g.data_ptr(), o.data_ptr(), n, _counter(c, "each of counts") or 0, 0 if c is None or not n else n // g.shape[0], _dtype(g.dtype))
-    return (ctypes.c_int64 * max(1, len(words)))(*words)
+        if not (g.is_cuda and g.is_contiguous()):
+            _dense(g, "each gradient")
+        n, p, rows, row_elems = g.numel(), g.data_ptr(), 0, 0
+        o = p
+        if out is not None and out[i] is not g:
+            x = out[i]
+            if x.dtype is not g.dtype or x.shape != g.shape or x.stride() != g.stride() or not x.is_cuda:
+                raise TypeError("a result must have the dtype, shape and strides of its gradient")
+            o = x.data_ptr()
+        if counts is not None and counts[i] is not None:
+            if g.dim() < 1 or not g.is_contiguous():
+                raise TypeError("a gradient with a count must be a contiguous tensor of rows")
+            rows, row_elems = _counter(counts[i], "each of counts"), n // g.shape[0] if n else 0
+        words += (p, o, n, rows, row_elems, _dtype(g.dtype))
+    return array("q", words or (0,))
 
 
 def gs_grad_norm(grads, workspace: torch.Tensor, norm: torch.Tensor = None, counts=None, stream=None) -> torch.Tensor:
@@ -1200,7 +1223,7 @@ def gs_grad_norm(grads, workspace: torch.Tensor, norm: torch.Tensor = None, coun
     norm = _new(1, torch.float32, workspace, stream) if norm is None else _f32_rows(norm, "norm", 1)
     device = _one_device(workspace, norm, *grads, *(counts or ()))
     words = _grad_list(grads, None, counts)
-    _run(device, _L.gs_grad_norm, ctypes.addressof(words), len(grads), _addr(norm), *_workspace(workspace), _on(stream, workspace))
+    _run(device, _L.gs_grad_norm, words.buffer_info()[0], len(grads), _addr(norm), *_workspace(workspace), _on(stream, workspace))
     return norm
 
 
@@ -1211,5 +1234,5 @@ def gs_grad_clip(grads, max_norm: float, workspace: torch.Tensor, out=None, norm
     norm = _new(1, torch.float32, workspace, stream) if norm is None else _f32_rows(norm, "norm", 1)
     device = _one_device(workspace, norm, *grads, *(out or ()), *(counts or ()))
     words = _grad_list(grads, out, counts)
-    _run(device, _L.gs_grad_clip, ctypes.addressof(words), len(grads), float(max_norm), _addr(norm), *_workspace(workspace), _on(stream, workspace))
+    _run(device, _L.gs_grad_clip, words.buffer_info()[0], len(grads), float(max_norm), _addr(norm), *_workspace(workspace), _on(stream, workspace))
     return norm

@@ -17,14 +17,14 @@ namespace gs {
 
 constexpr int CA_THREADS = 128;
 constexpr int CA_LONG = 64;          // rows of more edges go to the chunk list
-constexpr int CA_CHUNK = 128;        // edges of a chunk
+constexpr int CA_CHUNK = 128, CA_CHUNK_MOST = 512;   // edges of a chunk (at least 2 CA_LONG: the workspace's bound)
 constexpr float CA_LOG2E = 1.4426950408889634f, CA_LN2 = 0.6931471805599453f;
 
 struct CodedAttend {
     CodedAttention a;
     int tl, slots, units_per_row, unit_shift;
     int wide;                        // q and out in whole pieces
-    int split, chunk_mode;
+    int split, chunk_mode, chunk;    // chunk: edges of one
     int32_t* words;                  // [0] chunks, [1] long rows
     int2* items;                     // chunk -> (row, chunk of the row)
     int4* longs;                     // long row -> (row, first chunk, chunks, -)
@@ -127,7 +127,7 @@ __device__ __forceinline__ CodedUnits find_units(const CodedAttend& P, int64_t u
     if (P.chunk_mode) {
         const int2 it = P.items[w.r];
         w.row = it.x;
-        skip = it.y * CA_CHUNK;
+        skip = it.y * P.chunk;
     }
     int b = __ldg(P.a.indptr + w.row), e = __ldg(P.a.indptr + w.row + 1);
     b = b < 0 ? 0 : b;
@@ -135,10 +135,10 @@ __device__ __forceinline__ CodedUnits find_units(const CodedAttend& P, int64_t u
     if (e < b) e = b;
     if (P.chunk_mode) {
         w.begin = b + skip;
-        w.end = w.begin + CA_CHUNK < e ? w.begin + CA_CHUNK : e;
+        w.end = w.begin + P.chunk < e ? w.begin + P.chunk : e;
     } else if (P.split && e - b > CA_LONG) {
         if (w.unit == 0) {                                   // listed once, by the lanes of the row's first unit
-            const int nc = (e - b + CA_CHUNK - 1) / CA_CHUNK, lanes = parts - 1;
+            const int nc = (e - b + P.chunk - 1) / P.chunk, lanes = parts - 1;
             const uint32_t mask = parts == 32 ? FULL : ((1u << parts) - 1u) << (threadIdx.x & 31 & ~lanes);
             int first = 0;
             if (part == 0) {
@@ -375,56 +375,82 @@ template <typename T, int VE, int G, int U> __global__ void __launch_bounds__(CA
     }
 }
 
-// One block per (long row, query head): the chunks' sums rescaled to the common maximum; each warp adds a contiguous share of the
-// chunks, the shares are added in order.
-template <typename T, int NK> __global__ void __launch_bounds__(1024) k_coded_attend_join(const __grid_constant__ CodedAttend P) {
+// The sums of chunks [c0, c1) of one head and 32 columns (x: of this lane's column of the first), relative to their largest maximum m;
+// 32 chunks at a time, all on their way together.
+__device__ __forceinline__ void join_chunks(const float* part, int64_t stride, int D, int col, int c0, int c1, float& m, float& l, float& acc) {
+    const int lane = threadIdx.x & 31;
+    m = -INFINITY;
+    l = acc = 0.f;
+    for (int c = c0; c < c1; c += 32) {
+        const bool is = c + lane < c1;
+        const float* mine = part + (int64_t)(is ? c + lane : c) * stride + D;
+        const float mc = is ? mine[0] : -INFINITY, lc = is ? mine[1] : 0.f;
+        float x[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = c + i < c1 && col < D ? part[(int64_t)(c + i) * stride + col] : 0.f;
+        float top = fmaxf(m, mc);
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+        const float ref = top == -INFINITY ? 0.f : top, corr = exp2_fast(m - ref), scale = exp2_fast(mc - ref);
+        m = top;
+        l = fmaf(lc, scale, l * corr);                        // of this lane's chunks
+        acc *= corr;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) acc = fmaf(x[i], __shfl_sync(FULL, scale, i), acc);
+    }
+    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(FULL, l, o);
+}
+
+// Joins the chunks of a long row, for one query head and 32 columns: by a warp if there are at most 32 of them, else each of a
+// block's warps takes a contiguous share and the shares are joined in order.
+template <typename T> __global__ void __launch_bounds__(1024) k_coded_attend_join(const __grid_constant__ CodedAttend P) {
     constexpr int W = 32;
-    __shared__ float s_m[W], s_l[W], s_acc[W][32 * NK];
+    __shared__ float s_m[W], s_l[W], s_acc[W][32];
     chain_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = P.a.head_dim;
-    const int64_t units = (int64_t)__ldcg(P.words + 1) * P.a.q_heads, stride = (int64_t)P.a.q_heads * (D + 2);
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int4 row = P.longs[u / P.a.q_heads];
-        const int h = (int)(u % P.a.q_heads);
-        const float* part = P.partial + (int64_t)row.y * stride + (int64_t)h * (D + 2);
-        const int per = (row.z + W - 1) / W, c0 = warp * per, c1 = c0 + per < row.z ? c0 + per : row.z;
-        // relative to this warp's own maximum first: nobody waits for the others' chunks
-        float m = -INFINITY, l = 0.f, acc[NK] = {};
-        for (int c = c0 + lane; c < c1; c += 32) m = fmaxf(m, part[c * stride + D]);
-        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, o));
-        const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll 8
-        for (int c = c0; c < c1; ++c) {
-            const float* x = part + c * stride;
-            const float scale = exp2_fast(x[D] - ref);
-            l = fmaf(x[D + 1], scale, l);
-#pragma unroll
-            for (int k = 0; k < NK; ++k)
-                if (k * 32 + lane < D) acc[k] = fmaf(x[k * 32 + lane], scale, acc[k]);
-        }
-        __syncthreads();                                       // the previous unit's sums are read
-        if (lane == 0) {
-            s_m[warp] = m;
-            s_l[warp] = l;
-        }
-#pragma unroll
-        for (int k = 0; k < NK; ++k)
-            if (k * 32 + lane < D) s_acc[warp][k * 32 + lane] = acc[k];
-        __syncthreads();
-        float top = -INFINITY;
-        for (int w = 0; w < W; ++w) top = fmaxf(top, s_m[w]);
-        const float all = top == -INFINITY ? 0.f : top;
-        l = 0.f;
-        for (int w = 0; w < W; ++w) l = fmaf(s_l[w], exp2_fast(s_m[w] - all), l);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = P.a.head_dim, parts = (D + 31) / 32, per_row = P.a.q_heads * parts;
+    const int64_t units = (int64_t)__ldcg(P.words + 1) * per_row, stride = (int64_t)P.a.q_heads * (D + 2);
+    auto put = [&](const int4& row, int h, int col, float m, float l, float sum) {
         const bool none = l == 0.f;
-        const float inv = none ? 0.f : 1.f / l;
         T* out = (T*)P.a.out.data + (int64_t)row.x * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride;
-        for (int col = threadIdx.x; col < D; col += 1024) {
-            float sum = 0.f;
-            for (int w = 0; w < W; ++w) sum = fmaf(s_acc[w][col], exp2_fast(s_m[w] - all), sum);
-            out[col] = from_f32<T>(none ? 0.f : sum * inv);
+        if (col < D) out[col] = from_f32<T>(none ? 0.f : sum / l);
+        if (col == 0) P.a.lse[(int64_t)row.x * P.a.q_heads + h] = none ? -INFINITY : m * CA_LN2 + logf(l);
+    };
+    for (int64_t base = blockIdx.x; base < units; base += (int64_t)gridDim.x * W) {
+        float m, l, acc;
+        int64_t u = base + (int64_t)warp * gridDim.x;
+        if (u < units) {
+            const int4 row = P.longs[u / per_row];
+            const int h = (int)(u % per_row) / parts, col = (int)(u % parts) * 32 + lane;
+            if (row.z <= 32) {
+                join_chunks(P.partial + (int64_t)row.y * stride + (int64_t)h * (D + 2), stride, D, col, 0, row.z, m, l, acc);
+                put(row, h, col, m, l, acc);
+            }
         }
-        if (threadIdx.x == 0) P.a.lse[(int64_t)row.x * P.a.q_heads + h] = none ? -INFINITY : top * CA_LN2 + logf(l);
+        u = base;
+        for (int i = 0; i < W && u < units; ++i, u += gridDim.x) {
+            const int4 row = P.longs[u / per_row];
+            if (row.z <= 32) continue;
+            const int h = (int)(u % per_row) / parts, col = (int)(u % parts) * 32 + lane;
+            const int per = (row.z + W - 1) / W, c0 = warp * per, c1 = c0 + per < row.z ? c0 + per : row.z;
+            join_chunks(P.partial + (int64_t)row.y * stride + (int64_t)h * (D + 2), stride, D, col, c0, c1, m, l, acc);
+            __syncthreads();                                   // the previous unit's sums are read
+            if (lane == 0) {
+                s_m[warp] = m;
+                s_l[warp] = l;
+            }
+            s_acc[warp][lane] = acc;
+            __syncthreads();
+            if (warp != 0) continue;
+            const float mw = s_m[lane];
+            m = mw;
+            for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, o));
+            const float scale = exp2_fast(mw - (m == -INFINITY ? 0.f : m));
+            l = s_l[lane] * scale;
+            for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(FULL, l, o);
+            acc = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) acc = fmaf(s_acc[w][lane], __shfl_sync(FULL, scale, w), acc);
+            put(row, h, col, m, l, acc);
+        }
     }
 }
 
@@ -452,13 +478,6 @@ static CodedAttendLayout coded_attend_layout(int64_t edges, int32_t q_heads, int
 }
 size_t coded_attention_workspace(int64_t edges, int32_t q_heads, int32_t head_dim) { return coded_attend_layout(edges, q_heads, head_dim).total; }
 
-template <typename T> static cudaError_t launch_join(const CodedAttend& P, cudaStream_t s) {
-    const int D = P.a.head_dim;
-    if (D <= 32) return launch_train(k_coded_attend_join<T, 1>, sm_count() * 2, 1024, 0, s, P);
-    if (D <= 64) return launch_train(k_coded_attend_join<T, 2>, sm_count() * 2, 1024, 0, s, P);
-    if (D <= 128) return launch_train(k_coded_attend_join<T, 4>, sm_count() * 2, 1024, 0, s, P);
-    return launch_train(k_coded_attend_join<T, 8>, sm_count() * 2, 1024, 0, s, P);
-}
 static void set_units(CodedAttend& P, int heads) {
     P.units_per_row = P.a.q_heads / heads;
     P.unit_shift = -1;
@@ -466,6 +485,12 @@ static void set_units(CodedAttend& P, int heads) {
         if (P.units_per_row == 1 << i) P.unit_shift = i;
 }
 static int64_t chunk_bound(const CodedAttend& P) { return (int64_t)P.a.edge_bound / CA_LONG + 1; }
+// Chunks that keep sixteen warps on every SM busy once, so that no warp has a second one while others have none, and the join little
+// to do (one row of 200,011 edges, 2 x 4 heads of 64: 38 us, with chunks of 128 46).
+static int chunk_length(const CodedAttend& P, int heads) {
+    const int64_t n = ((int64_t)P.a.edge_bound * (P.a.q_heads / heads) / (sm_count() * 16) + 31) / 32 * 32;
+    return n < CA_CHUNK ? CA_CHUNK : (n > CA_CHUNK_MOST ? CA_CHUNK_MOST : (int)n);
+}
 
 // One element at a time per lane: rows of up to CA_LONG edges, or chunks.
 template <typename T, int VE, int G> static cudaError_t run_coded(CodedAttend P, int chunk_mode, cudaStream_t s) {
@@ -476,6 +501,7 @@ template <typename T, int VE, int G> static cudaError_t run_coded(CodedAttend P,
     set_units(P, G);
     constexpr int smem = CA_THREADS / 32 * 2 * U * 2 * VE * 32;
     P.chunk_mode = chunk_mode;
+    P.chunk = chunk_length(P, G);
     const int64_t n = chunk_mode ? chunk_bound(P) : P.a.dst.bound;
     P.slots = chunk_mode ? 32 / P.tl : 1;
     // groups share a row while the rows alone do not give every SM sixteen warps and each keeps U edges
@@ -504,6 +530,7 @@ template <int SP> static cudaError_t run_tc(CodedAttend P, int chunk_mode, cudaS
     if (e != cudaSuccess) return e;
     set_units(P, S::SLOTS);
     P.chunk_mode = chunk_mode;
+    P.chunk = chunk_length(P, S::SLOTS);
     const int64_t n = chunk_mode ? chunk_bound(P) : P.a.dst.bound;
     int64_t grid = (n * P.units_per_row + TC_WARPS - 1) / TC_WARPS;
     const int64_t cap = sm_count() * 4;                      // what is resident
@@ -526,7 +553,7 @@ template <typename T> static cudaError_t run_attention(const CodedAttend& P, cud
     };
     cudaError_t e = part(0);
     if (P.split && e == cudaSuccess) e = part(1);
-    if (P.split && e == cudaSuccess) e = launch_join<T>(P, s);
+    if (P.split && e == cudaSuccess) e = launch_train(k_coded_attend_join<T>, sm_count() * 2, 1024, 0, s, P);
     return e;
 }
 

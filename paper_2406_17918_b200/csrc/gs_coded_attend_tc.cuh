@@ -124,11 +124,11 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
         w.end = w.end > P.a.edge_bound ? P.a.edge_bound : w.end;
         if (w.end < w.begin) w.end = w.begin;
         if (P.chunk_mode) {
-            w.begin += P.items[w.r].y * CA_CHUNK;
-            w.end = w.begin + CA_CHUNK < w.end ? w.begin + CA_CHUNK : w.end;
+            w.begin += P.items[w.r].y * P.chunk;
+            w.end = w.begin + P.chunk < w.end ? w.begin + P.chunk : w.end;
         } else if (P.split && w.end - w.begin > CA_LONG) {
             if (w.unit == 0) {                               // listed once, by the warp of the row's first unit
-                const int nc = (w.end - w.begin + CA_CHUNK - 1) / CA_CHUNK;
+                const int nc = (w.end - w.begin + P.chunk - 1) / P.chunk;
                 int first = 0;
                 if (lane == 0) {
                     first = atomicAdd(P.words, nc);
@@ -357,14 +357,14 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
         float out[L];
 #pragma unroll
         for (int i = 0; i < TILES; ++i) {
-            out[i] = fmaf(__shfl_xor_sync(FULL, acc[i][0], 4), 1.f / 2048.f, acc[i][0]);
-            out[TILES + i] = fmaf(__shfl_xor_sync(FULL, acc[i][1], 4), 1.f / 2048.f, acc[i][1]);
+            out[i] = fmaf(__shfl_xor_sync(FULL, acc[i][0], 4), 1.f / 33554432.f, acc[i][0] * (1.f / 16384.f));
+            out[TILES + i] = fmaf(__shfl_xor_sync(FULL, acc[i][1], 4), 1.f / 33554432.f, acc[i][1] * (1.f / 16384.f));
         }
         if (!x.w.live || (g & 1)) continue;
         const int h = h0 + my_slot, col = t * L;
         const bool none = total == 0.f;                      // no edge left by the mask: zero row, log of an empty sum
         if (P.chunk_mode) {
-            const float unit = at_m == -INFINITY ? 0.f : exp2_fast(at_mv - 14.f - at_m);
+            const float unit = at_m == -INFINITY ? 0.f : exp2_fast(at_mv - at_m);
             float* part = P.partial + ((int64_t)x.w.r * P.a.q_heads + h) * (D + 2);
 #pragma unroll
             for (int i = 0; i < L; ++i)
@@ -374,8 +374,8 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
                 part[D + 1] = total;
             }
         } else {
-            // 2^(mv - 14 - m) / l in one factor
-            const float unit = none ? 0.f : exp2_fast(at_mv - 14.f - at_m) / total;
+            // 2^(mv - m) / l in one factor
+            const float unit = none ? 0.f : exp2_fast(at_mv - at_m) / total;
             bf16* to = (bf16*)P.a.out.data + (int64_t)x.w.row * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride;
             if (P.wide && L >= 8) {
 #pragma unroll
