@@ -70,7 +70,8 @@ template <typename T, int VE> __device__ __forceinline__ void unpack(const Raw<T
 }
 
 // Stores VE floats as VE elements of T in pieces of at most 16 bytes; the address is aligned to the piece.
-template <typename T, int VE> __device__ __forceinline__ void store_vec(T* p, const float (&x)[VE]) {
+// STREAM: results that are not read soon leave L2 first.
+template <typename T, int VE, bool STREAM = false> __device__ __forceinline__ void store_vec(T* p, const float (&x)[VE]) {
     constexpr int BYTES = (int)sizeof(T) * VE;
     uint32_t w[BYTES >= 4 ? BYTES / 4 : 1];
     if constexpr (sizeof(T) == 4) {
@@ -88,7 +89,11 @@ template <typename T, int VE> __device__ __forceinline__ void store_vec(T* p, co
         *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
     } else {
 #pragma unroll
-        for (int i = 0; i < BYTES / 16; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        for (int i = 0; i < BYTES / 16; ++i) {
+            const uint4 y = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+            if constexpr (STREAM) __stcs(reinterpret_cast<uint4*>(p) + i, y);
+            else reinterpret_cast<uint4*>(p)[i] = y;
+        }
     }
 }
 
