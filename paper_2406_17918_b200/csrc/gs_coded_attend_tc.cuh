@@ -6,11 +6,10 @@
 //   scores:  C[16 edges][slots] += K[16 edges][16 columns] q^T   (m16n8k16, sums in 32 bits; slot t is column 2 t, in lane t of a quad)
 //   values:  acc[slots][columns] += P[slots][16 edges] V[16 edges][8 columns]
 // P is not rounded to f16: a weight is hi + 2^-11 lo, two rows of the matrix, 22 bits of it.  The weights carry their value block's
-// scale; they are held relative to the largest weight times scale so far, as 2^14 (f16 keeps 2^-38 of that), with a maximum of its
-// own for lse.
+// scale; they are held relative to a power of two near the largest weight times scale so far, as 2^14 (f16 keeps 2^-38 of that).
 // What bounds it is instructions around the products (ALU 57%, issue slots 64%), not their rate, so the legacy matrix instruction
 // serves.  With fewer shared heads the other kernel needs fewer instructions.  Both measured, this : that (head groups, columns,
-// longest row): 4 x 64, 20 edges 326 : 617 us; 4 x 128, 30 edges 404 : 914; 4 x 64, 64 edges 600 : 1,674; one row of 200,011 edges 47 : 79;
+// longest row): 4 x 64, 20 edges 340 : 617 us; 4 x 128, 30 edges 418 : 914; 4 x 64, 64 edges 624 : 1,674; one row of 200,011 edges 41 : 79;
 // but 2 x 32, 20 edges 314 : 258; 1 x 32, 20 edges 527 : 284; 1 x 32, one row of 200,011 edges 44 : 43.
 //
 // Rows are gathered by cp.async into TC_STAGES buffers of 16 edges a warp, TC_STAGES - 1 tiles ahead; the columns of 32 edges are read
@@ -57,6 +56,8 @@ __device__ __forceinline__ float f16_lo(uint32_t x) {
     asm("{.reg .f16 a, b;\n\tmov.b32 {a, b}, %1;\n\tcvt.f32.f16 %0, a;}" : "=f"(y) : "r"(x));
     return y;
 }
+// 2^e; 0 below the range of f32 (and its largest power above: of no number that is not zero).
+__device__ __forceinline__ float power_of(int e) { return __uint_as_float((uint32_t)(min(max(e, -127), 127) + 127) << 23); }
 // Place of byte `at` of an edge's row in a buffer of 16 edges.
 __device__ __forceinline__ int tile_byte(int edge, int at) {
     const int c = (((edge & 1) << 1) | ((edge >> 1) & 1)) ^ ((edge >> 2 & 1) << 1), key = c << 1 | (edge & 1);
@@ -234,7 +235,8 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
 
     // what a unit keeps: the queries' fragments (lane g, t: slot g / 2, columns t L ...), sums, maxima (lane g, t: slot t)
     uint32_t q[SP][2];
-    float acc[TILES][2], m = 0.f, mv = 0.f, l = 0.f, qscale = 0.f;
+    float acc[TILES][2], m = 0.f, l = 0.f, qscale = 0.f;
+    int unit = 0;                                            // acc is in units of 2^(unit - 254 - 14)
     const float c2 = P.a.scale * CA_LOG2E;
     const int my_slot = g >> 1;
     while (ahead > 0) {
@@ -254,8 +256,9 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
         stage = stage + 1 == TC_STAGES ? 0 : stage + 1;
         const int h0 = x.w.unit * SLOTS;
         if (x.first) {
-            m = mv = -INFINITY;
+            m = -INFINITY;
             l = 0.f;
+            unit = 0;
 #pragma unroll
             for (int i = 0; i < TILES; ++i) acc[i][0] = acc[i][1] = 0.f;
             float y[L];
@@ -299,20 +302,23 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
         const uint32_t kb0 = __shfl_sync(FULL, x.scales, g), kb1 = __shfl_sync(FULL, x.scales, g + 8);
         const uint32_t vb0 = __shfl_sync(FULL, x.scales, g + 16), vb1 = __shfl_sync(FULL, x.scales, g + 24);
         const float s0 = x.on >> g & 1 ? c[0] * scale_of(kb0) * qscale : -INFINITY, s1 = x.on >> (g + 8) & 1 ? c[2] * scale_of(kb1) * qscale : -INFINITY;
-        const float y0 = s0 + (float)((int)vb0 - 127), y1 = s1 + (float)((int)vb1 - 127);
-        float top = fmaxf(s0, s1), topv = fmaxf(y0, y1);
+        float top = fmaxf(s0, s1);
 #pragma unroll
-        for (int o = 4; o < 32; o <<= 1) {
-            top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
-            topv = fmaxf(topv, __shfl_xor_sync(FULL, topv, o));
-        }
+        for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
         top = fmaxf(top, m);
-        topv = fmaxf(topv, mv);
-        const float ref = top == -INFINITY ? 0.f : top, refv = topv == -INFINITY ? 0.f : topv;   // nothing seen yet: all weights are zero
-        l = fmaf(l, exp2_fast(m - ref), exp2_fast(s0 - ref) + exp2_fast(s1 - ref));
-        const float corr = exp2_fast(mv - refv), x0 = exp2_fast(y0 - refv + 14.f), x1 = exp2_fast(y1 - refv + 14.f);
+        const float ref = top == -INFINITY ? 0.f : top;      // nothing seen yet: all weights are zero
+        const float fall = m - ref, p0 = exp2_fast(s0 - ref), p1 = exp2_fast(s1 - ref);
         m = top;
-        mv = topv;
+        l = fmaf(l, exp2_fast(fall), p0 + p1);
+        // exponents of weight times scale, both with their bias: the largest, and the one so far after the maximum's rise
+        const int e0 = p0 > 0.f ? (int)(__float_as_uint(p0) >> 23) + (int)vb0 : 0, e1 = p1 > 0.f ? (int)(__float_as_uint(p1) >> 23) + (int)vb1 : 0;
+        int most = max(e0, e1);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) most = max(most, __shfl_xor_sync(FULL, most, o));
+        most = max(most, unit + (int)ceilf(fmaxf(fall, -1000.f)));
+        const float corr = exp2_fast(fall) * power_of(unit - most);
+        const float x0 = p0 * 16384.f * power_of((int)vb0 - most + 127), x1 = p1 * 16384.f * power_of((int)vb1 - most + 127);
+        unit = most;
         const float hi0 = f16_lo(pack_f16(x0, 0.f)), hi1 = f16_lo(pack_f16(x1, 0.f));
         const uint32_t a0 = transpose8(pack_f16(x0, (x0 - hi0) * 2048.f)), a2 = transpose8(pack_f16(x1, (x1 - hi1) * 2048.f));
         if (__any_sync(FULL, corr != 1.f)) {
@@ -353,7 +359,7 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
         // ---- the unit's end: rows 2 slot (hi) and 2 slot + 1 (lo) of acc; a lane has columns 4 SP t ...
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(FULL, l, o);
-        const float total = __shfl_sync(FULL, l, my_slot), at_m = __shfl_sync(FULL, m, my_slot), at_mv = __shfl_sync(FULL, mv, my_slot);
+        const float total = __shfl_sync(FULL, l, my_slot), at_m = __shfl_sync(FULL, m, my_slot), in = scale_of((uint32_t)max(__shfl_sync(FULL, unit, my_slot) - 127, 0));
         float out[L];
 #pragma unroll
         for (int i = 0; i < TILES; ++i) {
@@ -364,31 +370,29 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
         const int h = h0 + my_slot, col = t * L;
         const bool none = total == 0.f;                      // no edge left by the mask: zero row, log of an empty sum
         if (P.chunk_mode) {
-            const float unit = at_m == -INFINITY ? 0.f : exp2_fast(at_mv - at_m);
             float* part = P.partial + ((int64_t)x.w.r * P.a.q_heads + h) * (D + 2);
 #pragma unroll
             for (int i = 0; i < L; ++i)
-                if (col + i < D) part[col + i] = none ? 0.f : out[i] * unit;
+                if (col + i < D) part[col + i] = none ? 0.f : out[i] * in;
             if (t == 0) {
                 part[D] = at_m;
                 part[D + 1] = total;
             }
         } else {
-            // 2^(mv - m) / l in one factor
-            const float unit = none ? 0.f : exp2_fast(at_mv - at_m) / total;
+            const float inv = none ? 0.f : 1.f / total;
             bf16* to = (bf16*)P.a.out.data + (int64_t)x.w.row * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride;
             if (P.wide && L >= 8) {
 #pragma unroll
                 for (int i = 0; i < L / 8; ++i) {
                     float z[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) z[j] = none ? 0.f : out[8 * i + j] * unit;
+                    for (int j = 0; j < 8; ++j) z[j] = none ? 0.f : out[8 * i + j] * in * inv;
                     if (col + 8 * i < D) store_vec<bf16, 8>(to + col + 8 * i, z);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < L; ++i)
-                    if (col + i < D) to[col + i] = from_f32<bf16>(none ? 0.f : out[i] * unit);
+                    if (col + i < D) to[col + i] = from_f32<bf16>(none ? 0.f : out[i] * in * inv);
             }
             if (t == 0) P.a.lse[(int64_t)x.w.row * P.a.q_heads + h] = none ? -INFINITY : at_m * CA_LN2 + logf(total);
         }

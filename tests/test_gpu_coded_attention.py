@@ -227,3 +227,120 @@ def test_no_rows_no_edges():
     assert out.shape == (0, 2, 16)
     out, lse = gs.gs_coded_attention_forward(zero.repeat(3), none, torch.randn(2, 2, 16, device="cuda"), k, v, _ws(2, 0, 2, 16))
     assert (out == 0).all() and torch.isneginf(lse).all()
+
+
+# Four query heads that share a key head, bf16: the products of the tensor cores.  A weight is held in 22 bits (2^-22 of itself, or
+# 2^-49 of the largest) and what is 2^-31 below a query row's largest element in fewer than its 8: both within the bounds above.
+@pytest.mark.parametrize("cap", [1, 3])
+@pytest.mark.parametrize("d", [16, 64, 100])
+def test_any_grid_shared_heads(cap, d):
+    g = _gen(8)
+    indptr, idx = _block([0, 700, 3] + [11] * 200 + [1500, 16, 17, 32, 33, 0], 300, g, masked=0.1)
+    n = indptr.numel() - 1
+    store = _store(300, 4, d, 16, g)
+    q = torch.randn(n, 8, d, generator=g, device="cuda").to(B)
+    args = (indptr, idx, q, store.heads(0, 2), store.heads(2, 4))
+    out, lse = gs.gs_coded_attention_forward(*args, _ws(n, idx.numel(), 8, d))
+    gs.gs_debug_set_grid_cap(cap)
+    try:
+        again, alse = gs.gs_coded_attention_forward(*args, _ws(n, idx.numel(), 8, d))
+    finally:
+        gs.gs_debug_set_grid_cap(0)
+    assert torch.equal(out, again) and torch.equal(lse, alse)
+
+
+def test_values_of_every_size_shared_heads():
+    g = _gen(9)
+    store = gs.gs_coded_rows(64, 2, 32, 1)
+    x = torch.randn(64, 2, 32, generator=g, device="cuda")
+    x[:, 0] *= torch.exp2(torch.linspace(-100, 9, 64, device="cuda"))[:, None]
+    x[:, 1] *= torch.exp2(torch.linspace(60, -100, 64, device="cuda"))[:, None]
+    gs.gs_coded_write(store, x)
+    indptr = torch.tensor([0, 64, 84, 100, 101], dtype=torch.int32, device="cuda")
+    idx = torch.cat([torch.randperm(64, generator=g, device="cuda"), torch.arange(0, 20, device="cuda"), torch.arange(40, 56, device="cuda"),
+                     torch.tensor([63], device="cuda")]).int()
+    q = torch.randn(4, 4, 32, generator=g, device="cuda")
+    q[:, 1] *= 2.0 ** 20
+    q[:, 2] *= 2.0 ** -90
+    q[:, 3, 1:] *= 2.0 ** -28
+    q = q.to(B)
+    out, lse = gs.gs_coded_attention_forward(indptr, idx, q, store.heads(0, 1), store.heads(1, 2), _ws(4, 101, 4, 32))
+    both = _values(store)
+    want = _reference(indptr, idx, q, both[:, :1], both[:, 1:], 32 ** -0.5, B)
+    _check("out", out, want["out"])
+    _check("lse", lse, want["lse"])
+    # one edge: its value as it is, however small
+    assert torch.equal(out[3], both[63, 1].to(B).expand(4, 32)) and (out[3] != 0).any()
+
+
+@pytest.mark.parametrize("hq", [4, 2])
+def test_nan_stays_in_its_place(hq):
+    """A NaN key makes the rows that meet it NaN in its own key head, a NaN value in its own column; zero queries are no special case."""
+    g = _gen(10)
+    x = torch.randn(50, 4, 32, generator=g, device="cuda")
+    x[7, 0, 3] = float("nan")                                # a key of key head 0
+    x[9, 3, 5] = float("inf")                                # a value of key head 1
+    store = gs.gs_coded_rows(50, 4, 32, 1)
+    gs.gs_coded_write(store, x)
+    indptr = torch.tensor([0, 20, 40, 40, 180], dtype=torch.int32, device="cuda")
+    idx = (torch.arange(180, device="cuda") % 6 + 10).int()
+    idx[5], idx[25], idx[100], idx[101] = 7, 9, 7, 9
+    q = torch.randn(4, 2 * hq, 32, generator=g, device="cuda").to(B)
+    q[:, hq + 1] = 0
+    out, lse = gs.gs_coded_attention_forward(indptr, idx, q, store.heads(0, 2), store.heads(2, 4), _ws(4, 180, 2 * hq, 32))
+    bad = torch.isnan(out)
+    want = torch.zeros_like(bad)
+    want[0, :hq] = want[3, :hq] = True
+    want[1, hq:, 5] = want[3, hq:, 5] = True
+    assert torch.equal(bad, want) and (out[2] == 0).all()
+    sums = torch.zeros(4, 2 * hq, dtype=torch.bool, device="cuda")
+    sums[0, :hq] = sums[3, :hq] = True
+    assert torch.equal(torch.isnan(lse), sums) and torch.isneginf(lse[2]).all()
+
+
+@pytest.mark.parametrize("t,hq,hk,d", [(F, 4, 4, 8), (B, 8, 2, 16), (B, 4, 4, 8)])
+def test_chunks_of_a_whole_neighbourhood(t, hq, hk, d):
+    """So many edges that the chunks are longer than the shortest; rows of a few chunks and of very many beside one another."""
+    g = _gen(11)
+    indptr, idx = _block([500000, 0, 65, 400, 30000, 1, 120000], 5000, g, masked=0.1)
+    n = indptr.numel() - 1
+    store = _store(5000, 2 * hk, d, 16, g)
+    q = torch.randn(n, hq, d, generator=g, device="cuda").to(t)
+    out, lse = gs.gs_coded_attention_forward(indptr, idx, q, store.heads(0, hk), store.heads(hk, 2 * hk), _ws(n, idx.numel(), hq, d))
+    both = _values(store)
+    want = _reference(indptr, idx, q, both[:, :hk], both[:, hk:], d ** -0.5, t)
+    _check("out", out, want["out"])
+    _check("lse", lse, want["lse"])
+
+
+def test_two_captured_graphs_with_one_workspace():
+    """Graphs replayed one after the other share a workspace; new inputs in the same places count."""
+    g = _gen(12)
+    ws = _ws(6, 1500, 8, 32)
+    store = _store(300, 4, 32, 16, g)
+    calls = []
+    for lengths in ([700, 3, 0], [5, 130, 64, 65]):
+        indptr, idx = _block(lengths, 300, g)
+        calls.append((indptr, idx, torch.randn(len(lengths), 8, 32, generator=g, device="cuda").to(B), store.heads(0, 2), store.heads(2, 4), ws))
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graphs, results = [], []
+    with torch.cuda.stream(stream):
+        for args in calls:
+            gs.gs_coded_attention_forward(*args)
+        for args in calls:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                results.append(gs.gs_coded_attention_forward(*args))
+            graphs.append(graph)
+    torch.cuda.synchronize()
+    for again in range(2):
+        for args in calls:
+            args[2].copy_(torch.randn(args[2].shape, generator=g, device="cuda").to(B))
+        ws.fill_(255)
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for args, got in zip(calls, results):
+            out, lse = gs.gs_coded_attention_forward(*args)
+            assert torch.equal(out, got[0]) and torch.equal(lse, got[1])
