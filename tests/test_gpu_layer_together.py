@@ -1,6 +1,8 @@
 """The operators around an attention layer used together: a training step with clipped gradients against 64-bit autograd, a served
 layer over a cache in 8 bits against the same layer on what the cache holds, both captured and replayed, calls on another stream."""
 import math
+import os
+import sys
 
 import pytest
 import torch
@@ -63,6 +65,26 @@ def test_a_training_step():
     for a, b in zip(grads, ref):
         b = b.grad * (0.7 / want)
         assert (a.double() - b).norm() <= 2e-4 * b.norm()
+
+
+@pytest.mark.parametrize("norm,max_norm", [("rms", 0.0), ("layer", 0.5), ("rms", 0.5)])
+def test_the_example_with_norm_and_clipping(norm, max_norm):
+    """It runs; the parameters' gradients of its last step have the norm they are clipped to, or less."""
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import train_context_nodes as example
+
+    made, model = [], example.Model
+    try:
+        example.Model = lambda *a, **k: made.append(model(*a, **k)) or made[0]
+        history = example.train("tiny", 3, log=lambda *_: None, norm=norm, max_norm=max_norm)
+    finally:
+        example.Model = model
+    assert len(history) == 3 and all(math.isfinite(x) for x in history)
+    grads = [p.grad for p in made[0].parameters()]
+    total = math.sqrt(sum(float((g.double() ** 2).sum()) for g in grads))
+    assert math.isfinite(total) and total > 0 and (not max_norm or total <= max_norm * (1 + 2.0 ** -19))
+    if norm == "rms":
+        assert all(float(p.grad.abs().sum()) > 0 for p in made[0].norm)
 
 
 class Served:

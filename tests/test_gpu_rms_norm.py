@@ -198,6 +198,18 @@ def test_in_eight_bits(t, heads, hd, n):
     _near(values, y, torch.maximum(2.0 ** -4 * y.abs(), 2.0 ** -10 * unit) + 2 * slack * y.abs(), "values")
 
 
+def test_rows_that_are_not_finite_in_eight_bits():
+    """An infinity makes its own element NaN and the others zeros, a NaN the row; squares beyond 32 bits are an infinity."""
+    x = torch.ones(5, 64, device="cuda")
+    x[0, 3], x[1, 4], x[2, 5] = float("inf"), float("nan"), 3e38
+    x[3] = 0
+    store = gs.gs_coded_rows(5, 2, 32, 1)
+    gs.gs_rms_norm_coded(x, store)
+    v = gs.gs_coded_read(store, num_rows=5, out_dtype=F).view(5, 64)
+    assert torch.isnan(v[0, 3]) and (torch.cat([v[0, :3], v[0, 4:]]) == 0).all() and torch.isnan(v[1]).all()
+    assert (v[2] == 0).all() and (v[3] == 0).all() and (v[4] == 1).all()
+
+
 def test_in_eight_bits_without_residual_and_with_a_count():
     x, _, w, _, _ = _inputs(40, 128, B, F)
     a, b = gs.gs_coded_rows(40, 4, 32, 1), gs.gs_coded_rows(40, 4, 32, 1)
