@@ -114,7 +114,11 @@ struct CodedUnits {
     bool live;
 };
 
-__device__ __forceinline__ CodedUnits find_units(const CodedAttend& P, int64_t u, int64_t units, int part, int parts) {
+// What a launch does with rows of more than CA_LONG edges: there are none (or they are no matter), they are listed, or their chunks are
+// its rows.
+enum { CA_ALL, CA_LIST, CA_CHUNKS };
+
+template <int MODE> __device__ __forceinline__ CodedUnits find_units(const CodedAttend& P, int64_t u, int64_t units, int part, int parts) {
     CodedUnits w;
     w.live = u < units;
     w.r = w.row = w.unit = w.begin = w.end = 0;
@@ -124,7 +128,7 @@ __device__ __forceinline__ CodedUnits find_units(const CodedAttend& P, int64_t u
     w.unit = (int)(u - (int64_t)w.r * P.units_per_row);
     w.row = w.r;
     int skip = 0;
-    if (P.chunk_mode) {
+    if constexpr (MODE == CA_CHUNKS) {
         const int2 it = P.items[w.r];
         w.row = it.x;
         skip = it.y * P.chunk;
@@ -133,10 +137,10 @@ __device__ __forceinline__ CodedUnits find_units(const CodedAttend& P, int64_t u
     b = b < 0 ? 0 : b;
     e = e > P.a.edge_bound ? P.a.edge_bound : e;
     if (e < b) e = b;
-    if (P.chunk_mode) {
+    if constexpr (MODE == CA_CHUNKS) {
         w.begin = b + skip;
         w.end = w.begin + P.chunk < e ? w.begin + P.chunk : e;
-    } else if (P.split && e - b > CA_LONG) {
+    } else if (MODE == CA_LIST && e - b > CA_LONG) {
         if (w.unit == 0) {                                   // listed once, by the lanes of the row's first unit
             const int nc = (e - b + P.chunk - 1) / P.chunk, lanes = parts - 1;
             const uint32_t mask = parts == 32 ? FULL : ((1u << parts) - 1u) << (threadIdx.x & 31 & ~lanes);
@@ -159,14 +163,14 @@ __device__ __forceinline__ CodedUnits find_units(const CodedAttend& P, int64_t u
 // The batches of a warp's sets are one stream: the codes of a batch are on their way to slots of the lane's own in shared memory
 // (zeros where there is no edge) while the batch before is worked on, the rows of the next one are looked up, and the next set's
 // offsets and query rows are fetched when its first batch is.  No lane reads what another has copied: no barriers.
-template <typename T, int VE, int G, int U> __global__ void __launch_bounds__(CA_THREADS, G == 1 ? 4 : 3) k_coded_attend(const __grid_constant__ CodedAttend P) {
+template <typename T, int VE, int G, int U, int MODE> __global__ void __launch_bounds__(CA_THREADS, G == 1 ? 4 : 3) k_coded_attend(const __grid_constant__ CodedAttend P) {
     constexpr int N2 = VE / 2;
     constexpr int SLOT = U * 2 * VE * 32;                    // bytes of a batch's copies, per warp
     extern __shared__ __align__(16) unsigned char ca_smem[];
     chain_wait();
     const int lane = threadIdx.x & 31, tl = P.tl, t = lane & (tl - 1), slot = (lane / tl) & (P.slots - 1);
     const int width = tl * P.slots, per_warp = 32 / width;
-    const int rows = P.chunk_mode ? __ldcg(P.words) : list_length(P.a.dst), cols = list_length(P.a.src);
+    const int rows = MODE == CA_CHUNKS ? __ldcg(P.words) : list_length(P.a.dst), cols = list_length(P.a.src);
     const int64_t units = (int64_t)rows * P.units_per_row;
     const int64_t step = (int64_t)gridDim.x * (CA_THREADS / 32) * per_warp;
     const float c2 = P.a.scale * CA_LOG2E;
@@ -178,7 +182,7 @@ template <typename T, int VE, int G, int U> __global__ void __launch_bounds__(CA
 
     // ---- ahead: the set whose batches are being fetched
     int64_t base = ((int64_t)blockIdx.x * (CA_THREADS / 32) + (threadIdx.x >> 5)) * per_warp;
-    CodedUnits w = find_units(P, base + lane / width, units, lane & (width - 1), width);
+    CodedUnits w = find_units<MODE>(P, base + lane / width, units, lane & (width - 1), width);
     const uint8_t* kbase = nullptr;
     const uint8_t* vbase = nullptr;
     const uint8_t* ksbase = nullptr;
@@ -262,7 +266,7 @@ template <typename T, int VE, int G, int U> __global__ void __launch_bounds__(CA
             base += step;
             more = base < units;
             if (more) {
-                w = find_units(P, base + lane / width, units, lane & (width - 1), width);
+                w = find_units<MODE>(P, base + lane / width, units, lane & (width - 1), width);
                 begin_set();
             }
         }
@@ -354,7 +358,7 @@ template <typename T, int VE, int G, int U> __global__ void __launch_bounds__(CA
             float y[VE];
 #pragma unroll
             for (int c = 0; c < N2; ++c) split(acc[i][c], y[2 * c], y[2 * c + 1]);
-            if (P.chunk_mode) {
+            if constexpr (MODE == CA_CHUNKS) {
                 float* part = P.partial + ((int64_t)cur.r * P.a.q_heads + h) * (D + 2);
 #pragma unroll
                 for (int c = 0; c < VE; ++c)
@@ -511,7 +515,9 @@ template <typename T, int VE, int G> static cudaError_t run_coded(CodedAttend P,
     int64_t grid = (n * P.units_per_row + per_block - 1) / per_block;
     const int64_t cap = sm_count() * 16;
     if (grid > cap) grid = cap;
-    return launch_train(k_coded_attend<T, VE, G, U>, grid, CA_THREADS, smem, s, P);
+    if (chunk_mode) return launch_train(k_coded_attend<T, VE, G, U, CA_CHUNKS>, grid, CA_THREADS, smem, s, P);
+    return P.split ? launch_train(k_coded_attend<T, VE, G, U, CA_LIST>, grid, CA_THREADS, smem, s, P)
+                   : launch_train(k_coded_attend<T, VE, G, U, CA_ALL>, grid, CA_THREADS, smem, s, P);
 }
 template <typename T> static cudaError_t coded_lanes(const CodedAttend& P, int chunk_mode, cudaStream_t s) {
     const int group = P.a.q_heads / P.a.kv_heads;
