@@ -8,6 +8,9 @@
 // pieces) or by a block, in pieces of 16 bytes.  Rows of odd widths begin anywhere within a piece: a block then takes the rows that
 // begin at one place of it (every 4th f32 row of 1,433, say), so that its threads keep their columns, and only the pieces at a
 // row's ends go one element at a time.  Arrays whose rows do not begin alike go one element at a time altogether.
+// Measured (reads and writes of both sides, of a copy's 6.56 TB/s): 2.03 M x 64 bf16 forward 159 us = 0.99, backward 177 = 0.90; 30,000 x 2,000
+// f32 156 and 157 = 0.93; 100,000 x 513 f32 (rows that begin anywhere) 164 and 231 = 0.76 and 0.54; 4,096 x 1,433 12 and 26: the latency of
+// a row's sums in a block.  Two rows of a block in flight: 15 and 31.
 // dw: a group keeps its columns' sums over all of its rows; blocks leave theirs in the workspace and a second kernel adds them in
 // order.
 // Results in 8 bits: the largest magnitude of a group of columns is found among the lanes that hold it, by shuffles where the
