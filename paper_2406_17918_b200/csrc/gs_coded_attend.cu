@@ -28,6 +28,7 @@ struct CodedAttend {
     int tl, slots, units_per_row, unit_shift;
     int wide;                        // q and out in whole pieces
     int split, chunk_mode, chunk;    // chunk: edges of one
+    int most;                        // places in the lists
     int32_t* words;                  // [0] chunks, [1] long rows
     int2* items;                     // chunk -> (row, chunk of the row)
     int4* longs;                     // long row -> (row, first chunk, chunks, -)
@@ -117,6 +118,16 @@ struct CodedUnits {
     bool live;
 };
 
+// Chunks of nc from `first` on that the lists have places for: all, where the offsets ascend.
+__device__ __forceinline__ int list_room(const CodedAttend& P, int first, int nc) {
+    const int room = (uint32_t)first < (uint32_t)P.most ? P.most - first : 0;
+    return nc < room ? nc : room;
+}
+__device__ __forceinline__ int listed_chunks(const CodedAttend& P) {
+    const int n = __ldcg(P.words);
+    return (uint32_t)n < (uint32_t)P.most ? n : P.most;
+}
+
 // What a launch does with rows of more than CA_LONG edges: there are none (or they are no matter), they are listed, or their chunks are
 // its rows.
 enum { CA_ALL, CA_LIST, CA_CHUNKS };
@@ -145,14 +156,16 @@ template <int MODE> __device__ __forceinline__ CodedUnits find_units(const Coded
         w.end = w.begin + P.chunk < e ? w.begin + P.chunk : e;
     } else if (MODE == CA_LIST && e - b > CA_LONG) {
         if (w.unit == 0) {                                   // listed once, by the lanes of the row's first unit
-            const int nc = (e - b + P.chunk - 1) / P.chunk, lanes = parts - 1;
+            const int lanes = parts - 1;
+            int nc = (e - b + P.chunk - 1) / P.chunk;
             const uint32_t mask = parts == 32 ? FULL : ((1u << parts) - 1u) << (threadIdx.x & 31 & ~lanes);
             int first = 0;
             if (part == 0) {
                 first = atomicAdd(P.words, nc);
-                P.longs[atomicAdd(P.words + 1, 1)] = make_int4(w.row, first, nc, 0);
+                if (list_room(P, first, nc) > 0) P.longs[atomicAdd(P.words + 1, 1)] = make_int4(w.row, first, list_room(P, first, nc), 0);
             }
             first = __shfl_sync(mask, first, threadIdx.x & 31 & ~lanes);
+            nc = list_room(P, first, nc);
             for (int c = part; c < nc; c += parts) P.items[first + c] = make_int2(w.row, c);
         }
         w.live = false;
@@ -173,7 +186,7 @@ template <typename T, int VE, int G, int U, int MODE> __global__ void __launch_b
     chain_wait();
     const int lane = threadIdx.x & 31, tl = P.tl, t = lane & (tl - 1), slot = (lane / tl) & (P.slots - 1);
     const int width = tl * P.slots, per_warp = 32 / width;
-    const int rows = MODE == CA_CHUNKS ? __ldcg(P.words) : list_length(P.a.dst), cols = list_length(P.a.src);
+    const int rows = MODE == CA_CHUNKS ? listed_chunks(P) : list_length(P.a.dst), cols = list_length(P.a.src);
     const int64_t units = (int64_t)rows * P.units_per_row;
     const int64_t step = (int64_t)gridDim.x * (CA_THREADS / 32) * per_warp;
     const float c2 = P.a.scale * CA_LOG2E;
@@ -471,11 +484,13 @@ namespace gs {
 struct CodedAttendLayout {
     size_t words, items, longs, partial, total;
 };
+// Chunks, and long rows: each has more than LONG edges.
+static int64_t coded_attend_most(int64_t edges) { return edges / CA_LONG + 1; }
 static CodedAttendLayout coded_attend_layout(int64_t edges, int32_t q_heads, int32_t head_dim) {
     CodedAttendLayout l{};
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
-    const int64_t most = edges / CA_LONG + 1;                // chunks, and long rows: each has more than LONG edges
+    const int64_t most = coded_attend_most(edges);
     l.words = take(256);
     l.items = take((size_t)most * 8);
     l.longs = take((size_t)most * 16);
@@ -491,7 +506,7 @@ static void set_units(CodedAttend& P, int heads) {
     for (int i = 0; i < 8; ++i)
         if (P.units_per_row == 1 << i) P.unit_shift = i;
 }
-static int64_t chunk_bound(const CodedAttend& P) { return (int64_t)P.a.edge_bound / CA_LONG + 1; }
+static int64_t chunk_bound(const CodedAttend& P) { return P.most; }
 // Chunks that keep sixteen warps on every SM busy once, so that no warp has a second one while others have none, and the join little
 // to do (one row of 200,011 edges, 2 x 4 heads of 64: 38 us, with chunks of 128 46).
 static int chunk_length(const CodedAttend& P, int heads) {
@@ -571,6 +586,7 @@ cudaError_t launch_coded_attention(const CodedAttention& a, void* workspace, cud
     P.a = a;
     const CodedAttendLayout l = coded_attend_layout(a.edge_bound, a.q_heads, a.head_dim);
     char* ws = (char*)workspace;
+    P.most = (int)coded_attend_most(a.edge_bound);
     P.words = (int32_t*)(ws + l.words);
     P.items = (int2*)(ws + l.items);
     P.longs = (int4*)(ws + l.longs);

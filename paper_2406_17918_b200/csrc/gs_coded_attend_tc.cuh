@@ -95,7 +95,7 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
     extern __shared__ __align__(16) unsigned char tc_smem[];
     chain_wait();
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int rows = P.chunk_mode ? __ldcg(P.words) : list_length(P.a.dst), cols = list_length(P.a.src);
+    const int rows = P.chunk_mode ? listed_chunks(P) : list_length(P.a.dst), cols = list_length(P.a.src);
     const int64_t units = (int64_t)rows * P.units_per_row, step = (int64_t)gridDim.x * TC_WARPS;
     const int D = P.a.head_dim, group = P.a.q_heads / P.a.kv_heads, pitch = P.a.k.pitch;
     const uint32_t kstep = (uint32_t)P.a.k.row_stride, vstep = (uint32_t)P.a.v.row_stride;
@@ -129,13 +129,13 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
             w.end = w.begin + P.chunk < w.end ? w.begin + P.chunk : w.end;
         } else if (P.split && w.end - w.begin > CA_LONG) {
             if (w.unit == 0) {                               // listed once, by the warp of the row's first unit
-                const int nc = (w.end - w.begin + P.chunk - 1) / P.chunk;
-                int first = 0;
+                int nc = (w.end - w.begin + P.chunk - 1) / P.chunk, first = 0;
                 if (lane == 0) {
                     first = atomicAdd(P.words, nc);
-                    P.longs[atomicAdd(P.words + 1, 1)] = make_int4(w.row, first, nc, 0);
+                    if (list_room(P, first, nc) > 0) P.longs[atomicAdd(P.words + 1, 1)] = make_int4(w.row, first, list_room(P, first, nc), 0);
                 }
                 first = __shfl_sync(FULL, first, 0);
+                nc = list_room(P, first, nc);
                 for (int c = lane; c < nc; c += 32) P.items[first + c] = make_int2(w.row, c);
             }
             w.live = false;

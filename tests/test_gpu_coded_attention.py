@@ -344,3 +344,21 @@ def test_two_captured_graphs_with_one_workspace():
         for args, got in zip(calls, results):
             out, lse = gs.gs_coded_attention_forward(*args)
             assert torch.equal(out, got[0]) and torch.equal(lse, got[1])
+
+
+@pytest.mark.parametrize("hq", [2, 8])
+def test_more_chunks_than_edges_allow(hq):
+    """Offsets that do not ascend name edges more than once.  The lists have room for the edges once: what does not fit is left out, rows
+    that are not cut are as ever, and nothing else is touched."""
+    g = _gen(13)
+    store = _store(300, 4, 32, 16, g)
+    idx = torch.randint(0, 300, (1000,), generator=g, device="cuda", dtype=torch.int32)
+    indptr = torch.tensor(([0, 1000] * 40) + [990, 1000], dtype=torch.int32, device="cuda")
+    n = indptr.numel() - 1
+    q = torch.randn(n, hq, 32, generator=g, device="cuda").to(B)
+    need = gs.gs_coded_attention_workspace_bytes(n, 1000, hq, 32)
+    ws = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
+    out, lse = gs.gs_coded_attention_forward(indptr, idx, q, store.heads(0, 2), store.heads(2, 4), ws[:need])
+    assert (ws[need:] == 77).all()
+    one, _ = gs.gs_coded_attention_forward(indptr[-2:], idx, q[-1:], store.heads(0, 2), store.heads(2, 4), _ws(1, 1000, hq, 32))
+    assert torch.equal(out[-1:], one)
