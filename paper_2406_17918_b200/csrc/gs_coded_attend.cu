@@ -23,13 +23,20 @@ constexpr int CA_LONG = 64;          // rows of more edges go to the chunk list
 constexpr int CA_CHUNK = 128, CA_CHUNK_MOST = 512;   // edges of a chunk (at least 2 CA_LONG: the workspace's bound)
 constexpr float CA_LOG2E = 1.4426950408889634f, CA_LN2 = 0.6931471805599453f;
 
+// Lengths of the lists.  The chunks that rows ask for are counted in 64 bits: offsets that do not ascend can name the same edges from
+// every row, 2^31 times 2^23 chunks, and a count that wraps would hand places out twice.
+struct ListWords {
+    unsigned long long chunks;
+    int longs;
+};
+
 struct CodedAttend {
     CodedAttention a;
     int tl, slots, units_per_row, unit_shift;
     int wide;                        // q and out in whole pieces
     int split, chunk_mode, chunk;    // chunk: edges of one
     int most;                        // places in the lists
-    int32_t* words;                  // [0] chunks, [1] long rows
+    ListWords* words;
     int2* items;                     // chunk -> (row, chunk of the row)
     int4* longs;                     // long row -> (row, first chunk, chunks, -)
     float* partial;                  // [chunk][q head][head_dim + 2]: sum, maximum, weight
@@ -118,14 +125,21 @@ struct CodedUnits {
     bool live;
 };
 
-// Chunks of nc from `first` on that the lists have places for: all, where the offsets ascend.
+// The chunks of a row from `first` on that the lists have places for: all, where the offsets ascend.
 __device__ __forceinline__ int list_room(const CodedAttend& P, int first, int nc) {
-    const int room = (uint32_t)first < (uint32_t)P.most ? P.most - first : 0;
+    const int room = P.most - first;
     return nc < room ? nc : room;
 }
+// Puts a row of nc chunks on the list of long rows, by one thread; the first of its places among the chunks.
+__device__ __forceinline__ int list_row(const CodedAttend& P, int row, int nc) {
+    const unsigned long long at = atomicAdd(&P.words->chunks, (unsigned long long)nc);
+    const int first = at < (unsigned long long)P.most ? (int)at : P.most;
+    if (list_room(P, first, nc) > 0) P.longs[atomicAdd(&P.words->longs, 1)] = make_int4(row, first, list_room(P, first, nc), 0);
+    return first;
+}
 __device__ __forceinline__ int listed_chunks(const CodedAttend& P) {
-    const int n = __ldcg(P.words);
-    return (uint32_t)n < (uint32_t)P.most ? n : P.most;
+    const unsigned long long n = __ldcg(&P.words->chunks);
+    return n < (unsigned long long)P.most ? (int)n : P.most;
 }
 
 // What a launch does with rows of more than CA_LONG edges: there are none (or they are no matter), they are listed, or their chunks are
@@ -160,10 +174,7 @@ template <int MODE> __device__ __forceinline__ CodedUnits find_units(const Coded
             int nc = (e - b + P.chunk - 1) / P.chunk;
             const uint32_t mask = parts == 32 ? FULL : ((1u << parts) - 1u) << (threadIdx.x & 31 & ~lanes);
             int first = 0;
-            if (part == 0) {
-                first = atomicAdd(P.words, nc);
-                if (list_room(P, first, nc) > 0) P.longs[atomicAdd(P.words + 1, 1)] = make_int4(w.row, first, list_room(P, first, nc), 0);
-            }
+            if (part == 0) first = list_row(P, w.row, nc);
             first = __shfl_sync(mask, first, threadIdx.x & 31 & ~lanes);
             nc = list_room(P, first, nc);
             for (int c = part; c < nc; c += parts) P.items[first + c] = make_int2(w.row, c);
@@ -427,7 +438,7 @@ template <typename T> __global__ void __launch_bounds__(1024) k_coded_attend_joi
     __shared__ float s_m[W], s_l[W], s_acc[W][32];
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = P.a.head_dim, parts = (D + 31) / 32, per_row = P.a.q_heads * parts;
-    const int64_t units = (int64_t)__ldcg(P.words + 1) * per_row, stride = (int64_t)P.a.q_heads * (D + 2);
+    const int64_t units = (int64_t)__ldcg(&P.words->longs) * per_row, stride = (int64_t)P.a.q_heads * (D + 2);
     auto put = [&](const int4& row, int h, int col, float m, float l, float sum) {
         const bool none = l == 0.f;
         T* out = (T*)P.a.out.data + (int64_t)row.x * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride;
@@ -587,7 +598,7 @@ cudaError_t launch_coded_attention(const CodedAttention& a, void* workspace, cud
     const CodedAttendLayout l = coded_attend_layout(a.edge_bound, a.q_heads, a.head_dim);
     char* ws = (char*)workspace;
     P.most = (int)coded_attend_most(a.edge_bound);
-    P.words = (int32_t*)(ws + l.words);
+    P.words = (ListWords*)(ws + l.words);
     P.items = (int2*)(ws + l.items);
     P.longs = (int4*)(ws + l.longs);
     P.partial = (float*)(ws + l.partial);
@@ -597,7 +608,7 @@ cudaError_t launch_coded_attention(const CodedAttention& a, void* workspace, cud
     auto on16 = [&](const HeadView& v) { return (uintptr_t)v.data % 16 == 0 && (v.row_stride * size) % 16 == 0 && (v.head_stride * size) % 16 == 0; };
     P.wide = a.head_dim % ve == 0 && on16(a.q) && on16(a.out);
     if (P.split) {
-        const cudaError_t e = cudaMemsetAsync(P.words, 0, 8, s);
+        const cudaError_t e = cudaMemsetAsync(P.words, 0, sizeof(ListWords), s);
         if (e != cudaSuccess) return e;
     }
     return a.dtype == GS_BF16 ? run_attention<bf16>(P, s) : run_attention<float>(P, s);

@@ -130,10 +130,7 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
         } else if (P.split && w.end - w.begin > CA_LONG) {
             if (w.unit == 0) {                               // listed once, by the warp of the row's first unit
                 int nc = (w.end - w.begin + P.chunk - 1) / P.chunk, first = 0;
-                if (lane == 0) {
-                    first = atomicAdd(P.words, nc);
-                    if (list_room(P, first, nc) > 0) P.longs[atomicAdd(P.words + 1, 1)] = make_int4(w.row, first, list_room(P, first, nc), 0);
-                }
+                if (lane == 0) first = list_row(P, w.row, nc);
                 first = __shfl_sync(FULL, first, 0);
                 nc = list_room(P, first, nc);
                 for (int c = lane; c < nc; c += 32) P.items[first + c] = make_int2(w.row, c);
