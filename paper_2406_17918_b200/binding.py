@@ -1077,7 +1077,10 @@ class _CCoded(ctypes.Structure):
 class CodedRows:
     """Rows in 8 bits over two caller-owned tensors (see gs_coded in include/gs.h): codes [rows, heads, pitch] (float8_e4m3fn or
     uint8; pitch = head_dim rounded up to 16) and scales uint8 [ceil(rows / block), heads].  Tensors of zeros are a store of zero
-    rows.  A store holds an int32 per row and two per block beside them, for writes by id; two of those on one store may not overlap."""
+    rows.  A store holds an int32 per row and two per block beside them, for writes by id; two of those on one store may not overlap.
+    Making a store waits until these are set, so that writes on any stream find them; their memory is not given back while a write that
+    was queued before the store went is still under way.  Codes and scales are tensors like any other in this; a graph that holds a
+    write needs the store to live as long as it is replayed."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, head_dim: int, block: int = 1):
         head_dim, block = int(head_dim), int(block)
@@ -1094,6 +1097,9 @@ class CodedRows:
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("a store cannot be made while a graph is captured")
         claims = torch.full((rows + (2 * scales.shape[0] + 2 if block > 1 else 0),), -1, dtype=torch.int32, device=torch.device("cuda", device))
+        made_on = torch.cuda.current_stream(device)
+        made_on.synchronize()
+        self._made_on = made_on.cuda_stream
         self._set(codes, scales, head_dim, block, claims)
 
     def _set(self, codes, scales, head_dim, block, claims):
@@ -1109,6 +1115,7 @@ class CodedRows:
         if not 0 <= first < end <= self.num_heads:
             raise ValueError("heads [%d, %d) of %d" % (first, end, self.num_heads))
         part = object.__new__(CodedRows)
+        part._made_on = self._made_on
         part._set(self.codes[:, first:end], self.scales[:, first:end], self.head_dim, self.block, self.claims)
         return part
 
@@ -1126,7 +1133,10 @@ def gs_coded_write(to: CodedRows, rows: torch.Tensor, ids: torch.Tensor = None, 
     n = rows.shape[0] if ids is None else _ids_1d(ids, "ids").numel()
     keep, (p,) = _heads(rows.dtype, (rows, "rows", n, to.num_heads, to.head_dim))
     device = _one_device(to.codes, rows, ids, count)
-    _run(device, _L.gs_coded_write, to.address, _dtype(rows.dtype), p, _addr(ids), int(first), _counter(count, "count"), n, _addr(to.claims), _on(stream, to.codes))
+    handle = _on(stream, to.codes)
+    if ids is not None and handle != to._made_on:            # the caller does not see the claims, and cannot guard their memory
+        to.claims.record_stream(torch.cuda.current_stream(device) if stream is None else stream)
+    _run(device, _L.gs_coded_write, to.address, _dtype(rows.dtype), p, _addr(ids), int(first), _counter(count, "count"), n, _addr(to.claims), handle)
     return to
 
 
