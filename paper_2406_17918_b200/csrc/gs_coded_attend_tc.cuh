@@ -5,8 +5,11 @@
 // element is rounded):
 //   scores:  C[16 edges][slots] += K[16 edges][16 columns] q^T   (m16n8k16, sums in 32 bits; slot t is column 2 t, in lane t of a quad)
 //   values:  acc[slots][columns] += P[slots][16 edges] V[16 edges][8 columns]
-// P is not rounded to f16: a weight is hi + 2^-11 lo, two rows of the matrix, 22 bits of it.  The weights carry their value block's
-// scale; they are held relative to a power of two near the largest weight times scale so far, as 2^14 (f16 keeps 2^-38 of that).
+// P is not rounded to f16: a weight is hi + 2^-11 lo, two rows of the matrix, to 2^-23 of itself.  The weights carry their value block's
+// scale; they are held relative to a power of two near the largest weight times scale so far, as 2^14.  f16 ends 2^-38 below that, and
+// yet such weights are the result where the heavier edges' values are zero: a tile that has weights below 2^-26 multiplies those
+// again by themselves, they and the sums brought up together, in full down to 2^-106 of the largest (what 32 bits hold of an exponential
+// ends at 2^-126).  It takes a score 18 below a row's largest.
 // What bounds it is instructions around the products (ALU 57%, issue slots 64%), not their rate, so the legacy matrix instruction
 // serves.  With fewer shared heads the other kernel needs fewer instructions.  Both measured, this : that (head groups, columns,
 // longest row): 4 x 64, 20 edges 340 : 617 us; 4 x 128, 30 edges 418 : 914; 4 x 64, 64 edges 624 : 1,674; one row of 200,011 edges 41 : 79;
@@ -21,6 +24,8 @@ namespace gs {
 
 constexpr int TC_STAGES = 3;
 constexpr int TC_WARPS = 4;
+constexpr int TC_MOST = 80;                   // the largest power that sums are brought up by: they stay within 32 bits
+constexpr float TC_NEAR = 1.f / 4096.f;       // weights (the largest is 2^14) whose two parts hold 2^-23 of them
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -74,6 +79,38 @@ template <int WORDS> __device__ __forceinline__ void read_words(const unsigned c
         for (int i = 0; i < WORDS / 4; ++i) {
             const uint4 x = *reinterpret_cast<const uint4*>(tile + tile_byte(edge, at + i * 16));
             w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+        }
+    }
+}
+
+// Two weights of slot t, of the edges g and g + 8, as an operand whose rows 2 slot are f16 and rows 2 slot + 1 the rest times 2^11.
+__device__ __forceinline__ uint2 split_weights(float x0, float x1) {
+    const float hi0 = f16_lo(pack_f16(x0, 0.f)), hi1 = f16_lo(pack_f16(x1, 0.f));
+    return make_uint2(transpose8(pack_f16(x0, (x0 - hi0) * 2048.f)), transpose8(pack_f16(x1, (x1 - hi1) * 2048.f)));
+}
+// The products of weights and a tile's values: edges 2 t, 2 t + 1, 2 t + 8, 2 t + 9, columns 2 SP g ...; mma(i, weights, values) for column i of them.
+template <int SP, typename M> __device__ __forceinline__ void multiply_values(const unsigned char* vt, uint2 a, M mma) {
+    const int t = threadIdx.x & 3, byte = ((threadIdx.x & 31) >> 2) * 2 * SP;
+    if constexpr (SP == 1) {
+        auto two = [&](int edge) { return (uint32_t)*reinterpret_cast<const uint16_t*>(vt + tile_byte(edge, byte)); };
+        const uint32_t low = __byte_perm(two(2 * t), two(2 * t + 1), 0x5140), high = __byte_perm(two(2 * t + 8), two(2 * t + 9), 0x5140);
+        mma(0, a, codes_to_f16(low), codes_to_f16(high));
+        mma(1, a, codes_to_f16(low >> 16), codes_to_f16(high >> 16));
+    } else {
+        constexpr int VW = SP / 2;
+        uint32_t v0[VW], v1[VW], v2[VW], v3[VW];
+        read_words<VW>(vt, 2 * t, byte, v0);
+        read_words<VW>(vt, 2 * t + 1, byte, v1);
+        read_words<VW>(vt, 2 * t + 8, byte, v2);
+        read_words<VW>(vt, 2 * t + 9, byte, v3);
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+            const uint32_t la = __byte_perm(v0[i], v1[i], 0x5140), lb = __byte_perm(v0[i], v1[i], 0x7362);
+            const uint32_t ha = __byte_perm(v2[i], v3[i], 0x5140), hb = __byte_perm(v2[i], v3[i], 0x7362);
+            mma(4 * i, a, codes_to_f16(la), codes_to_f16(ha));
+            mma(4 * i + 1, a, codes_to_f16(la >> 16), codes_to_f16(ha >> 16));
+            mma(4 * i + 2, a, codes_to_f16(lb), codes_to_f16(hb));
+            mma(4 * i + 3, a, codes_to_f16(lb >> 16), codes_to_f16(hb >> 16));
         }
     }
 }
@@ -313,44 +350,37 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) most = max(most, __shfl_xor_sync(FULL, most, o));
         most = max(most, unit + (int)ceilf(fmaxf(fall, -1000.f)));
-        const float corr = exp2_fast(fall) * power_of(unit - most);
-        const float x0 = p0 * 16384.f * power_of((int)vb0 - most + 127), x1 = p1 * 16384.f * power_of((int)vb1 - most + 127);
+        float corr = exp2_fast(fall) * power_of(unit - most);
+        float x0 = p0 * 16384.f * power_of((int)vb0 - most + 127), x1 = p1 * 16384.f * power_of((int)vb1 - most + 127);
         unit = most;
-        const float hi0 = f16_lo(pack_f16(x0, 0.f)), hi1 = f16_lo(pack_f16(x1, 0.f));
-        const uint32_t a0 = transpose8(pack_f16(x0, (x0 - hi0) * 2048.f)), a2 = transpose8(pack_f16(x1, (x1 - hi1) * 2048.f));
-        if (__any_sync(FULL, corr != 1.f)) {
-            const float mul = __shfl_sync(FULL, corr, my_slot);     // lane `slot` of the first quad
+        // ---- values: the weights near the largest first, then what is left, from the largest of each slot down
+        const unsigned char* vt = tile + S::TILE;
+        auto rescale = [&](float by) {
+            const float mul = __shfl_sync(FULL, by, my_slot);     // lane `slot` of the first quad
 #pragma unroll
             for (int i = 0; i < TILES; ++i) {
                 acc[i][0] *= mul;
                 acc[i][1] *= mul;
             }
-        }
-        // ---- values: edges 2 t, 2 t + 1, 2 t + 8, 2 t + 9, columns 2 SP g ...
-        const unsigned char* vt = tile + S::TILE;
-        const int byte = g * 2 * SP;
-        if constexpr (SP == 1) {
-            auto two = [&](int edge) { return (uint32_t)*reinterpret_cast<const uint16_t*>(vt + tile_byte(edge, byte)); };
-            const uint32_t low = __byte_perm(two(2 * t), two(2 * t + 1), 0x5140), high = __byte_perm(two(2 * t + 8), two(2 * t + 9), 0x5140);
-            mma_f16_half(acc[0], a0, a2, codes_to_f16(low), codes_to_f16(high));
-            mma_f16_half(acc[1], a0, a2, codes_to_f16(low >> 16), codes_to_f16(high >> 16));
-        } else {
-            constexpr int VW = SP / 2;
-            uint32_t v0[VW], v1[VW], v2[VW], v3[VW];
-            read_words<VW>(vt, 2 * t, byte, v0);
-            read_words<VW>(vt, 2 * t + 1, byte, v1);
-            read_words<VW>(vt, 2 * t + 8, byte, v2);
-            read_words<VW>(vt, 2 * t + 9, byte, v3);
+        };
+        int up = 0;
+        while (true) {
+            if (__any_sync(FULL, corr != 1.f)) rescale(corr);
+            const bool far0 = x0 < TC_NEAR && up < TC_MOST, far1 = x1 < TC_NEAR && up < TC_MOST;
+            multiply_values<SP>(vt, split_weights(far0 ? 0.f : x0, far1 ? 0.f : x1), [&](int i, uint2 a, uint32_t b0, uint32_t b1) { mma_f16_half(acc[i], a.x, a.y, b0, b1); });
+            x0 = far0 ? x0 : 0.f;
+            x1 = far1 ? x1 : 0.f;
+            if (!__any_sync(FULL, x0 + x1 > 0.f)) break;
+            float high = fmaxf(x0, x1);
 #pragma unroll
-            for (int i = 0; i < VW; ++i) {
-                const uint32_t la = __byte_perm(v0[i], v1[i], 0x5140), lb = __byte_perm(v0[i], v1[i], 0x7362);
-                const uint32_t ha = __byte_perm(v2[i], v3[i], 0x5140), hb = __byte_perm(v2[i], v3[i], 0x7362);
-                mma_f16_half(acc[4 * i], a0, a2, codes_to_f16(la), codes_to_f16(ha));
-                mma_f16_half(acc[4 * i + 1], a0, a2, codes_to_f16(la >> 16), codes_to_f16(ha >> 16));
-                mma_f16_half(acc[4 * i + 2], a0, a2, codes_to_f16(lb), codes_to_f16(hb));
-                mma_f16_half(acc[4 * i + 3], a0, a2, codes_to_f16(lb >> 16), codes_to_f16(hb >> 16));
-            }
+            for (int o = 4; o < 32; o <<= 1) high = fmaxf(high, __shfl_xor_sync(FULL, high, o));
+            const int more_up = high > 0.f ? min(141 - (int)(__float_as_uint(high) >> 23), TC_MOST - up) : 0;
+            up += more_up;
+            corr = power_of(more_up);
+            x0 *= corr;
+            x1 *= corr;
         }
+        if (__any_sync(FULL, up != 0)) rescale(power_of(-up));
         __syncwarp();                                        // the buffer is read before it is filled again
         if (!x.last) continue;
         // ---- the unit's end: rows 2 slot (hi) and 2 slot + 1 (lo) of acc; a lane has columns 4 SP t ...

@@ -1,0 +1,62 @@
+"""Attention over 8-bit rows where the results hang on edges of little weight: beside a sink without a value, in columns that the heavy
+edges leave at zero.  Definition, bounds and helpers are those of the attention's other tests; every
+bound is relative to what the element itself sums up, so none is met by leaving small weights out."""
+import pytest
+import torch
+
+import paper_2406_17918_b200 as gs
+from test_gpu_coded_attention import B, F, _block, _check, _gen, _reference, _values, _ws
+
+pytestmark = pytest.mark.gpu
+
+
+def _compare(indptr, idx, q, store, hk):
+    n, hq, d = q.shape
+    out, lse = gs.gs_coded_attention_forward(indptr, idx, q, store.heads(0, hk), store.heads(hk, 2 * hk), _ws(n, idx.numel(), hq, d))
+    both = _values(store)
+    want = _reference(indptr, idx, q, both[:, :hk], both[:, hk:], d ** -0.5, q.dtype)
+    _check("out", out, want["out"])
+    _check("lse", lse, want["lse"])
+    return out
+
+
+SHAPES = [(F, 4, 32), (B, 1, 32), (B, 4, 16), (B, 4, 32), (B, 4, 33), (B, 4, 64), (B, 8, 128), (B, 4, 256)]
+
+
+@pytest.mark.parametrize("t,hq,d", SHAPES)
+@pytest.mark.parametrize("nats", [10, 25, 40, 60])
+def test_sink_without_a_value(t, hq, d, nats):
+    """Node 0 takes nearly all weight and its value row is zero: the results are what is left, of weights about e^-nats."""
+    g = _gen(nats * 1000 + d + hq)
+    x = torch.randn(200, 2, d, generator=g, device="cuda")
+    x[:, 0, 0] = 0.0
+    x[0, 0] = 0.0
+    x[0, 0, 0] = 1.0                                          # column 0 of a query meets the sink's key alone
+    x[0, 1] = 0.0
+    store = gs.gs_coded_rows(200, 2, d, 16)
+    gs.gs_coded_write(store, x)
+    indptr, idx = _block([20, 1, 40, 700, 7], 199, g)
+    idx += 1
+    idx[3], idx[21 + 30], idx[61 + 500], idx[-1] = 0, 0, 0, 0    # in the first tile, in a later one, in a chunk, at a row's end
+    q = torch.randn(5, hq, d, generator=g, device="cuda")
+    q[:, :, 0] = nats * d ** 0.5
+    out = _compare(indptr, idx, q.to(t), store, 1)
+    assert (out[[0, 2, 3, 4]] != 0).all()
+
+
+@pytest.mark.parametrize("t,hq,d", SHAPES)
+def test_columns_that_the_heavy_edges_leave_at_zero(t, hq, d):
+    """Edges whose weights fall by 6 nats each; the values of all but the last few are zero in every other column."""
+    g = _gen(d + hq)
+    x = torch.zeros(14, 2, d, device="cuda")
+    x[:, 0, 0] = -torch.arange(14, device="cuda").float()
+    x[:, 1, ::2] = torch.randn(14, (d + 1) // 2, generator=g, device="cuda")
+    x[11:, 1] = torch.randn(3, d, generator=g, device="cuda")
+    store = gs.gs_coded_rows(14, 2, d, 1)
+    gs.gs_coded_write(store, x)
+    indptr = torch.tensor([0, 12, 24, 38, 41], dtype=torch.int32, device="cuda")
+    idx = torch.cat([torch.arange(12), torch.arange(11, -1, -1), torch.randperm(14), torch.tensor([13, 0, 12])]).int().cuda()
+    q = torch.zeros(4, hq, d, device="cuda")
+    q[:, :, 0] = 6 * d ** 0.5
+    out = _compare(indptr, idx, q.to(t), store, 1)
+    assert (out[[0, 1, 2, 3]] != 0).all()
