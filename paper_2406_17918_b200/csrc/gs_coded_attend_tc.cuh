@@ -1,8 +1,8 @@
 // Attention over rows in 8 bits for bf16 queries, four or more of whose heads share a key head: the products on the tensor cores.
 //
 // A warp owns one (row, four query heads of one key head: the "slots") at a time and takes its edges 16 at a time.  The codes are
-// e4m3 numbers, exact as f16, and so is a bf16 query once it is scaled by a power of two (what is 2^30 below its row's largest
-// element is rounded):
+// e4m3 numbers, exact as f16, and so is a bf16 query once it is scaled by a power of two (one that has an element other than zero 2^31
+// below its largest is found when it is scaled, and its units are done again at the warp's end, element by element in 32 bits):
 //   scores:  C[16 edges][slots] += K[16 edges][16 columns] q^T   (m16n8k16, sums in 32 bits; slot t is column 2 t, in lane t of a quad)
 //   values:  acc[slots][columns] += P[slots][16 edges] V[16 edges][8 columns]
 // P is not rounded to f16: a weight is hi + 2^-11 lo, two rows of the matrix, to 2^-23 of itself.  The weights carry their value block's
@@ -125,6 +125,99 @@ struct TcUnit {
     int r, row, unit, begin, end;    // r: the row, or the chunk
     bool live;
 };
+
+// Whether f16 keeps the 8 bits of all elements, given the bf16 bits of the largest and of the smallest that is not zero, less one: the
+// largest is scaled to 2^14 (see up_of), and 2^-17 is the least that f16 has 8 bits of.
+__device__ __forceinline__ int up_of(uint32_t top) {         // exponent, with its bias, of the power that does so, within the range of f32
+    const int e = (int)(top >> 7);
+    return e < 15 ? 253 : (e > 253 ? 15 : 268 - e);
+}
+__device__ __forceinline__ bool too_wide(uint32_t top, uint32_t least) { return least < 0x7F80u && (int)((least + 1) >> 7) + up_of(top) < 237; }
+
+// The units of a warp whose queries are too wide for f16, in 32 bits throughout: a lane has every 32nd column.
+template <int SP> __device__ __noinline__ void attend_wide_queries(const CodedAttend& P, int64_t units) {
+    constexpr int SLOTS = 4, C = (SP + 1) / 2;
+    const int lane = threadIdx.x & 31, D = P.a.head_dim, group = P.a.q_heads / P.a.kv_heads, cols = list_length(P.a.src);
+    const float c2 = P.a.scale * CA_LOG2E;
+    for (int64_t u = (int64_t)blockIdx.x * TC_WARPS + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * TC_WARPS) {
+        const int r = (int)(u / P.units_per_row), h0 = (int)(u - (int64_t)r * P.units_per_row) * SLOTS, kv = h0 / group;
+        const int2 it = P.chunk_mode ? P.items[r] : make_int2(r, 0);
+        float q[SLOTS][C], acc[SLOTS][C], m[SLOTS], l[SLOTS];
+        bool wide = false;
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
+            const bf16* row = (const bf16*)P.a.q.data + (int64_t)it.x * P.a.q.row_stride + (int64_t)(h0 + i) * P.a.q.head_stride;
+            uint32_t top = 0, least = 0xFFFFu;
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                q[i][j] = lane + 32 * j < D ? to_f32(row[lane + 32 * j]) : 0.f;
+                acc[i][j] = 0.f;
+                const uint32_t bits = (__float_as_uint(q[i][j]) >> 16) & 0x7FFFu;
+                if (bits <= 0x7F80u) top = max(top, bits);
+                least = min(least, (bits - 1) & 0xFFFFu);
+            }
+            wide |= too_wide(__reduce_max_sync(FULL, top), __reduce_min_sync(FULL, least));
+            m[i] = -INFINITY;
+            l[i] = 0.f;
+        }
+        int begin = max(__ldg(P.a.indptr + it.x), 0), end = min(__ldg(P.a.indptr + it.x + 1), P.a.edge_bound);
+        if (!wide || (!P.chunk_mode && P.split && end - begin > CA_LONG)) continue;
+        if (P.chunk_mode) {
+            begin += it.y * P.chunk;
+            end = min(end, begin + P.chunk);
+        }
+        for (int e = begin; e < end; ++e) {
+            int at = __ldg(P.a.indices + e);
+            if ((uint32_t)at >= (uint32_t)cols) continue;
+            if (P.a.row_of) at = __ldg(P.a.row_of + at);
+            if ((uint32_t)at >= (uint32_t)P.a.k.rows) continue;
+            const uint8_t* k = P.a.k.codes + (uint64_t)(uint32_t)at * (uint32_t)P.a.k.row_stride + (int64_t)kv * P.a.k.pitch;
+            const uint8_t* v = P.a.v.codes + (uint64_t)(uint32_t)at * (uint32_t)P.a.v.row_stride + (int64_t)kv * P.a.v.pitch;
+            const float ks = scale_of(P.a.k.scales[(uint64_t)((uint32_t)at >> P.a.k.shift) * (uint32_t)P.a.k.scale_stride + kv]);
+            const float vs = scale_of(P.a.v.scales[(uint64_t)((uint32_t)at >> P.a.v.shift) * (uint32_t)P.a.v.scale_stride + kv]);
+            float x[C], s[SLOTS] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                const bool is = lane + 32 * j < D;
+                const float y = is ? decode1(k[lane + 32 * j]) : 0.f;
+                x[j] = is ? decode1(v[lane + 32 * j]) : 0.f;
+#pragma unroll
+                for (int i = 0; i < SLOTS; ++i) s[i] = fmaf(q[i][j], y, s[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i) {
+                for (int o = 16; o; o >>= 1) s[i] += __shfl_xor_sync(FULL, s[i], o);
+                s[i] = s[i] * ks * c2;
+                const float top = fmaxf(m[i], s[i]), ref = top == -INFINITY ? 0.f : top, corr = exp2_fast(m[i] - ref), p = exp2_fast(s[i] - ref);
+                m[i] = top;
+                l[i] = fmaf(l[i], corr, p);
+#pragma unroll
+                for (int j = 0; j < C; ++j) acc[i][j] = fmaf(p * vs, x[j], acc[i][j] * corr);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
+            const int h = h0 + i;
+            const bool none = l[i] == 0.f;
+            float* part = P.partial + ((int64_t)r * P.a.q_heads + h) * (D + 2);
+            bf16* to = (bf16*)P.a.out.data + (int64_t)it.x * P.a.out.row_stride + (int64_t)h * P.a.out.head_stride;
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                const int c = lane + 32 * j;
+                if (c >= D) continue;
+                if (P.chunk_mode) part[c] = acc[i][j];
+                else to[c] = from_f32<bf16>(none ? 0.f : acc[i][j] / l[i]);
+            }
+            if (lane) continue;
+            if (P.chunk_mode) {
+                part[D] = m[i];
+                part[D + 1] = l[i];
+            } else {
+                P.a.lse[(int64_t)it.x * P.a.q_heads + h] = none ? -INFINITY : m[i] * CA_LN2 + logf(l[i]);
+            }
+        }
+    }
+}
 
 template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 : (SP >= 8 ? 3 : 4)) k_coded_attend_tc(const __grid_constant__ CodedAttend P) {
     using S = TcShape<SP>;
@@ -270,6 +363,7 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
     // what a unit keeps: the queries' fragments (lane g, t: slot g / 2, columns t L ...), sums, maxima (lane g, t: slot t)
     uint32_t q[SP][2];
     float acc[TILES][2], m = 0.f, l = 0.f, qscale = 0.f;
+    bool apart = false;                                      // queries whose elements are too far apart
     int unit = 0;                                            // acc is in units of 2^(unit - 254 - 14)
     const float c2 = P.a.scale * CA_LOG2E;
     const int my_slot = g >> 1;
@@ -295,28 +389,34 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
             unit = 0;
 #pragma unroll
             for (int i = 0; i < TILES; ++i) acc[i][0] = acc[i][1] = 0.f;
-            float y[L];
             const bool has = (g & 1) == 0 && x.w.live;
+            uint32_t w[L / 2], least = 0xFFFFFFFFu;
             if (P.wide) {
-                const uint32_t* w = reinterpret_cast<const uint32_t*>(tile + 2 * S::TILE + my_slot * SP * 32 + t * L * 2);
+                const uint32_t* from = reinterpret_cast<const uint32_t*>(tile + 2 * S::TILE + my_slot * SP * 32 + t * L * 2);
+#pragma unroll
+                for (int i = 0; i < L / 2; ++i) w[i] = has ? from[i] : 0u;
+            } else {
+                const uint16_t* from = (const uint16_t*)P.a.q.data + (has ? (int64_t)x.w.row * P.a.q.row_stride + (int64_t)(h0 + my_slot) * P.a.q.head_stride : 0);
 #pragma unroll
                 for (int i = 0; i < L / 2; ++i) {
-                    const uint32_t v = has ? w[i] : 0u;
-                    y[2 * i] = bf16_lo(v);
-                    y[2 * i + 1] = bf16_hi(v);
+                    const int c = t * L + 2 * i;
+                    w[i] = has && c < D ? from[c] : 0u;
+                    w[i] |= has && c + 1 < D ? (uint32_t)from[c + 1] << 16 : 0u;
                 }
-            } else {
-                const bf16* w = (const bf16*)P.a.q.data + (has ? (int64_t)x.w.row * P.a.q.row_stride + (int64_t)(h0 + my_slot) * P.a.q.head_stride : 0);
-#pragma unroll
-                for (int i = 0; i < L; ++i) y[i] = has && t * L + i < D ? to_f32(w[t * L + i]) : 0.f;
             }
-            float top = 0.f;
+            float y[L], top = 0.f;
 #pragma unroll
-            for (int i = 0; i < L; ++i) top = fmaxf(top, fabsf(y[i]));
+            for (int i = 0; i < L / 2; ++i) {
+                least = __viaddmin_u16x2(w[i] & 0x7FFF7FFFu, 0xFFFFFFFFu, least);        // zeros become the largest
+                y[2 * i] = bf16_lo(w[i]);
+                y[2 * i + 1] = bf16_hi(w[i]);
+                top = fmaxf(top, fmaxf(fabsf(y[2 * i]), fabsf(y[2 * i + 1])));
+            }
             top = fmaxf(top, __shfl_xor_sync(FULL, top, 1));
             top = fmaxf(top, __shfl_xor_sync(FULL, top, 2));
-            // 2^(14 - e) for a largest element of 2^e, within the range of f32
-            const int e = (int)(__float_as_uint(top) >> 23), up = e < 15 ? 253 : (e > 253 ? 15 : 268 - e);
+            // 2^(14 - e) for a largest element of 2^e
+            const int up = up_of(__float_as_uint(top) >> 16);
+            apart |= too_wide(__float_as_uint(top) >> 16, min(least & 0xFFFFu, least >> 16));
             const float scale = __uint_as_float((uint32_t)up << 23);
 #pragma unroll
             for (int i = 0; i < SP; ++i) {
@@ -425,6 +525,8 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
         }
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncwarp();                                            // what is overwritten has been written
+    if (__any_sync(FULL, apart)) attend_wide_queries<SP>(P, units);
 }
 
 }  // namespace gs

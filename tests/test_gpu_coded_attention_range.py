@@ -1,6 +1,6 @@
 """Attention over 8-bit rows where the results hang on edges of little weight: beside a sink without a value, in columns that the heavy
-edges leave at zero.  Definition, bounds and helpers are those of the attention's other tests; every
-bound is relative to what the element itself sums up, so none is met by leaving small weights out."""
+edges leave at zero, with scores from columns far below a query's largest.  Definition, bounds and helpers are those of the attention's
+other tests; every bound is relative to what the element itself sums up, so none is met by leaving small weights out."""
 import pytest
 import torch
 
@@ -60,3 +60,20 @@ def test_columns_that_the_heavy_edges_leave_at_zero(t, hq, d):
     q[:, :, 0] = 6 * d ** 0.5
     out = _compare(indptr, idx, q.to(t), store, 1)
     assert (out[[0, 1, 2, 3]] != 0).all()
+
+
+@pytest.mark.parametrize("t,hq,d", SHAPES)
+@pytest.mark.parametrize("apart", [20, 40, 60])
+def test_queries_whose_columns_are_far_apart(t, hq, d, apart):
+    """The largest columns of a query meet keys of zero: the scores come from columns 2^-apart of them."""
+    g = _gen(apart + d)
+    x = torch.randn(60, 2, d, generator=g, device="cuda")
+    x[:, 0, :3] = 0.0
+    x[:, 0] *= 2.0 ** (apart // 2)
+    store = gs.gs_coded_rows(60, 2, d, 4)
+    gs.gs_coded_write(store, x)
+    indptr, idx = _block([20, 300, 16, 1], 60, g)
+    q = torch.randn(4, hq, d, generator=g, device="cuda") * 2.0 ** -(apart // 2)
+    q[:, :, :3] *= 2.0 ** apart
+    q[2] = torch.randn(hq, d, generator=g, device="cuda") * 2.0 ** -(apart // 2)      # an ordinary row beside them
+    _compare(indptr, idx, q.to(t), store, 1)
