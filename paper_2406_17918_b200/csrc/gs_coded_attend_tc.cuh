@@ -362,7 +362,7 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
 
     // what a unit keeps: the queries' fragments (lane g, t: slot g / 2, columns t L ...), sums, maxima (lane g, t: slot t)
     uint32_t q[SP][2];
-    float acc[TILES][2], m = 0.f, l = 0.f, qscale = 0.f;
+    float acc[TILES][2], m = 0.f, l = 0.f, qhalf = 0.f, qscale = 0.f;
     bool apart = false;                                      // queries whose elements are too far apart
     int unit = 0;                                            // acc is in units of 2^(unit - 254 - 14)
     const float c2 = P.a.scale * CA_LOG2E;
@@ -423,7 +423,10 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
                 q[i][0] = pack_f16(y[4 * i] * scale, y[4 * i + 1] * scale);
                 q[i][1] = pack_f16(y[4 * i + 2] * scale, y[4 * i + 3] * scale);
             }
-            qscale = __uint_as_float((uint32_t)(254 - __shfl_sync(FULL, up, 8 * t)) << 23) * c2;
+            // back by two halves, around the key's scale: a large key and a small query do not pass the range of f32 between them
+            const int back = 127 - __shfl_sync(FULL, up, 8 * t);
+            qhalf = power_of(back >> 1);
+            qscale = power_of(back - (back >> 1)) * c2;
         }
         // ---- scores
         uint32_t k0[SP], k1[SP];
@@ -435,7 +438,7 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
         // ---- weights of slot t and the edges g and g + 8
         const uint32_t kb0 = __shfl_sync(FULL, x.scales, g), kb1 = __shfl_sync(FULL, x.scales, g + 8);
         const uint32_t vb0 = __shfl_sync(FULL, x.scales, g + 16), vb1 = __shfl_sync(FULL, x.scales, g + 24);
-        const float s0 = x.on >> g & 1 ? c[0] * scale_of(kb0) * qscale : -INFINITY, s1 = x.on >> (g + 8) & 1 ? c[2] * scale_of(kb1) * qscale : -INFINITY;
+        const float s0 = x.on >> g & 1 ? c[0] * qhalf * scale_of(kb0) * qscale : -INFINITY, s1 = x.on >> (g + 8) & 1 ? c[2] * qhalf * scale_of(kb1) * qscale : -INFINITY;
         float top = fmaxf(s0, s1);
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));

@@ -1,6 +1,6 @@
-"""Attention over 8-bit rows where the results hang on edges of little weight: beside a sink without a value, in columns that the heavy
-edges leave at zero, with scores from columns far below a query's largest.  Definition, bounds and helpers are those of the attention's
-other tests; every bound is relative to what the element itself sums up, so none is met by leaving small weights out."""
+"""Attention over 8-bit rows where the results hang on little: edges beside a sink without a value, columns that the heavy edges leave at
+zero, scores from columns far below a query's largest, keys and queries whose sizes cancel.  Definition, bounds and helpers are those of
+the attention's other tests; every bound is relative to what the element itself sums up, so none is met by leaving small things out."""
 import pytest
 import torch
 
@@ -76,4 +76,18 @@ def test_queries_whose_columns_are_far_apart(t, hq, d, apart):
     q = torch.randn(4, hq, d, generator=g, device="cuda") * 2.0 ** -(apart // 2)
     q[:, :, :3] *= 2.0 ** apart
     q[2] = torch.randn(hq, d, generator=g, device="cuda") * 2.0 ** -(apart // 2)      # an ordinary row beside them
+    _compare(indptr, idx, q.to(t), store, 1)
+
+
+@pytest.mark.parametrize("t,hq,d", SHAPES)
+@pytest.mark.parametrize("power", [-115, -100, 100, 110])
+def test_keys_and_queries_of_opposite_sizes(t, hq, d, power):
+    """Keys of 2^power and queries of 2^-power: scores of ordinary size."""
+    g = _gen(power + d)
+    x = torch.randn(60, 2, d, generator=g, device="cuda").clamp(-4, 4)
+    x[:, 0] *= 2.0 ** power
+    store = gs.gs_coded_rows(60, 2, d, 4)
+    gs.gs_coded_write(store, x)
+    indptr, idx = _block([20, 300, 16, 1], 60, g)
+    q = torch.randn(4, hq, d, generator=g, device="cuda") * 2.0 ** -power
     _compare(indptr, idx, q.to(t), store, 1)
