@@ -592,7 +592,7 @@ gs_status gs_rms_norm_backward(const void* d_hidden, int64_t hidden_ld, const vo
  *                   outside the store is skipped; of the positions with one id the last counts.  Where other rows of a block
  *                   stay, its scale does not fall, and their codes are requantised if it rises (exact, but for values that
  *                   fall below 2^-6 of it); a block whose rows are all written starts afresh.  The bytes between head_dim and pitch
- *                   are written as zeros.  d_claims (only with d_ids): int32[rows + (block > 1 ? 2 * ceil(rows / block) + 2 : 0)],
+ *                   are written as zeros, and nothing reads them.  d_claims (only with d_ids): int32[rows + (block > 1 ? 2 * ceil(rows / block) + 2 : 0)],
  *                   the caller's, all -1 before the first call and after each; calls that share it do not overlap.
  *   gs_coded_read   out[p] = row d_ids[p], or first + p; an id outside the store gives zeros.
  * d_count_or_null, count_bound: as for gs_gather_features. */

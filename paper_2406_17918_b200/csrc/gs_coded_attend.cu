@@ -202,7 +202,7 @@ template <typename T, int VE, int G, int U, int MODE> __global__ void __launch_b
     const int64_t step = (int64_t)gridDim.x * (CA_THREADS / 32) * per_warp;
     const float c2 = P.a.scale * CA_LOG2E;
     const int D = P.a.head_dim, c0 = t * VE, group = P.a.q_heads / P.a.kv_heads;
-    const int held = c0 < P.a.k.pitch ? VE : 0;              // this lane has a piece of the codes
+    const int held = min(VE, max(D - c0, 0));                // this lane's codes; what lies behind head_dim is not read
     const uint32_t kstep = (uint32_t)P.a.k.row_stride, vstep = (uint32_t)P.a.v.row_stride, ksstep = (uint32_t)P.a.k.scale_stride, vsstep = (uint32_t)P.a.v.scale_stride;
     unsigned char* mine = ca_smem + (threadIdx.x >> 5) * 2 * SLOT + lane * VE;
     const uint32_t mine_a = (uint32_t)__cvta_generic_to_shared(mine);

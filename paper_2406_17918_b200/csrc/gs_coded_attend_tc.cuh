@@ -309,11 +309,12 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 
             const int edge = PIECES > 8 ? (i >> 1) * edges_per + edge0 : i * edges_per + edge0, piece = PIECES > 8 ? piece0 + (i & 1) * 8 : piece0;
             const int from = __shfl_sync(FULL, mine_at, edge & 15), sub = piece * 16;
             if (edge >= 16) continue;                        // fewer pieces than lanes
-            const bool has = (x.on >> edge & 1) && sub < pitch;
+            const bool has = (x.on >> edge & 1) && sub < D;
+            const int bytes = has ? min(16, D - sub) : 0;    // what lies behind head_dim is not read
             const uint64_t row = has ? (uint32_t)from : 0u;
             const uint32_t to = base + tile_byte(edge, piece * 16), in = has ? kv0 * pitch + sub : 0;
-            copy_async<16>(to, P.a.k.codes + row * kstep + in, has ? 16 : 0);
-            copy_async<16>(to + S::TILE, P.a.v.codes + row * vstep + in, has ? 16 : 0);
+            copy_async<16>(to, P.a.k.codes + row * kstep + in, bytes);
+            copy_async<16>(to + S::TILE, P.a.v.codes + row * vstep + in, bytes);
         }
         if (x.first && P.wide) {
             for (int i = lane; i < SLOTS * SP * 2; i += 32) {

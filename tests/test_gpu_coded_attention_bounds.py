@@ -26,3 +26,20 @@ def test_rows_that_ask_for_more_chunks_than_32_bits_count(t, hq):
     listed = out[::2][(out[::2] != 5).flatten(1).any(1)]
     one, _ = gs.gs_coded_attention_forward(indptr[:2], idx, q[:1], store.heads(0, 1), store.heads(1, 2), _ws(1, edges, hq, 8))
     assert len(listed) == 9 and int((listed == one).flatten(1).all(1).sum()) == 8       # the ninth has one place for its many chunks
+
+
+@pytest.mark.parametrize("t,hq", [(F, 1), (F, 2), (F, 4), (B, 1), (B, 2), (B, 4)])
+@pytest.mark.parametrize("d", [1, 7, 8, 24, 33, 100, 130, 250])
+def test_bytes_behind_the_columns_have_no_part(t, hq, d):
+    """A store that other code has filled may hold anything between head_dim and the pitch, NaN codes among it."""
+    g = _gen(d)
+    store = _store(50, 4, d, 4, g)
+    lengths = [0, 300, 5, 20, 17]
+    indptr = torch.tensor([0] + lengths, device="cuda").cumsum(0).int()
+    idx = torch.randint(0, 50, (sum(lengths),), generator=g, device="cuda", dtype=torch.int32)
+    q = torch.randn(5, 2 * hq, d, generator=g, device="cuda").to(t)
+    args = (indptr, idx, q, store.heads(0, 2), store.heads(2, 4), _ws(5, idx.numel(), 2 * hq, d))
+    out, lse = gs.gs_coded_attention_forward(*args)
+    store.codes.view(torch.uint8)[:, :, d:] = 0x7F
+    again, alse = gs.gs_coded_attention_forward(*args)
+    assert torch.isfinite(out).all() and torch.equal(out, again) and torch.equal(lse, alse)
