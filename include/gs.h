@@ -557,14 +557,15 @@ gs_status gs_xent_backward(const void* d_hidden, int64_t hidden_ld, const void* 
 
 /* Root-mean-square norm of rows [rows][dim], 1 <= dim <= 8192, with the addition of a residual before it:
  *   h = x + residual, rounded to `dtype` (h = x without a residual);  out = weight h / sqrt(mean(h^2) + eps)
- * d_weight_or_null [dim] of weight_dtype (NULL: ones); eps >= 0.  d_hidden_or_null receives h, which the backward pass takes; it may
- * be the array of x or of the residual, and d_out that of x, at the same pitch.  d_count_or_null: as for gs_gather_features;
+ * d_weight_or_null [dim] of weight_dtype (NULL: ones); eps >= 0.  d_hidden_or_null receives h, which the backward pass takes.  Each of
+ * d_hidden_or_null and d_out may be the array of x or of the residual, at the same pitch, but not both the same one; other overlaps
+ * are errors.  d_count_or_null: as for gs_gather_features;
  * rows behind the count are left as they are.
  * gs_rms_norm_coded writes the result in 8 bits instead (gs_coded below): row p to row p of `out`, which has scales of its own for
  * every row (block 1) and heads * head_dim == dim: a scale per group of head_dim columns.
  * gs_rms_norm_backward takes h, the gradient dout of out and, if h is used elsewhere, the gradient dhidden that arrives there:
  *   dx = dhidden + the gradient through the norm (it is the residual's gradient too);  dweight[c] = sum over rows, or NULL
- * dx may be the array of dhidden or of dout.  Workspace: gs_rms_norm_workspace_bytes. */
+ * dx may be the array of h, dhidden or dout, at the same pitch; other overlaps are errors.  Workspace: gs_rms_norm_workspace_bytes. */
 typedef struct {
     void* d_codes;            /* [rows][row_stride] e4m3, head h from byte h * pitch on, pitch = head_dim rounded up to 16 */
     uint8_t* d_scales;        /* [ceil(rows / block)][scale_stride], head h's at h */

@@ -1023,7 +1023,7 @@ def _norm_inputs(x, weight, residual, hidden, stream, count):
 def gs_rms_norm_forward(x: torch.Tensor, weight: torch.Tensor = None, residual: torch.Tensor = None, eps: float = 1e-6, out: torch.Tensor = None,
                         hidden: torch.Tensor = None, count: torch.Tensor = None, stream=None):
     """h = x + residual; out = weight * h / sqrt(mean(h^2) + eps), row by row.  Returns (out, h); h is x itself without a residual.
-    `hidden` (h) may be x or residual, `out` may be x.  `count`: a 0-d int32 CUDA tensor with the number of rows (x is then the
+    `hidden` (h) and `out` may each be x or residual, but not both the same.  `count`: a 0-d int32 CUDA tensor with the number of rows (x is then the
     bound; rows behind it are zeros, or left as they are in given arrays)."""
     hidden, (w, wt) = _norm_inputs(x, weight, residual, hidden, stream, count)
     out = _new_like(x, stream, None if count is None else 0) if out is None else _norm_rows(out, "out", x)
@@ -1048,7 +1048,7 @@ def gs_rms_norm_coded(x: torch.Tensor, out: "CodedRows", weight: torch.Tensor = 
 def gs_rms_norm_backward(hidden: torch.Tensor, dout: torch.Tensor, workspace: torch.Tensor, weight: torch.Tensor = None, dhidden: torch.Tensor = None,
                          eps: float = 1e-6, dx: torch.Tensor = None, dweight: torch.Tensor = None, count: torch.Tensor = None, stream=None):
     """Gradients of gs_rms_norm_forward for what it normalised.  `dhidden`: the gradient that arrives at h itself.  Returns (dx,
-    dweight); dx is the residual's gradient too, dweight None without a weight.  `dx` may be dhidden or dout."""
+    dweight); dx is the residual's gradient too, dweight None without a weight.  `dx` may be hidden, dhidden or dout."""
     _rows_2d(hidden, "hidden")
     _norm_rows(dout, "dout", hidden)
     if dhidden is not None:

@@ -9,6 +9,24 @@ using namespace gs;
 
 namespace {
 
+// Rows [rows][dim] in memory; data NULL: no such operand.
+struct RowSpan {
+    const void* data;
+    int64_t ld;
+};
+
+// Whether two of them have elements in common.  Rows of one pitch may lie beside one another; of two pitches they are taken to meet
+// where their ranges do.
+bool rows_meet(RowSpan a, RowSpan b, int64_t rows, int64_t dim, size_t size) {
+    if (!a.data || !b.data) return false;
+    if (rows == 1) a.ld = b.ld = dim;
+    const uint64_t begin_a = (uint64_t)a.data, begin_b = (uint64_t)b.data, width = (uint64_t)dim * size, last = (uint64_t)rows - 1;
+    if (begin_a + last * (uint64_t)a.ld * size + width <= begin_b || begin_b + last * (uint64_t)b.ld * size + width <= begin_a) return false;
+    if (a.ld != b.ld) return true;
+    const uint64_t pitch = (uint64_t)a.ld * size, off = (begin_a < begin_b ? begin_b - begin_a : begin_a - begin_b) % pitch;
+    return off < width || pitch - off < width;
+}
+
 gs_status check_norm(const RmsNorm& p, bool backward) {
     if (!known(p.dtype) || (p.weight && !known(p.weight_dtype))) return set_error(GS_ERR_ARG, "unknown dtype");
     if (p.n.bound < 0) return set_error(GS_ERR_ARG, "rows is negative");
@@ -23,6 +41,15 @@ gs_status check_norm(const RmsNorm& p, bool backward) {
     if (!aligned_to(p.x, size) || !aligned_to(p.residual, size) || !aligned_to(p.hidden, size) || !aligned_to(p.out, size) || !aligned_to(p.dout, size) ||
         (p.weight && !aligned_to(p.weight, size_of(p.weight_dtype))) || (p.dweight && !aligned_to(p.dweight, size_of(p.weight_dtype))) || !aligned_to(p.n.d_n, 4))
         return set_error(GS_ERR_ALIGN, "misaligned argument");
+    if (p.n.bound > 0) {
+        // a row is written by the threads that have read it: a result may be an operand's array, but lie across none
+        const RowSpan results[] = {{p.hidden, p.hidden_ld}, {p.out, p.out_ld}}, operands[] = {{p.x, p.x_ld}, {p.residual, p.residual_ld}, {p.dout, p.dout_ld}};
+        if (rows_meet(results[0], results[1], p.n.bound, p.dim, size)) return set_error(GS_ERR_ARG, "hidden and out overlap");
+        for (const RowSpan& r : results)
+            for (const RowSpan& o : operands)
+                if (rows_meet(r, o, p.n.bound, p.dim, size) && (r.data != o.data || (p.n.bound > 1 && r.ld != o.ld)))
+                    return set_error(GS_ERR_ARG, "a result overlaps an operand without being its array");
+    }
     return GS_OK;
 }
 
