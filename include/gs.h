@@ -588,7 +588,7 @@ gs_status gs_rms_norm_backward(const void* d_hidden, int64_t hidden_ld, const vo
  * (4 exponent and 3 mantissa bits, largest 448, no infinities), scale a byte for each block of `block` consecutive rows (a power of
  * two, 1 to 64) and head.  A block's scale is the smallest with |x| <= 448 * 2^(scale - 127) for the finite values written to
  * it; infinities and NaN become NaN.  Storage that holds zeros is a valid store of zero rows.  d_codes is aligned to 16 bytes,
- * row_stride a multiple of 16 and at least heads * pitch; a range of heads of a store is a store (d_codes + h * pitch, d_scales + h).
+ * row_stride a multiple of 16 and at least heads * pitch, which is below 2^30; a range of heads of a store is a store (d_codes + h * pitch, d_scales + h).
  *   gs_coded_write  rows[p] (gs_heads of `dtype`, strides in elements) goes to row d_ids[p], or first + p if d_ids is NULL.  An id
  *                   outside the store is skipped; of the positions with one id the last counts.  Where other rows of a block
  *                   stay, its scale does not fall, and their codes are requantised if it rises (exact, but for values that

@@ -59,6 +59,7 @@ gs_status check_coded(const char* name, const gs_coded* c, CodedView* out) {
     if (c->heads < 1 || c->heads > (1 << 16) || c->head_dim < 1 || c->head_dim > (1 << 16)) return set_error(GS_ERR_ARG, "%s: heads or head_dim outside [1, 2^16]", name);
     if (c->block < 1 || c->block > 64 || (c->block & (c->block - 1))) return set_error(GS_ERR_ARG, "%s: block %d is not a power of two from 1 to 64", name, c->block);
     const int32_t pitch = (c->head_dim + 15) / 16 * 16;
+    if ((int64_t)c->heads * pitch >= ((int64_t)1 << 30)) return set_error(GS_ERR_ARG, "%s: a row has 2^30 bytes or more", name);
     if (c->rows > 0 && (!c->d_codes || !c->d_scales)) return set_error(GS_ERR_ARG, "%s has no arrays", name);
     if (c->row_stride % 16 || (c->rows > 1 && c->row_stride < (int64_t)c->heads * pitch)) return set_error(GS_ERR_ARG, "%s: row_stride is no multiple of 16, or too small", name);
     if (c->rows > c->block && c->scale_stride < c->heads) return set_error(GS_ERR_ARG, "%s: scale_stride is too small", name);

@@ -54,13 +54,27 @@ def test_gradient_across_operands(L):
         call(array, ld=D + 4)
 
 
-def test_norm_in_eight_bits(L):
-    class Coded(ctypes.Structure):
-        _fields_ = [("codes", vp), ("scales", vp), ("rows", i64), ("row_stride", i64), ("scale_stride", i64), ("heads", i32), ("head_dim", i32), ("block", i32)]
+class Coded(ctypes.Structure):
+    _fields_ = [("codes", vp), ("scales", vp), ("rows", i64), ("row_stride", i64), ("scale_stride", i64), ("heads", i32), ("head_dim", i32), ("block", i32)]
 
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", vp), ("row", i64), ("head", i64)]
+
+
+def test_norm_in_eight_bits(L):
     c = Coded(0x90000, 0xA0000, N, 16, 1, 1, D, 1)
     assert L.gs_rms_norm_coded(vp(X), i64(D), vp(R), i64(D), 0, None, 0, None, i32(N), i32(D), f32(1e-6), vp(X + 4), i64(D), ctypes.byref(c), None) == 1
     assert b"overlap" in L.gs_last_error()
+
+
+@pytest.mark.parametrize("heads,dim", [(1 << 16, 1 << 16), (1 << 16, 32769), (1 << 14, 1 << 16), (1 << 16, 16369)])
+def test_rows_in_eight_bits_of_2_30_bytes(L, heads, dim):
+    """A lane counts a row's pieces in 32 bits."""
+    c = Coded(0x90000, 0xA0000, 1, 0, 0, heads, dim, 1)
+    a = Heads(0x100000, 0, dim)
+    assert L.gs_coded_read(ctypes.byref(c), None, i64(0), None, i32(0), 1, ctypes.byref(a), None) == 1 and b"2^30" in L.gs_last_error()
+    assert L.gs_coded_write(ctypes.byref(c), 1, ctypes.byref(a), None, i64(0), None, i32(0), None, None) == 1 and b"2^30" in L.gs_last_error()
 
 
 def test_nothing_was_launched(L):
