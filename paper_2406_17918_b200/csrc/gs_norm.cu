@@ -11,8 +11,9 @@
 // Measured (reads and writes of both sides, of a copy's 6.56 TB/s): 2.03 M x 64 bf16 forward 159 us = 0.99, backward 177 = 0.90; 30,000 x 2,000
 // f32 156 and 157 = 0.93; 100,000 x 513 f32 (rows that begin anywhere) 164 and 231 = 0.76 and 0.54; 4,096 x 1,433 12 and 26: the latency of
 // a row's sums in a block.  Two rows of a block in flight: 15 and 31.
-// dw: a group keeps its columns' sums over all of its rows; blocks leave theirs in the workspace and a second kernel adds them in
-// order.
+// dw: a group keeps its columns' sums over NM_SUMMED rows and joins them to those before in 64 bits (2.03 M x 128: 3.8e-7 off without
+// that, 1.2e-7 with it, for 353 -> 364 us); a block with a row to itself keeps them over all of its rows.  Blocks leave theirs in the
+// workspace, and a second kernel adds them in order, in 64 bits.
 // Results in 8 bits: the largest magnitude of a group of columns is found among the lanes that hold it, by shuffles where the
 // group's pieces are a power of two and by integer maxima in shared memory otherwise.
 #include <type_traits>
@@ -23,6 +24,7 @@
 
 namespace gs {
 
+constexpr int NM_SUMMED = 32;        // rows that a lane adds dw of in 32 bits before the sum is joined to the others in 64
 constexpr int NM_THREADS = 256;      // of the kernels whose rows are held by lanes of a warp
 
 __device__ __forceinline__ int norm_rows(const Count& c) {
@@ -330,8 +332,7 @@ __global__ void __launch_bounds__(BLOCK ? 512 : NM_THREADS) k_norm_forward(const
 // dw_part: [blocks][dim] sums of the rows a block took.
 template <typename T, int VE, int NV, int U, bool BLOCK, bool EDGE>
 __global__ void __launch_bounds__(BLOCK ? 512 : NM_THREADS, BLOCK ? 1 : (VE * NV <= 8 ? 3 : 2)) k_norm_backward(const __grid_constant__ RmsNorm P, float* dw_part) {
-    constexpr int E = VE * NV;
-    extern __shared__ float norm_dw[];                       // groups: [warps][dim]
+    extern __shared__ double norm_dw[];                      // groups: [warps][dim], each lane its columns
     chain_wait();
     const int n = norm_rows(P.n), D = P.dim;
     const int width = BLOCK ? (int)blockDim.x : P.tl, t = BLOCK ? (int)threadIdx.x : (int)threadIdx.x & (P.tl - 1), own = BLOCK ? 0 : threadIdx.x / width;
@@ -357,7 +358,45 @@ __global__ void __launch_bounds__(BLOCK ? 512 : NM_THREADS, BLOCK ? 1 : (VE * NV
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < EL<VE>; ++i) dw[j][i] = v_all<VE>(0.f);
+    bool left = false;
+    // adds the columns' sums to what is kept of them: those of a warp's groups, in 64 bits, to its lanes' own in shared memory; a block's
+    // rows are few, and its threads put their sums into the workspace once
+    auto leave = [&]() {
+        int at = t;
+        asm volatile("" : "+r"(at));                         // addresses are made here, not kept over the rows
+        float* part = dw_part + (int64_t)blockIdx.x * D;
+        double* mine = norm_dw + (threadIdx.x >> 5) * D;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float x[VE];
+            v_unpack<VE>(dw[j], x);
+#pragma unroll
+            for (int i = 0; i < EL<VE>; ++i) dw[j][i] = v_all<VE>(0.f);
+            if constexpr (!BLOCK) {
+                for (int o = width; o < 32; o <<= 1) {       // the groups of a warp
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) x[i] += __shfl_xor_sync(FULL, x[i], o);
+                }
+                if ((int)(threadIdx.x & 31) >= width) continue;
+            }
+            const int c0 = (at + j * width) * VE - C.phase;
+#pragma unroll
+            for (int i = 0; i < VE; ++i) {
+                const int c = c0 + i;
+                if (c < 0 || c >= D) continue;
+                if constexpr (BLOCK) part[c] = x[i];
+                else mine[c] = (left ? mine[c] : 0.0) + x[i];
+            }
+        }
+        left = true;
+    };
+    int rows_added = 0;
     for (int64_t base = C.blk * per_block * U; base < C.n; base += step) {
+        if constexpr (!BLOCK)
+            if ((rows_added += U) > NM_SUMMED && P.dweight) {
+                leave();
+                rows_added = U;
+            }
         RowPart<T, VE, NV, EDGE> hc[U], dyc[U], dhc[U];
         float sum[2 * U];                                    // sum h^2, sum g h
 #pragma unroll
@@ -411,54 +450,25 @@ __global__ void __launch_bounds__(BLOCK ? 512 : NM_THREADS, BLOCK ? 1 : (VE * NV
         }
     }
     if (!P.dweight) return;
-    float sums[E];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        float x[VE];
-        v_unpack<VE>(dw[j], x);
-#pragma unroll
-        for (int i = 0; i < VE; ++i) sums[j * VE + i] = x[i];
-    }
-    float* part = dw_part + (int64_t)blockIdx.x * D;
-    if constexpr (BLOCK) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < VE; ++i) {
-                const int c = (t + j * width) * VE + i - C.phase;
-                if (c >= 0 && c < D) part[c] = sums[j * VE + i];
-            }
-    } else {
-        for (int o = width; o < 32; o <<= 1) {               // the groups of a warp
-#pragma unroll
-            for (int i = 0; i < E; ++i) sums[i] += __shfl_xor_sync(FULL, sums[i], o);
-        }
-        if ((threadIdx.x & 31) < width) {
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int i = 0; i < VE; ++i) {
-                    const int c = (t + j * width) * VE + i - C.phase;
-                    if (c >= 0 && c < D) norm_dw[(threadIdx.x >> 5) * D + c] = sums[j * VE + i];
-                }
-        }
+    leave();
+    if constexpr (!BLOCK) {
         __syncthreads();
         for (int c = threadIdx.x; c < D; c += NM_THREADS) {
-            float s = 0.f;
+            double s = 0.0;
             for (int i = 0; i < NM_THREADS / 32; ++i) s += norm_dw[i * D + c];
-            part[c] = s;
+            dw_part[(int64_t)blockIdx.x * D + c] = (float)s;
         }
     }
 }
 
 // dw = the blocks' sums, added in order: 32 columns per block, its warps over contiguous shares of the blocks.
 __global__ void __launch_bounds__(1024) k_norm_dweight(const float* __restrict__ part, int parts, int dim, void* dweight, gs_dtype dtype) {
-    __shared__ float s[32][33];
+    __shared__ double s[32][33];
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = (parts + 31) / 32;
     for (int c0 = blockIdx.x * 32; c0 < dim; c0 += gridDim.x * 32) {
         const int c = c0 + lane, p1 = (warp + 1) * per < parts ? (warp + 1) * per : parts;
-        float x = 0.f;
+        double x = 0.0;
         if (c < dim) {
 #pragma unroll 8
             for (int p = warp * per; p < p1; ++p) x += __ldcg(part + (int64_t)p * dim + c);
@@ -467,10 +477,10 @@ __global__ void __launch_bounds__(1024) k_norm_dweight(const float* __restrict__
         s[warp][lane] = x;
         __syncthreads();
         if (warp == 0 && c < dim) {
-            x = 0.f;
+            x = 0.0;
             for (int i = 0; i < 32; ++i) x += s[i][lane];
-            if (dtype == GS_BF16) static_cast<bf16*>(dweight)[c] = __float2bfloat16_rn(x);
-            else static_cast<float*>(dweight)[c] = x;
+            if (dtype == GS_BF16) static_cast<bf16*>(dweight)[c] = __float2bfloat16_rn((float)x);
+            else static_cast<float*>(dweight)[c] = (float)x;
         }
     }
 }
@@ -607,7 +617,7 @@ cudaError_t launch_norm_backward(const RmsNorm& p, void* workspace, cudaStream_t
         P.inv_dim = 1.f / (float)p.dim;
         P.phase = l.phase;
         const int threads = B ? tl : NM_THREADS, held = (B ? 1 : NM_THREADS / tl) * U;
-        const size_t smem = B ? 0 : (size_t)(NM_THREADS / 32) * p.dim * 4;
+        const size_t smem = B ? 0 : (size_t)(NM_THREADS / 32) * p.dim * sizeof(double);
         // as many blocks as are resident: each leaves its columns' sums once
         static std::atomic<uint64_t> known{0};
         auto kernel = k_norm_backward<T, VE, NV, U, B, EDGE>;
