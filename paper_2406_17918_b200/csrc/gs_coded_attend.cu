@@ -518,14 +518,14 @@ static void set_units(CodedAttend& P, int heads) {
         if (P.units_per_row == 1 << i) P.unit_shift = i;
 }
 static int64_t chunk_bound(const CodedAttend& P) { return P.most; }
-// Chunks that keep sixteen warps on every SM busy once, so that no warp has a second one while others have none, and the join little
+// Chunks that keep the warps that are resident busy once, so that no warp has a second one while others have none, and the join little
 // to do (one row of 200,011 edges, 2 x 4 heads of 64: 38 us, with chunks of 128 46).
-static int chunk_length(const CodedAttend& P, int heads) {
-    const int64_t n = ((int64_t)P.a.edge_bound * (P.a.q_heads / heads) / (sm_count() * 16) + 31) / 32 * 32;
+static int chunk_length(const CodedAttend& P, int heads, int64_t warps) {
+    const int64_t n = ((int64_t)P.a.edge_bound * (P.a.q_heads / heads) / warps + 31) / 32 * 32;
     return n < CA_CHUNK ? CA_CHUNK : (n > CA_CHUNK_MOST ? CA_CHUNK_MOST : (int)n);
 }
 
-// One element at a time per lane: rows of up to CA_LONG edges, or chunks.
+// Edges by groups of lanes: rows of up to CA_LONG edges, or chunks.
 template <typename T, int VE, int G> static cudaError_t run_coded(CodedAttend P, int chunk_mode, cudaStream_t s) {
     constexpr int U = 4;
     const int pieces = P.a.k.pitch / VE;
@@ -534,7 +534,6 @@ template <typename T, int VE, int G> static cudaError_t run_coded(CodedAttend P,
     set_units(P, G);
     constexpr int smem = CA_THREADS / 32 * 2 * U * 2 * VE * 32;
     P.chunk_mode = chunk_mode;
-    P.chunk = chunk_length(P, G);
     const int64_t n = chunk_mode ? chunk_bound(P) : P.a.dst.bound;
     P.slots = chunk_mode ? 32 / P.tl : 1;
     // groups share a row while the rows alone do not give every SM sixteen warps and each keeps U edges
@@ -544,52 +543,80 @@ template <typename T, int VE, int G> static cudaError_t run_coded(CodedAttend P,
     int64_t grid = (n * P.units_per_row + per_block - 1) / per_block;
     const int64_t cap = sm_count() * 16;
     if (grid > cap) grid = cap;
-    if (chunk_mode) return launch_train(k_coded_attend<T, VE, G, U, CA_CHUNKS>, grid, CA_THREADS, smem, s, P);
+    if constexpr (!(std::is_same<T, bf16>::value && G == 4))       // those chunks go to the tensor cores
+        if (chunk_mode) return launch_train(k_coded_attend<T, VE, G, U, CA_CHUNKS>, grid, CA_THREADS, smem, s, P);
     return P.split ? launch_train(k_coded_attend<T, VE, G, U, CA_LIST>, grid, CA_THREADS, smem, s, P)
                    : launch_train(k_coded_attend<T, VE, G, U, CA_ALL>, grid, CA_THREADS, smem, s, P);
 }
-template <typename T> static cudaError_t coded_lanes(const CodedAttend& P, int chunk_mode, cudaStream_t s) {
+// Query heads that share a key/value head are taken together; what a lane holds of them stays within its registers.
+static int lane_heads(const CodedAttend& P) {
     const int group = P.a.q_heads / P.a.kv_heads;
-    // query heads that share a key/value head are taken together; what a lane holds of them stays within its registers
-    if (group % 4 == 0) return run_coded<T, 8, 4>(P, chunk_mode, s);
-    if (group % 2 == 0) return run_coded<T, 8, 2>(P, chunk_mode, s);
+    return group % 4 == 0 ? 4 : (group % 2 == 0 ? 2 : 1);
+}
+template <typename T> static cudaError_t coded_lanes(const CodedAttend& P, int chunk_mode, cudaStream_t s) {
+    const int heads = lane_heads(P);
+    if (heads == 4) return run_coded<T, 8, 4>(P, chunk_mode, s);
+    if (heads == 2) return run_coded<T, 8, 2>(P, chunk_mode, s);
     return run_coded<T, 16, 1>(P, chunk_mode, s);
 }
 
-// On the tensor cores.
-template <int SP> static cudaError_t run_tc(CodedAttend P, int chunk_mode, cudaStream_t s) {
+// On the tensor cores.  warps: what is resident on the device.
+template <int SP> static cudaError_t tensor_warps(int64_t& warps) {
+    static std::atomic<uint64_t> allowed{0}, known{0};
+    const cudaError_t e = allow_smem(k_coded_attend_tc<SP>, TcShape<SP>::SMEM, allowed);
+    if (e == cudaSuccess) warps = (int64_t)sm_count() * resident_blocks(k_coded_attend_tc<SP>, TC_WARPS * 32, TcShape<SP>::SMEM, known) * TC_WARPS;
+    return e;
+}
+template <int SP> static cudaError_t run_tc(CodedAttend P, int chunk_mode, int64_t warps, cudaStream_t s) {
     using S = TcShape<SP>;
-    auto kernel = k_coded_attend_tc<SP>;
-    static std::atomic<uint64_t> allowed{0};
-    const cudaError_t e = allow_smem(kernel, S::SMEM, allowed);
-    if (e != cudaSuccess) return e;
     set_units(P, S::SLOTS);
     P.chunk_mode = chunk_mode;
-    P.chunk = chunk_length(P, S::SLOTS);
     const int64_t n = chunk_mode ? chunk_bound(P) : P.a.dst.bound;
     int64_t grid = (n * P.units_per_row + TC_WARPS - 1) / TC_WARPS;
-    const int64_t cap = sm_count() * 4;                      // what is resident
-    if (grid > cap) grid = cap;
-    return launch_train(kernel, grid, TC_WARPS * 32, S::SMEM, s, P);
+    if (grid > warps / TC_WARPS) grid = warps / TC_WARPS;
+    return launch_train(k_coded_attend_tc<SP>, grid, TC_WARPS * 32, S::SMEM, s, P);
 }
-static cudaError_t coded_tensor(const CodedAttend& P, int chunk_mode, cudaStream_t s) {
+// Where the rows of a block go whose heads share by fours (chunks always go to the tensor cores).  A tile costs the same however few
+// edges it has, and little less for narrow heads than for wide ones; but two rounds of the resident warps, or one, are sooner done with
+// than the lanes' longer work on a row.  Tensor cores : lanes, us, 2 x 4 heads, rows of as many edges on average, by columns:
+//          many rows (20,000 to 200,000)                        64 rows of 4    2,000 of 4    2,000 of 15
+//   16     3: 426 : 100    24: 229 : 135    48: 184 : 129        8.2 : 10.2      10 : 10       12 : 18
+//   32     3: 453 : 201    18: 152 : 139    24: 127 : 141        8.2 : 10.2      12 : 12       14 : 23
+//   64     3: 408 : 311     6: 209 : 217     9: 141 : 182        8.2 : 12.3      12 : 20       14 : 29
+//   128    3: 461 : 317     6: 236 : 219     9: 162 : 184       10.2 : 12.3      18 : 23       23 : 39
+//   256    3: 606 : 324     9: 338 : 307    12: 340 : 367       10.3 : 14.3      45 : 33       53 : 59
+static bool rows_to_tensor_cores(const CodedAttend& P, int64_t warps) {
+    if ((int64_t)P.a.dst.bound * (P.a.q_heads / 4) <= 2 * warps) return true;
+    int64_t edges = P.a.edge_bound / P.a.dst.bound;          // of a row
+    if (P.a.max_row > 0 && edges > P.a.max_row) edges = P.a.max_row;
     const int pieces = P.a.k.pitch / 16;
-    if (pieces <= 1) return run_tc<1>(P, chunk_mode, s);
-    if (pieces <= 2) return run_tc<2>(P, chunk_mode, s);
-    if (pieces <= 4) return run_tc<4>(P, chunk_mode, s);
-    if (pieces <= 8) return run_tc<8>(P, chunk_mode, s);
-    return run_tc<16>(P, chunk_mode, s);
+    return pieces > 1 && edges >= (pieces <= 2 ? 20 : (pieces <= 4 ? 5 : (pieces <= 8 ? 7 : 10)));
+}
+template <int SP> static cudaError_t run_shared(CodedAttend P, cudaStream_t s) {
+    int64_t warps = 0;
+    cudaError_t e = tensor_warps<SP>(warps);
+    if (e != cudaSuccess) return e;
+    P.chunk = chunk_length(P, 4, warps);
+    e = rows_to_tensor_cores(P, warps) ? run_tc<SP>(P, 0, warps, s) : coded_lanes<bf16>(P, 0, s);
+    return P.split && e == cudaSuccess ? run_tc<SP>(P, 1, warps, s) : e;
+}
+template <typename T> static cudaError_t run_parts(CodedAttend P, cudaStream_t s) {
+    if constexpr (std::is_same<T, bf16>::value)
+        if (lane_heads(P) == 4) {
+            const int pieces = P.a.k.pitch / 16;
+            if (pieces <= 1) return run_shared<1>(P, s);
+            if (pieces <= 2) return run_shared<2>(P, s);
+            if (pieces <= 4) return run_shared<4>(P, s);
+            if (pieces <= 8) return run_shared<8>(P, s);
+            return run_shared<16>(P, s);
+        }
+    P.chunk = chunk_length(P, lane_heads(P), sm_count() * 16);
+    const cudaError_t e = coded_lanes<T>(P, 0, s);
+    return P.split && e == cudaSuccess ? coded_lanes<T>(P, 1, s) : e;
 }
 template <typename T> static cudaError_t run_attention(const CodedAttend& P, cudaStream_t s) {
-    auto part = [&](int chunk_mode) {
-        if constexpr (std::is_same<T, bf16>::value)
-            if (P.a.q_heads / P.a.kv_heads % 4 == 0) return coded_tensor(P, chunk_mode, s);   // figures of both: at that kernel
-        return coded_lanes<T>(P, chunk_mode, s);
-    };
-    cudaError_t e = part(0);
-    if (P.split && e == cudaSuccess) e = part(1);
-    if (P.split && e == cudaSuccess) e = launch_train(k_coded_attend_join<T>, sm_count() * 2, 1024, 0, s, P);
-    return e;
+    const cudaError_t e = run_parts<T>(P, s);
+    return P.split && e == cudaSuccess ? launch_train(k_coded_attend_join<T>, sm_count() * 2, 1024, 0, s, P) : e;
 }
 
 cudaError_t launch_coded_attention(const CodedAttention& a, void* workspace, cudaStream_t s) {

@@ -11,9 +11,9 @@
 // again by themselves, they and the sums brought up together, in full down to 2^-106 of the largest (what 32 bits hold of an exponential
 // ends at 2^-126).  It takes a score 18 below a row's largest.
 // What bounds it is instructions around the products (ALU 57%, issue slots 64%), not their rate, so the legacy matrix instruction
-// serves.  With fewer shared heads the other kernel needs fewer instructions.  Both measured, this : that (head groups, columns,
-// longest row): 4 x 64, 20 edges 340 : 617 us; 4 x 128, 30 edges 418 : 914; 4 x 64, 64 edges 624 : 1,674; one row of 200,011 edges 41 : 79;
-// but 2 x 32, 20 edges 314 : 258; 1 x 32, 20 edges 527 : 284; 1 x 32, one row of 200,011 edges 44 : 43.
+// serves.  This : the other kernel (2 x 4 heads): one row of 200,011 edges, 64 columns 46 : 112 us, 16 columns 42 : 52; 4,096 rows of up to
+// 300, 64 columns 353 : 519.  Rows of few edges do not fill a tile: which go where, with both sides' figures, is at the dispatch.  With fewer shared heads
+// the other kernel needs fewer instructions (2 of 32 columns, 20 edges 314 : 258; 1 of 32, 20 edges 527 : 284; one row of 200,011 edges 44 : 43).
 //
 // Rows are gathered by cp.async into TC_STAGES buffers of 16 edges a warp, TC_STAGES - 1 tiles ahead; the columns of 32 edges are read
 // one unit (a row's first) and the offsets two units ahead of the gathers.  No block barriers.  16-byte pieces are permuted within
@@ -219,7 +219,7 @@ template <int SP> __device__ __noinline__ void attend_wide_queries(const CodedAt
     }
 }
 
-template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 2 : (SP >= 8 ? 3 : 4)) k_coded_attend_tc(const __grid_constant__ CodedAttend P) {
+template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 1 : (SP >= 8 ? 3 : 4)) k_coded_attend_tc(const __grid_constant__ CodedAttend P) {
     using S = TcShape<SP>;
     constexpr int SLOTS = S::SLOTS, L = 4 * SP, TILES = 2 * SP, PIECES = SP;
     extern __shared__ __align__(16) unsigned char tc_smem[];

@@ -548,17 +548,6 @@ template <typename F> static cudaError_t norm_shape(const RmsNorm& P, const RowL
     return l.edge ? norm_width<float, 4, true>(P, run) : norm_width<float, 4, false>(P, run);
 }
 
-// Resident blocks of a kernel on one SM, looked up once per device.
-template <typename F> static int resident_blocks(F* kernel, int threads, size_t smem, std::atomic<uint64_t>& known) {
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 1;
-    const uint64_t key = ((uint64_t)(dev + 1) << 48) | ((uint64_t)threads << 32) | (smem << 8), have = known.load(std::memory_order_relaxed);
-    if ((have & ~0xFFull) == key) return (int)(have & 0xFF);
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess || n < 1) n = 1;
-    known.store(key | (uint64_t)n, std::memory_order_relaxed);
-    return n;
-}
-
 cudaError_t launch_norm_forward(const RmsNorm& p, bool coded, cudaStream_t s) {
     const int size = p.dtype == GS_BF16 ? 2 : 4;
     RowLayout l{16 / size, 1, -1, false, 0};

@@ -52,6 +52,17 @@ template <typename F> inline cudaError_t allow_smem(F* kernel, int bytes, std::a
     return e;
 }
 
+// Resident blocks of a kernel on one SM, looked up once per device.
+template <typename F> inline int resident_blocks(F* kernel, int threads, size_t smem, std::atomic<uint64_t>& known) {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 1;
+    const uint64_t key = ((uint64_t)(dev + 1) << 48) | ((uint64_t)threads << 32) | (smem << 8), have = known.load(std::memory_order_relaxed);
+    if ((have & ~0xFFull) == key) return (int)(have & 0xFF);
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess || n < 1) n = 1;
+    known.store(key | (uint64_t)n, std::memory_order_relaxed);
+    return n;
+}
+
 // Memory to be cleared: 16-byte pieces (none: nothing) and fewer than 16 bytes behind them.
 struct Fill {
     uint4* p;
