@@ -2,14 +2,14 @@
 //
 // A warp owns one (row, four query heads of one key head: the "slots") at a time and takes its edges 16 at a time.  The codes are
 // e4m3 numbers, exact as f16, and so is a bf16 query once it is scaled by a power of two (one that has an element other than zero 2^31
-// below its largest is found when it is scaled, and its units are done again at the warp's end, element by element in 32 bits):
+// below its largest is found when it is scaled, and its units are done again at the warp's end, edge by edge in 32 bits):
 //   scores:  C[16 edges][slots] += K[16 edges][16 columns] q^T   (m16n8k16, sums in 32 bits; slot t is column 2 t, in lane t of a quad)
 //   values:  acc[slots][columns] += P[slots][16 edges] V[16 edges][8 columns]
 // P is not rounded to f16: a weight is hi + 2^-11 lo, two rows of the matrix, to 2^-23 of itself.  The weights carry their value block's
 // scale; they are held relative to a power of two near the largest weight times scale so far, as 2^14.  f16 ends 2^-38 below that, and
 // yet such weights are the result where the heavier edges' values are zero: a tile that has weights below 2^-26 multiplies those
-// again by themselves, they and the sums brought up together, in full down to 2^-106 of the largest (what 32 bits hold of an exponential
-// ends at 2^-126).  It takes a score 18 below a row's largest.
+// again by themselves, they and the sums brought up together, down to 2^-98 of the largest.  It takes a score 18 below a row's largest.  A unit
+// with lighter weights still (a score 68 below; 32 bits end at 87) is done again at the warp's end, edge by edge in 32 bits.
 // What bounds it is instructions around the products (ALU 57%, issue slots 64%), not their rate, so the legacy matrix instruction
 // serves.  This : the other kernel (2 x 4 heads): one row of 200,011 edges, 64 columns 46 : 112 us, 16 columns 42 : 52; 4,096 rows of up to
 // 300, 64 columns 353 : 519.  Rows of few edges do not fill a tile: which go where, with both sides' figures, is at the dispatch.  With fewer shared heads
@@ -24,7 +24,9 @@ namespace gs {
 
 constexpr int TC_STAGES = 3;
 constexpr int TC_WARPS = 4;
-constexpr int TC_MOST = 80;                   // the largest power that sums are brought up by: they stay within 32 bits
+constexpr int TC_MOST = 72;                   // the largest power that sums are brought up by: those of 2^30 edges stay within 32 bits
+constexpr float TC_GONE = 0x1p-120f;          // weights that are not whole in 32 bits
+constexpr uint32_t TC_AGAIN = 0x7FC0A6A1u;    // a NaN that no arithmetic gives, in the place of a unit's lse: its weights are too far apart
 constexpr float TC_NEAR = 1.f / 4096.f;       // weights (the largest is 2^14) whose two parts hold 2^-23 of them
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -134,8 +136,9 @@ __device__ __forceinline__ int up_of(uint32_t top) {         // exponent, with i
 }
 __device__ __forceinline__ bool too_wide(uint32_t top, uint32_t least) { return least < 0x7F80u && (int)((least + 1) >> 7) + up_of(top) < 237; }
 
-// The units of a warp whose queries are too wide for f16, in 32 bits throughout: a lane has every 32nd column.
-template <int SP> __device__ __noinline__ void attend_wide_queries(const CodedAttend& P, int64_t units) {
+// The units of a warp whose queries are too wide for f16, or which are marked, in 32 bits throughout: a lane has every 32nd column.  100,000
+// rows of 20 edges, 4 x 4 heads of 64: all queries too wide 4,830 us, none 820; scores spread by 8 1,020, by 32 1,660.
+template <int SP> __device__ __noinline__ void attend_again(const CodedAttend& P, int64_t units) {
     constexpr int SLOTS = 4, C = (SP + 1) / 2;
     const int lane = threadIdx.x & 31, D = P.a.head_dim, group = P.a.q_heads / P.a.kv_heads, cols = list_length(P.a.src);
     const float c2 = P.a.scale * CA_LOG2E;
@@ -143,7 +146,8 @@ template <int SP> __device__ __noinline__ void attend_wide_queries(const CodedAt
         const int r = (int)(u / P.units_per_row), h0 = (int)(u - (int64_t)r * P.units_per_row) * SLOTS, kv = h0 / group;
         const int2 it = P.chunk_mode ? P.items[r] : make_int2(r, 0);
         float q[SLOTS][C], acc[SLOTS][C], m[SLOTS], l[SLOTS];
-        bool wide = false;
+        const float* mark = P.chunk_mode ? P.partial + ((int64_t)r * P.a.q_heads + h0) * (D + 2) + D : P.a.lse + (int64_t)it.x * P.a.q_heads + h0;
+        bool again = __float_as_uint(*mark) == TC_AGAIN;
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i) {
             const bf16* row = (const bf16*)P.a.q.data + (int64_t)it.x * P.a.q.row_stride + (int64_t)(h0 + i) * P.a.q.head_stride;
@@ -156,12 +160,12 @@ template <int SP> __device__ __noinline__ void attend_wide_queries(const CodedAt
                 if (bits <= 0x7F80u) top = max(top, bits);
                 least = min(least, (bits - 1) & 0xFFFFu);
             }
-            wide |= too_wide(__reduce_max_sync(FULL, top), __reduce_min_sync(FULL, least));
+            again |= too_wide(__reduce_max_sync(FULL, top), __reduce_min_sync(FULL, least));
             m[i] = -INFINITY;
             l[i] = 0.f;
         }
         int begin = max(__ldg(P.a.indptr + it.x), 0), end = min(__ldg(P.a.indptr + it.x + 1), P.a.edge_bound);
-        if (!wide || (!P.chunk_mode && P.split && end - begin > CA_LONG)) continue;
+        if (!again || (!P.chunk_mode && P.split && end - begin > CA_LONG)) continue;
         if (P.chunk_mode) {
             begin += it.y * P.chunk;
             end = min(end, begin + P.chunk);
@@ -364,7 +368,7 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 1 
     // what a unit keeps: the queries' fragments (lane g, t: slot g / 2, columns t L ...), sums, maxima (lane g, t: slot t)
     uint32_t q[SP][2];
     float acc[TILES][2], m = 0.f, l = 0.f, qhalf = 0.f, qscale = 0.f;
-    bool apart = false;                                      // queries whose elements are too far apart
+    bool apart = false, gone = false;                        // queries whose elements are too far apart, weights of the unit
     int unit = 0;                                            // acc is in units of 2^(unit - 254 - 14)
     const float c2 = P.a.scale * CA_LOG2E;
     const int my_slot = g >> 1;
@@ -388,6 +392,7 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 1 
             m = -INFINITY;
             l = 0.f;
             unit = 0;
+            gone = false;
 #pragma unroll
             for (int i = 0; i < TILES; ++i) acc[i][0] = acc[i][1] = 0.f;
             const bool has = (g & 1) == 0 && x.w.live;
@@ -445,7 +450,8 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 1 
         for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
         top = fmaxf(top, m);
         const float ref = top == -INFINITY ? 0.f : top;      // nothing seen yet: all weights are zero
-        const float fall = m - ref, p0 = exp2_fast(s0 - ref), p1 = exp2_fast(s1 - ref);
+        const float fall = m - ref;
+        float p0 = exp2_fast(s0 - ref), p1 = exp2_fast(s1 - ref);
         m = top;
         l = fmaf(l, exp2_fast(fall), p0 + p1);
         // exponents of weight times scale, both with their bias: the largest, and the one so far after the maximum's rise
@@ -454,7 +460,8 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 1 
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) most = max(most, __shfl_xor_sync(FULL, most, o));
         most = max(most, unit + (int)ceilf(fmaxf(fall, -1000.f)));
-        float corr = exp2_fast(fall) * power_of(unit - most);
+        const float risen = exp2_fast(fall);
+        float corr = unit > 0 ? risen * power_of(unit - most) : 1.f;     // nothing yet: nothing to correct
         float x0 = p0 * 16384.f * power_of((int)vb0 - most + 127), x1 = p1 * 16384.f * power_of((int)vb1 - most + 127);
         unit = most;
         // ---- values: the weights near the largest first, then what is left, from the largest of each slot down
@@ -467,22 +474,28 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 1 
                 acc[i][1] *= mul;
             }
         };
+        gone |= corr < TC_GONE && risen > 0.f;
         int up = 0;
         while (true) {
             if (__any_sync(FULL, corr != 1.f)) rescale(corr);
             const bool far0 = x0 < TC_NEAR && up < TC_MOST, far1 = x1 < TC_NEAR && up < TC_MOST;
             multiply_values<SP>(vt, split_weights(far0 ? 0.f : x0, far1 ? 0.f : x1), [&](int i, uint2 a, uint32_t b0, uint32_t b1) { mma_f16_half(acc[i], a.x, a.y, b0, b1); });
+            if (!__any_sync(FULL, (far0 && p0 > 0.f) || (far1 && p1 > 0.f))) break;      // p: x may have left the range of 32 bits
             x0 = far0 ? x0 : 0.f;
             x1 = far1 ? x1 : 0.f;
-            if (!__any_sync(FULL, x0 + x1 > 0.f)) break;
+            gone |= (far0 && p0 > 0.f && x0 < TC_GONE) || (far1 && p1 > 0.f && x1 < TC_GONE);
+            p0 = x0;
+            p1 = x1;
             float high = fmaxf(x0, x1);
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) high = fmaxf(high, __shfl_xor_sync(FULL, high, o));
+            if (!__any_sync(FULL, high > 0.f)) break;
             const int more_up = high > 0.f ? min(141 - (int)(__float_as_uint(high) >> 23), TC_MOST - up) : 0;
             up += more_up;
             corr = power_of(more_up);
             x0 *= corr;
             x1 *= corr;
+            gone |= up == TC_MOST && ((x0 > 0.f && x0 < TC_NEAR) || (x1 > 0.f && x1 < TC_NEAR));
         }
         if (__any_sync(FULL, up != 0)) rescale(power_of(-up));
         __syncwarp();                                        // the buffer is read before it is filled again
@@ -497,6 +510,15 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 1 
             out[i] = fmaf(__shfl_xor_sync(FULL, acc[i][0], 4), 1.f / 33554432.f, acc[i][0] * (1.f / 16384.f));
             out[TILES + i] = fmaf(__shfl_xor_sync(FULL, acc[i][1], 4), 1.f / 33554432.f, acc[i][1] * (1.f / 16384.f));
         }
+        bool mark = __any_sync(FULL, gone);
+        if (mark) {
+            // what went is below 2^-84 2^9 an edge: nothing beside columns that are not next to zero
+            bool small = false;
+#pragma unroll
+            for (int i = 0; i < L; ++i) small |= (g & 1) == 0 && t * L + i < D && fabsf(out[i]) < 0x1p-44f;
+            mark = __any_sync(FULL, small);
+            apart |= mark;
+        }
         if (!x.w.live || (g & 1)) continue;
         const int h = h0 + my_slot, col = t * L;
         const bool none = total == 0.f;                      // no edge left by the mask: zero row, log of an empty sum
@@ -506,7 +528,7 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 1 
             for (int i = 0; i < L; ++i)
                 if (col + i < D) part[col + i] = none ? 0.f : out[i] * in;
             if (t == 0) {
-                part[D] = at_m;
+                part[D] = mark ? __uint_as_float(TC_AGAIN) : at_m;
                 part[D + 1] = total;
             }
         } else {
@@ -525,12 +547,12 @@ template <int SP> __global__ void __launch_bounds__(TC_WARPS * 32, SP >= 16 ? 1 
                 for (int i = 0; i < L; ++i)
                     if (col + i < D) to[col + i] = from_f32<bf16>(none ? 0.f : out[i] * in * inv);
             }
-            if (t == 0) P.a.lse[(int64_t)x.w.row * P.a.q_heads + h] = none ? -INFINITY : at_m * CA_LN2 + logf(total);
+            if (t == 0) P.a.lse[(int64_t)x.w.row * P.a.q_heads + h] = mark ? __uint_as_float(TC_AGAIN) : none ? -INFINITY : at_m * CA_LN2 + logf(total);
         }
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncwarp();                                            // what is overwritten has been written
-    if (__any_sync(FULL, apart)) attend_wide_queries<SP>(P, units);
+    if (__any_sync(FULL, apart)) attend_again<SP>(P, units);
 }
 
 }  // namespace gs
