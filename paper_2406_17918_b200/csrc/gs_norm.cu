@@ -12,7 +12,7 @@
 // f32 156 and 157 = 0.93; 100,000 x 513 f32 (rows that begin anywhere) 164 and 231 = 0.76 and 0.54; 4,096 x 1,433 12 and 26: the latency of
 // a row's sums in a block.  Two rows of a block in flight: 15 and 31.
 // dw: a group keeps its columns' sums over NM_SUMMED rows and joins them to those before in 64 bits (2.03 M x 128: 3.8e-7 off without
-// that, 1.2e-7 with it, for 353 -> 364 us); a block with a row to itself keeps them over all of its rows.  Blocks leave theirs in the
+// that, 1.2e-7 with it, for 353 -> 355 us); a block with a row to itself keeps them over all of its rows.  Blocks leave theirs in the
 // workspace, and a second kernel adds them in order, in 64 bits.
 // Results in 8 bits: the largest magnitude of a group of columns is found among the lanes that hold it, by shuffles where the
 // group's pieces are a power of two and by integer maxima in shared memory otherwise.
@@ -390,13 +390,8 @@ __global__ void __launch_bounds__(BLOCK ? 512 : NM_THREADS, BLOCK ? 1 : (VE * NV
         }
         left = true;
     };
-    int rows_added = 0;
-    for (int64_t base = C.blk * per_block * U; base < C.n; base += step) {
-        if constexpr (!BLOCK)
-            if ((rows_added += U) > NM_SUMMED && P.dweight) {
-                leave();
-                rows_added = U;
-            }
+    int64_t base = C.blk * per_block * U;
+    auto rows = [&]() {
         RowPart<T, VE, NV, EDGE> hc[U], dyc[U], dhc[U];
         float sum[2 * U];                                    // sum h^2, sum g h
 #pragma unroll
@@ -448,6 +443,14 @@ __global__ void __launch_bounds__(BLOCK ? 512 : NM_THREADS, BLOCK ? 1 : (VE * NV
             }
             hc[u].store((T*)P.out + row * P.out_ld, t, width, C.phase, D);
         }
+    };
+    if constexpr (BLOCK) {
+        for (; base < C.n; base += step) rows();
+    } else {
+        while (base < C.n) {
+            for (int i = 0; i < NM_SUMMED / U && base < C.n; ++i, base += step) rows();
+            if (base < C.n && P.dweight) leave();
+        }
     }
     if (!P.dweight) return;
     leave();
@@ -461,26 +464,37 @@ __global__ void __launch_bounds__(BLOCK ? 512 : NM_THREADS, BLOCK ? 1 : (VE * NV
     }
 }
 
-// dw = the blocks' sums, added in order: 32 columns per block, its warps over contiguous shares of the blocks.
+// dw = the blocks' sums, added in order: 32 columns per block, its warps over contiguous shares of the blocks, U on their way together, then
+// a column to a warp.
 __global__ void __launch_bounds__(1024) k_norm_dweight(const float* __restrict__ part, int parts, int dim, void* dweight, gs_dtype dtype) {
+    constexpr int U = 16;
     __shared__ double s[32][33];
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = (parts + 31) / 32;
     for (int c0 = blockIdx.x * 32; c0 < dim; c0 += gridDim.x * 32) {
         const int c = c0 + lane, p1 = (warp + 1) * per < parts ? (warp + 1) * per : parts;
-        double x = 0.0;
-        if (c < dim) {
-#pragma unroll 8
-            for (int p = warp * per; p < p1; ++p) x += __ldcg(part + (int64_t)p * dim + c);
+        double sum = 0.0;
+        for (int p = warp * per; p < p1; p += U) {
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = c < dim && p + u < p1 ? __ldcg(part + (int64_t)(p + u) * dim + c) : 0.f;
+            double y[U / 2];
+#pragma unroll
+            for (int u = 0; u < U / 2; ++u) y[u] = (double)x[2 * u] + (double)x[2 * u + 1];
+#pragma unroll
+            for (int n = U / 4; n; n /= 2)
+#pragma unroll
+                for (int u = 0; u < n; ++u) y[u] += y[u + n];
+            sum += y[0];
         }
         __syncthreads();
-        s[warp][lane] = x;
+        s[warp][lane] = sum;
         __syncthreads();
-        if (warp == 0 && c < dim) {
-            x = 0.0;
-            for (int i = 0; i < 32; ++i) x += s[i][lane];
-            if (dtype == GS_BF16) static_cast<bf16*>(dweight)[c] = __float2bfloat16_rn((float)x);
-            else static_cast<float*>(dweight)[c] = (float)x;
+        sum = s[lane][warp];
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(FULL, sum, o);
+        if (lane == 0 && c0 + warp < dim) {
+            if (dtype == GS_BF16) static_cast<bf16*>(dweight)[c0 + warp] = __float2bfloat16_rn((float)sum);
+            else static_cast<float*>(dweight)[c0 + warp] = (float)sum;
         }
     }
 }
