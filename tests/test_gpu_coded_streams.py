@@ -62,3 +62,25 @@ def test_dropped_while_a_write_is_queued(part, current):
     torch.cuda.synchronize()
     assert all((t == 5).all() for t in later)
     assert torch.equal(codes, want.codes) and torch.equal(scales, want.scales)
+
+
+def test_captured_on_another_stream():
+    """A write that a graph holds, on a stream that the store was not made on; the store goes when the graph has gone."""
+    codes, scales = _tensors(16)
+    x, ids = _rows()
+    want = gs.gs_coded_write(gs.CodedRows(codes.clone(), scales.clone(), 16, 16), x, ids=ids)
+    store = gs.CodedRows(codes, scales, 16, 16)
+    words = store.claims.numel()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        gs.gs_coded_write(store, x, ids=ids)
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(codes, want.codes) and torch.equal(scales, want.scales) and (store.claims == -1).all()
+    del graph, store
+    later = torch.full((words,), 5, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    assert (later == 5).all()
