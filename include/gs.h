@@ -557,10 +557,10 @@ gs_status gs_xent_backward(const void* d_hidden, int64_t hidden_ld, const void* 
 
 /* Root-mean-square norm of rows [rows][dim], 1 <= dim <= 8192, with the addition of a residual before it:
  *   h = x + residual, rounded to `dtype` (h = x without a residual);  out = weight h / sqrt(mean(h^2) + eps)
- * d_weight_or_null [dim] of weight_dtype (NULL: ones); eps >= 0.  d_hidden_or_null receives h, which the backward pass takes.  Each of
+ * d_weight_or_null [dim] of weight_dtype (NULL: ones); eps >= 0.  Squares are added in 32 bits: |h| of 1e19 / sqrt(dim) and more gives
+ * rows of zeros, and with eps = 0 |h| below 1e-19 no digits.  d_hidden_or_null receives h, which the backward pass takes.  Each of
  * d_hidden_or_null and d_out may be the array of x or of the residual, at the same pitch, but not both the same one; other overlaps
- * are errors.  d_count_or_null: as for gs_gather_features;
- * rows behind the count are left as they are.
+ * are errors.  d_count_or_null: as for gs_gather_features; rows behind the count are left as they are.
  * gs_rms_norm_coded writes the result in 8 bits instead (gs_coded below): row p to row p of `out`, which has scales of its own for
  * every row (block 1) and heads * head_dim == dim: a scale per group of head_dim columns.
  * gs_rms_norm_backward takes h, the gradient dout of out and, if h is used elsewhere, the gradient dhidden that arrives there:
@@ -603,7 +603,8 @@ gs_status gs_coded_read(const gs_coded* from, const int32_t* d_ids_or_null, int6
                         int32_t count_bound, gs_dtype dtype, const gs_heads* out, void* stream);
 
 /* gs_block_attention_forward with keys and values held in 8 bits: source j's are row d_rows[j] of k and v, or row j if d_rows is
- * NULL (max_src is then at most k->rows).  An edge whose source or row does not exist is masked.  k and v have one number of rows,
+ * NULL (max_src is then at most k->rows).  An edge whose source or row does not exist is masked.  Scores are added
+ * up as q times codes in 32 bits, |q| < 2^110, and outputs as weights (the largest 1) times values.  k and v have one number of rows,
  * heads and block size and may be parts of one store; q and out are of `dtype`.
  * Workspace: gs_coded_attention_workspace_bytes. */
 gs_status gs_coded_attention_workspace_bytes(int32_t max_edges, int32_t q_heads, int32_t head_dim, size_t* bytes);

@@ -9,11 +9,14 @@
 // scale; they are held relative to a power of two near the largest weight times scale so far, as 2^14.  f16 ends 2^-38 below that, and
 // yet such weights are the result where the heavier edges' values are zero: a tile that has weights below 2^-26 multiplies those
 // again by themselves, they and the sums brought up together, down to 2^-98 of the largest.  It takes a score 18 below a row's largest.  A unit
-// with lighter weights still (a score 68 below; 32 bits end at 87) is done again at the warp's end, edge by edge in 32 bits.
-// What bounds it is instructions around the products (ALU 57%, issue slots 64%), not their rate, so the legacy matrix instruction
-// serves.  This : the other kernel (2 x 4 heads): one row of 200,011 edges, 64 columns 46 : 112 us, 16 columns 42 : 52; 4,096 rows of up to
-// 300, 64 columns 353 : 519.  Rows of few edges do not fill a tile: which go where, with both sides' figures, is at the dispatch.  With fewer shared heads
-// the other kernel needs fewer instructions (2 of 32 columns, 20 edges 314 : 258; 1 of 32, 20 edges 527 : 284; one row of 200,011 edges 44 : 43).
+// with lighter weights still (a score 68 below; 32 bits end at 87) and a column next to zero is done again at the warp's end, edge by edge
+// in 32 bits.
+// What bounds it is instructions around the products (64 columns: ALU 54 %, issue slots 62 %; 513 a row and 427 a tile), not their rate, so
+// the legacy matrix instruction serves.  Above 128 columns one block of four warps fits an SM, and latency bounds it (issue slots 23 %).
+// Spills, bytes loaded: 88 for 65 to 128 columns, 108 above, none below.  This : the other kernel (2 x 4 heads): one row of 200,011 edges,
+// 64 columns 47 : 112 us, 16 columns 42 : 52; 4,096 rows of up to 300, 64 columns 353 : 519.  Rows of few edges do not fill a tile: which go
+// where, with both sides' figures, is at the dispatch.  With fewer shared heads the other kernel needs fewer instructions (2 of 32 columns, 20
+// edges 314 : 258; 1 of 32, 20 edges 527 : 284; one row of 200,011 edges 44 : 43).
 //
 // Rows are gathered by cp.async into TC_STAGES buffers of 16 edges a warp, TC_STAGES - 1 tiles ahead; the columns of 32 edges are read
 // one unit (a row's first) and the offsets two units ahead of the gathers.  No block barriers.  16-byte pieces are permuted within

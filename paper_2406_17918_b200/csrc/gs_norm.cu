@@ -8,9 +8,12 @@
 // pieces) or by a block, in pieces of 16 bytes.  Rows of odd widths begin anywhere within a piece: a block then takes the rows that
 // begin at one place of it (every 4th f32 row of 1,433, say), so that its threads keep their columns, and only the pieces at a
 // row's ends go one element at a time.  Arrays whose rows do not begin alike go one element at a time altogether.
-// Measured (reads and writes of both sides, of a copy's 6.56 TB/s): 2.03 M x 64 bf16 forward 159 us = 0.99, backward 177 = 0.90; 30,000 x 2,000
-// f32 156 and 157 = 0.93; 100,000 x 513 f32 (rows that begin anywhere) 164 and 231 = 0.76 and 0.54; 4,096 x 1,433 12 and 26: the latency of
-// a row's sums in a block.  Two rows of a block in flight: 15 and 31.
+// Measured with a residual (reads and writes of both sides, of a copy's 6.56 TB/s): 2.03 M x 64 bf16 forward 164 us = 0.97, backward 184 = 0.86;
+// 30,000 x 2,000 f32 161 and 161 = 0.91; 100,000 x 513 f32 (rows that begin anywhere) 170 and 239 = 0.74 and 0.52; 4,096 x 1,433 13 and 23 cold: the
+// latency of a row's sums in a block (two rows of a block in flight: 15 and 31).  300,000 x 33 bf16 76 and 115 = 0.16 and 0.10: a
+// row is five pieces on eight lanes, and one or two of them are ends, eight elements one at a time: issue slots 81 % and 66 %.
+// Forms of the backward pass that spill (bytes loaded): f32 rows of more than 4,096 columns 108 to 152, odd widths of up to 512 columns 32 to
+// 80, one element at a time 56 to 192; the others 0 to 40.
 // dw: a group keeps its columns' sums over NM_SUMMED rows and joins them to those before in 64 bits (2.03 M x 128: 3.8e-7 off without
 // that, 1.2e-7 with it, for 353 -> 355 us); a block with a row to itself keeps them over all of its rows.  Blocks leave theirs in the
 // workspace, and a second kernel adds them in order, in 64 bits.
