@@ -10,8 +10,8 @@
 // at its end; rows of more than LONG edges are cut into chunks of a warp each, whose results are joined in order by a second
 // kernel: no atomics on values, the result does not depend on the schedule.
 // What bounds it is instructions (issue slots 67 %, 41 % of the DRAM rate): 677 per warp and batch of 4 edges x 16 columns, 256 of them the
-// codes' conversion and the products.  262,144 rows, 4.36 M edges, 4 x 32 bf16: 281 to 299 us from box to box (1.1 GB gathered, 3.8 TB/s),
-// f32 8 more.  Timed on one box against 285: 2 or 3 edges a batch 370, 5 292, 8 328; 8 columns a lane 467, 32 404 (fewer warps).  Spills, bytes
+// codes' conversion and the products.  262,144 rows, 4.36 M edges, 4 x 32 bf16: 281 to 299 us from device to device (1.1 GB gathered, 3.8 TB/s),
+// f32 8 more.  Timed on one device against 285: 2 or 3 edges a batch 370, 5 292, 8 328; 8 columns a lane 467, 32 404 (fewer warps).  Spills, bytes
 // loaded: heads by fours 46 to 58 at 168 registers, the join 144 at 64.
 #include "gs_codes.cuh"
 #include "gs_device.cuh"

@@ -4,7 +4,7 @@
 //
 // Two passes over the bytes, because no element may be scaled before the last has been counted; what L2 still holds of the first
 // pass is met first by the second, which walks the tiles backwards: the first pass asks L2 to keep only its last GN_KEPT bytes, the
-// second's results are not kept (on one box 174 MB of f32: 85 -> 81 us, 708 MB 322 -> 308; 40 MB instead of 80: 84 and 313, all of them: 83
+// second's results are not kept (on one device 174 MB of f32: 85 -> 81 us, 708 MB 322 -> 308; 40 MB instead of 80: 84 and 313, all of them: 83
 // and 318).  Of the 522 MB that two passes over 174 ask for DRAM moves 447: 0.85 to 0.87 of a plain copy's rate in 78 to 80 us.  The tensors'
 // addresses travel as a kernel argument: nothing is copied to the device, and a captured call can be replayed.  Squares are added eight or four at a time in 32 bits, then in 64, each
 // block its tiles in order and the blocks' sums in order: the result does not depend on the schedule.  Squares that leave the range
